@@ -491,6 +491,159 @@ kvr_status kvr_cache_set_absorb_kernel(kvr_cache *cache, int kernel);
  * no synchronisation. */
 int kvr_cache_last_absorb_kernel(const kvr_cache *cache);
 
+/* ---- the full context held in 4 bits ------------------------------------ */
+
+/* The paper has no counterpart to these calls.  A full-context cache (the
+ * helper's, Sec. 3.1; App. D, Eq. 11) is read whole by every token, so its
+ * bytes are its cost.  This one holds each key and value in 4 bits: the 64
+ * channels of a group (one token, one KV head, channels 64j .. 64j + 63) share
+ * a minimum m and a scale s, both bfloat16, and channel x holds a code c:
+ *   lo, hi = least and greatest value of the group
+ *   m = bf16(lo),  s = bf16(hi * (1/15) - lo * (1/15))
+ *   c = (x - m) / s, rounded to the nearest even whole number, within 0..15
+ *       (0 where s is 0)
+ * in fp32, every operation rounded to nearest.  The row stands for m + s * c
+ * (formed in fp32).  A group that holds a NaN or an infinity stands for NaN
+ * throughout (m = NaN, s = 0, c = 0).  A row takes d + d/8 bytes for key and
+ * value together, against 4 d in bf16.
+ *
+ * A row's index is its position; nothing is evicted in place.  Rows are
+ * appended, dropped from the end (drafted tokens that were rejected), read by
+ * attention, and cut by accumulated attention weight into the evicted cache
+ * that a drafter decodes from.  A descriptor's kv_dtype is the element type of
+ * q, k and v; the cache itself is always 4-bit.  Tensors are dense, row-major
+ * and 16-byte aligned (KVR_EINVAL otherwise).  counts (host [n_seq] or NULL):
+ * how many of a call's tokens sequence s has, 0 .. the call's tokens; NULL
+ * means all of them.  Its tokens are the first counts[s] of its row.  The
+ * lengths live in the handle alone, so a call over several layers needs the
+ * same length in each of them, sequence by sequence (KVR_ESTATE otherwise).
+ * Calls on one handle must be ordered on one stream. */
+typedef struct kvr_kv4 kvr_kv4; /* opaque; host metadata only */
+
+/* Device bytes the cache needs (0 for an invalid descriptor; those of
+ * kvr_cache_required_bytes are valid). */
+size_t kvr_kv4_required_bytes(const kvr_cache_desc *desc);
+
+/* Create an empty cache over dev_buf (caller-owned, 256-byte aligned, >= the
+ * required bytes).  The scores are cleared on stream. */
+kvr_status kvr_kv4_create(const kvr_cache_desc *desc, void *dev_buf,
+                          size_t bytes, void *stream, kvr_kv4 **out);
+
+/* Free the handle's host metadata (not the buffer). NULL is a no-op. */
+void kvr_kv4_destroy(kvr_kv4 *cache);
+
+/* Replace sequence seq with n_rows rows in every layer and KV head:
+ * k, v dev [L][H][n_rows][d].  Scores start at 0.  KVR_ECAPACITY when they do
+ * not fit. */
+kvr_status kvr_kv4_load(kvr_kv4 *cache, int seq, const void *k, const void *v,
+                        int n_rows, void *stream);
+
+/* Append tokens to layers [layer_begin, layer_end) of every sequence:
+ *   k, v dev [S][nl][n_new][H][d]
+ * with score 0.  KVR_ECAPACITY, with nothing enqueued, when a sequence has no
+ * room. */
+kvr_status kvr_kv4_append(kvr_kv4 *cache, int layer_begin, int layer_end,
+                          int n_new, const int32_t *counts, const void *k,
+                          const void *v, void *stream);
+
+/* Sequence s keeps its first lens[s] rows in every layer (host [S], each at
+ * most the sequence's length; KVR_EINVAL otherwise, with nothing changed).
+ * Host state only: nothing is enqueued. */
+kvr_status kvr_kv4_truncate(kvr_kv4 *cache, const int32_t *lens);
+
+/* Host copy of the lengths, [S][L].  No synchronisation. */
+kvr_status kvr_kv4_lengths(const kvr_kv4 *cache, int32_t *host_len);
+
+/* What the newest rows stand for, in kv_dtype (rounded once from fp32):
+ *   k, v dev [S][nl][H][n_rows][d]
+ * Sequence s's newest counts[s] rows, oldest first, then zeros.  KVR_EINVAL
+ * where a sequence holds fewer. */
+kvr_status kvr_kv4_read(kvr_kv4 *cache, int layer_begin, int layer_end,
+                        int n_rows, const int32_t *counts, void *k, void *v,
+                        void *stream);
+
+/* Attention (Eq. 1) of each sequence's newest tokens, appended before:
+ *   q, out dev [S][nl][n_q][H*G][d] (out_dtype for out)
+ * Token j < counts[s] sits at position length - counts[s] + j and sees the
+ * rows up to its own; one that sees none, and the tokens from counts[s] on,
+ * get zeros.  Softmax statistics and sums are fp32.  With add_scores != 0 each
+ * row's score grows by the sum over the tokens that see it of the mean over
+ * the G heads of its probability (accumulated attention, Sec. 2.1).
+ * workspace: device, 16-byte aligned, caller-owned, at least
+ * kvr_kv4_attend_workspace_bytes(...) bytes (KVR_ENOMEM otherwise), which
+ * depends on the descriptor and the arguments alone; nothing in it is kept
+ * between calls.  A normaliser that is not finite sets the device error
+ * word. */
+size_t kvr_kv4_attend_workspace_bytes(const kvr_kv4 *cache, int layer_begin,
+                                      int layer_end, int n_q);
+kvr_status kvr_kv4_attend(kvr_kv4 *cache, int layer_begin, int layer_end,
+                          int n_q, const int32_t *counts, const void *q,
+                          void *out, int add_scores, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* Cut every sequence into dst, an evicted cache of the same sequences, layers,
+ * KV heads and head_dim (Eq. 1's TopB over accumulated attention): each unit
+ * of dst becomes the window most recent rows and the budget others of the
+ * highest score (ties to the lower position), or all of them where there are
+ * no more, in ascending order of position, with the values they stand for (in
+ * dst's kv_dtype), their scores and positions; decoding goes on with
+ * kvr_decode_step.  This cache is not changed.  A NaN score ranks above every
+ * number.  KVR_ECAPACITY when dst is too small, KVR_ESTATE while dst has a
+ * live fork or the layers' lengths differ. */
+kvr_status kvr_kv4_evict(kvr_kv4 *cache, kvr_cache *dst, int budget,
+                         int window, void *stream);
+
+/* Device pointer to the scores, [S][L][H][row_stride] fp32, inside the
+ * caller's buffer; a caller may also write them, stream-ordered. */
+kvr_status kvr_kv4_scores(const kvr_kv4 *cache, float **score,
+                          int64_t *row_stride);
+
+/* Number of kernels this handle has launched. */
+kvr_status kvr_kv4_launch_count(const kvr_kv4 *cache, uint64_t *count);
+
+/* Synchronising: wait for stream, read and clear the device error word. */
+kvr_status kvr_kv4_sync_status(kvr_kv4 *cache, void *stream);
+
+/* ---- verification of drafted tokens -------------------------------------- */
+
+/* The paper has no counterpart to this call either: a step that a cheap model
+ * drafted is checked against the model it stands in for, token by token, so
+ * that what is emitted is distributed as the target's own samples.  With
+ * p_t and q_t the softmax of the target's and the draft's logits over
+ * temperature, and given uniform numbers u_t in [0, 1), draft x_t is accepted
+ * while u_t * q_t(x_t) < p_t(x_t).  After a = the first that is not, the next
+ * token is drawn from the positive part of p_a - q_a (from p_a where that is
+ * empty), and after the last one from the target's next row.  The draw is a
+ * race: the token with the greatest weight / race, ties to the lowest, with
+ * one given exponential number (> 0) a vocabulary entry.
+ *   target dev [S][n_draft + 1] rows of target_stride elements, the first
+ *          vocab of each read; draft dev [S][n_draft] rows of draft_stride
+ *   tokens dev [S][n_draft] int32, u dev [S][n_draft] fp32,
+ *   race   dev [S][vocab] fp32
+ *   counts dev [S] int32 or NULL: sequence s has min(counts[s], n_draft)
+ *          drafts
+ *   accepted dev [S] int32: a; out_tokens dev [S][n_draft + 1] int32: the a
+ *          accepted tokens, the next one, then -1
+ * Logits of -inf have probability 0.  A row that has no softmax (a NaN, +inf,
+ * or only -inf) and a drafted token outside [0, vocab) end the sequence there,
+ * with -1 for the next token.  Statistics are fp32.  workspace as above. */
+typedef struct {
+  int n_seq;      /* S, 1..65535 */
+  int n_draft;    /* 0..64 */
+  int vocab;      /* >= 1 */
+  float temperature; /* > 0; 0 means 1 */
+  kvr_dtype logits_dtype;
+} kvr_verify_desc;
+
+size_t kvr_verify_workspace_bytes(const kvr_verify_desc *desc);
+kvr_status kvr_verify_drafts(const kvr_verify_desc *desc, const void *target,
+                             int64_t target_stride, const void *draft,
+                             int64_t draft_stride, const int32_t *tokens,
+                             const float *u, const float *race,
+                             const int32_t *counts, int32_t *accepted,
+                             int32_t *out_tokens, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
 /* ---- the same step for callers that cannot allocate -------------------- */
 
 /* The paper has no counterpart to this call: it is a deployment variant.
@@ -566,6 +719,11 @@ kvr_status kvr_cache_export(const kvr_cache *cache, int seq, void *host_k,
 kvr_status kvr_cache_scores(const kvr_cache *cache, float **score,
                             int32_t **pos, int32_t **state,
                             int64_t *row_stride);
+
+/* The rows themselves, with no copy: device pointers into the caller's cache
+ * buffer, k and v [S][L][H][capacity][d] of kv_dtype.  As kvr_cache_scores:
+ * slots [0, live length) of a unit hold its rows. */
+kvr_status kvr_cache_rows(const kvr_cache *cache, void **k, void **v);
 
 /* Host mirror of the live length of every (sequence, layer): host_len
  * [S][L].  Not synchronising (the mirror is exact after every call). */

@@ -921,6 +921,15 @@ int kvr::report_error(int st, const char *msg) {
   return fail(static_cast<kvr_status>(st), "%s", msg);
 }
 
+const CacheView &kvr::cache_view(const kvr_cache *c) { return c->view; }
+bool kvr::cache_forked(const kvr_cache *c) { return c->forks != 0; }
+void kvr::cache_set_length(kvr_cache *c, int seq, int32_t len, int32_t next_pos) {
+  const size_t at = (size_t)seq * c->desc.n_layers;
+  std::fill_n(c->len.begin() + at, c->desc.n_layers, len);
+  std::fill_n(c->next_pos.begin() + at, c->desc.n_layers, next_pos);
+}
+void kvr::cache_count_launch(kvr_cache *c) { c->launches += 1; }
+
 int kvr::decode_attend_score_ext(kvr_cache *c, int lb, int le, const void *q,
                                  const void *k_new, const void *v_new,
                                  void *out, float *ext, size_t ext_floats,
@@ -1319,6 +1328,13 @@ kvr_status kvr_cache_scores(const kvr_cache *c, float **score,
   if (pos) *pos = c->view.pos;
   if (state) *state = c->view.state;
   if (row_stride) *row_stride = c->view.sstride;
+  return KVR_OK;
+}
+
+kvr_status kvr_cache_rows(const kvr_cache *c, void **k, void **v) {
+  if (!c) return fail(KVR_EINVAL, "null cache");
+  if (k) *k = c->view.K;
+  if (v) *v = c->view.V;
   return KVR_OK;
 }
 

@@ -396,6 +396,12 @@ namespace kvr {
 int decode_attend_score_ext(kvr_cache *c, int lb, int le, const void *q,
                             const void *k_new, const void *v_new, void *out,
                             float *ext, size_t ext_floats, void *stream);
+// What an eviction from another kind of cache needs of the one it fills: its
+// view, whether a fork is alive; afterwards the lengths (host mirror).
+const CacheView &cache_view(const kvr_cache *c);
+bool cache_forked(const kvr_cache *c);
+void cache_set_length(kvr_cache *c, int seq, int32_t len, int32_t next_pos);
+void cache_count_launch(kvr_cache *c);
 // Record a CUDA failure as the thread's last error; returns KVR_ECUDA.
 int report_cuda_error(const char *where, cudaError_t e);
 // Record msg as the thread's last error; returns st.

@@ -84,6 +84,7 @@ _SIGS = {
     "kvr_cache_last_absorb_kernel": (_I, [_P]),
     "kvr_cache_last_chunk_groups": (_I, [_P, _P]),
     "kvr_cache_scores": (_S, [_P, _P, _P, _P, _P]),
+    "kvr_cache_rows": (_S, [_P, _P, _P]),
     "kvr_sync_status": (_S, [_P, _P]),
     "kvr_last_error": (ctypes.c_char_p, []),
 }
@@ -447,6 +448,19 @@ class Cache:
                 view(stp, self.S * self.L * self.H * 4, torch.int32).view(
                     self.S, self.L, self.H, 4))
 
+    def rows_view(self):
+        """(K, V) as device tensors viewing the cache buffer (no copy), each
+        [S][L][H][capacity][d] (kvr_cache_rows)."""
+        kp, vp = _P(), _P()
+        _check(lib.kvr_cache_rows(self.handle, ctypes.byref(kp),
+                                  ctypes.byref(vp)), "kvr_cache_rows")
+        shape = (self.S, self.L, self.H, self.cap, self.d)
+        es = 2 if self.kv_dtype == "bf16" else 4
+        n = int(np.prod(shape)) * es
+        base = self.buf.data_ptr()
+        return tuple(self.buf[p.value - base:p.value - base + n]
+                     .view(self.kv_torch_dtype).view(shape) for p in (kp, vp))
+
     def set_absorb_kernel(self, kernel: int):
         """kvr_absorb_chunk's one-launch kernel: 0 tcgen05, 1 mma.sync."""
         _check(lib.kvr_cache_set_absorb_kernel(self.handle, kernel),
@@ -794,3 +808,280 @@ class EntropyDetector:
 
     def sync_status(self, stream=None):
         kvr_entropy_sync_status(self.handle, stream)
+
+
+# ---- the full context held in 4 bits ----------------------------------------
+
+for _name, (_res, _args) in {
+    "kvr_kv4_required_bytes": (ctypes.c_size_t,
+                               [ctypes.POINTER(kvr_cache_desc)]),
+    "kvr_kv4_create": (_S, [ctypes.POINTER(kvr_cache_desc), _P,
+                            ctypes.c_size_t, _P, ctypes.POINTER(_P)]),
+    "kvr_kv4_destroy": (None, [_P]),
+    "kvr_kv4_load": (_S, [_P, _I, _P, _P, _I, _P]),
+    "kvr_kv4_append": (_S, [_P, _I, _I, _I, _P, _P, _P, _P]),
+    "kvr_kv4_truncate": (_S, [_P, _P]),
+    "kvr_kv4_lengths": (_S, [_P, _P]),
+    "kvr_kv4_read": (_S, [_P, _I, _I, _I, _P, _P, _P, _P]),
+    "kvr_kv4_attend_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I, _I]),
+    "kvr_kv4_attend": (_S, [_P, _I, _I, _I, _P, _P, _P, _I, _P,
+                            ctypes.c_size_t, _P]),
+    "kvr_kv4_evict": (_S, [_P, _P, _I, _I, _P]),
+    "kvr_kv4_scores": (_S, [_P, _P, _P]),
+    "kvr_kv4_launch_count": (_S, [_P, _P]),
+    "kvr_kv4_sync_status": (_S, [_P, _P]),
+}.items():
+    _f = getattr(lib, _name)
+    _f.restype = _res
+    _f.argtypes = _args
+
+
+def _host_ints(x, n, what):
+    """A host int32 array of n values for the library, or None."""
+    if x is None:
+        return None
+    a = np.ascontiguousarray(x, dtype=np.int32)
+    if a.shape != (n,):
+        raise ValueError(f"{what} must be {n} whole numbers")
+    return a
+
+
+def _scratch(nbytes, device, stream):
+    """Device scratch for one call on `stream`: the allocator is told where a
+    stream other than the current one uses it."""
+    t = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    if stream is not None:
+        s = stream if isinstance(stream, torch.cuda.Stream) else \
+            torch.cuda.ExternalStream(int(stream)) if int(stream) else \
+            torch.cuda.default_stream()
+        t.record_stream(s)
+    return t
+
+
+class Kv4Cache:
+    """A full-context cache held in 4 bits (kvr_kv4_*; the format stands in
+    include/kvr.h): owner of the handle and of the torch buffer it lives in."""
+
+    def __init__(self, n_seq, n_layers, n_kv_heads, group, head_dim, capacity,
+                 dtype="bf16", out_dtype="bf16", softmax_scale=0.0,
+                 device="cuda", stream=None, buf=None):
+        """dtype: element type of q, k and v.  buf: an optional caller-owned
+        uint8 device tensor of at least kvr_kv4_required_bytes (256-byte
+        aligned); by default one is allocated."""
+        self.desc = make_desc(n_seq, n_layers, n_kv_heads, group, head_dim,
+                              capacity, dtype, out_dtype, softmax_scale)
+        self.S, self.L, self.H, self.G, self.d = (n_seq, n_layers, n_kv_heads,
+                                                  group, head_dim)
+        self.cap = capacity
+        self.dtype, self.out_dtype = dtype, out_dtype
+        self.nbytes = int(lib.kvr_kv4_required_bytes(ctypes.byref(self.desc)))
+        if self.nbytes == 0:
+            raise KvrError(KVR_EINVAL, "Kv4Cache", "invalid descriptor")
+        if buf is None:
+            buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        elif buf.numel() < self.nbytes or buf.dtype != torch.uint8:
+            raise ValueError("buf must be uint8 with at least "
+                             f"{self.nbytes} bytes")
+        self.buf = buf
+        h = _P()
+        _check(lib.kvr_kv4_create(ctypes.byref(self.desc), _ptr(buf),
+                                  self.nbytes, _stream(stream),
+                                  ctypes.byref(h)), "kvr_kv4_create")
+        self.handle = h
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h:
+            lib.kvr_kv4_destroy(h)
+            self.handle = None
+
+    def _layers(self, layers):
+        return (0, self.L) if layers is None else layers
+
+    def _check_rows(self, x, lead, what):
+        """x is a tensor of the cache's element type, [*lead][d]."""
+        want = (*lead, self.d)
+        if tuple(x.shape) != want or x.dtype != TORCH_DTYPES[self.dtype]:
+            raise ValueError(f"{what} must be {self.dtype} {list(want)}, not "
+                             f"{x.dtype} {list(x.shape)}")
+
+    def load(self, seq, k, v, stream=None):
+        """Replace a sequence: k, v [L][H][n][d] (kvr_kv4_load)."""
+        n = k.shape[2]
+        for x, name in ((k, "k"), (v, "v")):
+            self._check_rows(x, (self.L, self.H, n), name)
+        _check(lib.kvr_kv4_load(self.handle, seq, _ptr(k), _ptr(v), n,
+                                _stream(stream)), "kvr_kv4_load")
+
+    def append(self, k, v, counts=None, layers=None, stream=None):
+        """Append tokens: k, v [S][nl][n][H][d]; counts: how many of them each
+        sequence has (kvr_kv4_append)."""
+        lb, le = self._layers(layers)
+        n = k.shape[2]
+        for x, name in ((k, "k"), (v, "v")):
+            self._check_rows(x, (self.S, le - lb, n, self.H), name)
+        counts = _host_ints(counts, self.S, "counts")
+        _check(lib.kvr_kv4_append(self.handle, lb, le, n, _ptr(counts),
+                                  _ptr(k), _ptr(v), _stream(stream)),
+               "kvr_kv4_append")
+
+    def truncate(self, lens):
+        """Each sequence keeps its first lens[s] rows (kvr_kv4_truncate)."""
+        _check(lib.kvr_kv4_truncate(self.handle, _ptr(_host_ints(
+            lens, self.S, "lens"))), "kvr_kv4_truncate")
+
+    def lengths(self):
+        a = np.zeros((self.S, self.L), np.int32)
+        _check(lib.kvr_kv4_lengths(self.handle, _ptr(a)), "kvr_kv4_lengths")
+        return a
+
+    def read_newest(self, n, counts=None, layers=None, stream=None):
+        """What the newest n rows stand for: (k, v) [S][nl][H][n][d]
+        (kvr_kv4_read)."""
+        lb, le = self._layers(layers)
+        counts = _host_ints(counts, self.S, "counts")
+        k, v = (torch.empty((self.S, le - lb, self.H, n, self.d),
+                            dtype=TORCH_DTYPES[self.dtype],
+                            device=self.buf.device) for _ in range(2))
+        _check(lib.kvr_kv4_read(self.handle, lb, le, n, _ptr(counts), _ptr(k),
+                                _ptr(v), _stream(stream)), "kvr_kv4_read")
+        return k, v
+
+    def attend_workspace(self, n_q, layers=None):
+        """A workspace for attend() of up to n_q tokens over these layers."""
+        lb, le = self._layers(layers)
+        return torch.empty(int(lib.kvr_kv4_attend_workspace_bytes(
+            self.handle, lb, le, n_q)), dtype=torch.uint8,
+            device=self.buf.device)
+
+    def attend(self, q, out=None, counts=None, layers=None, scores=False,
+               workspace=None, stream=None):
+        """Attention of the newest tokens: q [S][nl][n][H*G][d] -> out, the
+        same shape in out_dtype; scores: add each row's accumulated attention
+        weight (kvr_kv4_attend)."""
+        lb, le = self._layers(layers)
+        n = q.shape[2]
+        self._check_rows(q, (self.S, le - lb, n, self.H * self.G), "q")
+        counts = _host_ints(counts, self.S, "counts")
+        if out is None:
+            out = torch.empty(q.shape, dtype=TORCH_DTYPES[self.out_dtype],
+                              device=q.device)
+        elif out.shape != q.shape or \
+                out.dtype != TORCH_DTYPES[self.out_dtype]:
+            raise ValueError(f"out must be {self.out_dtype} {list(q.shape)}")
+        if workspace is None:
+            workspace = _scratch(int(lib.kvr_kv4_attend_workspace_bytes(
+                self.handle, lb, le, n)), q.device, stream)
+        _check(lib.kvr_kv4_attend(self.handle, lb, le, n, _ptr(counts),
+                                  _ptr(q), _ptr(out), 1 if scores else 0,
+                                  _ptr(workspace), workspace.numel(),
+                                  _stream(stream)), "kvr_kv4_attend")
+        return out
+
+    def evict_into(self, cache: Cache, budget, window, stream=None):
+        """Cut every sequence into an evicted cache (kvr_kv4_evict)."""
+        _check(lib.kvr_kv4_evict(self.handle, cache.handle, budget, window,
+                                 _stream(stream)), "kvr_kv4_evict")
+
+    def scores_view(self):
+        """The scores as a device tensor viewing the buffer,
+        [S][L][H][capacity]; it may be written."""
+        p, stride = _P(), ctypes.c_int64()
+        _check(lib.kvr_kv4_scores(self.handle, ctypes.byref(p),
+                                  ctypes.byref(stride)), "kvr_kv4_scores")
+        off = p.value - self.buf.data_ptr()
+        n = self.S * self.L * self.H * stride.value
+        return self.buf[off:off + 4 * n].view(torch.float32).view(
+            self.S, self.L, self.H, stride.value)[..., :self.cap]
+
+    def launch_count(self):
+        n = ctypes.c_uint64()
+        _check(lib.kvr_kv4_launch_count(self.handle, ctypes.byref(n)),
+               "kvr_kv4_launch_count")
+        return int(n.value)
+
+    def sync_status(self, stream=None):
+        _check(lib.kvr_kv4_sync_status(self.handle, _stream(stream)),
+               "kvr_kv4_sync_status")
+
+
+# ---- verification of drafted tokens -----------------------------------------
+
+class kvr_verify_desc(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int), ("n_draft", ctypes.c_int),
+                ("vocab", ctypes.c_int), ("temperature", ctypes.c_float),
+                ("logits_dtype", ctypes.c_int)]
+
+
+for _name, (_res, _args) in {
+    "kvr_verify_workspace_bytes": (ctypes.c_size_t,
+                                   [ctypes.POINTER(kvr_verify_desc)]),
+    "kvr_verify_drafts": (_S, [ctypes.POINTER(kvr_verify_desc), _P,
+                               ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P,
+                               _P, _P, _P, _P, ctypes.c_size_t, _P]),
+}.items():
+    _f = getattr(lib, _name)
+    _f.restype = _res
+    _f.argtypes = _args
+
+_LOGITS = {torch.bfloat16: KVR_BF16, torch.float32: KVR_F32}
+
+
+def verify_workspace(n_seq, n_draft, vocab, device="cuda"):
+    """A workspace for verify_drafts() of these sizes."""
+    d = kvr_verify_desc(n_seq, n_draft, vocab, 1.0, KVR_BF16)
+    n = int(lib.kvr_verify_workspace_bytes(ctypes.byref(d)))
+    if n == 0:
+        raise KvrError(KVR_EINVAL, "verify_workspace", "invalid descriptor")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _logit_rows(x, what, lead):
+    """Row stride of logits [S][n][V]: rows dense among themselves, each row's
+    logits side by side."""
+    if x.dim() != 3 or tuple(x.shape) != lead or x.dtype not in _LOGITS:
+        raise ValueError(f"{what} must be bf16 or f32 {list(lead)}")
+    stride = x.stride(1) if x.shape[1] > 1 else x.stride(0)
+    if x.stride(2) != 1 and x.shape[2] > 1 or x.shape[0] > 1 and \
+            x.stride(0) != x.shape[1] * stride:
+        raise ValueError(f"{what}: rows must lie one stride apart")
+    return max(stride, x.shape[2])
+
+
+def verify_drafts(target, draft, tokens, u, race, n_draft=None,
+                  temperature=1.0, accepted=None, out_tokens=None,
+                  workspace=None, stream=None):
+    """Accept or reject drafted tokens (kvr_verify_drafts): target logits
+    [S][T + 1][V], draft logits [S][T][V], tokens int32 and u fp32 [S][T], race
+    fp32 [S][V] (exponential, > 0), n_draft int32 [S] or None.  Returns
+    (accepted [S], tokens [S][T + 1]) on the device."""
+    S, n, V = target.shape
+    T = n - 1
+    ts = _logit_rows(target, "target", (S, T + 1, V))
+    ds = _logit_rows(draft, "draft", (S, T, V)) if T else V
+    if draft.dtype != target.dtype:
+        raise ValueError("target and draft logits must be of one type")
+    for x, name, shape, dt in (
+            (tokens, "tokens", (S, T), torch.int32),
+            (u, "u", (S, T), torch.float32),
+            (race, "race", (S, V), torch.float32),
+            (n_draft, "n_draft", (S,), torch.int32),
+            (accepted, "accepted", (S,), torch.int32),
+            (out_tokens, "out_tokens", (S, T + 1), torch.int32)):
+        if x is not None and (tuple(x.shape) != shape or x.dtype != dt):
+            raise ValueError(f"{name} must be {dt} {list(shape)}")
+    dev = target.device
+    if accepted is None:
+        accepted = torch.empty(S, dtype=torch.int32, device=dev)
+    if out_tokens is None:
+        out_tokens = torch.empty((S, T + 1), dtype=torch.int32, device=dev)
+    d = kvr_verify_desc(S, T, V, float(temperature), _LOGITS[target.dtype])
+    if workspace is None:
+        workspace = _scratch(int(lib.kvr_verify_workspace_bytes(
+            ctypes.byref(d))), dev, stream)
+    _check(lib.kvr_verify_drafts(
+        ctypes.byref(d), target.data_ptr(), ts, draft.data_ptr(), ds,
+        _ptr(tokens), _ptr(u), _ptr(race), _ptr(n_draft), _ptr(accepted),
+        _ptr(out_tokens), _ptr(workspace), workspace.numel(),
+        _stream(stream)), "kvr_verify_drafts")
+    return accepted, out_tokens
