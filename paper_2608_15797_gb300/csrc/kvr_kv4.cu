@@ -72,9 +72,10 @@ __global__ void __launch_bounds__(256)
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     fine &= __shfl_xor_sync(0xffffffffu, (int)fine, o) != 0;
   }
-  const uint32_t meta = group_meta(lo, hi, fine);
+  bool flat;
+  const uint32_t meta = group_meta(lo, hi, fine, flat);
 #pragma unroll
-  for (int e = 0; e < E; ++e) s_code[warp][lane * E + e] = (uint8_t)code_of(x[e], meta);
+  for (int e = 0; e < E; ++e) s_code[warp][lane * E + e] = (uint8_t)code_of(x[e], meta, flat);
   __syncwarp();
   const int r = q.len[s] - q.count[s] + t, rb = r % kBlock;
   const size_t u = unit_at(c, k.s0 + (int)s, k.lb, lr, h);

@@ -25,7 +25,8 @@ namespace kv4 {
 
 constexpr int kGroup = 64;   // channels that share a scale
 constexpr int kBlock = 32;   // tokens of a block
-constexpr int kMaxSeqs = 256;  // sequences of one launch
+constexpr int kMaxSeqs = 128;  // sequences of one launch
+constexpr int kPiece = 8;      // blocks of a piece of a unit, at most
 constexpr int kMaxTiles = 16;  // query tiles of a unit whose rows are split over CTAs
 
 __host__ __device__ constexpr int k_off() { return 0; }
@@ -92,20 +93,29 @@ __device__ __forceinline__ float s_of(uint32_t w) {
 
 // A group's (m, s) from its least and greatest value; `fine`: every value is
 // finite.  Each rounding is written out: the definition is fp32 arithmetic,
-// and no fused multiply-add may change it.
-__device__ __forceinline__ uint32_t group_meta(float lo, float hi, bool fine) {
-  if (!fine) return 0x00007FC0u;  // m = NaN, s = 0
+// and no fused multiply-add may change it.  `flat`: the group has one value
+// (s is 0 by definition) or none (m = NaN), and every code is 0.  What is held
+// as its s then multiplies 0 alone; it is |m| / 8, so that the attention can
+// write a value as s (c + m / s) for every group.
+__device__ __forceinline__ uint32_t group_meta(float lo, float hi, bool fine, bool &flat) {
+  const uint32_t least = 0x0080u;  // 2^-126
+  flat = true;
+  if (!fine) return 0x7FC0u | (least << 16);
   const float f = 1.0f / 15.0f;
   const float s = __fsub_rn(__fmul_rn(hi, f), __fmul_rn(lo, f));
   const uint32_t mb = __bfloat16_as_ushort(__float2bfloat16_rn(lo));
-  const uint32_t sb = __bfloat16_as_ushort(__float2bfloat16_rn(s));
+  uint32_t sb = __bfloat16_as_ushort(__float2bfloat16_rn(s));
+  flat = sb == 0;
+  if (flat) {
+    sb = mb & 0x7FFFu;                      // |m|
+    sb = sb > 0x0180u + least ? sb - 0x0180u : least;  // three exponents down
+  }
   return mb | (sb << 16);
 }
 // The code of x, 0..15, by the definition's division.
-__device__ __forceinline__ uint32_t code_of(float x, uint32_t meta) {
-  const float s = s_of(meta);
-  if (!(s > 0.f)) return 0;
-  const float c = rintf(__fdiv_rn(__fsub_rn(x, m_of(meta)), s));
+__device__ __forceinline__ uint32_t code_of(float x, uint32_t meta, bool flat) {
+  if (flat) return 0;
+  const float c = rintf(__fdiv_rn(__fsub_rn(x, m_of(meta)), s_of(meta)));
   return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
 }
 // What a code stands for.

@@ -1,140 +1,1002 @@
-// kvr_kv4_attend.cu -- attention over the 4-bit cache (kvr_kv4.cuh).
+// kvr_kv4_attend.cu -- attention over the 4-bit cache (kvr_kv4.cuh has its
+// layout).
+//
+// A unit's query rows (token, head of the group) are the columns of two small
+// matrix products per 16 cached tokens on warp-level tensor cores:
+//   S  [tokens x columns]  = K [tokens x d] Q^T
+//   O^T [d x columns]     += V^T [d x tokens] P^T
+// with the 4-bit codes as the A operand of both.  A code needs no conversion: a
+// masked nibble in a 16-bit half is the half-precision subnormal c 2^-24 (or
+// c 2^-20, one nibble up), which tensor cores multiply exactly; the powers of two
+// are taken up by q and by the epilogue.  The group's (m, s) enter outside the
+// product, in fp32:
+//   q . k = sum over groups of  s (c . q) + m sum(q)
+//   p . v = sum over tokens of  (p s) c + p m
+// so K's logits are formed from a product per group, and V's probabilities are
+// multiplied by s before they are rounded to 16 bits, w = half(p s).  With bf16
+// tensors the second term is w (m / s), so that a token's channels all have the
+// weight w / s and what the rounding costs is to scale with its values; with
+// fp32 tensors q and p s have two 16-bit terms, the second term is p m, and codes
+// are converted and count from 8 (m + 8 s in the place of m), so that sums do not
+// cancel.
+//
+// Rows stream through a ring of bulk copies for each warp, one 32-token block
+// (4,608 B at d = 128) a copy.  Units are cut into equal pieces of at most eight
+// blocks, and the list of all pieces into equal spans, one a CTA, so that lengths
+// of any mix fill the GPU; a unit that spans share is joined by the last of them
+// to finish, in order of the spans, so that results do not depend on scheduling.
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
+
+#include <algorithm>
 
 #include "kvr_device.cuh"
 #include "kvr_internal.h"
 #include "kvr_kv4.cuh"
+#include "kvr_ptx.cuh"
 
 namespace kvr {
 namespace kv4 {
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kWarps = kThreads / 32;
+using namespace ptx;
 
-// One CTA a (unit, token): its warps take every fourth row with an online
-// softmax for the G heads, and are merged at the end.
-template <typename T, typename O, int D>
-__global__ void __launch_bounds__(kThreads)
-    attend_kernel(const AttendParams p, const __grid_constant__ Seqs sq) {
-  pdl_begin();
-  const View &c = p.k.c;
-  constexpr int E = D / 32;
-  __shared__ float s_m[kWarps][8], s_z[kWarps][8], s_o[kWarps][8][D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int t = blockIdx.x, h = blockIdx.y % c.H, lr = blockIdx.y / c.H, s = blockIdx.z;
-  const size_t row = (((size_t)(p.k.s0 + s) * p.k.nl + lr) * p.n_q + t) * c.H + h;
-  const T *q = static_cast<const T *>(p.q) + row * c.G * D;
-  O *out = static_cast<O *>(p.out) + row * c.G * D;
-  const int count = sq.count[s], n = t < count ? sq.len[s] - count + t + 1 : 0;
-  const size_t u = unit_at(c, p.k.s0 + s, p.k.lb, lr, h);
-  float qv[8][E], o[8][E], m[8], z[8];
-  for (int g = 0; g < 8; ++g) {
-    m[g] = -1e30f;
-    z[g] = 0.f;
-    for (int e = 0; e < E; ++e) {
-      qv[g][e] = g < c.G ? dev::to_f(q[g * D + lane + 32 * e]) * c.scale : 0.f;
-      o[g][e] = 0.f;
-    }
-  }
-  for (int r = warp; r < n; r += kWarps) {
-    const uint8_t *block = block_at(c, u, r);
-    float k[E], v[E];
-    for (int e = 0; e < E; ++e) {
-      k[e] = k_value<D>(block, r % kBlock, lane + 32 * e);
-      v[e] = v_value<D>(block, r % kBlock, lane + 32 * e);
-    }
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStages = 2;      // blocks in flight a warp
+constexpr int kMaxGrid = 1024;  // CTAs of a split call, at most
+constexpr float kNone = -1e30f; // a maximum over nothing
+constexpr float kLog2e = 1.4426950408889634f;
+
+// How a launch is cut: item (sequence, unit, tile of query rows) i of sequence s
+// has pieces_of(blocks_of(s)) pieces; base[s] pieces precede sequence s.  A CTA
+// takes `span` pieces of the list, or one item where span == 0.
+struct Plan {
+  long long base[kMaxSeqs + 1];
+  long long span;
+  int tiles;
+};
+
+__host__ __device__ inline int blocks_of(int len) {
+  return len > kBlock ? (len + kBlock - 1) / kBlock : 1;
+}
+__host__ __device__ inline int pieces_of(int nb) { return (nb + kPiece - 1) / kPiece; }
+// First block of piece i of np.
+__device__ __forceinline__ int piece_at(int nb, int np, int i) {
+  return (int)((long long)i * nb / np);
+}
+
+// A run of blocks [begin, end) of one item, which are pieces [piece, piece + n).
+struct Run {
+  int s, item;        // sequence of the launch, item of the sequence
+  int begin, end, nb; // nb: all blocks of the item
+  int n;
+  long long at;       // list index of the first piece
+};
+
+template <int D, int NT>
+struct Smem {
+  static constexpr int kCols = 8 * NT;
+  static constexpr int kRow = D + 4;  // floats of an exchanged column
+  static constexpr int kRing = kWarps * kStages * block_bytes(D);
+  static constexpr int kExch = kWarps * kCols * (kRow + 2) * 4;
+  static constexpr int kBytes = kRing + kExch + kWarps * kStages * 8 + 16;
+};
+
+// 16-bit pairs of codes: field f (0..3) of a word, f + 4 in the high half.
+//  kRough: c 2^-24 (f even) or c 2^-20 (f odd): the fewest instructions, but the
+//    tensor core aligns products by their operands' exponents, a subnormal
+//    counting as 2^-14, and cuts below 2^-24 of the largest; a leading bit at
+//    2^-21 costs up to seven bits of that.  Enough for logits of bf16 outputs.
+//  kEven: c 2^-20; as exact as normal numbers.
+//  kCentred: c - 8.
+enum Codes { kRough, kEven, kCentred };
+template <Codes M>
+__device__ __forceinline__ void fields(uint32_t x, uint32_t (&f)[4]) {
+  if (M == kCentred) {
+    const __half2 off = __float2half2_rn(1032.f);
 #pragma unroll
-    for (int g = 0; g < 8; ++g) {
-      if (g >= c.G) break;
-      float x = 0.f;
-      for (int e = 0; e < E; ++e) x = fmaf(qv[g][e], k[e], x);
-      x = dev::warp_sum(x);
-      const float top = fmaxf(m[g], x), f = expf(m[g] - top), w = expf(x - top);
-      m[g] = top;
-      z[g] = fmaf(z[g], f, w);
-      for (int e = 0; e < E; ++e) o[g][e] = fmaf(w, v[e], o[g][e] * f);
+    for (int i = 0; i < 4; ++i) {
+      uint32_t y = ((x >> (4 * i)) & 0x000F000Fu) | 0x64006400u;  // 1024 + c
+      const __half2 z = __hsub2(*reinterpret_cast<__half2 *>(&y), off);
+      f[i] = *reinterpret_cast<const uint32_t *>(&z);
     }
+  } else if (M == kRough) {
+    const uint32_t y = x >> 8;
+    f[0] = x & 0x000F000Fu;
+    f[1] = x & 0x00F000F0u;
+    f[2] = y & 0x000F000Fu;
+    f[3] = y & 0x00F000F0u;
+  } else {
+    f[0] = (x << 4) & 0x00F000F0u;
+    f[1] = x & 0x00F000F0u;
+    f[2] = (x >> 4) & 0x00F000F0u;
+    f[3] = (x >> 8) & 0x00F000F0u;
   }
-  for (int g = 0; g < 8; ++g) {
-    if (lane == 0) {
-      s_m[warp][g] = m[g];
-      s_z[warp][g] = z[g];
-    }
-    for (int e = 0; e < E; ++e) s_o[warp][g][lane + 32 * e] = o[g][e];
+}
+__host__ __device__ constexpr Codes k_codes(int terms) { return terms == 2 ? kCentred : kRough; }
+__host__ __device__ constexpr Codes v_codes(int terms) { return terms == 2 ? kCentred : kEven; }
+// What field f of 1 stands for, inverted.
+__host__ __device__ constexpr float field_unit(Codes m) {
+  return m == kCentred ? 1.f : m == kEven ? 0x1p20f : 0x1p24f;
+}
+
+template <int W>
+__device__ __forceinline__ void lds_words(uint32_t at, uint32_t (&x)[W]) {
+  if (W == 4)
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2 % W]), "=r"(x[3 % W])
+                 : "r"(at));
+  else
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(x[0]), "=r"(x[1]) : "r"(at));
+}
+template <int N>
+__device__ __forceinline__ void lds_meta(uint32_t at, uint32_t (&x)[N]) {
+  if (N == 2)
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(x[0]), "=r"(x[1 % N]) : "r"(at));
+  else
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x[0]) : "r"(at));
+}
+
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t x) {
+  return __half22float2(*reinterpret_cast<const __half2 *>(&x));
+}
+
+// A warp's query columns as B fragments.  TERMS == 2: the second holds what
+// rounding to 16 bits left of the first.
+template <int D, int NT, int TERMS>
+struct Query {
+  uint32_t f[NT][TERMS][D / 16][2];
+  float sum[NT][D / kGroup][2];  // of the lane's two columns: sum of q, scaled as f
+  float unit[NT][2];             // what a scaled product is to be multiplied by
+  int limit[NT][2];              // last row that the column sees, or -1
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, float (&x)[8]);
+template <>
+__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4 *>(p)[0];
+  const float4 b = reinterpret_cast<const float4 *>(p)[1];
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
+  x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+template <>
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&x)[8]) {
+  const uint4 a = *reinterpret_cast<const uint4 *>(p);
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < c.G * D; i += kThreads) {
-    const int g = i / D, x = i % D;
-    float top = -1e30f, zz = 0.f, a = 0.f;
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][g]);
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = expf(s_m[w][g] - top);
-      zz = fmaf(s_z[w][g], f, zz);
-      a = fmaf(s_o[w][g][x], f, a);
-    }
-    dev::st1(&out[i], n > 0 ? a / zz : 0.f);
-    if (x == 0) {
-      if (n > 0 && !isfinite(zz)) atomicOr(c.err, ERR_NONFINITE);
-      if (p.stats) {
-        const size_t unit = ((size_t)(p.k.s0 + s) * p.k.nl + lr) * c.H + h;
-        float *st = p.stats + (unit * p.n_q * c.G + t * c.G + g) * 2;
-        st[0] = top;
-        st[1] = 1.f / (zz * c.G);
+}
+
+// q's columns [col0, col0 + 8 NT) of a unit.  Each column is scaled by a power of
+// two that puts its largest value in [2^14, 2^15): exact, and a 16-bit half then
+// holds all that matters of a bf16 value.
+template <typename T, Codes M, int D, int NT, int TERMS>
+__device__ __forceinline__ void load_query(Query<D, NT, TERMS> &q, const AttendParams &p,
+                                           const Seqs &sq, int s, int lr, int h, int col0) {
+  const View &c = p.k.c;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int rows = p.n_q * c.G, count = sq.count[s], before = sq.len[s] - count;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int col = col0 + 8 * n + g, tok = col / c.G;
+    const bool live = col < rows;
+    const T *src = static_cast<const T *>(p.q) +
+                   (((((size_t)(p.k.s0 + s) * p.k.nl + lr) * p.n_q + tok) * c.H + h) * c.G +
+                    (col - tok * c.G)) *
+                       D;
+    float x[D / 32][8], top = 0.f;
+    bool fine = true;
+#pragma unroll
+    for (int w = 0; w < D / 32; ++w) {
+      if (live)
+        load8<T>(src + 64 * (w >> 1) + 16 * t + 8 * (w & 1), x[w]);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[w][e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        top = fmaxf(top, fabsf(x[w][e]));
+        fine &= isfinite(x[w][e]);
       }
     }
-  }
-}
-
-// Adds every row's probabilities: a warp a row.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
-    score_kernel(const AttendParams p, const __grid_constant__ Seqs sq) {
-  pdl_begin();
-  const View &c = p.k.c;
-  constexpr int E = D / 32;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = blockIdx.x * kWarps + warp;
-  const int h = blockIdx.y % c.H, lr = blockIdx.y / c.H, s = blockIdx.z;
-  const int count = sq.count[s], n = sq.len[s];
-  if (r >= n) return;
-  const size_t u = unit_at(c, p.k.s0 + s, p.k.lb, lr, h);
-  const uint8_t *block = block_at(c, u, r);
-  float k[E], sum = 0.f;
-  for (int e = 0; e < E; ++e) k[e] = k_value<D>(block, r % kBlock, lane + 32 * e);
-  const size_t unit = ((size_t)(p.k.s0 + s) * p.k.nl + lr) * c.H + h;
-  for (int t = max(0, r - (n - count)); t < count; ++t) {
-    const size_t row = (((size_t)(p.k.s0 + s) * p.k.nl + lr) * p.n_q + t) * c.H + h;
-    const T *q = static_cast<const T *>(p.q) + row * c.G * D;
-    for (int g = 0; g < c.G; ++g) {
-      float x = 0.f;
-      for (int e = 0; e < E; ++e)
-        x = fmaf(dev::to_f(q[g * D + lane + 32 * e]) * c.scale, k[e], x);
-      x = dev::warp_sum(x);
-      const float *st = p.stats + (unit * p.n_q * c.G + t * c.G + g) * 2;
-      sum += expf(x - st[0]) * st[1];
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const unsigned bad = __ballot_sync(0xffffffffu, !fine);
+    fine = ((bad >> (lane & ~3)) & 15u) == 0;
+    int k = 14 - ((int)(__float_as_uint(top) >> 23) - 127);
+    k = top == 0.f || !fine ? 0 : max(-90, min(k, 100));
+    const float up = __uint_as_float((unsigned)(127 + k) << 23);
+    float sum[D / kGroup] = {};
+#pragma unroll
+    for (int w = 0; w < D / 32; ++w) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[w][e] *= up;
+        sum[w >> 1] += x[w][e];
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        // the odd nibbles stand for 2^4 times their code
+        const float f = M == kRough && e == 1 ? 0.0625f : 1.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const float lo = x[w][2 * b + e] * f, hi = x[w][2 * b + 4 + e] * f;
+          uint32_t y = pack_half(lo, hi);
+          q.f[n][0][2 * w + e][b] = y;
+          if (TERMS == 2) {
+            const float2 z = unpack_half(y);
+            q.f[n][TERMS - 1][2 * w + e][b] = pack_half(lo - z.x, hi - z.y);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < D / kGroup; ++j) {
+      sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
+      sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
+      sum[j] *= 1.f / field_unit(M);
+    }
+    const float unit =
+        field_unit(M) * __uint_as_float((unsigned)(127 - k) << 23) * (c.scale * kLog2e);
+    const int limit = live && tok < count ? before + tok : -1;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int from = 8 * t + 4 * e;  // a lane of column 2 t + e
+#pragma unroll
+      for (int j = 0; j < D / kGroup; ++j)
+        q.sum[n][j][e] = __shfl_sync(0xffffffffu, sum[j], from);
+      q.unit[n][e] = __shfl_sync(0xffffffffu, unit, from);
+      q.limit[n][e] = __shfl_sync(0xffffffffu, limit, from);
     }
   }
-  if (lane == 0) c.score[u * c.sstride + r] += sum;
 }
 
-template <typename T, typename O, int D>
-cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream, int *launches) {
+// A token's (m, s) as the products take them: with centred codes m stands for
+// code 8.  `gone`: the token does not exist.
+template <bool CENTRED>
+__device__ __forceinline__ void meta_of(uint32_t w, bool gone, float &m, float &s) {
+  if (gone) w = 0;
+  m = m_of(w);
+  s = s_of(w);
+  if (CENTRED) m = fmaf(8.f, s, m);
+}
+
+// The logits (base 2) of a block's 32 tokens: l[tile][n][0, 1]: token g of the
+// 16-token tile, columns 2 t and 2 t + 1; [2, 3]: token g + 8.
+template <Codes M, int D, int NT, int TERMS, bool MASK>
+__device__ __forceinline__ void block_logits(const Query<D, NT, TERMS> &q, uint32_t block,
+                                             int row0, int len, float (&l)[2][NT][4]) {
+  constexpr int W = D / 32, GR = D / kGroup;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) {
+    const int r = 16 * tt + g;
+    uint32_t x[W], y[W], mx[GR], my[GR];
+    lds_words<W>(block + k_off() + r * (D / 2) + t * (D / 8), x);
+    lds_words<W>(block + k_off() + (r + 8) * (D / 2) + t * (D / 8), y);
+    lds_meta<GR>(block + km_off(D) + r * GR * 4, mx);
+    lds_meta<GR>(block + km_off(D) + (r + 8) * GR * 4, my);
+    float acc[NT][GR][4] = {};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      uint32_t a[4], b[4];
+      fields<M>(x[w], a);
+      fields<M>(y[w], b);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int z = 0; z < TERMS; ++z) {
+          mma_f16(acc[n][w >> 1], a[0], b[0], a[2], b[2], q.f[n][z][2 * w][0],
+                  q.f[n][z][2 * w][1]);
+          mma_f16(acc[n][w >> 1], a[1], b[1], a[3], b[3], q.f[n][z][2 * w + 1][0],
+                  q.f[n][z][2 * w + 1][1]);
+        }
+    }
+    float m[2][GR], sc[2][GR];
+#pragma unroll
+    for (int j = 0; j < GR; ++j) {
+      meta_of<M == kCentred>(mx[j], MASK && row0 + r >= len, m[0][j], sc[0][j]);
+      meta_of<M == kCentred>(my[j], MASK && row0 + r + 8 >= len, m[1][j], sc[1][j]);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v = 0.f;
+#pragma unroll
+        for (int j = 0; j < GR; ++j) {
+          v = j == 0 ? m[i >> 1][j] * q.sum[n][j][i & 1]
+                     : fmaf(m[i >> 1][j], q.sum[n][j][i & 1], v);
+          v = fmaf(sc[i >> 1][j], acc[n][j][i], v);
+        }
+        v *= q.unit[n][i & 1];
+        if (MASK && row0 + r + 8 * (i >> 1) > q.limit[n][i & 1]) v = -INFINITY;
+        l[tt][n][i] = v;
+      }
+  }
+}
+
+// A warp's running result: columns 2 t, 2 t + 1 of each 8.
+template <int D, int NT, int TERMS>
+struct State {
+  float o[NT][D / 16][4];        // channels 16 i + g, + 8; scaled by 2^(6 - ref)
+  float bias[NT][D / kGroup][2]; // the lane's share of what the codes leave out
+  float top[NT][2], z[NT][2];
+  float ref;                     // 2^(6 - e), e the exponent of the largest scale of V
+  float back;                    // 1 / ref
+  uint32_t most;                 // scales up to these bits fit that ref
+};
+
+template <int D, int NT, int TERMS>
+__device__ __forceinline__ void clear(State<D, NT, TERMS> &a) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a.o[n][i][e] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      a.top[n][e] = kNone;
+      a.z[n][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < D / kGroup; ++j) a.bias[n][j][e] = 0.f;
+    }
+  }
+  a.ref = a.back = 1.f;
+  a.most = 0;
+}
+
+// One block: logits, their exponentials against a running maximum that may lag by
+// 2^8 (p s is scaled so that a half holds it all the same), and V's product.
+template <int D, int NT, int TERMS, bool MASK>
+__device__ __forceinline__ void block_step(State<D, NT, TERMS> &a, const Query<D, NT, TERMS> &q,
+                                           uint32_t block, int row0, int len) {
+  constexpr Codes kV = v_codes(TERMS);
+  constexpr int W = D / 32, GR = D / kGroup;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  float l[2][NT][4];
+  block_logits<k_codes(TERMS), D, NT, TERMS, MASK>(q, block, row0, len, l);
+
+  uint32_t vm[2][2][GR];
+  uint32_t scale = 0;
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int r = 16 * tt + g + 8 * b;
+      lds_meta<GR>(block + vm_off(D) + r * GR * 4, vm[tt][b]);
+#pragma unroll
+      for (int j = 0; j < GR; ++j) {
+        if (MASK && row0 + r >= len) vm[tt][b][j] = 0;
+        scale = max(scale, vm[tt][b][j] & 0xFFFF0000u);
+      }
+    }
+  bool grow = scale > a.most;
+  float best[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      best[n][e] = fmaxf(fmaxf(l[0][n][e], l[0][n][2 + e]), fmaxf(l[1][n][e], l[1][n][2 + e]));
+      grow |= best[n][e] > a.top[n][e] + 8.f;
+    }
+  if (__any_sync(0xffffffffu, grow)) {
+    scale = __reduce_max_sync(0xffffffffu, scale);
+    float shrink = 1.f;
+    if (scale > a.most) {
+      const int e = max((int)(scale >> 23) - 127, -110);
+      const float ref = __uint_as_float((unsigned)(127 + 6 - e) << 23);
+      shrink = a.most ? ref / a.ref : 0.f;
+      a.ref = ref;
+      a.back = __uint_as_float((unsigned)(127 - 6 + e) << 23);
+      a.most = ((unsigned)(127 + e) << 23) | 0x007FFFFFu;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = best[n][e];
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+        x = fmaxf(x, a.top[n][e]);
+        const float f = ex2(a.top[n][e] - x);
+        a.top[n][e] = x;
+        a.z[n][e] *= f;
+#pragma unroll
+        for (int j = 0; j < GR; ++j) a.bias[n][j][e] *= f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          a.o[n][i][e] *= f * shrink;
+          a.o[n][i][2 + e] *= f * shrink;
+        }
+      }
+  }
+
+  // P^T, times s, as B fragments
+  uint32_t pf[2][NT][GR][TERMS][2];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      float m[GR], sc[GR];
+#pragma unroll
+      for (int j = 0; j < GR; ++j) {
+        meta_of<kV == kCentred>(vm[tt][b][j], false, m[j], sc[j]);
+        if (TERMS == 1) m[j] = MASK && vm[tt][b][j] == 0 ? 0.f : m[j] * rcp(sc[j]) * a.back;
+        sc[j] *= a.ref;
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float pr[2];
+        bool hidden[2];  // a hidden row's m may be NaN
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float x = l[tt][n][2 * b + e];
+          hidden[e] = MASK && x == -INFINITY;
+          pr[e] = ex2(x - a.top[n][e]);
+          a.z[n][e] += pr[e];
+        }
+#pragma unroll
+        for (int j = 0; j < GR; ++j) {
+          const float x = pr[0] * sc[j], y = pr[1] * sc[j];
+          const uint32_t w = pack_half(x, y);
+          pf[tt][n][j][0][b] = movm_t(w);
+          const float2 z = unpack_half(w);
+          if (TERMS == 2) pf[tt][n][j][TERMS - 1][b] = movm_t(pack_half(x - z.x, y - z.y));
+          a.bias[n][j][0] =
+              fmaf(TERMS == 2 ? pr[0] : z.x, hidden[0] ? 0.f : m[j], a.bias[n][j][0]);
+          a.bias[n][j][1] =
+              fmaf(TERMS == 2 ? pr[1] : z.y, hidden[1] ? 0.f : m[j], a.bias[n][j][1]);
+        }
+      }
+    }
+
+  // V's product.  A block's sum is formed from zero and added in fp32: the tensor
+  // core's accumulator rounds towards zero, which over a long context would
+  // drift.
+  uint32_t v[2][2][W];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int pr = 8 * tt + t + 4 * b;
+      lds_words<W>(block + v_off(D) + pr * D + v_chunk<D>(pr, g) * (D / 8), v[tt][b]);
+    }
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    uint32_t x[2][2][4];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) fields<kV>(v[tt][b][w], x[tt][b]);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float sum[4] = {};
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int z = 0; z < TERMS; ++z)
+            mma_f16(sum, x[tt][0][i], x[tt][0][2 + i], x[tt][1][i], x[tt][1][2 + i],
+                    pf[tt][n][w >> 1][z][0], pf[tt][n][w >> 1][z][1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a.o[n][2 * w + i][e] += sum[e];
+      }
+  }
+}
+
+// What a column's result needs to be joined with others of the same column.
+struct Joined {
+  float top, z, o;
+};
+__device__ __forceinline__ void join(Joined &a, float top, float z, float o) {
+  const float x = fmaxf(a.top, top), f = ex2(a.top - x), h = ex2(top - x);
+  a.o = fmaf(a.o, f, o * h);
+  a.z = fmaf(a.z, f, z * h);
+  a.top = x;
+}
+
+// A finished column element: normalised and written.
+template <typename O, int D>
+__device__ __forceinline__ void finish(const AttendParams &p, const Seqs &sq, int s, int lr,
+                                       int h, int col, int x, const Joined &a) {
   const View &c = p.k.c;
-  cudaError_t e = launch_pdl(attend_kernel<T, O, D>, dim3(p.n_q, p.k.nl * c.H, p.k.n),
-                             dim3(kThreads), 0, stream, p, q);
+  const int tok = col / c.G, rows = p.n_q * c.G;
+  if (col >= rows) return;
+  const size_t call = (size_t)(p.k.s0 + s) * p.k.nl + lr;
+  const bool live = tok < sq.count[s] && a.z != 0.f;
+  O *out = static_cast<O *>(p.out) +
+           (((call * p.n_q + tok) * c.H + h) * c.G + (col - tok * c.G)) * D + x;
+  dev::st1(out, live ? a.o / a.z : 0.f);
+  if (x == 0) {
+    if (live && !isfinite(a.z)) atomicOr(c.err, ERR_NONFINITE);
+    if (p.stats) {
+      float2 *st = reinterpret_cast<float2 *>(p.stats) + (call * c.H + h) * rows + col;
+      *st = make_float2(a.top, live ? 1.f / (a.z * c.G) : 0.f);
+    }
+  }
+}
+
+template <typename T, typename O, int D, int NT, int TERMS>
+__global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
+    attend_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ Seqs sq,
+                  const __grid_constant__ Plan plan) {
+  using S = Smem<D, NT>;
+  constexpr int kCols = S::kCols, GR = D / kGroup;
+  constexpr uint32_t kBytes = block_bytes(D);
+  extern __shared__ __align__(128) uint8_t smem[];
+  float *exch = reinterpret_cast<float *>(smem + S::kRing);  // [warp][col][kRow]
+  float *stat = exch + kWarps * kCols * S::kRow;             // [warp][col][2]
+  int *flag = reinterpret_cast<int *>(smem + S::kRing + S::kExch + kWarps * kStages * 8);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t ring = smem_u32(smem) + warp * kStages * kBytes;
+  const uint32_t bars = smem_u32(smem) + S::kRing + S::kExch + warp * kStages * 8;
+  volatile int *abort = flag + 1;
+  const View &c = p.k.c;
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(bars + 8 * i, 1);
+    fence_mbar_init();
+  }
+  if (threadIdx.x == 0) flag[1] = 0;
+  __syncthreads();
+  pdl_begin();
+
+  const int per_seq = p.k.nl * c.H * plan.tiles;
+  long long last;  // list index behind the CTA's last piece
+  Run run;
+  if (plan.span) {
+    run.at = blockIdx.x * plan.span;
+    last = min(run.at + plan.span, plan.base[p.k.n]);
+    int lo = 0, hi = p.k.n;  // the sequence that holds run.at
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (plan.base[mid] <= run.at) lo = mid; else hi = mid;
+    }
+    run.s = lo;
+    run.nb = blocks_of(sq.len[lo]);
+    const int np = pieces_of(run.nb);
+    const long long rest = run.at - plan.base[lo];
+    run.item = (int)(rest / np);
+    const int piece = (int)(rest - (long long)run.item * np);
+    run.n = (int)min((long long)(np - piece), last - run.at);
+    run.begin = piece_at(run.nb, np, piece);
+    run.end = piece_at(run.nb, np, piece + run.n);
+  } else {
+    run.s = blockIdx.x / per_seq;
+    run.item = blockIdx.x - run.s * per_seq;
+    // no block past the last row that the tile's last token sees
+    const int tok = min(sq.count[run.s], ((run.item % plan.tiles + 1) * kCols - 1) / c.G + 1);
+    run.nb = blocks_of(sq.len[run.s] - sq.count[run.s] + tok);
+    run.begin = 0;
+    run.end = run.nb;
+    run.at = 0;
+    run.n = 1;
+    last = 1;
+  }
+  // The run behind r; false at the end of the span.
+  auto next_run = [&](Run &r) {
+    r.at += r.n;
+    if (r.at >= last) return false;
+    if (++r.item == per_seq) {
+      r.item = 0;
+      ++r.s;
+      r.nb = blocks_of(sq.len[r.s]);
+    }
+    const int np = pieces_of(r.nb);
+    r.n = (int)min((long long)np, last - r.at);
+    r.begin = 0;
+    r.end = piece_at(r.nb, np, r.n);
+    return true;
+  };
+  auto unit_of = [&](const Run &r) {
+    const int unit = r.item / plan.tiles;
+    return unit_at(c, p.k.s0 + r.s, p.k.lb, unit / c.H, unit % c.H);
+  };
+
+  // The warp's blocks: every fourth of each run.  `ahead` runs before the
+  // consumer by up to kStages blocks.
+  Run ahead = run;
+  int ahead_blk = run.begin + warp;
+  bool more = true;
+  const uint8_t *ahead_at = c.blocks + unit_of(ahead) * c.nb * (size_t)kBytes;
+  int issued = 0, taken = 0;
+  auto issue = [&]() {
+    while (more && ahead_blk >= ahead.end) {
+      more = next_run(ahead);
+      if (more) {
+        ahead_blk = ahead.begin + warp;
+        ahead_at = c.blocks + unit_of(ahead) * c.nb * (size_t)kBytes;
+      }
+    }
+    if (!more) return;
+    if (lane == 0) {
+      const uint32_t bar = bars + 8 * (issued % kStages);
+      mbar_expect_tx(bar, kBytes);
+      bulk_load(ring + (issued % kStages) * kBytes, ahead_at + (size_t)ahead_blk * kBytes,
+                kBytes, bar);
+    }
+    ++issued;
+    ahead_blk += kWarps;
+  };
+  for (int i = 0; i < kStages; ++i) issue();
+
+  bool ok = true;
+  do {
+    const int unit = run.item / plan.tiles, tile = run.item % plan.tiles;
+    const int lr = unit / c.H, h = unit % c.H, col0 = tile * kCols;
+    const int len = sq.len[run.s];
+    Query<D, NT, TERMS> q;
+    load_query<T, k_codes(TERMS)>(q, p, sq, run.s, lr, h, col0);
+    State<D, NT, TERMS> a;
+    clear(a);
+    // rows below `full` are seen by every column that has a token
+    const int first = col0 / c.G;
+    const int full = first < sq.count[run.s] ? len - sq.count[run.s] + first + 1 : len;
+    for (int blk = run.begin + warp; blk < run.end; blk += kWarps) {
+      if (ok) {
+        ok = __all_sync(0xffffffffu, mbar_wait_idle(bars + 8 * (taken % kStages),
+                                                    (taken / kStages) & 1, abort));
+        if (!ok && lane == 0) {
+          atomicOr(c.err, ERR_TIMEOUT);
+          *abort = 1;
+        }
+      }
+      if (!ok) break;
+      const uint32_t at = ring + (taken % kStages) * kBytes;
+      const int row0 = blk * kBlock;
+      if (row0 + kBlock <= full)
+        block_step<D, NT, TERMS, false>(a, q, at, row0, len);
+      else
+        block_step<D, NT, TERMS, true>(a, q, at, row0, len);
+      ++taken;
+      __syncwarp();
+      issue();
+    }
+    // Join the warps.
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          a.z[n][e] += __shfl_xor_sync(0xffffffffu, a.z[n][e], o);
+#pragma unroll
+          for (int j = 0; j < GR; ++j)
+            a.bias[n][j][e] += __shfl_xor_sync(0xffffffffu, a.bias[n][j][e], o);
+        }
+        const int col = 8 * n + 2 * t + e;
+        float *to = exch + (warp * kCols + col) * S::kRow;
+        const float f = field_unit(v_codes(TERMS)) * a.back;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          to[16 * i + g] = fmaf(a.o[n][i][e], f, a.bias[n][i >> 2][e]);
+          to[16 * i + g + 8] = fmaf(a.o[n][i][2 + e], f, a.bias[n][i >> 2][e]);
+        }
+        if (g == 0) {
+          stat[(warp * kCols + col) * 2] = a.top[n][e];
+          stat[(warp * kCols + col) * 2 + 1] = a.z[n][e];
+        }
+      }
+    __syncthreads();
+    const bool whole = run.end - run.begin == run.nb;
+    const int slot = blockIdx.x * 2 + (run.at == blockIdx.x * plan.span ? 0 : 1);
+    float *part = whole ? nullptr : p.parts + (size_t)slot * kCols * (D + 2);
+    for (int i = threadIdx.x; i < kCols * D; i += kThreads) {
+      const int col = i / D, x = i % D;
+      Joined r{kNone, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w)
+        join(r, stat[(w * kCols + col) * 2], stat[(w * kCols + col) * 2 + 1],
+             exch[(w * kCols + col) * S::kRow + x]);
+      if (whole) {
+        finish<O, D>(p, sq, run.s, lr, h, col0 + col, x, r);
+      } else {
+        __stcg(&part[col * (D + 2) + 2 + x], r.o);
+        if (x == 0) {
+          __stcg(&part[col * (D + 2)], r.top);
+          __stcg(&part[col * (D + 2) + 1], r.z);
+        }
+      }
+    }
+    if (!whole) {
+      // The last of the item's spans to finish joins them, in order.
+      const int np = pieces_of(run.nb);
+      const long long i0 = plan.base[run.s] + (long long)run.item * np;
+      const int c0 = (int)(i0 / plan.span), c1 = (int)((i0 + np - 1) / plan.span);
+      unsigned *ticket = c.ticket + unit_of(run) * kMaxTiles + tile;
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) flag[0] = atomicAdd(ticket, 1u) == (unsigned)(c1 - c0);
+      __syncthreads();
+      if (flag[0]) {
+        __threadfence();
+        if (threadIdx.x == 0) *ticket = 0;
+        for (int i = threadIdx.x; i < kCols * D; i += kThreads) {
+          const int col = i / D, x = i % D;
+          Joined r{kNone, 0.f, 0.f};
+          for (int w = c0; w <= c1; ++w) {
+            const float *from =
+                p.parts + ((size_t)w * 2 + (w * plan.span >= i0 ? 0 : 1)) * kCols * (D + 2) +
+                col * (D + 2);
+            join(r, __ldcg(from), __ldcg(from + 1), __ldcg(from + 2 + x));
+          }
+          finish<O, D>(p, sq, run.s, lr, h, col0 + col, x, r);
+        }
+      }
+    }
+    __syncthreads();  // the exchange area is free again
+  } while (next_run(run));
+  if (!ok) {  // copies in flight end before the CTA does
+    volatile int never = 0;
+    for (; taken < issued; ++taken)
+      mbar_wait(bars + 8 * (taken % kStages), (taken / kStages) & 1, &never);
+  }
+}
+
+// Adds every row's probabilities to its score, after the attention has left each
+// column's maximum and normaliser.  K alone is read again: a unit's logits would
+// take 4 G bytes a row and token to keep, its K half takes 72.  A CTA has a span
+// of one unit's blocks and all columns, whose fragments lie in shared memory; a
+// warp loads a block's K into registers, its next one ahead, and goes through the
+// columns, so that a row's sum stays with one warp and its order is fixed.
+template <int D, int TERMS>
+struct ScoreSmem {
+  static constexpr int kTiles = TERMS == 1 ? 16 : 8;         // tiles of 8 columns at once
+  static constexpr int kFrag = TERMS * (D / 16) * 2;         // words a lane and tile
+  static constexpr int kSide = 2 * (D / kGroup) + 8;         // floats a column pair
+  static constexpr int kBytes = kTiles * (32 * kFrag + 4 * kSide) * 4;
+};
+template <typename T, int D, int TERMS>
+__global__ void __launch_bounds__(kThreads)
+    score_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ Seqs sq,
+                 int span) {
+  using S = ScoreSmem<D, TERMS>;
+  constexpr Codes M = TERMS == 2 ? kCentred : kEven;
+  constexpr int W = D / 32, GR = D / kGroup;
+  extern __shared__ __align__(128) uint8_t smem[];
+  uint4 *frag = reinterpret_cast<uint4 *>(smem);  // [tile][word / 4][lane]
+  float *side = reinterpret_cast<float *>(smem + S::kTiles * 32 * S::kFrag * 4);
+  pdl_begin();
+  const View &c = p.k.c;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int h = blockIdx.y % c.H, lr = blockIdx.y / c.H, s = blockIdx.z;
+  const int len = sq.len[s], count = sq.count[s];
+  const int first = blockIdx.x * span, nb = (len + kBlock - 1) / kBlock;
+  if (first >= nb || count == 0) return;
+  const int end = min(nb, first + span);
+  const size_t u = unit_at(c, p.k.s0 + s, p.k.lb, lr, h);
+  const uint8_t *blocks = c.blocks + u * c.nb * (size_t)block_bytes(D);
+  float *score = c.score + u * c.sstride;
+  const int rows = p.n_q * c.G;
+  const float2 *stats = reinterpret_cast<const float2 *>(p.stats) +
+                        (((size_t)(p.k.s0 + s) * p.k.nl + lr) * c.H + h) * rows;
+  // the columns that have a token, then as many whole tiles
+  const int tiles = (count * c.G + 7) / 8;
+  for (int t0 = 0; t0 < tiles; t0 += S::kTiles) {
+    const int tn = min(S::kTiles, tiles - t0);
+    __syncthreads();
+    for (int i = warp; i < tn; i += kWarps) {
+      Query<D, 1, TERMS> q;
+      load_query<T, M>(q, p, sq, s, lr, h, 8 * (t0 + i));
+      const uint32_t *f = &q.f[0][0][0][0];
+#pragma unroll
+      for (int w = 0; w < S::kFrag; w += 4)
+        frag[(i * (S::kFrag / 4) + w / 4) * 32 + lane] =
+            make_uint4(f[w], f[w + 1], f[w + 2], f[w + 3]);
+      if (g == 0) {
+        float *to = side + (4 * i + t) * S::kSide;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int col = 8 * (t0 + i) + 2 * t + e;
+          const bool live = q.limit[0][e] >= 0;
+          const float2 st = live ? stats[col] : make_float2(-kNone, 0.f);
+          to[e] = q.unit[0][e];
+          to[2 + e] = st.x;
+          to[4 + e] = st.y;
+          to[6 + e] = __int_as_float(q.limit[0][e]);
+#pragma unroll
+          for (int j = 0; j < GR; ++j) to[8 + 2 * j + e] = q.sum[0][j][e];
+        }
+      }
+    }
+    __syncthreads();
+    uint32_t next[2][2][W], next_m[2][2][GR];
+    auto load = [&](int blk) {
+      const uint8_t *at = blocks + (size_t)blk * block_bytes(D);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int r = 16 * tt + 8 * b + g;
+          const uint32_t *k = reinterpret_cast<const uint32_t *>(
+              at + k_off() + r * (D / 2) + t * (D / 8));
+          if (W == 4) {
+            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(k));
+            next[tt][b][0] = x.x, next[tt][b][1] = x.y;
+            next[tt][b][2 % W] = x.z, next[tt][b][3 % W] = x.w;
+          } else {
+            const uint2 x = __ldg(reinterpret_cast<const uint2 *>(k));
+            next[tt][b][0] = x.x, next[tt][b][1] = x.y;
+          }
+          const uint32_t *m = reinterpret_cast<const uint32_t *>(at + km_off(D)) + r * GR;
+#pragma unroll
+          for (int j = 0; j < GR; ++j) next_m[tt][b][j] = __ldg(m + j);
+        }
+    };
+    if (first + warp < end) load(first + warp);
+    for (int blk = first + warp; blk < end; blk += kWarps) {
+      uint32_t a[2][2][W][4];
+      float m[2][2][GR], sc[2][2][GR], sum[2][2] = {};
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int w = 0; w < W; ++w) fields<M>(next[tt][b][w], a[tt][b][w]);
+#pragma unroll
+          for (int j = 0; j < GR; ++j)
+            meta_of<M == kCentred>(next_m[tt][b][j],
+                                   blk * kBlock + 16 * tt + 8 * b + g >= len, m[tt][b][j],
+                                   sc[tt][b][j]);
+        }
+      if (blk + kWarps < end) load(blk + kWarps);
+      const bool all = (blk + 1) * kBlock <= len - count;  // every token sees the block
+#pragma unroll 1
+      for (int i = 0; i < tn; ++i) {
+        const float *at = side + (4 * i + t) * S::kSide;
+        float acc[2][GR][4] = {};
+#pragma unroll
+        for (int z = 0; z < TERMS; ++z)
+#pragma unroll
+          for (int w = 0; w < W; ++w) {
+            const uint4 f = frag[(i * (S::kFrag / 4) + z * W + w) * 32 + lane];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+              mma_f16(acc[tt][w >> 1], a[tt][0][w][0], a[tt][1][w][0], a[tt][0][w][2],
+                      a[tt][1][w][2], f.x, f.y);
+              mma_f16(acc[tt][w >> 1], a[tt][0][w][1], a[tt][1][w][1], a[tt][0][w][3],
+                      a[tt][1][w][3], f.z, f.w);
+            }
+          }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float unit = at[e], top = at[2 + e], inv = at[4 + e];
+          const int limit = __float_as_int(at[6 + e]);
+          float qs[GR];
+#pragma unroll
+          for (int j = 0; j < GR; ++j) qs[j] = at[8 + 2 * j + e];
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              float v = 0.f;
+#pragma unroll
+              for (int j = 0; j < GR; ++j) {
+                v = j == 0 ? m[tt][b][j] * qs[j] : fmaf(m[tt][b][j], qs[j], v);
+                v = fmaf(sc[tt][b][j], acc[tt][j][2 * b + e], v);
+              }
+              v = ex2(fmaf(v, unit, -top));
+              if (!all && blk * kBlock + 16 * tt + 8 * b + g > limit) v = 0.f;
+              sum[tt][b] = fmaf(v, inv, sum[tt][b]);
+            }
+        }
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float x = sum[tt][b];
+          x += __shfl_xor_sync(0xffffffffu, x, 1);
+          x += __shfl_xor_sync(0xffffffffu, x, 2);
+          const int r = blk * kBlock + 16 * tt + 8 * b + g;
+          if (t == 0 && r < len) score[r] += x;
+        }
+    }
+  }
+}
+
+// Tiles of 8 query rows that a kernel takes at once.
+int tile_cols(const View &c, int n_q) {
+  const long long rows = (long long)n_q * c.G;
+  return rows <= 8 ? 8 : rows <= 16 || !(c.io_bf16 && c.out_bf16) ? 16 : 24;
+}
+long long tiles_of(const View &c, int n_q) {
+  const int cols = tile_cols(c, n_q);
+  return ((long long)n_q * c.G + cols - 1) / cols;
+}
+
+template <typename T, int D, int TERMS>
+cudaError_t launch_scores(const AttendParams &p, const Seqs &q, int resident,
+                          cudaStream_t stream) {
+  constexpr int kBytes = ScoreSmem<D, TERMS>::kBytes;
+  auto kern = score_kernel<T, D, TERMS>;
+  static bool ready = false;
+  if (!ready) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != cudaSuccess) return e;
+    ready = true;
+  }
+  const long long units = (long long)p.k.nl * p.k.c.H;
+  long long total = 0;
+  int most = 1;
+  for (int i = 0; i < p.k.n; ++i) {
+    total += units * blocks_of(q.len[i]);
+    most = std::max(most, blocks_of(q.len[i]));
+  }
+  // about three CTAs for each that the device holds at once, a block a warp at least
+  const int span = (int)std::max<long long>(kWarps, total / (3 * resident));
+  return launch_pdl(kern, dim3((most + span - 1) / span, (unsigned)units, p.k.n), dim3(kThreads),
+                    kBytes, stream, p, q, span);
+}
+
+template <typename T, typename O, int D, int NT, int TERMS>
+cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream, int *launches) {
+  using S = Smem<D, NT>;
+  const View &c = p.k.c;
+  auto kern = attend_kernel<T, O, D, NT, TERMS>;
+  static int resident = 0;  // CTAs that the device holds at once
+  if (!resident) {
+    int dev = 0, sms = 0, per = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess)
+      e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    if (e == cudaSuccess)
+      e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, kThreads, S::kBytes);
+    if (e != cudaSuccess) return e;
+    resident = std::max(1, std::min(kMaxGrid, sms * std::max(1, per)));
+  }
+  Plan plan;
+  const long long tiles = tiles_of(c, p.n_q), per_seq = (long long)p.k.nl * c.H * tiles;
+  if (tiles > INT32_MAX || per_seq > INT32_MAX) return cudaErrorInvalidValue;
+  plan.tiles = (int)tiles;
+  plan.base[0] = 0;
+  for (int i = 0; i < p.k.n; ++i)
+    plan.base[i + 1] = plan.base[i] + per_seq * pieces_of(blocks_of(q.len[i]));
+  long long grid;
+  if (tiles <= kMaxTiles) {
+    const long long total = plan.base[p.k.n];
+    plan.span = (total + resident - 1) / resident;
+    grid = (total + plan.span - 1) / plan.span;
+  } else {
+    plan.span = 0;
+    grid = per_seq * p.k.n;
+  }
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  cudaError_t e = launch_pdl(kern, dim3((unsigned)grid), dim3(kThreads), S::kBytes, stream, p, q,
+                             plan);
   *launches = 1;
   if (e != cudaSuccess || !p.stats) return e;
-  int most = 1;
-  for (int i = 0; i < p.k.n; ++i) most = q.len[i] > most ? q.len[i] : most;
   *launches = 2;
-  return launch_pdl(score_kernel<T, D>, dim3((most + kWarps - 1) / kWarps, p.k.nl * c.H, p.k.n),
-                    dim3(kThreads), 0, stream, p, q);
+  return launch_scores<T, D, TERMS>(p, q, resident, stream);
 }
-template <typename T, typename O>
+template <typename T, typename O, int D, int TERMS>
+cudaError_t launch_tiles(const AttendParams &p, const Seqs &q, cudaStream_t stream,
+                         int *launches) {
+  switch (tile_cols(p.k.c, p.n_q)) {
+    case 8: return launch_as<T, O, D, 1, TERMS>(p, q, stream, launches);
+    case 16: return launch_as<T, O, D, 2, TERMS>(p, q, stream, launches);
+    default: return launch_as<T, O, D, TERMS == 1 ? 3 : 2, TERMS>(p, q, stream, launches);
+  }
+}
+template <typename T, typename O, int TERMS>
 cudaError_t launch_io(const AttendParams &p, const Seqs &q, cudaStream_t stream, int *launches) {
-  return p.k.c.d == 128 ? launch_as<T, O, 128>(p, q, stream, launches)
-                        : launch_as<T, O, 64>(p, q, stream, launches);
+  return p.k.c.d == 128 ? launch_tiles<T, O, 128, TERMS>(p, q, stream, launches)
+                        : launch_tiles<T, O, 64, TERMS>(p, q, stream, launches);
 }
 
 }  // namespace
@@ -142,16 +1004,21 @@ cudaError_t launch_io(const AttendParams &p, const Seqs &q, cudaStream_t stream,
 size_t attend_stat_floats(const View &c, int nl, int n_q) {
   return ((size_t)c.S * nl * c.H * n_q * c.G * 2 + 3) / 4 * 4;
 }
-size_t attend_part_floats(const View &, int, int) { return 0; }
+size_t attend_part_floats(const View &c, int nl, int n_q) {
+  const long long tiles = tiles_of(c, n_q);
+  if (tiles > kMaxTiles) return 0;
+  const size_t pieces = (size_t)std::min(c.S, kMaxSeqs) * nl * c.H * tiles * pieces_of(c.nb);
+  return 2 * std::min<size_t>(kMaxGrid, pieces) * tile_cols(c, n_q) * (c.d + 2);
+}
 
 cudaError_t launch_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream,
                           int *launches) {
   const bool ob = p.k.c.out_bf16;
   if (p.k.c.io_bf16)
-    return ob ? launch_io<__nv_bfloat16, __nv_bfloat16>(p, q, stream, launches)
-              : launch_io<__nv_bfloat16, float>(p, q, stream, launches);
-  return ob ? launch_io<float, __nv_bfloat16>(p, q, stream, launches)
-            : launch_io<float, float>(p, q, stream, launches);
+    return ob ? launch_io<__nv_bfloat16, __nv_bfloat16, 1>(p, q, stream, launches)
+              : launch_io<__nv_bfloat16, float, 2>(p, q, stream, launches);
+  return ob ? launch_io<float, __nv_bfloat16, 2>(p, q, stream, launches)
+            : launch_io<float, float, 2>(p, q, stream, launches);
 }
 
 }  // namespace kv4
