@@ -15,206 +15,483 @@
 #include "kvr_device.cuh"
 #include "kvr_internal.h"
 #include "kvr_kv4.cuh"
+#include "kvr_ptx.cuh"
 
 namespace kvr {
 namespace kv4 {
 namespace {
 
 template <typename T>
-__device__ __forceinline__ T from_f(float x);
-template <>
-__device__ __forceinline__ float from_f<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) {
-  return __float2bfloat16_rn(x);
+struct Eight {  // eight channels in memory
+  uint4 w[sizeof(T) / 2];
+};
+__device__ __forceinline__ void widen(const Eight<float> &a, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    x[4 * i] = __uint_as_float(a.w[i].x), x[4 * i + 1] = __uint_as_float(a.w[i].y);
+    x[4 * i + 2] = __uint_as_float(a.w[i].z), x[4 * i + 3] = __uint_as_float(a.w[i].w);
+  }
+}
+__device__ __forceinline__ void widen(const Eight<__nv_bfloat16> &a, float (&x)[8]) {
+  const uint32_t w[4] = {a.w[0].x, a.w[0].y, a.w[0].z, a.w[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void narrow(const float (&x)[8], Eight<float> &a) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    a.w[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]),
+                        __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+}
+__device__ __forceinline__ void narrow(const float (&x)[8], Eight<__nv_bfloat16> &a) {
+  a.w[0] = make_uint4(ptx::pack_bf16(x[0], x[1]), ptx::pack_bf16(x[2], x[3]),
+                      ptx::pack_bf16(x[4], x[5]), ptx::pack_bf16(x[6], x[7]));
 }
 
-// Quantise the new rows.  One warp a (sequence, layer, head, token) and side
-// (key or value): its lanes hold D / 32 neighbouring channels each, agree on the
-// groups' extremes by shuffles, leave the codes in shared memory and write the
-// row's words from there.
-template <typename T, int D>
-__global__ void __launch_bounds__(256)
-    append_kernel(const Call k, const __grid_constant__ Seqs q, int tokens, const T *key,
-                  const T *val, RowStrides st) {
-  pdl_begin();
-  const View &c = k.c;
-  __shared__ uint8_t s_code[8][D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long row = (long long)blockIdx.x * 8 + warp;  // [seq][layer][token][head][side]
-  const int side = (int)(row & 1);
-  const int h = (int)((row >> 1) % c.H);
-  const long long rest = (row >> 1) / c.H;
-  const int t = (int)(rest % tokens);
-  const int lr = (int)(rest / tokens % k.nl);
-  const long long s = rest / tokens / k.nl;
-  if (s >= k.n || t >= q.count[s]) return;
-  constexpr int E = D / 32;
-  const T *src = (side ? val : key) + (s + k.s0) * st.seq + lr * st.layer + t * st.token +
-                 h * st.head + lane * E;
-  float x[E];
-  bool fine = true;
+// The codes of eight values as one word, code e in bits 4 e .. 4 e + 3.  A product
+// with 1 / s finds a code unless it lies within 2e-5 of half-way between two (the
+// product is off by less than 2^-21 of 15); those few are divided.
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], uint32_t meta, bool flat) {
+  const float m = m_of(meta), r = ptx::rcp(s_of(meta));
+  uint32_t w = 0;
+  float off = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    x[e] = dev::to_f(src[e]);
-    fine &= isfinite(x[e]);
+  for (int e = 0; e < 8; ++e) {
+    const float q = fminf(fmaxf(__fmul_rn(__fsub_rn(x[e], m), r), 0.f), 15.f);
+    const float k = __fadd_rn(q, 12582912.f);  // 1.5 2^23: the code in the low bits
+    off = fmaxf(off, fabsf(__fsub_rn(q, __fsub_rn(k, 12582912.f))));
+    w |= (__float_as_uint(k) & 15u) << (4 * e);
   }
-  float lo = x[0], hi = x[0];
+  // a scale that is nearly subnormal has no reciprocal, and a huge one flushes
+  if (off > 0.49998f || !(r < 1e37f && r > 1e-37f)) {
+    w = 0;
 #pragma unroll
-  for (int e = 1; e < E; ++e) {
-    lo = fminf(lo, x[e]);
-    hi = fmaxf(hi, x[e]);
+    for (int e = 0; e < 8; ++e) w |= code_of(x[e], meta, flat) << (4 * e);
   }
-  constexpr int kLanes = kGroup / E;  // lanes of a group: 16 or 32
-#pragma unroll
-  for (int o = kLanes / 2; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    fine &= __shfl_xor_sync(0xffffffffu, (int)fine, o) != 0;
-  }
-  bool flat;
-  const uint32_t meta = group_meta(lo, hi, fine, flat);
-#pragma unroll
-  for (int e = 0; e < E; ++e) s_code[warp][lane * E + e] = (uint8_t)code_of(x[e], meta, flat);
-  __syncwarp();
-  const int r = q.len[s] - q.count[s] + t, rb = r % kBlock;
-  const size_t u = unit_at(c, k.s0 + (int)s, k.lb, lr, h);
-  uint8_t *block = block_at(c, u, r);
-  if (lane % kLanes == 0)
-    *reinterpret_cast<uint32_t *>(block + (side ? vm_off(D) : km_off(D)) +
-                                  (rb * (D / kGroup) + lane / kLanes) * 4) = meta;
-  if (lane < D / 4) {  // four codes a lane, one 16-bit store
-    const uint8_t *z = s_code[warp];
-    uint32_t w;
-    int at;
-    if (side) {
-      const int x0 = 32 * (lane >> 3) + (lane & 7);
-      w = z[x0] | (z[x0 + 16] << 4) | (z[x0 + 8] << 8) | (z[x0 + 24] << 12);
-      at = v_half<D>(rb, lane >> 3, lane & 7);
-    } else {
-      int hi4;
-      w = z[4 * lane] | (z[4 * lane + 1] << 4) | (z[4 * lane + 2] << 8) |
-          (z[4 * lane + 3] << 12);
-      at = k_byte<D>(rb, 4 * lane, hi4);
-    }
-    *reinterpret_cast<uint16_t *>(block + at) = (uint16_t)w;
-  }
-  if (side == 0 && lane == 0) c.score[u * c.sstride + r] = 0.f;
+  return flat ? 0 : w;
 }
 
-// What the newest rows stand for: one warp a (unit, row).
+// Between a word of eight neighbouring channels' codes of a row and V's halves:
+// the four lanes of 32 channels hold channels 8 y .. 8 y + 7, and lane y ends up
+// with the halves of c = 2 y (low) and 2 y + 1, whose nibbles are c + {0, 16, 8,
+// 24}.  The same exchange takes the halves back.
+__device__ __forceinline__ uint32_t to_halves(uint32_t w) {
+  const int y = threadIdx.x & 3;
+  uint32_t z = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t v = i == 0 ? w : __shfl_xor_sync(0xffffffffu, w, i);
+    const int from = y ^ i;  // the lane that v comes from: channels 8 from + c
+    const int f = 4 * (((from & 1) << 1) | (from >> 1));
+    z |= ((v >> (8 * y)) & 15u) << f;
+    z |= ((v >> (8 * y + 4)) & 15u) << (16 + f);
+  }
+  return z;
+}
+__device__ __forceinline__ uint32_t from_halves(uint32_t z) {
+  const int y = threadIdx.x & 3, f = 4 * (((y & 1) << 1) | (y >> 1));
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t v = i == 0 ? z : __shfl_xor_sync(0xffffffffu, z, i);
+    const int from = y ^ i;  // channels c = 2 from, 2 from + 1
+    w |= ((v >> f) & 15u) << (8 * from);
+    w |= ((v >> (16 + f)) & 15u) << (8 * from + 4);
+  }
+  return w;
+}
+
+// Where a lane that holds channels 8 i .. 8 i + 7 of row r finds or puts them.
+template <int D>
+__device__ __forceinline__ uint32_t *k_word(uint8_t *block, int r, int i) {
+  int hi;
+  return reinterpret_cast<uint32_t *>(block + k_byte<D>(r, 8 * i, hi));
+}
+template <int D>
+__device__ __forceinline__ uint16_t *v_half_at(uint8_t *block, int r, int i, int c) {
+  return reinterpret_cast<uint16_t *>(block + v_half<D>(r, i >> 2, c));
+}
+template <int D>
+__device__ __forceinline__ uint32_t *meta_word(uint8_t *block, int side, int r, int i) {
+  return reinterpret_cast<uint32_t *>(block + (side ? vm_off(D) : km_off(D)) +
+                                      (r * (D / kGroup) + (i >> 3)) * 4);
+}
+
+// Quantise the new rows.  D / 8 lanes a row, eight channels a lane; a warp takes
+// kRows rows of one side (key or value) at a time, their loads in flight together.
+// Bound by the bytes read and written where tokens are many, else by latency.
+template <typename T, int D>
+struct Append {
+  static constexpr int kLanes = D / 8;             // of a row
+  static constexpr int kOnce = 32 / kLanes;        // rows of a warp at once
+  static constexpr int kRounds = 4;
+  static constexpr int kRows = kOnce * kRounds;    // rows of a warp
+};
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
-    read_kernel(const Call k, const __grid_constant__ Seqs q, int rows, T *key, T *val) {
+    append_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q, int tokens,
+                  const T *key, const T *val, RowStrides st) {
   pdl_begin();
+  using A = Append<T, D>;
   const View &c = k.c;
-  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);  // [seq][layer][head][row]
-  const int lane = threadIdx.x & 31;
-  const int t = (int)(w % rows);
-  const long long rest = w / rows;
-  const int h = (int)(rest % c.H), lr = (int)(rest / c.H % k.nl);
-  const long long s = rest / c.H / k.nl;
+  const int lane = threadIdx.x & 31, i = lane % A::kLanes;
+  // a warp: (sequence, layer, head), side, kRows tokens
+  const int groups = (tokens + A::kRows - 1) / A::kRows;
+  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int side = (int)(w & 1);
+  const int tg = (int)((w >> 1) % groups);
+  const long long unit = (w >> 1) / groups;
+  const int h = (int)(unit % c.H), lr = (int)(unit / c.H % k.nl);
+  const long long s = unit / c.H / k.nl;
   if (s >= k.n) return;
-  const size_t to = ((((size_t)(s + k.s0) * k.nl + lr) * c.H + h) * rows + t) * D;
-  if (t >= q.count[s]) {
-    for (int x = lane; x < D; x += 32) {
-      key[to + x] = from_f<T>(0.f);
-      val[to + x] = from_f<T>(0.f);
+  const int count = q.count[s], t0 = tg * A::kRows;
+  if (t0 >= count) return;
+  const T *src = (side ? val : key) + (s + k.s0) * st.seq + lr * st.layer + h * st.head + 8 * i;
+  Eight<T> in[A::kRounds];
+#pragma unroll
+  for (int n = 0; n < A::kRounds; ++n) {
+    const int t = min(t0 + n * A::kOnce + lane / A::kLanes, count - 1);
+    const uint4 *at = reinterpret_cast<const uint4 *>(src + t * st.token);
+#pragma unroll
+    for (int e = 0; e < (int)sizeof(T) / 2; ++e) in[n].w[e] = __ldcs(at + e);
+  }
+  const size_t u = unit_at(c, k.s0 + (int)s, k.lb, lr, h);
+  const int r0 = q.len[s] - count;
+#pragma unroll
+  for (int n = 0; n < A::kRounds; ++n) {
+    if (t0 + n * A::kOnce >= count) break;
+    const int t = t0 + n * A::kOnce + lane / A::kLanes;
+    float x[8];
+    widen(in[n], x);
+    float lo = x[0], hi = x[0], odd = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      lo = fminf(lo, x[e]);
+      hi = fmaxf(hi, x[e]);
+      odd = fmaf(x[e], 0.f, odd);  // NaN for what is not finite
     }
-    return;
-  }
-  const int r = q.len[s] - q.count[s] + t;
-  const uint8_t *block = block_at(c, unit_at(c, k.s0 + (int)s, k.lb, lr, h), r);
-  for (int x = lane; x < D; x += 32) {
-    key[to + x] = from_f<T>(k_value<D>(block, r % kBlock, x));
-    val[to + x] = from_f<T>(v_value<D>(block, r % kBlock, x));
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {  // the eight lanes of a group
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    const unsigned bad = __ballot_sync(0xffffffffu, odd != 0.f);
+    bool flat;
+    const uint32_t meta =
+        group_meta(lo, hi, ((bad >> (lane & ~7)) & 255u) == 0, flat);
+    uint32_t word = codes_of(x, meta, flat);
+    if (side) word = to_halves(word);
+    if (t < count) {
+      const int r = r0 + t, rb = r % kBlock;
+      uint8_t *block = block_at(c, u, r);
+      if (side) {
+        const int y = i & 3;
+        *v_half_at<D>(block, rb, i, 2 * y) = (uint16_t)word;
+        *v_half_at<D>(block, rb, i, 2 * y + 1) = (uint16_t)(word >> 16);
+      } else {
+        *k_word<D>(block, rb, i) = word;
+      }
+      if (i % 8 == 0) *meta_word<D>(block, side, rb, i) = meta;
+      if (side == 0 && i == 0) c.score[u * c.sstride + r] = 0.f;
+    }
   }
 }
 
-// A row's rank: higher score first, then lower position.  -0 counts as 0, and
-// every NaN as one above every number.
-__device__ __forceinline__ unsigned long long row_key(float x, int i) {
-  const unsigned b = __float_as_uint(x), a = b & 0x7FFFFFFFu;
-  const unsigned o = a > 0x7F800000u ? 0xFFFFFFFFu : a == 0 ? 0x80000000u
-                     : b != a        ? ~b
-                                     : (b | 0x80000000u);
-  return ((unsigned long long)o << 32) | (0xFFFFFFFFu - (unsigned)i);
+// The codes and (m, s) of channels 8 i .. 8 i + 7 of row r of a block (V's codes
+// as halves), and what they stand for.  All lanes call word_values.
+struct RowWords {
+  uint32_t w, meta;
+};
+template <int D>
+__device__ __forceinline__ RowWords row_words(const uint8_t *block, int side, int r, int i) {
+  uint8_t *at = const_cast<uint8_t *>(block);
+  RowWords x;
+  if (side) {
+    const int y = i & 3;
+    x.w = *v_half_at<D>(at, r, i, 2 * y) |
+          ((uint32_t)*v_half_at<D>(at, r, i, 2 * y + 1) << 16);
+  } else {
+    x.w = *k_word<D>(at, r, i);
+  }
+  x.meta = *meta_word<D>(at, side, r, i);
+  return x;
+}
+__device__ __forceinline__ void word_values(const RowWords &a, int side, float (&x)[8]) {
+  const uint32_t w = side ? from_halves(a.w) : a.w;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = value_of((w >> (4 * e)) & 15u, a.meta);
 }
 
-// Cut a unit into dst: one CTA a unit.  A radix select finds the budget-th
-// largest (score, lower position) among the rows before the window; the kept
-// rows are then listed in order, in dst's positions, and their values written.
+// What the newest rows stand for: D / 8 lanes a row and side.
 template <typename T, int D>
-__global__ void __launch_bounds__(dev::kThreads)
-    evict_kernel(const Call k, const __grid_constant__ Seqs q, const CacheView dst, int budget,
-                 int window) {
+__global__ void __launch_bounds__(256)
+    read_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q, int rows, T *key,
+                T *val) {
+  pdl_begin();
+  using A = Append<T, D>;
+  const View &c = k.c;
+  const int lane = threadIdx.x & 31, i = lane % A::kLanes;
+  const int groups = (rows + A::kRows - 1) / A::kRows;
+  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int side = (int)(w & 1);
+  const int tg = (int)((w >> 1) % groups);
+  const long long unit = (w >> 1) / groups;
+  const int h = (int)(unit % c.H), lr = (int)(unit / c.H % k.nl);
+  const long long s = unit / c.H / k.nl;
+  if (s >= k.n) return;
+  const int count = q.count[s], r0 = q.len[s] - count;
+  const size_t u = unit_at(c, k.s0 + (int)s, k.lb, lr, h);
+  T *to = (side ? val : key) +
+          (((size_t)(s + k.s0) * k.nl + lr) * c.H + h) * rows * D + 8 * i;
+  RowWords words[A::kRounds];
+#pragma unroll
+  for (int n = 0; n < A::kRounds; ++n) {
+    const int r = r0 + min(tg * A::kRows + n * A::kOnce + lane / A::kLanes, count - 1);
+    words[n] = RowWords{0, 0};
+    if (count > 0) words[n] = row_words<D>(block_at(c, u, r), side, r % kBlock, i);
+  }
+#pragma unroll
+  for (int n = 0; n < A::kRounds; ++n) {
+    const int t = tg * A::kRows + n * A::kOnce + lane / A::kLanes;
+    float x[8];
+    word_values(words[n], side, x);
+    if (t >= count)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    Eight<T> o;
+    narrow(x, o);
+    if (t < rows)
+#pragma unroll
+      for (int e = 0; e < (int)sizeof(T) / 2; ++e)
+        __stcs(reinterpret_cast<uint4 *>(to + (size_t)t * D) + e, o.w[e]);
+  }
+}
+
+// A score's rank, higher first: -0 counts as 0, and every NaN as one above every
+// number.
+__device__ __forceinline__ uint32_t score_rank(float x) {
+  const uint32_t b = __float_as_uint(x), a = b & 0x7FFFFFFFu;
+  return a > 0x7F800000u ? 0xFFFFFFFFu : a == 0 ? 0x80000000u : b != a ? ~b : (b | 0x80000000u);
+}
+
+// Cut a unit into dst: one CTA a unit, whose scores' ranks lie in shared memory
+// (or are formed from the scores anew, where a unit has too many rows).  Four
+// passes of eight bits find the rank of the budget-th row before the window, with
+// a histogram a warp; of the rows of that rank the first ones are kept.  The kept
+// rows are listed in order, in dst's positions, and their values written from
+// there, D / 8 lanes a row and side.
+constexpr int kEvictThreads = 1024;
+constexpr int kEvictWarps = kEvictThreads / 32;
+constexpr int kEvictHists = 8;  // histograms: one for every four warps
+constexpr int kEvictSmemRows = 24576;
+
+template <typename T, int D, bool IN_SMEM>
+__global__ void __launch_bounds__(kEvictThreads)
+    evict_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q,
+                 const __grid_constant__ CacheView dst, int budget, int window) {
+  extern __shared__ uint32_t s_rank[];
+  __shared__ unsigned s_hist[kEvictHists][256];
+  __shared__ int s_count[kEvictWarps], s_ties[kEvictWarps];
+  __shared__ unsigned s_digit, s_need;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_begin();
   const View &c = k.c;
-  __shared__ unsigned s_hist[256];
-  __shared__ unsigned long long s_prefix;
-  __shared__ int s_need, s_base, s_wsum[dev::kWarps];
   const int h = blockIdx.x % c.H, l = blockIdx.x / c.H, s = blockIdx.y;
   const size_t u = unit_at(c, k.s0 + s, 0, l, h);
   const float *score = c.score + u * c.sstride;
   const int n = q.len[s], first = max(0, n - window);  // rows [first, n): the window
   const int keep = min(n, budget + window);
-  auto key = [&](int i) { return row_key(score[i], i); };
-  unsigned long long least = 0;
-  if (first > budget) {
-    if (budget > 0)
-      least = dev::block_select(first, budget, [](int) { return true; }, key, s_hist,
-                                &s_prefix, &s_need);
-    else
-      least = ~0ull;
-  }
-  const bool none = first > budget && budget == 0;
-  int32_t *pos = dst.pos + u * dst.sstride;
-  const int got = dev::block_collect(
-      0, n, [&](int i) { return i >= first || (!none && key(i) >= least); }, pos, s_wsum,
-      &s_base);
-  if (got != keep && threadIdx.x == 0) atomicOr(c.err, ERR_LENGTH);
-  const int m = min(got, keep);
-  float *to_score = dst.score + u * dst.sstride;
-  for (int i = threadIdx.x; i < m; i += dev::kThreads) to_score[i] = score[pos[i]];
-  T *K = static_cast<T *>(dst.K) + u * (size_t)dst.cap * D;
-  T *V = static_cast<T *>(dst.V) + u * (size_t)dst.cap * D;
-  for (int i = threadIdx.x / 32; i < m; i += dev::kWarps) {
-    const int r = pos[i];
-    const uint8_t *block = block_at(c, u, r);
-    for (int x = threadIdx.x & 31; x < D; x += 32) {
-      K[(size_t)i * D + x] = from_f<T>(k_value<D>(block, r % kBlock, x));
-      V[(size_t)i * D + x] = from_f<T>(v_value<D>(block, r % kBlock, x));
+  const bool cut = first > budget;
+  if (IN_SMEM && cut) {
+    // rows of 16 floats start on 64 bytes, so whole vectors are within the row
+    for (int i = tid; 4 * i < first; i += kEvictThreads) {
+      const float4 x = __ldg(reinterpret_cast<const float4 *>(score) + i);
+      *reinterpret_cast<uint4 *>(s_rank + 4 * i) =
+          make_uint4(score_rank(x.x), score_rank(x.y), score_rank(x.z), score_rank(x.w));
     }
   }
-  if (threadIdx.x == 0) {
+  auto rank = [&](int i) { return IN_SMEM ? s_rank[i] : score_rank(score[i]); };
+  // The rank of the last row kept, and how many rows of that rank are kept.
+  uint32_t least = 0, mask = 0;
+  int need = budget;
+  if (cut && budget > 0) {
+#pragma unroll 1
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      for (int i = tid; i < kEvictHists * 256; i += kEvictThreads) (&s_hist[0][0])[i] = 0;
+      __syncthreads();
+      unsigned *hist = s_hist[warp % kEvictHists];
+      for (int i = tid; i < first; i += kEvictThreads) {
+        const uint32_t x = rank(i);
+        if ((x & mask) == least) atomicAdd(&hist[(x >> shift) & 255u], 1u);
+      }
+      __syncthreads();
+      if (warp == 0) {
+        // lane j: digits 255 - 8 j .. 248 - 8 j, counted from the top
+        unsigned d[8], sum = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          d[e] = 0;
+#pragma unroll
+          for (int z = 0; z < kEvictHists; ++z) d[e] += s_hist[z][255 - 8 * lane - e];
+          sum += d[e];
+        }
+        unsigned above = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const unsigned x = __shfl_up_sync(0xffffffffu, above, o);
+          if (lane >= o) above += x;
+        }
+        above -= sum;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (above < (unsigned)need && above + d[e] >= (unsigned)need) {
+            s_digit = 255 - 8 * lane - e;
+            s_need = need - above;
+          }
+          above += d[e];
+        }
+      }
+      __syncthreads();
+      least |= s_digit << shift;
+      need = s_need;
+      mask |= 255u << shift;
+    }
+  }
+  // List the kept rows in order: each warp counts those of its own stretch, and
+  // then knows where they go.
+  int32_t *pos = dst.pos + u * dst.sstride;
+  float *to_score = dst.score + u * dst.sstride;
+  const int stretch = (n + 32 * kEvictWarps - 1) / (32 * kEvictWarps) * 32;
+  const int i0 = min(n, warp * stretch), i1 = min(n, i0 + stretch);
+  const unsigned lower = (1u << lane) - 1u;
+  auto look = [&](int i, unsigned &over, unsigned &tie) {  // ballots of 32 rows
+    bool o = i < n && (i >= first || !cut), t = false;
+    if (cut && budget > 0 && i < first) {
+      const uint32_t x = rank(i);
+      o = x > least;
+      t = x == least;
+    }
+    over = __ballot_sync(0xffffffffu, o);
+    tie = __ballot_sync(0xffffffffu, t);
+  };
+  int overs = 0, ties = 0;
+  for (int b = i0; b < i1; b += 32) {
+    unsigned over, tie;
+    look(b + lane, over, tie);
+    overs += __popc(over);
+    ties += __popc(tie);
+  }
+  if (lane == 0) {
+    s_count[warp] = overs;
+    s_ties[warp] = ties;
+  }
+  __syncthreads();
+  overs = __reduce_add_sync(0xffffffffu, lane < warp ? s_count[lane] : 0);
+  ties = __reduce_add_sync(0xffffffffu, lane < warp ? s_ties[lane] : 0);
+  for (int b = i0; b < i1; b += 32) {
+    unsigned over, tie;
+    look(b + lane, over, tie);
+    const int tied = ties + __popc(tie & lower);
+    const bool kept = (over >> lane & 1u) || ((tie >> lane & 1u) && tied < need);
+    const int at = overs + __popc(over & lower) + min(tied, need);
+    if (kept && at < keep) {
+      pos[at] = b + lane;
+      to_score[at] = score[b + lane];
+    }
+    overs += __popc(over);
+    ties += __popc(tie);
+  }
+  if (tid == kEvictThreads - 1 && overs + min(ties, need) != keep && cut)
+    atomicOr(c.err, ERR_LENGTH);
+  __syncthreads();
+  // Their values: D / 8 lanes a row, kBatch rows of each in flight.
+  constexpr int kLanes = D / 8, kOnce = 32 / kLanes, kBatch = 4;
+  constexpr int kStride = kEvictWarps * kOnce;
+  const int m = keep, ch = lane % kLanes;
+  for (int j0 = warp * kOnce; j0 < m; j0 += kBatch * kStride) {
+    RowWords kw[kBatch], vw[kBatch];
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) {
+      const int r = pos[min(j0 + e * kStride + lane / kLanes, m - 1)];
+      const uint8_t *block = block_at(c, u, r);
+      kw[e] = row_words<D>(block, 0, r % kBlock, ch);
+      vw[e] = row_words<D>(block, 1, r % kBlock, ch);
+    }
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) {
+      const int j = j0 + e * kStride + lane / kLanes;
+      float x[8];
+      Eight<T> o;
+      const size_t to = (u * (size_t)dst.cap + j) * D + 8 * ch;
+      word_values(kw[e], 0, x);
+      narrow(x, o);
+      if (j < m)
+#pragma unroll
+        for (int z = 0; z < (int)sizeof(T) / 2; ++z)
+          reinterpret_cast<uint4 *>(static_cast<T *>(dst.K) + to)[z] = o.w[z];
+      word_values(vw[e], 1, x);
+      narrow(x, o);
+      if (j < m)
+#pragma unroll
+        for (int z = 0; z < (int)sizeof(T) / 2; ++z)
+          reinterpret_cast<uint4 *>(static_cast<T *>(dst.V) + to)[z] = o.w[z];
+    }
+  }
+  if (tid == 0) {
     dst.state[4 * u] = m;
     dst.state[4 * u + 1] = n;
     dst.state[4 * u + 2] = 0;  // no R-KV key sum yet
   }
 }
 
+// Grid of a launch of eight warps a CTA, kRows rows of one side a warp.
+template <typename T, int D>
+bool row_grid(const Call &k, int rows, dim3 *grid) {
+  constexpr int kRows = Append<T, D>::kRows;
+  const long long warps = 2ll * k.n * k.nl * k.c.H * ((rows + kRows - 1) / kRows);
+  *grid = dim3((unsigned)((warps + 7) / 8));
+  return (warps + 7) / 8 <= INT32_MAX;
+}
 template <typename T, int D>
 cudaError_t launch_read(const Call &k, const Seqs &q, int rows, void *key, void *val,
                         cudaStream_t stream) {
-  const long long warps = (long long)k.n * k.nl * k.c.H * rows;
-  return launch_pdl(read_kernel<T, D>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, stream,
-                    k, q, rows, static_cast<T *>(key), static_cast<T *>(val));
+  dim3 grid;
+  if (!row_grid<T, D>(k, rows, &grid)) return cudaErrorInvalidValue;
+  return launch_pdl(read_kernel<T, D>, grid, dim3(256), 0, stream, k, q, rows,
+                    static_cast<T *>(key), static_cast<T *>(val));
 }
 
 template <typename T, int D>
 cudaError_t launch_append_as(const Call &k, const Seqs &q, int tokens, const void *key,
                              const void *val, const RowStrides &st, cudaStream_t stream) {
-  const long long warps = 2ll * k.n * k.nl * k.c.H * tokens;
-  return launch_pdl(append_kernel<T, D>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0,
-                    stream, k, q, tokens, static_cast<const T *>(key),
-                    static_cast<const T *>(val), st);
+  dim3 grid;
+  if (!row_grid<T, D>(k, tokens, &grid)) return cudaErrorInvalidValue;
+  return launch_pdl(append_kernel<T, D>, grid, dim3(256), 0, stream, k, q, tokens,
+                    static_cast<const T *>(key), static_cast<const T *>(val), st);
 }
 
 template <typename T, int D>
 cudaError_t launch_evict(const Call &k, const Seqs &q, const CacheView &dst, int budget,
                          int window, cudaStream_t stream) {
-  return launch_pdl(evict_kernel<T, D>, dim3(k.c.L * k.c.H, k.n), dim3(dev::kThreads), 0,
-                    stream, k, q, dst, budget, window);
+  int most = 0;
+  for (int i = 0; i < k.n; ++i) most = std::max(most, q.len[i] - window);
+  const dim3 grid(k.c.L * k.c.H, k.n);
+  if (most > kEvictSmemRows)
+    return launch_pdl(evict_kernel<T, D, false>, grid, dim3(kEvictThreads), 0, stream, k, q, dst,
+                      budget, window);
+  auto kern = evict_kernel<T, D, true>;
+  static bool ready = false;
+  if (!ready) {
+    const cudaError_t e = cudaFuncSetAttribute(
+        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictSmemRows * 4);
+    if (e != cudaSuccess) return e;
+    ready = true;
+  }
+  const int bytes = most > budget ? round_up16(most) * 4 : 0;
+  return launch_pdl(kern, grid, dim3(kEvictThreads), bytes, stream, k, q, dst, budget, window);
 }
 
 }  // namespace

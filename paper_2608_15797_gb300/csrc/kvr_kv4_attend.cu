@@ -723,14 +723,33 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
       if (flag[0]) {
         __threadfence();
         if (threadIdx.x == 0) *ticket = 0;
+        auto part_of = [&](int w) {
+          return p.parts + ((size_t)w * 2 + (w * plan.span >= i0 ? 0 : 1)) * kCols * (D + 2);
+        };
+        for (int col = warp; col < kCols; col += kWarps) {
+          float top = kNone, z = 0.f;
+          for (int w = c0 + lane; w <= c1; w += 32) {
+            const float2 x = __ldcg(reinterpret_cast<const float2 *>(part_of(w) + col * (D + 2)));
+            const float m = fmaxf(top, x.x);
+            z = fmaf(z, ex2(top - m), x.y * ex2(x.x - m));
+            top = m;
+          }
+          const float all = dev::warp_max(top);
+          z = dev::warp_sum(z * ex2(top - all));
+          if (lane == 0) {
+            stat[2 * col] = all;
+            stat[2 * col + 1] = z;
+          }
+        }
+        __syncthreads();
         for (int i = threadIdx.x; i < kCols * D; i += kThreads) {
           const int col = i / D, x = i % D;
-          Joined r{kNone, 0.f, 0.f};
+          if (col0 + col >= p.n_q * c.G) break;
+          Joined r{stat[2 * col], stat[2 * col + 1], 0.f};
+#pragma unroll 8
           for (int w = c0; w <= c1; ++w) {
-            const float *from =
-                p.parts + ((size_t)w * 2 + (w * plan.span >= i0 ? 0 : 1)) * kCols * (D + 2) +
-                col * (D + 2);
-            join(r, __ldcg(from), __ldcg(from + 1), __ldcg(from + 2 + x));
+            const float *from = part_of(w) + col * (D + 2);
+            r.o = fmaf(__ldcg(from + 2 + x), ex2(__ldcg(from) - r.top), r.o);
           }
           finish<O, D>(p, sq, run.s, lr, h, col0 + col, x, r);
         }
