@@ -26,7 +26,7 @@ namespace kv4 {
 constexpr int kGroup = 64;   // channels that share a scale
 constexpr int kBlock = 32;   // tokens of a block
 constexpr int kMaxSeqs = 128;  // sequences of one launch
-constexpr int kPiece = 8;      // blocks of a piece of a unit, at most
+constexpr int kPiece = 4;      // blocks of a piece of a unit, at most
 constexpr int kMaxTiles = 16;  // query tiles of a unit whose rows are split over CTAs
 
 __host__ __device__ constexpr int k_off() { return 0; }

@@ -21,7 +21,7 @@
 // cancel.
 //
 // Rows stream through a ring of bulk copies for each warp, one 32-token block
-// (4,608 B at d = 128) a copy.  Units are cut into equal pieces of at most eight
+// (4,608 B at d = 128) a copy.  Units are cut into equal pieces of at most four
 // blocks, and the list of all pieces into equal spans, one a CTA, so that lengths
 // of any mix fill the GPU; a unit that spans share is joined by the last of them
 // to finish, in order of the spans, so that results do not depend on scheduling.
@@ -44,6 +44,7 @@ using namespace ptx;
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 2;      // blocks in flight a warp
+constexpr int kMinSpan = 2;     // pieces of a span, at least
 constexpr int kMaxGrid = 1024;  // CTAs of a split call, at most
 constexpr float kNone = -1e30f; // a maximum over nothing
 constexpr float kLog2e = 1.4426950408889634f;
@@ -52,9 +53,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 // has pieces_of(blocks_of(s)) pieces; base[s] pieces precede sequence s.  A CTA
 // takes `span` pieces of the list, or one item where span == 0.
 struct Plan {
-  long long base[kMaxSeqs + 1];
-  long long span;
-  int tiles;
+  int32_t base[kMaxSeqs + 1];
+  int32_t span, tiles;
 };
 
 __host__ __device__ inline int blocks_of(int len) {
@@ -62,8 +62,10 @@ __host__ __device__ inline int blocks_of(int len) {
 }
 __host__ __device__ inline int pieces_of(int nb) { return (nb + kPiece - 1) / kPiece; }
 // First block of piece i of np.
+// (nb is at most 2^19, so np * nb fits 36 bits: where it does not fit 32, in 64.)
 __device__ __forceinline__ int piece_at(int nb, int np, int i) {
-  return (int)((long long)i * nb / np);
+  if (nb > 65535) return (int)((long long)i * nb / np);
+  return (int)((unsigned)i * (unsigned)nb / (unsigned)np);
 }
 
 // A run of blocks [begin, end) of one item, which are pieces [piece, piece + n).
@@ -71,7 +73,7 @@ struct Run {
   int s, item;        // sequence of the launch, item of the sequence
   int begin, end, nb; // nb: all blocks of the item
   int n;
-  long long at;       // list index of the first piece
+  int at;             // list index of the first piece
 };
 
 template <int D, int NT>
@@ -79,8 +81,11 @@ struct Smem {
   static constexpr int kCols = 8 * NT;
   static constexpr int kRow = D + 4;  // floats of an exchanged column
   static constexpr int kRing = kWarps * kStages * block_bytes(D);
-  static constexpr int kExch = kWarps * kCols * (kRow + 2) * 4;
-  static constexpr int kBytes = kRing + kExch + kWarps * kStages * 8 + 16;
+  // sums of the warps, (maximum, normaliser) of them and of all, their factors
+  static constexpr int kExch = kWarps * kCols * (kRow + 2) * 4 + kCols * 8 + kWarps * kCols * 4;
+  static constexpr int kBars = kRing + kExch;
+  static constexpr int kTable = kBars + kWarps * kStages * 8 + 16;
+  static constexpr int kBytes = kTable + kCols * 16;
 };
 
 // 16-bit pairs of codes: field f (0..3) of a word, f + 4 in the high half.
@@ -497,36 +502,56 @@ __device__ __forceinline__ void block_step(State<D, NT, TERMS> &a, const Query<D
   }
 }
 
-// What a column's result needs to be joined with others of the same column.
-struct Joined {
-  float top, z, o;
+// Where a column's result goes.
+struct Place {
+  long long out;  // element of `out`, or -1: no such column
+  int stat;       // index of its statistics (its row in the unit)
+  int live;       // 0: no token, zeros
 };
-__device__ __forceinline__ void join(Joined &a, float top, float z, float o) {
-  const float x = fmaxf(a.top, top), f = ex2(a.top - x), h = ex2(top - x);
-  a.o = fmaf(a.o, f, o * h);
-  a.z = fmaf(a.z, f, z * h);
-  a.top = x;
-}
-
-// A finished column element: normalised and written.
-template <typename O, int D>
-__device__ __forceinline__ void finish(const AttendParams &p, const Seqs &sq, int s, int lr,
-                                       int h, int col, int x, const Joined &a) {
+__device__ __forceinline__ Place place_of(const AttendParams &p, const Seqs &sq, int s, int lr,
+                                          int h, int col) {
   const View &c = p.k.c;
-  const int tok = col / c.G, rows = p.n_q * c.G;
-  if (col >= rows) return;
+  Place a;
+  const int tok = col / c.G;
   const size_t call = (size_t)(p.k.s0 + s) * p.k.nl + lr;
-  const bool live = tok < sq.count[s] && a.z != 0.f;
-  O *out = static_cast<O *>(p.out) +
-           (((call * p.n_q + tok) * c.H + h) * c.G + (col - tok * c.G)) * D + x;
-  dev::st1(out, live ? a.o / a.z : 0.f);
+  a.out = tok < p.n_q ? (long long)((((call * p.n_q + tok) * c.H + h) * c.G + (col - tok * c.G)) *
+                                    c.d)
+                      : -1;
+  a.stat = col;
+  a.live = tok < sq.count[s];
+  return a;
+}
+// Four channels of a finished column, normalised and written.
+template <typename O>
+__device__ __forceinline__ void finish(const AttendParams &p, const Place &a, int x, float4 o,
+                                       float top, float z, size_t unit) {
+  if (a.out < 0) return;
+  const bool live = a.live && z != 0.f;
+  const float f = live ? 1.f / z : 0.f;
+  if (!live) o = make_float4(0.f, 0.f, 0.f, 0.f);
+  o.x *= f, o.y *= f, o.z *= f, o.w *= f;
+  O *to = static_cast<O *>(p.out) + a.out + x;
+  if (sizeof(O) == 2)
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+  else
+    *reinterpret_cast<float4 *>(to) = o;
   if (x == 0) {
-    if (live && !isfinite(a.z)) atomicOr(c.err, ERR_NONFINITE);
-    if (p.stats) {
-      float2 *st = reinterpret_cast<float2 *>(p.stats) + (call * c.H + h) * rows + col;
-      *st = make_float2(a.top, live ? 1.f / (a.z * c.G) : 0.f);
-    }
+    if (live && !isfinite(z)) atomicOr(p.k.c.err, ERR_NONFINITE);
+    if (p.stats)
+      reinterpret_cast<float2 *>(p.stats)[unit * (p.n_q * p.k.c.G) + a.stat] =
+          make_float2(top, f / p.k.c.G);
   }
+}
+__device__ __forceinline__ void add4(float4 &a, const float4 &b, float f) {
+  a.x = fmaf(b.x, f, a.x), a.y = fmaf(b.y, f, a.y);
+  a.z = fmaf(b.z, f, a.z), a.w = fmaf(b.w, f, a.w);
+}
+// Adds one to *at, behind all the CTA has written before the barrier that precedes
+// it and ahead of what it reads after the one that follows.
+__device__ __forceinline__ unsigned take_ticket(unsigned *at) {
+  unsigned old;
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(at) : "memory");
+  return old;
 }
 
 template <typename T, typename O, int D, int NT, int TERMS>
@@ -539,10 +564,13 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
   extern __shared__ __align__(128) uint8_t smem[];
   float *exch = reinterpret_cast<float *>(smem + S::kRing);  // [warp][col][kRow]
   float *stat = exch + kWarps * kCols * S::kRow;             // [warp][col][2]
-  int *flag = reinterpret_cast<int *>(smem + S::kRing + S::kExch + kWarps * kStages * 8);
+  float2 *col_stat = reinterpret_cast<float2 *>(stat + kWarps * kCols * 2);
+  float *factor = reinterpret_cast<float *>(col_stat + kCols);
+  int *flag = reinterpret_cast<int *>(smem + S::kBars + kWarps * kStages * 8);
+  Place *place = reinterpret_cast<Place *>(smem + S::kTable);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t ring = smem_u32(smem) + warp * kStages * kBytes;
-  const uint32_t bars = smem_u32(smem) + S::kRing + S::kExch + warp * kStages * 8;
+  const uint32_t bars = smem_u32(smem) + S::kBars + warp * kStages * 8;
   volatile int *abort = flag + 1;
   const View &c = p.k.c;
   if (lane == 0) {
@@ -554,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
   pdl_begin();
 
   const int per_seq = p.k.nl * c.H * plan.tiles;
-  long long last;  // list index behind the CTA's last piece
+  int last;  // list index behind the CTA's last piece
   Run run;
   if (plan.span) {
     run.at = blockIdx.x * plan.span;
@@ -567,10 +595,10 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
     run.s = lo;
     run.nb = blocks_of(sq.len[lo]);
     const int np = pieces_of(run.nb);
-    const long long rest = run.at - plan.base[lo];
-    run.item = (int)(rest / np);
-    const int piece = (int)(rest - (long long)run.item * np);
-    run.n = (int)min((long long)(np - piece), last - run.at);
+    const int rest = run.at - plan.base[lo];
+    run.item = rest / np;
+    const int piece = rest - run.item * np;
+    run.n = min(np - piece, last - run.at);
     run.begin = piece_at(run.nb, np, piece);
     run.end = piece_at(run.nb, np, piece + run.n);
   } else {
@@ -595,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
       r.nb = blocks_of(sq.len[r.s]);
     }
     const int np = pieces_of(r.nb);
-    r.n = (int)min((long long)np, last - r.at);
+    r.n = min(np, last - r.at);
     r.begin = 0;
     r.end = piece_at(r.nb, np, r.n);
     return true;
@@ -637,6 +665,8 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
     const int unit = run.item / plan.tiles, tile = run.item % plan.tiles;
     const int lr = unit / c.H, h = unit % c.H, col0 = tile * kCols;
     const int len = sq.len[run.s];
+    if (threadIdx.x < kCols)
+      place[threadIdx.x] = place_of(p, sq, run.s, lr, h, col0 + threadIdx.x);
     Query<D, NT, TERMS> q;
     load_query<T, k_codes(TERMS)>(q, p, sq, run.s, lr, h, col0);
     State<D, NT, TERMS> a;
@@ -691,67 +721,110 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
       }
     __syncthreads();
     const bool whole = run.end - run.begin == run.nb;
+    // Each column's maximum and normaliser over the warps, and the warps' factors;
+    // stat[0 .. kCols) then holds (maximum, normaliser), factor[warp][column].
+    float2 joined = make_float2(kNone, 0.f);
+    if (threadIdx.x < kCols) {
+      const float2 *of = reinterpret_cast<const float2 *>(stat) + threadIdx.x;
+      float2 x[kWarps];
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        x[w] = of[w * kCols];
+        joined.x = fmaxf(joined.x, x[w].x);
+      }
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        x[w].x = ex2(x[w].x - joined.x);
+        joined.y = fmaf(x[w].y, x[w].x, joined.y);
+      }
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) factor[w * kCols + threadIdx.x] = x[w].x;
+      col_stat[threadIdx.x] = joined;
+    }
+    __syncthreads();
+    constexpr int kPer = kCols * D / 4 / kThreads;  // groups of four channels a thread
+    const size_t call_unit = ((size_t)(p.k.s0 + run.s) * p.k.nl + lr) * c.H + h;
     const int slot = blockIdx.x * 2 + (run.at == blockIdx.x * plan.span ? 0 : 1);
-    float *part = whole ? nullptr : p.parts + (size_t)slot * kCols * (D + 2);
-    for (int i = threadIdx.x; i < kCols * D; i += kThreads) {
-      const int col = i / D, x = i % D;
-      Joined r{kNone, 0.f, 0.f};
+    float *part = p.parts + (size_t)slot * kCols * (D + 2);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = threadIdx.x + j * kThreads, col = 4 * i / D, x = 4 * i % D;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kWarps; ++w)
-        join(r, stat[(w * kCols + col) * 2], stat[(w * kCols + col) * 2 + 1],
-             exch[(w * kCols + col) * S::kRow + x]);
-      if (whole) {
-        finish<O, D>(p, sq, run.s, lr, h, col0 + col, x, r);
-      } else {
-        __stcg(&part[col * (D + 2) + 2 + x], r.o);
-        if (x == 0) {
-          __stcg(&part[col * (D + 2)], r.top);
-          __stcg(&part[col * (D + 2) + 1], r.z);
-        }
-      }
+        add4(o, *reinterpret_cast<const float4 *>(&exch[(w * kCols + col) * S::kRow + x]),
+             factor[w * kCols + col]);
+      if (whole)
+        finish<O>(p, place[col], x, o, col_stat[col].x, col_stat[col].y, call_unit);
+      else
+        __stcg(reinterpret_cast<float4 *>(part) + i, o);
     }
     if (!whole) {
+      if (threadIdx.x < kCols)
+        __stcg(reinterpret_cast<float2 *>(part + kCols * D) + threadIdx.x, joined);
       // The last of the item's spans to finish joins them, in order.
       const int np = pieces_of(run.nb);
-      const long long i0 = plan.base[run.s] + (long long)run.item * np;
-      const int c0 = (int)(i0 / plan.span), c1 = (int)((i0 + np - 1) / plan.span);
+      const int i0 = plan.base[run.s] + run.item * np;
+      const int c0 = i0 / plan.span, c1 = (i0 + np - 1) / plan.span;
       unsigned *ticket = c.ticket + unit_of(run) * kMaxTiles + tile;
-      __threadfence();
       __syncthreads();
-      if (threadIdx.x == 0) flag[0] = atomicAdd(ticket, 1u) == (unsigned)(c1 - c0);
+      if (threadIdx.x == 0) flag[0] = take_ticket(ticket) == (unsigned)(c1 - c0);
       __syncthreads();
       if (flag[0]) {
-        __threadfence();
         if (threadIdx.x == 0) *ticket = 0;
         auto part_of = [&](int w) {
           return p.parts + ((size_t)w * 2 + (w * plan.span >= i0 ? 0 : 1)) * kCols * (D + 2);
         };
+        // Columns' maxima first, a lane a contributor; then kSome contributors at a
+        // time, their sums' loads in flight together.
         for (int col = warp; col < kCols; col += kWarps) {
           float top = kNone, z = 0.f;
           for (int w = c0 + lane; w <= c1; w += 32) {
-            const float2 x = __ldcg(reinterpret_cast<const float2 *>(part_of(w) + col * (D + 2)));
+            const float2 x = __ldcg(reinterpret_cast<const float2 *>(part_of(w) + kCols * D) + col);
             const float m = fmaxf(top, x.x);
             z = fmaf(z, ex2(top - m), x.y * ex2(x.x - m));
             top = m;
           }
           const float all = dev::warp_max(top);
           z = dev::warp_sum(z * ex2(top - all));
-          if (lane == 0) {
-            stat[2 * col] = all;
-            stat[2 * col + 1] = z;
-          }
+          if (lane == 0) col_stat[col] = make_float2(all, z);
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < kCols * D; i += kThreads) {
-          const int col = i / D, x = i % D;
-          if (col0 + col >= p.n_q * c.G) break;
-          Joined r{stat[2 * col], stat[2 * col + 1], 0.f};
-#pragma unroll 8
-          for (int w = c0; w <= c1; ++w) {
-            const float *from = part_of(w) + col * (D + 2);
-            r.o = fmaf(__ldcg(from + 2 + x), ex2(__ldcg(from) - r.top), r.o);
+        constexpr int kSome = NT == 1 ? 16 : 8;
+        float4 sum[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w0 = c0; w0 <= c1; w0 += kSome) {
+          for (int i = threadIdx.x; i < kSome * kCols; i += kThreads) {
+            const int w = w0 + i / kCols, col = i % kCols;
+            exch[i] = w <= c1 ? ex2(__ldcg(part_of(w) + kCols * D + 2 * col) - col_stat[col].x)
+                              : 0.f;
           }
-          finish<O, D>(p, sq, run.s, lr, h, col0 + col, x, r);
+          __syncthreads();
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            float4 x[kSome / 2][kPer];
+#pragma unroll
+            for (int w = 0; w < kSome / 2; ++w)
+#pragma unroll
+              for (int j = 0; j < kPer; ++j)
+                x[w][j] = __ldcg(reinterpret_cast<const float4 *>(
+                                     part_of(min(c1, w0 + half * (kSome / 2) + w))) +
+                                 threadIdx.x + j * kThreads);
+#pragma unroll
+            for (int w = 0; w < kSome / 2; ++w)
+#pragma unroll
+              for (int j = 0; j < kPer; ++j)
+                add4(sum[j], x[w][j], exch[(half * (kSome / 2) + w) * kCols +
+                                           4 * (threadIdx.x + j * kThreads) / D]);
+          }
+          __syncthreads();
+        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const int i = threadIdx.x + j * kThreads, col = 4 * i / D;
+          finish<O>(p, place[col], 4 * i % D, sum[j], col_stat[col].x, col_stat[col].y,
+                    call_unit);
         }
       }
     }
@@ -983,13 +1056,15 @@ cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream,
   const long long tiles = tiles_of(c, p.n_q), per_seq = (long long)p.k.nl * c.H * tiles;
   if (tiles > INT32_MAX || per_seq > INT32_MAX) return cudaErrorInvalidValue;
   plan.tiles = (int)tiles;
-  plan.base[0] = 0;
-  for (int i = 0; i < p.k.n; ++i)
-    plan.base[i + 1] = plan.base[i] + per_seq * pieces_of(blocks_of(q.len[i]));
+  long long total = 0;
+  for (int i = 0; i < p.k.n; ++i) {
+    plan.base[i] = (int32_t)total;
+    total += per_seq * pieces_of(blocks_of(q.len[i]));
+  }
+  plan.base[p.k.n] = (int32_t)total;
   long long grid;
-  if (tiles <= kMaxTiles) {
-    const long long total = plan.base[p.k.n];
-    plan.span = (total + resident - 1) / resident;
+  if (tiles <= kMaxTiles && total <= INT32_MAX) {
+    plan.span = (int32_t)std::max<long long>(kMinSpan, (total + resident - 1) / resident);
     grid = (total + plan.span - 1) / plan.span;
   } else {
     plan.span = 0;
