@@ -33,6 +33,7 @@
 #include "kvr_device.cuh"
 #include "kvr_internal.h"
 #include "kvr_kv4.cuh"
+#include "kvr_kv4_attend.cuh"
 #include "kvr_ptx.cuh"
 
 namespace kvr {
@@ -46,8 +47,6 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 2;      // blocks in flight a warp
 constexpr int kMinSpan = 2;     // pieces of a span, at least
 constexpr int kMaxGrid = 1024;  // CTAs of a split call, at most
-constexpr float kNone = -1e30f; // a maximum over nothing
-constexpr float kLog2e = 1.4426950408889634f;
 
 // How a launch is cut: item (sequence, unit, tile of query rows) i of sequence s
 // has pieces_of(blocks_of(s)) pieces; base[s] pieces precede sequence s.  A CTA
@@ -57,9 +56,6 @@ struct Plan {
   int32_t span, tiles;
 };
 
-__host__ __device__ inline int blocks_of(int len) {
-  return len > kBlock ? (len + kBlock - 1) / kBlock : 1;
-}
 __host__ __device__ inline int pieces_of(int nb) { return (nb + kPiece - 1) / kPiece; }
 // First block of piece i of np.
 // (nb is at most 2^19, so np * nb fits 36 bits: where it does not fit 32, in 64.)
@@ -502,58 +498,6 @@ __device__ __forceinline__ void block_step(State<D, NT, TERMS> &a, const Query<D
   }
 }
 
-// Where a column's result goes.
-struct Place {
-  long long out;  // element of `out`, or -1: no such column
-  int stat;       // index of its statistics (its row in the unit)
-  int live;       // 0: no token, zeros
-};
-__device__ __forceinline__ Place place_of(const AttendParams &p, const Seqs &sq, int s, int lr,
-                                          int h, int col) {
-  const View &c = p.k.c;
-  Place a;
-  const int tok = col / c.G;
-  const size_t call = (size_t)(p.k.s0 + s) * p.k.nl + lr;
-  a.out = tok < p.n_q ? (long long)((((call * p.n_q + tok) * c.H + h) * c.G + (col - tok * c.G)) *
-                                    c.d)
-                      : -1;
-  a.stat = col;
-  a.live = tok < sq.count[s];
-  return a;
-}
-// Four channels of a finished column, normalised and written.
-template <typename O>
-__device__ __forceinline__ void finish(const AttendParams &p, const Place &a, int x, float4 o,
-                                       float top, float z, size_t unit) {
-  if (a.out < 0) return;
-  const bool live = a.live && z != 0.f;
-  const float f = live ? 1.f / z : 0.f;
-  if (!live) o = make_float4(0.f, 0.f, 0.f, 0.f);
-  o.x *= f, o.y *= f, o.z *= f, o.w *= f;
-  O *to = static_cast<O *>(p.out) + a.out + x;
-  if (sizeof(O) == 2)
-    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
-  else
-    *reinterpret_cast<float4 *>(to) = o;
-  if (x == 0) {
-    if (live && !isfinite(z)) atomicOr(p.k.c.err, ERR_NONFINITE);
-    if (p.stats)
-      reinterpret_cast<float2 *>(p.stats)[unit * (p.n_q * p.k.c.G) + a.stat] =
-          make_float2(top, f / p.k.c.G);
-  }
-}
-__device__ __forceinline__ void add4(float4 &a, const float4 &b, float f) {
-  a.x = fmaf(b.x, f, a.x), a.y = fmaf(b.y, f, a.y);
-  a.z = fmaf(b.z, f, a.z), a.w = fmaf(b.w, f, a.w);
-}
-// Adds one to *at, behind all the CTA has written before the barrier that precedes
-// it and ahead of what it reads after the one that follows.
-__device__ __forceinline__ unsigned take_ticket(unsigned *at) {
-  unsigned old;
-  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(at) : "memory");
-  return old;
-}
-
 template <typename T, typename O, int D, int NT, int TERMS>
 __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
     attend_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ Seqs sq,
@@ -676,8 +620,7 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
     const int full = first < sq.count[run.s] ? len - sq.count[run.s] + first + 1 : len;
     for (int blk = run.begin + warp; blk < run.end; blk += kWarps) {
       if (ok) {
-        ok = __all_sync(0xffffffffu, mbar_wait_idle(bars + 8 * (taken % kStages),
-                                                    (taken / kStages) & 1, abort));
+        ok = warp_wait(bars + 8 * (taken % kStages), (taken / kStages) & 1, abort);
         if (!ok && lane == 0) {
           atomicOr(c.err, ERR_TIMEOUT);
           *abort = 1;
@@ -1010,16 +953,18 @@ long long tiles_of(const View &c, int n_q) {
 }
 
 template <typename T, int D, int TERMS>
-cudaError_t launch_scores(const AttendParams &p, const Seqs &q, int resident,
-                          cudaStream_t stream) {
+cudaError_t launch_scores(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
   constexpr int kBytes = ScoreSmem<D, TERMS>::kBytes;
   auto kern = score_kernel<T, D, TERMS>;
-  static bool ready = false;
-  if (!ready) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+  static int sms = 0;
+  if (!sms) {
+    int dev = 0, n = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e != cudaSuccess) return e;
-    ready = true;
+    sms = n;
   }
   const long long units = (long long)p.k.nl * p.k.c.H;
   long long total = 0;
@@ -1028,14 +973,14 @@ cudaError_t launch_scores(const AttendParams &p, const Seqs &q, int resident,
     total += units * blocks_of(q.len[i]);
     most = std::max(most, blocks_of(q.len[i]));
   }
-  // about three CTAs for each that the device holds at once, a block a warp at least
-  const int span = (int)std::max<long long>(kWarps, total / (3 * resident));
+  // about twelve CTAs an SM, a block a warp at least
+  const int span = (int)std::max<long long>(kWarps, total / (12 * sms));
   return launch_pdl(kern, dim3((most + span - 1) / span, (unsigned)units, p.k.n), dim3(kThreads),
                     kBytes, stream, p, q, span);
 }
 
 template <typename T, typename O, int D, int NT, int TERMS>
-cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream, int *launches) {
+cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
   using S = Smem<D, NT>;
   const View &c = p.k.c;
   auto kern = attend_kernel<T, O, D, NT, TERMS>;
@@ -1071,26 +1016,27 @@ cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream,
     grid = per_seq * p.k.n;
   }
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  cudaError_t e = launch_pdl(kern, dim3((unsigned)grid), dim3(kThreads), S::kBytes, stream, p, q,
-                             plan);
-  *launches = 1;
-  if (e != cudaSuccess || !p.stats) return e;
-  *launches = 2;
-  return launch_scores<T, D, TERMS>(p, q, resident, stream);
+  return launch_pdl(kern, dim3((unsigned)grid), dim3(kThreads), S::kBytes, stream, p, q, plan);
 }
 template <typename T, typename O, int D, int TERMS>
-cudaError_t launch_tiles(const AttendParams &p, const Seqs &q, cudaStream_t stream,
-                         int *launches) {
+cudaError_t launch_tiles(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
   switch (tile_cols(p.k.c, p.n_q)) {
-    case 8: return launch_as<T, O, D, 1, TERMS>(p, q, stream, launches);
-    case 16: return launch_as<T, O, D, 2, TERMS>(p, q, stream, launches);
-    default: return launch_as<T, O, D, TERMS == 1 ? 3 : 2, TERMS>(p, q, stream, launches);
+    case 8: return launch_as<T, O, D, 1, TERMS>(p, q, stream);
+    case 16: return launch_as<T, O, D, 2, TERMS>(p, q, stream);
+    default: return launch_as<T, O, D, TERMS == 1 ? 3 : 2, TERMS>(p, q, stream);
   }
 }
 template <typename T, typename O, int TERMS>
 cudaError_t launch_io(const AttendParams &p, const Seqs &q, cudaStream_t stream, int *launches) {
-  return p.k.c.d == 128 ? launch_tiles<T, O, 128, TERMS>(p, q, stream, launches)
-                        : launch_tiles<T, O, 64, TERMS>(p, q, stream, launches);
+  const bool wide = p.k.c.d == 128;
+  cudaError_t e = tile_applies(p.k.c, p.n_q) ? launch_tile_attend(p, q, stream)
+                  : wide                     ? launch_tiles<T, O, 128, TERMS>(p, q, stream)
+                                             : launch_tiles<T, O, 64, TERMS>(p, q, stream);
+  *launches = 1;
+  if (e != cudaSuccess || !p.stats) return e;
+  *launches = 2;
+  return wide ? launch_scores<T, 128, TERMS>(p, q, stream)
+              : launch_scores<T, 64, TERMS>(p, q, stream);
 }
 
 }  // namespace
@@ -1099,6 +1045,7 @@ size_t attend_stat_floats(const View &c, int nl, int n_q) {
   return ((size_t)c.S * nl * c.H * n_q * c.G * 2 + 3) / 4 * 4;
 }
 size_t attend_part_floats(const View &c, int nl, int n_q) {
+  if (tile_applies(c, n_q)) return tile_part_floats(c, nl, n_q);
   const long long tiles = tiles_of(c, n_q);
   if (tiles > kMaxTiles) return 0;
   const size_t pieces = (size_t)std::min(c.S, kMaxSeqs) * nl * c.H * tiles * pieces_of(c.nb);

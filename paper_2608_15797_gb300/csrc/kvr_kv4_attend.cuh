@@ -1,0 +1,87 @@
+// kvr_kv4_attend.cuh -- what the kernels of the 4-bit cache's attention share: how
+// a column (a token's query head) is addressed, and how its partial results are
+// joined and written.
+#pragma once
+
+#include "kvr_device.cuh"
+#include "kvr_internal.h"
+#include "kvr_kv4.cuh"
+#include "kvr_ptx.cuh"
+
+namespace kvr {
+namespace kv4 {
+namespace {
+
+using namespace ptx;
+
+constexpr float kNone = -1e30f; // a maximum over nothing
+constexpr float kLog2e = 1.4426950408889634f;
+
+__host__ __device__ inline int blocks_of(int len) {
+  return len > kBlock ? (len + kBlock - 1) / kBlock : 1;
+}
+
+// A whole warp's bounded wait for a phase of a barrier: one lane asks, since each
+// lane's question is a turn of its own at the barrier (230 cycles for 32 of them,
+// and all other traffic of shared memory waits behind).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
+  int ok = 1;
+  ok = mbar_wait_idle(bar, parity, abort);
+  return __all_sync(0xffffffffu, ok);
+}
+
+// Where a column's result goes.
+struct Place {
+  long long out;  // element of `out`, or -1: no such column
+  int stat;       // index of its statistics (its row in the unit)
+  int live;       // 0: no token, zeros
+};
+__device__ __forceinline__ Place place_of(const AttendParams &p, const Seqs &sq, int s, int lr,
+                                          int h, int col) {
+  const View &c = p.k.c;
+  Place a;
+  const int tok = col / c.G;
+  const size_t call = (size_t)(p.k.s0 + s) * p.k.nl + lr;
+  a.out = tok < p.n_q ? (long long)((((call * p.n_q + tok) * c.H + h) * c.G + (col - tok * c.G)) *
+                                    c.d)
+                      : -1;
+  a.stat = col;
+  a.live = tok < sq.count[s];
+  return a;
+}
+// Four channels of a finished column, normalised and written.
+template <typename O>
+__device__ __forceinline__ void finish(const AttendParams &p, const Place &a, int x, float4 o,
+                                       float top, float z, size_t unit) {
+  if (a.out < 0) return;
+  const bool live = a.live && z != 0.f;
+  const float f = live ? 1.f / z : 0.f;
+  if (!live) o = make_float4(0.f, 0.f, 0.f, 0.f);
+  o.x *= f, o.y *= f, o.z *= f, o.w *= f;
+  O *to = static_cast<O *>(p.out) + a.out + x;
+  if (sizeof(O) == 2)
+    *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+  else
+    *reinterpret_cast<float4 *>(to) = o;
+  if (x == 0) {
+    if (live && !isfinite(z)) atomicOr(p.k.c.err, ERR_NONFINITE);
+    if (p.stats)
+      reinterpret_cast<float2 *>(p.stats)[unit * (p.n_q * p.k.c.G) + a.stat] =
+          make_float2(top, f / p.k.c.G);
+  }
+}
+__device__ __forceinline__ void add4(float4 &a, const float4 &b, float f) {
+  a.x = fmaf(b.x, f, a.x), a.y = fmaf(b.y, f, a.y);
+  a.z = fmaf(b.z, f, a.z), a.w = fmaf(b.w, f, a.w);
+}
+// Adds one to *at, behind all the CTA has written before the barrier that precedes
+// it and ahead of what it reads after the one that follows.
+__device__ __forceinline__ unsigned take_ticket(unsigned *at) {
+  unsigned old;
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(at) : "memory");
+  return old;
+}
+
+}  // namespace
+}  // namespace kv4
+}  // namespace kvr

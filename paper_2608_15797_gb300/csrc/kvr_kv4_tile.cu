@@ -1,0 +1,883 @@
+// kvr_kv4_tile.cu -- attention over the 4-bit cache for more than a few query rows
+// a unit, on 5th-generation tensor cores (bf16, d = 128; kvr_kv4.cuh has the
+// cache's layout, kvr_kv4_attend.cu the kernel for fewer rows).
+//
+// Columns are (token, head) pairs of a unit, N <= 64 of them a tile, and rows the
+// 128 cached tokens of four blocks:
+//   S_j [tokens x N] = K_j Q_j^T for the two channel groups j, in tensor memory
+//   P   [tokens x N] = 2^(logit - top of the column), 16 bits, in shared memory
+//   O^T [d x N]     += V^T P, in tensor memory
+// With tokens as rows a thread of the softmax owns a token: the scales and minima
+// of its key are registers, and a column's maximum, which would need the other
+// lanes, is only checked (P must not pass 2^15): it is taken on a unit's first tile
+// and again when a logit outgrows it.  K's operand is its codes as they are
+// (half-precision subnormals, scaled back by q and s); V's is m + s c rounded to
+// half precision once, relative to the token's largest value 2^e, and the power of
+// two that takes this back goes into the token's logits.
+//
+// One CTA an SM, its warps in roles with bounded waits on mbarriers between them:
+//   8 softmax   two groups of four warps (4 x 32 tokens); one takes the even tiles,
+//               the other the odd ones, each with references, sums and an O of
+//               its own, so that one works while the other waits
+//   6 dequant   raw blocks (which they load) -> K and V operands, the tokens'
+//               constants
+//   1 issuer    the matrix products
+// As in the other kernel, CTAs take equal spans of the list of all tiles and the
+// last of those that share a unit joins their results in order.
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "kvr_kv4_attend.cuh"
+#include "kvr_tmem.cuh"
+
+namespace kvr {
+namespace kv4 {
+namespace {
+
+constexpr int kD = 128;
+constexpr int kTok = 128;                   // tokens of a tile
+constexpr int kTileBlocks = kTok / kBlock;
+constexpr int kMaxN = 64;                   // columns of a tile
+constexpr int kSoft = 8, kDeq = 6;          // warps
+constexpr int kThr = 32 * (kSoft + kDeq + 1);
+constexpr int kRing = 3;                    // raw tiles in flight
+constexpr int kTileGrid = 256;              // CTAs of a split call, at most
+constexpr uint32_t kRaw = kTileBlocks * block_bytes(kD);
+constexpr uint32_t kHalf = kTok * 128;      // one 64-element half of an operand
+constexpr uint32_t kCols = 512;             // tensor memory: S (2 x 2 x 64), O (2 x 64)
+constexpr uint32_t kColO = 256;
+constexpr float kUnit = 0x1p24f;            // of K's codes
+
+// An item's place in the list counts its tiles and, before them, kSwitch more for
+// what a CTA spends on an item whatever its length (its queries, the first
+// maxima, the result).
+constexpr int kSwitch = 5;
+struct TilePlan {
+  int32_t base[kMaxSeqs + 1];
+  int32_t span;    // of a CTA, or 0: one item a CTA
+  int32_t tiles;   // column tiles of a unit
+  int32_t cols;    // columns of a tile, a multiple of 16
+};
+
+struct __align__(16) Side {
+  float4 key[2][kTok];          // s0, s1, m0, m1 of a token's key
+  float2 val[2][kTok];          // e + 1, 2^-(e + 1) of its value
+  uint2 vc[2][2][kTok / 2];     // [.][group][pair]: s 2^(18 - e - 1), m 2^-(e + 1), halves
+  float4 qs[kMaxN / 2];         // sums of q: group 0 of two columns, group 1
+  // of the even and the odd tiles:
+  float ntop[2][kMaxN];         // minus the columns' references
+  float factor[2][kMaxN], again[2][kMaxN];
+  float wmax[2][4][kMaxN];
+  float zsum[2][4][kMaxN];
+  int limit[kMaxN];             // last row a column sees, or -1
+  float2 stat[kMaxN];
+  Place place[kMaxN];
+  float qmax[kSoft];
+  int nan_row[4][2];            // [run % 4][group]: first row whose value is NaN
+  uint64_t raw_full[kRing], kf[2], k_free, vf[2], pv[2], sf[2], s_free[2], pf[2], qf, drain;
+  uint32_t tmem;
+  int abort, flag;
+};
+
+constexpr uint32_t kOffV = 2 * kHalf, kOffP = kOffV + 4 * kHalf, kOffQ = kOffP + 2 * kHalf,
+                   kOffRaw = kOffQ + 2 * kMaxN * 128, kOffSide = kOffRaw + kRing * kRaw;
+constexpr uint32_t kSmem = kOffSide + sizeof(Side);
+static_assert(kSmem <= 227 * 1024, "shared memory");
+
+// Instruction descriptor of kind::f16 with half-precision A and B, fp32 D, A
+// K-major.
+__device__ __forceinline__ uint32_t idesc_f16(int M, int N, bool b_mn_major) {
+  return (1u << 4) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(N >> 3) << 17) |
+         ((uint32_t)(M >> 4) << 24);
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t ta, float (&v)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]),
+        "=f"(v[7])
+      : "r"(ta));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t ta, const float (&v)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(ta),
+      "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+      : "memory");
+}
+// Barrier `id` of n threads with the OR of their predicates.
+__device__ __forceinline__ bool bar_any(int id, int n, bool x) {
+  int y;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(y)
+      : "r"((int)x), "r"(id), "r"(n)
+      : "memory");
+  return y != 0;
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c,
+                                       uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t half2_bits(__half2 x) {
+  return *reinterpret_cast<const uint32_t *>(&x);
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2 *>(&x); }
+
+// A run of tiles [t0, t1) of one item; np: all it has; at: the item's place.
+struct TileRun {
+  int s, item, t0, t1, np, at;
+};
+
+struct Walk {
+  const Seqs &sq;
+  int per_seq, last;  // the end of the CTA's span
+  __device__ static int tiles_of(int nb) { return (nb + kTileBlocks - 1) / kTileBlocks; }
+  // The next item with a tile in the span.
+  __device__ bool next(TileRun &r) const {
+    r.at += kSwitch + r.np;
+    if (r.at + kSwitch >= last) return false;
+    if (++r.item == per_seq) {
+      r.item = 0;
+      ++r.s;
+      r.np = tiles_of(blocks_of(sq.len[r.s]));
+    }
+    r.t0 = 0;
+    r.t1 = min(r.np, last - r.at - kSwitch);
+    return true;
+  }
+};
+
+__global__ void __launch_bounds__(kThr, 1)
+    tile_attend_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ Seqs sq,
+                       const __grid_constant__ TilePlan plan) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char *smem = smem_raw;
+  Side &S = *reinterpret_cast<Side *>(smem + kOffSide);
+  const View &c = p.k.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int N = plan.cols;
+  const uint32_t base = smem_u32(smem);
+  volatile int *abort = &S.abort;
+  // A whole warp's bounded wait for completion n of a barrier.
+  auto wait = [&](uint64_t &bar, int n) {
+    return warp_wait(smem_u32(&bar), (uint32_t)(n & 1), abort);
+  };
+  auto give_up = [&]() {
+    if (lane == 0) {
+      if (!*abort) atomicOr(c.err, ERR_TIMEOUT);
+      *abort = 1;
+    }
+  };
+  if (warp == kSoft) tmem_alloc(smem_u32(&S.tmem), kCols);
+  if (tid == 0) {
+    for (int b = 0; b < kRing; ++b) mbar_init(smem_u32(&S.raw_full[b]), 1);
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&S.kf[b]), kDeq);
+      mbar_init(smem_u32(&S.vf[b]), kDeq);
+      mbar_init(smem_u32(&S.pv[b]), 1);
+      mbar_init(smem_u32(&S.sf[b]), 1);
+      mbar_init(smem_u32(&S.s_free[b]), kSoft / 2);
+      mbar_init(smem_u32(&S.pf[b]), 1);
+    }
+    mbar_init(smem_u32(&S.k_free), 1);
+    mbar_init(smem_u32(&S.qf), 1);
+    mbar_init(smem_u32(&S.drain), 1);
+    S.abort = 0;
+    for (int i = 0; i < 4; ++i) S.nan_row[i][0] = S.nan_row[i][1] = INT32_MAX;
+    fence_mbar_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_begin();
+  const uint32_t tm = S.tmem;
+
+  // The CTA's first run.
+  Walk walk{sq, p.k.nl * c.H * plan.tiles, 0};
+  TileRun run;
+  bool any = true;  // a short span may lie before an item's first tile
+  if (plan.span) {
+    const int from = blockIdx.x * plan.span;
+    walk.last = min(from + plan.span, plan.base[p.k.n]);
+    int lo = 0, hi = p.k.n;  // the sequence that holds the span's start
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (plan.base[mid] <= from) lo = mid; else hi = mid;
+    }
+    run.s = lo;
+    run.np = Walk::tiles_of(blocks_of(sq.len[lo]));
+    const int rest = from - plan.base[lo], cost = kSwitch + run.np;
+    run.item = rest / cost;
+    run.at = plan.base[lo] + run.item * cost;
+    run.t0 = max(0, from - run.at - kSwitch);
+    run.t1 = min(run.np, walk.last - run.at - kSwitch);
+    any = run.t1 > run.t0;
+  } else {
+    run.s = blockIdx.x / walk.per_seq;
+    run.item = blockIdx.x - run.s * walk.per_seq;
+    // no tile past the last row that the column tile's last token sees
+    const int tok = min(sq.count[run.s], ((run.item % plan.tiles + 1) * N - 1) / c.G + 1);
+    run.np = Walk::tiles_of(blocks_of(sq.len[run.s] - sq.count[run.s] + tok));
+    run.at = 0;
+    run.t0 = 0;
+    run.t1 = run.np;
+    walk.last = 0;
+  }
+  auto unit_of = [&](const TileRun &r) {
+    const int unit = r.item / plan.tiles;
+    return unit_at(c, p.k.s0 + r.s, p.k.lb, unit / c.H, unit % c.H);
+  };
+
+  if (!any) {
+    // no work
+  } else if (warp == kSoft + kDeq) {
+    // ---- issuer
+    const uint32_t id_s = idesc_f16(kTok, N, false), id_o = idesc_f16(kD, N, true);
+    const uint64_t dk = sdesc_sw128(base, 16, 1024), dq = sdesc_sw128(base + kOffQ, 16, 1024);
+    const uint64_t dv = sdesc_sw128(base + kOffV, 16, 1024);
+    const uint64_t dp = sdesc_sw128(base + kOffP, kHalf, 1024);
+    int i = 0, runs = 0;
+    bool ok = true;
+    auto issue_pv = [&](int j, bool first) {  // tile j's P and V are there
+      ok = ok && wait(S.vf[j & 1], j / 2) && wait(S.pf[j & 1], j / 2);
+      if (!ok) return;
+      tc_fence_after();
+      if (lane == 0) {
+        const uint64_t a = dv + (uint64_t)(((j & 1) * 2 * kHalf) >> 4);
+        const uint64_t b = dp + (uint64_t)(((j & 1) * kHalf) >> 4);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          tc_mma(tm + kColO + (j & 1) * 64, a + (uint64_t)(((k >> 2) * kHalf + (k & 3) * 32) >> 4),
+                 b + (uint64_t)(k * 128), id_o, !(first && k == 0));
+        tc_commit(smem_u32(&S.pv[j & 1]));
+      }
+      __syncwarp();
+    };
+    do {
+      for (int t = run.t0; t < run.t1 && ok; ++t, ++i) {
+        ok = (t > run.t0 || wait(S.qf, runs)) && wait(S.kf[i & 1], i / 2);
+        if (!ok) break;
+        tc_fence_after();
+        if (lane == 0) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              tc_mma(tm + (i & 1) * 128 + j * 64, dk + (uint64_t)((j * kHalf + k * 32) >> 4),
+                     dq + (uint64_t)((j * N * 128 + k * 32) >> 4), id_s, k > 0);
+          tc_commit(smem_u32(&S.sf[i & 1]));
+          tc_commit(smem_u32(&S.k_free));
+        }
+        __syncwarp();
+        if (t > run.t0) issue_pv(i - 1, t - 1 - run.t0 < 2);
+      }
+      if (ok) issue_pv(i - 1, run.t1 - 1 - run.t0 < 2);
+      ++runs;
+    } while (ok && walk.next(run));
+    if (!ok) give_up();
+    if (lane == 0) {  // every product is done before tensor memory is freed
+      volatile int never = 0;
+      tc_commit(smem_u32(&S.drain));
+      mbar_wait(smem_u32(&S.drain), 0, &never);
+    }
+  } else if (warp >= kSoft) {
+    // ---- dequant
+    const int dt = tid - 32 * kSoft, dw = warp - kSoft;
+    int i = 0, runs = 0;
+    bool ok = true;
+    // Loads, kRing tiles ahead: `ahead` walks before the work, and a tile's place is
+    // free once all of the role has passed the next tile's barrier.
+    TileRun ahead = run;
+    int ahead_t = run.t0, issued = 0;
+    bool more = true;
+    auto load_next = [&]() {  // dt == 0
+      if (!more) return;
+      const uint32_t bytes =
+          (uint32_t)min(kTileBlocks, blocks_of(sq.len[ahead.s]) - ahead_t * kTileBlocks) *
+          block_bytes(kD);
+      const uint32_t bar = smem_u32(&S.raw_full[issued % kRing]);
+      mbar_expect_tx(bar, bytes);
+      bulk_load(base + kOffRaw + (issued % kRing) * kRaw,
+                c.blocks + unit_of(ahead) * c.nb * (size_t)block_bytes(kD) +
+                    (size_t)ahead_t * kRaw,
+                bytes, bar);
+      ++issued;
+      if (++ahead_t == ahead.t1) {
+        more = walk.next(ahead);
+        ahead_t = ahead.t0;
+      }
+    };
+    if (dt == 0)
+      for (int j = 0; j < kRing; ++j) load_next();
+    do {
+      const int len = sq.len[run.s];
+      for (int t = run.t0; t < run.t1; ++t, ++i) {
+        const int b = i & 1, rb = i % kRing;
+        const unsigned char *raw = smem + kOffRaw + rb * kRaw;
+        const uint32_t raw_at = base + kOffRaw + rb * kRaw;
+        ok = ok && wait(S.raw_full[rb], i / kRing) && (i < 2 || wait(S.s_free[b], i / 2 - 1));
+        // Tokens' constants, a thread a token.
+        if (ok && dt < kTok) {
+          const unsigned char *blk = raw + (dt / kBlock) * block_bytes(kD);
+          const int r = dt % kBlock, row = t * kTok + dt;
+          uint2 km = *reinterpret_cast<const uint2 *>(blk + km_off(kD) + r * 8);
+          uint2 vm = *reinterpret_cast<const uint2 *>(blk + vm_off(kD) + r * 8);
+          if (row >= len) km = vm = make_uint2(0, 0);
+          S.key[b][dt] = make_float4(s_of(km.x), s_of(km.y), m_of(km.x), m_of(km.y));
+          float m[2] = {m_of(vm.x), m_of(vm.y)}, s[2] = {s_of(vm.x), s_of(vm.y)};
+          float top = 0.f;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            if (m[g] != m[g]) {  // the group stands for NaN: told to those who see it
+              atomicMin(&S.nan_row[runs & 3][g], row);
+              m[g] = s[g] = 0.f;
+            }
+            top = fmaxf(top, fmaxf(fabsf(m[g]), fabsf(fmaf(15.f, s[g], m[g]))));
+          }
+          const int e = max(-60, min((int)(__float_as_uint(top) >> 23) - 127, 120)) + 1;
+          const float down = __uint_as_float((unsigned)(127 - e) << 23);
+          S.val[b][dt] = make_float2((float)e, down);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            __half *h = reinterpret_cast<__half *>(&S.vc[b][g][dt >> 1]) + (dt & 1);
+            h[0] = __float2half_rn(s[g] * down * 0x1p18f);
+            h[2] = __float2half_rn(m[g] * down);
+          }
+        }
+        if (dt == 0 && t == run.t0) {
+          S.nan_row[(runs + 1) & 3][0] = INT32_MAX;
+          S.nan_row[(runs + 1) & 3][1] = INT32_MAX;
+        }
+        if (ok && i > 0) ok = wait(S.k_free, i - 1);
+        ok = !bar_any(1, 32 * kDeq, !ok);
+        if (!ok) break;
+        if (dt == 0 && i > 0) load_next();  // in the place of tile i - 1
+        // K: a row's chunk t4 (four words) a lane
+#pragma unroll
+        for (int z = 0; z < (16 + kDeq - 1) / kDeq; ++z) {
+          if (dw + z * kDeq >= 16) break;
+          const int x = (dw + z * kDeq) * 32 + lane, row = x >> 2, t4 = x & 3;
+          const uint4 w = *reinterpret_cast<const uint4 *>(
+              raw + (row / kBlock) * block_bytes(kD) + k_off() + (row % kBlock) * (kD / 2) +
+              t4 * 16);
+          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t y = ws[k] >> 8;
+            sts128(base + (k >> 1) * kHalf + row * 128 + (((2 * t4 + (k & 1)) ^ (row & 7)) << 4),
+                   ws[k] & 0x000F000Fu, ws[k] & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u);
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.kf[b]));
+        if (i >= 2) ok = ok && wait(S.pv[b], i / 2 - 1);
+        // V: eight tokens (tg) of chunk ch, word w, a lane
+        const uint32_t to0 = base + kOffV + b * 2 * kHalf;
+#pragma unroll
+        for (int z = 0; z < (16 + kDeq - 1) / kDeq; ++z) {
+          const int wt = dw + z * kDeq;
+          if (wt >= 16) break;
+          const int w = wt & 3, tg = (wt >> 2) * 4 + (lane >> 3), ch = lane & 7;
+          uint32_t v[4];
+          __half2 sc[4], mn[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int pr = tg * 4 + k, pb = pr % (kBlock / 2);
+            const uint32_t at = raw_at + (pr / (kBlock / 2)) * block_bytes(kD) + v_off(kD) +
+                                pb * kD + v_chunk<kD>(pb, ch) * 16 + w * 4;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[k]) : "r"(at));
+            const uint2 x = S.vc[b][w >> 1][pr];
+            sc[k] = as_half2(x.x);
+            mn[k] = as_half2(x.y);
+          }
+          const uint32_t to = to0 + (tg >> 3) * kHalf + (32 * w + ch) * 128 +
+                              (((tg & 7) ^ ch) << 4);  // ch: the row within eight
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t x = v[k];
+              const uint32_t y =
+                  (f == 0 ? x << 6 : f == 1 ? x << 2 : f == 2 ? x >> 2 : x >> 6) & 0x03C003C0u;
+              o[k] = half2_bits(__hfma2(as_half2(y), sc[k], mn[k]));  // c 2^-18
+            }
+            sts128(to + (f == 0 ? 0 : f == 1 ? 16 : f == 2 ? 8 : 24) * 128, o[0], o[1], o[2],
+                   o[3]);
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.vf[b]));
+      }
+      ++runs;
+    } while (ok && walk.next(run));
+    if (!ok) give_up();
+    if (dt == 0) {  // every copy lands before the shared memory is given back
+      volatile int never = 0;
+      for (int j = max(0, issued - kRing); j < issued; ++j)
+        mbar_wait(smem_u32(&S.raw_full[j % kRing]), (uint32_t)((j / kRing) & 1), &never);
+    }
+  } else {
+    // ---- softmax
+    const int wq = warp & 3, grp = warp >> 2;
+    const int chunks = N >> 3;
+    const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+    const int tok = wq * 32 + lane, gt = tid & 127;  // of the group's threads
+    const uint32_t prow = base + kOffP + grp * kHalf + tok * 128;
+    const uint32_t ts = tm + grp * 128 + lanes, to = tm + kColO + grp * 64 + lanes;
+    float *const ntop = S.ntop[grp], *const factor = S.factor[grp], *const anew = S.again[grp];
+    auto all_ok = [&](bool ok) { return !bar_any(2, 32 * kSoft, !ok); };
+    auto group_ok = [&](bool ok) { return !bar_any(3 + grp, 16 * kSoft, !ok); };
+    int i = 0, runs = 0;  // i: tiles before the run
+    bool ok = true, more = true;
+    do {
+      // ---- a run's queries, scaled by one power of two for all columns, and columns
+      const int unit = run.item / plan.tiles, col0 = (run.item % plan.tiles) * N;
+      const int lr = unit / c.H, h = unit % c.H;
+      const int len = sq.len[run.s], count = sq.count[run.s];
+      if (tid < N) {
+        const Place a = place_of(p, sq, run.s, lr, h, col0 + tid);
+        S.place[tid] = a;
+        S.ntop[0][tid] = S.ntop[1][tid] = -kNone;
+        S.limit[tid] = a.out >= 0 && a.live ? len - count + (col0 + tid) / c.G : -1;
+      }
+      float x[kMaxN / 16][8];
+      float top = 0.f;
+      const int ci = tid & 15;
+#pragma unroll
+      for (int z = 0; z < kMaxN / 16; ++z) {
+        const int col = (tid >> 4) + 16 * z;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[z][e] = 0.f;
+        if (col < N) {
+          const Place a = place_of(p, sq, run.s, lr, h, col0 + col);
+          if (a.out >= 0) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(
+                static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci);
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[z][2 * e] = __uint_as_float(ws[e] << 16);
+              x[z][2 * e + 1] = __uint_as_float(ws[e] & 0xFFFF0000u);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float y = fabsf(x[z][e]);
+              if (y < INFINITY) top = fmaxf(top, y);
+            }
+          }
+        }
+      }
+      top = dev::warp_max(top);
+      if (lane == 0) S.qmax[warp] = top;
+      ok = all_ok(ok);
+      if (!ok) break;
+#pragma unroll
+      for (int w = 0; w < kSoft; ++w) top = fmaxf(top, S.qmax[w]);
+      int k2 = 14 - ((int)(__float_as_uint(top) >> 23) - 127);
+      k2 = top == 0.f ? 0 : max(-90, min(k2, 100));
+      const float up = __uint_as_float((unsigned)(127 + k2) << 23);
+      const float unit_s = kUnit * __uint_as_float((unsigned)(127 - k2) << 23) * (c.scale * kLog2e);
+#pragma unroll
+      for (int z = 0; z < kMaxN / 16; ++z) {
+        const int col = (tid >> 4) + 16 * z;
+        if (16 * z >= N) break;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[z][e] *= up;
+          sum += x[z][e];
+          if (e & 1) x[z][e] *= 0.0625f;  // the odd nibbles stand for 2^4 their code
+        }
+        const uint32_t at =
+            base + kOffQ + (ci >> 3) * N * 128 + col * 128 + (((ci & 7) ^ (col & 7)) << 4);
+        sts128(at, half2_bits(__floats2half2_rn(x[z][0], x[z][4])),
+               half2_bits(__floats2half2_rn(x[z][1], x[z][5])),
+               half2_bits(__floats2half2_rn(x[z][2], x[z][6])),
+               half2_bits(__floats2half2_rn(x[z][3], x[z][7])));
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if ((ci & 7) == 0) {
+          float *q = reinterpret_cast<float *>(&S.qs[col >> 1]) + 2 * (ci >> 3) + (col & 1);
+          *q = sum * (1.f / kUnit);
+        }
+      }
+      fence_proxy_async();
+      ok = all_ok(ok);
+      if (!ok) break;
+      if (tid == 0) mbar_arrive(smem_u32(&S.qf));
+
+      // rows below `full` are seen by every column that has a token
+      const int first = col0 / c.G;
+      const int full = first < count ? len - count + first + 1 : len;
+      uint64_t z2[kMaxN / 2];
+#pragma unroll
+      for (int e = 0; e < kMaxN / 2; ++e) z2[e] = 0;
+      const int many = run.t1 - run.t0;
+      int mine = 0;  // tiles of the run that this group has taken
+      for (int t = run.t0 + ((i ^ grp) & 1); t < run.t1; t += 2, ++mine) {
+        const int n = (i + t - run.t0) >> 1, row = t * kTok + tok;  // n: the group's tiles so far
+        const bool mask = (t + 1) * kTok > full;
+        if (ok) ok = wait(S.kf[grp], n) && wait(S.sf[grp], n);
+        if (ok && n > 0) ok = wait(S.pv[grp], n - 1);  // P's place, and O's
+        tc_fence_after();
+        const float4 key = S.key[grp][tok];
+        const float2 val = S.val[grp][tok];
+        const uint64_t s0 = pk2(key.x * unit_s, key.x * unit_s);
+        const uint64_t s1 = pk2(key.y * unit_s, key.y * unit_s);
+        const uint64_t m0 = pk2(key.z * unit_s, key.z * unit_s);
+        const uint64_t m1 = pk2(key.w * unit_s, key.w * unit_s);
+        const uint64_t e2 = pk2(val.x, val.x), down2 = pk2(val.y, val.y);
+        // Logits plus e, less the reference, of column pairs 4 k .. 4 k + 3.
+        auto logits = [&](int k, bool less, const float (&a0)[8], const float (&a1)[8],
+                          uint64_t (&l)[4]) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int col = 8 * k + 2 * e;
+            const float4 q = S.qs[col >> 1];
+            const float2 nt = *reinterpret_cast<const float2 *>(&ntop[col]);
+            uint64_t y = less ? add2(pk2(nt.x, nt.y), e2) : e2;
+            y = fma2(m1, pk2(q.z, q.w), y);
+            y = fma2(m0, pk2(q.x, q.y), y);
+            y = fma2(s1, pk2(a1[2 * e], a1[2 * e + 1]), y);
+            l[e] = fma2(s0, pk2(a0[2 * e], a0[2 * e + 1]), y);
+          }
+          if (mask) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int2 lim = *reinterpret_cast<const int2 *>(&S.limit[8 * k + 2 * e]);
+              float u, v;
+              upk2(l[e], u, v);
+              l[e] = pk2(row > lim.x ? -INFINITY : u, row > lim.y ? -INFINITY : v);
+            }
+          }
+        };
+        // P of the tile against the present references; true if one is too large.
+        // `again`: the references were raised; columns whose sums hold the tile
+        // already (anew 0) stay.
+        auto probabilities = [&](bool again) {
+          __half2 most = __float2half2_rn(0.f);
+          float a0[8], a1[8];
+          tmem_ld8(ts, a0);
+          tmem_ld8(ts + 64, a1);
+#pragma unroll
+          for (int k = 0; k < kMaxN / 8; ++k) {
+            if (k < chunks) {
+              uint64_t l[4];
+              uint32_t w[4];
+              tmem_wait_ld();
+              logits(k, true, a0, a1, l);
+              if (k + 1 < chunks) {  // the next columns come while these are worked on
+                tmem_ld8(ts + 8 * k + 8, a0);
+                tmem_ld8(ts + 64 + 8 * k + 8, a1);
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float u, v;
+                upk2(l[e], u, v);
+                u = ex2(u), v = ex2(v);
+                const __half2 ph = __floats2half2_rn(u, v);
+                most = __hmax2(most, ph);
+                w[e] = half2_bits(ph);
+                uint64_t p2 = pk2(u, v);
+                if (again) {
+                  const float2 f = *reinterpret_cast<const float2 *>(&anew[8 * k + 2 * e]);
+                  p2 = mul2(p2, pk2(f.x, f.y));
+                }
+                z2[4 * k + e] = fma2(p2, down2, z2[4 * k + e]);
+              }
+              sts128(prow + ((k ^ (tok & 7)) << 4), w[0], w[1], w[2], w[3]);
+            }
+          }
+          fence_proxy_async();
+          return __hgt(__hmax(__low2half(most), __high2half(most)), __float2half_rn(32768.f));
+        };
+        bool grow = mine == 0;
+        if (ok && !grow) {
+          grow = probabilities(false);
+          tc_fence_before();
+        }
+        if (bar_any(3 + grp, 16 * kSoft, grow || !ok)) {
+          // Raise the references to the columns' maxima so far.
+          ok = group_ok(ok);
+          if (!ok) break;
+#pragma unroll 1
+          for (int k = 0; k < chunks; ++k) {
+            uint64_t l[4];
+            float a0[8], a1[8];
+            tmem_ld8(ts + 8 * k, a0);
+            tmem_ld8(ts + 64 + 8 * k, a1);
+            tmem_wait_ld();
+            logits(k, false, a0, a1, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float u[2];
+              upk2(l[e], u[0], u[1]);
+#pragma unroll
+              for (int z = 0; z < 2; ++z) {
+                const unsigned o = dev::ord_bits(u[z] == u[z] ? u[z] : -INFINITY);
+                const unsigned most = __reduce_max_sync(0xffffffffu, o);
+                if (lane == 0)
+                  S.wmax[grp][wq][8 * k + 2 * e + z] =
+                      __uint_as_float(most & 0x80000000u ? most & 0x7FFFFFFFu : ~most);
+              }
+            }
+          }
+          ok = group_ok(ok);
+          if (!ok) break;
+          if (gt < N) {
+            const float old = -ntop[gt];
+            float now = old;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) now = fmaxf(now, S.wmax[grp][w][gt]);
+            // a sum over 2^64 behind, which may have overflowed, is begun anew
+            const bool fresh = mine == 0 || now - old > 64.f;
+            factor[gt] = ex2(old - now);
+            anew[gt] = fresh ? 1.f : 0.f;
+            ntop[gt] = -now;
+          }
+          ok = group_ok(ok);
+          if (!ok) break;
+          if (mine > 0) {
+#pragma unroll
+            for (int k = 0; k < kMaxN / 8; ++k) {
+              if (k < chunks) {
+                float o[8];
+                tmem_ld8(to + 8 * k, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] *= factor[8 * k + e];
+                tmem_st8(to + 8 * k, o);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int col = 8 * k + 2 * e;
+                  const float2 f = *reinterpret_cast<const float2 *>(&factor[col]);
+                  const float2 g = *reinterpret_cast<const float2 *>(&anew[col]);
+                  float u, v;
+                  upk2(z2[4 * k + e], u, v);
+                  z2[4 * k + e] = pk2(g.x > 0.f ? 0.f : u * f.x, g.y > 0.f ? 0.f : v * f.y);
+                }
+              }
+            }
+            tmem_wait_st();
+          }
+          probabilities(true);
+          tc_fence_before();
+          ok = group_ok(ok);
+          if (!ok) break;
+        }
+        if (lane == 0) mbar_arrive(smem_u32(&S.s_free[grp]));
+        if (gt == 0) mbar_arrive(smem_u32(&S.pf[grp]));
+      }
+      // ---- the run's result: both groups'
+      const bool whole = many == run.np;
+      i += many;
+      if (ok) ok = wait(S.pv[(i - 1) & 1], (i - 1) / 2) &&
+                   (many < 2 || wait(S.pv[i & 1], (i - 2) / 2));
+      tc_fence_after();
+#pragma unroll
+      for (int e = 0; e < kMaxN / 2; ++e) {
+        if (2 * e < N) {
+          float u, v;
+          upk2(z2[e], u, v);
+          u = dev::warp_sum(u), v = dev::warp_sum(v);
+          if (lane == 0) {
+            S.zsum[grp][wq][2 * e] = u;
+            S.zsum[grp][wq][2 * e + 1] = v;
+          }
+        }
+      }
+      ok = all_ok(ok);
+      if (!ok) break;
+      if (tid < N) {
+        const float t0 = -S.ntop[0][tid], t1 = -S.ntop[1][tid], top = fmaxf(t0, t1);
+        float z[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          z[g] = (S.zsum[g][0][tid] + S.zsum[g][1][tid]) + (S.zsum[g][2][tid] + S.zsum[g][3][tid]);
+        const float f0 = ex2(t0 - top), f1 = ex2(t1 - top), zz = fmaf(z[0], f0, z[1] * f1);
+        // a whole run's factors normalise, and make zeros of a column without a token
+        const float f = !whole ? 1.f : S.place[tid].live && zz != 0.f ? 1.f / zz : 0.f;
+        S.factor[0][tid] = f0 * f;
+        S.factor[1][tid] = f1 * f;
+        S.stat[tid] = make_float2(top, zz);
+      }
+      ok = all_ok(ok);
+      if (!ok) break;
+      const size_t call_unit = ((size_t)(p.k.s0 + run.s) * p.k.nl + lr) * c.H + h;
+      // a CTA's first run may lack its beginning, its last one its end
+      const int slot = blockIdx.x * 2 + (run.t0 > 0 ? 0 : 1);
+      float *part = p.parts + (size_t)slot * N * (kD + 2);
+      const int nan_row = S.nan_row[runs & 3][wq >> 1];  // dims 32 wq .. + 31: their group
+      // a group without a tile in the run has no O
+      const bool has0 = many > 1 || ((i - 1) & 1) == 0, has1 = many > 1 || ((i - 1) & 1) == 1;
+#pragma unroll 1
+      for (int k = grp; k < chunks; k += 2) {
+        float o[8], o1[8];
+        tmem_ld8(tm + kColO + 8 * k + lanes, o);
+        tmem_ld8(tm + kColO + 64 + 8 * k + lanes, o1);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int col = 8 * k + e;
+          const float f0 = S.factor[0][col], f1 = S.factor[1][col];
+          // (a factor of 0 stands for a column without a token, or a group without
+          // a row that it sees: nothing of O counts)
+          float y = has0 && f0 != 0.f ? o[e] * f0 : 0.f;
+          if (has1 && f1 != 0.f) y = fmaf(o1[e], f1, y);
+          if (nan_row <= S.limit[col]) y = NAN;
+          if (whole) {
+            const long long out = S.place[col].out;
+            if (out >= 0) static_cast<__nv_bfloat16 *>(p.out)[out + tok] = __float2bfloat16_rn(y);
+          } else {
+            __stcg(&part[col * kD + tok], y);
+          }
+        }
+      }
+      if (whole) {
+        if (tid < N && S.place[tid].out >= 0) {
+          const float z = S.stat[tid].y;
+          const bool live = S.place[tid].live && z != 0.f;
+          if (live && !isfinite(z)) atomicOr(c.err, ERR_NONFINITE);
+          if (p.stats)
+            reinterpret_cast<float2 *>(p.stats)[call_unit * (p.n_q * c.G) + S.place[tid].stat] =
+                make_float2(S.stat[tid].x, live ? 1.f / (z * c.G) : 0.f);
+        }
+      } else {
+        if (tid < N) __stcg(reinterpret_cast<float2 *>(part + N * kD) + tid, S.stat[tid]);
+        const int i0 = run.at + kSwitch;  // the first tile's place
+        const int w0 = i0 / plan.span, w1 = (i0 + run.np - 1) / plan.span;
+        unsigned *ticket = c.ticket + unit_of(run) * kMaxTiles + run.item % plan.tiles;
+        ok = all_ok(ok);
+        if (!ok) break;
+        if (tid == 0) S.flag = take_ticket(ticket) == (unsigned)(w1 - w0);
+        ok = all_ok(ok);
+        if (!ok) break;
+        if (S.flag) {
+          if (tid == 0) *ticket = 0;
+          auto part_of = [&](int w) {
+            return p.parts + ((size_t)w * 2 + (w == w0 ? 1 : 0)) * N * (kD + 2);
+          };
+          for (int col = warp; col < N; col += kSoft) {
+            float mx = kNone, z = 0.f;
+            for (int w = w0 + lane; w <= w1; w += 32) {
+              const float2 y =
+                  __ldcg(reinterpret_cast<const float2 *>(part_of(w) + N * kD) + col);
+              const float m = fmaxf(mx, y.x);
+              z = fmaf(z, ex2(mx - m), y.y * ex2(y.x - m));
+              mx = m;
+            }
+            const float all = dev::warp_max(mx);
+            z = dev::warp_sum(z * ex2(mx - all));
+            if (lane == 0) S.stat[col] = make_float2(all, z);
+          }
+          ok = all_ok(ok);
+          if (!ok) break;
+          // a thread has N / 8 groups of four channels, kSome at a time
+          constexpr int kSome = 2;
+          for (int j0 = 0; 8 * j0 < N; j0 += kSome) {
+            float4 sum[kSome];
+            float mx[kSome];
+#pragma unroll
+            for (int j = 0; j < kSome; ++j) {
+              sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+              mx[j] = S.stat[(tid + (j0 + j) * 32 * kSoft) * 4 / kD].x;
+            }
+#pragma unroll 4
+            for (int w = w0; w <= w1; ++w) {
+              const float *from = part_of(w);
+#pragma unroll
+              for (int j = 0; j < kSome; ++j) {
+                const int at = tid + (j0 + j) * 32 * kSoft;
+                add4(sum[j], __ldcg(reinterpret_cast<const float4 *>(from) + at),
+                     ex2(__ldcg(from + N * kD + 2 * (at * 4 / kD)) - mx[j]));
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < kSome; ++j) {
+              const int at = 4 * (tid + (j0 + j) * 32 * kSoft), col = at / kD;
+              finish<__nv_bfloat16>(p, S.place[col], at % kD, sum[j], S.stat[col].x,
+                                    S.stat[col].y, call_unit);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      ok = all_ok(ok);  // the columns' arrays are free again
+      if (!ok) break;
+      ++runs;
+      more = walk.next(run);
+    } while (more);
+    if (!ok) give_up();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kSoft) tmem_dealloc(tm, kCols);
+}
+
+int tile_n(const View &c, int n_q) {
+  const long long rows = (long long)n_q * c.G, tiles = (rows + kMaxN - 1) / kMaxN;
+  return (int)(((rows + tiles - 1) / tiles + 15) / 16 * 16);
+}
+long long col_tiles(const View &c, int n_q) {
+  return ((long long)n_q * c.G + tile_n(c, n_q) - 1) / tile_n(c, n_q);
+}
+
+}  // namespace
+
+bool tile_applies(const View &c, int n_q) {
+  return c.d == kD && c.io_bf16 && c.out_bf16 && (long long)n_q * c.G > 8;
+}
+
+size_t tile_part_floats(const View &c, int nl, int n_q) {
+  const long long tiles = col_tiles(c, n_q);
+  if (tiles > kMaxTiles) return 0;
+  const size_t all = (size_t)std::min(c.S, kMaxSeqs) * nl * c.H * tiles *
+                     ((c.nb + kTileBlocks - 1) / kTileBlocks);
+  return 2 * std::min<size_t>(kTileGrid, all) * tile_n(c, n_q) * (kD + 2);
+}
+
+cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+  const View &c = p.k.c;
+  static int sms = 0;
+  if (!sms) {
+    int dev = 0, n = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(tile_attend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               kSmem);
+    if (e != cudaSuccess) return e;
+    sms = std::min(n, kTileGrid);
+  }
+  TilePlan plan;
+  const long long tiles = col_tiles(c, p.n_q), per_seq = (long long)p.k.nl * c.H * tiles;
+  if (tiles > INT32_MAX || per_seq > INT32_MAX) return cudaErrorInvalidValue;
+  plan.tiles = (int)tiles;
+  plan.cols = tile_n(c, p.n_q);
+  long long total = 0;
+  for (int i = 0; i < p.k.n; ++i) {
+    plan.base[i] = (int32_t)total;
+    total += per_seq * (kSwitch + (blocks_of(q.len[i]) + kTileBlocks - 1) / kTileBlocks);
+  }
+  plan.base[p.k.n] = (int32_t)total;
+  long long grid;
+  if (tiles <= kMaxTiles && total <= INT32_MAX) {
+    plan.span = (int32_t)std::max<long long>(kSwitch + 1, (total + sms - 1) / sms);
+    grid = (total + plan.span - 1) / plan.span;
+  } else {
+    plan.span = 0;
+    grid = per_seq * p.k.n;
+  }
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  return launch_pdl(tile_attend_kernel, dim3((unsigned)grid), dim3(kThr), kSmem, stream, p, q,
+                    plan);
+}
+
+}  // namespace kv4
+}  // namespace kvr
