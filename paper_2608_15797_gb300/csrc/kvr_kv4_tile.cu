@@ -58,7 +58,6 @@ struct TilePlan {
   int32_t base[kMaxSeqs + 1];
   int32_t span;    // of a CTA, or 0: one item a CTA
   int32_t tiles;   // column tiles of a unit
-  int32_t cols;    // columns of a tile, a multiple of 16
 };
 
 struct __align__(16) Side {
@@ -116,10 +115,15 @@ __device__ __forceinline__ bool bar_any(int id, int n, bool x) {
       : "memory");
   return y != 0;
 }
+// Operands are written for the tensor cores alone, and a fence that orders memory
+// follows: no clobber here, so that loads may run ahead of these stores.
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c,
                                        uint32_t d) {
-  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
-               : "memory");
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d));
+}
+// As tmem_wait_ld, but other loads may pass it.
+__device__ __forceinline__ void tmem_landed() {
+  asm volatile("tcgen05.wait::ld.sync.aligned;");
 }
 __device__ __forceinline__ uint32_t half2_bits(__half2 x) {
   return *reinterpret_cast<const uint32_t *>(&x);
@@ -150,6 +154,8 @@ struct Walk {
   }
 };
 
+// CH: groups of eight columns of a tile.
+template <int CH>
 __global__ void __launch_bounds__(kThr, 1)
     tile_attend_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ Seqs sq,
                        const __grid_constant__ TilePlan plan) {
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(kThr, 1)
   Side &S = *reinterpret_cast<Side *>(smem + kOffSide);
   const View &c = p.k.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int N = plan.cols;
+  constexpr int N = 8 * CH;
   const uint32_t base = smem_u32(smem);
   volatile int *abort = &S.abort;
   // A whole warp's bounded wait for completion n of a barrier.
@@ -425,7 +431,6 @@ __global__ void __launch_bounds__(kThr, 1)
   } else {
     // ---- softmax
     const int wq = warp & 3, grp = warp >> 2;
-    const int chunks = N >> 3;
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     const int tok = wq * 32 + lane, gt = tid & 127;  // of the group's threads
     const uint32_t prow = base + kOffP + grp * kHalf + tok * 128;
@@ -446,30 +451,28 @@ __global__ void __launch_bounds__(kThr, 1)
         S.ntop[0][tid] = S.ntop[1][tid] = -kNone;
         S.limit[tid] = a.out >= 0 && a.live ? len - count + (col0 + tid) / c.G : -1;
       }
-      float x[kMaxN / 16][8];
+      float x[CH / 2][8];
       float top = 0.f;
       const int ci = tid & 15;
 #pragma unroll
-      for (int z = 0; z < kMaxN / 16; ++z) {
+      for (int z = 0; z < CH / 2; ++z) {
         const int col = (tid >> 4) + 16 * z;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[z][e] = 0.f;
-        if (col < N) {
-          const Place a = place_of(p, sq, run.s, lr, h, col0 + col);
-          if (a.out >= 0) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(
-                static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci);
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+        const Place a = place_of(p, sq, run.s, lr, h, col0 + col);
+        if (a.out >= 0) {
+          const uint4 w = *reinterpret_cast<const uint4 *>(
+              static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci);
+          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              x[z][2 * e] = __uint_as_float(ws[e] << 16);
-              x[z][2 * e + 1] = __uint_as_float(ws[e] & 0xFFFF0000u);
-            }
+          for (int e = 0; e < 4; ++e) {
+            x[z][2 * e] = __uint_as_float(ws[e] << 16);
+            x[z][2 * e + 1] = __uint_as_float(ws[e] & 0xFFFF0000u);
+          }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float y = fabsf(x[z][e]);
-              if (y < INFINITY) top = fmaxf(top, y);
-            }
+          for (int e = 0; e < 8; ++e) {
+            const float y = fabsf(x[z][e]);
+            if (y < INFINITY) top = fmaxf(top, y);
           }
         }
       }
@@ -484,9 +487,8 @@ __global__ void __launch_bounds__(kThr, 1)
       const float up = __uint_as_float((unsigned)(127 + k2) << 23);
       const float unit_s = kUnit * __uint_as_float((unsigned)(127 - k2) << 23) * (c.scale * kLog2e);
 #pragma unroll
-      for (int z = 0; z < kMaxN / 16; ++z) {
+      for (int z = 0; z < CH / 2; ++z) {
         const int col = (tid >> 4) + 16 * z;
-        if (16 * z >= N) break;
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -515,9 +517,9 @@ __global__ void __launch_bounds__(kThr, 1)
       // rows below `full` are seen by every column that has a token
       const int first = col0 / c.G;
       const int full = first < count ? len - count + first + 1 : len;
-      uint64_t z2[kMaxN / 2];
+      uint64_t z2[4 * CH];
 #pragma unroll
-      for (int e = 0; e < kMaxN / 2; ++e) z2[e] = 0;
+      for (int e = 0; e < 4 * CH; ++e) z2[e] = 0;
       const int many = run.t1 - run.t0;
       int mine = 0;  // tiles of the run that this group has taken
       for (int t = run.t0 + ((i ^ grp) & 1); t < run.t1; t += 2, ++mine) {
@@ -566,33 +568,31 @@ __global__ void __launch_bounds__(kThr, 1)
           tmem_ld8(ts, a0);
           tmem_ld8(ts + 64, a1);
 #pragma unroll
-          for (int k = 0; k < kMaxN / 8; ++k) {
-            if (k < chunks) {
-              uint64_t l[4];
-              uint32_t w[4];
-              tmem_wait_ld();
-              logits(k, true, a0, a1, l);
-              if (k + 1 < chunks) {  // the next columns come while these are worked on
-                tmem_ld8(ts + 8 * k + 8, a0);
-                tmem_ld8(ts + 64 + 8 * k + 8, a1);
-              }
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float u, v;
-                upk2(l[e], u, v);
-                u = ex2(u), v = ex2(v);
-                const __half2 ph = __floats2half2_rn(u, v);
-                most = __hmax2(most, ph);
-                w[e] = half2_bits(ph);
-                uint64_t p2 = pk2(u, v);
-                if (again) {
-                  const float2 f = *reinterpret_cast<const float2 *>(&anew[8 * k + 2 * e]);
-                  p2 = mul2(p2, pk2(f.x, f.y));
-                }
-                z2[4 * k + e] = fma2(p2, down2, z2[4 * k + e]);
-              }
-              sts128(prow + ((k ^ (tok & 7)) << 4), w[0], w[1], w[2], w[3]);
+          for (int k = 0; k < CH; ++k) {
+            uint64_t l[4];
+            uint32_t w[4];
+            tmem_landed();
+            logits(k, true, a0, a1, l);
+            if (k + 1 < CH) {  // the next columns come while these are worked on
+              tmem_ld8(ts + 8 * k + 8, a0);
+              tmem_ld8(ts + 64 + 8 * k + 8, a1);
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float u, v;
+              upk2(l[e], u, v);
+              u = ex2(u), v = ex2(v);
+              const __half2 ph = __floats2half2_rn(u, v);
+              most = __hmax2(most, ph);
+              w[e] = half2_bits(ph);
+              uint64_t p2 = pk2(u, v);
+              if (again) {
+                const float2 f = *reinterpret_cast<const float2 *>(&anew[8 * k + 2 * e]);
+                p2 = mul2(p2, pk2(f.x, f.y));
+              }
+              z2[4 * k + e] = fma2(p2, down2, z2[4 * k + e]);
+            }
+            sts128(prow + ((k ^ (tok & 7)) << 4), w[0], w[1], w[2], w[3]);
           }
           fence_proxy_async();
           return __hgt(__hmax(__low2half(most), __high2half(most)), __float2half_rn(32768.f));
@@ -607,7 +607,7 @@ __global__ void __launch_bounds__(kThr, 1)
           ok = group_ok(ok);
           if (!ok) break;
 #pragma unroll 1
-          for (int k = 0; k < chunks; ++k) {
+          for (int k = 0; k < CH; ++k) {
             uint64_t l[4];
             float a0[8], a1[8];
             tmem_ld8(ts + 8 * k, a0);
@@ -645,23 +645,21 @@ __global__ void __launch_bounds__(kThr, 1)
           if (!ok) break;
           if (mine > 0) {
 #pragma unroll
-            for (int k = 0; k < kMaxN / 8; ++k) {
-              if (k < chunks) {
-                float o[8];
-                tmem_ld8(to + 8 * k, o);
-                tmem_wait_ld();
+            for (int k = 0; k < CH; ++k) {
+              float o[8];
+              tmem_ld8(to + 8 * k, o);
+              tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] *= factor[8 * k + e];
-                tmem_st8(to + 8 * k, o);
+              for (int e = 0; e < 8; ++e) o[e] *= factor[8 * k + e];
+              tmem_st8(to + 8 * k, o);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int col = 8 * k + 2 * e;
-                  const float2 f = *reinterpret_cast<const float2 *>(&factor[col]);
-                  const float2 g = *reinterpret_cast<const float2 *>(&anew[col]);
-                  float u, v;
-                  upk2(z2[4 * k + e], u, v);
-                  z2[4 * k + e] = pk2(g.x > 0.f ? 0.f : u * f.x, g.y > 0.f ? 0.f : v * f.y);
-                }
+              for (int e = 0; e < 4; ++e) {
+                const int col = 8 * k + 2 * e;
+                const float2 f = *reinterpret_cast<const float2 *>(&factor[col]);
+                const float2 g = *reinterpret_cast<const float2 *>(&anew[col]);
+                float u, v;
+                upk2(z2[4 * k + e], u, v);
+                z2[4 * k + e] = pk2(g.x > 0.f ? 0.f : u * f.x, g.y > 0.f ? 0.f : v * f.y);
               }
             }
             tmem_wait_st();
@@ -681,15 +679,13 @@ __global__ void __launch_bounds__(kThr, 1)
                    (many < 2 || wait(S.pv[i & 1], (i - 2) / 2));
       tc_fence_after();
 #pragma unroll
-      for (int e = 0; e < kMaxN / 2; ++e) {
-        if (2 * e < N) {
-          float u, v;
-          upk2(z2[e], u, v);
-          u = dev::warp_sum(u), v = dev::warp_sum(v);
-          if (lane == 0) {
-            S.zsum[grp][wq][2 * e] = u;
-            S.zsum[grp][wq][2 * e + 1] = v;
-          }
+      for (int e = 0; e < 4 * CH; ++e) {
+        float u, v;
+        upk2(z2[e], u, v);
+        u = dev::warp_sum(u), v = dev::warp_sum(v);
+        if (lane == 0) {
+          S.zsum[grp][wq][2 * e] = u;
+          S.zsum[grp][wq][2 * e + 1] = v;
         }
       }
       ok = all_ok(ok);
@@ -717,7 +713,7 @@ __global__ void __launch_bounds__(kThr, 1)
       // a group without a tile in the run has no O
       const bool has0 = many > 1 || ((i - 1) & 1) == 0, has1 = many > 1 || ((i - 1) & 1) == 1;
 #pragma unroll 1
-      for (int k = grp; k < chunks; k += 2) {
+      for (int k = grp; k < CH; k += 2) {
         float o[8], o1[8];
         tmem_ld8(tm + kColO + 8 * k + lanes, o);
         tmem_ld8(tm + kColO + 64 + 8 * k + lanes, o1);
@@ -842,16 +838,17 @@ size_t tile_part_floats(const View &c, int nl, int n_q) {
   return 2 * std::min<size_t>(kTileGrid, all) * tile_n(c, n_q) * (kD + 2);
 }
 
-cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+template <int CH>
+cudaError_t launch_ch(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
   const View &c = p.k.c;
+  auto kern = tile_attend_kernel<CH>;
   static int sms = 0;
   if (!sms) {
     int dev = 0, n = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(tile_attend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               kSmem);
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     sms = std::min(n, kTileGrid);
   }
@@ -859,7 +856,6 @@ cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_
   const long long tiles = col_tiles(c, p.n_q), per_seq = (long long)p.k.nl * c.H * tiles;
   if (tiles > INT32_MAX || per_seq > INT32_MAX) return cudaErrorInvalidValue;
   plan.tiles = (int)tiles;
-  plan.cols = tile_n(c, p.n_q);
   long long total = 0;
   for (int i = 0; i < p.k.n; ++i) {
     plan.base[i] = (int32_t)total;
@@ -875,8 +871,16 @@ cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_
     grid = per_seq * p.k.n;
   }
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  return launch_pdl(tile_attend_kernel, dim3((unsigned)grid), dim3(kThr), kSmem, stream, p, q,
-                    plan);
+  return launch_pdl(kern, dim3((unsigned)grid), dim3(kThr), kSmem, stream, p, q, plan);
+}
+
+cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+  switch (tile_n(p.k.c, p.n_q)) {
+    case 16: return launch_ch<2>(p, q, stream);
+    case 32: return launch_ch<4>(p, q, stream);
+    case 48: return launch_ch<6>(p, q, stream);
+    default: return launch_ch<8>(p, q, stream);
+  }
 }
 
 }  // namespace kv4
