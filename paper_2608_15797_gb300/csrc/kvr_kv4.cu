@@ -21,90 +21,156 @@ namespace kvr {
 namespace kv4 {
 namespace {
 
+// Eight channels of a row and side are a lane's share, as they lie in a word of
+// codes: lane i has channels 8 i .. 8 i + 7 of a key, and of a value the pairs
+// (p, p + 1), p = 32 (i / 4) + 2 (i % 4) + {0, 16, 8, 24}, the first of each pair
+// first.
 template <typename T>
-struct Eight {  // eight channels in memory
-  uint4 w[sizeof(T) / 2];
+struct Eight {
+  uint32_t w[2 * sizeof(T)];
 };
-__device__ __forceinline__ void widen(const Eight<float> &a, float (&x)[8]) {
+__device__ __forceinline__ int pair_channel(int i, int f) {
+  return 32 * (i >> 2) + 2 * (i & 3) + (f == 0 ? 0 : f == 1 ? 16 : f == 2 ? 8 : 24);
+}
+template <typename T>
+__device__ __forceinline__ Eight<T> load_eight(const T *row, int side, int i) {
+  Eight<T> a;
+  if (side) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    x[4 * i] = __uint_as_float(a.w[i].x), x[4 * i + 1] = __uint_as_float(a.w[i].y);
-    x[4 * i + 2] = __uint_as_float(a.w[i].z), x[4 * i + 3] = __uint_as_float(a.w[i].w);
+    for (int f = 0; f < 4; ++f) {
+      const T *at = row + pair_channel(i, f);
+      if (sizeof(T) == 2) {
+        a.w[f] = __ldcs(reinterpret_cast<const uint32_t *>(at));
+      } else {
+        const uint2 x = __ldcs(reinterpret_cast<const uint2 *>(at));
+        a.w[2 * f % (2 * sizeof(T))] = x.x, a.w[(2 * f + 1) % (2 * sizeof(T))] = x.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int z = 0; z < (int)sizeof(T) / 2; ++z) {
+      const uint4 x = __ldcs(reinterpret_cast<const uint4 *>(row + 8 * i) + z);
+      a.w[4 * z] = x.x, a.w[4 * z + 1] = x.y, a.w[4 * z + 2] = x.z, a.w[4 * z + 3] = x.w;
+    }
+  }
+  return a;
+}
+// In the order of a word's nibbles.
+__device__ __forceinline__ void widen(const Eight<__nv_bfloat16> &a, int side, float (&x)[8]) {
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const float lo = __uint_as_float(a.w[f] << 16), hi = __uint_as_float(a.w[f] & 0xFFFF0000u);
+    x[side ? f : 2 * f] = lo;
+    x[side ? 4 + f : 2 * f + 1] = hi;
   }
 }
-__device__ __forceinline__ void widen(const Eight<__nv_bfloat16> &a, float (&x)[8]) {
-  const uint32_t w[4] = {a.w[0].x, a.w[0].y, a.w[0].z, a.w[0].w};
+__device__ __forceinline__ void widen(const Eight<float> &a, int side, float (&x)[8]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  for (int f = 0; f < 4; ++f) {
+    x[side ? f : 2 * f] = __uint_as_float(a.w[2 * f]);
+    x[side ? 4 + f : 2 * f + 1] = __uint_as_float(a.w[2 * f + 1]);
   }
 }
-__device__ __forceinline__ void narrow(const float (&x)[8], Eight<float> &a) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    a.w[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]),
-                        __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
-}
-__device__ __forceinline__ void narrow(const float (&x)[8], Eight<__nv_bfloat16> &a) {
-  a.w[0] = make_uint4(ptx::pack_bf16(x[0], x[1]), ptx::pack_bf16(x[2], x[3]),
-                      ptx::pack_bf16(x[4], x[5]), ptx::pack_bf16(x[6], x[7]));
-}
-
-// The codes of eight values as one word, code e in bits 4 e .. 4 e + 3.  A product
-// with 1 / s finds a code unless it lies within 2e-5 of half-way between two (the
-// product is off by less than 2^-21 of 15); those few are divided.
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], uint32_t meta, bool flat) {
-  const float m = m_of(meta), r = ptx::rcp(s_of(meta));
-  uint32_t w = 0;
-  float off = 0.f;
+// The least and the greatest of the eight; true if one is not finite.
+__device__ __forceinline__ bool extremes(const Eight<float> &, const float (&x)[8], float &lo,
+                                         float &hi) {
+  float odd = 0.f;
+  lo = hi = x[0];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float q = fminf(fmaxf(__fmul_rn(__fsub_rn(x[e], m), r), 0.f), 15.f);
-    const float k = __fadd_rn(q, 12582912.f);  // 1.5 2^23: the code in the low bits
-    off = fmaxf(off, fabsf(__fsub_rn(q, __fsub_rn(k, 12582912.f))));
-    w |= (__float_as_uint(k) & 15u) << (4 * e);
+    lo = fminf(lo, x[e]);
+    hi = fmaxf(hi, x[e]);
+    odd = fmaf(x[e], 0.f, odd);  // NaN for what is not finite
   }
-  // a scale that is nearly subnormal has no reciprocal, and a huge one flushes
-  if (off > 0.49998f || !(r < 1e37f && r > 1e-37f)) {
-    w = 0;
+  return odd != 0.f;
+}
+__device__ __forceinline__ bool extremes(const Eight<__nv_bfloat16> &a, const float (&)[8],
+                                         float &lo, float &hi) {
+  __nv_bfloat162 w[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w |= code_of(x[e], meta, flat) << (4 * e);
+  for (int f = 0; f < 4; ++f) w[f] = *reinterpret_cast<const __nv_bfloat162 *>(&a.w[f]);
+  const __nv_bfloat162 least = __hmin2(__hmin2(w[0], w[1]), __hmin2(w[2], w[3]));
+  const __nv_bfloat162 most = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+  const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+  __nv_bfloat162 odd = __hfma2(w[0], zero, zero);
+#pragma unroll
+  for (int f = 1; f < 4; ++f) odd = __hfma2(w[f], zero, odd);
+  lo = fminf(__low2float(least), __high2float(least));
+  hi = fmaxf(__low2float(most), __high2float(most));
+  return (*reinterpret_cast<const uint32_t *>(&odd) & 0x7FFF7FFFu) != 0;
+}
+__device__ __forceinline__ void store_eight(const float (&x)[8], int side, int i,
+                                            __nv_bfloat16 *row) {
+  if (side) {
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      *reinterpret_cast<uint32_t *>(row + pair_channel(i, f)) = ptx::pack_bf16(x[f], x[4 + f]);
+  } else {
+    *reinterpret_cast<uint4 *>(row + 8 * i) =
+        make_uint4(ptx::pack_bf16(x[0], x[1]), ptx::pack_bf16(x[2], x[3]),
+                   ptx::pack_bf16(x[4], x[5]), ptx::pack_bf16(x[6], x[7]));
   }
-  return flat ? 0 : w;
+}
+__device__ __forceinline__ void store_eight(const float (&x)[8], int side, int i, float *row) {
+  if (side) {
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      *reinterpret_cast<float2 *>(row + pair_channel(i, f)) = make_float2(x[f], x[4 + f]);
+  } else {
+    reinterpret_cast<float4 *>(row + 8 * i)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4 *>(row + 8 * i)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
 }
 
-// Between a word of eight neighbouring channels' codes of a row and V's halves:
-// the four lanes of 32 channels hold channels 8 y .. 8 y + 7, and lane y ends up
-// with the halves of c = 2 y (low) and 2 y + 1, whose nibbles are c + {0, 16, 8,
-// 24}.  The same exchange takes the halves back.
-__device__ __forceinline__ uint32_t to_halves(uint32_t w) {
-  const int y = threadIdx.x & 3;
-  uint32_t z = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t v = i == 0 ? w : __shfl_xor_sync(0xffffffffu, w, i);
-    const int from = y ^ i;  // the lane that v comes from: channels 8 from + c
-    const int f = 4 * (((from & 1) << 1) | (from >> 1));
-    z |= ((v >> (8 * y)) & 15u) << f;
-    z |= ((v >> (8 * y + 4)) & 15u) << (16 + f);
-  }
-  return z;
-}
-__device__ __forceinline__ uint32_t from_halves(uint32_t z) {
-  const int y = threadIdx.x & 3, f = 4 * (((y & 1) << 1) | (y >> 1));
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t v = i == 0 ? z : __shfl_xor_sync(0xffffffffu, z, i);
-    const int from = y ^ i;  // channels c = 2 from, 2 from + 1
-    w |= ((v >> f) & 15u) << (8 * from);
-    w |= ((v >> (16 + f)) & 15u) << (8 * from + 4);
-  }
-  return w;
+// A code by the definition's division.  Not inlined: with its divisions in every
+// round the kernel outgrew the instruction cache (append of 2 x 8,191 tokens: 309 us
+// against 226).
+__device__ __noinline__ uint32_t divided_code(float x, uint32_t meta) {
+  return code_of(x, meta, false);
 }
 
-// Where a lane that holds channels 8 i .. 8 i + 7 of row r finds or puts them.
+// The codes of eight values as one word, code e in bits 4 e .. 4 e + 3.  x r - m r
+// (r about 1 / s, m / s at most 64) is off by less than 2e-5, so it finds a code
+// unless it lies that near to half-way between two (of bf16 values one in 450 lies
+// exactly there), and it stays within -0.2 and 15.3, so that nothing needs to be
+// cut to 0..15; the rest is divided.
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], uint32_t meta, bool flat) {
+  using namespace ptx;
+  const float m = m_of(meta), r = rcp(s_of(meta)), mr = m * r;
+  const uint64_t r2 = pk2(r, r), d2 = pk2(-mr, -mr), magic = pk2(12582912.f, 12582912.f);
+  const uint64_t minus = pk2(-12582912.f, -12582912.f), neg = pk2(-1.f, -1.f);
+  uint32_t k[8];
+  float d[8], off = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const uint64_t q = fma2(pk2(x[e], x[e + 1]), r2, d2);
+    const uint64_t t = add2(q, magic);  // 1.5 2^23: the code in the low bits
+    float a, b;
+    upk2(fma2(add2(t, minus), neg, q), d[e], d[e + 1]);
+    off = fmaxf(off, fmaxf(fabsf(d[e]), fabsf(d[e + 1])));
+    upk2(t, a, b);
+    k[e] = __float_as_uint(a), k[e + 1] = __float_as_uint(b);
+  }
+  constexpr float kNear = 0.49996f;
+  // (a scale that is nearly subnormal has no reciprocal, and a huge one flushes)
+  const bool all = !(fabsf(mr) < 64.f) || !(r < 1e37f && r > 1e-37f);
+  if (!(off < kNear) || all) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!(fabsf(d[e]) < kNear) || all) k[e] = divided_code(x[e], meta);
+  }
+  // low bytes, two codes a byte
+  uint32_t z[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t y = __byte_perm(__byte_perm(k[4 * h], k[4 * h + 1], 0x0040),
+                                   __byte_perm(k[4 * h + 2], k[4 * h + 3], 0x0040), 0x5410);
+    z[h] = y | (y >> 4);
+  }
+  return flat ? 0 : __byte_perm(z[0], z[1], 0x6420);
+}
+
+// Where the lane finds or puts them.
 template <int D>
 __device__ __forceinline__ uint32_t *k_word(uint8_t *block, int r, int i) {
   int hi;
@@ -120,6 +186,24 @@ __device__ __forceinline__ uint32_t *meta_word(uint8_t *block, int side, int r, 
                                       (r * (D / kGroup) + (i >> 3)) * 4);
 }
 
+// Which (unit, side, token group) a warp of a launch over units x groups x 2 is.
+struct Task {
+  int s, lr, h, side, group;
+  bool any;
+};
+__device__ __forceinline__ Task task_of(const Call &k, int groups) {
+  Task t;
+  const unsigned w = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const unsigned unit = (w >> 1) / (unsigned)groups;
+  t.s = blockIdx.y;
+  t.side = (int)(w & 1);
+  t.group = (int)((w >> 1) - unit * groups);
+  t.lr = (int)(unit / (unsigned)k.c.H);
+  t.h = (int)(unit - (unsigned)t.lr * k.c.H);
+  t.any = t.lr < k.nl;
+  return t;
+}
+
 // Quantise the new rows.  D / 8 lanes a row, eight channels a lane; a warp takes
 // kRows rows of one side (key or value) at a time, their loads in flight together.
 // Bound by the bytes read and written where tokens are many, else by latency.
@@ -130,78 +214,68 @@ struct Append {
   static constexpr int kRounds = 4;
   static constexpr int kRows = kOnce * kRounds;    // rows of a warp
 };
-template <typename T, int D>
-__global__ void __launch_bounds__(256)
-    append_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q, int tokens,
-                  const T *key, const T *val, RowStrides st) {
-  pdl_begin();
+template <typename T, int D, int SIDE>
+__device__ __forceinline__ void append_rows(const Call &k, const Seqs &q, const Task &at,
+                                            const T *src, long long token_stride) {
   using A = Append<T, D>;
   const View &c = k.c;
   const int lane = threadIdx.x & 31, i = lane % A::kLanes;
-  // a warp: (sequence, layer, head), side, kRows tokens
-  const int groups = (tokens + A::kRows - 1) / A::kRows;
-  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int side = (int)(w & 1);
-  const int tg = (int)((w >> 1) % groups);
-  const long long unit = (w >> 1) / groups;
-  const int h = (int)(unit % c.H), lr = (int)(unit / c.H % k.nl);
-  const long long s = unit / c.H / k.nl;
-  if (s >= k.n) return;
-  const int count = q.count[s], t0 = tg * A::kRows;
-  if (t0 >= count) return;
-  const T *src = (side ? val : key) + (s + k.s0) * st.seq + lr * st.layer + h * st.head + 8 * i;
+  const int count = q.count[at.s], t0 = at.group * A::kRows;
   Eight<T> in[A::kRounds];
 #pragma unroll
   for (int n = 0; n < A::kRounds; ++n) {
     const int t = min(t0 + n * A::kOnce + lane / A::kLanes, count - 1);
-    const uint4 *at = reinterpret_cast<const uint4 *>(src + t * st.token);
-#pragma unroll
-    for (int e = 0; e < (int)sizeof(T) / 2; ++e) in[n].w[e] = __ldcs(at + e);
+    in[n] = load_eight(src + t * token_stride, SIDE, i);
   }
-  const size_t u = unit_at(c, k.s0 + (int)s, k.lb, lr, h);
-  const int r0 = q.len[s] - count;
+  const size_t u = unit_at(c, k.s0 + at.s, k.lb, at.lr, at.h);
+  const int r0 = q.len[at.s] - count;
 #pragma unroll
   for (int n = 0; n < A::kRounds; ++n) {
     if (t0 + n * A::kOnce >= count) break;
     const int t = t0 + n * A::kOnce + lane / A::kLanes;
-    float x[8];
-    widen(in[n], x);
-    float lo = x[0], hi = x[0], odd = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      lo = fminf(lo, x[e]);
-      hi = fmaxf(hi, x[e]);
-      odd = fmaf(x[e], 0.f, odd);  // NaN for what is not finite
-    }
+    float x[8], lo, hi;
+    widen(in[n], SIDE, x);
+    const bool odd = extremes(in[n], x, lo, hi);
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) {  // the eight lanes of a group
       lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
       hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
-    const unsigned bad = __ballot_sync(0xffffffffu, odd != 0.f);
+    const unsigned bad = __ballot_sync(0xffffffffu, odd);
     bool flat;
     const uint32_t meta =
         group_meta(lo, hi, ((bad >> (lane & ~7)) & 255u) == 0, flat);
-    uint32_t word = codes_of(x, meta, flat);
-    if (side) word = to_halves(word);
+    const uint32_t word = codes_of(x, meta, flat);
     if (t < count) {
       const int r = r0 + t, rb = r % kBlock;
       uint8_t *block = block_at(c, u, r);
-      if (side) {
+      if (SIDE) {
         const int y = i & 3;
         *v_half_at<D>(block, rb, i, 2 * y) = (uint16_t)word;
         *v_half_at<D>(block, rb, i, 2 * y + 1) = (uint16_t)(word >> 16);
       } else {
         *k_word<D>(block, rb, i) = word;
       }
-      if (i % 8 == 0) *meta_word<D>(block, side, rb, i) = meta;
-      if (side == 0 && i == 0) c.score[u * c.sstride + r] = 0.f;
+      if (i % 8 == 0) *meta_word<D>(block, SIDE, rb, i) = meta;
+      if (SIDE == 0 && i == 0) c.score[u * c.sstride + r] = 0.f;
     }
   }
 }
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+    append_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q, int groups,
+                  const T *key, const T *val, RowStrides st) {
+  pdl_begin();
+  const Task at = task_of(k, groups);
+  if (!at.any || at.group * Append<T, D>::kRows >= q.count[at.s]) return;
+  const long long from = (at.s + k.s0) * st.seq + at.lr * st.layer + at.h * st.head;
+  if (at.side)
+    append_rows<T, D, 1>(k, q, at, val + from, st.token);
+  else
+    append_rows<T, D, 0>(k, q, at, key + from, st.token);
+}
 
-// The codes and (m, s) of channels 8 i .. 8 i + 7 of row r of a block (V's codes
-// as halves), and what they stand for.  All lanes call word_values.
+// The lane's word of codes and its (m, s), and what they stand for.
 struct RowWords {
   uint32_t w, meta;
 };
@@ -219,54 +293,48 @@ __device__ __forceinline__ RowWords row_words(const uint8_t *block, int side, in
   x.meta = *meta_word<D>(at, side, r, i);
   return x;
 }
-__device__ __forceinline__ void word_values(const RowWords &a, int side, float (&x)[8]) {
-  const uint32_t w = side ? from_halves(a.w) : a.w;
+__device__ __forceinline__ void word_values(const RowWords &a, float (&x)[8]) {
+  const float m = m_of(a.meta), s = s_of(a.meta);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = value_of((w >> (4 * e)) & 15u, a.meta);
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t c = ((a.w >> (4 * e)) & 15u) | 0x4B000000u;  // 2^23 + c
+    x[e] = fmaf(__uint_as_float(c) - 8388608.f, s, m);
+  }
 }
 
 // What the newest rows stand for: D / 8 lanes a row and side.
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
-    read_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q, int rows, T *key,
-                T *val) {
+    read_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q, int groups,
+                int rows, T *key, T *val) {
   pdl_begin();
   using A = Append<T, D>;
   const View &c = k.c;
   const int lane = threadIdx.x & 31, i = lane % A::kLanes;
-  const int groups = (rows + A::kRows - 1) / A::kRows;
-  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int side = (int)(w & 1);
-  const int tg = (int)((w >> 1) % groups);
-  const long long unit = (w >> 1) / groups;
-  const int h = (int)(unit % c.H), lr = (int)(unit / c.H % k.nl);
-  const long long s = unit / c.H / k.nl;
-  if (s >= k.n) return;
-  const int count = q.count[s], r0 = q.len[s] - count;
-  const size_t u = unit_at(c, k.s0 + (int)s, k.lb, lr, h);
-  T *to = (side ? val : key) +
-          (((size_t)(s + k.s0) * k.nl + lr) * c.H + h) * rows * D + 8 * i;
+  const Task at = task_of(k, groups);
+  if (!at.any) return;
+  const int count = q.count[at.s], r0 = q.len[at.s] - count, t0 = at.group * A::kRows;
+  const size_t u = unit_at(c, k.s0 + at.s, k.lb, at.lr, at.h);
+  T *to = (at.side ? val : key) +
+          (((size_t)(at.s + k.s0) * k.nl + at.lr) * c.H + at.h) * rows * D;
   RowWords words[A::kRounds];
 #pragma unroll
   for (int n = 0; n < A::kRounds; ++n) {
-    const int r = r0 + min(tg * A::kRows + n * A::kOnce + lane / A::kLanes, count - 1);
+    const int r = r0 + min(t0 + n * A::kOnce + lane / A::kLanes, count - 1);
     words[n] = RowWords{0, 0};
-    if (count > 0) words[n] = row_words<D>(block_at(c, u, r), side, r % kBlock, i);
+    if (count > 0) words[n] = row_words<D>(block_at(c, u, r), at.side, r % kBlock, i);
   }
 #pragma unroll
   for (int n = 0; n < A::kRounds; ++n) {
-    const int t = tg * A::kRows + n * A::kOnce + lane / A::kLanes;
+    const int t = t0 + n * A::kOnce + lane / A::kLanes;
+    if (t >= rows) break;
     float x[8];
-    word_values(words[n], side, x);
-    if (t >= count)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    Eight<T> o;
-    narrow(x, o);
-    if (t < rows)
-#pragma unroll
-      for (int e = 0; e < (int)sizeof(T) / 2; ++e)
-        __stcs(reinterpret_cast<uint4 *>(to + (size_t)t * D) + e, o.w[e]);
+    if (t >= count) words[n] = RowWords{0, 0};
+    word_values(words[n], x);
+    if (at.side)
+      store_eight(x, 1, i, to + (size_t)t * D);
+    else
+      store_eight(x, 0, i, to + (size_t)t * D);
   }
 }
 
@@ -423,21 +491,13 @@ __global__ void __launch_bounds__(kEvictThreads)
 #pragma unroll
     for (int e = 0; e < kBatch; ++e) {
       const int j = j0 + e * kStride + lane / kLanes;
+      if (j >= m) continue;
+      const size_t to = (u * (size_t)dst.cap + j) * D;
       float x[8];
-      Eight<T> o;
-      const size_t to = (u * (size_t)dst.cap + j) * D + 8 * ch;
-      word_values(kw[e], 0, x);
-      narrow(x, o);
-      if (j < m)
-#pragma unroll
-        for (int z = 0; z < (int)sizeof(T) / 2; ++z)
-          reinterpret_cast<uint4 *>(static_cast<T *>(dst.K) + to)[z] = o.w[z];
-      word_values(vw[e], 1, x);
-      narrow(x, o);
-      if (j < m)
-#pragma unroll
-        for (int z = 0; z < (int)sizeof(T) / 2; ++z)
-          reinterpret_cast<uint4 *>(static_cast<T *>(dst.V) + to)[z] = o.w[z];
+      word_values(kw[e], x);
+      store_eight(x, 0, ch, static_cast<T *>(dst.K) + to);
+      word_values(vw[e], x);
+      store_eight(x, 1, ch, static_cast<T *>(dst.V) + to);
     }
   }
   if (tid == 0) {
@@ -449,18 +509,20 @@ __global__ void __launch_bounds__(kEvictThreads)
 
 // Grid of a launch of eight warps a CTA, kRows rows of one side a warp.
 template <typename T, int D>
-bool row_grid(const Call &k, int rows, dim3 *grid) {
+bool row_grid(const Call &k, int rows, int *groups, dim3 *grid) {
   constexpr int kRows = Append<T, D>::kRows;
-  const long long warps = 2ll * k.n * k.nl * k.c.H * ((rows + kRows - 1) / kRows);
-  *grid = dim3((unsigned)((warps + 7) / 8));
-  return (warps + 7) / 8 <= INT32_MAX;
+  *groups = (rows + kRows - 1) / kRows;
+  const long long warps = 2ll * k.nl * k.c.H * *groups;
+  *grid = dim3((unsigned)((warps + 7) / 8), k.n);
+  return warps + 7 <= UINT32_MAX;
 }
 template <typename T, int D>
 cudaError_t launch_read(const Call &k, const Seqs &q, int rows, void *key, void *val,
                         cudaStream_t stream) {
   dim3 grid;
-  if (!row_grid<T, D>(k, rows, &grid)) return cudaErrorInvalidValue;
-  return launch_pdl(read_kernel<T, D>, grid, dim3(256), 0, stream, k, q, rows,
+  int groups;
+  if (!row_grid<T, D>(k, rows, &groups, &grid)) return cudaErrorInvalidValue;
+  return launch_pdl(read_kernel<T, D>, grid, dim3(256), 0, stream, k, q, groups, rows,
                     static_cast<T *>(key), static_cast<T *>(val));
 }
 
@@ -468,8 +530,9 @@ template <typename T, int D>
 cudaError_t launch_append_as(const Call &k, const Seqs &q, int tokens, const void *key,
                              const void *val, const RowStrides &st, cudaStream_t stream) {
   dim3 grid;
-  if (!row_grid<T, D>(k, tokens, &grid)) return cudaErrorInvalidValue;
-  return launch_pdl(append_kernel<T, D>, grid, dim3(256), 0, stream, k, q, tokens,
+  int groups;
+  if (!row_grid<T, D>(k, tokens, &groups, &grid)) return cudaErrorInvalidValue;
+  return launch_pdl(append_kernel<T, D>, grid, dim3(256), 0, stream, k, q, groups,
                     static_cast<const T *>(key), static_cast<const T *>(val), st);
 }
 

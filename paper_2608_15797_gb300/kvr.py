@@ -303,6 +303,7 @@ class Cache:
                                                   group, head_dim)
         self.cap = capacity
         self.kv_dtype, self.out_dtype = kv_dtype, out_dtype
+        self._rows = self._scores = None  # views of the buffer, once asked for
         self.nbytes = kvr_cache_required_bytes(self.desc)
         if self.nbytes == 0:
             raise KvrError(KVR_EINVAL, "Cache", "invalid descriptor")
@@ -430,6 +431,11 @@ class Cache:
     def scores_view(self):
         """(score, pos, state) as device tensors viewing the cache buffer (no
         copy): score and pos [S][L][H][row_stride], state [S][L][H][4]."""
+        if self._scores is None:  # the buffer stays where it is
+            self._scores = self._view_scores()
+        return self._scores
+
+    def _view_scores(self):
         sp, pp, stp = _P(), _P(), _P()
         stride = ctypes.c_int64()
         _check(lib.kvr_cache_scores(self.handle, ctypes.byref(sp), ctypes.byref(pp),
@@ -451,6 +457,11 @@ class Cache:
     def rows_view(self):
         """(K, V) as device tensors viewing the cache buffer (no copy), each
         [S][L][H][capacity][d] (kvr_cache_rows)."""
+        if self._rows is None:  # the buffer stays where it is
+            self._rows = self._view_rows()
+        return self._rows
+
+    def _view_rows(self):
         kp, vp = _P(), _P()
         _check(lib.kvr_cache_rows(self.handle, ctypes.byref(kp),
                                   ctypes.byref(vp)), "kvr_cache_rows")
@@ -836,16 +847,6 @@ for _name, (_res, _args) in {
     _f.argtypes = _args
 
 
-def _host_ints(x, n, what):
-    """A host int32 array of n values for the library, or None."""
-    if x is None:
-        return None
-    a = np.ascontiguousarray(x, dtype=np.int32)
-    if a.shape != (n,):
-        raise ValueError(f"{what} must be {n} whole numbers")
-    return a
-
-
 def _scratch(nbytes, device, stream):
     """Device scratch for one call on `stream`: the allocator is told where a
     stream other than the current one uses it."""
@@ -874,6 +875,8 @@ class Kv4Cache:
                                                   group, head_dim)
         self.cap = capacity
         self.dtype, self.out_dtype = dtype, out_dtype
+        self._io, self._out = TORCH_DTYPES[dtype], TORCH_DTYPES[out_dtype]
+        self._all, self._scores = (0, n_layers), None
         self.nbytes = int(lib.kvr_kv4_required_bytes(ctypes.byref(self.desc)))
         if self.nbytes == 0:
             raise KvrError(KVR_EINVAL, "Kv4Cache", "invalid descriptor")
@@ -895,40 +898,48 @@ class Kv4Cache:
             lib.kvr_kv4_destroy(h)
             self.handle = None
 
-    def _layers(self, layers):
-        return (0, self.L) if layers is None else layers
+    def _rows(self, x, shape, what):
+        """The address of x, a dense tensor of the cache's element type."""
+        if x.shape != shape or x.dtype is not self._io or \
+                not x.is_contiguous():
+            raise ValueError(f"{what} must be contiguous {self.dtype} "
+                             f"{list(shape)}, not {x.dtype} {list(x.shape)}")
+        return x.data_ptr()
 
-    def _check_rows(self, x, lead, what):
-        """x is a tensor of the cache's element type, [*lead][d]."""
-        want = (*lead, self.d)
-        if tuple(x.shape) != want or x.dtype != TORCH_DTYPES[self.dtype]:
-            raise ValueError(f"{what} must be {self.dtype} {list(want)}, not "
-                             f"{x.dtype} {list(x.shape)}")
+    def _counts(self, x, what="counts"):
+        """A host int32 array of one value a sequence, or None."""
+        if x is None:
+            return None
+        a = np.ascontiguousarray(x, dtype=np.int32)
+        if a.shape != (self.S,):
+            raise ValueError(f"{what} must be {self.S} whole numbers")
+        return a
 
     def load(self, seq, k, v, stream=None):
         """Replace a sequence: k, v [L][H][n][d] (kvr_kv4_load)."""
-        n = k.shape[2]
-        for x, name in ((k, "k"), (v, "v")):
-            self._check_rows(x, (self.L, self.H, n), name)
-        _check(lib.kvr_kv4_load(self.handle, seq, _ptr(k), _ptr(v), n,
+        shape = (self.L, self.H, k.shape[2], self.d)
+        _check(lib.kvr_kv4_load(self.handle, seq, self._rows(k, shape, "k"),
+                                self._rows(v, shape, "v"), shape[2],
                                 _stream(stream)), "kvr_kv4_load")
 
     def append(self, k, v, counts=None, layers=None, stream=None):
         """Append tokens: k, v [S][nl][n][H][d]; counts: how many of them each
         sequence has (kvr_kv4_append)."""
-        lb, le = self._layers(layers)
-        n = k.shape[2]
-        for x, name in ((k, "k"), (v, "v")):
-            self._check_rows(x, (self.S, le - lb, n, self.H), name)
-        counts = _host_ints(counts, self.S, "counts")
-        _check(lib.kvr_kv4_append(self.handle, lb, le, n, _ptr(counts),
-                                  _ptr(k), _ptr(v), _stream(stream)),
-               "kvr_kv4_append")
+        lb, le = layers or self._all
+        shape = (self.S, le - lb, k.shape[2], self.H, self.d)
+        counts = self._counts(counts)
+        _check(lib.kvr_kv4_append(
+            self.handle, lb, le, shape[2],
+            None if counts is None else counts.ctypes.data,
+            self._rows(k, shape, "k"), self._rows(v, shape, "v"),
+            _stream(stream)), "kvr_kv4_append")
 
     def truncate(self, lens):
         """Each sequence keeps its first lens[s] rows (kvr_kv4_truncate)."""
-        _check(lib.kvr_kv4_truncate(self.handle, _ptr(_host_ints(
-            lens, self.S, "lens"))), "kvr_kv4_truncate")
+        lens = self._counts(lens, "lens")
+        _check(lib.kvr_kv4_truncate(
+            self.handle, None if lens is None else lens.ctypes.data),
+            "kvr_kv4_truncate")
 
     def lengths(self):
         a = np.zeros((self.S, self.L), np.int32)
@@ -938,44 +949,47 @@ class Kv4Cache:
     def read_newest(self, n, counts=None, layers=None, stream=None):
         """What the newest n rows stand for: (k, v) [S][nl][H][n][d]
         (kvr_kv4_read)."""
-        lb, le = self._layers(layers)
-        counts = _host_ints(counts, self.S, "counts")
-        k, v = (torch.empty((self.S, le - lb, self.H, n, self.d),
-                            dtype=TORCH_DTYPES[self.dtype],
-                            device=self.buf.device) for _ in range(2))
-        _check(lib.kvr_kv4_read(self.handle, lb, le, n, _ptr(counts), _ptr(k),
-                                _ptr(v), _stream(stream)), "kvr_kv4_read")
+        lb, le = layers or self._all
+        counts = self._counts(counts)
+        shape = (self.S, le - lb, self.H, n, self.d)
+        k = torch.empty(shape, dtype=self._io, device=self.buf.device)
+        v = torch.empty_like(k)
+        _check(lib.kvr_kv4_read(self.handle, lb, le, n,
+                                None if counts is None else counts.ctypes.data,
+                                k.data_ptr(), v.data_ptr(), _stream(stream)),
+               "kvr_kv4_read")
         return k, v
 
     def attend_workspace(self, n_q, layers=None):
         """A workspace for attend() of up to n_q tokens over these layers."""
-        lb, le = self._layers(layers)
-        return torch.empty(int(lib.kvr_kv4_attend_workspace_bytes(
-            self.handle, lb, le, n_q)), dtype=torch.uint8,
-            device=self.buf.device)
+        lb, le = layers or self._all
+        n = max(int(lib.kvr_kv4_attend_workspace_bytes(self.handle, lb, le, i))
+                for i in range(1, n_q + 1))
+        return torch.empty(n, dtype=torch.uint8, device=self.buf.device)
 
     def attend(self, q, out=None, counts=None, layers=None, scores=False,
                workspace=None, stream=None):
         """Attention of the newest tokens: q [S][nl][n][H*G][d] -> out, the
         same shape in out_dtype; scores: add each row's accumulated attention
         weight (kvr_kv4_attend)."""
-        lb, le = self._layers(layers)
-        n = q.shape[2]
-        self._check_rows(q, (self.S, le - lb, n, self.H * self.G), "q")
-        counts = _host_ints(counts, self.S, "counts")
+        lb, le = layers or self._all
+        shape = (self.S, le - lb, q.shape[2], self.H * self.G, self.d)
+        qp = self._rows(q, shape, "q")
+        counts = self._counts(counts)
         if out is None:
-            out = torch.empty(q.shape, dtype=TORCH_DTYPES[self.out_dtype],
-                              device=q.device)
-        elif out.shape != q.shape or \
-                out.dtype != TORCH_DTYPES[self.out_dtype]:
-            raise ValueError(f"out must be {self.out_dtype} {list(q.shape)}")
+            out = torch.empty(shape, dtype=self._out, device=q.device)
+        elif out.shape != shape or out.dtype is not self._out or \
+                not out.is_contiguous():
+            raise ValueError(f"out must be contiguous {self.out_dtype} "
+                             f"{list(shape)}")
         if workspace is None:
             workspace = _scratch(int(lib.kvr_kv4_attend_workspace_bytes(
-                self.handle, lb, le, n)), q.device, stream)
-        _check(lib.kvr_kv4_attend(self.handle, lb, le, n, _ptr(counts),
-                                  _ptr(q), _ptr(out), 1 if scores else 0,
-                                  _ptr(workspace), workspace.numel(),
-                                  _stream(stream)), "kvr_kv4_attend")
+                self.handle, lb, le, shape[2])), q.device, stream)
+        _check(lib.kvr_kv4_attend(
+            self.handle, lb, le, shape[2],
+            None if counts is None else counts.ctypes.data, qp,
+            out.data_ptr(), 1 if scores else 0, workspace.data_ptr(),
+            workspace.numel(), _stream(stream)), "kvr_kv4_attend")
         return out
 
     def evict_into(self, cache: Cache, budget, window, stream=None):
@@ -986,13 +1000,15 @@ class Kv4Cache:
     def scores_view(self):
         """The scores as a device tensor viewing the buffer,
         [S][L][H][capacity]; it may be written."""
-        p, stride = _P(), ctypes.c_int64()
-        _check(lib.kvr_kv4_scores(self.handle, ctypes.byref(p),
-                                  ctypes.byref(stride)), "kvr_kv4_scores")
-        off = p.value - self.buf.data_ptr()
-        n = self.S * self.L * self.H * stride.value
-        return self.buf[off:off + 4 * n].view(torch.float32).view(
-            self.S, self.L, self.H, stride.value)[..., :self.cap]
+        if self._scores is None:  # the buffer stays where it is
+            p, stride = _P(), ctypes.c_int64()
+            _check(lib.kvr_kv4_scores(self.handle, ctypes.byref(p),
+                                      ctypes.byref(stride)), "kvr_kv4_scores")
+            off = p.value - self.buf.data_ptr()
+            n = self.S * self.L * self.H * stride.value
+            self._scores = self.buf[off:off + 4 * n].view(torch.float32).view(
+                self.S, self.L, self.H, stride.value)[..., :self.cap]
+        return self._scores
 
     def launch_count(self):
         n = ctypes.c_uint64()
@@ -1036,16 +1052,16 @@ def verify_workspace(n_seq, n_draft, vocab, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _logit_rows(x, what, lead):
+def _logit_rows(x, what):
     """Row stride of logits [S][n][V]: rows dense among themselves, each row's
     logits side by side."""
-    if x.dim() != 3 or tuple(x.shape) != lead or x.dtype not in _LOGITS:
-        raise ValueError(f"{what} must be bf16 or f32 {list(lead)}")
-    stride = x.stride(1) if x.shape[1] > 1 else x.stride(0)
-    if x.stride(2) != 1 and x.shape[2] > 1 or x.shape[0] > 1 and \
-            x.stride(0) != x.shape[1] * stride:
+    S, n, V = x.shape
+    if x.is_contiguous():
+        return V
+    rows, col = x.stride()[1:] if n > 1 else (x.stride(0), x.stride(2))
+    if col != 1 and V > 1 or S > 1 and x.stride(0) != n * rows:
         raise ValueError(f"{what}: rows must lie one stride apart")
-    return max(stride, x.shape[2])
+    return max(rows, V)
 
 
 def verify_drafts(target, draft, tokens, u, race, n_draft=None,
@@ -1057,31 +1073,35 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
     (accepted [S], tokens [S][T + 1]) on the device."""
     S, n, V = target.shape
     T = n - 1
-    ts = _logit_rows(target, "target", (S, T + 1, V))
-    ds = _logit_rows(draft, "draft", (S, T, V)) if T else V
-    if draft.dtype != target.dtype:
-        raise ValueError("target and draft logits must be of one type")
+    if draft.shape != (S, T, V) or draft.dtype is not target.dtype or \
+            target.dtype not in _LOGITS:
+        raise ValueError(f"target and draft must be bf16 or f32 {[S, n, V]} "
+                         f"and {[S, T, V]}")
+    ts = _logit_rows(target, "target")
+    ds = _logit_rows(draft, "draft") if T else V
     for x, name, shape, dt in (
             (tokens, "tokens", (S, T), torch.int32),
             (u, "u", (S, T), torch.float32),
             (race, "race", (S, V), torch.float32),
             (n_draft, "n_draft", (S,), torch.int32),
             (accepted, "accepted", (S,), torch.int32),
-            (out_tokens, "out_tokens", (S, T + 1), torch.int32)):
-        if x is not None and (tuple(x.shape) != shape or x.dtype != dt):
-            raise ValueError(f"{name} must be {dt} {list(shape)}")
+            (out_tokens, "out_tokens", (S, n), torch.int32)):
+        if x is not None and (x.shape != shape or x.dtype is not dt or
+                              not x.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous {dt} {list(shape)}")
     dev = target.device
     if accepted is None:
         accepted = torch.empty(S, dtype=torch.int32, device=dev)
     if out_tokens is None:
-        out_tokens = torch.empty((S, T + 1), dtype=torch.int32, device=dev)
-    d = kvr_verify_desc(S, T, V, float(temperature), _LOGITS[target.dtype])
+        out_tokens = torch.empty((S, n), dtype=torch.int32, device=dev)
+    d = kvr_verify_desc(S, T, V, temperature, _LOGITS[target.dtype])
     if workspace is None:
         workspace = _scratch(int(lib.kvr_verify_workspace_bytes(
             ctypes.byref(d))), dev, stream)
     _check(lib.kvr_verify_drafts(
         ctypes.byref(d), target.data_ptr(), ts, draft.data_ptr(), ds,
-        _ptr(tokens), _ptr(u), _ptr(race), _ptr(n_draft), _ptr(accepted),
-        _ptr(out_tokens), _ptr(workspace), workspace.numel(),
+        tokens.data_ptr(), u.data_ptr(), race.data_ptr(),
+        None if n_draft is None else n_draft.data_ptr(), accepted.data_ptr(),
+        out_tokens.data_ptr(), workspace.data_ptr(), workspace.numel(),
         _stream(stream)), "kvr_verify_drafts")
     return accepted, out_tokens
