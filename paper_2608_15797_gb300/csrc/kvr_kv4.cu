@@ -351,13 +351,13 @@ __device__ __forceinline__ uint32_t score_rank(float x) {
 // a histogram a warp; of the rows of that rank the first ones are kept.  The kept
 // rows are listed in order, in dst's positions, and their values written from
 // there, D / 8 lanes a row and side.
-constexpr int kEvictThreads = 1024;
+constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictHists = 8;  // histograms: one for every four warps
 constexpr int kEvictSmemRows = 24576;
 
 template <typename T, int D, bool IN_SMEM>
-__global__ void __launch_bounds__(kEvictThreads)
+__global__ void __launch_bounds__(kEvictThreads, 2)
     evict_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q,
                  const __grid_constant__ CacheView dst, int budget, int window) {
   extern __shared__ uint32_t s_rank[];
@@ -457,8 +457,8 @@ __global__ void __launch_bounds__(kEvictThreads)
     s_ties[warp] = ties;
   }
   __syncthreads();
-  overs = __reduce_add_sync(0xffffffffu, lane < warp ? s_count[lane] : 0);
-  ties = __reduce_add_sync(0xffffffffu, lane < warp ? s_ties[lane] : 0);
+  overs = __reduce_add_sync(0xffffffffu, lane < warp ? s_count[lane % kEvictWarps] : 0);
+  ties = __reduce_add_sync(0xffffffffu, lane < warp ? s_ties[lane % kEvictWarps] : 0);
   for (int b = i0; b < i1; b += 32) {
     unsigned over, tie;
     look(b + lane, over, tie);

@@ -28,7 +28,7 @@
 namespace {
 
 using kvr::dev::to_f;
-using kvr::ptx::ex2;
+using namespace kvr::ptx;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
@@ -122,7 +122,30 @@ struct Row {
   }
 };
 
-// Sum of 2^((x - m) c) given the maximum; a NaN, or +inf less itself, makes it NaN.
+// The greatest element of a lane's groups; NaN does not count.
+template <typename T>
+__device__ __forceinline__ float greatest(const uint4 (&w)[kLoads]);
+template <>
+__device__ __forceinline__ float greatest<float>(const uint4 (&w)[kLoads]) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k)
+    m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[k].x), __uint_as_float(w[k].y)),
+                       fmaxf(__uint_as_float(w[k].z), __uint_as_float(w[k].w))));
+  return m;
+}
+template <>
+__device__ __forceinline__ float greatest<__nv_bfloat16>(const uint4 (&w)[kLoads]) {
+  auto two = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162 *>(&x); };
+  __nv_bfloat162 m = two(0xFF80FF80u);
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k)
+    m = __hmax2(m, __hmax2(__hmax2(two(w[k].x), two(w[k].y)), __hmax2(two(w[k].z), two(w[k].w))));
+  return fmaxf(__low2float(m), __high2float(m));
+}
+
+// What logits are taken relative to: the maximum.  A NaN, or +inf less itself, makes
+// the sum NaN.
 __device__ __forceinline__ float above(float m) { return m == -INFINITY ? 0.f : m; }
 
 template <typename T>
@@ -155,23 +178,23 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const __grid_constant__
       const uint32_t none = N == 8 ? 0xFF80FF80u : 0xFF800000u;
       w[k] = v < nv ? r.load(v) : make_uint4(none, none, none, none);
     }
-    float m = -INFINITY, z = 0.f;
+    const float m = kvr::dev::warp_max(greatest<T>(w));
+    const uint64_t c2 = pk2(p.c, p.c), ref2 = pk2(-above(m) * p.c, -above(m) * p.c);
+    uint64_t z2[2] = {0, 0};
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
       float x[N];
       r.widen(w[k], x);
 #pragma unroll
-      for (int e = 0; e < N; ++e) m = fmaxf(m, x[e]);
+      for (int e = 0; e < N; e += 2) {
+        float a, b;
+        upk2(fma2(pk2(x[e], x[e + 1]), c2, ref2), a, b);
+        z2[(e >> 1) & 1] = add2(z2[(e >> 1) & 1], pk2(ex2(a), ex2(b)));
+      }
     }
-    m = kvr::dev::warp_max(m);
-    const float ref = above(m) * p.c;
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k) {
-      float x[N];
-      r.widen(w[k], x);
-#pragma unroll
-      for (int e = 0; e < N; ++e) z += ex2(fmaf(x[e], p.c, -ref));
-    }
+    float z, zb;
+    upk2(add2(z2[0], z2[1]), z, zb);
+    z += zb;
     z = kvr::dev::warp_sum(z);
     if (lane == 0) p.part[at] = make_float2(m, z);
   }
@@ -203,34 +226,56 @@ __device__ unsigned long long race_best(const Params &p, const T *tr, const T *d
   constexpr int N = Row<T>::N;
   const Row<T> t(tr, p.V), d(dr ? dr : tr, p.V);
   const bool even = (reinterpret_cast<uintptr_t>(race) & 15) == 0;
-  unsigned long long best = 0;
-  for (int v = first + threadIdx.x; v * N < p.V; v += step) {
-    const uint4 tw = t.load(v), dw = dr ? d.load(v) : make_uint4(0, 0, 0, 0);
-    float x[N], y[N], e[N];
-    if (even && v * N + N <= p.V) {
+  const int groups = (p.V + N - 1) / N;
+  float most = 0.f;  // a thread's tokens ascend, so the first of equals stays
+  int at = -1;
+  constexpr int kAhead = 2;  // groups of a thread in flight
+  for (int v0 = first + threadIdx.x; v0 < groups; v0 += kAhead * step) {
+    uint4 tw[kAhead], dw[kAhead];
+    float e[kAhead][N];
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        const float4 f = __ldg(reinterpret_cast<const float4 *>(race + v * N) + i);
-        e[4 * i] = f.x, e[4 * i + 1] = f.y, e[4 * i + 2] = f.z, e[4 * i + 3] = f.w;
+    for (int k = 0; k < kAhead; ++k) {
+      const int v = v0 + k * step;
+      const uint32_t none = N == 8 ? 0xFF80FF80u : 0xFF800000u;
+      tw[k] = make_uint4(none, none, none, none);
+      if (v < groups) {
+        tw[k] = t.load(v);
+        dw[k] = dr ? d.load(v) : make_uint4(0, 0, 0, 0);
+        if (even && v * N + N <= p.V) {
+#pragma unroll
+          for (int i = 0; i < N / 4; ++i) {
+            const float4 f = __ldg(reinterpret_cast<const float4 *>(race + v * N) + i);
+            e[k][4 * i] = f.x, e[k][4 * i + 1] = f.y, e[k][4 * i + 2] = f.z,
+                    e[k][4 * i + 3] = f.w;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i) e[k][i] = v * N + i < p.V ? __ldg(race + v * N + i) : 1.f;
+        }
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) e[i] = v * N + i < p.V ? __ldg(race + v * N + i) : 1.f;
     }
-    t.widen(tw, x);
-    d.widen(dw, y);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float w = ex2((x[i] - tp.x) * p.c) * tp.y;
-      if (dr) w -= ex2((y[i] - tq.x) * p.c) * tq.y;
-      if (w > 0.f) {  // not beyond the row, where x is -inf
-        const unsigned long long k =
-            ((unsigned long long)__float_as_uint(w / e[i]) << 32) |
-            (0xFFFFFFFFu - (unsigned)(v * N + i));
-        if (k > best) best = k;
+    for (int k = 0; k < kAhead; ++k) {
+      const int v = v0 + k * step;
+      if (v >= groups) break;
+      float x[N], y[N];
+      t.widen(tw[k], x);
+      d.widen(dw[k], y);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float w = ex2((x[i] - tp.x) * p.c) * tp.y;
+        if (dr) w -= ex2((y[i] - tq.x) * p.c) * tq.y;
+        w *= rcp(e[k][i]);
+        if (w > most) {  // not beyond the row, where x is -inf
+          most = w;
+          at = v * N + i;
+        }
       }
     }
   }
+  unsigned long long best =
+      at < 0 ? 0
+             : ((unsigned long long)__float_as_uint(most) << 32) | (0xFFFFFFFFu - (unsigned)at);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const unsigned long long k = __shfl_xor_sync(0xffffffffu, best, o);
@@ -329,7 +374,7 @@ cudaError_t launch(Params &p, cudaStream_t st) {
   e = kvr::launch_pdl(stats_kernel<T>, dim3((unsigned)grid), dim3(kThreads), 0, st, p);
   if (e != cudaSuccess) return e;
   // CTAs of a sequence: about four an SM over all sequences, a group a thread at
-  // least
+  // least (64 sequences of 152,064: 10 a sequence)
   const int ctas = (int)std::max<long long>(
       1, std::min<long long>((4 * sms + p.S - 1) / p.S, p.V / (N * kThreads)));
   return kvr::launch_pdl(decide_kernel<T>, dim3(ctas, p.S), dim3(kThreads), 0, st, p);
