@@ -346,14 +346,17 @@ __device__ __forceinline__ uint32_t score_rank(float x) {
 }
 
 // Cut a unit into dst: one CTA a unit, whose scores' ranks lie in shared memory
-// (or are formed from the scores anew, where a unit has too many rows).  Four
-// passes of eight bits find the rank of the budget-th row before the window, with
-// a histogram a warp; of the rows of that rank the first ones are kept.  The kept
-// rows are listed in order, in dst's positions, and their values written from
-// there, D / 8 lanes a row and side.
+// (or are formed from the scores anew, where a unit has too many rows).  Three
+// passes of 11, 11 and 10 bits find the rank of the budget-th row before the
+// window; of the rows of that rank the first ones are kept.  (Attention leaves
+// scores within a few octaves: bins of a quarter octave keep the lanes of a warp
+// off each other's counters.)  The kept rows are listed in order, in dst's
+// positions, and their values written from there, D / 8 lanes a row and side.
+// What costs is latency: every step has its loads in flight together.
 constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
-constexpr int kEvictHists = 8;  // histograms: one for every four warps
+constexpr int kEvictHists = 1;  // histograms, one for every kEvictHists-th warp
+constexpr int kEvictBins = 2048;
 constexpr int kEvictSmemRows = 24576;
 
 template <typename T, int D, bool IN_SMEM>
@@ -361,24 +364,29 @@ __global__ void __launch_bounds__(kEvictThreads, 2)
     evict_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q,
                  const __grid_constant__ CacheView dst, int budget, int window) {
   extern __shared__ uint32_t s_rank[];
-  __shared__ unsigned s_hist[kEvictHists][256];
+  __shared__ unsigned s_hist[kEvictHists][kEvictBins];
   __shared__ int s_count[kEvictWarps], s_ties[kEvictWarps];
   __shared__ unsigned s_digit, s_need;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_begin();
   const View &c = k.c;
-  const int h = blockIdx.x % c.H, l = blockIdx.x / c.H, s = blockIdx.y;
+  const int h = blockIdx.x % c.H, l = blockIdx.x / c.H;
+  const int s = q.count[blockIdx.y];  // the longest sequences first
   const size_t u = unit_at(c, k.s0 + s, 0, l, h);
   const float *score = c.score + u * c.sstride;
   const int n = q.len[s], first = max(0, n - window);  // rows [first, n): the window
   const int keep = min(n, budget + window);
   const bool cut = first > budget;
   if (IN_SMEM && cut) {
-    // rows of 16 floats start on 64 bytes, so whole vectors are within the row
+    // rows of 16 floats start on 64 bytes, so whole vectors are within the row; what
+    // is beyond `first` gets rank 0, which no score has
+#pragma unroll 8
     for (int i = tid; 4 * i < first; i += kEvictThreads) {
       const float4 x = __ldg(reinterpret_cast<const float4 *>(score) + i);
       *reinterpret_cast<uint4 *>(s_rank + 4 * i) =
-          make_uint4(score_rank(x.x), score_rank(x.y), score_rank(x.z), score_rank(x.w));
+          make_uint4(score_rank(x.x), 4 * i + 1 < first ? score_rank(x.y) : 0u,
+                     4 * i + 2 < first ? score_rank(x.z) : 0u,
+                     4 * i + 3 < first ? score_rank(x.w) : 0u);
     }
   }
   auto rank = [&](int i) { return IN_SMEM ? s_rank[i] : score_rank(score[i]); };
@@ -387,45 +395,59 @@ __global__ void __launch_bounds__(kEvictThreads, 2)
   int need = budget;
   if (cut && budget > 0) {
 #pragma unroll 1
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < kEvictHists * 256; i += kEvictThreads) (&s_hist[0][0])[i] = 0;
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t digits = pass == 2 ? 1023u : 2047u;
+      for (int i = tid; i < kEvictHists * kEvictBins; i += kEvictThreads) (&s_hist[0][0])[i] = 0;
       __syncthreads();
       unsigned *hist = s_hist[warp % kEvictHists];
-      for (int i = tid; i < first; i += kEvictThreads) {
-        const uint32_t x = rank(i);
-        if ((x & mask) == least) atomicAdd(&hist[(x >> shift) & 255u], 1u);
+      auto count = [&](uint32_t x) {
+        if ((x & mask) == least && x) atomicAdd(&hist[(x >> shift) & digits], 1u);
+      };
+      if (IN_SMEM) {
+#pragma unroll 4
+        for (int i = tid; 4 * i < first; i += kEvictThreads) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(s_rank + 4 * i);
+          count(x.x), count(x.y), count(x.z), count(x.w);
+        }
+      } else {
+#pragma unroll 4
+        for (int i = tid; i < first; i += kEvictThreads) count(rank(i));
       }
       __syncthreads();
-      if (warp == 0) {
-        // lane j: digits 255 - 8 j .. 248 - 8 j, counted from the top
-        unsigned d[8], sum = 0;
+      // a thread's four digits, counted from the top
+      constexpr int kPer = kEvictBins / kEvictThreads;
+      unsigned d[kPer], sum = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          d[e] = 0;
+      for (int e = 0; e < kPer; ++e) {
+        d[e] = 0;
 #pragma unroll
-          for (int z = 0; z < kEvictHists; ++z) d[e] += s_hist[z][255 - 8 * lane - e];
-          sum += d[e];
+        for (int z = 0; z < kEvictHists; ++z) d[e] += s_hist[z][kEvictBins - 1 - kPer * tid - e];
+        sum += d[e];
+      }
+      unsigned above = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned x = __shfl_up_sync(0xffffffffu, above, o);
+        if (lane >= o) above += x;
+      }
+      if (lane == 31) s_count[warp] = (int)above;
+      __syncthreads();
+      above += __reduce_add_sync(0xffffffffu,
+                                 lane < warp ? (unsigned)s_count[lane % kEvictWarps] : 0u) -
+               sum;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        if (above < (unsigned)need && above + d[e] >= (unsigned)need) {
+          s_digit = kEvictBins - 1 - kPer * tid - e;
+          s_need = need - above;
         }
-        unsigned above = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const unsigned x = __shfl_up_sync(0xffffffffu, above, o);
-          if (lane >= o) above += x;
-        }
-        above -= sum;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (above < (unsigned)need && above + d[e] >= (unsigned)need) {
-            s_digit = 255 - 8 * lane - e;
-            s_need = need - above;
-          }
-          above += d[e];
-        }
+        above += d[e];
       }
       __syncthreads();
       least |= s_digit << shift;
       need = s_need;
-      mask |= 255u << shift;
+      mask |= digits << shift;
     }
   }
   // List the kept rows in order: each warp counts those of its own stretch, and
@@ -446,6 +468,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2)
     tie = __ballot_sync(0xffffffffu, t);
   };
   int overs = 0, ties = 0;
+#pragma unroll 4
   for (int b = i0; b < i1; b += 32) {
     unsigned over, tie;
     look(b + lane, over, tie);
@@ -459,24 +482,23 @@ __global__ void __launch_bounds__(kEvictThreads, 2)
   __syncthreads();
   overs = __reduce_add_sync(0xffffffffu, lane < warp ? s_count[lane % kEvictWarps] : 0);
   ties = __reduce_add_sync(0xffffffffu, lane < warp ? s_ties[lane % kEvictWarps] : 0);
+#pragma unroll 4
   for (int b = i0; b < i1; b += 32) {
     unsigned over, tie;
     look(b + lane, over, tie);
     const int tied = ties + __popc(tie & lower);
     const bool kept = (over >> lane & 1u) || ((tie >> lane & 1u) && tied < need);
     const int at = overs + __popc(over & lower) + min(tied, need);
-    if (kept && at < keep) {
-      pos[at] = b + lane;
-      to_score[at] = score[b + lane];
-    }
+    if (kept && at < keep) pos[at] = b + lane;
     overs += __popc(over);
     ties += __popc(tie);
   }
   if (tid == kEvictThreads - 1 && overs + min(ties, need) != keep && cut)
     atomicOr(c.err, ERR_LENGTH);
   __syncthreads();
+  for (int j = tid; j < keep; j += kEvictThreads) to_score[j] = score[pos[j]];
   // Their values: D / 8 lanes a row, kBatch rows of each in flight.
-  constexpr int kLanes = D / 8, kOnce = 32 / kLanes, kBatch = 4;
+  constexpr int kLanes = D / 8, kOnce = 32 / kLanes, kBatch = 8;
   constexpr int kStride = kEvictWarps * kOnce;
   const int m = keep, ch = lane % kLanes;
   for (int j0 = warp * kOnce; j0 < m; j0 += kBatch * kStride) {
@@ -537,10 +559,11 @@ cudaError_t launch_append_as(const Call &k, const Seqs &q, int tokens, const voi
 }
 
 template <typename T, int D>
-cudaError_t launch_evict(const Call &k, const Seqs &q, const CacheView &dst, int budget,
-                         int window, cudaStream_t stream) {
-  int most = 0;
-  for (int i = 0; i < k.n; ++i) most = std::max(most, q.len[i] - window);
+cudaError_t launch_evict(const Call &k, Seqs q, const CacheView &dst, int budget, int window,
+                         cudaStream_t stream) {
+  for (int i = 0; i < k.n; ++i) q.count[i] = i;
+  std::sort(q.count, q.count + k.n, [&](int a, int b) { return q.len[a] > q.len[b]; });
+  const int most = std::max(0, q.len[q.count[0]] - window);
   const dim3 grid(k.c.L * k.c.H, k.n);
   if (most > kEvictSmemRows)
     return launch_pdl(evict_kernel<T, D, false>, grid, dim3(kEvictThreads), 0, stream, k, q, dst,
