@@ -45,18 +45,26 @@ using namespace ptx;
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 2;      // blocks in flight a warp
-constexpr int kMinSpan = 2;     // pieces of a span, at least
+constexpr int kMinSpan = 3;     // pieces of a span, at least (2 to 4: within 3% for 28 small calls)
+constexpr int kTurn = 3;        // pieces that a turn to another item is worth
 constexpr int kMaxGrid = 1024;  // CTAs of a split call, at most
 
-// How a launch is cut: item (sequence, unit, tile of query rows) i of sequence s
-// has pieces_of(blocks_of(s)) pieces; base[s] pieces precede sequence s.  A CTA
-// takes `span` pieces of the list, or one item where span == 0.
+// How a launch is cut.  An item (unit, tile of query rows) of sequence s has
+// pieces_of(blocks_of(s)) pieces.
+//  kSpans: all pieces form one list, and a CTA takes `span` of them, whatever
+//    items they belong to; base[s] pieces precede sequence s.
+//  kParts: an item is cut into as few equal parts as keep each within `span`
+//    pieces, and a CTA takes one; base[s] parts precede sequence s.  No CTA turns
+//    from one item to another, which costs as much as a few pieces.
+//  kItems: a CTA takes an item.
+enum Cut { kSpans, kParts, kItems };
 struct Plan {
   int32_t base[kMaxSeqs + 1];
-  int32_t span, tiles;
+  int32_t cut, span, tiles;
 };
 
 __host__ __device__ inline int pieces_of(int nb) { return (nb + kPiece - 1) / kPiece; }
+__host__ __device__ inline int parts_of(int np, int span) { return (np + span - 1) / span; }
 // First block of piece i of np.
 // (nb is at most 2^19, so np * nb fits 36 bits: where it does not fit 32, in 64.)
 __device__ __forceinline__ int piece_at(int nb, int np, int i) {
@@ -523,13 +531,12 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
   }
   if (threadIdx.x == 0) flag[1] = 0;
   __syncthreads();
-  pdl_begin();
 
   const int per_seq = p.k.nl * c.H * plan.tiles;
   int last;  // list index behind the CTA's last piece
   Run run;
-  if (plan.span) {
-    run.at = blockIdx.x * plan.span;
+  if (plan.cut != kItems) {
+    run.at = plan.cut == kSpans ? (int)blockIdx.x * plan.span : (int)blockIdx.x;
     last = min(run.at + plan.span, plan.base[p.k.n]);
     int lo = 0, hi = p.k.n;  // the sequence that holds run.at
     while (hi - lo > 1) {
@@ -540,11 +547,21 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
     run.nb = blocks_of(sq.len[lo]);
     const int np = pieces_of(run.nb);
     const int rest = run.at - plan.base[lo];
-    run.item = rest / np;
-    const int piece = rest - run.item * np;
-    run.n = min(np - piece, last - run.at);
-    run.begin = piece_at(run.nb, np, piece);
-    run.end = piece_at(run.nb, np, piece + run.n);
+    if (plan.cut == kSpans) {
+      run.item = rest / np;
+      const int piece = rest - run.item * np;
+      run.n = min(np - piece, last - run.at);
+      run.begin = piece_at(run.nb, np, piece);
+      run.end = piece_at(run.nb, np, piece + run.n);
+    } else {
+      const int parts = parts_of(np, plan.span);
+      run.item = rest / parts;
+      const int part = rest - run.item * parts;
+      run.begin = piece_at(run.nb, np, piece_at(np, parts, part));
+      run.end = piece_at(run.nb, np, piece_at(np, parts, part + 1));
+      run.n = 1;
+      last = run.at + 1;
+    }
   } else {
     run.s = blockIdx.x / per_seq;
     run.item = blockIdx.x - run.s * per_seq;
@@ -602,6 +619,8 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
     ++issued;
     ahead_blk += kWarps;
   };
+  // Nothing before this read what earlier launches write.
+  pdl_begin();
   for (int i = 0; i < kStages; ++i) issue();
 
   bool ok = true;
@@ -687,7 +706,8 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
     __syncthreads();
     constexpr int kPer = kCols * D / 4 / kThreads;  // groups of four channels a thread
     const size_t call_unit = ((size_t)(p.k.s0 + run.s) * p.k.nl + lr) * c.H + h;
-    const int slot = blockIdx.x * 2 + (run.at == blockIdx.x * plan.span ? 0 : 1);
+    // a CTA's first run may lack its beginning, its last one its end
+    const int slot = blockIdx.x * 2 + (run.begin > 0 ? 0 : 1);
     float *part = p.parts + (size_t)slot * kCols * (D + 2);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
@@ -706,9 +726,10 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
       if (threadIdx.x < kCols)
         __stcg(reinterpret_cast<float2 *>(part + kCols * D) + threadIdx.x, joined);
       // The last of the item's spans to finish joins them, in order.
-      const int np = pieces_of(run.nb);
-      const int i0 = plan.base[run.s] + run.item * np;
-      const int c0 = i0 / plan.span, c1 = (i0 + np - 1) / plan.span;
+      const int np = pieces_of(run.nb), parts = parts_of(np, plan.span);
+      const int i0 = plan.base[run.s] + run.item * (plan.cut == kSpans ? np : parts);
+      const int c0 = plan.cut == kSpans ? i0 / plan.span : i0;
+      const int c1 = plan.cut == kSpans ? (i0 + np - 1) / plan.span : i0 + parts - 1;
       unsigned *ticket = c.ticket + unit_of(run) * kMaxTiles + tile;
       __syncthreads();
       if (threadIdx.x == 0) flag[0] = take_ticket(ticket) == (unsigned)(c1 - c0);
@@ -716,58 +737,52 @@ __global__ void __launch_bounds__(kThreads, NT * TERMS == 1 ? 4 : 2)
       if (flag[0]) {
         if (threadIdx.x == 0) *ticket = 0;
         auto part_of = [&](int w) {
-          return p.parts + ((size_t)w * 2 + (w * plan.span >= i0 ? 0 : 1)) * kCols * (D + 2);
+          return p.parts + ((size_t)w * 2 + (w == c0 ? 1 : 0)) * kCols * (D + 2);
         };
-        // Columns' maxima first, a lane a contributor; then kSome contributors at a
-        // time, their sums' loads in flight together.
-        for (int col = warp; col < kCols; col += kWarps) {
-          float top = kNone, z = 0.f;
-          for (int w = c0 + lane; w <= c1; w += 32) {
-            const float2 x = __ldcg(reinterpret_cast<const float2 *>(part_of(w) + kCols * D) + col);
-            const float m = fmaxf(top, x.x);
-            z = fmaf(z, ex2(top - m), x.y * ex2(x.x - m));
-            top = m;
-          }
-          const float all = dev::warp_max(top);
-          z = dev::warp_sum(z * ex2(top - all));
-          if (lane == 0) col_stat[col] = make_float2(all, z);
-        }
-        __syncthreads();
-        constexpr int kSome = NT == 1 ? 16 : 8;
+        // kSome contributors at a time, all their loads in flight together.
+        constexpr int kSome = NT == 1 ? 8 : NT == 2 ? 4 : 2;
         float4 sum[kPer];
+        float top[kPer], z[kPer];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int j = 0; j < kPer; ++j) {
+          sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+          top[j] = kNone;
+          z[j] = 0.f;
+        }
         for (int w0 = c0; w0 <= c1; w0 += kSome) {
-          for (int i = threadIdx.x; i < kSome * kCols; i += kThreads) {
-            const int w = w0 + i / kCols, col = i % kCols;
-            exch[i] = w <= c1 ? ex2(__ldcg(part_of(w) + kCols * D + 2 * col) - col_stat[col].x)
-                              : 0.f;
+          float2 st[kSome][kPer];
+          float4 x[kSome][kPer];
+#pragma unroll
+          for (int w = 0; w < kSome; ++w)
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+              const int i = threadIdx.x + j * kThreads;
+              const float *from = part_of(min(c1, w0 + w));
+              st[w][j] = __ldcg(reinterpret_cast<const float2 *>(from + kCols * D) + 4 * i / D);
+              x[w][j] = __ldcg(reinterpret_cast<const float4 *>(from) + i);
+            }
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) {
+            float m = top[j];
+#pragma unroll
+            for (int w = 0; w < kSome; ++w) m = fmaxf(m, st[w][j].x);
+            const float f = ex2(top[j] - m);
+            top[j] = m;
+            z[j] *= f;
+            sum[j].x *= f, sum[j].y *= f, sum[j].z *= f, sum[j].w *= f;
+#pragma unroll
+            for (int w = 0; w < kSome; ++w) {
+              if (w0 + w > c1) break;
+              const float g = ex2(st[w][j].x - m);
+              z[j] = fmaf(st[w][j].y, g, z[j]);
+              add4(sum[j], x[w][j], g);
+            }
           }
-          __syncthreads();
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float4 x[kSome / 2][kPer];
-#pragma unroll
-            for (int w = 0; w < kSome / 2; ++w)
-#pragma unroll
-              for (int j = 0; j < kPer; ++j)
-                x[w][j] = __ldcg(reinterpret_cast<const float4 *>(
-                                     part_of(min(c1, w0 + half * (kSome / 2) + w))) +
-                                 threadIdx.x + j * kThreads);
-#pragma unroll
-            for (int w = 0; w < kSome / 2; ++w)
-#pragma unroll
-              for (int j = 0; j < kPer; ++j)
-                add4(sum[j], x[w][j], exch[(half * (kSome / 2) + w) * kCols +
-                                           4 * (threadIdx.x + j * kThreads) / D]);
-          }
-          __syncthreads();
         }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-          const int i = threadIdx.x + j * kThreads, col = 4 * i / D;
-          finish<O>(p, place[col], 4 * i % D, sum[j], col_stat[col].x, col_stat[col].y,
-                    call_unit);
+          const int i = threadIdx.x + j * kThreads;
+          finish<O>(p, place[4 * i / D], 4 * i % D, sum[j], top[j], z[j], call_unit);
         }
       }
     }
@@ -1001,18 +1016,35 @@ cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream)
   const long long tiles = tiles_of(c, p.n_q), per_seq = (long long)p.k.nl * c.H * tiles;
   if (tiles > INT32_MAX || per_seq > INT32_MAX) return cudaErrorInvalidValue;
   plan.tiles = (int)tiles;
-  long long total = 0;
-  for (int i = 0; i < p.k.n; ++i) {
-    plan.base[i] = (int32_t)total;
-    total += per_seq * pieces_of(blocks_of(q.len[i]));
-  }
-  plan.base[p.k.n] = (int32_t)total;
+  auto total_of = [&](int span) {  // parts, or pieces for span == 1
+    long long n = 0;
+    for (int i = 0; i < p.k.n; ++i) {
+      plan.base[i] = (int32_t)std::min<long long>(n, INT32_MAX);
+      n += per_seq * parts_of(pieces_of(blocks_of(q.len[i])), span);
+    }
+    plan.base[p.k.n] = (int32_t)std::min<long long>(n, INT32_MAX);
+    return n;
+  };
+  const long long total = total_of(1);
   long long grid;
   if (tiles <= kMaxTiles && total <= INT32_MAX) {
-    plan.span = (int32_t)std::max<long long>(kMinSpan, (total + resident - 1) / resident);
-    grid = (total + plan.span - 1) / plan.span;
+    const int even = (int)std::max<long long>(kMinSpan, (total + resident - 1) / resident);
+    plan.cut = kSpans;
+    plan.span = even;
+    grid = (total + even - 1) / even;
+    // parts where they fit on the GPU at once and are not much longer
+    for (int span = even; span <= even + kTurn; ++span) {
+      const long long parts = total_of(span);
+      if (parts > resident) continue;
+      plan.cut = kParts;
+      plan.span = span;
+      grid = parts;
+      break;
+    }
+    if (plan.cut == kSpans) total_of(1);
   } else {
-    plan.span = 0;
+    plan.cut = kItems;
+    plan.span = 1;
     grid = per_seq * p.k.n;
   }
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
