@@ -9,7 +9,9 @@
 // thread loads its fragment's words whole and masks give 16-bit pairs:
 //  - K word: 8 channels of one token, channel 64 j + 16 t + 8 i + e of a row
 //    in chunk t (of four), word 2 j + i, bits 4 e .. 4 e + 3.  Thread t of a
-//    fragment's row owns chunk t; its words 2 j, 2 j + 1 belong to group j.
+//    fragment's row owns chunk t; its words 2 j, 2 j + 1 belong to group j.  Chunks
+//    lie permuted by the row (k_chunk), so that threads that read one chunk of
+//    eight neighbouring rows hit different banks.
 //  - V word: 4 channels of two tokens (even token low half): the row of chunk c
 //    (of eight), word w holds channels 32 w + c + {0, 16, 8, 24}, in order of
 //    bits.  Chunks lie permuted by the pair's index (v_chunk), so that the
@@ -64,12 +66,15 @@ __device__ __forceinline__ int v_chunk(int p, int c) {
   return D == 128 ? c ^ ((p & 3) << 1) : c ^ (((p >> 1) & 1) << 2);
 }
 
+// Physical chunk of chunk t of row r.
+__device__ __forceinline__ int k_chunk(int r, int t) { return t ^ ((r >> 1) & 3); }
+
 // Byte of the block, and whether it is the high nibble, of a channel's code.
 template <int D>
 __device__ __forceinline__ int k_byte(int r, int x, int &hi) {
   const int j = x >> 6, t = (x >> 4) & 3, i = (x >> 3) & 1, e = x & 7;
   hi = e & 1;
-  return k_off() + r * (D / 2) + t * (D / 8) + (2 * j + i) * 4 + (e >> 1);
+  return k_off() + r * (D / 2) + k_chunk(r, t) * (D / 8) + (2 * j + i) * 4 + (e >> 1);
 }
 // 16-bit half (byte offset of the block) that holds channels
 // 32 w + c + {0, 16, 8, 24} of token r.

@@ -290,8 +290,8 @@ __device__ __forceinline__ void block_logits(const Query<D, NT, TERMS> &q, uint3
   for (int tt = 0; tt < 2; ++tt) {
     const int r = 16 * tt + g;
     uint32_t x[W], y[W], mx[GR], my[GR];
-    lds_words<W>(block + k_off() + r * (D / 2) + t * (D / 8), x);
-    lds_words<W>(block + k_off() + (r + 8) * (D / 2) + t * (D / 8), y);
+    lds_words<W>(block + k_off() + r * (D / 2) + k_chunk(r, t) * (D / 8), x);
+    lds_words<W>(block + k_off() + (r + 8) * (D / 2) + k_chunk(r + 8, t) * (D / 8), y);
     lds_meta<GR>(block + km_off(D) + r * GR * 4, mx);
     lds_meta<GR>(block + km_off(D) + (r + 8) * GR * 4, my);
     float acc[NT][GR][4] = {};
@@ -871,7 +871,7 @@ __global__ void __launch_bounds__(kThreads)
         for (int b = 0; b < 2; ++b) {
           const int r = 16 * tt + 8 * b + g;
           const uint32_t *k = reinterpret_cast<const uint32_t *>(
-              at + k_off() + r * (D / 2) + t * (D / 8));
+              at + k_off() + r * (D / 2) + k_chunk(r, t) * (D / 8));
           if (W == 4) {
             const uint4 x = __ldg(reinterpret_cast<const uint4 *>(k));
             next[tt][b][0] = x.x, next[tt][b][1] = x.y;

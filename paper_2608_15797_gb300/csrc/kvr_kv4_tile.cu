@@ -19,8 +19,8 @@
 //   8 softmax   two groups of four warps (4 x 32 tokens); one takes the even tiles,
 //               the other the odd ones, each with references, sums and an O of
 //               its own, so that one works while the other waits
-//   6 dequant   raw blocks (which they load) -> K and V operands, the tokens'
-//               constants
+//   7 dequant   raw blocks (which they load) -> K's operand in tensor memory, V's
+//               in shared memory, the tokens' constants
 //   1 issuer    the matrix products
 // As in the other kernel, CTAs take equal spans of the list of all tiles and the
 // last of those that share a unit joins their results in order.
@@ -40,14 +40,15 @@ constexpr int kD = 128;
 constexpr int kTok = 128;                   // tokens of a tile
 constexpr int kTileBlocks = kTok / kBlock;
 constexpr int kMaxN = 64;                   // columns of a tile
-constexpr int kSoft = 8, kDeq = 6;          // warps
+constexpr int kSoft = 8, kDeq = 7;          // warps
 constexpr int kThr = 32 * (kSoft + kDeq + 1);
 constexpr int kRing = 3;                    // raw tiles in flight
 constexpr int kTileGrid = 256;              // CTAs of a split call, at most
 constexpr uint32_t kRaw = kTileBlocks * block_bytes(kD);
 constexpr uint32_t kHalf = kTok * 128;      // one 64-element half of an operand
-constexpr uint32_t kCols = 512;             // tensor memory: S (2 x 2 x 64), O (2 x 64)
-constexpr uint32_t kColO = 256;
+constexpr uint32_t kCols = 512;             // tensor memory: S (2 x 2 x 64), O (2 x 64),
+constexpr uint32_t kColO = 256;             // K (2 x 64)
+constexpr uint32_t kColK = 384;
 constexpr float kUnit = 0x1p24f;            // of K's codes
 
 // An item's place in the list counts its tiles and, before them, kSwitch more for
@@ -75,12 +76,12 @@ struct __align__(16) Side {
   Place place[kMaxN];
   float qmax[kSoft];
   int nan_row[4][2];            // [run % 4][group]: first row whose value is NaN
-  uint64_t raw_full[kRing], kf[2], k_free, vf[2], pv[2], sf[2], s_free[2], pf[2], qf, drain;
+  uint64_t raw_full[kRing], kf[2], vf[2], pv[2], sf[2], s_free[2], pf[2], qf, drain;
   uint32_t tmem;
   int abort, flag;
 };
 
-constexpr uint32_t kOffV = 2 * kHalf, kOffP = kOffV + 4 * kHalf, kOffQ = kOffP + 2 * kHalf,
+constexpr uint32_t kOffV = 0, kOffP = kOffV + 4 * kHalf, kOffQ = kOffP + 2 * kHalf,
                    kOffRaw = kOffQ + 2 * kMaxN * 128, kOffSide = kOffRaw + kRing * kRaw;
 constexpr uint32_t kSmem = kOffSide + sizeof(Side);
 static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -181,14 +182,13 @@ __global__ void __launch_bounds__(kThr, 1)
   if (tid == 0) {
     for (int b = 0; b < kRing; ++b) mbar_init(smem_u32(&S.raw_full[b]), 1);
     for (int b = 0; b < 2; ++b) {
-      mbar_init(smem_u32(&S.kf[b]), kDeq);
+      mbar_init(smem_u32(&S.kf[b]), 4);
       mbar_init(smem_u32(&S.vf[b]), kDeq);
       mbar_init(smem_u32(&S.pv[b]), 1);
       mbar_init(smem_u32(&S.sf[b]), 1);
       mbar_init(smem_u32(&S.s_free[b]), kSoft / 2);
       mbar_init(smem_u32(&S.pf[b]), 1);
     }
-    mbar_init(smem_u32(&S.k_free), 1);
     mbar_init(smem_u32(&S.qf), 1);
     mbar_init(smem_u32(&S.drain), 1);
     S.abort = 0;
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kThr, 1)
   } else if (warp == kSoft + kDeq) {
     // ---- issuer
     const uint32_t id_s = idesc_f16(kTok, N, false), id_o = idesc_f16(kD, N, true);
-    const uint64_t dk = sdesc_sw128(base, 16, 1024), dq = sdesc_sw128(base + kOffQ, 16, 1024);
+    const uint64_t dq = sdesc_sw128(base + kOffQ, 16, 1024);
     const uint64_t dv = sdesc_sw128(base + kOffV, 16, 1024);
     const uint64_t dp = sdesc_sw128(base + kOffP, kHalf, 1024);
     int i = 0, runs = 0;
@@ -272,10 +272,9 @@ __global__ void __launch_bounds__(kThr, 1)
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              tc_mma(tm + (i & 1) * 128 + j * 64, dk + (uint64_t)((j * kHalf + k * 32) >> 4),
-                     dq + (uint64_t)((j * N * 128 + k * 32) >> 4), id_s, k > 0);
+              tc_mma_ts(tm + (i & 1) * 128 + j * 64, tm + kColK + (i & 1) * 64 + j * 32 + k * 8,
+                        dq + (uint64_t)((j * N * 128 + k * 32) >> 4), id_s, k > 0);
           tc_commit(smem_u32(&S.sf[i & 1]));
-          tc_commit(smem_u32(&S.k_free));
         }
         __syncwarp();
         if (t > run.t0) issue_pv(i - 1, t - 1 - run.t0 < 2);
@@ -357,36 +356,47 @@ __global__ void __launch_bounds__(kThr, 1)
           S.nan_row[(runs + 1) & 3][0] = INT32_MAX;
           S.nan_row[(runs + 1) & 3][1] = INT32_MAX;
         }
-        if (ok && i > 0) ok = wait(S.k_free, i - 1);
         ok = !bar_any(1, 32 * kDeq, !ok);
         if (!ok) break;
         if (dt == 0 && i > 0) load_next();  // in the place of tile i - 1
-        // K: a row's chunk t4 (four words) a lane
+        // K: a token a thread of the first four warps, into tensor memory (its place is
+        // free: S of tile i - 2, which was read, is the product it was for).  A
+        // word's fields are the pairs of nibbles 0 4, 1 5, 2 6, 3 7.
+        if (dw < 4) {
+          const unsigned char *at =
+              raw + (dt / kBlock) * block_bytes(kD) + k_off() + (dt % kBlock) * (kD / 2);
+          uint4 w[4];
 #pragma unroll
-        for (int z = 0; z < (16 + kDeq - 1) / kDeq; ++z) {
-          if (dw + z * kDeq >= 16) break;
-          const int x = (dw + z * kDeq) * 32 + lane, row = x >> 2, t4 = x & 3;
-          const uint4 w = *reinterpret_cast<const uint4 *>(
-              raw + (row / kBlock) * block_bytes(kD) + k_off() + (row % kBlock) * (kD / 2) +
-              t4 * 16);
-          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+          for (int t4 = 0; t4 < 4; ++t4)
+            w[t4] = *reinterpret_cast<const uint4 *>(at + k_chunk(dt, t4) * 16);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t y = ws[k] >> 8;
-            sts128(base + (k >> 1) * kHalf + row * 128 + (((2 * t4 + (k & 1)) ^ (row & 7)) << 4),
-                   ws[k] & 0x000F000Fu, ws[k] & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u);
+          for (int j = 0; j < 2; ++j) {  // channels 64 j ..: words 2 j, 2 j + 1 of each chunk
+            uint32_t o[32];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              const uint4 &c4 = w[x >> 1];
+              const uint32_t v = j == 0 ? (x & 1 ? c4.y : c4.x) : (x & 1 ? c4.w : c4.z);
+              const uint32_t y = v >> 8;
+              o[4 * x] = v & 0x000F000Fu;
+              o[4 * x + 1] = v & 0x00F000F0u;
+              o[4 * x + 2] = y & 0x000F000Fu;
+              o[4 * x + 3] = y & 0x00F000F0u;
+            }
+            tmem_st32(tm + ((uint32_t)(dw * 32) << 16) + kColK + b * 64 + j * 32, o);
           }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&S.kf[b]));
         }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&S.kf[b]));
         if (i >= 2) ok = ok && wait(S.pv[b], i / 2 - 1);
         // V: eight tokens (tg) of chunk ch, word w, a lane
         const uint32_t to0 = base + kOffV + b * 2 * kHalf;
-#pragma unroll
-        for (int z = 0; z < (16 + kDeq - 1) / kDeq; ++z) {
-          const int wt = dw + z * kDeq;
-          if (wt >= 16) break;
+        // (sixteen tasks: one for a warp that had a part in K, four for the others)
+        static_assert(kDeq == 7, "tasks");
+        const int first_task = dw < 4 ? dw : 4 * dw - 12, tasks = dw < 4 ? 1 : 4;
+#pragma unroll 2
+        for (int wt = first_task; wt < first_task + tasks; ++wt) {
           const int w = wt & 3, tg = (wt >> 2) * 4 + (lane >> 3), ch = lane & 7;
           uint32_t v[4];
           __half2 sc[4], mn[4];
