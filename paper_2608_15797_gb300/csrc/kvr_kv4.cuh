@@ -182,10 +182,11 @@ struct AttendParams {
 cudaError_t launch_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream,
                           int *launches);
 // kvr_kv4_tile.cu: the same, on 5th-generation tensor cores, where it applies
-// (bf16, d = 128, more than eight query rows a unit), without the scores.
+// (bf16, d = 128, more than eight query rows a unit), and the scores' sums.
 bool tile_applies(const View &c, int n_q);
 size_t tile_part_floats(const View &c, int nl, int n_q);
 cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream);
+cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, cudaStream_t stream);
 // Floats of workspace: statistics of every query row, then partial results.
 size_t attend_stat_floats(const View &c, int nl, int n_q);
 size_t attend_part_floats(const View &c, int nl, int n_q);

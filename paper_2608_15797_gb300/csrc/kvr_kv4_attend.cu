@@ -1067,6 +1067,7 @@ cudaError_t launch_io(const AttendParams &p, const Seqs &q, cudaStream_t stream,
   *launches = 1;
   if (e != cudaSuccess || !p.stats) return e;
   *launches = 2;
+  if (tile_applies(p.k.c, p.n_q)) return launch_tile_scores(p, q, stream);
   return wide ? launch_scores<T, 128, TERMS>(p, q, stream)
               : launch_scores<T, 64, TERMS>(p, q, stream);
 }

@@ -122,14 +122,45 @@ __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint
                                        uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d));
 }
-// As tmem_wait_ld, but other loads may pass it.
-__device__ __forceinline__ void tmem_landed() {
-  asm volatile("tcgen05.wait::ld.sync.aligned;");
+// As tmem_wait_ld, but only what was loaded waits: memory's loads may pass it.
+__device__ __forceinline__ void tmem_landed(float (&a)[8], float (&b)[8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(a[0]), "+f"(a[1]), "+f"(a[2]), "+f"(a[3]), "+f"(a[4]), "+f"(a[5]),
+                 "+f"(a[6]), "+f"(a[7]), "+f"(b[0]), "+f"(b[1]), "+f"(b[2]), "+f"(b[3]),
+                 "+f"(b[4]), "+f"(b[5]), "+f"(b[6]), "+f"(b[7]));
+}
+// A token's products with N columns, where some columns do not see it: they get
+// minus infinity (what multiplies it is above zero), which keeps the mask out of the
+// loops over all tiles.  A key that stands for NaN gives it to those who see it, and
+// its constants are made harmless.
+__device__ __forceinline__ void mask_row(uint32_t ts, int n, const int *limit, int row,
+                                         float4 &key) {
+  const bool bad = key.z != key.z || key.w != key.w;
+#pragma unroll 1
+  for (int k = 0; k < n; k += 8) {
+    float a[8];
+    tmem_ld8(ts + k, a);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = row > limit[k + e] ? -INFINITY : bad ? NAN : a[e];
+    tmem_st8(ts + k, a);
+  }
+  tmem_wait_st();
+  if (bad) key = make_float4(1.f, 1.f, 0.f, 0.f);
 }
 __device__ __forceinline__ uint32_t half2_bits(__half2 x) {
   return *reinterpret_cast<const uint32_t *>(&x);
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2 *>(&x); }
+
+// The pairs of nibbles 0 4, 1 5, 2 6, 3 7 of a word as half-precision c 2^-20, on which
+// the tensor core keeps its full precision.
+__device__ __forceinline__ void even_fields(uint32_t x, uint32_t *f) {
+  f[0] = (x << 4) & 0x00F000F0u;
+  f[1] = x & 0x00F000F0u;
+  f[2] = (x >> 4) & 0x00F000F0u;
+  f[3] = (x >> 8) & 0x00F000F0u;
+}
 
 // A run of tiles [t0, t1) of one item; np: all it has; at: the item's place.
 struct TileRun {
@@ -470,7 +501,7 @@ __global__ void __launch_bounds__(kThr, 1)
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[z][e] = 0.f;
         const Place a = place_of(p, sq, run.s, lr, h, col0 + col);
-        if (a.out >= 0) {
+        if (a.out >= 0 && a.live) {
           const uint4 w = *reinterpret_cast<const uint4 *>(
               static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci);
           const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
@@ -534,13 +565,14 @@ __global__ void __launch_bounds__(kThr, 1)
       int mine = 0;  // tiles of the run that this group has taken
       for (int t = run.t0 + ((i ^ grp) & 1); t < run.t1; t += 2, ++mine) {
         const int n = (i + t - run.t0) >> 1, row = t * kTok + tok;  // n: the group's tiles so far
-        const bool mask = (t + 1) * kTok > full;
         if (ok) ok = wait(S.kf[grp], n) && wait(S.sf[grp], n);
         if (ok && n > 0) ok = wait(S.pv[grp], n - 1);  // P's place, and O's
         tc_fence_after();
-        const float4 key = S.key[grp][tok];
+        float4 key = S.key[grp][tok];
         const float2 val = S.val[grp][tok];
-        const uint64_t s0 = pk2(key.x * unit_s, key.x * unit_s);
+        if (ok && (t + 1) * kTok > full) mask_row(ts, N, S.limit, row, key);
+        const float k0 = fmaxf(key.x * unit_s, 0x1p-126f);
+        const uint64_t s0 = pk2(k0, k0);
         const uint64_t s1 = pk2(key.y * unit_s, key.y * unit_s);
         const uint64_t m0 = pk2(key.z * unit_s, key.z * unit_s);
         const uint64_t m1 = pk2(key.w * unit_s, key.w * unit_s);
@@ -559,15 +591,6 @@ __global__ void __launch_bounds__(kThr, 1)
             y = fma2(s1, pk2(a1[2 * e], a1[2 * e + 1]), y);
             l[e] = fma2(s0, pk2(a0[2 * e], a0[2 * e + 1]), y);
           }
-          if (mask) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int2 lim = *reinterpret_cast<const int2 *>(&S.limit[8 * k + 2 * e]);
-              float u, v;
-              upk2(l[e], u, v);
-              l[e] = pk2(row > lim.x ? -INFINITY : u, row > lim.y ? -INFINITY : v);
-            }
-          }
         };
         // P of the tile against the present references; true if one is too large.
         // `again`: the references were raised; columns whose sums hold the tile
@@ -581,7 +604,7 @@ __global__ void __launch_bounds__(kThr, 1)
           for (int k = 0; k < CH; ++k) {
             uint64_t l[4];
             uint32_t w[4];
-            tmem_landed();
+            tmem_landed(a0, a1);
             logits(k, true, a0, a1, l);
             if (k + 1 < CH) {  // the next columns come while these are worked on
               tmem_ld8(ts + 8 * k + 8, a0);
@@ -826,6 +849,409 @@ __global__ void __launch_bounds__(kThr, 1)
   if (warp == kSoft) tmem_dealloc(tm, kCols);
 }
 
+// ---- accumulated weights -----------------------------------------------------
+
+// Adds to each row's score what the attention's columns gave it: 2^(logit - top)
+// / (z G) over all columns, from their statistics.  K alone is read, once for all
+// columns (kScoreCols at a time); S comes as in the attention, and as a thread has a
+// token, its sum needs no other thread but the one of the other group, which has
+// the odd column tiles.
+constexpr int kScoreTiles = 4;
+constexpr int kScoreCols = kScoreTiles * kMaxN;
+constexpr int kScoreThr = 32 * (kSoft + 4 + 1);
+constexpr uint32_t kScoreColK = 256;  // of tensor memory: S (2 x 2 x 64), K (2 x 64)
+
+struct __align__(16) ScoreSide {
+  float4 key[2][kTok];              // s0, s1, m0, m1 of a token's key
+  float4 qs[kScoreCols / 2];        // sums of q: group 0 of two columns, group 1
+  float4 ref[kScoreCols / 2];       // minus the references of two columns, 1 / (z G)
+  int limit[kScoreCols];
+  float part[2][kTok];
+  float qmax[kSoft];
+  uint64_t raw_full[kRing], kf[2], k_free[2], t_free[2], sf[2], s_free[2], qf, drain;
+  uint32_t tmem;
+  int abort;
+};
+constexpr uint32_t kScoreOffRaw = kScoreCols * 256, kScoreOffSide = kScoreOffRaw + kRing * kRaw;
+constexpr uint32_t kScoreSmem = kScoreOffSide + sizeof(ScoreSide);
+static_assert(kScoreSmem <= 227 * 1024, "shared memory");
+
+template <int CH>
+__global__ void __launch_bounds__(kScoreThr, 1)
+    tile_score_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ Seqs sq,
+                      const __grid_constant__ TilePlan plan) {
+  constexpr int N = 8 * CH;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  unsigned char *smem = smem_raw;
+  ScoreSide &S = *reinterpret_cast<ScoreSide *>(smem + kScoreOffSide);
+  const View &c = p.k.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t base = smem_u32(smem);
+  volatile int *abort = &S.abort;
+  auto wait = [&](uint64_t &bar, int n) {
+    return warp_wait(smem_u32(&bar), (uint32_t)(n & 1), abort);
+  };
+  auto give_up = [&]() {
+    if (lane == 0) {
+      if (!*abort) atomicOr(c.err, ERR_TIMEOUT);
+      *abort = 1;
+    }
+  };
+  if (warp == kSoft) tmem_alloc(smem_u32(&S.tmem), kCols);
+  if (tid == 0) {
+    for (int b = 0; b < kRing; ++b) mbar_init(smem_u32(&S.raw_full[b]), 1);
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&S.kf[b]), 4);
+      mbar_init(smem_u32(&S.k_free[b]), 1);
+      mbar_init(smem_u32(&S.t_free[b]), kSoft);
+      mbar_init(smem_u32(&S.sf[b]), 1);
+      mbar_init(smem_u32(&S.s_free[b]), kSoft / 2);
+    }
+    mbar_init(smem_u32(&S.qf), 1);
+    mbar_init(smem_u32(&S.drain), 1);
+    S.abort = 0;
+    fence_mbar_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+
+  // Spans of the list of all units' tiles; a unit's columns are taken kScoreCols at a
+  // time by the CTA that has its tiles.
+  Walk walk{sq, p.k.nl * c.H, 0};
+  const int from = blockIdx.x * plan.span;
+  walk.last = min(from + plan.span, plan.base[p.k.n]);
+  TileRun first;
+  int lo = 0, hi = p.k.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (plan.base[mid] <= from) lo = mid; else hi = mid;
+  }
+  first.s = lo;
+  first.np = Walk::tiles_of(blocks_of(sq.len[lo]));
+  const int rest = from - plan.base[lo], cost = kSwitch + first.np;
+  first.item = rest / cost;
+  first.at = plan.base[lo] + first.item * cost;
+  first.t0 = max(0, from - first.at - kSwitch);
+  first.t1 = min(first.np, walk.last - first.at - kSwitch);
+  const bool any = first.t1 > first.t0;
+  pdl_begin();
+  const uint32_t tm = S.tmem;
+  // A run's passes over its tiles, and the column tiles of pass g.
+  auto passes_of = [&](const TileRun &r) {
+    return (sq.count[r.s] * c.G + kScoreTiles * N - 1) / (kScoreTiles * N);
+  };
+  auto chunks_of = [&](const TileRun &r, int g) {
+    return min(kScoreTiles, (sq.count[r.s] * c.G - g * kScoreTiles * N + N - 1) / N);
+  };
+  // With one column tile the groups take turns by tile, else by column tile.
+  auto owner = [](int chunks, int tile, int ch) { return (chunks == 1 ? tile : ch) & 1; };
+
+  if (!any) {
+    // no work
+  } else if (warp == kSoft + 4) {
+    // ---- issuer
+    const uint32_t id_s = idesc_f16(kTok, N, false);
+    const uint64_t dq = sdesc_sw128(base, 16, 1024);
+    int i = 0, passes = 0, m[2] = {0, 0};
+    bool ok = true;
+    TileRun run = first;
+    do {
+      const int np = passes_of(run);
+      for (int g = 0; g < np && ok; ++g, ++passes) {
+        const int chunks = chunks_of(run, g);
+        ok = wait(S.qf, passes);
+        for (int t = run.t0; t < run.t1 && ok; ++t, ++i) {
+          ok = wait(S.kf[i & 1], i / 2);
+          for (int ch = 0; ch < chunks && ok; ++ch) {
+            const int w = owner(chunks, i, ch);
+            if (m[w] > 0) ok = wait(S.s_free[w], m[w] - 1);
+            if (!ok) break;
+            tc_fence_after();
+            if (lane == 0) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  tc_mma_ts(tm + w * 128 + j * 64, tm + kScoreColK + (i & 1) * 64 + j * 32 + k * 8,
+                            dq + (uint64_t)(((ch * 2 + j) * N * 128 + k * 32) >> 4), id_s, k > 0);
+              tc_commit(smem_u32(&S.sf[w]));
+              if (ch + 1 == chunks) tc_commit(smem_u32(&S.k_free[i & 1]));
+            }
+            __syncwarp();
+            ++m[w];
+          }
+        }
+      }
+    } while (ok && walk.next(run));
+    if (!ok) give_up();
+    if (lane == 0) {  // every product is done before tensor memory is freed
+      volatile int never = 0;
+      tc_commit(smem_u32(&S.drain));
+      mbar_wait(smem_u32(&S.drain), 0, &never);
+    }
+  } else if (warp >= kSoft) {
+    // ---- dequant: a token a thread, K's half of the raw blocks alone
+    const int dt = tid - 32 * kSoft, dw = warp - kSoft;
+    int i = 0, issued = 0;
+    bool ok = true, more = true;
+    TileRun ahead = first, run = first;
+    int ahead_t = first.t0, ahead_g = 0;
+    auto skip_empty = [&]() {  // runs without a token have no pass
+      while (more && passes_of(ahead) == 0) {
+        more = walk.next(ahead);
+        ahead_t = ahead.t0;
+      }
+    };
+    auto load_next = [&]() {  // dt == 0
+      if (!more) return;
+      const int nb = min(kTileBlocks, blocks_of(sq.len[ahead.s]) - ahead_t * kTileBlocks);
+      const uint32_t bar = smem_u32(&S.raw_full[issued % kRing]);
+      constexpr uint32_t kCodes = kBlock * kD / 2, kMeta = kBlock * (kD / kGroup) * 4;
+      mbar_expect_tx(bar, (uint32_t)nb * (kCodes + kMeta));
+      const int unit = ahead.item;
+      const uint8_t *at =
+          c.blocks + unit_at(c, p.k.s0 + ahead.s, p.k.lb, unit / c.H, unit % c.H) * c.nb *
+                         (size_t)block_bytes(kD) +
+          (size_t)ahead_t * kRaw;
+      const uint32_t to = base + kScoreOffRaw + (issued % kRing) * kRaw;
+      for (int b = 0; b < nb; ++b) {
+        bulk_load(to + b * block_bytes(kD), at + b * block_bytes(kD), kCodes, bar);
+        bulk_load(to + b * block_bytes(kD) + km_off(kD), at + b * block_bytes(kD) + km_off(kD),
+                  kMeta, bar);
+      }
+      ++issued;
+      if (++ahead_t == ahead.t1) {
+        ahead_t = ahead.t0;
+        if (++ahead_g == passes_of(ahead)) {
+          ahead_g = 0;
+          more = walk.next(ahead);
+          ahead_t = ahead.t0;
+          skip_empty();
+        }
+      }
+    };
+    if (dt == 0) {
+      skip_empty();
+      for (int j = 0; j < kRing; ++j) load_next();
+    }
+    do {
+      const int len = sq.len[run.s], np = passes_of(run);
+      for (int g = 0; g < np && ok; ++g)
+        for (int t = run.t0; t < run.t1; ++t, ++i) {
+          const int b = i & 1, rb = i % kRing;
+          const unsigned char *blk = smem + kScoreOffRaw + rb * kRaw + (dt / kBlock) * block_bytes(kD);
+          ok = ok && wait(S.raw_full[rb], i / kRing) &&
+               (i < 2 || (wait(S.t_free[b], i / 2 - 1) && wait(S.k_free[b], i / 2 - 1)));
+          ok = !bar_any(1, 128, !ok);
+          if (!ok) break;
+          if (dt == 0 && i > 0) load_next();  // in the place of tile i - 1
+          tc_fence_after();
+          const int r = dt % kBlock;
+          uint2 km = *reinterpret_cast<const uint2 *>(blk + km_off(kD) + r * 8);
+          if (t * kTok + dt >= len) km = make_uint2(0, 0);
+          S.key[b][dt] = make_float4(s_of(km.x), s_of(km.y), m_of(km.x), m_of(km.y));
+          uint4 w[4];
+#pragma unroll
+          for (int t4 = 0; t4 < 4; ++t4)
+            w[t4] = *reinterpret_cast<const uint4 *>(blk + k_off() + r * (kD / 2) +
+                                                     k_chunk(r, t4) * 16);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t o[32];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              const uint4 &c4 = w[x >> 1];
+              const uint32_t v = j == 0 ? (x & 1 ? c4.y : c4.x) : (x & 1 ? c4.w : c4.z);
+              even_fields(v, o + 4 * x);
+            }
+            tmem_st32(tm + ((uint32_t)(dw * 32) << 16) + kScoreColK + b * 64 + j * 32, o);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&S.kf[b]));
+        }
+    } while (ok && walk.next(run));
+    if (!ok) give_up();
+    if (dt == 0) {  // every copy lands before the shared memory is given back
+      volatile int never = 0;
+      for (int j = max(0, issued - kRing); j < issued; ++j)
+        mbar_wait(smem_u32(&S.raw_full[j % kRing]), (uint32_t)((j / kRing) & 1), &never);
+    }
+  } else {
+    // ---- sums
+    const int wq = warp & 3, grp = warp >> 2, tok = wq * 32 + lane;
+    const uint32_t ts = tm + grp * 128 + ((uint32_t)(wq * 32) << 16);
+    auto all_ok = [&](bool ok) { return !bar_any(2, 32 * kSoft, !ok); };
+    int i = 0, m = 0;
+    bool ok = true, more = true;
+    TileRun run = first;
+    do {
+      const int lr = run.item / c.H, h = run.item % c.H;
+      const int len = sq.len[run.s], count = sq.count[run.s];
+      const size_t call_unit = ((size_t)(p.k.s0 + run.s) * p.k.nl + lr) * c.H + h;
+      float *score = c.score + unit_at(c, p.k.s0 + run.s, p.k.lb, lr, h) * c.sstride;
+      const int np = passes_of(run);
+      for (int g = 0; g < np; ++g) {
+        const int chunks = chunks_of(run, g), col0 = g * kScoreTiles * N;
+        // ---- the pass's queries, scaled by one power of two for all columns
+        if (tid < chunks * N) {
+          const int col = col0 + tid, k = tid >> 1;
+          const Place a = place_of(p, sq, run.s, lr, h, col);
+          const bool live = a.out >= 0 && a.live;
+          const float2 st = live ? reinterpret_cast<const float2 *>(
+                                       p.stats)[call_unit * (p.n_q * c.G) + a.stat]
+                                 : make_float2(-kNone, 0.f);
+          S.limit[tid] = live ? len - count + col / c.G : -1;
+          float *ref = reinterpret_cast<float *>(&S.ref[k]) + (tid & 1);
+          ref[0] = -st.x;
+          ref[2] = st.y;
+        }
+        float top = 0.f;
+        const int ci = tid & 15;
+        auto load_q = [&](int col, float (&x)[8]) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = 0.f;
+          const Place a = place_of(p, sq, run.s, lr, h, col0 + col);
+          if (a.out < 0 || !a.live) return;
+          const uint4 w = *reinterpret_cast<const uint4 *>(
+              static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci);
+          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(ws[e] << 16);
+            x[2 * e + 1] = __uint_as_float(ws[e] & 0xFFFF0000u);
+          }
+        };
+#pragma unroll 2
+        for (int col = tid >> 4; col < chunks * N; col += 16) {
+          float x[8];
+          load_q(col, x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (fabsf(x[e]) < INFINITY) top = fmaxf(top, fabsf(x[e]));
+        }
+        top = dev::warp_max(top);
+        if (lane == 0) S.qmax[warp] = top;
+        ok = all_ok(ok);
+        if (!ok) break;
+#pragma unroll
+        for (int w = 0; w < kSoft; ++w) top = fmaxf(top, S.qmax[w]);
+        int k2 = 14 - ((int)(__float_as_uint(top) >> 23) - 127);
+        k2 = top == 0.f ? 0 : max(-90, min(k2, 100));
+        const float up = __uint_as_float((unsigned)(127 + k2) << 23);
+        constexpr float kEvenUnit = 0x1p20f;
+        const float unit_s =
+            kEvenUnit * __uint_as_float((unsigned)(127 - k2) << 23) * (c.scale * kLog2e);
+#pragma unroll 2
+        for (int col = tid >> 4; col < chunks * N; col += 16) {
+          float x[8], sum = 0.f;
+          load_q(col, x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[e] *= up;
+            sum += x[e];
+          }
+          const int ch = col / N, cc = col % N;
+          sts128(base + (ch * 2 + (ci >> 3)) * N * 128 + cc * 128 + (((ci & 7) ^ (cc & 7)) << 4),
+                 half2_bits(__floats2half2_rn(x[0], x[4])),
+                 half2_bits(__floats2half2_rn(x[1], x[5])),
+                 half2_bits(__floats2half2_rn(x[2], x[6])),
+                 half2_bits(__floats2half2_rn(x[3], x[7])));
+#pragma unroll
+          for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          if ((ci & 7) == 0) {
+            float *q = reinterpret_cast<float *>(&S.qs[col >> 1]) + 2 * (ci >> 3) + (col & 1);
+            *q = sum * (1.f / kEvenUnit);
+          }
+        }
+        fence_proxy_async();
+        ok = all_ok(ok);
+        if (!ok) break;
+        if (tid == 0) mbar_arrive(smem_u32(&S.qf));
+
+        // rows up to the first of the pass's tokens are seen by all its columns
+        const int all_rows = len - count + col0 / c.G + 1;
+        for (int t = run.t0; t < run.t1; ++t, ++i) {
+          const int b = i & 1, row = t * kTok + tok;
+          const bool mask = (t + 1) * kTok > all_rows;
+          if (ok) ok = wait(S.kf[b], i / 2);
+          const float4 key = S.key[b][tok];
+          uint64_t sum[2] = {0, 0};
+          bool mine = false;
+#pragma unroll 1
+          for (int ch = 0; ch < chunks; ++ch) {
+            if (owner(chunks, i, ch) != grp) continue;
+            mine = true;
+            if (ok) ok = wait(S.sf[grp], m);
+            if (!ok) break;
+            ++m;
+            tc_fence_after();
+            const float4 *qs = S.qs + ch * (N / 2), *ref = S.ref + ch * (N / 2);
+            float4 y = key;
+            if (mask) mask_row(ts, N, S.limit + ch * N, row, y);
+            const float k0 = fmaxf(y.x * unit_s, 0x1p-126f), k1 = y.y * unit_s;
+            const uint64_t s0 = pk2(k0, k0), s1 = pk2(k1, k1);
+            const uint64_t m0 = pk2(y.z * unit_s, y.z * unit_s);
+            const uint64_t m1 = pk2(y.w * unit_s, y.w * unit_s);
+            float a0[8], a1[8];
+            tmem_ld8(ts, a0);
+            tmem_ld8(ts + 64, a1);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+              uint64_t l[4], inv[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float4 f = ref[4 * k + e], q = qs[4 * k + e];
+                inv[e] = pk2(f.z, f.w);
+                l[e] = fma2(m1, pk2(q.z, q.w), fma2(m0, pk2(q.x, q.y), pk2(f.x, f.y)));
+              }
+              tmem_landed(a0, a1);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                l[e] = fma2(s0, pk2(a0[2 * e], a0[2 * e + 1]),
+                            fma2(s1, pk2(a1[2 * e], a1[2 * e + 1]), l[e]));
+              if (k + 1 < CH) {
+                tmem_ld8(ts + 8 * k + 8, a0);
+                tmem_ld8(ts + 64 + 8 * k + 8, a1);
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float u, v;
+                upk2(l[e], u, v);
+                sum[e & 1] = fma2(pk2(ex2(u), ex2(v)), inv[e], sum[e & 1]);
+              }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&S.s_free[grp]));
+          }
+          float u, v;
+          upk2(add2(sum[0], sum[1]), u, v);
+          float add = u + v;
+          if (chunks > 1) {
+            if (grp == 1) S.part[b][tok] = add;
+            ok = all_ok(ok);
+            if (!ok) break;
+            if (grp == 0) add += S.part[b][tok];
+            mine = grp == 0;
+          }
+          if (mine && row < len) score[row] += add;
+          if (lane == 0) mbar_arrive(smem_u32(&S.t_free[b]));
+        }
+        ok = all_ok(ok);  // the pass's arrays are free again
+        if (!ok) break;
+      }
+      if (ok) more = walk.next(run);
+    } while (ok && more);
+    if (!ok) give_up();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kSoft) tmem_dealloc(tm, kCols);
+}
+
 int tile_n(const View &c, int n_q) {
   const long long rows = (long long)n_q * c.G, tiles = (rows + kMaxN - 1) / kMaxN;
   return (int)(((rows + tiles - 1) / tiles + 15) / 16 * 16);
@@ -882,6 +1308,44 @@ cudaError_t launch_ch(const AttendParams &p, const Seqs &q, cudaStream_t stream)
   }
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
   return launch_pdl(kern, dim3((unsigned)grid), dim3(kThr), kSmem, stream, p, q, plan);
+}
+
+template <int CH>
+cudaError_t launch_score_ch(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+  const View &c = p.k.c;
+  auto kern = tile_score_kernel<CH>;
+  static int sms = 0;
+  if (!sms) {
+    int dev = 0, n = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kScoreSmem);
+    if (e != cudaSuccess) return e;
+    sms = n;
+  }
+  TilePlan plan;
+  plan.tiles = 1;
+  long long total = 0;
+  for (int i = 0; i < p.k.n; ++i) {
+    plan.base[i] = (int32_t)std::min<long long>(total, INT32_MAX);
+    total += (long long)p.k.nl * c.H *
+             (kSwitch + (blocks_of(q.len[i]) + kTileBlocks - 1) / kTileBlocks);
+  }
+  if (total > INT32_MAX) return cudaErrorInvalidValue;
+  plan.base[p.k.n] = (int32_t)total;
+  plan.span = (int32_t)std::max<long long>(kSwitch + 1, (total + sms - 1) / sms);
+  return launch_pdl(kern, dim3((unsigned)((total + plan.span - 1) / plan.span)), dim3(kScoreThr),
+                    kScoreSmem, stream, p, q, plan);
+}
+
+cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+  switch (tile_n(p.k.c, p.n_q)) {
+    case 16: return launch_score_ch<2>(p, q, stream);
+    case 32: return launch_score_ch<4>(p, q, stream);
+    case 48: return launch_score_ch<6>(p, q, stream);
+    default: return launch_score_ch<8>(p, q, stream);
+  }
 }
 
 cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
