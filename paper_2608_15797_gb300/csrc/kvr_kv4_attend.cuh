@@ -21,13 +21,9 @@ __host__ __device__ inline int blocks_of(int len) {
   return len > kBlock ? (len + kBlock - 1) / kBlock : 1;
 }
 
-// A whole warp's bounded wait for a phase of a barrier: one lane asks, since each
-// lane's question is a turn of its own at the barrier (230 cycles for 32 of them,
-// and all other traffic of shared memory waits behind).
+// A whole warp's bounded wait for a phase of a barrier.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort) {
-  int ok = 1;
-  ok = mbar_wait_idle(bar, parity, abort);
-  return __all_sync(0xffffffffu, ok);
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
 }
 
 // Where a column's result goes.

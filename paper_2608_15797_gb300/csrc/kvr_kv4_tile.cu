@@ -40,9 +40,18 @@ constexpr int kD = 128;
 constexpr int kTok = 128;                   // tokens of a tile
 constexpr int kTileBlocks = kTok / kBlock;
 constexpr int kMaxN = 64;                   // columns of a tile
-constexpr int kSoft = 8, kDeq = 7;          // warps
-constexpr int kThr = 32 * (kSoft + kDeq + 1);
-constexpr int kRing = 3;                    // raw tiles in flight
+// Warps, in warpgroups of four: softmax (two), K, V, and one with the issuer and the
+// loader.
+constexpr int kSoft = 8, kKey = 4, kVal = 4;
+constexpr int kIssuer = kSoft + kKey + kVal, kLoader = kIssuer + 1;
+constexpr int kThr = 32 * (kIssuer + 4);
+// Registers a thread: at launch, then for the softmax and for the others.
+constexpr int kRegs = 96, kRegsSoft = 144, kRegsRest = 64;
+static_assert(32 * kSoft * kRegsSoft + (kThr - 32 * kSoft) * kRegsRest <= kThr * kRegs,
+              "the shares come out of what the CTA was launched with");
+constexpr int kRing = 4;                    // raw tiles in flight
+static_assert(kVal == kTileBlocks && kKey == 4, "a warp's 32 tokens");
+constexpr int kConst = 4;                   // tiles whose tokens' constants are held
 constexpr int kTileGrid = 256;              // CTAs of a split call, at most
 constexpr uint32_t kRaw = kTileBlocks * block_bytes(kD);
 constexpr uint32_t kHalf = kTok * 128;      // one 64-element half of an operand
@@ -62,9 +71,9 @@ struct TilePlan {
 };
 
 struct __align__(16) Side {
-  float4 key[2][kTok];          // s0, s1, m0, m1 of a token's key
-  float2 val[2][kTok];          // e + 1, 2^-(e + 1) of its value
-  uint2 vc[2][2][kTok / 2];     // [.][group][pair]: s 2^(18 - e - 1), m 2^-(e + 1), halves
+  float4 key[kConst][kTok];     // s0, s1, m0, m1 of a token's key
+  float2 val[kConst][kTok];     // e + 1, 2^-(e + 1) of its value
+  uint2 vc[2][kTok / 2];        // [group][pair]: s 2^(18 - e - 1), m 2^-(e + 1), halves
   float4 qs[kMaxN / 2];         // sums of q: group 0 of two columns, group 1
   // of the even and the odd tiles:
   float ntop[2][kMaxN];         // minus the columns' references
@@ -75,8 +84,9 @@ struct __align__(16) Side {
   float2 stat[kMaxN];
   Place place[kMaxN];
   float qmax[kSoft];
-  int nan_row[4][2];            // [run % 4][group]: first row whose value is NaN
-  uint64_t raw_full[kRing], kf[2], vf[2], pv[2], sf[2], s_free[2], pf[2], qf, drain;
+  int nan_row[16][2];           // [run % 16][group]: first row whose value is NaN
+  uint64_t raw_full[kRing], raw_free[kRing];
+  uint64_t cf[kConst], c_free[kConst], kf[2], vf[2], pv[2], sf[2], s_free[2], pf[2], qf, drain;
   uint32_t tmem;
   int abort, flag;
 };
@@ -122,6 +132,19 @@ __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint
                                        uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d));
 }
+// True for one lane of a whole warp.  (The tensor cores' instructions take their
+// operands from uniform registers; under lane == 0 eight products took the issuer
+// some 1,000 cycles.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t y;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+               : "=r"(y));
+  return y != 0;
+}
+// Gives registers of a warpgroup to the softmax.
+__device__ __forceinline__ void give_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+}
 // As tmem_wait_ld, but only what was loaded waits: memory's loads may pass it.
 __device__ __forceinline__ void tmem_landed(float (&a)[8], float (&b)[8]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -153,7 +176,15 @@ __device__ __forceinline__ uint32_t half2_bits(__half2 x) {
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2 *>(&x); }
 
-// The pairs of nibbles 0 4, 1 5, 2 6, 3 7 of a word as half-precision c 2^-20, on which
+// The pairs of nibbles 0 4, 1 5, 2 6, 3 7 of a word as half-precision c 2^-24, the odd
+// ones 2^4 times that.
+__device__ __forceinline__ void rough_fields(uint32_t x, uint32_t *f) {
+  f[0] = x & 0x000F000Fu;
+  f[1] = x & 0x00F000F0u;
+  f[2] = (x >> 8) & 0x000F000Fu;
+  f[3] = (x >> 8) & 0x00F000F0u;
+}
+// As half-precision c 2^-20 all, on which
 // the tensor core keeps its full precision.
 __device__ __forceinline__ void even_fields(uint32_t x, uint32_t *f) {
   f[0] = (x << 4) & 0x00F000F0u;
@@ -211,10 +242,17 @@ __global__ void __launch_bounds__(kThr, 1)
   };
   if (warp == kSoft) tmem_alloc(smem_u32(&S.tmem), kCols);
   if (tid == 0) {
-    for (int b = 0; b < kRing; ++b) mbar_init(smem_u32(&S.raw_full[b]), 1);
+    for (int b = 0; b < kRing; ++b) {
+      mbar_init(smem_u32(&S.raw_full[b]), 1);
+      mbar_init(smem_u32(&S.raw_free[b]), kKey + kVal);
+    }
+    for (int b = 0; b < kConst; ++b) {
+      mbar_init(smem_u32(&S.cf[b]), kKey + kVal);
+      mbar_init(smem_u32(&S.c_free[b]), kSoft / 2);
+    }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(smem_u32(&S.kf[b]), 4);
-      mbar_init(smem_u32(&S.vf[b]), kDeq);
+      mbar_init(smem_u32(&S.kf[b]), kKey);
+      mbar_init(smem_u32(&S.vf[b]), kVal);
       mbar_init(smem_u32(&S.pv[b]), 1);
       mbar_init(smem_u32(&S.sf[b]), 1);
       mbar_init(smem_u32(&S.s_free[b]), kSoft / 2);
@@ -223,7 +261,7 @@ __global__ void __launch_bounds__(kThr, 1)
     mbar_init(smem_u32(&S.qf), 1);
     mbar_init(smem_u32(&S.drain), 1);
     S.abort = 0;
-    for (int i = 0; i < 4; ++i) S.nan_row[i][0] = S.nan_row[i][1] = INT32_MAX;
+    for (int i = 0; i < 16; ++i) S.nan_row[i][0] = S.nan_row[i][1] = INT32_MAX;
     fence_mbar_init();
   }
   tc_fence_before();
@@ -270,7 +308,9 @@ __global__ void __launch_bounds__(kThr, 1)
 
   if (!any) {
     // no work
-  } else if (warp == kSoft + kDeq) {
+  } else if (warp >= kIssuer) {
+    give_registers();
+    if (warp == kIssuer) {
     // ---- issuer
     const uint32_t id_s = idesc_f16(kTok, N, false), id_o = idesc_f16(kD, N, true);
     const uint64_t dq = sdesc_sw128(base + kOffQ, 16, 1024);
@@ -282,7 +322,7 @@ __global__ void __launch_bounds__(kThr, 1)
       ok = ok && wait(S.vf[j & 1], j / 2) && wait(S.pf[j & 1], j / 2);
       if (!ok) return;
       tc_fence_after();
-      if (lane == 0) {
+      if (elect_one()) {
         const uint64_t a = dv + (uint64_t)(((j & 1) * 2 * kHalf) >> 4);
         const uint64_t b = dp + (uint64_t)(((j & 1) * kHalf) >> 4);
 #pragma unroll
@@ -295,10 +335,11 @@ __global__ void __launch_bounds__(kThr, 1)
     };
     do {
       for (int t = run.t0; t < run.t1 && ok; ++t, ++i) {
-        ok = (t > run.t0 || wait(S.qf, runs)) && wait(S.kf[i & 1], i / 2);
+        ok = (t > run.t0 || wait(S.qf, runs)) && wait(S.kf[i & 1], i / 2) &&
+             (i < 2 || wait(S.s_free[i & 1], i / 2 - 1));
         if (!ok) break;
         tc_fence_after();
-        if (lane == 0) {
+        if (elect_one()) {
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -319,158 +360,185 @@ __global__ void __launch_bounds__(kThr, 1)
       tc_commit(smem_u32(&S.drain));
       mbar_wait(smem_u32(&S.drain), 0, &never);
     }
-  } else if (warp >= kSoft) {
-    // ---- dequant
-    const int dt = tid - 32 * kSoft, dw = warp - kSoft;
+    } else if (warp == kLoader) {
+    // ---- loader: raw tiles, kRing ahead of their use
+    int issued = 0;
+    bool ok = true;
+    do {
+      const int unit = run.item / plan.tiles;
+      const uint8_t *blocks =
+          c.blocks + unit_at(c, p.k.s0 + run.s, p.k.lb, unit / c.H, unit % c.H) * c.nb *
+                         (size_t)block_bytes(kD);
+      const int nb = blocks_of(sq.len[run.s]);
+      for (int t = run.t0; t < run.t1 && ok; ++t) {
+        const int rb = issued % kRing;
+        if (issued >= kRing) ok = wait(S.raw_free[rb], issued / kRing - 1);
+        if (!ok) break;
+        if (lane == 0) {
+          const uint32_t bytes =
+              (uint32_t)min(kTileBlocks, nb - t * kTileBlocks) * block_bytes(kD);
+          mbar_expect_tx(smem_u32(&S.raw_full[rb]), bytes);
+          bulk_load(base + kOffRaw + rb * kRaw, blocks + (size_t)t * kRaw, bytes,
+                    smem_u32(&S.raw_full[rb]));
+        }
+        __syncwarp();
+        ++issued;
+      }
+    } while (ok && walk.next(run));
+    if (!ok) give_up();
+    if (lane == 0) {  // every copy lands before the shared memory is given back
+      volatile int never = 0;
+      for (int j = max(0, issued - kRing); j < issued; ++j)
+        mbar_wait(smem_u32(&S.raw_full[j % kRing]), (uint32_t)((j / kRing) & 1), &never);
+    }
+    }
+  } else if (warp >= kSoft + kKey) {
+    // ---- V
+    give_registers();
+    const int vw = warp - kSoft - kKey, vt = tid - 32 * (kSoft + kKey);
     int i = 0, runs = 0;
     bool ok = true;
-    // Loads, kRing tiles ahead: `ahead` walks before the work, and a tile's place is
-    // free once all of the role has passed the next tile's barrier.
-    TileRun ahead = run;
-    int ahead_t = run.t0, issued = 0;
-    bool more = true;
-    auto load_next = [&]() {  // dt == 0
-      if (!more) return;
-      const uint32_t bytes =
-          (uint32_t)min(kTileBlocks, blocks_of(sq.len[ahead.s]) - ahead_t * kTileBlocks) *
-          block_bytes(kD);
-      const uint32_t bar = smem_u32(&S.raw_full[issued % kRing]);
-      mbar_expect_tx(bar, bytes);
-      bulk_load(base + kOffRaw + (issued % kRing) * kRaw,
-                c.blocks + unit_of(ahead) * c.nb * (size_t)block_bytes(kD) +
-                    (size_t)ahead_t * kRaw,
-                bytes, bar);
-      ++issued;
-      if (++ahead_t == ahead.t1) {
-        more = walk.next(ahead);
-        ahead_t = ahead.t0;
-      }
-    };
-    if (dt == 0)
-      for (int j = 0; j < kRing; ++j) load_next();
     do {
       const int len = sq.len[run.s];
       for (int t = run.t0; t < run.t1; ++t, ++i) {
-        const int b = i & 1, rb = i % kRing;
+        const int b = i & 1, cb = i % kConst, rb = i % kRing;
         const unsigned char *raw = smem + kOffRaw + rb * kRaw;
-        const uint32_t raw_at = base + kOffRaw + rb * kRaw;
-        ok = ok && wait(S.raw_full[rb], i / kRing) && (i < 2 || wait(S.s_free[b], i / 2 - 1));
-        // Tokens' constants, a thread a token.
-        if (ok && dt < kTok) {
-          const unsigned char *blk = raw + (dt / kBlock) * block_bytes(kD);
-          const int r = dt % kBlock, row = t * kTok + dt;
-          uint2 km = *reinterpret_cast<const uint2 *>(blk + km_off(kD) + r * 8);
-          uint2 vm = *reinterpret_cast<const uint2 *>(blk + vm_off(kD) + r * 8);
-          if (row >= len) km = vm = make_uint2(0, 0);
-          S.key[b][dt] = make_float4(s_of(km.x), s_of(km.y), m_of(km.x), m_of(km.y));
+        ok = ok && wait(S.raw_full[rb], i / kRing) &&
+             (i < kConst || wait(S.c_free[cb], i / kConst - 1));
+        if (!ok) break;
+        // The slot of eight runs ahead: none of this role has reached it, and the
+        // softmax, at most four tiles behind, has left the run that had it.
+        if (vt == 0 && t == run.t0)
+          S.nan_row[(runs + 8) & 15][0] = S.nan_row[(runs + 8) & 15][1] = INT32_MAX;
+        {  // a token's constants
+          const int row = t * kTok + vt;
+          uint2 vm = *reinterpret_cast<const uint2 *>(raw + vw * block_bytes(kD) + vm_off(kD) +
+                                                      lane * 8);
+          if (row >= len) vm = make_uint2(0, 0);
           float m[2] = {m_of(vm.x), m_of(vm.y)}, s[2] = {s_of(vm.x), s_of(vm.y)};
           float top = 0.f;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             if (m[g] != m[g]) {  // the group stands for NaN: told to those who see it
-              atomicMin(&S.nan_row[runs & 3][g], row);
+              atomicMin(&S.nan_row[runs & 15][g], row);
               m[g] = s[g] = 0.f;
             }
             top = fmaxf(top, fmaxf(fabsf(m[g]), fabsf(fmaf(15.f, s[g], m[g]))));
           }
           const int e = max(-60, min((int)(__float_as_uint(top) >> 23) - 127, 120)) + 1;
           const float down = __uint_as_float((unsigned)(127 - e) << 23);
-          S.val[b][dt] = make_float2((float)e, down);
+          S.val[cb][vt] = make_float2((float)e, down);
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            __half *h = reinterpret_cast<__half *>(&S.vc[b][g][dt >> 1]) + (dt & 1);
+            __half *h = reinterpret_cast<__half *>(&S.vc[g][vt >> 1]) + (vt & 1);
             h[0] = __float2half_rn(s[g] * down * 0x1p18f);
             h[2] = __float2half_rn(m[g] * down);
           }
         }
-        if (dt == 0 && t == run.t0) {
-          S.nan_row[(runs + 1) & 3][0] = INT32_MAX;
-          S.nan_row[(runs + 1) & 3][1] = INT32_MAX;
-        }
-        ok = !bar_any(1, 32 * kDeq, !ok);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.cf[cb]));
+        ok = i < 2 || wait(S.pv[b], i / 2 - 1);
         if (!ok) break;
-        if (dt == 0 && i > 0) load_next();  // in the place of tile i - 1
-        // K: a token a thread of the first four warps, into tensor memory (its place is
-        // free: S of tile i - 2, which was read, is the product it was for).  A
-        // word's fields are the pairs of nibbles 0 4, 1 5, 2 6, 3 7.
-        if (dw < 4) {
-          const unsigned char *at =
-              raw + (dt / kBlock) * block_bytes(kD) + k_off() + (dt % kBlock) * (kD / 2);
-          uint4 w[4];
+        // Eight tokens (tg) of chunk ch a lane, a channel group (w, w + 1) at a time; the
+        // warp's tokens are those of one block.
+        const int tg = vw * 4 + (lane >> 3), ch = lane & 7;
 #pragma unroll
-          for (int t4 = 0; t4 < 4; ++t4)
-            w[t4] = *reinterpret_cast<const uint4 *>(at + k_chunk(dt, t4) * 16);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {  // channels 64 j ..: words 2 j, 2 j + 1 of each chunk
-            uint32_t o[32];
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              const uint4 &c4 = w[x >> 1];
-              const uint32_t v = j == 0 ? (x & 1 ? c4.y : c4.x) : (x & 1 ? c4.w : c4.z);
-              const uint32_t y = v >> 8;
-              o[4 * x] = v & 0x000F000Fu;
-              o[4 * x + 1] = v & 0x00F000F0u;
-              o[4 * x + 2] = y & 0x000F000Fu;
-              o[4 * x + 3] = y & 0x00F000F0u;
-            }
-            tmem_st32(tm + ((uint32_t)(dw * 32) << 16) + kColK + b * 64 + j * 32, o);
-          }
-          tmem_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&S.kf[b]));
-        }
-        if (i >= 2) ok = ok && wait(S.pv[b], i / 2 - 1);
-        // V: eight tokens (tg) of chunk ch, word w, a lane
-        const uint32_t to0 = base + kOffV + b * 2 * kHalf;
-        // (sixteen tasks: one for a warp that had a part in K, four for the others)
-        static_assert(kDeq == 7, "tasks");
-        const int first_task = dw < 4 ? dw : 4 * dw - 12, tasks = dw < 4 ? 1 : 4;
-#pragma unroll 2
-        for (int wt = first_task; wt < first_task + tasks; ++wt) {
-          const int w = wt & 3, tg = (wt >> 2) * 4 + (lane >> 3), ch = lane & 7;
-          uint32_t v[4];
+        for (int w = 0; w < 4; w += 2) {
+          uint2 v[4];
           __half2 sc[4], mn[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const int pr = tg * 4 + k, pb = pr % (kBlock / 2);
-            const uint32_t at = raw_at + (pr / (kBlock / 2)) * block_bytes(kD) + v_off(kD) +
-                                pb * kD + v_chunk<kD>(pb, ch) * 16 + w * 4;
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[k]) : "r"(at));
-            const uint2 x = S.vc[b][w >> 1][pr];
+            v[k] = *reinterpret_cast<const uint2 *>(raw + vw * block_bytes(kD) + v_off(kD) + pb * kD +
+                                                    v_chunk<kD>(pb, ch) * 16 + w * 4);
+            const uint2 x = S.vc[w >> 1][pr];
             sc[k] = as_half2(x.x);
             mn[k] = as_half2(x.y);
           }
-          const uint32_t to = to0 + (tg >> 3) * kHalf + (32 * w + ch) * 128 +
-                              (((tg & 7) ^ ch) << 4);  // ch: the row within eight
+          // (ch: the row within eight)
+          const uint32_t to = base + kOffV + b * 2 * kHalf + (tg >> 3) * kHalf +
+                              (32 * w + ch) * 128 + (((tg & 7) ^ ch) << 4);
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            uint32_t o[4];
+          for (int z = 0; z < 2; ++z)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t x = v[k];
-              const uint32_t y =
-                  (f == 0 ? x << 6 : f == 1 ? x << 2 : f == 2 ? x >> 2 : x >> 6) & 0x03C003C0u;
-              o[k] = half2_bits(__hfma2(as_half2(y), sc[k], mn[k]));  // c 2^-18
+            for (int f = 0; f < 4; ++f) {
+              uint32_t o[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t x = z ? v[k].y : v[k].x;
+                const uint32_t y =
+                    (f == 0 ? x << 6 : f == 1 ? x << 2 : f == 2 ? x >> 2 : x >> 6) & 0x03C003C0u;
+                o[k] = half2_bits(__hfma2(as_half2(y), sc[k], mn[k]));  // c 2^-18
+              }
+              sts128(to + (32 * z + (f == 0 ? 0 : f == 1 ? 16 : f == 2 ? 8 : 24)) * 128, o[0],
+                     o[1], o[2], o[3]);
             }
-            sts128(to + (f == 0 ? 0 : f == 1 ? 16 : f == 2 ? 8 : 24) * 128, o[0], o[1], o[2],
-                   o[3]);
-          }
         }
         fence_proxy_async();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&S.vf[b]));
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&S.vf[b]));
+          mbar_arrive(smem_u32(&S.raw_free[rb]));
+        }
       }
       ++runs;
     } while (ok && walk.next(run));
     if (!ok) give_up();
-    if (dt == 0) {  // every copy lands before the shared memory is given back
-      volatile int never = 0;
-      for (int j = max(0, issued - kRing); j < issued; ++j)
-        mbar_wait(smem_u32(&S.raw_full[j % kRing]), (uint32_t)((j / kRing) & 1), &never);
-    }
+  } else if (warp >= kSoft) {
+    // ---- K: a token a thread, into tensor memory
+    give_registers();
+    const int dt = tid - 32 * kSoft, dw = warp - kSoft;
+    int i = 0;
+    bool ok = true;
+    do {
+      const int len = sq.len[run.s];
+      for (int t = run.t0; t < run.t1; ++t, ++i) {
+        const int b = i & 1, cb = i % kConst, rb = i % kRing;
+        const unsigned char *blk = smem + kOffRaw + rb * kRaw + (dt / kBlock) * block_bytes(kD);
+        // (its place is free once tile i - 2's product is there)
+        ok = ok && wait(S.raw_full[rb], i / kRing) && (i < 2 || wait(S.sf[b], i / 2 - 1)) &&
+             (i < kConst || wait(S.c_free[cb], i / kConst - 1));
+        if (!ok) break;
+        const int r = dt % kBlock;
+        uint2 km = *reinterpret_cast<const uint2 *>(blk + km_off(kD) + r * 8);
+        if (t * kTok + dt >= len) km = make_uint2(0, 0);
+        S.key[cb][dt] = make_float4(s_of(km.x), s_of(km.y), m_of(km.x), m_of(km.y));
+        uint4 w[4];
+#pragma unroll
+        for (int t4 = 0; t4 < 4; ++t4)
+          w[t4] = *reinterpret_cast<const uint4 *>(blk + k_off() + r * (kD / 2) +
+                                                   k_chunk(r, t4) * 16);
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&S.raw_free[rb]));
+          mbar_arrive(smem_u32(&S.cf[cb]));
+        }
+        tc_fence_after();
+        // A word's fields are the pairs of nibbles 0 4, 1 5, 2 6, 3 7; channels 64 j ..
+        // are words 2 j, 2 j + 1 of each chunk.
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint32_t o[16];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint4 &c4 = w[2 * y + (x >> 1)];
+              const uint32_t v = j == 0 ? (x & 1 ? c4.y : c4.x) : (x & 1 ? c4.w : c4.z);
+              rough_fields(v, o + 4 * x);
+            }
+            tmem_st16(tm + ((uint32_t)(dw * 32) << 16) + kColK + b * 64 + j * 32 + y * 16, o);
+          }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.kf[b]));
+      }
+    } while (ok && walk.next(run));
+    if (!ok) give_up();
   } else {
     // ---- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
     const int wq = warp & 3, grp = warp >> 2;
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     const int tok = wq * 32 + lane, gt = tid & 127;  // of the group's threads
@@ -481,6 +549,20 @@ __global__ void __launch_bounds__(kThr, 1)
     auto group_ok = [&](bool ok) { return !bar_any(3 + grp, 16 * kSoft, !ok); };
     int i = 0, runs = 0;  // i: tiles before the run
     bool ok = true, more = true;
+    // A run's queries, eight channels (ci) of every sixteenth column a thread.
+    const int ci = tid & 15;
+    uint4 raw[CH / 2];
+    auto load_q = [&](const TileRun &r) {
+      const int unit = r.item / plan.tiles, col0 = (r.item % plan.tiles) * N;
+#pragma unroll
+      for (int z = 0; z < CH / 2; ++z) {
+        const Place a = place_of(p, sq, r.s, unit / c.H, unit % c.H, col0 + (tid >> 4) + 16 * z);
+        raw[z] = a.out >= 0 && a.live ? *reinterpret_cast<const uint4 *>(
+                                            static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci)
+                                      : make_uint4(0, 0, 0, 0);
+      }
+    };
+    load_q(run);
     do {
       // ---- a run's queries, scaled by one power of two for all columns, and columns
       const int unit = run.item / plan.tiles, col0 = (run.item % plan.tiles) * N;
@@ -494,27 +576,18 @@ __global__ void __launch_bounds__(kThr, 1)
       }
       float x[CH / 2][8];
       float top = 0.f;
-      const int ci = tid & 15;
 #pragma unroll
       for (int z = 0; z < CH / 2; ++z) {
-        const int col = (tid >> 4) + 16 * z;
+        const uint32_t ws[4] = {raw[z].x, raw[z].y, raw[z].z, raw[z].w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[z][e] = 0.f;
-        const Place a = place_of(p, sq, run.s, lr, h, col0 + col);
-        if (a.out >= 0 && a.live) {
-          const uint4 w = *reinterpret_cast<const uint4 *>(
-              static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci);
-          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+        for (int e = 0; e < 4; ++e) {
+          x[z][2 * e] = __uint_as_float(ws[e] << 16);
+          x[z][2 * e + 1] = __uint_as_float(ws[e] & 0xFFFF0000u);
+        }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[z][2 * e] = __uint_as_float(ws[e] << 16);
-            x[z][2 * e + 1] = __uint_as_float(ws[e] & 0xFFFF0000u);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float y = fabsf(x[z][e]);
-            if (y < INFINITY) top = fmaxf(top, y);
-          }
+        for (int e = 0; e < 8; ++e) {
+          const float y = fabsf(x[z][e]);
+          if (y < INFINITY) top = fmaxf(top, y);
         }
       }
       top = dev::warp_max(top);
@@ -564,12 +637,15 @@ __global__ void __launch_bounds__(kThr, 1)
       const int many = run.t1 - run.t0;
       int mine = 0;  // tiles of the run that this group has taken
       for (int t = run.t0 + ((i ^ grp) & 1); t < run.t1; t += 2, ++mine) {
-        const int n = (i + t - run.t0) >> 1, row = t * kTok + tok;  // n: the group's tiles so far
-        if (ok) ok = wait(S.kf[grp], n) && wait(S.sf[grp], n);
+        const int at = i + t - run.t0, cb = at % kConst, row = t * kTok + tok;
+        const int n = at >> 1;  // the group's tiles so far
+        if (ok) ok = wait(S.cf[cb], at / kConst) && wait(S.sf[grp], n);
         if (ok && n > 0) ok = wait(S.pv[grp], n - 1);  // P's place, and O's
         tc_fence_after();
-        float4 key = S.key[grp][tok];
-        const float2 val = S.val[grp][tok];
+        float4 key = S.key[cb][tok];
+        const float2 val = S.val[cb][tok];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&S.c_free[cb]));
         if (ok && (t + 1) * kTok > full) mask_row(ts, N, S.limit, row, key);
         const float k0 = fmaxf(key.x * unit_s, 0x1p-126f);
         const uint64_t s0 = pk2(k0, k0);
@@ -630,7 +706,43 @@ __global__ void __launch_bounds__(kThr, 1)
           fence_proxy_async();
           return __hgt(__hmax(__low2half(most), __high2half(most)), __float2half_rn(32768.f));
         };
+        // The largest of column chunk k's logits over the warp's tokens, to `to`.
+        auto chunk_max = [&](int k, float *to) {
+          uint64_t l[4];
+          float a0[8], a1[8];
+          tmem_ld8(ts + 8 * k, a0);
+          tmem_ld8(ts + 64 + 8 * k, a1);
+          tmem_wait_ld();
+          logits(k, false, a0, a1, l);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float u[2];
+            upk2(l[e], u[0], u[1]);
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const unsigned o = dev::ord_bits(u[z] == u[z] ? u[z] : -INFINITY);
+              const unsigned most = __reduce_max_sync(0xffffffffu, o);
+              if (lane == 0)
+                to[8 * k + 2 * e + z] =
+                    __uint_as_float(most & 0x80000000u ? most & 0x7FFFFFFFu : ~most);
+            }
+          }
+        };
         bool grow = mine == 0;
+        if (grow && (t + 1) * kTok <= full) {
+          // A run's first references: a column's largest over 32 of the tokens will
+          // do, so that a warp has a quarter of the columns.
+          grow = false;
+          if (ok) {
+#pragma unroll 1
+            for (int k = wq; k < CH; k += 4) chunk_max(k, S.wmax[grp][0]);
+          }
+          ok = group_ok(ok);
+          if (!ok) break;
+          if (gt < N) ntop[gt] = -fmaxf(kNone, S.wmax[grp][0][gt]);
+          ok = group_ok(ok);
+          if (!ok) break;
+        }
         if (ok && !grow) {
           grow = probabilities(false);
           tc_fence_before();
@@ -640,27 +752,7 @@ __global__ void __launch_bounds__(kThr, 1)
           ok = group_ok(ok);
           if (!ok) break;
 #pragma unroll 1
-          for (int k = 0; k < CH; ++k) {
-            uint64_t l[4];
-            float a0[8], a1[8];
-            tmem_ld8(ts + 8 * k, a0);
-            tmem_ld8(ts + 64 + 8 * k, a1);
-            tmem_wait_ld();
-            logits(k, false, a0, a1, l);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float u[2];
-              upk2(l[e], u[0], u[1]);
-#pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                const unsigned o = dev::ord_bits(u[z] == u[z] ? u[z] : -INFINITY);
-                const unsigned most = __reduce_max_sync(0xffffffffu, o);
-                if (lane == 0)
-                  S.wmax[grp][wq][8 * k + 2 * e + z] =
-                      __uint_as_float(most & 0x80000000u ? most & 0x7FFFFFFFu : ~most);
-              }
-            }
-          }
+          for (int k = 0; k < CH; ++k) chunk_max(k, S.wmax[grp][wq]);
           ok = group_ok(ok);
           if (!ok) break;
           if (gt < N) {
@@ -677,7 +769,7 @@ __global__ void __launch_bounds__(kThr, 1)
           ok = group_ok(ok);
           if (!ok) break;
           if (mine > 0) {
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < CH; ++k) {
               float o[8];
               tmem_ld8(to + 8 * k, o);
@@ -685,17 +777,16 @@ __global__ void __launch_bounds__(kThr, 1)
 #pragma unroll
               for (int e = 0; e < 8; ++e) o[e] *= factor[8 * k + e];
               tmem_st8(to + 8 * k, o);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int col = 8 * k + 2 * e;
-                const float2 f = *reinterpret_cast<const float2 *>(&factor[col]);
-                const float2 g = *reinterpret_cast<const float2 *>(&anew[col]);
-                float u, v;
-                upk2(z2[4 * k + e], u, v);
-                z2[4 * k + e] = pk2(g.x > 0.f ? 0.f : u * f.x, g.y > 0.f ? 0.f : v * f.y);
-              }
             }
             tmem_wait_st();
+          }
+#pragma unroll
+          for (int e = 0; e < 4 * CH; ++e) {
+            const float2 f = *reinterpret_cast<const float2 *>(&factor[2 * e]);
+            const float2 g = *reinterpret_cast<const float2 *>(&anew[2 * e]);
+            float u, v;
+            upk2(z2[e], u, v);
+            z2[e] = pk2(g.x > 0.f ? 0.f : u * f.x, g.y > 0.f ? 0.f : v * f.y);
           }
           probabilities(true);
           tc_fence_before();
@@ -711,16 +802,27 @@ __global__ void __launch_bounds__(kThr, 1)
       if (ok) ok = wait(S.pv[(i - 1) & 1], (i - 1) / 2) &&
                    (many < 2 || wait(S.pv[i & 1], (i - 2) / 2));
       tc_fence_after();
+      // Sums over the warp's tokens, sixteen columns at a time: each exchange halves a
+      // lane's columns and doubles the tokens in its sums.
 #pragma unroll
-      for (int e = 0; e < 4 * CH; ++e) {
-        float u, v;
-        upk2(z2[e], u, v);
-        u = dev::warp_sum(u), v = dev::warp_sum(v);
-        if (lane == 0) {
-          S.zsum[grp][wq][2 * e] = u;
-          S.zsum[grp][wq][2 * e + 1] = v;
-        }
+      for (int k = 0; k < CH / 2; ++k) {
+        float u[16];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) upk2(z2[8 * k + e], u[2 * e], u[2 * e + 1]);
+#pragma unroll
+        for (int o = 16, n = 8; n > 0; o >>= 1, n >>= 1)
+#pragma unroll
+          for (int e = 0; e < n; ++e) {
+            const bool high = lane & o;
+            const float give = high ? u[e] : u[e + n];
+            u[e] = (high ? u[e + n] : u[e]) + __shfl_xor_sync(0xffffffffu, give, o);
+          }
+        u[0] += __shfl_xor_sync(0xffffffffu, u[0], 1);
+        if ((lane & 1) == 0) S.zsum[grp][wq][16 * k + (lane >> 1)] = u[0];
       }
+      TileRun then = run;
+      more = walk.next(then);
+      if (more) load_q(then);  // on its way during what follows
       ok = all_ok(ok);
       if (!ok) break;
       if (tid < N) {
@@ -742,7 +844,7 @@ __global__ void __launch_bounds__(kThr, 1)
       // a CTA's first run may lack its beginning, its last one its end
       const int slot = blockIdx.x * 2 + (run.t0 > 0 ? 0 : 1);
       float *part = p.parts + (size_t)slot * N * (kD + 2);
-      const int nan_row = S.nan_row[runs & 3][wq >> 1];  // dims 32 wq .. + 31: their group
+      const int nan_row = S.nan_row[runs & 15][wq >> 1];  // dims 32 wq .. + 31: their group
       // a group without a tile in the run has no O
       const bool has0 = many > 1 || ((i - 1) & 1) == 0, has1 = many > 1 || ((i - 1) & 1) == 1;
 #pragma unroll 1
@@ -757,15 +859,21 @@ __global__ void __launch_bounds__(kThr, 1)
           const float f0 = S.factor[0][col], f1 = S.factor[1][col];
           // (a factor of 0 stands for a column without a token, or a group without
           // a row that it sees: nothing of O counts)
-          float y = has0 && f0 != 0.f ? o[e] * f0 : 0.f;
-          if (has1 && f1 != 0.f) y = fmaf(o1[e], f1, y);
-          if (nan_row <= S.limit[col]) y = NAN;
-          if (whole) {
-            const long long out = S.place[col].out;
-            if (out >= 0) static_cast<__nv_bfloat16 *>(p.out)[out + tok] = __float2bfloat16_rn(y);
-          } else {
-            __stcg(&part[col * kD + tok], y);
-          }
+          o[e] = has0 && f0 != 0.f ? o[e] * f0 : 0.f;
+          if (has1 && f1 != 0.f) o[e] = fmaf(o1[e], f1, o[e]);
+          if (nan_row <= S.limit[col]) o[e] = NAN;
+        }
+        if (whole) {
+          long long out[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) out[e] = S.place[8 * k + e].out;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (out[e] >= 0)
+              static_cast<__nv_bfloat16 *>(p.out)[out[e] + tok] = __float2bfloat16_rn(o[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) __stcg(&part[(8 * k + e) * kD + tok], o[e]);
         }
       }
       if (whole) {
@@ -840,7 +948,7 @@ __global__ void __launch_bounds__(kThr, 1)
       ok = all_ok(ok);  // the columns' arrays are free again
       if (!ok) break;
       ++runs;
-      more = walk.next(run);
+      run = then;
     } while (more);
     if (!ok) give_up();
   }
@@ -968,7 +1076,7 @@ __global__ void __launch_bounds__(kScoreThr, 1)
             if (m[w] > 0) ok = wait(S.s_free[w], m[w] - 1);
             if (!ok) break;
             tc_fence_after();
-            if (lane == 0) {
+            if (elect_one()) {
 #pragma unroll
               for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -1285,6 +1393,10 @@ cudaError_t launch_ch(const AttendParams &p, const Seqs &q, cudaStream_t stream)
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    // (the kernel's split of the registers counts on as many at launch)
+    cudaFuncAttributes attr;
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, kern);
+    if (e == cudaSuccess && attr.numRegs != kRegs) e = cudaErrorInvalidConfiguration;
     if (e != cudaSuccess) return e;
     sms = std::min(n, kTileGrid);
   }
