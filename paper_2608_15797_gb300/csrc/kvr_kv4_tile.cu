@@ -49,7 +49,7 @@ constexpr int kThr = 32 * (kIssuer + 4);
 constexpr int kRegs = 96, kRegsSoft = 144, kRegsRest = 64;
 static_assert(32 * kSoft * kRegsSoft + (kThr - 32 * kSoft) * kRegsRest <= kThr * kRegs,
               "the shares come out of what the CTA was launched with");
-constexpr int kRing = 4;                    // raw tiles in flight
+constexpr int kRing = 3;                    // raw tiles in flight
 static_assert(kVal == kTileBlocks && kKey == 4, "a warp's 32 tokens");
 constexpr int kConst = 4;                   // tiles whose tokens' constants are held
 constexpr int kTileGrid = 256;              // CTAs of a split call, at most
@@ -86,12 +86,12 @@ struct __align__(16) Side {
   float qmax[kSoft];
   int nan_row[16][2];           // [run % 16][group]: first row whose value is NaN
   uint64_t raw_full[kRing], raw_free[kRing];
-  uint64_t cf[kConst], c_free[kConst], kf[2], vf[2], pv[2], sf[2], s_free[2], pf[2], qf, drain;
+  uint64_t cf[kConst], c_free[kConst], kf[2], vf[2], pv[4], sf[2], s_free[2], pf[4], qf, drain;
   uint32_t tmem;
   int abort, flag;
 };
 
-constexpr uint32_t kOffV = 0, kOffP = kOffV + 4 * kHalf, kOffQ = kOffP + 2 * kHalf,
+constexpr uint32_t kOffV = 0, kOffP = kOffV + 4 * kHalf, kOffQ = kOffP + 4 * kHalf,
                    kOffRaw = kOffQ + 2 * kMaxN * 128, kOffSide = kOffRaw + kRing * kRaw;
 constexpr uint32_t kSmem = kOffSide + sizeof(Side);
 static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -246,6 +246,10 @@ __global__ void __launch_bounds__(kThr, 1)
       mbar_init(smem_u32(&S.raw_full[b]), 1);
       mbar_init(smem_u32(&S.raw_free[b]), kKey + kVal);
     }
+    for (int b = 0; b < 4; ++b) {
+      mbar_init(smem_u32(&S.pf[b]), 1);
+      mbar_init(smem_u32(&S.pv[b]), 1);
+    }
     for (int b = 0; b < kConst; ++b) {
       mbar_init(smem_u32(&S.cf[b]), kKey + kVal);
       mbar_init(smem_u32(&S.c_free[b]), kSoft / 2);
@@ -253,10 +257,8 @@ __global__ void __launch_bounds__(kThr, 1)
     for (int b = 0; b < 2; ++b) {
       mbar_init(smem_u32(&S.kf[b]), kKey);
       mbar_init(smem_u32(&S.vf[b]), kVal);
-      mbar_init(smem_u32(&S.pv[b]), 1);
       mbar_init(smem_u32(&S.sf[b]), 1);
       mbar_init(smem_u32(&S.s_free[b]), kSoft / 2);
-      mbar_init(smem_u32(&S.pf[b]), 1);
     }
     mbar_init(smem_u32(&S.qf), 1);
     mbar_init(smem_u32(&S.drain), 1);
@@ -319,17 +321,17 @@ __global__ void __launch_bounds__(kThr, 1)
     int i = 0, runs = 0;
     bool ok = true;
     auto issue_pv = [&](int j, bool first) {  // tile j's P and V are there
-      ok = ok && wait(S.vf[j & 1], j / 2) && wait(S.pf[j & 1], j / 2);
+      ok = ok && wait(S.vf[j & 1], j / 2) && wait(S.pf[j & 3], j / 4);
       if (!ok) return;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t a = dv + (uint64_t)(((j & 1) * 2 * kHalf) >> 4);
-        const uint64_t b = dp + (uint64_t)(((j & 1) * kHalf) >> 4);
+        const uint64_t b = dp + (uint64_t)(((j & 3) * kHalf) >> 4);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
           tc_mma(tm + kColO + (j & 1) * 64, a + (uint64_t)(((k >> 2) * kHalf + (k & 3) * 32) >> 4),
                  b + (uint64_t)(k * 128), id_o, !(first && k == 0));
-        tc_commit(smem_u32(&S.pv[j & 1]));
+        tc_commit(smem_u32(&S.pv[j & 3]));
       }
       __syncwarp();
     };
@@ -349,9 +351,12 @@ __global__ void __launch_bounds__(kThr, 1)
           tc_commit(smem_u32(&S.sf[i & 1]));
         }
         __syncwarp();
-        if (t > run.t0) issue_pv(i - 1, t - 1 - run.t0 < 2);
+        // (after S, which the same softmax warps wait for first)
+        if (t > run.t0 + 1) issue_pv(i - 2, t - run.t0 < 4);
       }
-      if (ok) issue_pv(i - 1, run.t1 - 1 - run.t0 < 2);
+      const int many = run.t1 - run.t0;
+      if (many > 1) issue_pv(i - 2, many < 4);
+      issue_pv(i - 1, many < 3);
       ++runs;
     } while (ok && walk.next(run));
     if (!ok) give_up();
@@ -437,7 +442,7 @@ __global__ void __launch_bounds__(kThr, 1)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&S.cf[cb]));
-        ok = i < 2 || wait(S.pv[b], i / 2 - 1);
+        ok = i < 2 || wait(S.pv[(i - 2) & 3], (i - 2) / 4);
         if (!ok) break;
         // Eight tokens (tg) of chunk ch a lane, a channel group (w, w + 1) at a time; the
         // warp's tokens are those of one block.
@@ -542,7 +547,6 @@ __global__ void __launch_bounds__(kThr, 1)
     const int wq = warp & 3, grp = warp >> 2;
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     const int tok = wq * 32 + lane, gt = tid & 127;  // of the group's threads
-    const uint32_t prow = base + kOffP + grp * kHalf + tok * 128;
     const uint32_t ts = tm + grp * 128 + lanes, to = tm + kColO + grp * 64 + lanes;
     float *const ntop = S.ntop[grp], *const factor = S.factor[grp], *const anew = S.again[grp];
     auto all_ok = [&](bool ok) { return !bar_any(2, 32 * kSoft, !ok); };
@@ -639,8 +643,9 @@ __global__ void __launch_bounds__(kThr, 1)
       for (int t = run.t0 + ((i ^ grp) & 1); t < run.t1; t += 2, ++mine) {
         const int at = i + t - run.t0, cb = at % kConst, row = t * kTok + tok;
         const int n = at >> 1;  // the group's tiles so far
+        const uint32_t prow = base + kOffP + (at & 3) * kHalf + tok * 128;
         if (ok) ok = wait(S.cf[cb], at / kConst) && wait(S.sf[grp], n);
-        if (ok && n > 0) ok = wait(S.pv[grp], n - 1);  // P's place, and O's
+        if (ok && at >= 4) ok = wait(S.pv[at & 3], at / 4 - 1);  // P's place
         tc_fence_after();
         float4 key = S.key[cb][tok];
         const float2 val = S.val[cb][tok];
@@ -769,6 +774,8 @@ __global__ void __launch_bounds__(kThr, 1)
           ok = group_ok(ok);
           if (!ok) break;
           if (mine > 0) {
+            ok = wait(S.pv[(at - 2) & 3], (at - 2) / 4);
+            tc_fence_after();
 #pragma unroll 1
             for (int k = 0; k < CH; ++k) {
               float o[8];
@@ -794,13 +801,13 @@ __global__ void __launch_bounds__(kThr, 1)
           if (!ok) break;
         }
         if (lane == 0) mbar_arrive(smem_u32(&S.s_free[grp]));
-        if (gt == 0) mbar_arrive(smem_u32(&S.pf[grp]));
+        if (gt == 0) mbar_arrive(smem_u32(&S.pf[at & 3]));
       }
       // ---- the run's result: both groups'
       const bool whole = many == run.np;
       i += many;
-      if (ok) ok = wait(S.pv[(i - 1) & 1], (i - 1) / 2) &&
-                   (many < 2 || wait(S.pv[i & 1], (i - 2) / 2));
+      if (ok) ok = wait(S.pv[(i - 1) & 3], (i - 1) / 4) &&
+                   (many < 2 || wait(S.pv[(i - 2) & 3], (i - 2) / 4));
       tc_fence_after();
       // Sums over the warp's tokens, sixteen columns at a time: each exchange halves a
       // lane's columns and doubles the tokens in its sums.
