@@ -46,10 +46,10 @@ constexpr int kSoft = 8, kKey = 4, kVal = 4;
 constexpr int kIssuer = kSoft + kKey + kVal, kLoader = kIssuer + 1;
 constexpr int kThr = 32 * (kIssuer + 4);
 // Registers a thread: at launch, then for the softmax and for the others.
-constexpr int kRegs = 96, kRegsSoft = 144, kRegsRest = 64;
+constexpr int kRegs = 96, kRegsSoft = 168, kRegsRest = 48;
 static_assert(32 * kSoft * kRegsSoft + (kThr - 32 * kSoft) * kRegsRest <= kThr * kRegs,
               "the shares come out of what the CTA was launched with");
-constexpr int kRing = 3;                    // raw tiles in flight
+constexpr int kRing = 4;                    // raw tiles in flight
 static_assert(kVal == kTileBlocks && kKey == 4, "a warp's 32 tokens");
 constexpr int kConst = 4;                   // tiles whose tokens' constants are held
 constexpr int kTileGrid = 256;              // CTAs of a split call, at most
@@ -62,8 +62,10 @@ constexpr float kUnit = 0x1p24f;            // of K's codes
 
 // An item's place in the list counts its tiles and, before them, kSwitch more for
 // what a CTA spends on an item whatever its length (its queries, the first
-// maxima, the result).
+// maxima, the result).  One of kWhole tiles or fewer is not cut, but its first
+// tile's CTA has all of it: that is one result instead of a join.
 constexpr int kSwitch = 5;
+constexpr int kWhole = 4;
 struct TilePlan {
   int32_t base[kMaxSeqs + 1];
   int32_t span;    // of a CTA, or 0: one item a CTA
@@ -75,23 +77,21 @@ struct __align__(16) Side {
   float2 val[kConst][kTok];     // e + 1, 2^-(e + 1) of its value
   uint2 vc[2][kTok / 2];        // [group][pair]: s 2^(18 - e - 1), m 2^-(e + 1), halves
   float4 qs[kMaxN / 2];         // sums of q: group 0 of two columns, group 1
-  // of the even and the odd tiles:
-  float ntop[2][kMaxN];         // minus the columns' references
-  float factor[2][kMaxN], again[2][kMaxN];
-  float wmax[2][4][kMaxN];
-  float zsum[2][4][kMaxN];
+  float ntop[kMaxN];            // minus the columns' references
+  float factor[kMaxN], again[kMaxN];
+  float wmax[4][kMaxN], zsum[4][kMaxN];
   int limit[kMaxN];             // last row a column sees, or -1
   float2 stat[kMaxN];
   Place place[kMaxN];
   float qmax[kSoft];
   int nan_row[16][2];           // [run % 16][group]: first row whose value is NaN
   uint64_t raw_full[kRing], raw_free[kRing];
-  uint64_t cf[kConst], c_free[kConst], kf[2], vf[2], pv[4], sf[2], s_free[2], pf[4], qf, drain;
+  uint64_t cf[kConst], c_free[kConst], kf[2], vf[2], pv[2], sf[2], s_free[2], pf[2], qf, drain;
   uint32_t tmem;
   int abort, flag;
 };
 
-constexpr uint32_t kOffV = 0, kOffP = kOffV + 4 * kHalf, kOffQ = kOffP + 4 * kHalf,
+constexpr uint32_t kOffV = 0, kOffP = kOffV + 4 * kHalf, kOffQ = kOffP + 2 * kHalf,
                    kOffRaw = kOffQ + 2 * kMaxN * 128, kOffSide = kOffRaw + kRing * kRaw;
 constexpr uint32_t kSmem = kOffSide + sizeof(Side);
 static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -200,9 +200,32 @@ struct TileRun {
 
 struct Walk {
   const Seqs &sq;
+  const TilePlan &plan;
   int per_seq, last;  // the end of the CTA's span
   __device__ static int tiles_of(int nb) { return (nb + kTileBlocks - 1) / kTileBlocks; }
-  // The next item with a tile in the span.
+  __device__ int end_of(const TileRun &r) const {
+    return r.np <= kWhole ? r.np : min(r.np, last - r.at - kSwitch);
+  }
+  // The span's first item with a tile in it.
+  __device__ bool first(TileRun &r, int seqs) {
+    const int from = blockIdx.x * plan.span;
+    last = min(from + plan.span, plan.base[seqs]);
+    int lo = 0, hi = seqs;  // the sequence that holds the span's start
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (plan.base[mid] <= from) lo = mid; else hi = mid;
+    }
+    r.s = lo;
+    r.np = tiles_of(blocks_of(sq.len[lo]));
+    const int rest = from - plan.base[lo], cost = kSwitch + r.np;
+    r.item = rest / cost;
+    r.at = plan.base[lo] + r.item * cost;
+    r.t0 = max(0, from - r.at - kSwitch);
+    if (r.t0 > 0 && r.np <= kWhole) return next(r);
+    if (r.at + kSwitch >= last) return false;  // a short span may lie before the tile
+    r.t1 = end_of(r);
+    return true;
+  }
   __device__ bool next(TileRun &r) const {
     r.at += kSwitch + r.np;
     if (r.at + kSwitch >= last) return false;
@@ -212,7 +235,7 @@ struct Walk {
       r.np = tiles_of(blocks_of(sq.len[r.s]));
     }
     r.t0 = 0;
-    r.t1 = min(r.np, last - r.at - kSwitch);
+    r.t1 = end_of(r);
     return true;
   }
 };
@@ -246,19 +269,17 @@ __global__ void __launch_bounds__(kThr, 1)
       mbar_init(smem_u32(&S.raw_full[b]), 1);
       mbar_init(smem_u32(&S.raw_free[b]), kKey + kVal);
     }
-    for (int b = 0; b < 4; ++b) {
-      mbar_init(smem_u32(&S.pf[b]), 1);
-      mbar_init(smem_u32(&S.pv[b]), 1);
-    }
     for (int b = 0; b < kConst; ++b) {
       mbar_init(smem_u32(&S.cf[b]), kKey + kVal);
-      mbar_init(smem_u32(&S.c_free[b]), kSoft / 2);
+      mbar_init(smem_u32(&S.c_free[b]), kSoft);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(smem_u32(&S.kf[b]), kKey);
       mbar_init(smem_u32(&S.vf[b]), kVal);
       mbar_init(smem_u32(&S.sf[b]), 1);
-      mbar_init(smem_u32(&S.s_free[b]), kSoft / 2);
+      mbar_init(smem_u32(&S.s_free[b]), kSoft);
+      mbar_init(smem_u32(&S.pf[b]), 2);
+      mbar_init(smem_u32(&S.pv[b]), 1);
     }
     mbar_init(smem_u32(&S.qf), 1);
     mbar_init(smem_u32(&S.drain), 1);
@@ -273,25 +294,11 @@ __global__ void __launch_bounds__(kThr, 1)
   const uint32_t tm = S.tmem;
 
   // The CTA's first run.
-  Walk walk{sq, p.k.nl * c.H * plan.tiles, 0};
+  Walk walk{sq, plan, p.k.nl * c.H * plan.tiles, 0};
   TileRun run;
-  bool any = true;  // a short span may lie before an item's first tile
+  bool any = true;
   if (plan.span) {
-    const int from = blockIdx.x * plan.span;
-    walk.last = min(from + plan.span, plan.base[p.k.n]);
-    int lo = 0, hi = p.k.n;  // the sequence that holds the span's start
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (plan.base[mid] <= from) lo = mid; else hi = mid;
-    }
-    run.s = lo;
-    run.np = Walk::tiles_of(blocks_of(sq.len[lo]));
-    const int rest = from - plan.base[lo], cost = kSwitch + run.np;
-    run.item = rest / cost;
-    run.at = plan.base[lo] + run.item * cost;
-    run.t0 = max(0, from - run.at - kSwitch);
-    run.t1 = min(run.np, walk.last - run.at - kSwitch);
-    any = run.t1 > run.t0;
+    any = walk.first(run, p.k.n);
   } else {
     run.s = blockIdx.x / walk.per_seq;
     run.item = blockIdx.x - run.s * walk.per_seq;
@@ -321,17 +328,17 @@ __global__ void __launch_bounds__(kThr, 1)
     int i = 0, runs = 0;
     bool ok = true;
     auto issue_pv = [&](int j, bool first) {  // tile j's P and V are there
-      ok = ok && wait(S.vf[j & 1], j / 2) && wait(S.pf[j & 3], j / 4);
+      ok = ok && wait(S.vf[j & 1], j / 2) && wait(S.pf[j & 1], j / 2);
       if (!ok) return;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t a = dv + (uint64_t)(((j & 1) * 2 * kHalf) >> 4);
-        const uint64_t b = dp + (uint64_t)(((j & 3) * kHalf) >> 4);
+        const uint64_t b = dp + (uint64_t)(((j & 1) * kHalf) >> 4);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          tc_mma(tm + kColO + (j & 1) * 64, a + (uint64_t)(((k >> 2) * kHalf + (k & 3) * 32) >> 4),
+          tc_mma(tm + kColO, a + (uint64_t)(((k >> 2) * kHalf + (k & 3) * 32) >> 4),
                  b + (uint64_t)(k * 128), id_o, !(first && k == 0));
-        tc_commit(smem_u32(&S.pv[j & 3]));
+        tc_commit(smem_u32(&S.pv[j & 1]));
       }
       __syncwarp();
     };
@@ -351,12 +358,9 @@ __global__ void __launch_bounds__(kThr, 1)
           tc_commit(smem_u32(&S.sf[i & 1]));
         }
         __syncwarp();
-        // (after S, which the same softmax warps wait for first)
-        if (t > run.t0 + 1) issue_pv(i - 2, t - run.t0 < 4);
+        if (t > run.t0) issue_pv(i - 1, t - 1 == run.t0);
       }
-      const int many = run.t1 - run.t0;
-      if (many > 1) issue_pv(i - 2, many < 4);
-      issue_pv(i - 1, many < 3);
+      issue_pv(i - 1, run.t1 - 1 == run.t0);
       ++runs;
     } while (ok && walk.next(run));
     if (!ok) give_up();
@@ -442,7 +446,7 @@ __global__ void __launch_bounds__(kThr, 1)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&S.cf[cb]));
-        ok = i < 2 || wait(S.pv[(i - 2) & 3], (i - 2) / 4);
+        ok = i < 2 || wait(S.pv[b], i / 2 - 1);
         if (!ok) break;
         // Eight tokens (tg) of chunk ch a lane, a channel group (w, w + 1) at a time; the
         // warp's tokens are those of one block.
@@ -547,8 +551,10 @@ __global__ void __launch_bounds__(kThr, 1)
     const int wq = warp & 3, grp = warp >> 2;
     const uint32_t lanes = (uint32_t)(wq * 32) << 16;
     const int tok = wq * 32 + lane, gt = tid & 127;  // of the group's threads
-    const uint32_t ts = tm + grp * 128 + lanes, to = tm + kColO + grp * 64 + lanes;
-    float *const ntop = S.ntop[grp], *const factor = S.factor[grp], *const anew = S.again[grp];
+    constexpr int NG = N / 2, CG = CH / 2;  // columns of the group, and their eights
+    const int c0 = grp * NG;
+    const uint32_t to = tm + kColO + c0 + lanes;
+    float *const ntop = S.ntop + c0, *const factor = S.factor + c0, *const anew = S.again + c0;
     auto all_ok = [&](bool ok) { return !bar_any(2, 32 * kSoft, !ok); };
     auto group_ok = [&](bool ok) { return !bar_any(3 + grp, 16 * kSoft, !ok); };
     int i = 0, runs = 0;  // i: tiles before the run
@@ -575,7 +581,7 @@ __global__ void __launch_bounds__(kThr, 1)
       if (tid < N) {
         const Place a = place_of(p, sq, run.s, lr, h, col0 + tid);
         S.place[tid] = a;
-        S.ntop[0][tid] = S.ntop[1][tid] = -kNone;
+        S.ntop[tid] = -kNone;
         S.limit[tid] = a.out >= 0 && a.live ? len - count + (col0 + tid) / c.G : -1;
       }
       float x[CH / 2][8];
@@ -635,23 +641,25 @@ __global__ void __launch_bounds__(kThr, 1)
       // rows below `full` are seen by every column that has a token
       const int first = col0 / c.G;
       const int full = first < count ? len - count + first + 1 : len;
-      uint64_t z2[4 * CH];
+      uint64_t z2[4 * CG], q0[4 * CG], q1[4 * CG];
 #pragma unroll
-      for (int e = 0; e < 4 * CH; ++e) z2[e] = 0;
-      const int many = run.t1 - run.t0;
-      int mine = 0;  // tiles of the run that this group has taken
-      for (int t = run.t0 + ((i ^ grp) & 1); t < run.t1; t += 2, ++mine) {
-        const int at = i + t - run.t0, cb = at % kConst, row = t * kTok + tok;
-        const int n = at >> 1;  // the group's tiles so far
-        const uint32_t prow = base + kOffP + (at & 3) * kHalf + tok * 128;
-        if (ok) ok = wait(S.cf[cb], at / kConst) && wait(S.sf[grp], n);
-        if (ok && at >= 4) ok = wait(S.pv[at & 3], at / 4 - 1);  // P's place
+      for (int e = 0; e < 4 * CG; ++e) {
+        const float4 q = S.qs[c0 / 2 + e];
+        q0[e] = pk2(q.x, q.y), q1[e] = pk2(q.z, q.w);
+        z2[e] = 0;
+      }
+      for (int t = run.t0; t < run.t1; ++t) {
+        const int at = i + t - run.t0, b = at & 1, cb = at % kConst, row = t * kTok + tok;
+        const uint32_t ts = tm + b * 128 + c0 + lanes;
+        unsigned char *const prow = smem + kOffP + b * kHalf + tok * 128;
+        if (ok) ok = wait(S.cf[cb], at / kConst) && wait(S.sf[b], at / 2);
+        if (ok && at >= 2) ok = wait(S.pv[b], at / 2 - 1);  // P's place
         tc_fence_after();
         float4 key = S.key[cb][tok];
         const float2 val = S.val[cb][tok];
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&S.c_free[cb]));
-        if (ok && (t + 1) * kTok > full) mask_row(ts, N, S.limit, row, key);
+        if (ok && (t + 1) * kTok > full) mask_row(ts, NG, S.limit + c0, row, key);
         const float k0 = fmaxf(key.x * unit_s, 0x1p-126f);
         const uint64_t s0 = pk2(k0, k0);
         const uint64_t s1 = pk2(key.y * unit_s, key.y * unit_s);
@@ -663,12 +671,10 @@ __global__ void __launch_bounds__(kThr, 1)
                           uint64_t (&l)[4]) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int col = 8 * k + 2 * e;
-            const float4 q = S.qs[col >> 1];
-            const float2 nt = *reinterpret_cast<const float2 *>(&ntop[col]);
+            const float2 nt = *reinterpret_cast<const float2 *>(&ntop[8 * k + 2 * e]);
             uint64_t y = less ? add2(pk2(nt.x, nt.y), e2) : e2;
-            y = fma2(m1, pk2(q.z, q.w), y);
-            y = fma2(m0, pk2(q.x, q.y), y);
+            y = fma2(m1, q1[4 * k + e], y);
+            y = fma2(m0, q0[4 * k + e], y);
             y = fma2(s1, pk2(a1[2 * e], a1[2 * e + 1]), y);
             l[e] = fma2(s0, pk2(a0[2 * e], a0[2 * e + 1]), y);
           }
@@ -682,12 +688,12 @@ __global__ void __launch_bounds__(kThr, 1)
           tmem_ld8(ts, a0);
           tmem_ld8(ts + 64, a1);
 #pragma unroll
-          for (int k = 0; k < CH; ++k) {
+          for (int k = 0; k < CG; ++k) {
             uint64_t l[4];
             uint32_t w[4];
             tmem_landed(a0, a1);
             logits(k, true, a0, a1, l);
-            if (k + 1 < CH) {  // the next columns come while these are worked on
+            if (k + 1 < CG) {  // the next columns come while these are worked on
               tmem_ld8(ts + 8 * k + 8, a0);
               tmem_ld8(ts + 64 + 8 * k + 8, a1);
             }
@@ -706,7 +712,8 @@ __global__ void __launch_bounds__(kThr, 1)
               }
               z2[4 * k + e] = fma2(p2, down2, z2[4 * k + e]);
             }
-            sts128(prow + ((k ^ (tok & 7)) << 4), w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4 *>(prow + (((grp * CG + k) ^ (tok & 7)) << 4)) =
+                make_uint4(w[0], w[1], w[2], w[3]);
           }
           fence_proxy_async();
           return __hgt(__hmax(__low2half(most), __high2half(most)), __float2half_rn(32768.f));
@@ -733,18 +740,20 @@ __global__ void __launch_bounds__(kThr, 1)
             }
           }
         };
-        bool grow = mine == 0;
+        const bool begin = t == run.t0;
+        bool grow = begin;
         if (grow && (t + 1) * kTok <= full) {
           // A run's first references: a column's largest over 32 of the tokens will
           // do, so that a warp has a quarter of the columns.
           grow = false;
           if (ok) {
-#pragma unroll 1
-            for (int k = wq; k < CH; k += 4) chunk_max(k, S.wmax[grp][0]);
+#pragma unroll
+            for (int k = 0; k < CG; ++k)
+              if (k == wq) chunk_max(k, S.wmax[0] + c0);
           }
           ok = group_ok(ok);
           if (!ok) break;
-          if (gt < N) ntop[gt] = -fmaxf(kNone, S.wmax[grp][0][gt]);
+          if (gt < NG) ntop[gt] = -fmaxf(kNone, S.wmax[0][c0 + gt]);
           ok = group_ok(ok);
           if (!ok) break;
         }
@@ -756,28 +765,28 @@ __global__ void __launch_bounds__(kThr, 1)
           // Raise the references to the columns' maxima so far.
           ok = group_ok(ok);
           if (!ok) break;
-#pragma unroll 1
-          for (int k = 0; k < CH; ++k) chunk_max(k, S.wmax[grp][wq]);
+#pragma unroll
+          for (int k = 0; k < CG; ++k) chunk_max(k, S.wmax[wq] + c0);
           ok = group_ok(ok);
           if (!ok) break;
-          if (gt < N) {
+          if (gt < NG) {
             const float old = -ntop[gt];
             float now = old;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) now = fmaxf(now, S.wmax[grp][w][gt]);
+            for (int w = 0; w < 4; ++w) now = fmaxf(now, S.wmax[w][c0 + gt]);
             // a sum over 2^64 behind, which may have overflowed, is begun anew
-            const bool fresh = mine == 0 || now - old > 64.f;
+            const bool fresh = begin || now - old > 64.f;
             factor[gt] = ex2(old - now);
             anew[gt] = fresh ? 1.f : 0.f;
             ntop[gt] = -now;
           }
           ok = group_ok(ok);
           if (!ok) break;
-          if (mine > 0) {
-            ok = wait(S.pv[(at - 2) & 3], (at - 2) / 4);
+          if (!begin) {
+            ok = wait(S.pv[b ^ 1], (at - 1) / 2);
             tc_fence_after();
 #pragma unroll 1
-            for (int k = 0; k < CH; ++k) {
+            for (int k = 0; k < CG; ++k) {
               float o[8];
               tmem_ld8(to + 8 * k, o);
               tmem_wait_ld();
@@ -788,7 +797,7 @@ __global__ void __launch_bounds__(kThr, 1)
             tmem_wait_st();
           }
 #pragma unroll
-          for (int e = 0; e < 4 * CH; ++e) {
+          for (int e = 0; e < 4 * CG; ++e) {
             const float2 f = *reinterpret_cast<const float2 *>(&factor[2 * e]);
             const float2 g = *reinterpret_cast<const float2 *>(&anew[2 * e]);
             float u, v;
@@ -800,100 +809,88 @@ __global__ void __launch_bounds__(kThr, 1)
           ok = group_ok(ok);
           if (!ok) break;
         }
-        if (lane == 0) mbar_arrive(smem_u32(&S.s_free[grp]));
-        if (gt == 0) mbar_arrive(smem_u32(&S.pf[at & 3]));
+        if (lane == 0) mbar_arrive(smem_u32(&S.s_free[b]));
+        if (gt == 0) mbar_arrive(smem_u32(&S.pf[b]));
       }
-      // ---- the run's result: both groups'
-      const bool whole = many == run.np;
-      i += many;
-      if (ok) ok = wait(S.pv[(i - 1) & 3], (i - 1) / 4) &&
-                   (many < 2 || wait(S.pv[(i - 2) & 3], (i - 2) / 4));
+      // ---- the run's result: each group's columns
+      const bool whole = run.t1 - run.t0 == run.np;
+      i += run.t1 - run.t0;
+      if (ok) ok = wait(S.pv[(i - 1) & 1], (i - 1) / 2);
       tc_fence_after();
-      // Sums over the warp's tokens, sixteen columns at a time: each exchange halves a
+      // Sums over the warp's tokens, eight columns at a time: each exchange halves a
       // lane's columns and doubles the tokens in its sums.
 #pragma unroll
-      for (int k = 0; k < CH / 2; ++k) {
-        float u[16];
+      for (int k = 0; k < CG; ++k) {
+        float u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) upk2(z2[8 * k + e], u[2 * e], u[2 * e + 1]);
+        for (int e = 0; e < 4; ++e) upk2(z2[4 * k + e], u[2 * e], u[2 * e + 1]);
 #pragma unroll
-        for (int o = 16, n = 8; n > 0; o >>= 1, n >>= 1)
+        for (int o = 16, n = 4; n > 0; o >>= 1, n >>= 1)
 #pragma unroll
           for (int e = 0; e < n; ++e) {
             const bool high = lane & o;
             const float give = high ? u[e] : u[e + n];
             u[e] = (high ? u[e + n] : u[e]) + __shfl_xor_sync(0xffffffffu, give, o);
           }
+        u[0] += __shfl_xor_sync(0xffffffffu, u[0], 2);
         u[0] += __shfl_xor_sync(0xffffffffu, u[0], 1);
-        if ((lane & 1) == 0) S.zsum[grp][wq][16 * k + (lane >> 1)] = u[0];
+        if ((lane & 3) == 0) S.zsum[wq][c0 + 8 * k + (lane >> 2)] = u[0];
       }
       TileRun then = run;
       more = walk.next(then);
       if (more) load_q(then);  // on its way during what follows
       ok = all_ok(ok);
       if (!ok) break;
-      if (tid < N) {
-        const float t0 = -S.ntop[0][tid], t1 = -S.ntop[1][tid], top = fmaxf(t0, t1);
-        float z[2];
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-          z[g] = (S.zsum[g][0][tid] + S.zsum[g][1][tid]) + (S.zsum[g][2][tid] + S.zsum[g][3][tid]);
-        const float f0 = ex2(t0 - top), f1 = ex2(t1 - top), zz = fmaf(z[0], f0, z[1] * f1);
+      if (gt < NG) {
+        const int col = c0 + gt;
+        const float z = (S.zsum[0][col] + S.zsum[1][col]) + (S.zsum[2][col] + S.zsum[3][col]);
         // a whole run's factors normalise, and make zeros of a column without a token
-        const float f = !whole ? 1.f : S.place[tid].live && zz != 0.f ? 1.f / zz : 0.f;
-        S.factor[0][tid] = f0 * f;
-        S.factor[1][tid] = f1 * f;
-        S.stat[tid] = make_float2(top, zz);
+        factor[gt] = !whole ? 1.f : S.place[col].live && z != 0.f ? 1.f / z : 0.f;
+        S.stat[col] = make_float2(-ntop[gt], z);
       }
-      ok = all_ok(ok);
+      ok = group_ok(ok);
       if (!ok) break;
       const size_t call_unit = ((size_t)(p.k.s0 + run.s) * p.k.nl + lr) * c.H + h;
       // a CTA's first run may lack its beginning, its last one its end
       const int slot = blockIdx.x * 2 + (run.t0 > 0 ? 0 : 1);
       float *part = p.parts + (size_t)slot * N * (kD + 2);
       const int nan_row = S.nan_row[runs & 15][wq >> 1];  // dims 32 wq .. + 31: their group
-      // a group without a tile in the run has no O
-      const bool has0 = many > 1 || ((i - 1) & 1) == 0, has1 = many > 1 || ((i - 1) & 1) == 1;
 #pragma unroll 1
-      for (int k = grp; k < CH; k += 2) {
-        float o[8], o1[8];
-        tmem_ld8(tm + kColO + 8 * k + lanes, o);
-        tmem_ld8(tm + kColO + 64 + 8 * k + lanes, o1);
+      for (int k = 0; k < CG; ++k) {
+        float o[8];
+        tmem_ld8(to + 8 * k, o);
         tmem_wait_ld();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int col = 8 * k + e;
-          const float f0 = S.factor[0][col], f1 = S.factor[1][col];
-          // (a factor of 0 stands for a column without a token, or a group without
-          // a row that it sees: nothing of O counts)
-          o[e] = has0 && f0 != 0.f ? o[e] * f0 : 0.f;
-          if (has1 && f1 != 0.f) o[e] = fmaf(o1[e], f1, o[e]);
-          if (nan_row <= S.limit[col]) o[e] = NAN;
+          const float f = factor[8 * k + e];
+          o[e] = f != 0.f ? o[e] * f : 0.f;  // (0: a column without a token)
+          if (nan_row <= S.limit[c0 + 8 * k + e]) o[e] = NAN;
         }
         if (whole) {
           long long out[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) out[e] = S.place[8 * k + e].out;
+          for (int e = 0; e < 8; ++e) out[e] = S.place[c0 + 8 * k + e].out;
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (out[e] >= 0)
               static_cast<__nv_bfloat16 *>(p.out)[out[e] + tok] = __float2bfloat16_rn(o[e]);
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) __stcg(&part[(8 * k + e) * kD + tok], o[e]);
+          for (int e = 0; e < 8; ++e) __stcg(&part[(c0 + 8 * k + e) * kD + tok], o[e]);
         }
       }
       if (whole) {
-        if (tid < N && S.place[tid].out >= 0) {
-          const float z = S.stat[tid].y;
-          const bool live = S.place[tid].live && z != 0.f;
+        const int col = c0 + gt;
+        if (gt < NG && S.place[col].out >= 0) {
+          const float z = S.stat[col].y;
+          const bool live = S.place[col].live && z != 0.f;
           if (live && !isfinite(z)) atomicOr(c.err, ERR_NONFINITE);
           if (p.stats)
-            reinterpret_cast<float2 *>(p.stats)[call_unit * (p.n_q * c.G) + S.place[tid].stat] =
-                make_float2(S.stat[tid].x, live ? 1.f / (z * c.G) : 0.f);
+            reinterpret_cast<float2 *>(p.stats)[call_unit * (p.n_q * c.G) + S.place[col].stat] =
+                make_float2(S.stat[col].x, live ? 1.f / (z * c.G) : 0.f);
         }
       } else {
-        if (tid < N) __stcg(reinterpret_cast<float2 *>(part + N * kD) + tid, S.stat[tid]);
+        if (gt < NG) __stcg(reinterpret_cast<float2 *>(part + N * kD) + c0 + gt, S.stat[c0 + gt]);
         const int i0 = run.at + kSwitch;  // the first tile's place
         const int w0 = i0 / plan.span, w1 = (i0 + run.np - 1) / plan.span;
         unsigned *ticket = c.ticket + unit_of(run) * kMaxTiles + run.item % plan.tiles;
@@ -1033,23 +1030,9 @@ __global__ void __launch_bounds__(kScoreThr, 1)
 
   // Spans of the list of all units' tiles; a unit's columns are taken kScoreCols at a
   // time by the CTA that has its tiles.
-  Walk walk{sq, p.k.nl * c.H, 0};
-  const int from = blockIdx.x * plan.span;
-  walk.last = min(from + plan.span, plan.base[p.k.n]);
+  Walk walk{sq, plan, p.k.nl * c.H, 0};
   TileRun first;
-  int lo = 0, hi = p.k.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (plan.base[mid] <= from) lo = mid; else hi = mid;
-  }
-  first.s = lo;
-  first.np = Walk::tiles_of(blocks_of(sq.len[lo]));
-  const int rest = from - plan.base[lo], cost = kSwitch + first.np;
-  first.item = rest / cost;
-  first.at = plan.base[lo] + first.item * cost;
-  first.t0 = max(0, from - first.at - kSwitch);
-  first.t1 = min(first.np, walk.last - first.at - kSwitch);
-  const bool any = first.t1 > first.t0;
+  const bool any = walk.first(first, p.k.n);
   pdl_begin();
   const uint32_t tm = S.tmem;
   // A run's passes over its tiles, and the column tiles of pass g.
