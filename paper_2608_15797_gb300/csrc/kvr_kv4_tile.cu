@@ -257,6 +257,8 @@ __global__ void __launch_bounds__(kThr, 1)
   auto wait = [&](uint64_t &bar, int n) {
     return warp_wait(smem_u32(&bar), (uint32_t)(n & 1), abort);
   };
+  auto at = [&](uint64_t &bar, int n) { return Phase{smem_u32(&bar), (uint32_t)(n & 1)}; };
+  auto wait_for = [&](Phase a, Phase b, Phase c, int n) { return warp_wait(a, b, c, n, abort); };
   auto give_up = [&]() {
     if (lane == 0) {
       if (!*abort) atomicOr(c.err, ERR_TIMEOUT);
@@ -328,7 +330,7 @@ __global__ void __launch_bounds__(kThr, 1)
     int i = 0, runs = 0;
     bool ok = true;
     auto issue_pv = [&](int j, bool first) {  // tile j's P and V are there
-      ok = ok && wait(S.vf[j & 1], j / 2) && wait(S.pf[j & 1], j / 2);
+      ok = ok && wait_for(at(S.vf[j & 1], j / 2), at(S.pf[j & 1], j / 2), {}, 2);
       if (!ok) return;
       tc_fence_after();
       if (elect_one()) {
@@ -344,8 +346,8 @@ __global__ void __launch_bounds__(kThr, 1)
     };
     do {
       for (int t = run.t0; t < run.t1 && ok; ++t, ++i) {
-        ok = (t > run.t0 || wait(S.qf, runs)) && wait(S.kf[i & 1], i / 2) &&
-             (i < 2 || wait(S.s_free[i & 1], i / 2 - 1));
+        ok = wait_for(at(S.kf[i & 1], i / 2), at(S.qf, runs), at(S.s_free[i & 1], i / 2 - 1),
+                      i < 2 ? 2 : 3);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
@@ -412,8 +414,8 @@ __global__ void __launch_bounds__(kThr, 1)
       for (int t = run.t0; t < run.t1; ++t, ++i) {
         const int b = i & 1, cb = i % kConst, rb = i % kRing;
         const unsigned char *raw = smem + kOffRaw + rb * kRaw;
-        ok = ok && wait(S.raw_full[rb], i / kRing) &&
-             (i < kConst || wait(S.c_free[cb], i / kConst - 1));
+        ok = ok && wait_for(at(S.raw_full[rb], i / kRing), at(S.c_free[cb], i / kConst - 1), {},
+                            i < kConst ? 1 : 2);
         if (!ok) break;
         // The slot of eight runs ahead: none of this role has reached it, and the
         // softmax, at most four tiles behind, has left the run that had it.
@@ -505,8 +507,8 @@ __global__ void __launch_bounds__(kThr, 1)
         const int b = i & 1, cb = i % kConst, rb = i % kRing;
         const unsigned char *blk = smem + kOffRaw + rb * kRaw + (dt / kBlock) * block_bytes(kD);
         // (its place is free once tile i - 2's product is there)
-        ok = ok && wait(S.raw_full[rb], i / kRing) && (i < 2 || wait(S.sf[b], i / 2 - 1)) &&
-             (i < kConst || wait(S.c_free[cb], i / kConst - 1));
+        ok = ok && wait_for(at(S.raw_full[rb], i / kRing), at(S.sf[b], i / 2 - 1),
+                            at(S.c_free[cb], i / kConst - 1), i < 2 ? 1 : i < kConst ? 2 : 3);
         if (!ok) break;
         const int r = dt % kBlock;
         uint2 km = *reinterpret_cast<const uint2 *>(blk + km_off(kD) + r * 8);
@@ -649,11 +651,12 @@ __global__ void __launch_bounds__(kThr, 1)
         z2[e] = 0;
       }
       for (int t = run.t0; t < run.t1; ++t) {
-        const int at = i + t - run.t0, b = at & 1, cb = at % kConst, row = t * kTok + tok;
+        const int n = i + t - run.t0, b = n & 1, cb = n % kConst, row = t * kTok + tok;
         const uint32_t ts = tm + b * 128 + c0 + lanes;
         unsigned char *const prow = smem + kOffP + b * kHalf + tok * 128;
-        if (ok) ok = wait(S.cf[cb], at / kConst) && wait(S.sf[b], at / 2);
-        if (ok && at >= 2) ok = wait(S.pv[b], at / 2 - 1);  // P's place
+        // the constants, S and P's place
+        if (ok) ok = wait_for(at(S.cf[cb], n / kConst), at(S.sf[b], n / 2),
+                              at(S.pv[b], n / 2 - 1), n < 2 ? 2 : 3);
         tc_fence_after();
         float4 key = S.key[cb][tok];
         const float2 val = S.val[cb][tok];
@@ -783,7 +786,7 @@ __global__ void __launch_bounds__(kThr, 1)
           ok = group_ok(ok);
           if (!ok) break;
           if (!begin) {
-            ok = wait(S.pv[b ^ 1], (at - 1) / 2);
+            ok = wait(S.pv[b ^ 1], (n - 1) / 2);
             tc_fence_after();
 #pragma unroll 1
             for (int k = 0; k < CG; ++k) {
