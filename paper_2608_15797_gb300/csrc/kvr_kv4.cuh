@@ -83,13 +83,6 @@ __device__ __forceinline__ int v_half(int r, int w, int c) {
   const int p = r >> 1;
   return v_off(D) + p * D + v_chunk<D>(p, c) * (D / 8) + w * 4 + (r & 1) * 2;
 }
-template <int D>
-__device__ __forceinline__ int v_byte(int r, int x, int &hi) {
-  const int w = x >> 5, c = x & 7, y = (x >> 3) & 3;  // y: 0, 8, 16, 24
-  const int f = ((y & 1) << 1) | (y >> 1);
-  hi = f & 1;
-  return v_half<D>(r, w, c) + (f >> 1);
-}
 
 __device__ __forceinline__ float m_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float s_of(uint32_t w) {
@@ -123,29 +116,6 @@ __device__ __forceinline__ uint32_t code_of(float x, uint32_t meta, bool flat) {
   const float c = rintf(__fdiv_rn(__fsub_rn(x, m_of(meta)), s_of(meta)));
   return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
 }
-// What a code stands for.
-__device__ __forceinline__ float value_of(uint32_t c, uint32_t meta) {
-  return fmaf((float)c, s_of(meta), m_of(meta));
-}
-
-template <int D>
-__device__ __forceinline__ uint32_t meta_at(const uint8_t *block, int off, int r, int x) {
-  return *reinterpret_cast<const uint32_t *>(block + off +
-                                             (r * (D / kGroup) + (x >> 6)) * 4);
-}
-template <int D>
-__device__ __forceinline__ float k_value(const uint8_t *block, int r, int x) {
-  int hi;
-  const int b = k_byte<D>(r, x, hi);
-  return value_of((block[b] >> (4 * hi)) & 15u, meta_at<D>(block, km_off(D), r, x));
-}
-template <int D>
-__device__ __forceinline__ float v_value(const uint8_t *block, int r, int x) {
-  int hi;
-  const int b = v_byte<D>(r, x, hi);
-  return value_of((block[b] >> (4 * hi)) & 15u, meta_at<D>(block, vm_off(D), r, x));
-}
-
 // Unit x in [0, n * nl * H) of a launch over sequences [s0, s0 + n) and layers
 // [lb, lb + nl): its index in the cache.
 __device__ __forceinline__ size_t unit_at(const View &c, int s, int lb, int lr, int h) {
@@ -182,7 +152,7 @@ struct AttendParams {
 cudaError_t launch_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream,
                           int *launches);
 // kvr_kv4_tile.cu: the same, on 5th-generation tensor cores, where it applies
-// (bf16, d = 128, more than eight query rows a unit), and the scores' sums.
+// (bf16, d = 128, more than a few query rows a unit), and the scores' sums.
 bool tile_applies(const View &c, int n_q);
 size_t tile_part_floats(const View &c, int nl, int n_q);
 cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream);

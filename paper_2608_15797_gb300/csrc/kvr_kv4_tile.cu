@@ -5,25 +5,38 @@
 // Columns are (token, head) pairs of a unit, N <= 64 of them a tile, and rows the
 // 128 cached tokens of four blocks:
 //   S_j [tokens x N] = K_j Q_j^T for the two channel groups j, in tensor memory
-//   P   [tokens x N] = 2^(logit - top of the column), 16 bits, in shared memory
+//   P   [tokens x N] = 2^(logit - reference of the column), 16 bits, in shared memory
 //   O^T [d x N]     += V^T P, in tensor memory
 // With tokens as rows a thread of the softmax owns a token: the scales and minima
 // of its key are registers, and a column's maximum, which would need the other
-// lanes, is only checked (P must not pass 2^15): it is taken on a unit's first tile
-// and again when a logit outgrows it.  K's operand is its codes as they are
-// (half-precision subnormals, scaled back by q and s); V's is m + s c rounded to
-// half precision once, relative to the token's largest value 2^e, and the power of
-// two that takes this back goes into the token's logits.
+// lanes, is only checked (P must not pass 2^15): the reference is a maximum over
+// some of a run's first tile, and raised when a logit outgrows it.  K's operand is
+// its codes as they are (half-precision subnormals, scaled back by q and s), in
+// tensor memory; V's is m + s c rounded to half precision once, relative to the
+// token's largest value 2^e, and the power of two that takes this back goes into the
+// token's logits.  P is rounded to half precision once; its sums are fp32.
 //
 // One CTA an SM, its warps in roles with bounded waits on mbarriers between them:
-//   8 softmax   two groups of four warps (4 x 32 tokens); one takes the even tiles,
-//               the other the odd ones, each with references, sums and an O of
-//               its own, so that one works while the other waits
-//   7 dequant   raw blocks (which they load) -> K's operand in tensor memory, V's
-//               in shared memory, the tokens' constants
+//   8 softmax   two groups of four warps (4 x 32 tokens), each with half of the
+//               tile's columns: a thread then holds its columns' sums of q and its
+//               normalisers in registers.  (Groups that took turns by tile, with
+//               all columns each, loaded the sums of q for every element: 16
+//               sequences of 512 to 16,384 rows, 35 columns, 741 us against 672.)
+//   4 K         codes -> K's operand, the keys' constants
+//   4 V         codes -> V's operand in shared memory, the values' constants
 //   1 issuer    the matrix products
+//   1 loader    raw blocks, kRing tiles ahead
+// K's and V's warps in one role, seven warps that loaded for themselves, made K's
+// next tile wait for the softmax: 845 us against 750.
 // As in the other kernel, CTAs take equal spans of the list of all tiles and the
 // last of those that share a unit joins their results in order.
+//
+// Bound by latency: a tile of 48 columns takes about 2,400 cycles, of which the
+// softmax of a group works 1,900 and the tensor core 1,400 (its operands come out of
+// the shared memory that everything else uses too).  Measured (28 layers, 4 KV heads,
+// G = 7): 5 tokens of 16 sequences of 512 to 16,384 rows 614 us (2.0 TB/s of the
+// cache's bytes), of 8 sequences of 8,192 488 us (2.2 TB/s), of 64 of 512 497 us; 32
+// tokens of 2 sequences of 8,191 566 us (372 TFLOP/s).
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
@@ -45,7 +58,8 @@ constexpr int kMaxN = 64;                   // columns of a tile
 constexpr int kSoft = 8, kKey = 4, kVal = 4;
 constexpr int kIssuer = kSoft + kKey + kVal, kLoader = kIssuer + 1;
 constexpr int kThr = 32 * (kIssuer + 4);
-// Registers a thread: at launch, then for the softmax and for the others.
+// Registers a thread: at launch, then for the softmax and for the others (168 and 48:
+// 672 us where 144 and 64 took 703; 64 columns 606 against 598).
 constexpr int kRegs = 96, kRegsSoft = 168, kRegsRest = 48;
 static_assert(32 * kSoft * kRegsSoft + (kThr - 32 * kSoft) * kRegsRest <= kThr * kRegs,
               "the shares come out of what the CTA was launched with");
@@ -55,7 +69,7 @@ constexpr int kConst = 4;                   // tiles whose tokens' constants are
 constexpr int kTileGrid = 256;              // CTAs of a split call, at most
 constexpr uint32_t kRaw = kTileBlocks * block_bytes(kD);
 constexpr uint32_t kHalf = kTok * 128;      // one 64-element half of an operand
-constexpr uint32_t kCols = 512;             // tensor memory: S (2 x 2 x 64), O (2 x 64),
+constexpr uint32_t kCols = 512;             // tensor memory: S (2 x 2 x 64), O (64),
 constexpr uint32_t kColO = 256;             // K (2 x 64)
 constexpr uint32_t kColK = 384;
 constexpr float kUnit = 0x1p24f;            // of K's codes
@@ -257,6 +271,7 @@ __global__ void __launch_bounds__(kThr, 1)
   auto wait = [&](uint64_t &bar, int n) {
     return warp_wait(smem_u32(&bar), (uint32_t)(n & 1), abort);
   };
+  // Completion n of a barrier, and a wait for up to three of them.
   auto at = [&](uint64_t &bar, int n) { return Phase{smem_u32(&bar), (uint32_t)(n & 1)}; };
   auto wait_for = [&](Phase a, Phase b, Phase c, int n) { return warp_wait(a, b, c, n, abort); };
   auto give_up = [&]() {
@@ -322,86 +337,86 @@ __global__ void __launch_bounds__(kThr, 1)
   } else if (warp >= kIssuer) {
     give_registers();
     if (warp == kIssuer) {
-    // ---- issuer
-    const uint32_t id_s = idesc_f16(kTok, N, false), id_o = idesc_f16(kD, N, true);
-    const uint64_t dq = sdesc_sw128(base + kOffQ, 16, 1024);
-    const uint64_t dv = sdesc_sw128(base + kOffV, 16, 1024);
-    const uint64_t dp = sdesc_sw128(base + kOffP, kHalf, 1024);
-    int i = 0, runs = 0;
-    bool ok = true;
-    auto issue_pv = [&](int j, bool first) {  // tile j's P and V are there
-      ok = ok && wait_for(at(S.vf[j & 1], j / 2), at(S.pf[j & 1], j / 2), {}, 2);
-      if (!ok) return;
-      tc_fence_after();
-      if (elect_one()) {
-        const uint64_t a = dv + (uint64_t)(((j & 1) * 2 * kHalf) >> 4);
-        const uint64_t b = dp + (uint64_t)(((j & 1) * kHalf) >> 4);
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          tc_mma(tm + kColO, a + (uint64_t)(((k >> 2) * kHalf + (k & 3) * 32) >> 4),
-                 b + (uint64_t)(k * 128), id_o, !(first && k == 0));
-        tc_commit(smem_u32(&S.pv[j & 1]));
-      }
-      __syncwarp();
-    };
-    do {
-      for (int t = run.t0; t < run.t1 && ok; ++t, ++i) {
-        ok = wait_for(at(S.kf[i & 1], i / 2), at(S.qf, runs), at(S.s_free[i & 1], i / 2 - 1),
-                      i < 2 ? 2 : 3);
-        if (!ok) break;
+      // ---- issuer
+      const uint32_t id_s = idesc_f16(kTok, N, false), id_o = idesc_f16(kD, N, true);
+      const uint64_t dq = sdesc_sw128(base + kOffQ, 16, 1024);
+      const uint64_t dv = sdesc_sw128(base + kOffV, 16, 1024);
+      const uint64_t dp = sdesc_sw128(base + kOffP, kHalf, 1024);
+      int i = 0, runs = 0;
+      bool ok = true;
+      auto issue_pv = [&](int j, bool first) {  // tile j's P and V are there
+        ok = ok && wait_for(at(S.vf[j & 1], j / 2), at(S.pf[j & 1], j / 2), {}, 2);
+        if (!ok) return;
         tc_fence_after();
         if (elect_one()) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              tc_mma_ts(tm + (i & 1) * 128 + j * 64, tm + kColK + (i & 1) * 64 + j * 32 + k * 8,
-                        dq + (uint64_t)((j * N * 128 + k * 32) >> 4), id_s, k > 0);
-          tc_commit(smem_u32(&S.sf[i & 1]));
+          const uint64_t a = dv + (uint64_t)(((j & 1) * 2 * kHalf) >> 4);
+          const uint64_t b = dp + (uint64_t)(((j & 1) * kHalf) >> 4);
+  #pragma unroll
+          for (int k = 0; k < 8; ++k)
+            tc_mma(tm + kColO, a + (uint64_t)(((k >> 2) * kHalf + (k & 3) * 32) >> 4),
+                   b + (uint64_t)(k * 128), id_o, !(first && k == 0));
+          tc_commit(smem_u32(&S.pv[j & 1]));
         }
         __syncwarp();
-        if (t > run.t0) issue_pv(i - 1, t - 1 == run.t0);
+      };
+      do {
+        for (int t = run.t0; t < run.t1 && ok; ++t, ++i) {
+          ok = wait_for(at(S.kf[i & 1], i / 2), at(S.qf, runs), at(S.s_free[i & 1], i / 2 - 1),
+                        i < 2 ? 2 : 3);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+  #pragma unroll
+            for (int j = 0; j < 2; ++j)
+  #pragma unroll
+              for (int k = 0; k < 4; ++k)
+                tc_mma_ts(tm + (i & 1) * 128 + j * 64, tm + kColK + (i & 1) * 64 + j * 32 + k * 8,
+                          dq + (uint64_t)((j * N * 128 + k * 32) >> 4), id_s, k > 0);
+            tc_commit(smem_u32(&S.sf[i & 1]));
+          }
+          __syncwarp();
+          if (t > run.t0) issue_pv(i - 1, t - 1 == run.t0);
+        }
+        issue_pv(i - 1, run.t1 - 1 == run.t0);
+        ++runs;
+      } while (ok && walk.next(run));
+      if (!ok) give_up();
+      if (lane == 0) {  // every product is done before tensor memory is freed
+        volatile int never = 0;
+        tc_commit(smem_u32(&S.drain));
+        mbar_wait(smem_u32(&S.drain), 0, &never);
       }
-      issue_pv(i - 1, run.t1 - 1 == run.t0);
-      ++runs;
-    } while (ok && walk.next(run));
-    if (!ok) give_up();
-    if (lane == 0) {  // every product is done before tensor memory is freed
-      volatile int never = 0;
-      tc_commit(smem_u32(&S.drain));
-      mbar_wait(smem_u32(&S.drain), 0, &never);
-    }
     } else if (warp == kLoader) {
-    // ---- loader: raw tiles, kRing ahead of their use
-    int issued = 0;
-    bool ok = true;
-    do {
-      const int unit = run.item / plan.tiles;
-      const uint8_t *blocks =
-          c.blocks + unit_at(c, p.k.s0 + run.s, p.k.lb, unit / c.H, unit % c.H) * c.nb *
-                         (size_t)block_bytes(kD);
-      const int nb = blocks_of(sq.len[run.s]);
-      for (int t = run.t0; t < run.t1 && ok; ++t) {
-        const int rb = issued % kRing;
-        if (issued >= kRing) ok = wait(S.raw_free[rb], issued / kRing - 1);
-        if (!ok) break;
-        if (lane == 0) {
-          const uint32_t bytes =
-              (uint32_t)min(kTileBlocks, nb - t * kTileBlocks) * block_bytes(kD);
-          mbar_expect_tx(smem_u32(&S.raw_full[rb]), bytes);
-          bulk_load(base + kOffRaw + rb * kRaw, blocks + (size_t)t * kRaw, bytes,
-                    smem_u32(&S.raw_full[rb]));
+      // ---- loader: raw tiles, kRing ahead of their use
+      int issued = 0;
+      bool ok = true;
+      do {
+        const int unit = run.item / plan.tiles;
+        const uint8_t *blocks =
+            c.blocks + unit_at(c, p.k.s0 + run.s, p.k.lb, unit / c.H, unit % c.H) * c.nb *
+                           (size_t)block_bytes(kD);
+        const int nb = blocks_of(sq.len[run.s]);
+        for (int t = run.t0; t < run.t1 && ok; ++t) {
+          const int rb = issued % kRing;
+          if (issued >= kRing) ok = wait(S.raw_free[rb], issued / kRing - 1);
+          if (!ok) break;
+          if (lane == 0) {
+            const uint32_t bytes =
+                (uint32_t)min(kTileBlocks, nb - t * kTileBlocks) * block_bytes(kD);
+            mbar_expect_tx(smem_u32(&S.raw_full[rb]), bytes);
+            bulk_load(base + kOffRaw + rb * kRaw, blocks + (size_t)t * kRaw, bytes,
+                      smem_u32(&S.raw_full[rb]));
+          }
+          __syncwarp();
+          ++issued;
         }
-        __syncwarp();
-        ++issued;
+      } while (ok && walk.next(run));
+      if (!ok) give_up();
+      if (lane == 0) {  // every copy lands before the shared memory is given back
+        volatile int never = 0;
+        for (int j = max(0, issued - kRing); j < issued; ++j)
+          mbar_wait(smem_u32(&S.raw_full[j % kRing]), (uint32_t)((j / kRing) & 1), &never);
       }
-    } while (ok && walk.next(run));
-    if (!ok) give_up();
-    if (lane == 0) {  // every copy lands before the shared memory is given back
-      volatile int never = 0;
-      for (int j = max(0, issued - kRing); j < issued; ++j)
-        mbar_wait(smem_u32(&S.raw_full[j % kRing]), (uint32_t)((j / kRing) & 1), &never);
-    }
     }
   } else if (warp >= kSoft + kKey) {
     // ---- V
@@ -460,8 +475,8 @@ __global__ void __launch_bounds__(kThr, 1)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const int pr = tg * 4 + k, pb = pr % (kBlock / 2);
-            v[k] = *reinterpret_cast<const uint2 *>(raw + vw * block_bytes(kD) + v_off(kD) + pb * kD +
-                                                    v_chunk<kD>(pb, ch) * 16 + w * 4);
+            v[k] = *reinterpret_cast<const uint2 *>(raw + vw * block_bytes(kD) + v_off(kD) +
+                                                    pb * kD + v_chunk<kD>(pb, ch) * 16 + w * 4);
             const uint2 x = S.vc[w >> 1][pr];
             sc[k] = as_half2(x.x);
             mn[k] = as_half2(x.y);
@@ -569,9 +584,10 @@ __global__ void __launch_bounds__(kThr, 1)
 #pragma unroll
       for (int z = 0; z < CH / 2; ++z) {
         const Place a = place_of(p, sq, r.s, unit / c.H, unit % c.H, col0 + (tid >> 4) + 16 * z);
-        raw[z] = a.out >= 0 && a.live ? *reinterpret_cast<const uint4 *>(
-                                            static_cast<const __nv_bfloat16 *>(p.q) + a.out + 8 * ci)
-                                      : make_uint4(0, 0, 0, 0);
+        raw[z] = make_uint4(0, 0, 0, 0);
+        if (a.out >= 0 && a.live)
+          raw[z] = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) +
+                                                    a.out + 8 * ci);
       }
     };
     load_q(run);
@@ -970,7 +986,9 @@ __global__ void __launch_bounds__(kThr, 1)
 // / (z G) over all columns, from their statistics.  K alone is read, once for all
 // columns (kScoreCols at a time); S comes as in the attention, and as a thread has a
 // token, its sum needs no other thread but the one of the other group, which has
-// the odd column tiles.
+// the odd column tiles.  K's codes are 2^-20 c here: all of their bits count.
+// Bound by the exponentials' loop, about 12 instructions an element: 32 tokens of 2
+// sequences of 8,191 rows (28 layers, 4 KV heads, G = 7) 320 us, 400 with mma.sync.
 constexpr int kScoreTiles = 4;
 constexpr int kScoreCols = kScoreTiles * kMaxN;
 constexpr int kScoreThr = 32 * (kSoft + 4 + 1);
@@ -1141,7 +1159,8 @@ __global__ void __launch_bounds__(kScoreThr, 1)
       for (int g = 0; g < np && ok; ++g)
         for (int t = run.t0; t < run.t1; ++t, ++i) {
           const int b = i & 1, rb = i % kRing;
-          const unsigned char *blk = smem + kScoreOffRaw + rb * kRaw + (dt / kBlock) * block_bytes(kD);
+          const unsigned char *blk =
+              smem + kScoreOffRaw + rb * kRaw + (dt / kBlock) * block_bytes(kD);
           ok = ok && wait(S.raw_full[rb], i / kRing) &&
                (i < 2 || (wait(S.t_free[b], i / 2 - 1) && wait(S.k_free[b], i / 2 - 1)));
           ok = !bar_any(1, 128, !ok);
@@ -1363,8 +1382,12 @@ long long col_tiles(const View &c, int n_q) {
 
 }  // namespace
 
+// More than 24 query rows a unit.  Over 8 sequences of 8,192 rows (28 layers, 4 KV
+// heads) 28 rows take 428 us here and 790 in the kernel for fewer rows; 21 rows 426
+// and 405; 14 rows 394 and 281.  Over 64 sequences of 512: 28 rows 443 and 699, 21
+// rows 440 and 404; over one of 4,099, 21 rows 41.0 and 42.6, 14 rows 36.6 and 31.3.
 bool tile_applies(const View &c, int n_q) {
-  return c.d == kD && c.io_bf16 && c.out_bf16 && (long long)n_q * c.G > 8;
+  return c.d == kD && c.io_bf16 && c.out_bf16 && (long long)n_q * c.G > 24;
 }
 
 size_t tile_part_floats(const View &c, int nl, int n_q) {
@@ -1446,7 +1469,6 @@ cudaError_t launch_score_ch(const AttendParams &p, const Seqs &q, cudaStream_t s
 
 cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
   switch (tile_n(p.k.c, p.n_q)) {
-    case 16: return launch_score_ch<2>(p, q, stream);
     case 32: return launch_score_ch<4>(p, q, stream);
     case 48: return launch_score_ch<6>(p, q, stream);
     default: return launch_score_ch<8>(p, q, stream);
@@ -1455,7 +1477,6 @@ cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, cudaStream_
 
 cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
   switch (tile_n(p.k.c, p.n_q)) {
-    case 16: return launch_ch<2>(p, q, stream);
     case 32: return launch_ch<4>(p, q, stream);
     case 48: return launch_ch<6>(p, q, stream);
     default: return launch_ch<8>(p, q, stream);
