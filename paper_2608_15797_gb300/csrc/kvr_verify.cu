@@ -377,10 +377,10 @@ cudaError_t launch(Params &p, cudaStream_t st) {
   const long long grid = std::min<long long>((total + kWarps - 1) / kWarps, 4 * sms);
   e = kvr::launch_pdl(stats_kernel<T>, dim3((unsigned)grid), dim3(kThreads), 0, st, p);
   if (e != cudaSuccess) return e;
-  // CTAs of a sequence: about four an SM over all sequences, a group a thread at
-  // least (64 sequences of 152,064: 10 a sequence)
+  // CTAs of a sequence: at most four an SM over all sequences, which run at once, a
+  // group a thread at least (64 sequences of 152,064: 9 a sequence)
   const int ctas = (int)std::max<long long>(
-      1, std::min<long long>((4 * sms + p.S - 1) / p.S, p.V / (N * kThreads)));
+      1, std::min<long long>(4 * sms / p.S, p.V / (N * kThreads)));
   return kvr::launch_pdl(decide_kernel<T>, dim3(ctas, p.S), dim3(kThreads), 0, st, p);
 }
 
