@@ -950,7 +950,10 @@ kvr_status kvr_kv4_sync_status(kvr_kv4 *c, void *stream) {
   e = cudaMemcpy(&word, c->view.err, sizeof word, cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return cuda_fail("kvr_kv4_sync_status: read", e);
   if (!word) return KVR_OK;
-  e = cudaMemset(c->view.err, 0, sizeof word);
+  // The tickets lie ahead of the word, and a launch that gave up a wait may have
+  // left some of its arrivals there.
+  auto *from = reinterpret_cast<uint8_t *>(c->view.ticket);
+  e = cudaMemset(from, 0, reinterpret_cast<uint8_t *>(c->view.err) + sizeof word - from);
   if (e != cudaSuccess) return cuda_fail("kvr_kv4_sync_status: clear", e);
   return fail(KVR_EDEVICE, "device error word 0x%x (%s%s%s)", word,
               word & kvr::ERR_NONFINITE ? "non-finite " : "",

@@ -142,3 +142,19 @@ def test_rows_past_31_bits(T, G):
     want = [sum(1 / (t + 1) for t in range(j, T)) for j in range(T)]
     np.testing.assert_allclose(score[n:n + T].cpu().numpy(), want, rtol=1e-4)
     c.sync_status()
+
+
+@pytest.mark.parametrize("T", [1, 5])
+def test_status_clears_what_a_launch_that_gave_up_left(T):
+    """Behind the scores lie the arrivals of units that CTAs share and the
+    error word; with the error reported all of them are cleared, and units that
+    are cut are joined rightly again."""
+    p = Pair(1, 1, 1, 7, 128, 5000)
+    p.load(0, 5000, 11)
+    view = p.c.scores_view()
+    end = view.data_ptr() - p.c.buf.data_ptr() + 4 * view.stride(2)
+    p.c.buf[end:p.c.nbytes] = 1
+    with pytest.raises(kvr.KvrError, match="KVR_EDEVICE"):
+        p.c.sync_status()
+    p.check_attend(rnd(6, (1, 1, T, 7, 128)), scores=True)
+    p.c.sync_status()
