@@ -71,7 +71,8 @@ __device__ __forceinline__ void widen(const Eight<float> &a, int side, float (&x
     x[side ? 4 + f : 2 * f + 1] = __uint_as_float(a.w[2 * f + 1]);
   }
 }
-// The least and the greatest of the eight; true if one is not finite.
+// The least and the greatest of a group, over its eight lanes; true if one of the
+// lane's own is not finite.
 __device__ __forceinline__ bool extremes(const Eight<float> &, const float (&x)[8], float &lo,
                                          float &hi) {
   float odd = 0.f;
@@ -81,6 +82,11 @@ __device__ __forceinline__ bool extremes(const Eight<float> &, const float (&x)[
     lo = fminf(lo, x[e]);
     hi = fmaxf(hi, x[e]);
     odd = fmaf(x[e], 0.f, odd);  // NaN for what is not finite
+  }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
   }
   return odd != 0.f;
 }
@@ -95,8 +101,20 @@ __device__ __forceinline__ bool extremes(const Eight<__nv_bfloat16> &a, const fl
   __nv_bfloat162 odd = __hfma2(w[0], zero, zero);
 #pragma unroll
   for (int f = 1; f < 4; ++f) odd = __hfma2(w[f], zero, odd);
-  lo = fminf(__low2float(least), __high2float(least));
-  hi = fmaxf(__low2float(most), __high2float(most));
+  // the least and minus the greatest as one word: an exchange and a minimum for both
+  const __nv_bfloat162 l = __hmin2(least, __lowhigh2highlow(least));
+  const __nv_bfloat162 h = __hmax2(most, __lowhigh2highlow(most));
+  uint32_t both = (*reinterpret_cast<const uint32_t *>(&l) & 0xFFFFu) |
+                  ((*reinterpret_cast<const uint32_t *>(&h) & 0xFFFF0000u) ^ 0x80000000u);
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) {
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, both, o);
+    const __nv_bfloat162 y = __hmin2(*reinterpret_cast<const __nv_bfloat162 *>(&both),
+                                     *reinterpret_cast<const __nv_bfloat162 *>(&other));
+    both = *reinterpret_cast<const uint32_t *>(&y);
+  }
+  lo = __uint_as_float(both << 16);
+  hi = __uint_as_float((both & 0xFFFF0000u) ^ 0x80000000u);
   return (*reinterpret_cast<const uint32_t *>(&odd) & 0x7FFF7FFFu) != 0;
 }
 __device__ __forceinline__ void store_eight(const float (&x)[8], int side, int i,
@@ -238,11 +256,6 @@ __device__ __forceinline__ void append_rows(const Call &k, const Seqs &q, const 
     float x[8], lo, hi;
     widen(in[n], SIDE, x);
     const bool odd = extremes(in[n], x, lo, hi);
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) {  // the eight lanes of a group
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
     const unsigned bad = __ballot_sync(0xffffffffu, odd);
     bool flat;
     const uint32_t meta =
