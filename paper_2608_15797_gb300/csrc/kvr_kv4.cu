@@ -224,9 +224,9 @@ __device__ __forceinline__ Task task_of(const Call &k, int groups) {
 
 // Quantise the new rows.  D / 8 lanes a row, eight channels a lane; a warp takes
 // kRows rows of one side (key or value) at a time, their loads in flight together.
-// Many tokens are bound by instructions as much as by bytes (2 x 8,191 tokens of 28
-// layers, 2 KV heads: 321 us, 3.8 TB/s read and written), few by latency (one token of
-// 28 layers, 4 KV heads: 4 us).
+// Many tokens are bound by instructions (2 x 8,191 tokens of 28 layers, 2 KV heads: 196
+// us, 3.1 TB/s read and written), few by latency (one token of 28 layers, 4 KV heads
+// and its reading back: 4 us).
 template <typename T, int D>
 struct Append {
   static constexpr int kLanes = D / 8;             // of a row
@@ -317,7 +317,8 @@ __device__ __forceinline__ void word_values(const RowWords &a, float (&x)[8]) {
   }
 }
 
-// What the newest rows stand for: D / 8 lanes a row and side.
+// What the newest rows stand for: D / 8 lanes a row and side.  Bound by the bytes: the
+// same 2 x 8,191 rows 123 us, 4.9 TB/s.
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
     read_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q, int groups,
