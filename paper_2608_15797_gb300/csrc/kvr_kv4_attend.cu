@@ -200,11 +200,12 @@ __device__ __forceinline__ void load_query(Query<D, NT, TERMS> &q, const AttendP
                                            const Seqs &sq, int s, int lr, int h, int col0) {
   const View &c = p.k.c;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int rows = p.n_q * c.G, count = sq.count[s], before = sq.len[s] - count;
+  const int count = sq.count[s], before = sq.len[s] - count;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int col = col0 + 8 * n + g, tok = col / c.G;
-    const bool live = col < rows;
+    // (a token that the sequence has not may hold anything: its columns are zeros)
+    const bool live = tok < count;
     const T *src = static_cast<const T *>(p.q) +
                    (((((size_t)(p.k.s0 + s) * p.k.nl + lr) * p.n_q + tok) * c.H + h) * c.G +
                     (col - tok * c.G)) *
@@ -263,7 +264,7 @@ __device__ __forceinline__ void load_query(Query<D, NT, TERMS> &q, const AttendP
     }
     const float unit =
         field_unit(M) * __uint_as_float((unsigned)(127 - k) << 23) * (c.scale * kLog2e);
-    const int limit = live && tok < count ? before + tok : -1;
+    const int limit = live ? before + tok : -1;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int from = 8 * t + 4 * e;  // a lane of column 2 t + e
