@@ -1055,14 +1055,17 @@ def verify_workspace(n_seq, n_draft, vocab, device="cuda"):
 
 
 def _logit_rows(x, what):
-    """Row stride of logits [S][n][V]: rows dense among themselves, each row's
-    logits side by side."""
+    """Row stride of logits [S][n][V]: a row's logits side by side, the rows one
+    stride apart, which is V at least where there is more than one of them."""
     S, n, V = x.shape
     if x.is_contiguous():
         return V
     rows, col = x.stride()[1:] if n > 1 else (x.stride(0), x.stride(2))
     if col != 1 and V > 1 or S > 1 and x.stride(0) != n * rows:
         raise ValueError(f"{what}: rows must lie one stride apart")
+    if S * n > 1 and rows < V:
+        raise ValueError(f"{what}: rows must not overlap (stride {rows} of "
+                         f"{V} logits)")
     return max(rows, V)
 
 
