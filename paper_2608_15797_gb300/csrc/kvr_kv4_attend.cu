@@ -450,7 +450,12 @@ __device__ __forceinline__ void block_step(State<D, NT, TERMS> &a, const Query<D
 #pragma unroll
       for (int j = 0; j < GR; ++j) {
         meta_of<kV == kCentred>(vm[tt][b][j], false, m[j], sc[j]);
-        if (TERMS == 1) m[j] = MASK && vm[tt][b][j] == 0 ? 0.f : m[j] * rcp(sc[j]) * a.back;
+        if (TERMS == 1) {
+          // A subnormal s has no reciprocal.  It counts as 2^-126, which moves a
+          // value by less than 15 2^-126.  (So does that of a row that is not.)
+          sc[j] = fmaxf(sc[j], 0x1p-126f);
+          m[j] *= rcp(sc[j]) * a.back;
+        }
         sc[j] *= a.ref;
       }
 #pragma unroll
