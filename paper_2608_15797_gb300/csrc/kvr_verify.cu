@@ -183,7 +183,9 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const __grid_constant__
       w[k] = v < nv ? r.load(v) : make_uint4(none, none, none, none);
     }
     const float m = kvr::dev::warp_max(greatest<T>(w));
-    const uint64_t c2 = pk2(p.c, p.c), ref2 = pk2(-above(m) * p.c, -above(m) * p.c);
+    // Subtracted first, then scaled, as everywhere below: exact at the maximum.  (The
+    // product c m rounds by 0.1 and more where m is 20 and the temperature 1e-5.)
+    const uint64_t c2 = pk2(p.c, p.c), ref2 = pk2(-above(m), -above(m));
     uint64_t z2[2] = {0, 0};
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
@@ -192,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const __grid_constant__
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
         float a, b;
-        upk2(fma2(pk2(x[e], x[e + 1]), c2, ref2), a, b);
+        upk2(mul2(add2(pk2(x[e], x[e + 1]), ref2), c2), a, b);
         z2[(e >> 1) & 1] = add2(z2[(e >> 1) & 1], pk2(ex2(a), ex2(b)));
       }
     }
