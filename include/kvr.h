@@ -631,7 +631,9 @@ typedef struct {
   int n_seq;      /* S, 1..65535 */
   int n_draft;    /* 0..64 */
   int vocab;      /* >= 1 */
-  float temperature; /* > 0; 0 means 1 */
+  float temperature; /* > 0, log2(e) / temperature finite.  0, a sampler's
+                        greedy choice, is refused: a greedy draft is checked
+                        by comparing tokens */
   kvr_dtype logits_dtype;
 } kvr_verify_desc;
 

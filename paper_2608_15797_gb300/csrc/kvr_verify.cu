@@ -356,9 +356,14 @@ kvr_status fail(kvr_status st, const char *msg) {
   return static_cast<kvr_status>(kvr::report_error(st, msg));
 }
 
+// log2(e) / temperature; infinite or NaN where the temperature cannot be used.
+float scale_of(float temperature) {
+  return temperature > 0.f && std::isfinite(temperature) ? kLog2e / temperature : NAN;
+}
+
 bool desc_ok(const kvr_verify_desc *d) {
   return d && d->n_seq >= 1 && d->n_seq <= 65535 && d->n_draft >= 0 && d->n_draft <= 64 &&
-         d->vocab >= 1 && d->temperature >= 0.f && std::isfinite(d->temperature) &&
+         d->vocab >= 1 && std::isfinite(scale_of(d->temperature)) &&
          (d->logits_dtype == KVR_BF16 || d->logits_dtype == KVR_F32);
 }
 
@@ -436,7 +441,7 @@ kvr_status kvr_verify_drafts(const kvr_verify_desc *d, const void *target,
   p.S = d->n_seq;
   p.T = d->n_draft;
   p.V = d->vocab;
-  p.c = kLog2e / (d->temperature > 0.f ? d->temperature : 1.f);
+  p.c = scale_of(d->temperature);
   p.target = target;
   p.draft = draft;
   p.ts = target_stride;

@@ -1074,8 +1074,8 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
                   workspace=None, stream=None):
     """Accept or reject drafted tokens (kvr_verify_drafts): target logits
     [S][T + 1][V], draft logits [S][T][V], tokens int32 and u fp32 [S][T], race
-    fp32 [S][V] (exponential, > 0), n_draft int32 [S] or None.  Returns
-    (accepted [S], tokens [S][T + 1]) on the device."""
+    fp32 [S][V] (exponential, > 0), n_draft int32 [S] or None; temperature > 0
+    (0 is refused).  Returns (accepted [S], tokens [S][T + 1]) on the device."""
     S, n, V = target.shape
     T = n - 1
     if draft.shape != (S, T, V) or draft.dtype is not target.dtype or \
