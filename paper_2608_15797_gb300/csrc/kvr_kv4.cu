@@ -958,16 +958,19 @@ kvr_status kvr_kv4_launch_count(const kvr_kv4 *c, uint64_t *count) {
 
 kvr_status kvr_kv4_sync_status(kvr_kv4 *c, void *stream) {
   if (!c) return fail(KVR_EINVAL, "null cache");
-  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
-  if (e != cudaSuccess) return cuda_fail("kvr_kv4_sync_status: sync", e);
+  // All on the caller's stream: one that does not wait for the default stream would
+  // not wait for what is cleared there either.
+  const cudaStream_t cs = static_cast<cudaStream_t>(stream);
   unsigned word = 0;
-  e = cudaMemcpy(&word, c->view.err, sizeof word, cudaMemcpyDeviceToHost);
+  cudaError_t e = cudaMemcpyAsync(&word, c->view.err, sizeof word, cudaMemcpyDeviceToHost, cs);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cs);
   if (e != cudaSuccess) return cuda_fail("kvr_kv4_sync_status: read", e);
   if (!word) return KVR_OK;
   // The tickets lie ahead of the word, and a launch that gave up a wait may have
   // left some of its arrivals there.
   auto *from = reinterpret_cast<uint8_t *>(c->view.ticket);
-  e = cudaMemset(from, 0, reinterpret_cast<uint8_t *>(c->view.err) + sizeof word - from);
+  e = cudaMemsetAsync(from, 0, reinterpret_cast<uint8_t *>(c->view.err) + sizeof word - from, cs);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cs);
   if (e != cudaSuccess) return cuda_fail("kvr_kv4_sync_status: clear", e);
   return fail(KVR_EDEVICE, "device error word 0x%x (%s%s%s)", word,
               word & kvr::ERR_NONFINITE ? "non-finite " : "",
