@@ -1276,36 +1276,41 @@ kvr_status kvr_cache_import(kvr_cache *c, int seq, const void *host_k,
                       "layer %d head %d: live positions must be distinct and "
                       "in [0, %d)", l, h, np);
     }
-  cudaError_t e = cudaStreamSynchronize(as_stream(stream));
-  if (e != cudaSuccess) return cuda_fail("kvr_cache_import: sync", e);
+  // All on the caller's stream, and waited for: a copy from pageable memory on the
+  // default stream may still be on its way when the call returns, and a stream that
+  // does not wait for that one would decode from rows that are not there yet.
+  const cudaStream_t cs = as_stream(stream);
   const size_t units = (size_t)L * H, rows = units * cap;
   const size_t ebytes = (size_t)v.d * esize(c->desc.kv_dtype);
-  e = cudaMemcpy(static_cast<char *>(v.K) + seq * rows * ebytes, host_k,
-                 rows * ebytes, cudaMemcpyHostToDevice);
-  if (e == cudaSuccess)
-    e = cudaMemcpy(static_cast<char *>(v.V) + seq * rows * ebytes, host_v,
-                   rows * ebytes, cudaMemcpyHostToDevice);
-  if (e == cudaSuccess)
-    e = cudaMemcpy2D(v.score + seq * units * v.sstride, (size_t)v.sstride * 4,
-                     host_score, (size_t)cap * 4, (size_t)cap * 4, units,
-                     cudaMemcpyHostToDevice);
-  if (e == cudaSuccess)
-    e = cudaMemcpy2D(v.pos + seq * units * v.sstride, (size_t)v.sstride * 4,
-                     host_pos, (size_t)cap * 4, (size_t)cap * 4, units,
-                     cudaMemcpyHostToDevice);
   std::vector<int32_t> st(units * 4);
-  if (e == cudaSuccess)
-    e = cudaMemcpy(st.data(), v.state + seq * units * 4,
-                   st.size() * sizeof(int32_t), cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess) {
-    for (size_t i = 0; i < units; ++i) {
-      st[4 * i] = host_len[i];
-      st[4 * i + 1] = host_next_pos[i];
-      st[4 * i + 2] = 0;  // no R-KV key sum for the imported rows
-    }
-    e = cudaMemcpy(v.state + seq * units * 4, st.data(),
-                   st.size() * sizeof(int32_t), cudaMemcpyHostToDevice);
+  int32_t *state = v.state + seq * units * 4;
+  cudaError_t e = cudaMemcpyAsync(st.data(), state, st.size() * sizeof(int32_t),
+                                  cudaMemcpyDeviceToHost, cs);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cs);
+  if (e != cudaSuccess) return cuda_fail("kvr_cache_import: sync", e);
+  for (size_t i = 0; i < units; ++i) {
+    st[4 * i] = host_len[i];
+    st[4 * i + 1] = host_next_pos[i];
+    st[4 * i + 2] = 0;  // no R-KV key sum for the imported rows
   }
+  e = cudaMemcpyAsync(static_cast<char *>(v.K) + seq * rows * ebytes, host_k,
+                      rows * ebytes, cudaMemcpyHostToDevice, cs);
+  if (e == cudaSuccess)
+    e = cudaMemcpyAsync(static_cast<char *>(v.V) + seq * rows * ebytes, host_v,
+                        rows * ebytes, cudaMemcpyHostToDevice, cs);
+  if (e == cudaSuccess)
+    e = cudaMemcpy2DAsync(v.score + seq * units * v.sstride,
+                          (size_t)v.sstride * 4, host_score, (size_t)cap * 4,
+                          (size_t)cap * 4, units, cudaMemcpyHostToDevice, cs);
+  if (e == cudaSuccess)
+    e = cudaMemcpy2DAsync(v.pos + seq * units * v.sstride,
+                          (size_t)v.sstride * 4, host_pos, (size_t)cap * 4,
+                          (size_t)cap * 4, units, cudaMemcpyHostToDevice, cs);
+  if (e == cudaSuccess)
+    e = cudaMemcpyAsync(state, st.data(), st.size() * sizeof(int32_t),
+                        cudaMemcpyHostToDevice, cs);
+  const cudaError_t done = cudaStreamSynchronize(cs);  // host buffers are free again
+  if (e == cudaSuccess) e = done;
   if (e != cudaSuccess) return cuda_fail("kvr_cache_import", e);
   for (int l = 0; l < L; ++l) {
     c->len[(size_t)seq * L + l] = host_len[(size_t)l * H];
@@ -1346,13 +1351,16 @@ kvr_status kvr_cache_launch_count(const kvr_cache *c, uint64_t *count) {
 
 kvr_status kvr_sync_status(kvr_cache *c, void *stream) {
   if (!c) return fail(KVR_EINVAL, "null cache");
-  cudaError_t e = cudaStreamSynchronize(as_stream(stream));
-  if (e != cudaSuccess) return cuda_fail("kvr_sync_status: sync", e);
+  const cudaStream_t cs = as_stream(stream);
   unsigned word = 0;
-  e = cudaMemcpy(&word, c->view.err, sizeof word, cudaMemcpyDeviceToHost);
+  cudaError_t e = cudaMemcpyAsync(&word, c->view.err, sizeof word,
+                                  cudaMemcpyDeviceToHost, cs);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cs);
   if (e != cudaSuccess) return cuda_fail("kvr_sync_status: read", e);
   if (!word) return KVR_OK;
-  e = cudaMemset(c->view.err, 0, sizeof word);
+  // on the caller's stream, so that it cannot clear what a later launch reports
+  e = cudaMemsetAsync(c->view.err, 0, sizeof word, cs);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cs);
   if (e != cudaSuccess) return cuda_fail("kvr_sync_status: clear", e);
   return fail(KVR_EDEVICE, "device error word 0x%x (%s%s%s%s)", word,
               word & kvr::ERR_CAPACITY ? "capacity " : "",

@@ -855,13 +855,16 @@ kvr_status kvr_entropy_export(kvr_entropy *det, float *host_hist,
 
 kvr_status kvr_entropy_sync_status(kvr_entropy *det, void *stream) {
   if (!det) return fail(KVR_EINVAL, "null detector");
-  cudaError_t e = cudaStreamSynchronize(as_stream(stream));
-  if (e != cudaSuccess) return cuda_fail("kvr_entropy_sync_status: sync", e);
+  const cudaStream_t st = as_stream(stream);
   unsigned word = 0;
-  e = cudaMemcpy(&word, det->v.err, sizeof word, cudaMemcpyDeviceToHost);
+  cudaError_t e = cudaMemcpyAsync(&word, det->v.err, sizeof word,
+                                  cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
   if (e != cudaSuccess) return cuda_fail("kvr_entropy_sync_status: read", e);
   if (!word) return KVR_OK;
-  e = cudaMemset(det->v.err, 0, sizeof word);
+  // on the caller's stream, so that it cannot clear what a later step reports
+  e = cudaMemsetAsync(det->v.err, 0, sizeof word, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
   if (e != cudaSuccess) return cuda_fail("kvr_entropy_sync_status: clear", e);
   return fail(KVR_EDEVICE, "non-finite logits in a row (entropy is NaN)");
 }

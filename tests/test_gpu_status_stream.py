@@ -48,3 +48,50 @@ def test_kv4_status_on_a_stream_of_its_own():
     st.synchronize()
     assert not event.query()
     assert torch.equal(out, want)
+
+
+def test_cache_status_and_import_on_a_stream_of_their_own():
+    """The evicted cache's status, with an error and without, and an import that
+    a step on the same stream decodes from."""
+    c = kvr.Cache(1, 1, 1, 2, 128, 40)
+    x = dev(rnd(1, (1, 1, 20, 128)))
+    c.load(0, x, x)
+    step = [dev(rnd(2 + i, (1, 1, h, 128))) for i, h in enumerate((2, 1, 1))]
+    state = c.export(0)
+    want = c.step(*step, 16, 8)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = torch.empty_like(want)
+    bad = torch.full_like(step[0], float("nan"))
+    torch.cuda.synchronize()
+    c.import_state(0, state, st)
+    c.sync_status(st)
+    event = busy_default_stream()
+    c.step(bad, *step[1:], 16, 8, out=out, stream=st)
+    with pytest.raises(kvr.KvrError, match="KVR_EDEVICE"):
+        kvr.kvr_sync_status(c.handle, st)
+    c.import_state(0, state, st)
+    c.step(*step, 16, 8, out=out, stream=st)
+    kvr.kvr_sync_status(c.handle, st)
+    assert not event.query()
+    assert torch.equal(out, want)
+
+
+def test_detector_status_on_a_stream_of_its_own():
+    det = kvr.EntropyDetector(2, 1000)
+    logits = dev(rnd(1, (2, 1000)))
+    bad = logits.clone()
+    bad[1, 7] = float("nan")
+    st = torch.cuda.Stream()
+    outs = [torch.empty(2, dtype=t, device="cuda") for t in
+            (torch.float32, torch.float32, torch.int32)]
+    det.step(logits, *outs)
+    torch.cuda.synchronize()
+    det.sync_status(st)
+    event = busy_default_stream()
+    det.step(bad, *outs, stream=st)
+    with pytest.raises(kvr.KvrError, match="KVR_EDEVICE"):
+        det.sync_status(st)
+    det.step(logits, *outs, stream=st)
+    det.sync_status(st)
+    assert not event.query()
