@@ -92,7 +92,7 @@ struct __align__(16) Side {
   uint2 vc[2][kTok / 2];        // [group][pair]: s 2^(18 - e - 1), m 2^-(e + 1), halves
   float4 qs[kMaxN / 2];         // sums of q: group 0 of two columns, group 1
   float ntop[kMaxN];            // minus the columns' references
-  float factor[kMaxN], again[kMaxN];
+  float factor[kMaxN];
   float wmax[4][kMaxN], zsum[4][kMaxN];
   int limit[kMaxN];             // last row a column sees, or -1
   float2 stat[kMaxN];
@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(kThr, 1)
     constexpr int NG = N / 2, CG = CH / 2;  // columns of the group, and their eights
     const int c0 = grp * NG;
     const uint32_t to = tm + kColO + c0 + lanes;
-    float *const ntop = S.ntop + c0, *const factor = S.factor + c0, *const anew = S.again + c0;
+    float *const ntop = S.ntop + c0, *const factor = S.factor + c0;
     auto all_ok = [&](bool ok) { return !bar_any(2, 32 * kSoft, !ok); };
     auto group_ok = [&](bool ok) { return !bar_any(3 + grp, 16 * kSoft, !ok); };
     int i = 0, runs = 0;  // i: tiles before the run
@@ -699,9 +699,9 @@ __global__ void __launch_bounds__(kThr, 1)
           }
         };
         // P of the tile against the present references; true if one is too large.
-        // `again`: the references were raised; columns whose sums hold the tile
-        // already (anew 0) stay.
-        auto probabilities = [&](bool again) {
+        // `again`: the references were raised; the lane's sums hold the tile already,
+        // but for the columns (a bit each) of `anew`.
+        auto probabilities = [&](bool again, uint32_t anew) {
           __half2 most = __float2half2_rn(0.f);
           float a0[8], a1[8];
           tmem_ld8(ts, a0);
@@ -726,8 +726,8 @@ __global__ void __launch_bounds__(kThr, 1)
               w[e] = half2_bits(ph);
               uint64_t p2 = pk2(u, v);
               if (again) {
-                const float2 f = *reinterpret_cast<const float2 *>(&anew[8 * k + 2 * e]);
-                p2 = mul2(p2, pk2(f.x, f.y));
+                const uint32_t mine = anew >> (8 * k + 2 * e);
+                p2 = pk2(mine & 1 ? u : 0.f, mine & 2 ? v : 0.f);
               }
               z2[4 * k + e] = fma2(p2, down2, z2[4 * k + e]);
             }
@@ -777,7 +777,7 @@ __global__ void __launch_bounds__(kThr, 1)
           if (!ok) break;
         }
         if (ok && !grow) {
-          grow = probabilities(false);
+          grow = probabilities(false, 0);
           tc_fence_before();
         }
         if (bar_any(3 + grp, 16 * kSoft, grow || !ok)) {
@@ -793,10 +793,7 @@ __global__ void __launch_bounds__(kThr, 1)
             float now = old;
 #pragma unroll
             for (int w = 0; w < 4; ++w) now = fmaxf(now, S.wmax[w][c0 + gt]);
-            // a sum over 2^64 behind, which may have overflowed, is begun anew
-            const bool fresh = begin || now - old > 64.f;
             factor[gt] = ex2(old - now);
-            anew[gt] = fresh ? 1.f : 0.f;
             ntop[gt] = -now;
           }
           ok = group_ok(ok);
@@ -815,15 +812,21 @@ __global__ void __launch_bounds__(kThr, 1)
             }
             tmem_wait_st();
           }
+          // A sum that the tile made infinite is begun anew.  Against its token's
+          // probability, 2^(128 - e) of the old reference's or more, what it held was
+          // nothing: 2^15 a tile for values like that token's, and 2^74 where they are
+          // next to nothing (e = -59).
+          uint32_t anew = 0;
 #pragma unroll
           for (int e = 0; e < 4 * CG; ++e) {
             const float2 f = *reinterpret_cast<const float2 *>(&factor[2 * e]);
-            const float2 g = *reinterpret_cast<const float2 *>(&anew[2 * e]);
             float u, v;
             upk2(z2[e], u, v);
-            z2[e] = pk2(g.x > 0.f ? 0.f : u * f.x, g.y > 0.f ? 0.f : v * f.y);
+            const bool fu = begin || u == INFINITY, fv = begin || v == INFINITY;
+            anew |= (fu ? 1u : 0u) << (2 * e) | (fv ? 2u : 0u) << (2 * e);
+            z2[e] = pk2(fu ? 0.f : u * f.x, fv ? 0.f : v * f.y);
           }
-          probabilities(true);
+          probabilities(true, anew);
           tc_fence_before();
           ok = group_ok(ok);
           if (!ok) break;
