@@ -450,13 +450,11 @@ __device__ __forceinline__ void block_step(State<D, NT, TERMS> &a, const Query<D
 #pragma unroll
       for (int j = 0; j < GR; ++j) {
         meta_of<kV == kCentred>(vm[tt][b][j], false, m[j], sc[j]);
-        if (TERMS == 1) {
-          // A subnormal s has no reciprocal.  It counts as 2^-126, which moves a
-          // value by less than 15 2^-126.  (So does that of a row that is not.)
-          sc[j] = fmaxf(sc[j], 0x1p-126f);
-          m[j] *= rcp(sc[j]) * a.back;
-        }
+        // m / s over what has been held against a.ref: a step that is subnormal itself
+        // has no reciprocal, 2^116 times it has.  Below 2^-126, half precision leaves
+        // nothing of p s, and any finite number will do.
         sc[j] *= a.ref;
+        if (TERMS == 1) m[j] *= rcp(fmaxf(sc[j], 0x1p-126f));
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
