@@ -587,15 +587,20 @@ cudaError_t launch_evict(const Call &k, Seqs q, const CacheView &dst, int budget
     return launch_pdl(evict_kernel<T, D, false>, grid, dim3(kEvictThreads), 0, stream, k, q, dst,
                       budget, window);
   auto kern = evict_kernel<T, D, true>;
-  static bool ready = false;
-  if (!ready) {
-    const cudaError_t e = cudaFuncSetAttribute(
-        kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictSmemRows * 4);
-    if (e != cudaSuccess) return e;
-    ready = true;
-  }
   const int bytes = most > budget ? round_up16(most) * 4 : 0;
   return launch_pdl(kern, grid, dim3(kEvictThreads), bytes, stream, k, q, dst, budget, window);
+}
+
+// The destination may be of either type.
+template <int D>
+cudaError_t prepare_evict() {
+  cudaError_t e = cudaFuncSetAttribute(evict_kernel<__nv_bfloat16, D, true>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kEvictSmemRows * 4);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(evict_kernel<float, D, true>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictSmemRows * 4);
+  return e;
 }
 
 }  // namespace
@@ -621,6 +626,7 @@ using kvr::kv4::View;
 struct kvr_kv4 {
   kvr_cache_desc desc;
   View view;
+  kvr::kv4::Device device;
   std::vector<int32_t> len;  // [S][L]
   uint64_t launches = 0;
 };
@@ -751,9 +757,12 @@ kvr_status kvr_kv4_create(const kvr_cache_desc *desc, void *dev_buf, size_t byte
     delete c;
     return fail(KVR_ENOMEM, "host allocation failed");
   }
+  cudaError_t e = kvr::kv4::prepare_attend(v, &c->device);
+  if (e == cudaSuccess)
+    e = v.d == 128 ? kvr::kv4::prepare_evict<128>() : kvr::kv4::prepare_evict<64>();
   // scores, tickets and the error word lie side by side
-  const cudaError_t e = cudaMemsetAsync(b + l.score, 0, l.total - l.score,
-                                        static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess)
+    e = cudaMemsetAsync(b + l.score, 0, l.total - l.score, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) {
     delete c;
     return cuda_fail("kvr_kv4_create", e);
@@ -896,7 +905,7 @@ kvr_status kvr_kv4_attend(kvr_kv4 *c, int lb, int le, int n_q, const int32_t *co
     p.k = call;
     int n = 0;
     const cudaError_t e =
-        kvr::kv4::launch_attend(p, sq, static_cast<cudaStream_t>(stream), &n);
+        kvr::kv4::launch_attend(p, sq, c->device, static_cast<cudaStream_t>(stream), &n);
     c->launches += n;
     return e == cudaSuccess ? KVR_OK : cuda_fail("kvr_kv4_attend", e);
   });

@@ -149,14 +149,25 @@ struct AttendParams {
   float *stats;  // [unit of the call][n_q * G][2], or null: no scores
   float *parts;  // partial results
 };
-cudaError_t launch_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream,
-                          int *launches);
+// What launches need to know of the handle's device, which is the current one when
+// the handle is made.  (Limits of shared memory are raised then too, as they belong
+// to the device.)
+struct Device {
+  int sms;
+  int resident[3];  // CTAs of the kernel for few query rows, by tiles of 8 columns
+};
+cudaError_t prepare_attend(const View &c, Device *dev);
+cudaError_t launch_attend(const AttendParams &p, const Seqs &q, const Device &dev,
+                          cudaStream_t stream, int *launches);
 // kvr_kv4_tile.cu: the same, on 5th-generation tensor cores, where it applies
 // (bf16, d = 128, more than a few query rows a unit), and the scores' sums.
 bool tile_applies(const View &c, int n_q);
 size_t tile_part_floats(const View &c, int nl, int n_q);
-cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream);
-cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, cudaStream_t stream);
+cudaError_t prepare_tile();
+cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, const Device &dev,
+                               cudaStream_t stream);
+cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, const Device &dev,
+                               cudaStream_t stream);
 // Floats of workspace: statistics of every query row, then partial results.
 size_t attend_stat_floats(const View &c, int nl, int n_q);
 size_t attend_part_floats(const View &c, int nl, int n_q);

@@ -979,19 +979,11 @@ long long tiles_of(const View &c, int n_q) {
 }
 
 template <typename T, int D, int TERMS>
-cudaError_t launch_scores(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+cudaError_t launch_scores(const AttendParams &p, const Seqs &q, const Device &dev,
+                          cudaStream_t stream) {
   constexpr int kBytes = ScoreSmem<D, TERMS>::kBytes;
   auto kern = score_kernel<T, D, TERMS>;
-  static int sms = 0;
-  if (!sms) {
-    int dev = 0, n = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (e != cudaSuccess) return e;
-    sms = n;
-  }
+  const int sms = dev.sms;
   const long long units = (long long)p.k.nl * p.k.c.H;
   long long total = 0;
   int most = 1;
@@ -1006,23 +998,40 @@ cudaError_t launch_scores(const AttendParams &p, const Seqs &q, cudaStream_t str
 }
 
 template <typename T, typename O, int D, int NT, int TERMS>
-cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+cudaError_t prepare_as(Device *dev) {
+  using S = Smem<D, NT>;
+  auto kern = attend_kernel<T, O, D, NT, TERMS>;
+  int per = 0;
+  cudaError_t e =
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+  if (e == cudaSuccess)
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, kThreads, S::kBytes);
+  dev->resident[NT - 1] = std::max(1, std::min(kMaxGrid, dev->sms * std::max(1, per)));
+  return e;
+}
+template <typename T, typename O, int D, int TERMS>
+cudaError_t prepare_tiles(Device *dev) {
+  cudaError_t e = prepare_as<T, O, D, 1, TERMS>(dev);
+  if (e == cudaSuccess) e = prepare_as<T, O, D, 2, TERMS>(dev);
+  if (e == cudaSuccess && TERMS == 1) e = prepare_as<T, O, D, TERMS == 1 ? 3 : 2, TERMS>(dev);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(score_kernel<T, D, TERMS>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             ScoreSmem<D, TERMS>::kBytes);
+  return e;
+}
+template <typename T, typename O, int TERMS>
+cudaError_t prepare_io(const View &c, Device *dev) {
+  return c.d == 128 ? prepare_tiles<T, O, 128, TERMS>(dev) : prepare_tiles<T, O, 64, TERMS>(dev);
+}
+
+template <typename T, typename O, int D, int NT, int TERMS>
+cudaError_t launch_as(const AttendParams &p, const Seqs &q, const Device &dev,
+                      cudaStream_t stream) {
   using S = Smem<D, NT>;
   const View &c = p.k.c;
   auto kern = attend_kernel<T, O, D, NT, TERMS>;
-  static int resident = 0;  // CTAs that the device holds at once
-  if (!resident) {
-    int dev = 0, sms = 0, per = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess)
-      e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
-    if (e == cudaSuccess)
-      e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, kThreads, S::kBytes);
-    if (e != cudaSuccess) return e;
-    resident = std::max(1, std::min(kMaxGrid, sms * std::max(1, per)));
-  }
+  const int resident = dev.resident[NT - 1];  // CTAs that the device holds at once
   Plan plan;
   const long long tiles = tiles_of(c, p.n_q), per_seq = (long long)p.k.nl * c.H * tiles;
   if (tiles > INT32_MAX || per_seq > INT32_MAX) return cudaErrorInvalidValue;
@@ -1062,25 +1071,27 @@ cudaError_t launch_as(const AttendParams &p, const Seqs &q, cudaStream_t stream)
   return launch_pdl(kern, dim3((unsigned)grid), dim3(kThreads), S::kBytes, stream, p, q, plan);
 }
 template <typename T, typename O, int D, int TERMS>
-cudaError_t launch_tiles(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+cudaError_t launch_tiles(const AttendParams &p, const Seqs &q, const Device &dev,
+                         cudaStream_t stream) {
   switch (tile_cols(p.k.c, p.n_q)) {
-    case 8: return launch_as<T, O, D, 1, TERMS>(p, q, stream);
-    case 16: return launch_as<T, O, D, 2, TERMS>(p, q, stream);
-    default: return launch_as<T, O, D, TERMS == 1 ? 3 : 2, TERMS>(p, q, stream);
+    case 8: return launch_as<T, O, D, 1, TERMS>(p, q, dev, stream);
+    case 16: return launch_as<T, O, D, 2, TERMS>(p, q, dev, stream);
+    default: return launch_as<T, O, D, TERMS == 1 ? 3 : 2, TERMS>(p, q, dev, stream);
   }
 }
 template <typename T, typename O, int TERMS>
-cudaError_t launch_io(const AttendParams &p, const Seqs &q, cudaStream_t stream, int *launches) {
+cudaError_t launch_io(const AttendParams &p, const Seqs &q, const Device &dev,
+                      cudaStream_t stream, int *launches) {
   const bool wide = p.k.c.d == 128;
-  cudaError_t e = tile_applies(p.k.c, p.n_q) ? launch_tile_attend(p, q, stream)
-                  : wide                     ? launch_tiles<T, O, 128, TERMS>(p, q, stream)
-                                             : launch_tiles<T, O, 64, TERMS>(p, q, stream);
+  cudaError_t e = tile_applies(p.k.c, p.n_q) ? launch_tile_attend(p, q, dev, stream)
+                  : wide                     ? launch_tiles<T, O, 128, TERMS>(p, q, dev, stream)
+                                             : launch_tiles<T, O, 64, TERMS>(p, q, dev, stream);
   *launches = 1;
   if (e != cudaSuccess || !p.stats) return e;
   *launches = 2;
-  if (tile_applies(p.k.c, p.n_q)) return launch_tile_scores(p, q, stream);
-  return wide ? launch_scores<T, 128, TERMS>(p, q, stream)
-              : launch_scores<T, 64, TERMS>(p, q, stream);
+  if (tile_applies(p.k.c, p.n_q)) return launch_tile_scores(p, q, dev, stream);
+  return wide ? launch_scores<T, 128, TERMS>(p, q, dev, stream)
+              : launch_scores<T, 64, TERMS>(p, q, dev, stream);
 }
 
 }  // namespace
@@ -1096,14 +1107,31 @@ size_t attend_part_floats(const View &c, int nl, int n_q) {
   return 2 * std::min<size_t>(kMaxGrid, pieces) * tile_cols(c, n_q) * (c.d + 2);
 }
 
-cudaError_t launch_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream,
-                          int *launches) {
+cudaError_t prepare_attend(const View &c, Device *dev) {
+  *dev = Device{};
+  int id = 0;
+  cudaError_t e = cudaGetDevice(&id);
+  if (e == cudaSuccess)
+    e = cudaDeviceGetAttribute(&dev->sms, cudaDevAttrMultiProcessorCount, id);
+  if (e != cudaSuccess) return e;
+  if (c.io_bf16)
+    e = c.out_bf16 ? prepare_io<__nv_bfloat16, __nv_bfloat16, 1>(c, dev)
+                   : prepare_io<__nv_bfloat16, float, 2>(c, dev);
+  else
+    e = c.out_bf16 ? prepare_io<float, __nv_bfloat16, 2>(c, dev)
+                   : prepare_io<float, float, 2>(c, dev);
+  // (whether the tensor-memory kernels apply depends on a call's tokens: many, here)
+  return e == cudaSuccess && tile_applies(c, 1 << 10) ? prepare_tile() : e;
+}
+
+cudaError_t launch_attend(const AttendParams &p, const Seqs &q, const Device &dev,
+                          cudaStream_t stream, int *launches) {
   const bool ob = p.k.c.out_bf16;
   if (p.k.c.io_bf16)
-    return ob ? launch_io<__nv_bfloat16, __nv_bfloat16, 1>(p, q, stream, launches)
-              : launch_io<__nv_bfloat16, float, 2>(p, q, stream, launches);
-  return ob ? launch_io<float, __nv_bfloat16, 2>(p, q, stream, launches)
-            : launch_io<float, float, 2>(p, q, stream, launches);
+    return ob ? launch_io<__nv_bfloat16, __nv_bfloat16, 1>(p, q, dev, stream, launches)
+              : launch_io<__nv_bfloat16, float, 2>(p, q, dev, stream, launches);
+  return ob ? launch_io<float, __nv_bfloat16, 2>(p, q, dev, stream, launches)
+            : launch_io<float, float, 2>(p, q, dev, stream, launches);
 }
 
 }  // namespace kv4

@@ -1402,23 +1402,31 @@ size_t tile_part_floats(const View &c, int nl, int n_q) {
 }
 
 template <int CH>
-cudaError_t launch_ch(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+cudaError_t prepare_ch() {
+  auto kern = tile_attend_kernel<CH>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+  // (the kernel's split of the registers counts on as many at launch)
+  cudaFuncAttributes attr;
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, kern);
+  if (e == cudaSuccess && attr.numRegs != kRegs) e = cudaErrorInvalidConfiguration;
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(tile_score_kernel<CH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             kScoreSmem);
+  return e;
+}
+cudaError_t prepare_tile() {
+  cudaError_t e = prepare_ch<4>();
+  if (e == cudaSuccess) e = prepare_ch<6>();
+  if (e == cudaSuccess) e = prepare_ch<8>();
+  return e;
+}
+
+template <int CH>
+cudaError_t launch_ch(const AttendParams &p, const Seqs &q, const Device &dev,
+                      cudaStream_t stream) {
   const View &c = p.k.c;
   auto kern = tile_attend_kernel<CH>;
-  static int sms = 0;
-  if (!sms) {
-    int dev = 0, n = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    // (the kernel's split of the registers counts on as many at launch)
-    cudaFuncAttributes attr;
-    if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, kern);
-    if (e == cudaSuccess && attr.numRegs != kRegs) e = cudaErrorInvalidConfiguration;
-    if (e != cudaSuccess) return e;
-    sms = std::min(n, kTileGrid);
-  }
+  const int sms = std::min(dev.sms, kTileGrid);
   TilePlan plan;
   const long long tiles = col_tiles(c, p.n_q), per_seq = (long long)p.k.nl * c.H * tiles;
   if (tiles > INT32_MAX || per_seq > INT32_MAX) return cudaErrorInvalidValue;
@@ -1442,19 +1450,11 @@ cudaError_t launch_ch(const AttendParams &p, const Seqs &q, cudaStream_t stream)
 }
 
 template <int CH>
-cudaError_t launch_score_ch(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+cudaError_t launch_score_ch(const AttendParams &p, const Seqs &q, const Device &dev,
+                            cudaStream_t stream) {
   const View &c = p.k.c;
   auto kern = tile_score_kernel<CH>;
-  static int sms = 0;
-  if (!sms) {
-    int dev = 0, n = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kScoreSmem);
-    if (e != cudaSuccess) return e;
-    sms = n;
-  }
+  const int sms = dev.sms;
   TilePlan plan;
   plan.tiles = 1;
   long long total = 0;
@@ -1470,19 +1470,21 @@ cudaError_t launch_score_ch(const AttendParams &p, const Seqs &q, cudaStream_t s
                     kScoreSmem, stream, p, q, plan);
 }
 
-cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+cudaError_t launch_tile_scores(const AttendParams &p, const Seqs &q, const Device &dev,
+                               cudaStream_t stream) {
   switch (tile_n(p.k.c, p.n_q)) {
-    case 32: return launch_score_ch<4>(p, q, stream);
-    case 48: return launch_score_ch<6>(p, q, stream);
-    default: return launch_score_ch<8>(p, q, stream);
+    case 32: return launch_score_ch<4>(p, q, dev, stream);
+    case 48: return launch_score_ch<6>(p, q, dev, stream);
+    default: return launch_score_ch<8>(p, q, dev, stream);
   }
 }
 
-cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, cudaStream_t stream) {
+cudaError_t launch_tile_attend(const AttendParams &p, const Seqs &q, const Device &dev,
+                               cudaStream_t stream) {
   switch (tile_n(p.k.c, p.n_q)) {
-    case 32: return launch_ch<4>(p, q, stream);
-    case 48: return launch_ch<6>(p, q, stream);
-    default: return launch_ch<8>(p, q, stream);
+    case 32: return launch_ch<4>(p, q, dev, stream);
+    case 48: return launch_ch<6>(p, q, dev, stream);
+    default: return launch_ch<8>(p, q, dev, stream);
   }
 }
 
