@@ -570,10 +570,10 @@ kvr_status kvr_kv4_read(kvr_kv4 *cache, int layer_begin, int layer_end,
  * row's score grows by the sum over the tokens that see it of the mean over
  * the G heads of its probability (accumulated attention, Sec. 2.1).
  * workspace: device, 16-byte aligned, caller-owned, at least
- * kvr_kv4_attend_workspace_bytes(...) bytes (KVR_ENOMEM otherwise), which
- * depends on the descriptor and the arguments alone; nothing in it is kept
- * between calls.  A normaliser that is not finite sets the device error
- * word. */
+ * kvr_kv4_attend_workspace_bytes(...) bytes (KVR_ENOMEM where a call needs
+ * more), which depends on the descriptor and the arguments alone and serves
+ * every call of n_q tokens or fewer; nothing in it is kept between calls.  A
+ * normaliser that is not finite sets the device error word. */
 size_t kvr_kv4_attend_workspace_bytes(const kvr_kv4 *cache, int layer_begin,
                                       int layer_end, int n_q);
 kvr_status kvr_kv4_attend(kvr_kv4 *cache, int layer_begin, int layer_end,

@@ -710,6 +710,12 @@ kvr_status check_call(const kvr_kv4 *c, int lb, int le, int tokens, const int32_
   return KVR_OK;
 }
 
+// Of a workspace for statistics of n_q tokens and so many floats of partial results.
+size_t bytes_of(const kvr_kv4 *c, int nl, int n_q, size_t parts) {
+  return std::max<size_t>(16, (kvr::kv4::attend_stat_floats(c->view, nl, n_q) + parts) *
+                                  sizeof(float));
+}
+
 }  // namespace
 
 extern "C" {
@@ -878,9 +884,12 @@ kvr_status kvr_kv4_read(kvr_kv4 *c, int lb, int le, int n_rows, const int32_t *c
 
 size_t kvr_kv4_attend_workspace_bytes(const kvr_kv4 *c, int lb, int le, int n_q) {
   if (!c || lb < 0 || le > c->desc.n_layers || lb >= le || n_q < 1 || n_q > (1 << 24)) return 0;
-  return std::max<size_t>(16, (kvr::kv4::attend_stat_floats(c->view, le - lb, n_q) +
-                               kvr::kv4::attend_part_floats(c->view, le - lb, n_q)) *
-                                  sizeof(float));
+  // Partial results depend on how query rows are tiled, so that fewer tokens may need
+  // more of them; there are none above kMaxTiles tiles, of 64 rows at most.
+  size_t parts = 0;
+  for (int n = std::min(n_q, 64 * kvr::kv4::kMaxTiles); n > 0; --n)
+    parts = std::max(parts, kvr::kv4::attend_part_floats(c->view, le - lb, n));
+  return bytes_of(c, le - lb, n_q, parts);
 }
 
 kvr_status kvr_kv4_attend(kvr_kv4 *c, int lb, int le, int n_q, const int32_t *counts,
@@ -891,7 +900,8 @@ kvr_status kvr_kv4_attend(kvr_kv4 *c, int lb, int le, int n_q, const int32_t *co
   if (!q || !out || !workspace) return fail(KVR_EINVAL, "null q, out or workspace");
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace))
     return fail(KVR_EINVAL, "q, out and workspace must be 16-byte aligned");
-  const size_t need = kvr_kv4_attend_workspace_bytes(c, lb, le, n_q);
+  const size_t need = bytes_of(c, le - lb, n_q,
+                               kvr::kv4::attend_part_floats(c->view, le - lb, n_q));
   if (workspace_bytes < need)
     return fail(KVR_ENOMEM, "workspace of %zu bytes < required %zu", workspace_bytes, need);
   kvr::kv4::AttendParams p{};

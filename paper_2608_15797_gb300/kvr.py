@@ -963,10 +963,7 @@ class Kv4Cache:
     def attend_workspace(self, n_q, layers=None):
         """A workspace for attend() of up to n_q tokens over these layers."""
         lb, le = layers or self._all
-        # Partial results depend on how the query rows are tiled, and are kept
-        # for up to 1,024 of them a unit; the rest grows with the tokens.
-        n = max(int(lib.kvr_kv4_attend_workspace_bytes(self.handle, lb, le, i))
-                for i in {*range(1, min(n_q, 1024) + 1), n_q})
+        n = int(lib.kvr_kv4_attend_workspace_bytes(self.handle, lb, le, n_q))
         return torch.empty(n, dtype=torch.uint8, device=self.buf.device)
 
     def attend(self, q, out=None, counts=None, layers=None, scores=False,
