@@ -146,9 +146,9 @@ __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint
                                        uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d));
 }
-// True for one lane of a whole warp.  (The tensor cores' instructions take their
-// operands from uniform registers; under lane == 0 eight products took the issuer
-// some 1,000 cycles.)
+// True for one lane of a whole warp, the same one every time.  (The tensor cores'
+// instructions take their operands from uniform registers; under lane == 0 eight
+// products took the issuer some 1,000 cycles.)
 __device__ __forceinline__ bool elect_one() {
   uint32_t y;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}"
@@ -381,7 +381,10 @@ __global__ void __launch_bounds__(kThr, 1)
         ++runs;
       } while (ok && walk.next(run));
       if (!ok) give_up();
-      if (lane == 0) {  // every product is done before tensor memory is freed
+      __syncwarp();
+      // Every product is done before tensor memory is freed.  (A commit covers what its
+      // own lane issued: the same one is elected every time.)
+      if (elect_one()) {
         volatile int never = 0;
         tc_commit(smem_u32(&S.drain));
         mbar_wait(smem_u32(&S.drain), 0, &never);
@@ -1107,7 +1110,8 @@ __global__ void __launch_bounds__(kScoreThr, 1)
       }
     } while (ok && walk.next(run));
     if (!ok) give_up();
-    if (lane == 0) {  // every product is done before tensor memory is freed
+    __syncwarp();
+    if (elect_one()) {  // every product is done before tensor memory is freed
       volatile int never = 0;
       tc_commit(smem_u32(&S.drain));
       mbar_wait(smem_u32(&S.drain), 0, &never);
