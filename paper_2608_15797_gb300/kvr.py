@@ -847,21 +847,28 @@ for _name, (_res, _args) in {
     _f.argtypes = _args
 
 
-def _scratch(nbytes, device, stream):
-    """Device scratch for one call on `stream`: the allocator is told where a
-    stream other than the current one uses it."""
-    t = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
-    if stream is not None:
-        s = stream if isinstance(stream, torch.cuda.Stream) else \
-            torch.cuda.ExternalStream(int(stream)) if int(stream) else \
+def _empty(shape, dtype, device, stream):
+    """Device memory that a call on `stream` writes, from that stream's own pool:
+    what another stream gave back it may still be working on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else \
             torch.cuda.default_stream()
-        t.record_stream(s)
-    return t
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _scratch(nbytes, device, stream):
+    """Device scratch for one call on `stream`."""
+    return _empty(max(nbytes, 16), torch.uint8, device, stream)
 
 
 class Kv4Cache:
     """A full-context cache held in 4 bits (kvr_kv4_*; the format stands in
-    include/kvr.h): owner of the handle and of the torch buffer it lives in."""
+    include/kvr.h): owner of the handle and of the torch buffer it lives in.
+    What a call allocates, outputs that it was not given among them, belongs to
+    the call's stream, as tensors do that are made under torch.cuda.stream."""
 
     def __init__(self, n_seq, n_layers, n_kv_heads, group, head_dim, capacity,
                  dtype="bf16", out_dtype="bf16", softmax_scale=0.0,
@@ -881,7 +888,7 @@ class Kv4Cache:
         if self.nbytes == 0:
             raise KvrError(KVR_EINVAL, "Kv4Cache", "invalid descriptor")
         if buf is None:
-            buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+            buf = _empty(self.nbytes, torch.uint8, device, stream)
         elif buf.numel() < self.nbytes or buf.dtype != torch.uint8:
             raise ValueError("buf must be uint8 with at least "
                              f"{self.nbytes} bytes")
@@ -952,8 +959,8 @@ class Kv4Cache:
         lb, le = layers or self._all
         counts = self._counts(counts)
         shape = (self.S, le - lb, self.H, n, self.d)
-        k = torch.empty(shape, dtype=self._io, device=self.buf.device)
-        v = torch.empty_like(k)
+        k, v = (_empty(shape, self._io, self.buf.device, stream)
+                for _ in range(2))
         _check(lib.kvr_kv4_read(self.handle, lb, le, n,
                                 None if counts is None else counts.ctypes.data,
                                 k.data_ptr(), v.data_ptr(), _stream(stream)),
@@ -976,7 +983,7 @@ class Kv4Cache:
         qp = self._rows(q, shape, "q")
         counts = self._counts(counts)
         if out is None:
-            out = torch.empty(shape, dtype=self._out, device=q.device)
+            out = _empty(shape, self._out, q.device, stream)
         elif out.shape != shape or out.dtype is not self._out or \
                 not out.is_contiguous():
             raise ValueError(f"out must be contiguous {self.out_dtype} "
@@ -1072,7 +1079,8 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
     """Accept or reject drafted tokens (kvr_verify_drafts): target logits
     [S][T + 1][V], draft logits [S][T][V], tokens int32 and u fp32 [S][T], race
     fp32 [S][V] (exponential, > 0), n_draft int32 [S] or None; temperature > 0
-    (0 is refused).  Returns (accepted [S], tokens [S][T + 1]) on the device."""
+    (0 is refused).  Returns (accepted [S], tokens [S][T + 1]) on the device;
+    where they are not given they belong to the call's stream."""
     S, n, V = target.shape
     T = n - 1
     if draft.shape != (S, T, V) or draft.dtype is not target.dtype or \
@@ -1093,9 +1101,9 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
             raise ValueError(f"{name} must be contiguous {dt} {list(shape)}")
     dev = target.device
     if accepted is None:
-        accepted = torch.empty(S, dtype=torch.int32, device=dev)
+        accepted = _empty(S, torch.int32, dev, stream)
     if out_tokens is None:
-        out_tokens = torch.empty((S, n), dtype=torch.int32, device=dev)
+        out_tokens = _empty((S, n), torch.int32, dev, stream)
     d = kvr_verify_desc(S, T, V, temperature, _LOGITS[target.dtype])
     if workspace is None:
         workspace = _scratch(int(lib.kvr_verify_workspace_bytes(
