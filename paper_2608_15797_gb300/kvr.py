@@ -859,6 +859,23 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _on_device(x, what, device=None):
+    """The GPU that x lies on; a ValueError where that is none, or not `device`:
+    an address of another memory must not reach a kernel."""
+    at = x.get_device()
+    if at < 0 or device is not None and at != device:
+        raise ValueError(f"{what} must lie on the GPU"
+                         + ("" if device is None else f" cuda:{device}")
+                         + f", not on {x.device}")
+    return at
+
+
+def _given_workspace(x, device):
+    _on_device(x, "workspace", device)
+    if not x.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+
+
 def _scratch(nbytes, device, stream):
     """Device scratch for one call on `stream`."""
     return _empty(max(nbytes, 16), torch.uint8, device, stream)
@@ -893,6 +910,7 @@ class Kv4Cache:
             raise ValueError("buf must be uint8 with at least "
                              f"{self.nbytes} bytes")
         self.buf = buf
+        self._device = _on_device(buf, "buf")
         h = _P()
         _check(lib.kvr_kv4_create(ctypes.byref(self.desc), _ptr(buf),
                                   self.nbytes, _stream(stream),
@@ -906,11 +924,13 @@ class Kv4Cache:
             self.handle = None
 
     def _rows(self, x, shape, what):
-        """The address of x, a dense tensor of the cache's element type."""
+        """The address of x, a dense tensor of the cache's element type on the
+        cache's device."""
         if x.shape != shape or x.dtype is not self._io or \
                 not x.is_contiguous():
             raise ValueError(f"{what} must be contiguous {self.dtype} "
                              f"{list(shape)}, not {x.dtype} {list(x.shape)}")
+        _on_device(x, what, self._device)
         return x.data_ptr()
 
     def _counts(self, x, what="counts"):
@@ -988,18 +1008,25 @@ class Kv4Cache:
                 not out.is_contiguous():
             raise ValueError(f"out must be contiguous {self.out_dtype} "
                              f"{list(shape)}")
+        else:
+            _on_device(out, "out", self._device)
         if workspace is None:
             workspace = _scratch(int(lib.kvr_kv4_attend_workspace_bytes(
                 self.handle, lb, le, shape[2])), q.device, stream)
+        else:
+            _given_workspace(workspace, self._device)
         _check(lib.kvr_kv4_attend(
             self.handle, lb, le, shape[2],
             None if counts is None else counts.ctypes.data, qp,
             out.data_ptr(), 1 if scores else 0, workspace.data_ptr(),
-            workspace.numel(), _stream(stream)), "kvr_kv4_attend")
+            workspace.nbytes, _stream(stream)), "kvr_kv4_attend")
         return out
 
     def evict_into(self, cache: Cache, budget, window, stream=None):
         """Cut every sequence into an evicted cache (kvr_kv4_evict)."""
+        if not isinstance(cache, Cache):
+            raise ValueError(f"the destination must be a Cache, not {cache!r}")
+        _on_device(cache.buf, "the destination", self._device)
         _check(lib.kvr_kv4_evict(self.handle, cache.handle, budget, window,
                                  _stream(stream)), "kvr_kv4_evict")
 
@@ -1087,18 +1114,24 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
             target.dtype not in _LOGITS:
         raise ValueError(f"target and draft must be bf16 or f32 {[S, n, V]} "
                          f"and {[S, T, V]}")
+    device = _on_device(target, "target")
     ts = _logit_rows(target, "target")
     ds = _logit_rows(draft, "draft") if T else V
     for x, name, shape, dt in (
+            (draft, "draft", (S, T, V), target.dtype),
             (tokens, "tokens", (S, T), torch.int32),
             (u, "u", (S, T), torch.float32),
             (race, "race", (S, V), torch.float32),
             (n_draft, "n_draft", (S,), torch.int32),
             (accepted, "accepted", (S,), torch.int32),
             (out_tokens, "out_tokens", (S, n), torch.int32)):
-        if x is not None and (x.shape != shape or x.dtype is not dt or
-                              not x.is_contiguous()):
+        if x is None:
+            continue
+        if x.shape != shape or x.dtype is not dt or \
+                not (x is draft or x.is_contiguous()):
             raise ValueError(f"{name} must be contiguous {dt} {list(shape)}")
+        if T or x.numel():  # (without drafts theirs are empty)
+            _on_device(x, name, device)
     dev = target.device
     if accepted is None:
         accepted = _empty(S, torch.int32, dev, stream)
@@ -1108,10 +1141,12 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
     if workspace is None:
         workspace = _scratch(int(lib.kvr_verify_workspace_bytes(
             ctypes.byref(d))), dev, stream)
+    else:
+        _given_workspace(workspace, device)
     _check(lib.kvr_verify_drafts(
         ctypes.byref(d), target.data_ptr(), ts, draft.data_ptr(), ds,
         tokens.data_ptr(), u.data_ptr(), race.data_ptr(),
         None if n_draft is None else n_draft.data_ptr(), accepted.data_ptr(),
-        out_tokens.data_ptr(), workspace.data_ptr(), workspace.numel(),
+        out_tokens.data_ptr(), workspace.data_ptr(), workspace.nbytes,
         _stream(stream)), "kvr_verify_drafts")
     return accepted, out_tokens
