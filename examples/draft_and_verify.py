@@ -8,11 +8,13 @@ decodes from an evicted Cache of budget + window rows a KV head.  A round:
 
 1. the drafter proposes `draft` tokens, a Cache.step a layer and token;
 2. the pending token and the drafts enter the full cache (append) and attend
-   over it at once (attend, which also accumulates the rows' scores);
+   over it at once (attend, which leaves the rows' scores alone: some of these
+   tokens may never have been);
 3. verify_drafts accepts a prefix of the drafts and draws the next token, so
    that what is emitted is distributed as the model's own samples;
-4. truncate drops the rejected rows, and evict_into cuts the drafter's cache
-   from the full one by the accumulated scores.
+4. truncate drops the rejected rows, the tokens that stay attend once more and
+   accumulate the rows' scores, and evict_into cuts the drafter's cache from the
+   full one by them.
 """
 from __future__ import annotations
 
@@ -60,13 +62,22 @@ class Decoder:
             h = h + o.float().view(S, n, -1) @ self.wo[l]
         return torch.nn.functional.rms_norm(h, h.shape[-1:]) @ self.head
 
-    def full(self, cache, tokens, counts=None, scores=True):
-        """Append the tokens to a Kv4Cache and run them over it."""
+    def full(self, cache, tokens, counts=None, scores=True, queries=None):
+        """Append the tokens to a Kv4Cache and run them over it.  queries: a
+        list that gets each layer's."""
         def attend(l, q, k, v):
+            if queries is not None:
+                queries.append(q)
             cache.append(k, v, counts=counts, layers=(l, l + 1))
             return cache.attend(q, counts=counts, layers=(l, l + 1),
                                 scores=scores)
         return self.forward(tokens, attend)
+
+    def weigh(self, cache, queries, counts):
+        """Accumulate the scores that the newest counts[s] tokens give the rows,
+        which are the first ones of their call."""
+        for l, q in enumerate(queries):
+            cache.attend(q, counts=counts, layers=(l, l + 1), scores=True)
 
     def draft(self, cache, tokens, budget, window):
         """One token a sequence over an evicted Cache -> logits [S][V]."""
@@ -120,7 +131,9 @@ def generate(m, prompts, new, draft=4, budget=64, window=16, temperature=1.0,
             tokens.append(x)
         tokens = torch.stack(tokens, 1).int()
         before = full.lengths()[:, 0]
-        target = m.full(full, torch.cat((pending[:, None].int(), tokens), 1))
+        queries = []
+        target = m.full(full, torch.cat((pending[:, None].int(), tokens), 1),
+                        scores=False, queries=queries)
         u = torch.rand((S, draft), generator=g, device="cuda")
         race = torch.empty((S, m.V), device="cuda").exponential_(generator=g)
         accepted, emitted = kvr.verify_drafts(
@@ -129,8 +142,9 @@ def generate(m, prompts, new, draft=4, budget=64, window=16, temperature=1.0,
         accepted, emitted = accepted.tolist(), emitted.tolist()
         # Sequences that have enough stay where they are.
         done = [len(o) >= new for o in out]
-        full.truncate([int(n) + (0 if d else 1 + a)
-                       for n, d, a in zip(before, done, accepted)])
+        kept_rows = [0 if d else 1 + a for d, a in zip(done, accepted)]
+        full.truncate([int(n) + k for n, k in zip(before, kept_rows)])
+        m.weigh(full, queries, kept_rows)
         nxt = pending.tolist()
         for s in range(S):
             if not done[s]:

@@ -568,7 +568,10 @@ kvr_status kvr_kv4_read(kvr_kv4 *cache, int layer_begin, int layer_end,
  * rows up to its own; one that sees none, and the tokens from counts[s] on,
  * get zeros.  Softmax statistics and sums are fp32.  With add_scores != 0 each
  * row's score grows by the sum over the tokens that see it of the mean over
- * the G heads of its probability (accumulated attention, Sec. 2.1).
+ * the G heads of its probability (accumulated attention, Sec. 2.1).  Scores
+ * have no way back: drafted tokens attend without, and once the rejected ones
+ * are truncated the call is repeated with add_scores for those that stay
+ * (counts), whose queries come first in q as before.
  * workspace: device, 16-byte aligned, caller-owned, at least
  * kvr_kv4_attend_workspace_bytes(...) bytes (KVR_ENOMEM where a call needs
  * more), which depends on the descriptor and the arguments alone and serves
