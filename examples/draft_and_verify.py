@@ -109,11 +109,25 @@ def prefill(m, full, prompts):
     return torch.tensor([p[-1] for p in prompts], device="cuda")
 
 
+def check_sizes(new, draft, budget, window, temperature):
+    if new < 1:
+        raise ValueError(f"new must be 1 or more, not {new}")
+    if not 1 <= draft <= 64:
+        raise ValueError(f"draft must be 1 to 64, not {draft}")
+    if budget < 0 or window < 0 or budget + window < 1:
+        raise ValueError(f"budget {budget} and window {window} keep no row")
+    if not temperature > 0:
+        raise ValueError(f"temperature must be above 0, not {temperature}")
+
+
 def generate(m, prompts, new, draft=4, budget=64, window=16, temperature=1.0,
              seed=1):
     """At least `new` tokens a prompt.  Returns them, and the share of drafted
     tokens that were accepted."""
+    check_sizes(new, draft, budget, window, temperature)
     S = len(prompts)
+    if not S or not all(prompts):
+        raise ValueError("every prompt needs a token")
     g = torch.Generator("cuda").manual_seed(seed)
     most = max(len(p) for p in prompts) + new + 2 * draft + 2
     full, small = caches(m, S, most, budget, window)
@@ -179,6 +193,12 @@ def main(argv=None):
     ap.add_argument("--temperature", type=float, default=1.0)
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="bf16")
     a = ap.parse_args(argv)
+    try:
+        check_sizes(a.new, a.draft, a.budget, a.window, a.temperature)
+    except ValueError as e:
+        ap.error(str(e))
+    if a.seqs < 1:
+        ap.error(f"seqs must be 1 or more, not {a.seqs}")
     m = Decoder(d=128 if a.dtype == "bf16" else 64, dtype=a.dtype)
     g = torch.Generator().manual_seed(3)
     prompts = [torch.randint(m.V, (max(1, a.prompt - 37 * s),),
