@@ -928,7 +928,6 @@ void kvr::cache_set_length(kvr_cache *c, int seq, int32_t len, int32_t next_pos)
   std::fill_n(c->len.begin() + at, c->desc.n_layers, len);
   std::fill_n(c->next_pos.begin() + at, c->desc.n_layers, next_pos);
 }
-void kvr::cache_count_launch(kvr_cache *c) { c->launches += 1; }
 
 int kvr::decode_attend_score_ext(kvr_cache *c, int lb, int le, const void *q,
                                  const void *k_new, const void *v_new,

@@ -401,7 +401,6 @@ int decode_attend_score_ext(kvr_cache *c, int lb, int le, const void *q,
 const CacheView &cache_view(const kvr_cache *c);
 bool cache_forked(const kvr_cache *c);
 void cache_set_length(kvr_cache *c, int seq, int32_t len, int32_t next_pos);
-void cache_count_launch(kvr_cache *c);
 // Record a CUDA failure as the thread's last error; returns KVR_ECUDA.
 int report_cuda_error(const char *where, cudaError_t e);
 // Record msg as the thread's last error; returns st.

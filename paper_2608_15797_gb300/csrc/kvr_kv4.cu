@@ -373,7 +373,6 @@ __device__ __forceinline__ uint32_t score_rank(float x) {
 // cut to 512 + 128: 66 us, of which the bytes need 30.
 constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
-constexpr int kEvictHists = 1;  // histograms, one for every kEvictHists-th warp
 constexpr int kEvictBins = 2048;
 constexpr int kEvictSmemRows = 24576;
 
@@ -382,7 +381,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2)
     evict_kernel(const __grid_constant__ Call k, const __grid_constant__ Seqs q,
                  const __grid_constant__ CacheView dst, int budget, int window) {
   extern __shared__ uint32_t s_rank[];
-  __shared__ unsigned s_hist[kEvictHists][kEvictBins];
+  __shared__ unsigned s_hist[kEvictBins];
   __shared__ int s_count[kEvictWarps], s_ties[kEvictWarps];
   __shared__ unsigned s_digit, s_need;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -416,11 +415,10 @@ __global__ void __launch_bounds__(kEvictThreads, 2)
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
       const uint32_t digits = pass == 2 ? 1023u : 2047u;
-      for (int i = tid; i < kEvictHists * kEvictBins; i += kEvictThreads) (&s_hist[0][0])[i] = 0;
+      for (int i = tid; i < kEvictBins; i += kEvictThreads) s_hist[i] = 0;
       __syncthreads();
-      unsigned *hist = s_hist[warp % kEvictHists];
       auto count = [&](uint32_t x) {
-        if ((x & mask) == least && x) atomicAdd(&hist[(x >> shift) & digits], 1u);
+        if ((x & mask) == least && x) atomicAdd(&s_hist[(x >> shift) & digits], 1u);
       };
       if (IN_SMEM) {
 #pragma unroll 4
@@ -438,9 +436,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2)
       unsigned d[kPer], sum = 0;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
-        d[e] = 0;
-#pragma unroll
-        for (int z = 0; z < kEvictHists; ++z) d[e] += s_hist[z][kEvictBins - 1 - kPer * tid - e];
+        d[e] = s_hist[kEvictBins - 1 - kPer * tid - e];
         sum += d[e];
       }
       unsigned above = sum;

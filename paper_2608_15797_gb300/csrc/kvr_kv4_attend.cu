@@ -99,43 +99,9 @@ struct Smem {
   static constexpr int kBytes = kTable + kCols * 16;
 };
 
-// 16-bit pairs of codes: field f (0..3) of a word, f + 4 in the high half.
-//  kRough: c 2^-24 (f even) or c 2^-20 (f odd): the fewest instructions, but the
-//    tensor core aligns products by their operands' exponents, a subnormal
-//    counting as 2^-14, and cuts below 2^-24 of the largest; a leading bit at
-//    2^-21 costs up to seven bits of that.  Enough for logits of bf16 outputs.
-//  kEven: c 2^-20; as exact as normal numbers.
-//  kCentred: c - 8.
-enum Codes { kRough, kEven, kCentred };
-template <Codes M>
-__device__ __forceinline__ void fields(uint32_t x, uint32_t (&f)[4]) {
-  if (M == kCentred) {
-    const __half2 off = __float2half2_rn(1032.f);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t y = ((x >> (4 * i)) & 0x000F000Fu) | 0x64006400u;  // 1024 + c
-      const __half2 z = __hsub2(*reinterpret_cast<__half2 *>(&y), off);
-      f[i] = *reinterpret_cast<const uint32_t *>(&z);
-    }
-  } else if (M == kRough) {
-    const uint32_t y = x >> 8;
-    f[0] = x & 0x000F000Fu;
-    f[1] = x & 0x00F000F0u;
-    f[2] = y & 0x000F000Fu;
-    f[3] = y & 0x00F000F0u;
-  } else {
-    f[0] = (x << 4) & 0x00F000F0u;
-    f[1] = x & 0x00F000F0u;
-    f[2] = (x >> 4) & 0x00F000F0u;
-    f[3] = (x >> 8) & 0x00F000F0u;
-  }
-}
+// The forms of K and V.
 __host__ __device__ constexpr Codes k_codes(int terms) { return terms == 2 ? kCentred : kRough; }
 __host__ __device__ constexpr Codes v_codes(int terms) { return terms == 2 ? kCentred : kEven; }
-// What field f of 1 stands for, inverted.
-__host__ __device__ constexpr float field_unit(Codes m) {
-  return m == kCentred ? 1.f : m == kEven ? 0x1p20f : 0x1p24f;
-}
 
 template <int W>
 __device__ __forceinline__ void lds_words(uint32_t at, uint32_t (&x)[W]) {

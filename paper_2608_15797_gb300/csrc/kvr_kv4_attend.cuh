@@ -1,7 +1,9 @@
-// kvr_kv4_attend.cuh -- what the kernels of the 4-bit cache's attention share: how
-// a column (a token's query head) is addressed, and how its partial results are
-// joined and written.
+// kvr_kv4_attend.cuh -- what the kernels of the 4-bit cache's attention share: codes
+// as 16-bit operands, how a column (a token's query head) is addressed, and how its
+// partial results are joined and written.
 #pragma once
+
+#include <cuda_fp16.h>
 
 #include "kvr_device.cuh"
 #include "kvr_internal.h"
@@ -16,6 +18,42 @@ using namespace ptx;
 
 constexpr float kNone = -1e30f; // a maximum over nothing
 constexpr float kLog2e = 1.4426950408889634f;
+
+// 16-bit pairs of codes: field f (0..3) of a word, f + 4 in the high half.
+//  kRough: c 2^-24 (f even) or c 2^-20 (f odd): the fewest instructions, but the
+//    tensor core aligns products by their operands' exponents, a subnormal
+//    counting as 2^-14, and cuts below 2^-24 of the largest; a leading bit at
+//    2^-21 costs up to seven bits of that.  Enough for logits of bf16 outputs.
+//  kEven: c 2^-20; as exact as normal numbers.
+//  kCentred: c - 8.
+enum Codes { kRough, kEven, kCentred };
+template <Codes M>
+__device__ __forceinline__ void fields(uint32_t x, uint32_t *f) {
+  if (M == kCentred) {
+    const __half2 off = __float2half2_rn(1032.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t y = ((x >> (4 * i)) & 0x000F000Fu) | 0x64006400u;  // 1024 + c
+      const __half2 z = __hsub2(*reinterpret_cast<__half2 *>(&y), off);
+      f[i] = *reinterpret_cast<const uint32_t *>(&z);
+    }
+  } else if (M == kRough) {
+    const uint32_t y = x >> 8;
+    f[0] = x & 0x000F000Fu;
+    f[1] = x & 0x00F000F0u;
+    f[2] = y & 0x000F000Fu;
+    f[3] = y & 0x00F000F0u;
+  } else {
+    f[0] = (x << 4) & 0x00F000F0u;
+    f[1] = x & 0x00F000F0u;
+    f[2] = (x >> 4) & 0x00F000F0u;
+    f[3] = (x >> 8) & 0x00F000F0u;
+  }
+}
+// What field f of 1 stands for, inverted.
+__host__ __device__ constexpr float field_unit(Codes m) {
+  return m == kCentred ? 1.f : m == kEven ? 0x1p20f : 0x1p24f;
+}
 
 __host__ __device__ inline int blocks_of(int len) {
   return len > kBlock ? (len + kBlock - 1) / kBlock : 1;

@@ -72,7 +72,7 @@ constexpr uint32_t kHalf = kTok * 128;      // one 64-element half of an operand
 constexpr uint32_t kCols = 512;             // tensor memory: S (2 x 2 x 64), O (64),
 constexpr uint32_t kColO = 256;             // K (2 x 64)
 constexpr uint32_t kColK = 384;
-constexpr float kUnit = 0x1p24f;            // of K's codes
+constexpr float kUnit = field_unit(kRough);  // of K's codes
 
 // An item's place in the list counts its tiles and, before them, kSwitch more for
 // what a CTA spends on an item whatever its length (its queries, the first
@@ -189,23 +189,6 @@ __device__ __forceinline__ uint32_t half2_bits(__half2 x) {
   return *reinterpret_cast<const uint32_t *>(&x);
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return *reinterpret_cast<__half2 *>(&x); }
-
-// The pairs of nibbles 0 4, 1 5, 2 6, 3 7 of a word as half-precision c 2^-24, the odd
-// ones 2^4 times that.
-__device__ __forceinline__ void rough_fields(uint32_t x, uint32_t *f) {
-  f[0] = x & 0x000F000Fu;
-  f[1] = x & 0x00F000F0u;
-  f[2] = (x >> 8) & 0x000F000Fu;
-  f[3] = (x >> 8) & 0x00F000F0u;
-}
-// As half-precision c 2^-20 all, on which
-// the tensor core keeps its full precision.
-__device__ __forceinline__ void even_fields(uint32_t x, uint32_t *f) {
-  f[0] = (x << 4) & 0x00F000F0u;
-  f[1] = x & 0x00F000F0u;
-  f[2] = (x >> 4) & 0x00F000F0u;
-  f[3] = (x >> 8) & 0x00F000F0u;
-}
 
 // A run of tiles [t0, t1) of one item; np: all it has; at: the item's place.
 struct TileRun {
@@ -554,7 +537,7 @@ __global__ void __launch_bounds__(kThr, 1)
             for (int x = 0; x < 4; ++x) {
               const uint4 &c4 = w[2 * y + (x >> 1)];
               const uint32_t v = j == 0 ? (x & 1 ? c4.y : c4.x) : (x & 1 ? c4.w : c4.z);
-              rough_fields(v, o + 4 * x);
+              fields<kRough>(v, o + 4 * x);
             }
             tmem_st16(tm + ((uint32_t)(dw * 32) << 16) + kColK + b * 64 + j * 32 + y * 16, o);
           }
@@ -1190,7 +1173,7 @@ __global__ void __launch_bounds__(kScoreThr, 1)
             for (int x = 0; x < 8; ++x) {
               const uint4 &c4 = w[x >> 1];
               const uint32_t v = j == 0 ? (x & 1 ? c4.y : c4.x) : (x & 1 ? c4.w : c4.z);
-              even_fields(v, o + 4 * x);
+              fields<kEven>(v, o + 4 * x);
             }
             tmem_st32(tm + ((uint32_t)(dw * 32) << 16) + kScoreColK + b * 64 + j * 32, o);
           }
@@ -1268,7 +1251,7 @@ __global__ void __launch_bounds__(kScoreThr, 1)
         int k2 = 14 - ((int)(__float_as_uint(top) >> 23) - 127);
         k2 = top == 0.f ? 0 : max(-90, min(k2, 100));
         const float up = __uint_as_float((unsigned)(127 + k2) << 23);
-        constexpr float kEvenUnit = 0x1p20f;
+        constexpr float kEvenUnit = field_unit(kEven);
         const float unit_s =
             kEvenUnit * __uint_as_float((unsigned)(127 - k2) << 23) * (c.scale * kLog2e);
 #pragma unroll 2
