@@ -930,7 +930,8 @@ class Kv4Cache:
                 not x.is_contiguous():
             raise ValueError(f"{what} must be contiguous {self.dtype} "
                              f"{list(shape)}, not {x.dtype} {list(x.shape)}")
-        _on_device(x, what, self._device)
+        if x.get_device() != self._device:
+            _on_device(x, what, self._device)  # raises
         return x.data_ptr()
 
     def _counts(self, x, what="counts"):
@@ -1008,8 +1009,8 @@ class Kv4Cache:
                 not out.is_contiguous():
             raise ValueError(f"out must be contiguous {self.out_dtype} "
                              f"{list(shape)}")
-        else:
-            _on_device(out, "out", self._device)
+        elif out.get_device() != self._device:
+            _on_device(out, "out", self._device)  # raises
         if workspace is None:
             workspace = _scratch(int(lib.kvr_kv4_attend_workspace_bytes(
                 self.handle, lb, le, shape[2])), q.device, stream)
@@ -1115,10 +1116,11 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
         raise ValueError(f"target and draft must be bf16 or f32 {[S, n, V]} "
                          f"and {[S, T, V]}")
     device = _on_device(target, "target")
+    if T and draft.get_device() != device:
+        _on_device(draft, "draft", device)  # raises
     ts = _logit_rows(target, "target")
     ds = _logit_rows(draft, "draft") if T else V
     for x, name, shape, dt in (
-            (draft, "draft", (S, T, V), target.dtype),
             (tokens, "tokens", (S, T), torch.int32),
             (u, "u", (S, T), torch.float32),
             (race, "race", (S, V), torch.float32),
@@ -1127,11 +1129,10 @@ def verify_drafts(target, draft, tokens, u, race, n_draft=None,
             (out_tokens, "out_tokens", (S, n), torch.int32)):
         if x is None:
             continue
-        if x.shape != shape or x.dtype is not dt or \
-                not (x is draft or x.is_contiguous()):
+        if x.shape != shape or x.dtype is not dt or not x.is_contiguous():
             raise ValueError(f"{name} must be contiguous {dt} {list(shape)}")
-        if T or x.numel():  # (without drafts theirs are empty)
-            _on_device(x, name, device)
+        if x.get_device() != device and x.numel():  # (no drafts: empty)
+            _on_device(x, name, device)  # raises
     dev = target.device
     if accepted is None:
         accepted = _empty(S, torch.int32, dev, stream)
