@@ -566,12 +566,15 @@ kvr_status kvr_kv4_read(kvr_kv4 *cache, int layer_begin, int layer_end,
  *   q, out dev [S][nl][n_q][H*G][d] (out_dtype for out)
  * Token j < counts[s] sits at position length - counts[s] + j and sees the
  * rows up to its own; one that sees none, and the tokens from counts[s] on,
- * get zeros.  Softmax statistics and sums are fp32.  With add_scores != 0 each
- * row's score grows by the sum over the tokens that see it of the mean over
- * the G heads of its probability (accumulated attention, Sec. 2.1).  Scores
- * have no way back: drafted tokens attend without, and once the rejected ones
- * are truncated the call is repeated with add_scores for those that stay
- * (counts), whose queries come first in q as before.
+ * get zeros.  Softmax statistics and sums are fp32; values are summed before
+ * they are normalised, so |v| times the rows has to stay below 2^112, and |q|
+ * below 2^104.  What q holds for tokens from counts[s] on does not matter.
+ * With add_scores != 0 each row's score grows by the sum over the tokens that
+ * see it of the mean over the G heads of its probability (accumulated
+ * attention, Sec. 2.1).  Scores have no way back: drafted tokens attend
+ * without, and once the rejected ones are truncated the call is repeated with
+ * add_scores for those that stay (counts), whose queries come first in q as
+ * before.
  * workspace: device, 16-byte aligned, caller-owned, at least
  * kvr_kv4_attend_workspace_bytes(...) bytes (KVR_ENOMEM where a call needs
  * more), which depends on the descriptor and the arguments alone and serves

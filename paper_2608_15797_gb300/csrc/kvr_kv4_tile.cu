@@ -14,7 +14,12 @@
 // its codes as they are (half-precision subnormals, scaled back by q and s), in
 // tensor memory; V's is m + s c rounded to half precision once, relative to the
 // token's largest value 2^e, and the power of two that takes this back goes into the
-// token's logits.  P is rounded to half precision once; its sums are fp32.
+// token's logits.  P is rounded to half precision once; its sums are fp32.  Below
+// 2^-14 that rounding is 2^-25 of the reference and no longer of P, so that rows which
+// all weigh 2^-20 of the greatest and less are summed to a few percent of themselves
+// (1e-3 of the output and less).  References 2^4 to 2^8 lower would move that limit as
+// far, but are outgrown more often: 5 tokens of 16 sequences, keys of uneven size, 722
+// and 908 us against 640.  Values below 2^-84 count as zero.
 //
 // One CTA an SM, its warps in roles with bounded waits on mbarriers between them:
 //   8 softmax   two groups of four warps (4 x 32 tokens), each with half of the
@@ -34,9 +39,9 @@
 // Bound by latency: a tile of 48 columns takes about 2,400 cycles, of which the
 // softmax of a group works 1,900 and the tensor core 1,400 (its operands come out of
 // the shared memory that everything else uses too).  Measured (28 layers, 4 KV heads,
-// G = 7): 5 tokens of 16 sequences of 512 to 16,384 rows 614 us (2.0 TB/s of the
-// cache's bytes), of 8 sequences of 8,192 488 us (2.2 TB/s), of 64 of 512 497 us; 32
-// tokens of 2 sequences of 8,191 566 us (372 TFLOP/s).
+// G = 7): 5 tokens of 16 sequences of 512 to 16,384 rows 619 us (2.0 TB/s of the
+// cache's bytes), of 8 sequences of 8,192 493 us (2.1 TB/s), of 64 of 512 498 us; 32
+// tokens of 2 sequences of 8,191 561 us (375 TFLOP/s).
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
