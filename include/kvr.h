@@ -610,6 +610,133 @@ kvr_status kvr_kv4_launch_count(const kvr_kv4 *cache, uint64_t *count);
 /* Synchronising: wait for stream, read and clear the device error word. */
 kvr_status kvr_kv4_sync_status(kvr_kv4 *cache, void *stream);
 
+/* ---- the full context in pages ------------------------------------------- */
+
+/* The paper's engine keeps its caches in pages (App. C, "fresh blocks") and
+ * says no more of it.  Here the full contexts (the helper's, Sec. 3.1) of
+ * sequences that come and go share a pool of pages.  A page holds page_rows
+ * rows of every layer and KV head; a sequence's table lists its pages in order,
+ * and row r of it lies in page table[r / page_rows] at r % page_rows, which is
+ * slot page * page_rows + r % page_rows.  Everything that changes from token to
+ * token, lengths, tables and free pages, lives on the device: no call below
+ * waits, and a captured decode step (plan, append, attend) replays as sequences
+ * grow, come and go.
+ *
+ * Tensors are dense, row-major and 16-byte aligned (KVR_EINVAL otherwise).  What
+ * only the device can see goes to the error word (kvr_paged_sync_status).  Calls
+ * on one handle must be ordered on one stream. */
+typedef struct {
+  int n_seq;           /* S, places for sequences, 1..65535 */
+  int n_layers;        /* L (>= 1) */
+  int n_kv_heads;      /* H (>= 1); L * H <= 65535, L * H * S < 2^31 - 1 */
+  int group;           /* G = query heads per KV head, 1..8 */
+  int head_dim;        /* d: 64 or 128 */
+  int n_pages;         /* pages of the pool (>= 1), n_pages * page_rows < 2^31 */
+  int page_rows;       /* 16, 32, 64 or 128 */
+  int table_pages;     /* pages of a sequence at most (>= 1), times page_rows < 2^31 */
+  kvr_dtype kv_dtype;  /* K, V and q element type */
+  kvr_dtype out_dtype; /* attention output element type */
+  float softmax_scale; /* 0 selects 1/sqrt(d) */
+} kvr_paged_desc;
+
+typedef struct kvr_paged kvr_paged; /* opaque; host metadata only */
+
+/* Device bytes the cache needs (0 for an invalid descriptor). */
+size_t kvr_paged_required_bytes(const kvr_paged_desc *desc);
+
+/* Create a cache over dev_buf (caller-owned, 256-byte aligned, >= the required
+ * bytes): no sequence has rows, every page is free.  The initialisation is
+ * enqueued on stream; rows are not cleared. */
+kvr_status kvr_paged_create(const kvr_paged_desc *desc, void *dev_buf,
+                            size_t bytes, void *stream, kvr_paged **out);
+
+/* Free the handle's host metadata (not the buffer). NULL is a no-op. */
+void kvr_paged_destroy(kvr_paged *cache);
+
+/* The lengths become lens (dev [S] int32): a shorter sequence gives back the
+ * pages behind its new end (length 0: all of them), a longer one takes free
+ * pages, and by at most n_new tokens it grows.  slots (dev [S][n_new] int32, NULL
+ * where n_new is 0): where token t of the growth goes, -1 behind a sequence's
+ * last.  Rows of new tokens hold anything until kvr_paged_append wrote them.
+ * Free pages are a stack, page 0 on top at first.  Pages go back before any are
+ * taken: the first that goes back, in order of sequence and page, comes to lie on
+ * top, the i-th that is taken is the i-th from the top.  Taking tokens back that
+ * the last plan added restores the stack as it was.
+ * All or nothing: where a length is negative or above table_pages * page_rows or
+ * grows by more than n_new (error word: length), or the free pages do not reach
+ * (error word: capacity), nothing changes and every slot is -1. */
+kvr_status kvr_paged_plan(kvr_paged *cache, const int32_t *lens, int n_new,
+                          int32_t *slots, void *stream);
+
+/* The keys and values of n sequences' new tokens go to their slots, in layers
+ * [layer_begin, layer_end):
+ *   k, v  dev [n][nl][n_new][H][d]
+ *   slots dev [n][n_new] int32: a row of kvr_paged_plan's for each of the n
+ * n need not be n_seq: any rows of a plan's slots, in any order, each once.  A row
+ * ends at its first -1.  A page whose last row is written by the call gets its
+ * bounds, the least and the greatest of its page_rows keys in every channel (NaN
+ * where one is NaN), which kvr_paged_attend_pages reads.  Slots that do not follow
+ * one another as a plan's do, or lie outside the pool, are not written where that
+ * shows, and set the error word (length); slots given twice leave either's row. */
+kvr_status kvr_paged_append(kvr_paged *cache, int layer_begin, int layer_end,
+                            int n, int n_new, const int32_t *slots,
+                            const void *k, const void *v, void *stream);
+
+/* Attention (Eq. 1) of one token a sequence, the newest, whose key and value are
+ * appended, over all rows of its sequence:
+ *   q, out dev [S][nl][H*G][d] (out_dtype for out)
+ * A sequence without rows gets zeros.  Softmax statistics and sums are fp32;
+ * values are summed before they are normalised, so |v| times the rows has to stay
+ * below 2^127.  A normaliser that is not finite sets the error word.  Results do
+ * not depend on which pages hold the rows, and equal calls give equal bits.
+ * workspace: device, 16-byte aligned, caller-owned, at least
+ * kvr_paged_attend_workspace_bytes(...) bytes (KVR_ENOMEM otherwise); nothing in
+ * it is kept between calls. */
+size_t kvr_paged_attend_workspace_bytes(const kvr_paged *cache, int layer_begin,
+                                        int layer_end);
+kvr_status kvr_paged_attend(kvr_paged *cache, int layer_begin, int layer_end,
+                            const void *q, void *out, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
+/* The same over some of the pages, chosen for each sequence, layer and KV head:
+ * the window newest, and of the others the budget of the greatest score
+ *   max over the G heads of sum_c q_c * (q_c > 0 ? greatest_c : least_c)
+ * with the page's bounds.  No logit (before the scale) of a page's rows is above
+ * its score.  Equal scores keep the lower page; a NaN ranks above every number.
+ * Scores are those of the bounds and q in 64 bits.  window >= 1, budget >= 0; a
+ * sequence of no more than budget + window pages is read whole.
+ *   pages  dev [S][nl][H][budget + window] int32 or NULL: the chosen pages as
+ *          positions in the table, ascending, then -1
+ * The workspace depends on budget and window too. */
+size_t kvr_paged_attend_pages_workspace_bytes(const kvr_paged *cache,
+                                              int layer_begin, int layer_end,
+                                              int budget, int window);
+kvr_status kvr_paged_attend_pages(kvr_paged *cache, int layer_begin,
+                                  int layer_end, const void *q, int budget,
+                                  int window, void *out, int32_t *pages,
+                                  void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
+/* The state, with no copy: device pointers into the caller's buffer, to be read
+ * stream-ordered and not written.  table [S][row_stride] int32, -1 behind a
+ * sequence's pages; lens [S] int32; n_free int32: free pages.  Any output pointer
+ * may be NULL. */
+kvr_status kvr_paged_tables(const kvr_paged *cache, const int32_t **table,
+                            int64_t *row_stride, const int32_t **lens,
+                            const int32_t **n_free);
+
+/* The pool, likewise: k, v [L][n_pages][H][page_rows][d], bounds
+ * [L][n_pages][H][2][d] (least, greatest; of pages that an append filled), all of
+ * kv_dtype. */
+kvr_status kvr_paged_rows(const kvr_paged *cache, void **k, void **v,
+                          void **bounds);
+
+/* Number of kernels this handle has launched. */
+kvr_status kvr_paged_launch_count(const kvr_paged *cache, uint64_t *count);
+
+/* Synchronising: wait for stream, read and clear the device error word. */
+kvr_status kvr_paged_sync_status(kvr_paged *cache, void *stream);
+
 /* ---- verification of drafted tokens -------------------------------------- */
 
 /* The paper has no counterpart to this call either: a step that a cheap model

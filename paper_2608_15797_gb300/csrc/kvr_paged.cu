@@ -1,0 +1,663 @@
+// kvr_paged.cu -- the paged full-context cache (include/kvr.h, kvr_paged_*): its
+// handle, the plan of pages and slots, and the append.
+#include "kvr_paged.cuh"
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstdio>
+#include <new>
+
+#include "../../include/kvr.h"
+#include "kvr_internal.h"
+
+namespace kvr {
+namespace paged {
+namespace {
+
+// ---- plan -------------------------------------------------------------------
+
+constexpr int kPlan = 1024;          // threads of the plan's CTA, sequences of a span
+constexpr int kPlanWarps = kPlan / 32;
+
+__global__ void __launch_bounds__(256) init_kernel(const __grid_constant__ View c) {
+  kvr::pdl_begin();
+  const long long i0 = (long long)blockIdx.x * 256 + threadIdx.x, step = (long long)gridDim.x * 256;
+  for (long long i = i0; i < (long long)c.S * c.tstride; i += step) c.table[i] = -1;
+  for (long long i = i0; i < c.n_pages; i += step) c.stack[i] = c.n_pages - 1 - (int)i;
+  for (long long i = i0; i < c.S; i += step) c.len[i] = c.from[i] = 0;
+  for (long long i = i0; i <= c.S; i += step) c.tiles[i] = 0;
+  if (i0 == 0) c.free[0] = c.n_pages, c.free[1] = 1;
+}
+
+// What a sequence's new length takes and gives back.
+struct Change {
+  int old, want, have, need;  // rows and pages, before and after
+  bool bad;
+  __device__ int back() const { return max(have - need, 0); }
+  __device__ int take() const { return max(need - have, 0); }
+};
+__device__ __forceinline__ Change change_of(const View &c, const int32_t *want, int s, int n_new) {
+  Change x{};
+  if (s >= c.S) return x;
+  const long long most = (long long)c.tstride << c.psh;
+  x.old = (int)min((long long)max(c.len[s], 0), most);
+  x.want = want[s];
+  x.bad = x.want < 0 || x.want > most || (long long)x.want - x.old > n_new;
+  if (x.bad) x.want = x.old;
+  x.have = (int)(((long long)x.old + c.P - 1) >> c.psh);
+  x.need = (int)(((long long)x.want + c.P - 1) >> c.psh);
+  return x;
+}
+
+// Sum over the CTA of the values before this thread's, and of all of them.
+__device__ long long scan(long long x, long long *s_warp, long long *total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long y = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long z = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) y += z;
+  }
+  __syncthreads();
+  if (lane == 31) s_warp[warp] = y;
+  __syncthreads();
+  long long before = 0, all = 0;
+  for (int w = 0; w < kPlanWarps; ++w) {
+    if (w == warp) before = all;
+    all += s_warp[w];
+  }
+  *total = all;
+  return before + y - x;
+}
+
+// Sequence whose entries hold entry e: the last one that starts at or before it.
+__device__ __forceinline__ int find(const int *start, int e) {
+  int lo = 0;
+#pragma unroll
+  for (int step = kPlan / 2; step > 0; step >>= 1)
+    if (start[lo + step] <= e) lo += step;
+  return lo;
+}
+
+__device__ __forceinline__ int slot_of(const View &c, const int32_t *slots, int s, int t, int from,
+                                       int len) {
+  const int pos = from + t;
+  if (pos >= len) return -1;
+  return (c.table[(long long)s * c.tstride + (pos >> c.psh)] << c.psh) + (pos & (c.P - 1));
+}
+
+// One CTA: S lengths are little work, and what they ask of the stack is a sum over
+// all of them.  Entries of tables (a prompt has hundreds of pages) are dealt out to
+// all threads, each finding its sequence in the sums.
+__global__ void __launch_bounds__(kPlan) plan_kernel(const __grid_constant__ View c,
+                                                     const int32_t *want, int n_new,
+                                                     int32_t *slots) {
+  kvr::pdl_begin();
+  __shared__ long long s_warp[kPlanWarps];
+  __shared__ int s_start[kPlan], s_page[kPlan];
+  const int tid = threadIdx.x;
+  const int spans = (c.S + kPlan - 1) / kPlan;
+  long long back = 0, take = 0;
+  bool bad = false;
+  for (int k = 0; k < spans; ++k) {
+    const Change x = change_of(c, want, k * kPlan + tid, n_new);
+    long long all;
+    scan(x.back(), s_warp, &all);
+    back += all;
+    scan(x.take(), s_warp, &all);
+    take += all;
+    bad |= x.bad;
+  }
+  bad = __syncthreads_or(bad);
+  const long long top = (long long)c.free[0] + back;
+  const bool short_of = take > top || top > c.n_pages;
+  __syncthreads();  // every thread has read the count
+  if (bad || short_of) {
+    if (tid == 0) {
+      atomicOr(c.err, bad ? (unsigned)kvr::ERR_LENGTH : (unsigned)kvr::ERR_CAPACITY);
+      c.free[1] = 0;
+    }
+    if (slots)
+      for (long long i = tid; i < (long long)c.S * n_new; i += kPlan) slots[i] = -1;
+    return;
+  }
+  // pages go back before any are taken
+  for (int pass = 0; pass < 2; ++pass) {
+    long long done = 0;
+    for (int k = 0; k < spans; ++k) {
+      const Change x = change_of(c, want, k * kPlan + tid, n_new);
+      long long all;
+      s_start[tid] = (int)scan(pass ? x.take() : x.back(), s_warp, &all);
+      s_page[tid] = pass ? x.have : x.need;
+      __syncthreads();
+      for (int e = tid; e < all; e += kPlan) {
+        const int i = find(s_start, e);
+        int32_t *entry = c.table + (long long)(k * kPlan + i) * c.tstride + s_page[i] +
+                         (e - s_start[i]);
+        const long long at = top - 1 - (done + e);
+        if (at < 0 || at >= c.n_pages) continue;
+        if (pass)
+          *entry = c.stack[at];
+        else
+          c.stack[at] = *entry, *entry = -1;
+      }
+      done += all;
+      __syncthreads();
+    }
+  }
+  long long before = 0;
+  for (int k = 0; k < spans; ++k) {
+    const int s = k * kPlan + tid;
+    const Change x = change_of(c, want, s, n_new);
+    long long all;
+    const long long at = before + scan((x.want + kTile - 1) / kTile, s_warp, &all);
+    before += all;
+    if (s < c.S) {
+      c.len[s] = x.want;
+      c.from[s] = min(x.old, x.want);
+      c.tiles[s] = (int)at;
+      if (s == c.S - 1) c.tiles[c.S] = (int)before;
+    }
+  }
+  if (tid == 0) c.free[0] = (int)(top - take), c.free[1] = 1;
+  __syncthreads();
+  if (slots)
+    for (long long i = tid; i < (long long)c.S * n_new; i += kPlan) {
+      const int s = (int)(i / n_new), t = (int)(i % n_new);
+      slots[i] = slot_of(c, slots, s, t, c.from[s], c.len[s]);
+    }
+}
+
+// ---- append -----------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b, __nv_bfloat16) {
+  uint32_t r;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b, __nv_bfloat16) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b, float) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+  return __float_as_uint(r);
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b, float) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+  return __float_as_uint(r);
+}
+template <typename T>
+__device__ __forceinline__ void widen(const uint4 &x, uint4 &lo, uint4 &hi) {
+  lo.x = min2(lo.x, x.x, T{}), hi.x = max2(hi.x, x.x, T{});
+  lo.y = min2(lo.y, x.y, T{}), hi.y = max2(hi.y, x.y, T{});
+  lo.z = min2(lo.z, x.z, T{}), hi.z = max2(hi.z, x.z, T{});
+  lo.w = min2(lo.w, x.w, T{}), hi.w = max2(hi.w, x.w, T{});
+}
+
+struct AppendParams {
+  View c;
+  int lb, nl, n, n_new, runs;
+  const int32_t *slots;  // [n][n_new]
+  const uint8_t *k, *v;  // [n][nl][n_new][H][d]
+};
+
+// A warp takes the tokens of a call that fall into one page, for one layer and
+// head.  It alone writes that page's part, so it also knows when the page is full
+// and can say what its keys lie between.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendParams p) {
+  kvr::pdl_begin();
+  constexpr int kRow = D * (int)sizeof(T), kVec = kRow / 16, kPer = 32 / kVec;
+  const View &c = p.c;
+  const int lane = threadIdx.x & 31, vec = lane % kVec, sub = lane / kVec;
+  const long long items = (long long)p.n * p.nl * c.H * p.runs;
+  for (long long it = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); it < items;
+       it += (long long)gridDim.x * 8) {
+    const int h = (int)(it % c.H);
+    const int run = (int)(it / c.H % p.runs);
+    const int lr = (int)(it / ((long long)c.H * p.runs) % p.nl);
+    const int n = (int)(it / ((long long)c.H * p.runs * p.nl));
+    const int32_t *slots = p.slots + (long long)n * p.n_new;
+    const int first = slots[0];
+    if (first < 0) continue;
+    const int r0 = first & (c.P - 1);
+    const int t0 = run == 0 ? 0 : (run << c.psh) - r0;  // the run's first token
+    if (t0 >= p.n_new) continue;
+    const int most = min(p.n_new - t0, c.P - (run == 0 ? r0 : 0));
+    const int slot = slots[t0];
+    if (slot < 0) continue;
+    const int row0 = slot & (c.P - 1), page = slot >> c.psh;
+    // slots follow one another, up to the page's end or the sequence's
+    int count = 0;
+    bool wrong = page >= c.n_pages || (run > 0 && row0 != 0);
+    for (int i = 0; i < most && !wrong; i += 32) {
+      const int x = i + lane < most ? slots[t0 + i + lane] : -1;
+      const unsigned fits = __ballot_sync(0xffffffffu, x == slot + i + lane);
+      wrong = __any_sync(0xffffffffu, x >= 0 && x != slot + i + lane);
+      const int good = fits == 0xffffffffu ? 32 : __ffs(~fits) - 1;
+      count += good;
+      if (good < 32) break;
+    }
+    if (wrong) {
+      if (lane == 0) atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
+      continue;
+    }
+    const long long in = ((((long long)n * p.nl + lr) * p.n_new + t0) * c.H + h) * kRow;
+    const long long in_step = (long long)c.H * kRow;
+    uint8_t *kp = c.K + pool_row(c, p.lb + lr, page, h) * kRow;
+    uint8_t *vp = c.V + pool_row(c, p.lb + lr, page, h) * kRow;
+    const bool full = row0 + count == c.P;
+    uint4 lo, hi;
+    bool any = false;
+    for (int i = sub; i < count; i += kPer) {
+      const uint4 k = __ldg(reinterpret_cast<const uint4 *>(p.k + in + i * in_step) + vec);
+      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p.v + in + i * in_step) + vec);
+      reinterpret_cast<uint4 *>(kp + (long long)(row0 + i) * kRow)[vec] = k;
+      reinterpret_cast<uint4 *>(vp + (long long)(row0 + i) * kRow)[vec] = v;
+      if (!any) lo = hi = k, any = true;
+      widen<T>(k, lo, hi);
+    }
+    if (!full) continue;
+    for (int i = sub; i < row0; i += kPer) {  // rows of earlier calls
+      const uint4 k = reinterpret_cast<const uint4 *>(kp + (long long)i * kRow)[vec];
+      if (!any) lo = hi = k, any = true;
+      widen<T>(k, lo, hi);
+    }
+    // (a page has 16 rows at least: every part of the warp has seen some)
+#pragma unroll
+    for (int o = kVec; o < 32; o <<= 1) {
+      uint4 a, b;
+      a.x = __shfl_xor_sync(0xffffffffu, lo.x, o), b.x = __shfl_xor_sync(0xffffffffu, hi.x, o);
+      a.y = __shfl_xor_sync(0xffffffffu, lo.y, o), b.y = __shfl_xor_sync(0xffffffffu, hi.y, o);
+      a.z = __shfl_xor_sync(0xffffffffu, lo.z, o), b.z = __shfl_xor_sync(0xffffffffu, hi.z, o);
+      a.w = __shfl_xor_sync(0xffffffffu, lo.w, o), b.w = __shfl_xor_sync(0xffffffffu, hi.w, o);
+      widen<T>(a, lo, hi);
+      widen<T>(b, lo, hi);
+    }
+    if (sub == 0) {
+      uint4 *bp = reinterpret_cast<uint4 *>(
+          c.bounds + (((long long)(p.lb + lr) * c.n_pages + page) * c.H + h) * 2 * kRow);
+      bp[vec] = lo;
+      bp[kVec + vec] = hi;
+    }
+  }
+}
+
+template <typename T, int D>
+cudaError_t launch_append(const AppendParams &p, int sms, cudaStream_t st) {
+  const long long items = (long long)p.n * p.nl * p.c.H * p.runs;
+  const long long grid = std::min<long long>((items + 7) / 8, 8ll * sms);
+  return kvr::launch_pdl(append_kernel<T, D>, dim3((unsigned)grid), dim3(256), 0, st, p);
+}
+
+}  // namespace
+}  // namespace paged
+}  // namespace kvr
+
+using kvr::report_error;
+using kvr::paged::View;
+
+struct kvr_paged {
+  kvr_paged_desc desc;
+  View view;
+  int sms = 0;
+  uint64_t launches = 0;
+};
+
+namespace {
+
+constexpr size_t kAlign = 256;
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+template <typename... A>
+kvr_status fail(kvr_status st, const char *fmt, A... a) {
+  char buf[256];
+  snprintf(buf, sizeof buf, fmt, a...);
+  return static_cast<kvr_status>(report_error(st, buf));
+}
+kvr_status fail(kvr_status st, const char *msg) {
+  return static_cast<kvr_status>(report_error(st, msg));
+}
+kvr_status cuda_fail(const char *where, cudaError_t e) {
+  return static_cast<kvr_status>(kvr::report_cuda_error(where, e));
+}
+cudaStream_t as_stream(void *s) { return static_cast<cudaStream_t>(s); }
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+struct Layout {
+  size_t K, V, bounds, table, len, from, tiles, stack, free, ticket, err, total;
+};
+
+constexpr int kMaxCtas = 4096;  // of the attention, on any device
+
+bool layout_of(const kvr_paged_desc *d, Layout *l) {
+  if (!d || d->n_seq < 1 || d->n_seq > 65535 || d->n_layers < 1 || d->n_kv_heads < 1 ||
+      d->group < 1 || d->group > kvr::paged::kHeads ||
+      (d->head_dim != 64 && d->head_dim != 128) || d->n_pages < 1 || d->table_pages < 1 ||
+      (d->page_rows != 16 && d->page_rows != 32 && d->page_rows != 64 && d->page_rows != 128) ||
+      (long long)d->n_pages * d->page_rows > INT_MAX ||
+      (long long)d->table_pages * d->page_rows > INT_MAX ||
+      (long long)d->n_layers * d->n_kv_heads > 65535 ||
+      (long long)d->n_layers * d->n_kv_heads * d->n_seq >= INT_MAX ||
+      (d->kv_dtype != KVR_BF16 && d->kv_dtype != KVR_F32) ||
+      (d->out_dtype != KVR_BF16 && d->out_dtype != KVR_F32) ||
+      !(d->softmax_scale >= 0.f && std::isfinite(d->softmax_scale)))
+    return false;
+  const size_t es = d->kv_dtype == KVR_BF16 ? 2 : 4;
+  const size_t units = (size_t)d->n_layers * d->n_pages * d->n_kv_heads, row = d->head_dim * es;
+  // (65,535 units of 2^31 rows of 512 bytes stay below 2^63)
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes);
+    return at;
+  };
+  l->K = take(units * d->page_rows * row);
+  l->V = take(units * d->page_rows * row);
+  l->bounds = take(units * 2 * row);
+  l->table = take((size_t)d->n_seq * d->table_pages * 4);
+  l->len = take((size_t)d->n_seq * 4);
+  l->from = take((size_t)d->n_seq * 4);
+  l->tiles = take(((size_t)d->n_seq + 1) * 4);
+  l->stack = take((size_t)d->n_pages * 4);
+  l->free = take(2 * 4);
+  l->ticket = take(kMaxCtas * 4);
+  l->err = take(16);
+  l->total = off;
+  return true;
+}
+
+kvr_status check_layers(const kvr_paged *c, int lb, int le) {
+  if (!c) return fail(KVR_EINVAL, "null cache");
+  if (lb < 0 || le > c->desc.n_layers || lb >= le)
+    return fail(KVR_EINVAL, "layer range [%d, %d) outside [0, %d)", lb, le, c->desc.n_layers);
+  return KVR_OK;
+}
+
+bool choice_ok(int budget, int window) {
+  return budget >= 0 && window >= 1 && (long long)budget + window <= (1 << 24);
+}
+
+// Parts of a workspace of either attention; `pages` of a choice, or none.
+struct Work {
+  size_t parts, score, list, rows, tiles, total;
+  int keep;
+};
+Work work_of(const kvr_paged *c, int nl, int budget, int window) {
+  const kvr_paged_desc &d = c->desc;
+  Work w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += (bytes + 15) / 16 * 16;
+    return at;
+  };
+  w.parts = take((size_t)2 * kvr::paged::attend_ctas(c->sms) *
+                 kvr::paged::part_floats(d.head_dim) * sizeof(float));
+  if (window > 0) {
+    const size_t units = (size_t)d.n_seq * nl * d.n_kv_heads;
+    w.keep = (int)std::min<long long>((long long)budget + window, d.table_pages);
+    w.score = take(units * d.table_pages * sizeof(float2));
+    w.list = take(units * w.keep * sizeof(int32_t));
+    w.rows = take((size_t)d.n_seq * sizeof(int32_t));
+    w.tiles = take(((size_t)d.n_seq + 1) * sizeof(int32_t));
+  }
+  w.total = off;
+  return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kvr_paged_required_bytes(const kvr_paged_desc *desc) {
+  Layout l;
+  return layout_of(desc, &l) ? l.total : 0;
+}
+
+kvr_status kvr_paged_create(const kvr_paged_desc *desc, void *dev_buf, size_t bytes,
+                            void *stream, kvr_paged **out) {
+  if (!out) return fail(KVR_EINVAL, "null output handle");
+  *out = nullptr;
+  Layout l;
+  if (!layout_of(desc, &l)) return fail(KVR_EINVAL, "invalid paged cache descriptor");
+  if (!dev_buf) return fail(KVR_EINVAL, "null device buffer");
+  if (reinterpret_cast<uintptr_t>(dev_buf) % kAlign)
+    return fail(KVR_EINVAL, "device buffer not %zu-byte aligned", kAlign);
+  if (bytes < l.total)
+    return fail(KVR_ENOMEM, "buffer of %zu bytes < required %zu", bytes, l.total);
+  kvr_paged *c = new (std::nothrow) kvr_paged();
+  if (!c) return fail(KVR_ENOMEM, "host allocation failed");
+  c->desc = *desc;
+  uint8_t *b = static_cast<uint8_t *>(dev_buf);
+  auto i32 = [&](size_t at) { return reinterpret_cast<int32_t *>(b + at); };
+  View &v = c->view;
+  v.K = b + l.K;
+  v.V = b + l.V;
+  v.bounds = b + l.bounds;
+  v.table = i32(l.table);
+  v.len = i32(l.len);
+  v.from = i32(l.from);
+  v.tiles = i32(l.tiles);
+  v.stack = i32(l.stack);
+  v.free = i32(l.free);
+  v.ticket = reinterpret_cast<unsigned *>(b + l.ticket);
+  v.err = reinterpret_cast<unsigned *>(b + l.err);
+  v.S = desc->n_seq;
+  v.L = desc->n_layers;
+  v.H = desc->n_kv_heads;
+  v.G = desc->group;
+  v.d = desc->head_dim;
+  v.P = desc->page_rows;
+  v.n_pages = desc->n_pages;
+  v.tstride = desc->table_pages;
+  v.psh = 31 - __builtin_clz((unsigned)desc->page_rows);
+  v.scale = desc->softmax_scale > 0.f ? desc->softmax_scale
+                                      : 1.0f / std::sqrt((float)desc->head_dim);
+  v.io_bf16 = desc->kv_dtype == KVR_BF16;
+  v.out_bf16 = desc->out_dtype == KVR_BF16;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess)
+    e = cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = kvr::paged::prepare_attend(v);
+  // tickets and the error word lie side by side
+  if (e == cudaSuccess)
+    e = cudaMemsetAsync(b + l.ticket, 0, l.total - l.ticket, as_stream(stream));
+  if (e == cudaSuccess) {
+    const long long most = std::max<long long>((long long)v.S * v.tstride, v.n_pages);
+    const int grid = (int)std::min<long long>((most + 255) / 256, 4ll * c->sms);
+    e = kvr::launch_pdl(kvr::paged::init_kernel, dim3(grid), dim3(256), 0, as_stream(stream), v);
+  }
+  if (e != cudaSuccess) {
+    delete c;
+    return cuda_fail("kvr_paged_create", e);
+  }
+  c->launches = 1;
+  *out = c;
+  return KVR_OK;
+}
+
+void kvr_paged_destroy(kvr_paged *cache) { delete cache; }
+
+kvr_status kvr_paged_plan(kvr_paged *c, const int32_t *lens, int n_new, int32_t *slots,
+                          void *stream) {
+  if (!c || !lens) return fail(KVR_EINVAL, "null cache or lengths");
+  if (n_new < 0 || n_new > (1 << 24)) return fail(KVR_EINVAL, "%d new tokens", n_new);
+  if ((n_new > 0) != (slots != nullptr))
+    return fail(KVR_EINVAL, "slots go with new tokens: %d of them", n_new);
+  const cudaError_t e =
+      kvr::launch_pdl(kvr::paged::plan_kernel, dim3(1), dim3(kvr::paged::kPlan), 0,
+                      as_stream(stream), c->view, lens, n_new, slots);
+  if (e != cudaSuccess) return cuda_fail("kvr_paged_plan", e);
+  c->launches += 1;
+  return KVR_OK;
+}
+
+kvr_status kvr_paged_append(kvr_paged *c, int lb, int le, int n, int n_new,
+                            const int32_t *slots, const void *k, const void *v, void *stream) {
+  kvr_status st = check_layers(c, lb, le);
+  if (st != KVR_OK) return st;
+  if (n < 1 || n_new < 1 || n_new > (1 << 24))
+    return fail(KVR_EINVAL, "%d sequences of %d tokens", n, n_new);
+  if (!slots || !k || !v) return fail(KVR_EINVAL, "null slots, k or v");
+  if (!aligned16(k) || !aligned16(v))
+    return fail(KVR_EINVAL, "k and v must be 16-byte aligned");
+  kvr::paged::AppendParams p{};
+  p.c = c->view;
+  p.lb = lb;
+  p.nl = le - lb;
+  p.n = n;
+  p.n_new = n_new;
+  // pages that n_new rows in a row can touch
+  p.runs = (n_new + c->view.P - 2) / c->view.P + 1;
+  p.slots = slots;
+  p.k = static_cast<const uint8_t *>(k);
+  p.v = static_cast<const uint8_t *>(v);
+  const cudaStream_t cs = as_stream(stream);
+  cudaError_t e;
+  if (c->view.io_bf16)
+    e = c->view.d == 128 ? kvr::paged::launch_append<__nv_bfloat16, 128>(p, c->sms, cs)
+                         : kvr::paged::launch_append<__nv_bfloat16, 64>(p, c->sms, cs);
+  else
+    e = c->view.d == 128 ? kvr::paged::launch_append<float, 128>(p, c->sms, cs)
+                         : kvr::paged::launch_append<float, 64>(p, c->sms, cs);
+  if (e != cudaSuccess) return cuda_fail("kvr_paged_append", e);
+  c->launches += 1;
+  return KVR_OK;
+}
+
+size_t kvr_paged_attend_workspace_bytes(const kvr_paged *c, int lb, int le) {
+  if (!c || lb < 0 || le > c->desc.n_layers || lb >= le) return 0;
+  return work_of(c, le - lb, 0, 0).total;
+}
+
+size_t kvr_paged_attend_pages_workspace_bytes(const kvr_paged *c, int lb, int le, int budget,
+                                              int window) {
+  if (!c || lb < 0 || le > c->desc.n_layers || lb >= le || !choice_ok(budget, window)) return 0;
+  return work_of(c, le - lb, budget, window).total;
+}
+
+kvr_status kvr_paged_attend(kvr_paged *c, int lb, int le, const void *q, void *out,
+                            void *workspace, size_t workspace_bytes, void *stream) {
+  kvr_status st = check_layers(c, lb, le);
+  if (st != KVR_OK) return st;
+  if (!q || !out || !workspace) return fail(KVR_EINVAL, "null q, out or workspace");
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace))
+    return fail(KVR_EINVAL, "q, out and workspace must be 16-byte aligned");
+  const Work w = work_of(c, le - lb, 0, 0);
+  if (workspace_bytes < w.total)
+    return fail(KVR_ENOMEM, "workspace of %zu bytes < required %zu", workspace_bytes, w.total);
+  const View &v = c->view;
+  kvr::paged::AttendParams p{};
+  p.c = v;
+  p.src = {v.table, v.tstride, 0, v.len, v.tiles};
+  p.lb = lb;
+  p.nl = le - lb;
+  p.q = q;
+  p.out = out;
+  p.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.parts);
+  const cudaError_t e = kvr::paged::launch_attend(p, c->sms, as_stream(stream));
+  if (e != cudaSuccess) return cuda_fail("kvr_paged_attend", e);
+  c->launches += 1;
+  return KVR_OK;
+}
+
+kvr_status kvr_paged_attend_pages(kvr_paged *c, int lb, int le, const void *q, int budget,
+                                  int window, void *out, int32_t *pages, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+  kvr_status st = check_layers(c, lb, le);
+  if (st != KVR_OK) return st;
+  if (!choice_ok(budget, window))
+    return fail(KVR_EINVAL, "bad budget %d / window %d", budget, window);
+  if (!q || !out || !workspace) return fail(KVR_EINVAL, "null q, out or workspace");
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace))
+    return fail(KVR_EINVAL, "q, out and workspace must be 16-byte aligned");
+  const Work w = work_of(c, le - lb, budget, window);
+  if (workspace_bytes < w.total)
+    return fail(KVR_ENOMEM, "workspace of %zu bytes < required %zu", workspace_bytes, w.total);
+  const View &v = c->view;
+  char *ws = static_cast<char *>(workspace);
+  kvr::paged::SelectParams s{};
+  s.c = v;
+  s.lb = lb;
+  s.nl = le - lb;
+  s.q = q;
+  s.budget = budget;
+  s.window = window;
+  s.keep = w.keep;
+  s.score = reinterpret_cast<float2 *>(ws + w.score);
+  s.list = reinterpret_cast<int32_t *>(ws + w.list);
+  s.rows = reinterpret_cast<int32_t *>(ws + w.rows);
+  s.tiles = reinterpret_cast<int32_t *>(ws + w.tiles);
+  s.chosen = pages;
+  int n = 0;
+  cudaError_t e = kvr::paged::launch_select(s, c->sms, as_stream(stream), &n);
+  c->launches += n;
+  if (e != cudaSuccess) return cuda_fail("kvr_paged_attend_pages: choice", e);
+  const long long units = (long long)(le - lb) * v.H;
+  kvr::paged::AttendParams p{};
+  p.c = v;
+  p.src = {s.list, units * w.keep, w.keep, s.rows, s.tiles};
+  p.lb = lb;
+  p.nl = le - lb;
+  p.q = q;
+  p.out = out;
+  p.parts = reinterpret_cast<float *>(ws + w.parts);
+  e = kvr::paged::launch_attend(p, c->sms, as_stream(stream));
+  if (e != cudaSuccess) return cuda_fail("kvr_paged_attend_pages", e);
+  c->launches += 1;
+  return KVR_OK;
+}
+
+kvr_status kvr_paged_tables(const kvr_paged *c, const int32_t **table, int64_t *row_stride,
+                            const int32_t **lens, const int32_t **n_free) {
+  if (!c) return fail(KVR_EINVAL, "null cache");
+  if (table) *table = c->view.table;
+  if (row_stride) *row_stride = c->view.tstride;
+  if (lens) *lens = c->view.len;
+  if (n_free) *n_free = c->view.free;
+  return KVR_OK;
+}
+
+kvr_status kvr_paged_rows(const kvr_paged *c, void **k, void **v, void **bounds) {
+  if (!c) return fail(KVR_EINVAL, "null cache");
+  if (k) *k = c->view.K;
+  if (v) *v = c->view.V;
+  if (bounds) *bounds = c->view.bounds;
+  return KVR_OK;
+}
+
+kvr_status kvr_paged_launch_count(const kvr_paged *c, uint64_t *count) {
+  if (!c || !count) return fail(KVR_EINVAL, "null argument");
+  *count = c->launches;
+  return KVR_OK;
+}
+
+kvr_status kvr_paged_sync_status(kvr_paged *c, void *stream) {
+  if (!c) return fail(KVR_EINVAL, "null cache");
+  // all on the caller's stream, as for the 4-bit cache
+  const cudaStream_t cs = as_stream(stream);
+  unsigned word = 0;
+  cudaError_t e = cudaMemcpyAsync(&word, c->view.err, sizeof word, cudaMemcpyDeviceToHost, cs);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cs);
+  if (e != cudaSuccess) return cuda_fail("kvr_paged_sync_status: read", e);
+  if (!word) return KVR_OK;
+  e = cudaMemsetAsync(c->view.err, 0, sizeof word, cs);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cs);
+  if (e != cudaSuccess) return cuda_fail("kvr_paged_sync_status: clear", e);
+  return fail(KVR_EDEVICE, "device error word 0x%x (%s%s%s)", word,
+              word & kvr::ERR_CAPACITY ? "capacity " : "",
+              word & kvr::ERR_NONFINITE ? "non-finite " : "",
+              word & kvr::ERR_LENGTH ? "length" : "");
+}
+
+}  // extern "C"

@@ -1,0 +1,544 @@
+// kvr_paged_attend.cu -- attention of one new token a sequence over the paged
+// cache (include/kvr.h, kvr_paged_attend): out = softmax(scale q K^T) V, every row of
+// K and V read once.
+//
+// The call's rows are tiles of 16, in order of sequence, layer, head and position;
+// every warp of the grid takes an equal span of them, whatever units (sequence,
+// layer, head) it runs through, so that lengths on the device alone decide who does
+// what.  A lane copies ahead, by cp.async, exactly what it will read itself: no
+// barrier and no wait between warps.  A unit that lies in one warp's span is written
+// out by it; the pieces (greatest logit, sum, weighted values) of one that does not
+// are joined in the CTA in order, and where it goes on in another CTA by the last of
+// its CTAs to arrive, in order again, so that results do not depend on who is last.
+#include "kvr_paged.cuh"
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "kvr_device.cuh"
+#include "kvr_internal.h"
+#include "kvr_ptx.cuh"
+
+namespace kvr {
+namespace paged {
+namespace {
+
+using namespace kvr::ptx;
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 16 bytes to shared memory, zeros where `bytes` is 0 (nothing is read then).
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+template <typename T>
+struct Elems;
+template <>
+struct Elems<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void get(const uint4 &w, float (&x)[4]) {
+    x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y);
+    x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
+  }
+};
+template <>
+struct Elems<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(const uint4 &w, float (&x)[8]) {
+    const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(a[i] << 16);
+      x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+    }
+  }
+};
+
+__device__ __forceinline__ void put4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
+__device__ __forceinline__ void put4(__nv_bfloat16 *p, float4 x) {
+  *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+}
+
+// What a lane copies and reads of a tile: its x-th vector of K and of V.
+template <typename T, int D>
+struct Shape {
+  static constexpr int kRow = D * (int)sizeof(T);  // bytes of a row
+  static constexpr int kVecs = kRow / 16;
+  static constexpr int kPer = kVecs / 2;           // vectors of a lane, K or V
+  static constexpr int kStage = 2 * kTile * kRow;
+  static constexpr int E = Elems<T>::N;
+};
+
+// Plain arithmetic in fp32, for either type.  Logits: four lanes share a row, each a
+// quarter of its channels.  Values: a lane owns E channels.
+template <typename T, int D>
+struct Fma : Shape<T, D> {
+  using S = Shape<T, D>;
+  static constexpr int kWarps = 4, kStages = 3;
+  static constexpr int kRowsAtOnce = 32 / S::kVecs;
+  // of a warp: q fp32 [8][D], probabilities [16][8], the rescaling [8]
+  static constexpr int kOwn = (kHeads * D + kTile * kHeads + kHeads) * 4;
+  float *q, *p, *up;
+  float scale;
+  float m[2], l[2];          // heads 2 j, 2 j + 1
+  float o[kHeads][S::E];
+
+  static __device__ __forceinline__ int k_row(int lane, int x) { return (lane >> 2) + 8 * (x & 1); }
+  static __device__ __forceinline__ int k_vec(int lane, int x) { return (lane & 3) + 4 * (x >> 1); }
+  static __device__ __forceinline__ int v_row(int lane, int x) {
+    return lane / S::kVecs + kRowsAtOnce * x;
+  }
+  static __device__ __forceinline__ int v_vec(int lane, int) { return lane % S::kVecs; }
+
+  __device__ __forceinline__ void init(uint8_t *own, float scale_log2e) {
+    q = reinterpret_cast<float *>(own);
+    p = q + kHeads * D;
+    up = p + kTile * kHeads;
+    scale = scale_log2e;
+  }
+  __device__ __forceinline__ void start(const T *from, int G, int lane) {
+    __syncwarp();
+    for (int i = lane; i < kHeads * D; i += 32)
+      q[i] = i < G * D ? kvr::dev::to_f(from[i]) * scale : 0.f;
+    __syncwarp();
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g)
+#pragma unroll
+      for (int e = 0; e < S::E; ++e) o[g][e] = 0.f;
+  }
+  // One tile; rows from `limit` on do not exist.
+  __device__ __forceinline__ void step(const uint4 *stage, int limit, int lane) {
+    const int j = lane & 3;
+    float x[2][kHeads];
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) x[0][g] = x[1][g] = 0.f;
+#pragma unroll 2
+    for (int i = 0; i < S::kPer / 2; ++i) {
+      float a[S::E], b[S::E];
+      Elems<T>::get(stage[(2 * i) * 32 + lane], a);
+      Elems<T>::get(stage[(2 * i + 1) * 32 + lane], b);
+      const float *qc = q + (j + 4 * i) * S::E;
+#pragma unroll
+      for (int g = 0; g < kHeads; ++g)
+#pragma unroll
+        for (int e = 0; e < S::E; e += 4) {
+          const float4 w = *reinterpret_cast<const float4 *>(qc + g * D + e);
+          x[0][g] = fmaf(a[e], w.x, x[0][g]), x[1][g] = fmaf(b[e], w.x, x[1][g]);
+          x[0][g] = fmaf(a[e + 1], w.y, x[0][g]), x[1][g] = fmaf(b[e + 1], w.y, x[1][g]);
+          x[0][g] = fmaf(a[e + 2], w.z, x[0][g]), x[1][g] = fmaf(b[e + 2], w.z, x[1][g]);
+          x[0][g] = fmaf(a[e + 3], w.w, x[0][g]), x[1][g] = fmaf(b[e + 3], w.w, x[1][g]);
+        }
+    }
+    float mine[2][2];
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float y = x[r][g];
+        y += __shfl_xor_sync(0xffffffffu, y, 1);
+        y += __shfl_xor_sync(0xffffffffu, y, 2);
+        if ((g >> 1) == j) mine[r][g & 1] = (lane >> 2) + 8 * r < limit ? y : -INFINITY;
+      }
+    __syncwarp();  // the last tile's probabilities have been read
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      float t = fmaxf(mine[0][g], mine[1][g]);
+#pragma unroll
+      for (int s = 4; s < 32; s <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, s));
+      const float now = fmaxf(m[g], t), ref = now == -INFINITY ? 0.f : now;
+      const float a = ex2(m[g] - ref);
+      m[g] = now;
+      const float p0 = ex2(mine[0][g] - ref), p1 = ex2(mine[1][g] - ref);
+      l[g] = fmaf(l[g], a, p0 + p1);
+      p[(lane >> 2) * kHeads + 2 * j + g] = p0;
+      p[((lane >> 2) + 8) * kHeads + 2 * j + g] = p1;
+      if (lane < 4) up[2 * j + g] = a;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+      const float a = up[g];
+#pragma unroll
+      for (int e = 0; e < S::E; ++e) o[g][e] *= a;
+    }
+    const uint4 *vs = stage + S::kPer * 32;
+#pragma unroll 4
+    for (int i = 0; i < S::kPer; ++i) {
+      float v[S::E];
+      Elems<T>::get(vs[i * 32 + lane], v);
+      const float4 *pr = reinterpret_cast<const float4 *>(p + v_row(lane, i) * kHeads);
+      const float4 pa = pr[0], pb = pr[1];
+      const float w[kHeads] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
+#pragma unroll
+      for (int g = 0; g < kHeads; ++g)
+#pragma unroll
+        for (int e = 0; e < S::E; ++e) o[g][e] = fmaf(w[g], v[e], o[g][e]);
+    }
+  }
+  // Sums over the lanes; then f(head, channel, four weighted sums, greatest logit,
+  // sum of weights) for every head and channel, once each.
+  template <typename F>
+  __device__ __forceinline__ void finish(int lane, F f) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int s = 4; s < 32; s <<= 1) l[g] += __shfl_xor_sync(0xffffffffu, l[g], s);
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+      const float mg = __shfl_sync(0xffffffffu, m[g & 1], g >> 1);
+      const float lg = __shfl_sync(0xffffffffu, l[g & 1], g >> 1);
+#pragma unroll
+      for (int e = 0; e < S::E; ++e)
+#pragma unroll
+        for (int s = S::kVecs; s < 32; s <<= 1) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], s);
+      if (lane < S::kVecs)
+#pragma unroll
+        for (int e = 0; e < S::E; e += 4)
+          f(g, lane * S::E + e, make_float4(o[g][e], o[g][e + 1], o[g][e + 2], o[g][e + 3]), mg,
+            lg);
+    }
+  }
+};
+
+// A place in the list of tiles.
+struct Place {
+  int s, u, tile, n, rows;  // unit u of the sequence's nl * H; its tiles and rows
+};
+
+// A piece of a unit: tiles [first, first + count) of the n of unit `unit`.
+struct Piece {
+  long long unit;
+  int first, count, n;
+};
+
+template <typename T, int D, typename P, typename O>
+__global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_constant__ AttendParams p) {
+  kvr::pdl_begin();
+  using S = Shape<T, D>;
+  constexpr int kWarps = P::kWarps, kStages = P::kStages, kPart = part_floats(D);
+  static_assert(kStages * S::kStage >= kPart * 4, "a warp's last piece takes its copies' place");
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Piece s_piece[2 * kWarps];
+  __shared__ int s_last[2];
+  const View &c = p.c;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint8_t *ring = smem + warp * (kStages * S::kStage);
+  float *early = reinterpret_cast<float *>(smem + kWarps * kStages * S::kStage) + warp * kPart;
+  uint8_t *own = smem + kWarps * (kStages * S::kStage + kPart * 4) + warp * P::kOwn;
+  const uint32_t ring32 = smem_u32(ring);
+  const int U = p.nl * c.H;  // units of a sequence
+  const long long total = (long long)p.src.tiles[c.S] * U;
+  const long long span = (total + (long long)gridDim.x * kWarps - 1) / ((long long)gridDim.x * kWarps);
+  const long long cta_span = span * kWarps;
+  const long long t0 = min(total, ((long long)blockIdx.x * kWarps + warp) * span);
+  const long long t1 = min(total, t0 + span);
+
+  // sequences without rows: zeros
+  for (int s = blockIdx.x; s < c.S; s += gridDim.x) {
+    if (p.src.tiles[s + 1] != p.src.tiles[s]) continue;
+    uint4 *o = reinterpret_cast<uint4 *>(static_cast<O *>(p.out) + (long long)s * U * c.G * D);
+    for (long long i = threadIdx.x; i < (long long)U * c.G * D * (int)sizeof(O) / 16;
+         i += kWarps * 32)
+      o[i] = make_uint4(0, 0, 0, 0);
+  }
+
+  auto locate = [&](long long t) {
+    // the last sequence that starts at or before t (32 of them asked at a time)
+    const int key = (int)(t / U);
+    int lo = 0, hi = c.S;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+      const unsigned in = __ballot_sync(0xffffffffu, at < hi && p.src.tiles[at] <= key);
+      lo += (__popc(in) - 1) * step;
+      hi = min(hi, lo + step);
+    }
+    Place x;
+    x.s = lo;
+    const int base = p.src.tiles[lo];
+    x.n = p.src.tiles[lo + 1] - base;
+    x.rows = p.src.rows[lo];
+    const long long off = t - (long long)base * U;
+    x.u = (int)(off / x.n);
+    x.tile = (int)(off - (long long)x.u * x.n);
+    return x;
+  };
+  auto page_of = [&](const Place &x) {
+    return p.src.pages[x.s * p.src.seq_stride + x.u * p.src.unit_stride +
+                       ((long long)x.tile * kTile >> c.psh)];
+  };
+  auto advance = [&](Place &x, long long next) {
+    if (++x.tile < x.n) return;
+    if (x.u + 1 < U)
+      x.tile = 0, x.u += 1;
+    else if (next < t1)
+      x = locate(next);
+  };
+
+  Place at{}, ahead{};
+  long long issued = t0;
+  int page = 0;
+  bool bad_page = false;
+  auto issue = [&]() {
+    if (issued < t1) {
+      const uint32_t dst = ring32 + (uint32_t)((issued - t0) % kStages) * S::kStage + lane * 16;
+      const bool there = (unsigned)page < (unsigned)c.n_pages;
+      bad_page |= !there;
+      const int row = ahead.tile * kTile, limit = there ? ahead.rows - row : 0;
+      const int lr = ahead.u / c.H, h = ahead.u - lr * c.H;
+      const long long from =
+          (pool_row(c, p.lb + lr, there ? page : 0, h) + (row & (c.P - 1))) * S::kRow;
+#pragma unroll
+      for (int x = 0; x < S::kPer; ++x) {
+        const int r = P::k_row(lane, x);
+        copy16(dst + x * 512, c.K + from + r * S::kRow + P::k_vec(lane, x) * 16,
+               r < limit ? 16 : 0);
+      }
+#pragma unroll
+      for (int x = 0; x < S::kPer; ++x) {
+        const int r = P::v_row(lane, x);
+        copy16(dst + (S::kPer + x) * 512, c.V + from + r * S::kRow + P::v_vec(lane, x) * 16,
+               r < limit ? 16 : 0);
+      }
+      ++issued;
+      advance(ahead, issued);
+      if (issued < t1) page = page_of(ahead);
+    }
+    copies_end();
+  };
+
+  P work;
+  work.init(own, c.scale * kLog2e);
+  if (lane < 2) s_piece[2 * warp + lane] = Piece{-1, 0, 0, 0};
+  __syncwarp();
+  bool infinite = false;
+  auto out_of = [&](long long unit) {
+    return static_cast<O *>(p.out) + unit * c.G * D;
+  };
+  if (t0 < t1) {
+    at = ahead = locate(t0);
+    page = page_of(ahead);
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) issue();
+    int first = at.tile;
+    work.start(static_cast<const T *>(p.q) + ((long long)at.s * U + at.u) * c.G * D, c.G, lane);
+    for (long long t = t0; t < t1; ++t) {
+      copies_wait<kStages - 2>();
+      issue();  // where tile t - 1 was, which this lane has read
+      work.step(reinterpret_cast<const uint4 *>(ring + (uint32_t)((t - t0) % kStages) * S::kStage),
+                at.rows - at.tile * kTile, lane);
+      const bool last = t + 1 == t1;
+      if (at.tile + 1 < at.n && !last) {
+        ++at.tile;
+        continue;
+      }
+      const long long unit = (long long)at.s * U + at.u;
+      if (first == 0 && at.tile + 1 == at.n) {
+        O *o = out_of(unit);
+        work.finish(lane, [&](int g, int ch, float4 v, float, float s) {
+          if (g >= c.G) return;
+          const float r = 1.f / s;
+          infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
+          put4(o + g * D + ch, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+        });
+      } else {
+        // a warp's first piece beside its copies, its last one in their place
+        if (lane == 0)
+          s_piece[2 * warp + last] = Piece{unit, first, at.tile + 1 - first, at.n};
+        if (last) {
+          copies_wait<0>();
+          __syncwarp();
+        }
+        float *dst = last ? reinterpret_cast<float *>(ring) : early;
+        work.finish(lane, [&](int g, int ch, float4 v, float m, float s) {
+          put4(dst + g * D + ch, v);
+          if (ch == 0) dst[kHeads * D + g] = m, dst[kHeads * D + kHeads + g] = s;
+        });
+      }
+      if (!last) {
+        advance(at, t + 1);
+        first = 0;
+        work.start(static_cast<const T *>(p.q) + ((long long)at.s * U + at.u) * c.G * D, c.G,
+                   lane);
+      }
+    }
+  }
+  copies_wait<0>();
+  __syncthreads();
+
+  // Join the pieces that lie side by side.  Thread x owns 4 channels of a head.
+  auto piece_at = [&](int i) {
+    return reinterpret_cast<const float *>(
+        (i & 1) ? smem + (i >> 1) * (kStages * S::kStage)
+                : smem + kWarps * kStages * S::kStage + (i >> 1) * kPart * 4);
+  };
+  constexpr int kMine = kHeads * D / 4 / (kWarps * 32) > 0 ? kHeads * D / 4 / (kWarps * 32) : 1;
+  const bool busy = (int)threadIdx.x < kHeads * D / 4;
+  if (threadIdx.x < 2) s_last[threadIdx.x] = 0;
+  long long owed[2] = {-1, -1};  // units that go on in other CTAs: before, behind
+  int owed_first[2], owed_n[2];
+  for (int i = 0; i < 2 * kWarps;) {
+    const Piece a = s_piece[i];
+    if (a.unit < 0) {
+      ++i;
+      continue;
+    }
+    int end = i, upto = 0;
+    for (int k = i; k < 2 * kWarps; ++k)
+      if (s_piece[k].unit == a.unit)
+        end = k + 1, upto = s_piece[k].first + s_piece[k].count;
+      else if (s_piece[k].unit >= 0)
+        break;
+    const bool whole = a.first == 0 && upto == a.n;
+    const int which = a.first == 0 ? 1 : 0;
+    float *part = p.parts + (2ll * blockIdx.x + which) * kPart;
+    if (busy)
+#pragma unroll
+      for (int y = 0; y < kMine; ++y) {
+        const int x = threadIdx.x + y * kWarps * 32, g = x / (D / 4);
+        float m = -INFINITY;
+        for (int k = i; k < end; ++k)
+          if (s_piece[k].unit >= 0) m = fmaxf(m, piece_at(k)[kHeads * D + g]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float s = 0.f;
+        for (int k = i; k < end; ++k) {
+          if (s_piece[k].unit < 0) continue;
+          const float *from = piece_at(k);
+          const float a = ex2(from[kHeads * D + g] - ref);
+          const float4 w = reinterpret_cast<const float4 *>(from)[x];
+          v.x = fmaf(w.x, a, v.x), v.y = fmaf(w.y, a, v.y);
+          v.z = fmaf(w.z, a, v.z), v.w = fmaf(w.w, a, v.w);
+          s = fmaf(from[kHeads * D + kHeads + g], a, s);
+        }
+        if (!whole) {
+          put4(part + 4 * x, v);
+          if (x % (D / 4) == 0) part[kHeads * D + g] = m, part[kHeads * D + kHeads + g] = s;
+        } else if (g < c.G) {
+          const float r = 1.f / s;
+          infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
+          put4(out_of(a.unit) + 4 * x, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+        }
+      }
+    if (!whole) {
+      owed[which] = a.unit;
+      owed_first[which] = a.first;
+      owed_n[which] = a.n;
+    }
+    i = end;
+  }
+  if (bad_page && lane == 0) atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
+  if (owed[0] >= 0 || owed[1] >= 0) {
+    // position of the unit's first tile, and with it the CTAs that share it
+    long long from[2], upto[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      if (owed[w] < 0) continue;
+      const int s = (int)(owed[w] / U);
+      const long long begin = (long long)p.src.tiles[s] * U + (owed[w] - (long long)s * U) * owed_n[w];
+      from[w] = begin / cta_span;
+      upto[w] = (begin + owed_n[w] - 1) / cta_span;
+    }
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x < 2 && owed[threadIdx.x] >= 0) {
+      const int w = threadIdx.x;
+      const unsigned there = (unsigned)(upto[w] - from[w]);
+      if (atomicAdd(c.ticket + from[w], 1u) == there) {
+        c.ticket[from[w]] = 0;
+        s_last[w] = 1;
+      }
+    }
+    __syncthreads();
+    __threadfence();
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      if (owed[w] < 0 || !s_last[w] || !busy) continue;
+#pragma unroll
+      for (int y = 0; y < kMine; ++y) {
+        const int x = threadIdx.x + y * kWarps * 32, g = x / (D / 4);
+        auto part = [&](long long k) { return p.parts + (2 * k + (k == from[w])) * kPart; };
+        float m = -INFINITY;
+        for (long long k = from[w]; k <= upto[w]; ++k) m = fmaxf(m, __ldcg(part(k) + kHeads * D + g));
+        const float ref = m == -INFINITY ? 0.f : m;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float s = 0.f;
+        for (long long k = from[w]; k <= upto[w]; ++k) {
+          const float a = ex2(__ldcg(part(k) + kHeads * D + g) - ref);
+          const float4 z = __ldcg(reinterpret_cast<const float4 *>(part(k)) + x);
+          v.x = fmaf(z.x, a, v.x), v.y = fmaf(z.y, a, v.y);
+          v.z = fmaf(z.z, a, v.z), v.w = fmaf(z.w, a, v.w);
+          s = fmaf(__ldcg(part(k) + kHeads * D + kHeads + g), a, s);
+        }
+        if (g < c.G) {
+          const float r = 1.f / s;
+          infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
+          put4(out_of(owed[w]) + 4 * x, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+        }
+      }
+    }
+  }
+  if (infinite) atomicOr(c.err, (unsigned)kvr::ERR_NONFINITE);
+}
+
+template <typename T, int D, typename P>
+constexpr size_t smem_bytes() {
+  return (size_t)P::kWarps * (P::kStages * Shape<T, D>::kStage + part_floats(D) * 4 + P::kOwn);
+}
+
+template <typename T, int D>
+struct Choice {
+  using P = Fma<T, D>;
+};
+
+template <typename T, int D>
+cudaError_t prepare() {
+  using P = typename Choice<T, D>::P;
+  constexpr size_t bytes = smem_bytes<T, D, P>();
+  static_assert(bytes + 2 * P::kWarps * sizeof(Piece) + 64 <= 227 * 1024, "shared memory");
+  cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, P, float>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(attend_kernel<T, D, P, __nv_bfloat16>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  return e;
+}
+
+template <typename T, int D>
+cudaError_t launch(const AttendParams &p, int sms, cudaStream_t st) {
+  using P = typename Choice<T, D>::P;
+  const dim3 grid(attend_ctas(sms)), block(P::kWarps * 32);
+  return p.c.out_bf16 ? kvr::launch_pdl(attend_kernel<T, D, P, __nv_bfloat16>, grid, block,
+                                        smem_bytes<T, D, P>(), st, p)
+                      : kvr::launch_pdl(attend_kernel<T, D, P, float>, grid, block,
+                                        smem_bytes<T, D, P>(), st, p);
+}
+
+}  // namespace
+
+int attend_ctas(int sms) { return std::min(sms, 4096); }
+
+cudaError_t prepare_attend(const View &c) {
+  if (c.io_bf16) return c.d == 128 ? prepare<__nv_bfloat16, 128>() : prepare<__nv_bfloat16, 64>();
+  return c.d == 128 ? prepare<float, 128>() : prepare<float, 64>();
+}
+
+cudaError_t launch_attend(const AttendParams &p, int sms, cudaStream_t st) {
+  if (p.c.io_bf16)
+    return p.c.d == 128 ? launch<__nv_bfloat16, 128>(p, sms, st)
+                        : launch<__nv_bfloat16, 64>(p, sms, st);
+  return p.c.d == 128 ? launch<float, 128>(p, sms, st) : launch<float, 64>(p, sms, st);
+}
+
+}  // namespace paged
+}  // namespace kvr

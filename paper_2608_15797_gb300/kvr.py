@@ -1055,6 +1055,266 @@ class Kv4Cache:
                "kvr_kv4_sync_status")
 
 
+# ---- the full context in pages ----------------------------------------------
+
+class kvr_paged_desc(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int), ("n_layers", ctypes.c_int),
+                ("n_kv_heads", ctypes.c_int), ("group", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("n_pages", ctypes.c_int),
+                ("page_rows", ctypes.c_int), ("table_pages", ctypes.c_int),
+                ("kv_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int),
+                ("softmax_scale", ctypes.c_float)]
+
+
+for _name, (_res, _args) in {
+    "kvr_paged_required_bytes": (ctypes.c_size_t,
+                                 [ctypes.POINTER(kvr_paged_desc)]),
+    "kvr_paged_create": (_S, [ctypes.POINTER(kvr_paged_desc), _P,
+                              ctypes.c_size_t, _P, ctypes.POINTER(_P)]),
+    "kvr_paged_destroy": (None, [_P]),
+    "kvr_paged_plan": (_S, [_P, _P, _I, _P, _P]),
+    "kvr_paged_append": (_S, [_P, _I, _I, _I, _I, _P, _P, _P, _P]),
+    "kvr_paged_attend_workspace_bytes": (ctypes.c_size_t, [_P, _I, _I]),
+    "kvr_paged_attend": (_S, [_P, _I, _I, _P, _P, _P, ctypes.c_size_t, _P]),
+    "kvr_paged_attend_pages_workspace_bytes": (ctypes.c_size_t,
+                                               [_P, _I, _I, _I, _I]),
+    "kvr_paged_attend_pages": (_S, [_P, _I, _I, _P, _I, _I, _P, _P, _P,
+                                    ctypes.c_size_t, _P]),
+    "kvr_paged_tables": (_S, [_P, _P, _P, _P, _P]),
+    "kvr_paged_rows": (_S, [_P, _P, _P, _P]),
+    "kvr_paged_launch_count": (_S, [_P, _P]),
+    "kvr_paged_sync_status": (_S, [_P, _P]),
+}.items():
+    _f = getattr(lib, _name)
+    _f.restype = _res
+    _f.argtypes = _args
+
+
+class PagedCache:
+    """Full contexts in pages of a shared pool (kvr_paged_*; include/kvr.h says
+    how they are kept): owner of the handle and of the torch buffer it lives in.
+    What a call allocates belongs to the call's stream, as with Kv4Cache.
+    Calls run on the current device, which has to be the cache's."""
+
+    @staticmethod
+    def make_desc(n_seq, n_layers, n_kv_heads, group, head_dim, n_pages,
+                  page_rows=64, table_pages=None, dtype="bf16",
+                  out_dtype="bf16", softmax_scale=0.0):
+        """table_pages: pages a sequence may hold, by default the whole pool."""
+        return kvr_paged_desc(
+            n_seq, n_layers, n_kv_heads, group, head_dim, n_pages, page_rows,
+            n_pages if table_pages is None else table_pages, DTYPES[dtype],
+            DTYPES[out_dtype], float(softmax_scale))
+
+    @staticmethod
+    def required_bytes(*args, **kw):
+        """Bytes of the buffer, for __init__'s arguments up to softmax_scale."""
+        d = PagedCache.make_desc(*args, **kw)
+        return int(lib.kvr_paged_required_bytes(ctypes.byref(d)))
+
+    def __init__(self, n_seq, n_layers, n_kv_heads, group, head_dim, n_pages,
+                 page_rows=64, table_pages=None, dtype="bf16",
+                 out_dtype="bf16", softmax_scale=0.0, device="cuda",
+                 stream=None, buf=None):
+        """dtype: element type of q, k and v.  buf: an optional caller-owned
+        uint8 device tensor of at least required_bytes(...) (256-byte aligned);
+        by default one is allocated."""
+        self.desc = self.make_desc(n_seq, n_layers, n_kv_heads, group,
+                                   head_dim, n_pages, page_rows, table_pages,
+                                   dtype, out_dtype, softmax_scale)
+        self.S, self.L, self.H, self.G, self.d = (n_seq, n_layers, n_kv_heads,
+                                                  group, head_dim)
+        self.n_pages, self.page_rows = n_pages, page_rows
+        self.table_pages = self.desc.table_pages
+        self.dtype, self.out_dtype = dtype, out_dtype
+        self._io, self._out = TORCH_DTYPES[dtype], TORCH_DTYPES[out_dtype]
+        self._all, self._tables, self._pool = (0, n_layers), None, None
+        self.nbytes = int(lib.kvr_paged_required_bytes(ctypes.byref(self.desc)))
+        if self.nbytes == 0:
+            raise KvrError(KVR_EINVAL, "PagedCache", "invalid descriptor")
+        if buf is None:
+            buf = _empty(self.nbytes, torch.uint8, device, stream)
+        elif buf.numel() < self.nbytes or buf.dtype != torch.uint8 or \
+                not buf.is_contiguous():
+            raise ValueError("buf must be contiguous uint8 with at least "
+                             f"{self.nbytes} bytes")
+        self.buf = buf
+        self._device = _on_device(buf, "buf")
+        h = _P()
+        _check(lib.kvr_paged_create(ctypes.byref(self.desc), _ptr(buf),
+                                    self.nbytes, self._at(stream),
+                                    ctypes.byref(h)), "kvr_paged_create")
+        self.handle = h
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h:
+            lib.kvr_paged_destroy(h)
+            self.handle = None
+
+    def _at(self, stream):
+        """The call's stream; a ValueError where kernels would run on another
+        device than the cache's."""
+        if _raw_device is not None and _raw_device() != self._device:
+            raise ValueError(f"the cache lies on cuda:{self._device}, the "
+                             f"current device is cuda:{_raw_device()}")
+        return _stream(stream)
+
+    def _tensor(self, x, shape, dtype, what):
+        """The address of x, a dense tensor of this shape on the cache's
+        device."""
+        if x.shape != shape or x.dtype is not dtype or not x.is_contiguous():
+            raise ValueError(f"{what} must be contiguous {dtype} "
+                             f"{list(shape)}, not {x.dtype} {list(x.shape)}")
+        if x.get_device() != self._device:
+            _on_device(x, what, self._device)  # raises
+        return x.data_ptr()
+
+    def plan(self, lens, n_new=0, slots=None, stream=None):
+        """The sequences' lengths become lens (int32 [S] on the device); returns
+        the slots [S][n_new] of the tokens they grow by, None where n_new is 0
+        (kvr_paged_plan)."""
+        at = self._at(stream)
+        want = self._tensor(lens, (self.S,), torch.int32, "lens")
+        if n_new < 0 or n_new > 1 << 24:
+            raise ValueError(f"{n_new} new tokens")
+        if slots is None and n_new:
+            slots = _empty((self.S, n_new), torch.int32, self.buf.device,
+                           stream)
+        to = None if slots is None else self._tensor(
+            slots, (self.S, n_new), torch.int32, "slots")
+        _check(lib.kvr_paged_plan(self.handle, want, n_new,
+                                  to if n_new else None, at), "kvr_paged_plan")
+        return slots
+
+    def append(self, k, v, slots, layers=None, stream=None):
+        """New tokens' keys and values: k, v [n][nl][n_new][H][d], slots int32
+        [n][n_new], rows of a plan's (kvr_paged_append)."""
+        lb, le = layers or self._all
+        n, n_new = slots.shape
+        shape = (n, le - lb, n_new, self.H, self.d)
+        _check(lib.kvr_paged_append(
+            self.handle, lb, le, n, n_new,
+            self._tensor(slots, (n, n_new), torch.int32, "slots"),
+            self._tensor(k, shape, self._io, "k"),
+            self._tensor(v, shape, self._io, "v"), self._at(stream)),
+            "kvr_paged_append")
+
+    def _workspace(self, name, *args):
+        n = int(getattr(lib, name)(self.handle, *args))
+        if n == 0:
+            raise KvrError(KVR_EINVAL, name, "invalid arguments")
+        return torch.empty(n, dtype=torch.uint8, device=self.buf.device)
+
+    def attend_workspace(self, layers=None):
+        """A workspace for attend() over these layers."""
+        return self._workspace("kvr_paged_attend_workspace_bytes",
+                               *(layers or self._all))
+
+    def attend_pages_workspace(self, budget, window=1, layers=None):
+        """A workspace for attend_pages() with this choice over these layers."""
+        return self._workspace("kvr_paged_attend_pages_workspace_bytes",
+                               *(layers or self._all), budget, window)
+
+    def _outputs(self, q, out, layers, stream):
+        lb, le = layers
+        shape = (self.S, le - lb, self.H * self.G, self.d)
+        qp = self._tensor(q, shape, self._io, "q")
+        if out is None:
+            out = _empty(shape, self._out, q.device, stream)
+        return qp, out, self._tensor(out, shape, self._out, "out")
+
+    def attend(self, q, out=None, layers=None, workspace=None, stream=None):
+        """Attention of each sequence's newest token: q [S][nl][H*G][d] -> out,
+        the same shape in out_dtype (kvr_paged_attend)."""
+        lb, le = layers or self._all
+        at = self._at(stream)
+        qp, out, op = self._outputs(q, out, (lb, le), stream)
+        if workspace is None:
+            workspace = _scratch(int(lib.kvr_paged_attend_workspace_bytes(
+                self.handle, lb, le)), q.device, stream)
+        else:
+            _given_workspace(workspace, self._device)
+        _check(lib.kvr_paged_attend(self.handle, lb, le, qp, op,
+                                    workspace.data_ptr(), workspace.nbytes,
+                                    at), "kvr_paged_attend")
+        return out
+
+    def attend_pages(self, q, budget, window=1, out=None, pages=None,
+                     layers=None, workspace=None, stream=None):
+        """The same over each unit's window newest pages and the budget others
+        of the greatest score (kvr_paged_attend_pages); pages: an int32 tensor
+        [S][nl][H][budget + window] for the choice."""
+        lb, le = layers or self._all
+        at = self._at(stream)
+        qp, out, op = self._outputs(q, out, (lb, le), stream)
+        pp = None if pages is None else self._tensor(
+            pages, (self.S, le - lb, self.H, budget + window), torch.int32,
+            "pages")
+        if workspace is None:
+            workspace = _scratch(
+                int(lib.kvr_paged_attend_pages_workspace_bytes(
+                    self.handle, lb, le, budget, window)), q.device, stream)
+        else:
+            _given_workspace(workspace, self._device)
+        _check(lib.kvr_paged_attend_pages(
+            self.handle, lb, le, qp, budget, window, op, pp,
+            workspace.data_ptr(), workspace.nbytes, at),
+            "kvr_paged_attend_pages")
+        return out
+
+    def tables_view(self):
+        """(table [S][table_pages], lens [S], free pages [1]) as device tensors
+        viewing the buffer, to be read only."""
+        if self._tables is None:  # the buffer stays where it is
+            p = [_P() for _ in range(3)]
+            stride = ctypes.c_int64()
+            _check(lib.kvr_paged_tables(
+                self.handle, ctypes.byref(p[0]), ctypes.byref(stride),
+                ctypes.byref(p[1]), ctypes.byref(p[2])), "kvr_paged_tables")
+            self._tables = tuple(
+                self._view(at, shape, torch.int32)
+                for at, shape in zip(p, ((self.S, stride.value), (self.S,),
+                                         (1,))))
+        return self._tables
+
+    def _view(self, at, shape, dtype):
+        off = at.value - self.buf.data_ptr()
+        n = int(np.prod(shape, dtype=np.int64)) * dtype.itemsize
+        return self.buf.view(-1)[off:off + n].view(dtype).view(shape)
+
+    def _views(self):
+        if self._pool is None:
+            p = [_P() for _ in range(3)]
+            _check(lib.kvr_paged_rows(self.handle, *map(ctypes.byref, p)),
+                   "kvr_paged_rows")
+            lead = (self.L, self.n_pages, self.H)
+            self._pool = tuple(
+                self._view(at, (*lead, rows, self.d), self._io)
+                for at, rows in zip(p, (self.page_rows, self.page_rows, 2)))
+        return self._pool
+
+    def rows_view(self):
+        """(K, V) as device tensors viewing the buffer, each
+        [L][n_pages][H][page_rows][d], to be read only."""
+        return self._views()[:2]
+
+    def bounds_view(self):
+        """The least and greatest keys of full pages, [L][n_pages][H][2][d], as
+        a device tensor viewing the buffer, to be read only."""
+        return self._views()[2]
+
+    def launch_count(self):
+        n = ctypes.c_uint64()
+        _check(lib.kvr_paged_launch_count(self.handle, ctypes.byref(n)),
+               "kvr_paged_launch_count")
+        return int(n.value)
+
+    def sync_status(self, stream=None):
+        _check(lib.kvr_paged_sync_status(self.handle, _stream(stream)),
+               "kvr_paged_sync_status")
+
+
 # ---- verification of drafted tokens -----------------------------------------
 
 class kvr_verify_desc(ctypes.Structure):
