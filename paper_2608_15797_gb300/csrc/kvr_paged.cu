@@ -336,7 +336,7 @@ struct Layout {
   size_t K, V, bounds, table, len, from, tiles, stack, free, ticket, err, total;
 };
 
-constexpr int kMaxCtas = 4096;  // of the attention, on any device
+constexpr int kMaxCtas = 1024;  // of the attention, on any device
 
 bool layout_of(const kvr_paged_desc *d, Layout *l) {
   if (!d || d->n_seq < 1 || d->n_seq > 65535 || d->n_layers < 1 || d->n_kv_heads < 1 ||

@@ -28,6 +28,7 @@ namespace {
 using namespace kvr::ptx;
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxCtas = 1024;  // whose weights the last one holds for 8 heads
 
 // 16 bytes to shared memory, zeros where `bytes` is 0 (nothing is read then).
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {
@@ -78,7 +79,7 @@ struct Shape {
   static constexpr int E = Elems<T>::N;
 };
 
-// Plain arithmetic in fp32, for either type.  Logits: four lanes share a row, each a
+// Plain arithmetic in fp32, for fp32 rows.  Logits: four lanes share a row, each a
 // quarter of its channels.  Values: a lane owns E channels.
 template <typename T, int D>
 struct Fma : Shape<T, D> {
@@ -208,6 +209,117 @@ struct Fma : Shape<T, D> {
           f(g, lane * S::E + e, make_float4(o[g][e], o[g][e + 1], o[g][e + 2], o[g][e + 3]), mg,
             lg);
     }
+  }
+};
+
+// bf16 on warp-level tensor cores (a unit has eight query rows at most: what binds is
+// bytes).  Products run over 16 channels or 16 rows whatever their order, so a lane's
+// 16-byte vectors are fragments as they come: of K, eight channels of a row, which are
+// two steps' share of a lane; of V, eight channels of four rows, whose halves are
+// paired by byte permutation.  Probabilities go in as two bf16 numbers each (the 8
+// rows that heads leave free hold the low ones), which keeps 2^-16 of them; a tile's
+// sum is formed from zero and added in fp32, because the accumulator truncates.
+template <int D>
+struct Mma : Shape<__nv_bfloat16, D> {
+  using S = Shape<__nv_bfloat16, D>;
+  static constexpr int kWarps = 8, kStages = D == 128 ? 3 : 6;
+  static constexpr int kOwn = 0;
+  static constexpr int kK = D / 32, kV = D / 64;  // vectors of a row, K or V
+  uint4 q[kK];
+  float scale;
+  float m, l;          // head lane / 4
+  float o[kV][8][2];   // channels 64 v + 8 (2 (lane & 3) + i) + e at [v][e][i]
+
+  static __device__ __forceinline__ int k_row(int lane, int x) { return (lane >> 2) + 8 * (x & 1); }
+  static __device__ __forceinline__ int k_vec(int lane, int x) { return (lane & 3) + 4 * (x >> 1); }
+  static __device__ __forceinline__ int v_row(int lane, int x) {
+    return 2 * (lane & 3) + (x & 1) + 8 * ((x >> 1) & 1);
+  }
+  static __device__ __forceinline__ int v_vec(int lane, int x) { return (lane >> 2) + 8 * (x >> 2); }
+
+  __device__ __forceinline__ void init(uint8_t *, float scale_log2e) { scale = scale_log2e; }
+  __device__ __forceinline__ void start(const __nv_bfloat16 *from, int G, int lane) {
+    const int g = lane >> 2;
+#pragma unroll
+    for (int i = 0; i < kK; ++i)
+      q[i] = g < G ? __ldg(reinterpret_cast<const uint4 *>(from + g * D) + (lane & 3) + 4 * i)
+                   : make_uint4(0, 0, 0, 0);
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int v = 0; v < kV; ++v)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[v][e][0] = o[v][e][1] = 0.f;
+  }
+  __device__ __forceinline__ void step(const uint4 *stage, int limit, int lane) {
+    float s[2][4];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[r][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kK; ++i) {
+        const uint4 k = stage[(2 * i + r) * 32 + lane];
+        mma_bf16(s[r], q[i].x, 0u, q[i].y, 0u, k.x, k.y);
+        mma_bf16(s[r], q[i].z, 0u, q[i].w, 0u, k.z, k.w);
+      }
+    }
+    // rows 8 r + 2 (lane & 3) + i at [r][i]
+    float x[2][2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        x[r][i] = 8 * r + 2 * (lane & 3) + i < limit ? s[r][i] * scale : -INFINITY;
+    float t = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
+    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
+    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+    const float now = fmaxf(m, t), ref = now == -INFINITY ? 0.f : now;
+    const float a = ex2(m - ref);
+    m = now;
+    uint32_t hi[2], lo[2];
+    l *= a;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const float p0 = ex2(x[r][0] - ref), p1 = ex2(x[r][1] - ref);
+      l += p0 + p1;
+      hi[r] = pack_bf16(p0, p1);
+      lo[r] = pack_bf16(p0 - __uint_as_float(hi[r] << 16),
+                        p1 - __uint_as_float(hi[r] & 0xFFFF0000u));
+    }
+    const uint4 *vs = stage + S::kPer * 32 + lane;
+    // what the accumulators of head lane / 4 are multiplied by is the lane's own a
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      const uint4 w0 = vs[(4 * v) * 32], w1 = vs[(4 * v + 1) * 32];
+      const uint4 w2 = vs[(4 * v + 2) * 32], w3 = vs[(4 * v + 3) * 32];
+      const uint32_t b[4][4] = {{w0.x, w0.y, w0.z, w0.w},
+                                {w1.x, w1.y, w1.z, w1.w},
+                                {w2.x, w2.y, w2.z, w2.w},
+                                {w3.x, w3.y, w3.z, w3.w}};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t sel = e & 1 ? 0x7632u : 0x5410u;
+        float d[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_bf16(d, hi[0], lo[0], hi[1], lo[1], __byte_perm(b[0][e >> 1], b[1][e >> 1], sel),
+                 __byte_perm(b[2][e >> 1], b[3][e >> 1], sel));
+        o[v][e][0] = fmaf(o[v][e][0], a, d[0] + d[2]);
+        o[v][e][1] = fmaf(o[v][e][1], a, d[1] + d[3]);
+      }
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void finish(int lane, F f) {
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+#pragma unroll
+    for (int v = 0; v < kV; ++v)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; e += 4)
+          f(lane >> 2, 64 * v + 16 * (lane & 3) + 8 * i + e,
+            make_float4(o[v][e][i], o[v][e + 1][i], o[v][e + 2][i], o[v][e + 3][i]), m, l);
   }
 };
 
@@ -461,30 +573,51 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
     }
     __syncthreads();
     __threadfence();
+    // (a piece that lies in one CTA never comes here, so shared memory is free: the
+    // weights of all pieces first, then their sums with loads in flight together)
+    float *weight = reinterpret_cast<float *>(smem), *sum = weight + kHeads * kMaxCtas;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      if (owed[w] < 0 || !s_last[w] || !busy) continue;
+      if (owed[w] < 0 || !s_last[w]) continue;
+      const int many = (int)(upto[w] - from[w]) + 1;
+      auto part = [&](int k) { return p.parts + (2 * (from[w] + k) + (k == 0)) * kPart; };
+      __syncthreads();
+      for (int g = warp; g < c.G; g += kWarps) {
+        float m = -INFINITY;
+        for (int k = lane; k < many; k += 32) {
+          const float x = __ldcg(part(k) + kHeads * D + g);
+          weight[g * kMaxCtas + k] = x;
+          m = fmaxf(m, x);
+        }
+        m = kvr::dev::warp_max(m);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float s = 0.f;
+        for (int k = lane; k < many; k += 32) {
+          const float a = ex2(weight[g * kMaxCtas + k] - ref);
+          weight[g * kMaxCtas + k] = a;
+          s = fmaf(__ldcg(part(k) + kHeads * D + kHeads + g), a, s);
+        }
+        s = kvr::dev::warp_sum(s);
+        if (lane == 0) sum[g] = s;
+      }
+      __syncthreads();
+      if (!busy) continue;
 #pragma unroll
       for (int y = 0; y < kMine; ++y) {
         const int x = threadIdx.x + y * kWarps * 32, g = x / (D / 4);
-        auto part = [&](long long k) { return p.parts + (2 * k + (k == from[w])) * kPart; };
-        float m = -INFINITY;
-        for (long long k = from[w]; k <= upto[w]; ++k) m = fmaxf(m, __ldcg(part(k) + kHeads * D + g));
-        const float ref = m == -INFINITY ? 0.f : m;
+        if (g >= c.G) continue;
+        const float *wt = weight + g * kMaxCtas;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        float s = 0.f;
-        for (long long k = from[w]; k <= upto[w]; ++k) {
-          const float a = ex2(__ldcg(part(k) + kHeads * D + g) - ref);
+#pragma unroll 8
+        for (int k = 0; k < many; ++k) {
           const float4 z = __ldcg(reinterpret_cast<const float4 *>(part(k)) + x);
+          const float a = wt[k];
           v.x = fmaf(z.x, a, v.x), v.y = fmaf(z.y, a, v.y);
           v.z = fmaf(z.z, a, v.z), v.w = fmaf(z.w, a, v.w);
-          s = fmaf(__ldcg(part(k) + kHeads * D + kHeads + g), a, s);
         }
-        if (g < c.G) {
-          const float r = 1.f / s;
-          infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
-          put4(out_of(owed[w]) + 4 * x, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-        }
+        const float s = sum[g], r = 1.f / s;
+        infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
+        put4(out_of(owed[w]) + 4 * x, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
       }
     }
   }
@@ -499,6 +632,10 @@ constexpr size_t smem_bytes() {
 template <typename T, int D>
 struct Choice {
   using P = Fma<T, D>;
+};
+template <int D>
+struct Choice<__nv_bfloat16, D> {
+  using P = Mma<D>;
 };
 
 template <typename T, int D>
@@ -526,7 +663,7 @@ cudaError_t launch(const AttendParams &p, int sms, cudaStream_t st) {
 
 }  // namespace
 
-int attend_ctas(int sms) { return std::min(sms, 4096); }
+int attend_ctas(int sms) { return std::min(sms, kMaxCtas); }
 
 cudaError_t prepare_attend(const View &c) {
   if (c.io_bf16) return c.d == 128 ? prepare<__nv_bfloat16, 128>() : prepare<__nv_bfloat16, 64>();
