@@ -336,8 +336,6 @@ struct Layout {
   size_t K, V, bounds, table, len, from, tiles, stack, free, ticket, err, total;
 };
 
-constexpr int kMaxCtas = 1024;  // of the attention, on any device
-
 bool layout_of(const kvr_paged_desc *d, Layout *l) {
   if (!d || d->n_seq < 1 || d->n_seq > 65535 || d->n_layers < 1 || d->n_kv_heads < 1 ||
       d->group < 1 || d->group > kvr::paged::kHeads ||
@@ -369,7 +367,7 @@ bool layout_of(const kvr_paged_desc *d, Layout *l) {
   l->tiles = take(((size_t)d->n_seq + 1) * 4);
   l->stack = take((size_t)d->n_pages * 4);
   l->free = take(2 * 4);
-  l->ticket = take(kMaxCtas * 4);
+  l->ticket = take(kvr::paged::kMostCtas * 4);
   l->err = take(16);
   l->total = off;
   return true;
@@ -386,6 +384,16 @@ bool choice_ok(int budget, int window) {
   return budget >= 0 && window >= 1 && (long long)budget + window <= (1 << 24);
 }
 
+// Tiles of an attention over nl layers at most: of a pool that is full, or of `keep`
+// pages of every unit.
+long long most_tiles(const kvr_paged *c, int nl, int keep) {
+  const kvr_paged_desc &d = c->desc;
+  const long long a_page = d.page_rows / kvr::paged::kTile, units = (long long)nl * d.n_kv_heads;
+  const long long pages = std::min<long long>(d.n_pages, (long long)d.n_seq *
+                                              (keep ? std::min(keep, d.table_pages) : d.table_pages));
+  return pages * a_page * units;
+}
+
 // Parts of a workspace of either attention; `pages` of a choice, or none.
 struct Work {
   size_t parts, score, list, rows, tiles, total;
@@ -400,11 +408,15 @@ Work work_of(const kvr_paged *c, int nl, int budget, int window) {
     off += (bytes + 15) / 16 * 16;
     return at;
   };
-  w.parts = take((size_t)2 * kvr::paged::attend_ctas(c->sms) *
+  if (window > 0) w.keep = (int)std::min<long long>((long long)budget + window, d.table_pages);
+  kvr::paged::AttendParams p{};
+  p.c = c->view;
+  p.nl = nl;
+  p.most = most_tiles(c, nl, w.keep);
+  w.parts = take((size_t)2 * kvr::paged::attend_ctas(p, c->sms) *
                  kvr::paged::part_floats(d.head_dim) * sizeof(float));
   if (window > 0) {
     const size_t units = (size_t)d.n_seq * nl * d.n_kv_heads;
-    w.keep = (int)std::min<long long>((long long)budget + window, d.table_pages);
     w.score = take(units * d.table_pages * sizeof(float2));
     w.list = take(units * w.keep * sizeof(int32_t));
     w.rows = take((size_t)d.n_seq * sizeof(int32_t));
@@ -564,6 +576,7 @@ kvr_status kvr_paged_attend(kvr_paged *c, int lb, int le, const void *q, void *o
   p.nl = le - lb;
   p.q = q;
   p.out = out;
+  p.most = most_tiles(c, p.nl, 0);
   p.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.parts);
   const cudaError_t e = kvr::paged::launch_attend(p, c->sms, as_stream(stream));
   if (e != cudaSuccess) return cuda_fail("kvr_paged_attend", e);
@@ -611,6 +624,7 @@ kvr_status kvr_paged_attend_pages(kvr_paged *c, int lb, int le, const void *q, i
   p.nl = le - lb;
   p.q = q;
   p.out = out;
+  p.most = most_tiles(c, p.nl, w.keep);
   p.parts = reinterpret_cast<float *>(ws + w.parts);
   e = kvr::paged::launch_attend(p, c->sms, as_stream(stream));
   if (e != cudaSuccess) return cuda_fail("kvr_paged_attend_pages", e);

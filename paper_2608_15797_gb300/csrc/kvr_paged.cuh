@@ -48,10 +48,13 @@ struct AttendParams {
   const void *q;   // [S][nl][H * G][d]
   void *out;
   float *parts;    // [2 * CTAs][part_floats(d)]
+  long long most;  // tiles that the call can have, whatever the lengths
 };
 __host__ __device__ constexpr int part_floats(int d) { return kHeads * d + 2 * kHeads; }
 
-int attend_ctas(int sms);
+// CTAs of a launch, a matter of p.c, p.nl and p.most.
+constexpr int kMostCtas = 2560;
+int attend_ctas(const AttendParams &p, int sms);
 cudaError_t prepare_attend(const View &c);
 cudaError_t launch_attend(const AttendParams &p, int sms, cudaStream_t st);
 

@@ -28,7 +28,8 @@ namespace {
 using namespace kvr::ptx;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxCtas = 1024;  // whose weights the last one holds for 8 heads
+constexpr int kMaxCtas = kMostCtas;  // whose weights the last one holds for 8 heads
+constexpr int kLeast = 3;       // tiles of a warp, where there are as many
 
 // 16 bytes to shared memory, zeros where `bytes` is 0 (nothing is read then).
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {
@@ -222,7 +223,7 @@ struct Fma : Shape<T, D> {
 template <int D>
 struct Mma : Shape<__nv_bfloat16, D> {
   using S = Shape<__nv_bfloat16, D>;
-  static constexpr int kWarps = 8, kStages = D == 128 ? 3 : 6;
+  static constexpr int kWarps = 4, kStages = D == 128 ? 3 : 6;
   static constexpr int kOwn = 0;
   static constexpr int kK = D / 32, kV = D / 64;  // vectors of a row, K or V
   uint4 q[kK];
@@ -340,6 +341,8 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
   using S = Shape<T, D>;
   constexpr int kWarps = P::kWarps, kStages = P::kStages, kPart = part_floats(D);
   static_assert(kStages * S::kStage >= kPart * 4, "a warp's last piece takes its copies' place");
+  static_assert(kWarps * kStages * S::kStage >= kHeads * (kMaxCtas + 1) * 4,
+                "the weights of a unit's parts");
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Piece s_piece[2 * kWarps];
   __shared__ int s_last[2];
@@ -351,7 +354,8 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
   const uint32_t ring32 = smem_u32(ring);
   const int U = p.nl * c.H;  // units of a sequence
   const long long total = (long long)p.src.tiles[c.S] * U;
-  const long long span = (total + (long long)gridDim.x * kWarps - 1) / ((long long)gridDim.x * kWarps);
+  const long long warps = (long long)gridDim.x * kWarps;
+  const long long span = max((long long)kLeast, (total + warps - 1) / warps);
   const long long cta_span = span * kWarps;
   const long long t0 = min(total, ((long long)blockIdx.x * kWarps + warp) * span);
   const long long t1 = min(total, t0 + span);
@@ -561,26 +565,39 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
       from[w] = begin / cta_span;
       upto[w] = (begin + owed_n[w] - 1) / cta_span;
     }
-    __threadfence();
     __syncthreads();
     if (threadIdx.x < 2 && owed[threadIdx.x] >= 0) {
       const int w = threadIdx.x;
+      // (the barrier and this fence order every thread's part before the arrival)
+      __threadfence();
       const unsigned there = (unsigned)(upto[w] - from[w]);
       if (atomicAdd(c.ticket + from[w], 1u) == there) {
         c.ticket[from[w]] = 0;
         s_last[w] = 1;
       }
+      __threadfence();
     }
     __syncthreads();
-    __threadfence();
-    // (a piece that lies in one CTA never comes here, so shared memory is free: the
-    // weights of all pieces first, then their sums with loads in flight together)
+    // Shared memory is free now: the weights of all parts there, while the first
+    // parts' values are on their way.
     float *weight = reinterpret_cast<float *>(smem), *sum = weight + kHeads * kMaxCtas;
+    constexpr int kAhead = 8;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       if (owed[w] < 0 || !s_last[w]) continue;
       const int many = (int)(upto[w] - from[w]) + 1;
       auto part = [&](int k) { return p.parts + (2 * (from[w] + k) + (k == 0)) * kPart; };
+      float4 z[kMine][kAhead];
+      auto fetch = [&](int k0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+          for (int y = 0; y < kMine; ++y)
+            if (busy && k0 + k < many)
+              z[y][k] = __ldcg(reinterpret_cast<const float4 *>(part(k0 + k)) + threadIdx.x +
+                               y * kWarps * 32);
+      };
+      fetch(0);
       __syncthreads();
       for (int g = warp; g < c.G; g += kWarps) {
         float m = -INFINITY;
@@ -602,22 +619,33 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
       }
       __syncthreads();
       if (!busy) continue;
+      float4 v[kMine];
+#pragma unroll
+      for (int y = 0; y < kMine; ++y) v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k0 = 0;;) {
+#pragma unroll
+        for (int y = 0; y < kMine; ++y) {
+          const int g = (threadIdx.x + y * kWarps * 32) / (D / 4);
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) {
+            if (k0 + k >= many || g >= c.G) continue;
+            const float a = weight[g * kMaxCtas + k0 + k];
+            v[y].x = fmaf(z[y][k].x, a, v[y].x), v[y].y = fmaf(z[y][k].y, a, v[y].y);
+            v[y].z = fmaf(z[y][k].z, a, v[y].z), v[y].w = fmaf(z[y][k].w, a, v[y].w);
+          }
+        }
+        k0 += kAhead;
+        if (k0 >= many) break;
+        fetch(k0);
+      }
 #pragma unroll
       for (int y = 0; y < kMine; ++y) {
         const int x = threadIdx.x + y * kWarps * 32, g = x / (D / 4);
         if (g >= c.G) continue;
-        const float *wt = weight + g * kMaxCtas;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int k = 0; k < many; ++k) {
-          const float4 z = __ldcg(reinterpret_cast<const float4 *>(part(k)) + x);
-          const float a = wt[k];
-          v.x = fmaf(z.x, a, v.x), v.y = fmaf(z.y, a, v.y);
-          v.z = fmaf(z.z, a, v.z), v.w = fmaf(z.w, a, v.w);
-        }
         const float s = sum[g], r = 1.f / s;
         infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
-        put4(out_of(owed[w]) + 4 * x, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+        put4(out_of(owed[w]) + 4 * x,
+             make_float4(v[y].x * r, v[y].y * r, v[y].z * r, v[y].w * r));
       }
     }
   }
@@ -651,10 +679,25 @@ cudaError_t prepare() {
   return e;
 }
 
+// CTAs of a launch: as many as run at once, or several times as many, where the
+// largest call would still give every warp 24 tiles: SMs do not get the same share of
+// the memory's rate, and shorter spans even that out.
+template <typename T, int D>
+int ctas_of(const AttendParams &p, int sms) {
+  using P = typename Choice<T, D>::P;
+  // (of an SM's 228 KB a CTA takes 1 KB more than it asks for)
+  constexpr int kResident =
+      228 * 1024 / (int)(smem_bytes<T, D, P>() + 2 * P::kWarps * sizeof(Piece) + 64 + 1024);
+  static_assert(kResident >= 1, "shared memory");
+  const int at_once = std::min(sms * kResident, kMaxCtas);
+  const long long waves = p.most / ((long long)at_once * P::kWarps * 24);
+  return at_once * (int)std::max(1ll, std::min<long long>(waves, std::min(8, kMaxCtas / at_once)));
+}
+
 template <typename T, int D>
 cudaError_t launch(const AttendParams &p, int sms, cudaStream_t st) {
   using P = typename Choice<T, D>::P;
-  const dim3 grid(attend_ctas(sms)), block(P::kWarps * 32);
+  const dim3 grid(ctas_of<T, D>(p, sms)), block(P::kWarps * 32);
   return p.c.out_bf16 ? kvr::launch_pdl(attend_kernel<T, D, P, __nv_bfloat16>, grid, block,
                                         smem_bytes<T, D, P>(), st, p)
                       : kvr::launch_pdl(attend_kernel<T, D, P, float>, grid, block,
@@ -663,7 +706,11 @@ cudaError_t launch(const AttendParams &p, int sms, cudaStream_t st) {
 
 }  // namespace
 
-int attend_ctas(int sms) { return std::min(sms, kMaxCtas); }
+int attend_ctas(const AttendParams &p, int sms) {
+  if (p.c.io_bf16)
+    return p.c.d == 128 ? ctas_of<__nv_bfloat16, 128>(p, sms) : ctas_of<__nv_bfloat16, 64>(p, sms);
+  return p.c.d == 128 ? ctas_of<float, 128>(p, sms) : ctas_of<float, 64>(p, sms);
+}
 
 cudaError_t prepare_attend(const View &c) {
   if (c.io_bf16) return c.d == 128 ? prepare<__nv_bfloat16, 128>() : prepare<__nv_bfloat16, 64>();
