@@ -631,7 +631,8 @@ typedef struct {
   int n_kv_heads;      /* H (>= 1); L * H <= 65535, L * H * S < 2^31 - 1 */
   int group;           /* G = query heads per KV head, 1..8 */
   int head_dim;        /* d: 64 or 128 */
-  int n_pages;         /* pages of the pool (>= 1), n_pages * page_rows < 2^31 */
+  int n_pages;         /* pages of the pool (>= 1), n_pages * page_rows < 2^31,
+                          L * H * n_pages * page_rows < 2^35 */
   int page_rows;       /* 16, 32, 64 or 128 */
   int table_pages;     /* pages of a sequence at most (>= 1), times page_rows < 2^31 */
   kvr_dtype kv_dtype;  /* K, V and q element type */

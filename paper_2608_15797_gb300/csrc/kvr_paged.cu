@@ -20,15 +20,17 @@ namespace {
 
 // ---- plan -------------------------------------------------------------------
 
-constexpr int kPlan = 1024;          // threads of the plan's CTA, sequences of a span
-constexpr int kPlanWarps = kPlan / 32;
+constexpr int kPlan = 1024;       // threads of the plan's CTA, sequences of a span
+constexpr int kPlanFew = 256;     // the same of a small call
+constexpr int kOneCta = 16384;    // slots that the plan's CTA writes itself
+constexpr int kFill = 256, kFillTokens = 2048;  // of a CTA that writes slots alone
 
 __global__ void __launch_bounds__(256) init_kernel(const __grid_constant__ View c) {
   kvr::pdl_begin();
   const long long i0 = (long long)blockIdx.x * 256 + threadIdx.x, step = (long long)gridDim.x * 256;
   for (long long i = i0; i < (long long)c.S * c.tstride; i += step) c.table[i] = -1;
   for (long long i = i0; i < c.n_pages; i += step) c.stack[i] = c.n_pages - 1 - (int)i;
-  for (long long i = i0; i < c.S; i += step) c.len[i] = c.from[i] = 0;
+  for (long long i = i0; i < c.S; i += step) c.len[i] = c.from[i] = c.first[i] = 0;
   for (long long i = i0; i <= c.S; i += step) c.tiles[i] = 0;
   if (i0 == 0) c.free[0] = c.n_pages, c.free[1] = 1;
 }
@@ -53,123 +55,172 @@ __device__ __forceinline__ Change change_of(const View &c, const int32_t *want, 
   return x;
 }
 
+// What sequences ask for, summed: pages taken (any number may be asked for), given
+// back, and tiles (which only matter where the plan is carried out).
+struct Sums {
+  long long take;
+  int back, tiles;
+};
+__device__ __forceinline__ Sums operator+(Sums a, const Sums &b) {
+  a.take += b.take, a.back += b.back, a.tiles += b.tiles;
+  return a;
+}
+__device__ __forceinline__ Sums operator-(Sums a, const Sums &b) {
+  a.take -= b.take, a.back -= b.back, a.tiles -= b.tiles;
+  return a;
+}
+
 // Sum over the CTA of the values before this thread's, and of all of them.
-__device__ long long scan(long long x, long long *s_warp, long long *total) {
+template <int N>
+__device__ Sums scan(const Sums &x, Sums *s_warp, Sums *total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long y = x;
+  Sums y = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long z = __shfl_up_sync(0xffffffffu, y, o);
-    if (lane >= o) y += z;
+    Sums z;
+    z.take = __shfl_up_sync(0xffffffffu, y.take, o);
+    z.back = __shfl_up_sync(0xffffffffu, y.back, o);
+    z.tiles = __shfl_up_sync(0xffffffffu, y.tiles, o);
+    if (lane >= o) y = y + z;
   }
   __syncthreads();
   if (lane == 31) s_warp[warp] = y;
   __syncthreads();
-  long long before = 0, all = 0;
-  for (int w = 0; w < kPlanWarps; ++w) {
+  Sums before{}, all{};
+#pragma unroll
+  for (int w = 0; w < N / 32; ++w) {
     if (w == warp) before = all;
-    all += s_warp[w];
+    all = all + s_warp[w];
   }
   *total = all;
   return before + y - x;
 }
 
 // Sequence whose entries hold entry e: the last one that starts at or before it.
+template <int N>
 __device__ __forceinline__ int find(const int *start, int e) {
   int lo = 0;
 #pragma unroll
-  for (int step = kPlan / 2; step > 0; step >>= 1)
+  for (int step = N / 2; step > 0; step >>= 1)
     if (start[lo + step] <= e) lo += step;
   return lo;
 }
 
-__device__ __forceinline__ int slot_of(const View &c, const int32_t *slots, int s, int t, int from,
-                                       int len) {
+// Token t of a sequence's growth: its slot, and its page's entry in the table where
+// the page is new.  Pages behind the first `have` are the stack's, from `top` down.
+__device__ __forceinline__ int place(const View &c, int s, int t, int from, int len, int top) {
   const int pos = from + t;
   if (pos >= len) return -1;
-  return (c.table[(long long)s * c.tstride + (pos >> c.psh)] << c.psh) + (pos & (c.P - 1));
+  const int at = pos >> c.psh, have = (from + c.P - 1) >> c.psh;
+  int32_t *entry = c.table + (long long)s * c.tstride + at;
+  const int page = at < have ? *entry : c.stack[top - (at - have)];
+  if (at >= have && (pos & (c.P - 1)) == 0) *entry = page;
+  return (page << c.psh) + (pos & (c.P - 1));
 }
 
 // One CTA: S lengths are little work, and what they ask of the stack is a sum over
-// all of them.  Entries of tables (a prompt has hundreds of pages) are dealt out to
-// all threads, each finding its sequence in the sums.
-__global__ void __launch_bounds__(kPlan) plan_kernel(const __grid_constant__ View c,
-                                                     const int32_t *want, int n_new,
-                                                     int32_t *slots) {
+// all of them.  Pages that go back (an ended sequence has hundreds) are dealt out to
+// all threads.  Pages are taken by whoever
+// writes the slots of their tokens: this CTA, or for many slots the launch that
+// follows (256 prompts of up to 8,191 tokens, both plans of a pass: 641 us with this
+// CTA alone).
+template <int N>
+__global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
+                                                 const int32_t *want, int n_new, int32_t *slots) {
   kvr::pdl_begin();
-  __shared__ long long s_warp[kPlanWarps];
-  __shared__ int s_start[kPlan], s_page[kPlan];
+  __shared__ Sums s_warp[N / 32];
+  __shared__ int s_start[N], s_page[N], s_many[N];
   const int tid = threadIdx.x;
-  const int spans = (c.S + kPlan - 1) / kPlan;
-  long long back = 0, take = 0;
+  const int spans = (c.S + N - 1) / N;
+  const int had = c.free[0];
+  Change x{};
+  Sums all{}, at{};
+  // one span: its sums are kept
+  auto sums = [&](int k) {
+    x = change_of(c, want, k * N + tid, n_new);
+    at = scan<N>(Sums{x.take(), x.back(), (x.want + kTile - 1) / kTile}, s_warp, &all);
+  };
+  Sums total{};
   bool bad = false;
   for (int k = 0; k < spans; ++k) {
-    const Change x = change_of(c, want, k * kPlan + tid, n_new);
-    long long all;
-    scan(x.back(), s_warp, &all);
-    back += all;
-    scan(x.take(), s_warp, &all);
-    take += all;
+    sums(k);
+    total = total + all;
     bad |= x.bad;
   }
   bad = __syncthreads_or(bad);
-  const long long top = (long long)c.free[0] + back;
-  const bool short_of = take > top || top > c.n_pages;
-  __syncthreads();  // every thread has read the count
-  if (bad || short_of) {
+  const long long top = (long long)had + total.back;
+  if (bad || total.take > top || top > c.n_pages) {
     if (tid == 0) {
       atomicOr(c.err, bad ? (unsigned)kvr::ERR_LENGTH : (unsigned)kvr::ERR_CAPACITY);
       c.free[1] = 0;
     }
-    if (slots)
-      for (long long i = tid; i < (long long)c.S * n_new; i += kPlan) slots[i] = -1;
+    if (slots && (long long)c.S * n_new <= kOneCta)
+      for (int i = tid; i < c.S * n_new; i += N) slots[i] = -1;
     return;
   }
-  // pages go back before any are taken
-  for (int pass = 0; pass < 2; ++pass) {
-    long long done = 0;
-    for (int k = 0; k < spans; ++k) {
-      const Change x = change_of(c, want, k * kPlan + tid, n_new);
-      long long all;
-      s_start[tid] = (int)scan(pass ? x.take() : x.back(), s_warp, &all);
-      s_page[tid] = pass ? x.have : x.need;
+  Sums before{};
+  for (int k = 0; k < spans; ++k) {
+    if (spans > 1) sums(k);
+    const int s = k * N + tid;
+    if (all.back > 0) {
+      s_start[tid] = at.back;
+      s_page[tid] = x.need;
+      s_many[tid] = x.back();
       __syncthreads();
-      for (int e = tid; e < all; e += kPlan) {
-        const int i = find(s_start, e);
-        int32_t *entry = c.table + (long long)(k * kPlan + i) * c.tstride + s_page[i] +
-                         (e - s_start[i]);
-        const long long at = top - 1 - (done + e);
-        if (at < 0 || at >= c.n_pages) continue;
-        if (pass)
-          *entry = c.stack[at];
-        else
-          c.stack[at] = *entry, *entry = -1;
+      auto give = [&](int i, int e) {
+        int32_t *entry = c.table + (long long)(k * N + i) * c.tstride + s_page[i] + e;
+        const long long to = top - 1 - (before.back + s_start[i] + e);
+        if (to >= 0 && to < c.n_pages) c.stack[to] = *entry;
+        *entry = -1;
+      };
+      if (c.S >= N / 32) {  // a warp a sequence
+        for (int i = tid >> 5; i < min(N, c.S - k * N); i += N / 32) {
+          const int many = s_many[i];
+#pragma unroll 4
+          for (int e = tid & 31; e < many; e += 32) give(i, e);
+        }
+      } else {  // few sequences: each page looks for its own
+#pragma unroll 4
+        for (int e = tid; e < all.back; e += N) {
+          const int i = find<N>(s_start, e);
+          give(i, e - s_start[i]);
+        }
       }
-      done += all;
       __syncthreads();
     }
-  }
-  long long before = 0;
-  for (int k = 0; k < spans; ++k) {
-    const int s = k * kPlan + tid;
-    const Change x = change_of(c, want, s, n_new);
-    long long all;
-    const long long at = before + scan((x.want + kTile - 1) / kTile, s_warp, &all);
-    before += all;
     if (s < c.S) {
+      const Sums mine = before + at;
       c.len[s] = x.want;
       c.from[s] = min(x.old, x.want);
-      c.tiles[s] = (int)at;
-      if (s == c.S - 1) c.tiles[c.S] = (int)before;
+      c.first[s] = (int)(top - 1 - mine.take);
+      c.tiles[s] = mine.tiles;
+      if (s == c.S - 1) c.tiles[c.S] = total.tiles;
+    }
+    before = before + all;
+  }
+  if (tid == 0) c.free[0] = (int)(top - total.take), c.free[1] = 1;
+  if (!slots || (long long)c.S * n_new > kOneCta) return;
+  __syncthreads();
+  for (int i = tid; i < c.S * n_new; i += N) {
+    const int s = i / n_new;
+    slots[i] = place(c, s, i - s * n_new, c.from[s], c.len[s], c.first[s]);
+  }
+}
+
+__global__ void __launch_bounds__(kFill) fill_kernel(const __grid_constant__ View c, int n_new,
+                                                     int32_t *slots) {
+  kvr::pdl_begin();
+  const bool done = c.free[1] != 0;
+  for (int s = blockIdx.y; s < c.S; s += gridDim.y) {
+    const int from = c.from[s], len = c.len[s], first = c.first[s];
+    int32_t *to = slots + (long long)s * n_new;
+    const int t0 = blockIdx.x * kFillTokens;
+#pragma unroll
+    for (int i = 0; i < kFillTokens / kFill; ++i) {
+      const int t = t0 + i * kFill + threadIdx.x;
+      if (t < n_new) to[t] = done ? place(c, s, t, from, len, first) : -1;
     }
   }
-  if (tid == 0) c.free[0] = (int)(top - take), c.free[1] = 1;
-  __syncthreads();
-  if (slots)
-    for (long long i = tid; i < (long long)c.S * n_new; i += kPlan) {
-      const int s = (int)(i / n_new), t = (int)(i % n_new);
-      slots[i] = slot_of(c, slots, s, t, c.from[s], c.len[s]);
-    }
 }
 
 // ---- append -----------------------------------------------------------------
@@ -333,7 +384,7 @@ cudaStream_t as_stream(void *s) { return static_cast<cudaStream_t>(s); }
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 struct Layout {
-  size_t K, V, bounds, table, len, from, tiles, stack, free, ticket, err, total;
+  size_t K, V, bounds, table, len, from, first, tiles, stack, free, ticket, err, total;
 };
 
 bool layout_of(const kvr_paged_desc *d, Layout *l) {
@@ -345,13 +396,15 @@ bool layout_of(const kvr_paged_desc *d, Layout *l) {
       (long long)d->table_pages * d->page_rows > INT_MAX ||
       (long long)d->n_layers * d->n_kv_heads > 65535 ||
       (long long)d->n_layers * d->n_kv_heads * d->n_seq >= INT_MAX ||
+      // tiles are counted in 32 bits (2^31 of them are 8 TB of keys and values)
+      (long long)d->n_layers * d->n_kv_heads * d->n_pages >
+          INT_MAX / (d->page_rows / kvr::paged::kTile) ||
       (d->kv_dtype != KVR_BF16 && d->kv_dtype != KVR_F32) ||
       (d->out_dtype != KVR_BF16 && d->out_dtype != KVR_F32) ||
       !(d->softmax_scale >= 0.f && std::isfinite(d->softmax_scale)))
     return false;
   const size_t es = d->kv_dtype == KVR_BF16 ? 2 : 4;
   const size_t units = (size_t)d->n_layers * d->n_pages * d->n_kv_heads, row = d->head_dim * es;
-  // (65,535 units of 2^31 rows of 512 bytes stay below 2^63)
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -364,6 +417,7 @@ bool layout_of(const kvr_paged_desc *d, Layout *l) {
   l->table = take((size_t)d->n_seq * d->table_pages * 4);
   l->len = take((size_t)d->n_seq * 4);
   l->from = take((size_t)d->n_seq * 4);
+  l->first = take((size_t)d->n_seq * 4);
   l->tiles = take(((size_t)d->n_seq + 1) * 4);
   l->stack = take((size_t)d->n_pages * 4);
   l->free = take(2 * 4);
@@ -458,6 +512,7 @@ kvr_status kvr_paged_create(const kvr_paged_desc *desc, void *dev_buf, size_t by
   v.table = i32(l.table);
   v.len = i32(l.len);
   v.from = i32(l.from);
+  v.first = i32(l.first);
   v.tiles = i32(l.tiles);
   v.stack = i32(l.stack);
   v.free = i32(l.free);
@@ -506,11 +561,25 @@ kvr_status kvr_paged_plan(kvr_paged *c, const int32_t *lens, int n_new, int32_t 
   if (n_new < 0 || n_new > (1 << 24)) return fail(KVR_EINVAL, "%d new tokens", n_new);
   if ((n_new > 0) != (slots != nullptr))
     return fail(KVR_EINVAL, "slots go with new tokens: %d of them", n_new);
-  const cudaError_t e =
-      kvr::launch_pdl(kvr::paged::plan_kernel, dim3(1), dim3(kvr::paged::kPlan), 0,
-                      as_stream(stream), c->view, lens, n_new, slots);
+  const View &w = c->view;
+  const cudaStream_t cs = as_stream(stream);
+  const long long many = (long long)w.S * n_new;
+  cudaError_t e =
+      w.S <= kvr::paged::kPlanFew && (many <= 4096 || many > kvr::paged::kOneCta)
+          ? kvr::launch_pdl(kvr::paged::plan_kernel<kvr::paged::kPlanFew>, dim3(1),
+                            dim3(kvr::paged::kPlanFew), 0, cs, w, lens, n_new, slots)
+          : kvr::launch_pdl(kvr::paged::plan_kernel<kvr::paged::kPlan>, dim3(1),
+                            dim3(kvr::paged::kPlan), 0, cs, w, lens, n_new, slots);
   if (e != cudaSuccess) return cuda_fail("kvr_paged_plan", e);
   c->launches += 1;
+  if (many > kvr::paged::kOneCta) {
+    const dim3 grid((n_new + kvr::paged::kFillTokens - 1) / kvr::paged::kFillTokens,
+                    std::min(w.S, 65535));
+    e = kvr::launch_pdl(kvr::paged::fill_kernel, grid, dim3(kvr::paged::kFill), 0, cs, w, n_new,
+                        slots);
+    if (e != cudaSuccess) return cuda_fail("kvr_paged_plan: slots", e);
+    c->launches += 1;
+  }
   return KVR_OK;
 }
 

@@ -20,6 +20,7 @@ struct View {
   int32_t *table;    // [S][tstride], -1 behind a sequence's pages
   int32_t *len;      // [S]
   int32_t *from;     // [S] rows that the last plan kept: its new tokens follow them
+  int32_t *first;    // [S] where in the stack the last plan's new pages of s begin
   int32_t *tiles;    // [S + 1] tiles of the sequences before s
   int32_t *stack;    // [n_pages] free pages, the next one to go at free[0] - 1
   int32_t *free;     // [0]: how many; [1]: whether the last plan was carried out

@@ -340,10 +340,11 @@ struct Place {
   int s, u, tile, n, rows;  // unit u of the sequence's nl * H; its tiles and rows
 };
 
-// A piece of a unit: tiles [first, first + count) of the n of unit `unit`.
+// A piece of a unit: tiles [first, upto) of the n of unit `unit`, whose first is tile
+// `begin` of the call.
 struct Piece {
-  long long unit;
-  int first, count, n;
+  int unit, first, upto, n;
+  unsigned begin;
 };
 
 template <typename T, int D, typename P, typename O>
@@ -351,91 +352,96 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
   kvr::pdl_begin();
   using S = Shape<T, D>;
   constexpr int kWarps = P::kWarps, kStages = P::kStages, kPart = part_floats(D);
+  constexpr int kThreads = kWarps * 32, kStats = kHeads * D;
   static_assert(kStages * S::kStage >= kPart * 4, "a warp's last piece takes its copies' place");
-  static_assert(kWarps * kStages * S::kStage >= kHeads * (kMaxCtas + 1) * 4,
-                "the weights of a unit's parts");
+  static_assert(kWarps * kStages * S::kStage >= kHeads * kMaxCtas * 4, "logits of a unit's parts");
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Piece s_piece[2 * kWarps];
   __shared__ int s_last[2];
+  __shared__ float2 s_stat[kWarps][kHeads];
   const View &c = p.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // All that is known of sequences is asked for at once: the end of the list, and a
+  // first probe of where sequences start in it.
+  const int stride = (c.S + 31) / 32;
+  const unsigned tiles = p.src.tiles[c.S];
+  const unsigned probe = p.src.tiles[min(lane * stride, c.S)];
+  const int probe_rows = p.src.rows[min(lane, c.S - 1)];
   uint8_t *ring = smem + warp * (kStages * S::kStage);
   float *early = reinterpret_cast<float *>(smem + kWarps * kStages * S::kStage) + warp * kPart;
   uint8_t *own = smem + kWarps * (kStages * S::kStage + kPart * 4) + warp * P::kOwn;
   const uint32_t ring32 = smem_u32(ring);
-  const int U = p.nl * c.H;  // units of a sequence
-  const long long total = (long long)p.src.tiles[c.S] * U;
-  const long long warps = (long long)gridDim.x * kWarps;
-  const long long span = max((long long)kLeast, (total + warps - 1) / warps);
-  const long long cta_span = span * kWarps;
-  const long long t0 = min(total, ((long long)blockIdx.x * kWarps + warp) * span);
-  const long long t1 = min(total, t0 + span);
+  const unsigned U = p.nl * c.H;  // units of a sequence
+  const unsigned total = tiles * U, warps = gridDim.x * kWarps;
+  const unsigned span = max((unsigned)kLeast, (total + warps - 1) / warps);
+  const unsigned t0 = min(total, (blockIdx.x * kWarps + warp) * span), t1 = min(total, t0 + span);
 
-  // sequences without rows: zeros
-  for (int s = blockIdx.x; s < c.S; s += gridDim.x) {
-    if (p.src.tiles[s + 1] != p.src.tiles[s]) continue;
-    uint4 *o = reinterpret_cast<uint4 *>(static_cast<O *>(p.out) + (long long)s * U * c.G * D);
-    for (long long i = threadIdx.x; i < (long long)U * c.G * D * (int)sizeof(O) / 16;
-         i += kWarps * 32)
-      o[i] = make_uint4(0, 0, 0, 0);
-  }
-
-  auto locate = [&](long long t) {
-    // the last sequence that starts at or before t (32 of them asked at a time)
-    const int key = (int)(t / U);
-    int lo = 0, hi = c.S;
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-      const unsigned in = __ballot_sync(0xffffffffu, at < hi && p.src.tiles[at] <= key);
-      lo += (__popc(in) - 1) * step;
-      hi = min(hi, lo + step);
-    }
+  auto locate = [&](unsigned t) {
+    // the last sequence that starts at or before t, 32 of them asked at a time
+    const unsigned key = t / U;
+    const int m = __popc(__ballot_sync(0xffffffffu, lane * stride < c.S && probe <= key)) - 1;
     Place x;
-    x.s = lo;
-    const int base = p.src.tiles[lo];
-    x.n = p.src.tiles[lo + 1] - base;
-    x.rows = p.src.rows[lo];
-    const long long off = t - (long long)base * U;
-    x.u = (int)(off / x.n);
-    x.tile = (int)(off - (long long)x.u * x.n);
+    x.s = m * stride;
+    unsigned base = __shfl_sync(0xffffffffu, probe, m), next;
+    if (stride == 1) {
+      next = __shfl_sync(0xffffffffu, probe, (m + 1) & 31);
+      if (m + 1 >= c.S) next = tiles;
+      x.rows = __shfl_sync(0xffffffffu, probe_rows, m);
+    } else {
+      int hi = min(c.S, x.s + stride);
+      while (hi - x.s > 1) {
+        const int step = (hi - x.s + 31) / 32, at = x.s + lane * step;
+        const unsigned in =
+            __ballot_sync(0xffffffffu, at < hi && (unsigned)p.src.tiles[at] <= key);
+        x.s += (__popc(in) - 1) * step;
+        hi = min(hi, x.s + step);
+      }
+      base = p.src.tiles[x.s];
+      next = p.src.tiles[x.s + 1];
+      x.rows = p.src.rows[x.s];
+    }
+    x.n = next - base;
+    const unsigned off = t - base * U;
+    x.u = off / (unsigned)x.n;
+    x.tile = off - x.u * x.n;
     return x;
   };
   auto page_of = [&](const Place &x) {
     return p.src.pages[x.s * p.src.seq_stride + x.u * p.src.unit_stride +
-                       ((long long)x.tile * kTile >> c.psh)];
+                       (x.tile * kTile >> c.psh)];
   };
-  auto advance = [&](Place &x, long long next) {
+  auto advance = [&](Place &x, unsigned next) {
     if (++x.tile < x.n) return;
-    if (x.u + 1 < U)
+    if (x.u + 1 < (int)U)
       x.tile = 0, x.u += 1;
     else if (next < t1)
       x = locate(next);
   };
 
-  Place at{}, ahead{};
-  long long issued = t0;
-  int page = 0;
+  Place ahead{};
+  unsigned issued = t0;
+  int page = 0, to = 0;  // to: the stage that the next copies go to
   bool bad_page = false;
   auto issue = [&]() {
     if (issued < t1) {
-      const uint32_t dst = ring32 + (uint32_t)((issued - t0) % kStages) * S::kStage;
+      const uint32_t dst = ring32 + (uint32_t)to * S::kStage;
       const bool there = (unsigned)page < (unsigned)c.n_pages;
       bad_page |= !there;
       const int row = ahead.tile * kTile, limit = there ? ahead.rows - row : 0;
       const int lr = ahead.u / c.H, h = ahead.u - lr * c.H;
       const long long from =
-          (pool_row(c, p.lb + lr, there ? page : 0, h) + (row & (c.P - 1))) * S::kRow;
+          (pool_row(c, p.lb + lr, there ? page : 0, h) + (row & (c.P - 1))) * S::kRow + lane * 16;
 #pragma unroll
       for (int x = 0; x < S::kPer; ++x) {
         const int r = (x * 32 + lane) / S::kVecs, v = lane % S::kVecs;
-        copy16(dst + P::k_at(r, v), c.K + from + (x * 32 + lane) * 16, r < limit ? 16 : 0);
+        copy16(dst + P::k_at(r, v), c.K + from + x * 512, r < limit ? 16 : 0);
       }
 #pragma unroll
       for (int x = 0; x < S::kPer; ++x) {
         const int r = (x * 32 + lane) / S::kVecs, v = lane % S::kVecs;
-        copy16(dst + S::kPer * 512 + P::v_at(r, v), c.V + from + (x * 32 + lane) * 16,
-               r < limit ? 16 : 0);
+        copy16(dst + S::kPer * 512 + P::v_at(r, v), c.V + from + x * 512, r < limit ? 16 : 0);
       }
+      to = to + 1 == kStages ? 0 : to + 1;
       ++issued;
       advance(ahead, issued);
       if (issued < t1) page = page_of(ahead);
@@ -445,221 +451,245 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
 
   P work;
   work.init(own, c.scale * kLog2e);
-  if (lane < 2) s_piece[2 * warp + lane] = Piece{-1, 0, 0, 0};
+  if (lane < 2) s_piece[2 * warp + lane] = Piece{-1, 0, 0, 0, 0};
   __syncwarp();
   bool infinite = false;
-  auto out_of = [&](long long unit) {
-    return static_cast<O *>(p.out) + unit * c.G * D;
+  auto out_of = [&](int unit) { return static_cast<O *>(p.out) + (long long)unit * c.G * D; };
+  // Four channels of a head, normalised.
+  auto put = [&](O *o, float4 v, float s) {
+    const float r = 1.f / s;
+    infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
+    put4(o, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
   };
+  // (one copy of everything below: a call of a few tiles spends its time on fetching
+  // instructions)
   if (t0 < t1) {
-    at = ahead = locate(t0);
+    Place at = locate(t0);
+    ahead = at;
     page = page_of(ahead);
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) issue();
-    int first = at.tile;
-    work.start(static_cast<const T *>(p.q) + ((long long)at.s * U + at.u) * c.G * D, c.G, lane);
-    for (long long t = t0; t < t1; ++t) {
-      copies_wait<kStages - 2>();
-      __syncwarp();
-      issue();  // where tile t - 1 was, which the warp has read
-      work.step(reinterpret_cast<const uint4 *>(ring + (uint32_t)((t - t0) % kStages) * S::kStage),
+    int first = at.tile, stage = 0;
+    bool fresh = true;
+#pragma unroll 1
+    for (int k = 1 - kStages; t0 + k != t1; ++k) {
+      if (k >= 0) {
+        if (fresh) {
+          work.start(static_cast<const T *>(p.q) + ((long long)at.s * U + at.u) * c.G * D, c.G,
+                     lane);
+          fresh = false;
+        }
+        copies_wait<kStages - 2>();
+        __syncwarp();
+      }
+      issue();  // where tile k - 1 was, which the warp has read
+      if (k < 0) continue;
+      work.step(reinterpret_cast<const uint4 *>(ring + (uint32_t)stage * S::kStage),
                 at.rows - at.tile * kTile, lane);
-      const bool last = t + 1 == t1;
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+      const bool last = t0 + k + 1 == t1;
       if (at.tile + 1 < at.n && !last) {
         ++at.tile;
         continue;
       }
-      const long long unit = (long long)at.s * U + at.u;
-      if (first == 0 && at.tile + 1 == at.n) {
-        O *o = out_of(unit);
-        work.finish(lane, [&](int g, int ch, float4 v, float, float s) {
-          if (g >= c.G) return;
-          const float r = 1.f / s;
-          infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
-          put4(o + g * D + ch, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-        });
-      } else {
-        // a warp's first piece beside its copies, its last one in their place
-        if (lane == 0)
-          s_piece[2 * warp + last] = Piece{unit, first, at.tile + 1 - first, at.n};
-        if (last) {
-          copies_wait<0>();
-          __syncwarp();
-        }
-        float *dst = last ? reinterpret_cast<float *>(ring) : early;
-        work.finish(lane, [&](int g, int ch, float4 v, float m, float s) {
-          put4(dst + g * D + ch, v);
-          if (ch == 0) dst[kHeads * D + g] = m, dst[kHeads * D + kHeads + g] = s;
-        });
+      const int unit = at.s * U + at.u;
+      const bool whole = first == 0 && at.tile + 1 == at.n;
+      // a warp's first piece goes beside its copies, its last one takes their place
+      if (last) {
+        copies_wait<0>();
+        __syncwarp();
       }
+      float *dst = last ? reinterpret_cast<float *>(ring) : early;
+      if (!whole && lane == 0)
+        s_piece[2 * warp + last] = Piece{unit, first, at.tile + 1, at.n, t0 + k - at.tile};
+      O *o = out_of(unit);
+      work.finish(lane, [&](int g, int ch, float4 v, float m, float s) {
+        if (!whole) {
+          put4(dst + g * D + ch, v);
+          if (ch == 0) reinterpret_cast<float2 *>(dst + kStats)[g] = make_float2(m, s);
+        } else if (g < c.G) {
+          put(o + g * D + ch, v, s);
+        }
+      });
       if (!last) {
-        advance(at, t + 1);
+        advance(at, t0 + k + 1);
         first = 0;
-        work.start(static_cast<const T *>(p.q) + ((long long)at.s * U + at.u) * c.G * D, c.G,
-                   lane);
+        fresh = true;
       }
     }
   }
   copies_wait<0>();
   __syncthreads();
 
-  // Join the pieces that lie side by side.  Thread x owns 4 channels of a head.
+  // Join the pieces that lie side by side.  A thread owns 4 channels of a head, or of
+  // kMine heads.
   auto piece_at = [&](int i) {
     return reinterpret_cast<const float *>(
         (i & 1) ? smem + (i >> 1) * (kStages * S::kStage)
                 : smem + kWarps * kStages * S::kStage + (i >> 1) * kPart * 4);
   };
-  constexpr int kMine = kHeads * D / 4 / (kWarps * 32) > 0 ? kHeads * D / 4 / (kWarps * 32) : 1;
-  const bool busy = (int)threadIdx.x < kHeads * D / 4;
+  constexpr int kMine = (kHeads * D / 4 + kThreads - 1) / kThreads;
+  static_assert(kHeads * D / 4 % kThreads == 0, "all threads own the same");
   if (threadIdx.x < 2) s_last[threadIdx.x] = 0;
-  long long owed[2] = {-1, -1};  // units that go on in other CTAs: before, behind
-  int owed_first[2], owed_n[2];
-  for (int i = 0; i < 2 * kWarps;) {
-    const Piece a = s_piece[i];
-    if (a.unit < 0) {
-      ++i;
-      continue;
-    }
-    int end = i, upto = 0;
-    for (int k = i; k < 2 * kWarps; ++k)
-      if (s_piece[k].unit == a.unit)
-        end = k + 1, upto = s_piece[k].first + s_piece[k].count;
-      else if (s_piece[k].unit >= 0)
-        break;
-    const bool whole = a.first == 0 && upto == a.n;
-    const int which = a.first == 0 ? 1 : 0;
+  Piece mine{-1, 0, 0, 0, 0};
+  if (lane < 2 * kWarps) mine = s_piece[lane];
+  int owed[2] = {-1, -1}, owed_n[2] = {0, 0};  // units that go on in CTAs before, behind
+  unsigned owed_begin[2] = {0, 0};
+#pragma unroll 1
+  for (unsigned left = __ballot_sync(0xffffffffu, mine.unit >= 0); left;) {
+    const int i = __ffs(left) - 1, unit = __shfl_sync(0xffffffffu, mine.unit, i);
+    const unsigned same = __ballot_sync(0xffffffffu, mine.unit == unit);
+    left &= ~same;
+    const int n = __shfl_sync(0xffffffffu, mine.n, i);
+    const int first = __shfl_sync(0xffffffffu, mine.first, i);
+    const unsigned begin = __shfl_sync(0xffffffffu, mine.begin, i);
+    const int upto = __shfl_sync(0xffffffffu, mine.upto, 31 - __clz(same));
+    const bool whole = first == 0 && upto == n;
+    const int which = first == 0;
     float *part = p.parts + (2ll * blockIdx.x + which) * kPart;
-    if (busy)
 #pragma unroll
-      for (int y = 0; y < kMine; ++y) {
-        const int x = threadIdx.x + y * kWarps * 32, g = x / (D / 4);
-        float m = -INFINITY;
-        for (int k = i; k < end; ++k)
-          if (s_piece[k].unit >= 0) m = fmaxf(m, piece_at(k)[kHeads * D + g]);
-        const float ref = m == -INFINITY ? 0.f : m;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        float s = 0.f;
-        for (int k = i; k < end; ++k) {
-          if (s_piece[k].unit < 0) continue;
-          const float *from = piece_at(k);
-          const float a = ex2(from[kHeads * D + g] - ref);
-          const float4 w = reinterpret_cast<const float4 *>(from)[x];
-          v.x = fmaf(w.x, a, v.x), v.y = fmaf(w.y, a, v.y);
-          v.z = fmaf(w.z, a, v.z), v.w = fmaf(w.w, a, v.w);
-          s = fmaf(from[kHeads * D + kHeads + g], a, s);
-        }
-        if (!whole) {
-          put4(part + 4 * x, v);
-          if (x % (D / 4) == 0) part[kHeads * D + g] = m, part[kHeads * D + kHeads + g] = s;
-        } else if (g < c.G) {
-          const float r = 1.f / s;
-          infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
-          put4(out_of(a.unit) + 4 * x, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-        }
+    for (int y = 0; y < kMine; ++y) {
+      const int x = threadIdx.x + y * kThreads, g = x / (D / 4);
+      float m = -INFINITY;
+      for (unsigned k = same; k; k &= k - 1)
+        m = fmaxf(m, piece_at(__ffs(k) - 1)[kStats + 2 * g]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      float s = 0.f;
+      for (unsigned k = same; k; k &= k - 1) {
+        const float *from = piece_at(__ffs(k) - 1);
+        const float2 ms = reinterpret_cast<const float2 *>(from + kStats)[g];
+        const float a = ex2(ms.x - ref);
+        const float4 w = reinterpret_cast<const float4 *>(from)[x];
+        v.x = fmaf(w.x, a, v.x), v.y = fmaf(w.y, a, v.y);
+        v.z = fmaf(w.z, a, v.z), v.w = fmaf(w.w, a, v.w);
+        s = fmaf(ms.y, a, s);
       }
+      if (!whole) {
+        put4(part + 4 * x, v);
+        if (x % (D / 4) == 0) reinterpret_cast<float2 *>(part + kStats)[g] = make_float2(m, s);
+      } else if (g < c.G) {
+        put(out_of(unit) + 4 * x, v, s);
+      }
+    }
     if (!whole) {
-      owed[which] = a.unit;
-      owed_first[which] = a.first;
-      owed_n[which] = a.n;
+      // (no dynamic index: which is 0 or 1)
+      owed[0] = which ? owed[0] : unit, owed[1] = which ? unit : owed[1];
+      owed_n[0] = which ? owed_n[0] : n, owed_n[1] = which ? n : owed_n[1];
+      owed_begin[0] = which ? owed_begin[0] : begin, owed_begin[1] = which ? begin : owed_begin[1];
     }
-    i = end;
   }
-  if (bad_page && lane == 0) atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
   if (owed[0] >= 0 || owed[1] >= 0) {
-    // position of the unit's first tile, and with it the CTAs that share it
-    long long from[2], upto[2];
+    // CTAs that share the unit: the first has its part behind, the others before
+    unsigned from[2], many[2];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      if (owed[w] < 0) continue;
-      const int s = (int)(owed[w] / U);
-      const long long begin = (long long)p.src.tiles[s] * U + (owed[w] - (long long)s * U) * owed_n[w];
-      from[w] = begin / cta_span;
-      upto[w] = (begin + owed_n[w] - 1) / cta_span;
+      from[w] = owed_begin[w] / (span * kWarps);
+      many[w] = (owed_begin[w] + owed_n[w] - 1) / (span * kWarps) - from[w] + 1;
     }
     __syncthreads();
-    if (threadIdx.x < 2 && owed[threadIdx.x] >= 0) {
+    if (threadIdx.x < 2) {
       const int w = threadIdx.x;
-      // (the barrier and this fence order every thread's part before the arrival)
-      __threadfence();
-      const unsigned there = (unsigned)(upto[w] - from[w]);
-      if (atomicAdd(c.ticket + from[w], 1u) == there) {
-        c.ticket[from[w]] = 0;
-        s_last[w] = 1;
+      if ((w ? owed[1] : owed[0]) >= 0) {
+        unsigned *ticket = c.ticket + (w ? from[1] : from[0]);
+        // (the barrier and this fence order every thread's part before the arrival)
+        __threadfence();
+        if (atomicAdd(ticket, 1u) == (w ? many[1] : many[0]) - 1) {
+          *ticket = 0;
+          s_last[w] = 1;
+        }
+        __threadfence();
       }
-      __threadfence();
     }
     __syncthreads();
-    // Shared memory is free now: the weights of all parts there, while the first
-    // parts' values are on their way.
-    float *weight = reinterpret_cast<float *>(smem), *sum = weight + kHeads * kMaxCtas;
+    // Shared memory is free now, for the greatest logits of all parts.
+    float *logit = reinterpret_cast<float *>(smem);
     constexpr int kAhead = 8;
-#pragma unroll
+#pragma unroll 1
     for (int w = 0; w < 2; ++w) {
-      if (owed[w] < 0 || !s_last[w]) continue;
-      const int many = (int)(upto[w] - from[w]) + 1;
-      auto part = [&](int k) { return p.parts + (2 * (from[w] + k) + (k == 0)) * kPart; };
+      if (!s_last[w]) continue;
+      const int N = w ? many[1] : many[0], first = w ? from[1] : from[0];
+      auto part = [&](int k) { return p.parts + (2ll * (first + k) + (k == 0)) * kPart; };
+      // values of the first parts are on their way meanwhile
       float4 z[kMine][kAhead];
       auto fetch = [&](int k0) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
 #pragma unroll
           for (int y = 0; y < kMine; ++y)
-            if (busy && k0 + k < many)
+            if (k0 + k < N)
               z[y][k] = __ldcg(reinterpret_cast<const float4 *>(part(k0 + k)) + threadIdx.x +
-                               y * kWarps * 32);
+                               y * kThreads);
       };
       fetch(0);
-      __syncthreads();
-      for (int g = warp; g < c.G; g += kWarps) {
-        float m = -INFINITY;
-        for (int k = lane; k < many; k += 32) {
-          const float x = __ldcg(part(k) + kHeads * D + g);
-          weight[g * kMaxCtas + k] = x;
-          m = fmaxf(m, x);
+      {
+        const int g = lane & 7;
+        float m = -INFINITY, s = 0.f;
+        for (int k = threadIdx.x >> 3; k < N; k += kThreads / 8) {
+          const float2 ms = __ldcg(reinterpret_cast<const float2 *>(part(k) + kStats) + g);
+          logit[k * kHeads + g] = ms.x;
+          const float now = fmaxf(m, ms.x), ref = now == -INFINITY ? 0.f : now;
+          s = fmaf(s, ex2(m - ref), ms.y * ex2(ms.x - ref));
+          m = now;
         }
-        m = kvr::dev::warp_max(m);
-        const float ref = m == -INFINITY ? 0.f : m;
-        float s = 0.f;
-        for (int k = lane; k < many; k += 32) {
-          const float a = ex2(weight[g * kMaxCtas + k] - ref);
-          weight[g * kMaxCtas + k] = a;
-          s = fmaf(__ldcg(part(k) + kHeads * D + kHeads + g), a, s);
+#pragma unroll
+        for (int o = 8; o < 32; o <<= 1) {
+          const float m2 = __shfl_xor_sync(0xffffffffu, m, o);
+          const float s2 = __shfl_xor_sync(0xffffffffu, s, o);
+          const float now = fmaxf(m, m2), ref = now == -INFINITY ? 0.f : now;
+          s = s * ex2(m - ref) + s2 * ex2(m2 - ref);
+          m = now;
         }
-        s = kvr::dev::warp_sum(s);
-        if (lane == 0) sum[g] = s;
+        if (lane < kHeads) s_stat[warp][lane] = make_float2(m, s);
       }
       __syncthreads();
-      if (!busy) continue;
       float4 v[kMine];
+      float ref[kMine], sum[kMine];
 #pragma unroll
-      for (int y = 0; y < kMine; ++y) v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int y = 0; y < kMine; ++y) {
+        const int g = (threadIdx.x + y * kThreads) / (D / 4);
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) m = fmaxf(m, s_stat[i][g].x);
+        ref[y] = m == -INFINITY ? 0.f : m;
+        sum[y] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i)
+          sum[y] = fmaf(s_stat[i][g].y, ex2(s_stat[i][g].x - ref[y]), sum[y]);
+        v[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll 1
       for (int k0 = 0;;) {
 #pragma unroll
-        for (int y = 0; y < kMine; ++y) {
-          const int g = (threadIdx.x + y * kWarps * 32) / (D / 4);
+        for (int k = 0; k < kAhead; ++k) {
+          if (k0 + k >= N) break;
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            if (k0 + k >= many || g >= c.G) continue;
-            const float a = weight[g * kMaxCtas + k0 + k];
+          for (int y = 0; y < kMine; ++y) {
+            const int g = (threadIdx.x + y * kThreads) / (D / 4);
+            const float a = ex2(logit[(k0 + k) * kHeads + g] - ref[y]);
             v[y].x = fmaf(z[y][k].x, a, v[y].x), v[y].y = fmaf(z[y][k].y, a, v[y].y);
             v[y].z = fmaf(z[y][k].z, a, v[y].z), v[y].w = fmaf(z[y][k].w, a, v[y].w);
           }
         }
         k0 += kAhead;
-        if (k0 >= many) break;
+        if (k0 >= N) break;
         fetch(k0);
       }
 #pragma unroll
       for (int y = 0; y < kMine; ++y) {
-        const int x = threadIdx.x + y * kWarps * 32, g = x / (D / 4);
-        if (g >= c.G) continue;
-        const float s = sum[g], r = 1.f / s;
-        infinite |= !(fabsf(s) < INFINITY) || s == 0.f;
-        put4(out_of(owed[w]) + 4 * x,
-             make_float4(v[y].x * r, v[y].y * r, v[y].z * r, v[y].w * r));
+        const int x = threadIdx.x + y * kThreads, g = x / (D / 4);
+        if (g < c.G) put(out_of(w ? owed[1] : owed[0]) + 4 * x, v[y], sum[y]);
       }
+      __syncthreads();  // the logits are read
     }
   }
+
+  // sequences without rows: zeros
+  for (int s = blockIdx.x; s < c.S; s += gridDim.x) {
+    if (p.src.rows[s] > 0) continue;
+    uint4 *o = reinterpret_cast<uint4 *>(out_of(s * U));
+    for (int i = threadIdx.x; i < (int)U * c.G * D * (int)sizeof(O) / 16; i += kThreads)
+      o[i] = make_uint4(0, 0, 0, 0);
+  }
+  if (bad_page && lane == 0) atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
   if (infinite) atomicOr(c.err, (unsigned)kvr::ERR_NONFINITE);
 }
 

@@ -19,6 +19,7 @@
 
 #include "kvr_device.cuh"
 #include "kvr_internal.h"
+#include "kvr_ptx.cuh"
 
 namespace kvr {
 namespace paged {
@@ -110,6 +111,124 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
   }
 }
 
+// 32 bytes of a lane, so that the four lanes of a row ask for whole lines.
+struct Words {
+  uint32_t w[8];
+};
+__device__ __forceinline__ Words ld32(const void *p) {
+  Words r;
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]),
+                 "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+               : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// bf16 on tensor cores: 16 pages a warp against the 8 query heads, the positive part
+// of q with the greatest keys and the negative part with the least.  A third product,
+// |q| with max(|least|, |greatest|), says how large the terms of the sums are.
+template <int D>
+__global__ void __launch_bounds__(kThreads) score_mma_kernel(const __grid_constant__ SelectParams p) {
+  kvr::pdl_begin();
+  constexpr int kX = D / 64;  // 32-byte pieces of a lane in a row
+  const View &c = p.c;
+  const int lane = threadIdx.x & 31, row = lane >> 2, j = lane & 3;
+  const int groups = (c.tstride + 15) / 16;
+  const long long items = (long long)c.S * p.nl * c.H * groups;
+  const uint8_t *qs = static_cast<const uint8_t *>(p.q);
+  for (long long it = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); it < items;
+       it += (long long)gridDim.x * kWarps) {
+    const long long unit = it / groups;
+    const int first = (int)(it - unit * groups) * 16;
+    const int s = (int)(unit / ((long long)p.nl * c.H)), u = (int)(unit - (long long)s * p.nl * c.H);
+    const int lr = u / c.H, h = u - lr * c.H;
+    const int have = pages_of(c, s), end = have - p.window;
+    if (have <= p.budget + p.window || first >= end) continue;
+    const int32_t *table = c.table + (long long)s * c.tstride + first;
+    Words lo[2][kX], hi[2][kX];
+    bool there[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int at = row + 8 * r;
+      const int page = table[first + at < end ? at : 0];
+      there[r] = (unsigned)page < (unsigned)c.n_pages;
+      const uint8_t *b = c.bounds +
+                         (((long long)(p.lb + lr) * c.n_pages + (there[r] ? page : 0)) * c.H + h) *
+                             (4 * D) +
+                         j * 32;
+#pragma unroll
+      for (int x = 0; x < kX; ++x) {
+        lo[r][x] = ld32(b + x * 128);
+        hi[r][x] = ld32(b + 2 * D + x * 128);
+      }
+    }
+    float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f}, size[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < kX; ++x) {
+      Words q{};
+      if (row < c.G) {  // (16-byte aligned, no more)
+        const uint4 *at = reinterpret_cast<const uint4 *>(qs + ((unit * c.G + row) * D) * 2 +
+                                                          j * 32 + x * 128);
+        const uint4 a = __ldg(at), b = __ldg(at + 1);
+        q = Words{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t pos[2], neg[2], mag[2], big[2][2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t w = q.w[2 * i + y];
+          const uint32_t below = ((w & 0x8000u) ? 0xFFFFu : 0u) | ((w >> 31) ? 0xFFFF0000u : 0u);
+          pos[y] = w & ~below;
+          neg[y] = w & below;
+          mag[y] = w & 0x7FFF7FFFu;
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            big[r][y] = max2(lo[r][x].w[2 * i + y] & 0x7FFF7FFFu, hi[r][x].w[2 * i + y] & 0x7FFF7FFFu);
+        }
+        kvr::ptx::mma_bf16(up, hi[0][x].w[2 * i], hi[1][x].w[2 * i], hi[0][x].w[2 * i + 1],
+                           hi[1][x].w[2 * i + 1], pos[0], pos[1]);
+        kvr::ptx::mma_bf16(down, lo[0][x].w[2 * i], lo[1][x].w[2 * i], lo[0][x].w[2 * i + 1],
+                           lo[1][x].w[2 * i + 1], neg[0], neg[1]);
+        kvr::ptx::mma_bf16(size, big[0][0], big[1][0], big[0][1], big[1][1], mag[0], mag[1]);
+      }
+    }
+    // pages row and row + 8, heads 2 j and 2 j + 1
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float score = -INFINITY, err = 0.f;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        if (2 * j + y < c.G) {
+          score = nan_max(score, up[2 * r + y] + down[2 * r + y]);
+          err = nan_max(err, size[2 * r + y]);
+        }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        score = nan_max(score, __shfl_xor_sync(0xffffffffu, score, o));
+        err = nan_max(err, __shfl_xor_sync(0xffffffffu, err, o));
+      }
+      const int at = first + row + 8 * r;
+      if (j == 0 && at < end) {
+        if (!there[r]) {
+          score = -INFINITY;
+          err = 0.f;
+          atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
+        }
+        // Of each of the D / 16 products of a chain, 17 terms may be cut at 2^-23 of
+        // the sum of magnitudes: 136 x 2^-23 of it for d = 128, the same again for
+        // the other chain and for the sum of magnitudes itself.
+        p.score[unit * c.tstride + at] = make_float2(score, fmaf(err, 0x1p-14f, 1e-37f));
+      }
+    }
+  }
+}
+
 __device__ __forceinline__ unsigned key32(float x) {
   return x != x ? 0xFFFFFFFFu : kvr::dev::ord_bits(x + 0.f);
 }
@@ -119,43 +238,72 @@ __device__ __forceinline__ unsigned long long key64(double x) {
   return (b >> 63) ? ~b : b | (1ull << 63);
 }
 
-// The need-th greatest of key(0 .. n - 1), bits * 8 wide; *left: how many equal to it
-// belong to the first `need`.
+// One warp: the digit (of 256, from the greatest) in which the need-th falls, and how
+// many of that digit are needed.
+__device__ __forceinline__ void digit_of(const unsigned *hist, int need, int lane, int *digit,
+                                         int *left) {
+  unsigned mine[8], sum = 0;  // lane 0 has the greatest digits
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    mine[i] = hist[255 - 8 * lane - i];
+    sum += mine[i];
+  }
+  unsigned upto = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  unsigned before = upto - sum;
+  if (before < (unsigned)need && upto >= (unsigned)need) {
+    int i = 0;
+    for (; i < 7 && before + mine[i] < (unsigned)need; ++i) before += mine[i];
+    *digit = 255 - 8 * lane - i;
+    *left = need - (int)before;
+  }
+}
+
+// The need-th greatest of key(0 .. n - 1), by digits of 8 bits from bit `top` down
+// (above it all keys are alike); *left: how many equal to it belong to the first
+// `need`.
 template <typename K, typename F>
-__device__ K nth(int n, int need, F key, unsigned *hist, K *s_prefix, int *s_need) {
+__device__ K nth(int n, int need, int top, F key, unsigned *hist, int *s_digit, int *s_left,
+                 int *left) {
+  const int lane = threadIdx.x & 31;
   K prefix = 0, mask = 0;
-  for (int shift = (int)sizeof(K) * 8 - 8; shift >= 0; shift -= 8) {
+  bool first = true;
+  for (int shift = top - 7; ; shift -= 8) {
+    const int low = max(shift, 0), width = shift + 8 - low;
     hist[threadIdx.x] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads) {
       const K k = key(i);
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1u);
+      if (first || ((k ^ prefix) & mask) == 0)
+        atomicAdd(&hist[(unsigned)(k >> low) & ((1u << width) - 1u)], 1u);
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      int seen = 0, d = 255;
-      for (; d > 0 && seen + (int)hist[d] < need; --d) seen += (int)hist[d];
-      *s_prefix = prefix | ((K)d << shift);
-      *s_need = need - seen;
-    }
+    if (threadIdx.x < 32) digit_of(hist, need, lane, s_digit, s_left);
     __syncthreads();
-    prefix = *s_prefix;
-    need = *s_need;
-    mask |= (K)0xFF << shift;
-    __syncthreads();
+    prefix |= (K)*s_digit << low;
+    mask |= ((K)((1u << width) - 1u)) << low;
+    need = *s_left;
+    first = false;
+    if (low == 0) break;
   }
+  *left = need;
   return prefix;
 }
+
+constexpr int kHeld = 8192;  // scores of a unit that are held on chip
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
   static_assert(kThreads == 256, "a thread a digit");
   __shared__ unsigned hist[256];
-  __shared__ unsigned s_key;
-  __shared__ unsigned long long s_key64;
-  __shared__ int s_need, s_base, s_warp[kWarps], s_count[2];
+  __shared__ int s_digit, s_left, s_warp[kWarps], s_ties[kWarps], s_count[2];
   __shared__ float s_err[kWarps];
+  __shared__ unsigned s_and[kWarps], s_or[kWarps], s_held[kHeld];
   const View &c = p.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int U = p.nl * c.H;
@@ -163,7 +311,6 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
   if (unit == (long long)c.S * U) {
     // what the attention reads of each sequence
     int before = 0;
-    if (tid == 0) s_base = 0;
     for (int s0 = 0; s0 < c.S; s0 += kThreads) {
       const int s = s0 + tid;
       int rows = 0;
@@ -211,45 +358,70 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
   }
   const int old = have - p.window, B = p.budget;
   float2 *sc = p.score + unit * c.tstride;
-  // pages from `top` up stay; of those between `top` and `low` the settled ones do
-  float top = INFINITY, low = INFINITY;
+  auto held = [&](int i) { return i < kHeld ? s_held[i] : key32(sc[i].x); };
+  // Keys from `top` up stay, those from `low` to it do if there is room for all of
+  // them; else 64-bit keys say which.
+  unsigned low = ~0u, top = ~0u;
   bool settle = false;
   unsigned long long cut = 0;  // settled: the last key that stays
   int equal = 0;               // and how many with that key do
+  unsigned long long *keys = reinterpret_cast<unsigned long long *>(sc);
   if (B > 0) {
     float err = 0.f;
-    for (int i = tid; i < old; i += kThreads) err = nan_max(err, sc[i].y);
+    unsigned both = ~0u, any = 0;
+    for (int i = tid; i < old; i += kThreads) {
+      const float2 x = sc[i];
+      const unsigned k = key32(x.x);
+      if (i < kHeld) s_held[i] = k;
+      err = nan_max(err, x.y);
+      both &= k, any |= k;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) err = nan_max(err, __shfl_xor_sync(0xffffffffu, err, o));
-    if (lane == 0) s_err[warp] = err;
+    both = __reduce_and_sync(0xffffffffu, both);
+    any = __reduce_or_sync(0xffffffffu, any);
+    if (lane == 0) s_err[warp] = err, s_and[warp] = both, s_or[warp] = any;
     if (tid < 2) s_count[tid] = 0;
-    const unsigned k = nth<unsigned>(old, B, [&](int i) { return key32(sc[i].x); }, hist, &s_key,
-                                     &s_need);
-    for (int w = 0; w < kWarps; ++w) err = nan_max(err, s_err[w]);
+    __syncthreads();
+    err = s_err[0], both = s_and[0], any = s_or[0];
+    for (int w = 1; w < kWarps; ++w) {
+      err = nan_max(err, s_err[w]);
+      both &= s_and[w], any |= s_or[w];
+    }
+    // bits above the first that differs are alike in all keys
+    const unsigned differ = both ^ any;
+    unsigned k = both;
+    if (differ) {
+      const int bit = 31 - __clz(differ);
+      int left;
+      const unsigned rest = bit == 31 ? ~0u : (1u << (bit + 1)) - 1u;
+      k = (both & ~rest) | nth<unsigned>(old, B, bit, [&](int i) { return held(i) & rest; }, hist,
+                                         &s_digit, &s_left, &left);
+    }
     const float t = __uint_as_float((k >> 31) ? k & 0x7FFFFFFFu : ~k);
+    const bool all = !(fabsf(t) < INFINITY && err < INFINITY);
     // twice the error on either side, rounded away from t
-    top = __fadd_ru(t, 2.f * err);
-    low = __fadd_rd(t, -2.f * err);
-    if (!(fabsf(t) < INFINITY && err < INFINITY)) top = INFINITY, low = -INFINITY;
-    const bool all = low == -INFINITY;
-    auto sure = [&](float x) { return !all && x > top; };
-    auto near = [&](float x) { return all || (x >= low && x <= top); };
+    top = all ? ~0u : key32(__fadd_ru(t, 2.f * err));
+    low = all ? 0u : key32(__fadd_rd(t, -2.f * err));
     int n_sure = 0, n_near = 0;
     for (int i = tid; i < old; i += kThreads) {
-      n_sure += sure(sc[i].x);
-      n_near += near(sc[i].x);
+      const unsigned x = held(i);
+      n_sure += !all && x > top;
+      n_near += all || (x >= low && x <= top);
     }
-    atomicAdd(&s_count[0], n_sure);
-    atomicAdd(&s_count[1], n_near);
+    n_sure = __reduce_add_sync(0xffffffffu, n_sure);
+    n_near = __reduce_add_sync(0xffffffffu, n_near);
+    if (lane == 0) atomicAdd(&s_count[0], n_sure), atomicAdd(&s_count[1], n_near);
     __syncthreads();
     settle = s_count[0] + s_count[1] != B;
     if (settle) {
       const T *q = static_cast<const T *>(p.q) + unit * c.G * D;
       for (int i0 = warp * 32; i0 < old; i0 += kThreads) {
         const int i = i0 + lane;
-        const float x = i < old ? sc[i].x : 0.f;
-        unsigned ask = __ballot_sync(0xffffffffu, i < old && near(x));
-        unsigned long long key = i < old && sure(x) ? ~0ull : 0ull;
+        const unsigned x = i < old ? held(i) : 0u;
+        const bool sure = i < old && !all && x > top;
+        unsigned ask = __ballot_sync(0xffffffffu, i < old && (all || (x >= low && x <= top)));
+        unsigned long long key = sure ? ~0ull : 0ull;
         while (ask) {
           const int at = __ffs(ask) - 1;
           ask &= ask - 1;
@@ -268,67 +440,74 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
           }
           if (lane == at) key = best;
         }
-        if (i < old) reinterpret_cast<unsigned long long *>(sc)[i] = key;
+        if (i < old) keys[i] = key;
       }
       __syncthreads();
-      const unsigned long long *keys = reinterpret_cast<const unsigned long long *>(sc);
-      cut = nth<unsigned long long>(old, B, [&](int i) { return keys[i]; }, hist, &s_key64,
-                                    &s_need);
-      equal = s_need;
+      // no bounds of a page: key 0, below every score's
+      cut = nth<unsigned long long>(old, B, 63, [&](int i) { return keys[i]; }, hist, &s_digit,
+                                    &s_left, &equal);
     }
   }
-  // the pages that stay, in order
-  if (tid == 0) s_base = 0, s_count[0] = 0;
-  __syncthreads();
-  for (int i0 = 0; i0 < have; i0 += kThreads) {
-    const int i = i0 + tid;
-    bool keep = false, tie = false;
-    if (i >= old) {
-      keep = i < have;
-    } else if (settle) {
-      const unsigned long long k = reinterpret_cast<const unsigned long long *>(sc)[i];
-      keep = k > cut;
+  // The pages that stay, in order: a warp goes through an equal part of them, once to
+  // count and once to write.
+  const int part = ((have + kWarps - 1) / kWarps + 31) / 32 * 32;
+  const int from = min(warp * part, have), upto = min(from + part, have);
+  auto state = [&](int i, bool &tie) {  // does page i stay, or is it a tie
+    tie = false;
+    if (i >= old) return i < have;
+    if (settle) {
+      const unsigned long long k = keys[i];
       tie = k == cut;
-    } else if (B > 0) {
-      keep = sc[i].x >= low;
+      return k > cut;
     }
-    // ties stay in order of position while there are some to stay
-    const unsigned ties = __ballot_sync(0xffffffffu, tie);
-    if (lane == 0) s_warp[warp] = __popc(ties);
-    __syncthreads();
-    int rank = s_count[0] + __popc(ties & ((1u << lane) - 1u)), all = 0;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) rank += s_warp[w];
-      all += s_warp[w];
+    return B > 0 && held(i) >= low;
+  };
+  int stay = 0, ties = 0;
+  for (int i0 = from; i0 < upto; i0 += 32) {
+    bool tie;
+    const bool in = state(i0 + lane, tie) && i0 + lane < upto;
+    stay += __popc(__ballot_sync(0xffffffffu, in));
+    ties += __popc(__ballot_sync(0xffffffffu, tie && i0 + lane < upto));
+  }
+  if (lane == 0) s_warp[warp] = stay, s_ties[warp] = ties;
+  __syncthreads();
+  int at = 0, rank = 0;  // of the warp's first page that stays, of its first tie
+  for (int w = 0; w < warp; ++w) {
+    at += s_warp[w] + min(max(equal - rank, 0), s_ties[w]);
+    rank += s_ties[w];
+  }
+  for (int i0 = from; i0 < upto; i0 += 32) {
+    const int i = i0 + lane;
+    bool tie;
+    bool in = state(i, tie) && i < upto;
+    // ties stay in order of position while there is room
+    const unsigned tied = __ballot_sync(0xffffffffu, tie && i < upto);
+    in |= tie && i < upto && rank + __popc(tied & ((1u << lane) - 1u)) < equal;
+    const unsigned kept_here = __ballot_sync(0xffffffffu, in);
+    const int to = at + __popc(kept_here & ((1u << lane) - 1u));
+    if (in && to < kept) {
+      list[to] = table[i];
+      if (chosen) chosen[to] = i;
     }
-    keep |= tie && rank < equal;
-    __syncthreads();
-    const unsigned in = __ballot_sync(0xffffffffu, keep);
-    if (lane == 0) s_warp[warp] = __popc(in);
-    __syncthreads();
-    int at = s_base + __popc(in & ((1u << lane) - 1u)), count = 0;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) at += s_warp[w];
-      count += s_warp[w];
-    }
-    if (keep && at < kept) {
-      list[at] = table[i];
-      if (chosen) chosen[at] = i;
-    }
-    __syncthreads();
-    if (tid == 0) s_base += count, s_count[0] += all;
-    __syncthreads();
+    at += __popc(kept_here);
+    rank += __popc(tied);
   }
 }
 
 template <typename T, int D>
 cudaError_t launch(const SelectParams &p, int sms, cudaStream_t st, int *launches) {
   const long long units = (long long)p.c.S * p.nl * p.c.H;
-  const long long items = units * ((p.c.tstride + kChunk - 1) / kChunk);
   if (p.budget > 0) {
-    const cudaError_t e =
-        kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(items, 8ll * sms)),
-                        dim3(kThreads), 0, st, p);
+    cudaError_t e;
+    if constexpr (sizeof(T) == 2) {
+      const long long ctas = (units * ((p.c.tstride + 15) / 16) + kWarps - 1) / kWarps;
+      e = kvr::launch_pdl(score_mma_kernel<D>, dim3((unsigned)std::min<long long>(ctas, 8ll * sms)),
+                          dim3(kThreads), 0, st, p);
+    } else {
+      const long long ctas = units * ((p.c.tstride + kChunk - 1) / kChunk);
+      e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(ctas, 8ll * sms)),
+                          dim3(kThreads), 0, st, p);
+    }
     if (e != cudaSuccess) return e;
     *launches += 1;
   }

@@ -226,7 +226,9 @@ def test_refused_plans_change_nothing():
                         ([44, 3, 1], 3),        # grows by more than n_new
                         ([41, 3, 0], 0),
                         ([80, 17, 17], 80),     # the pool ends
-                        ([2**31 - 1, 3, 0], 9)):
+                        ([2**31 - 1, 3, 0], 9),
+                        ([81, 3, 0], 6000),     # slots by a launch of their own
+                        ([80, 17, 17], 6000)):
         b.plan(lens, n_new)
     assert torch.equal(rows, bits(b.c.rows_view()[0]))
     b.plan([80, 16, 17], 80)                    # all eight

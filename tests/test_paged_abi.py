@@ -28,6 +28,7 @@ def test_required_bytes():
                 dict(n_pages=1 << 25), dict(table_pages=1 << 25),
                 dict(n_layers=65535, n_kv_heads=2),
                 dict(n_seq=65535, n_layers=32768),
+                dict(n_layers=80, n_kv_heads=8, n_pages=840000),
                 dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")),
                 dict(softmax_scale=float("inf"))):
         d = desc(**bad)
@@ -38,9 +39,9 @@ def test_required_bytes():
         assert lib.kvr_paged_required_bytes(ctypes.byref(d)) == 0
     assert lib.kvr_paged_required_bytes(None) == 0
     # the largest pool: byte counts pass 32 bits
-    big = desc(n_pages=(1 << 25) - 1, n_layers=80, n_kv_heads=8)
+    big = desc(n_pages=800000, n_layers=80, n_kv_heads=8)
     assert lib.kvr_paged_required_bytes(ctypes.byref(big)) > \
-        2 * 80 * 8 * ((1 << 31) - 64) * 256
+        2 * 80 * 8 * 800000 * 64 * 256
 
 
 def test_create_and_null_handles():
