@@ -264,25 +264,26 @@ struct Mma : Shape<__nv_bfloat16, D> {
       for (int e = 0; e < 8; ++e) o[v][e][0] = o[v][e][1] = 0.f;
   }
   __device__ __forceinline__ void step(const uint4 *stage, int limit, int lane) {
-    float s[2][4];
+    float s[2][4], s2[2][4];  // two chains a row of the tile
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
+    for (int r = 0; r < 2; ++r)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[r][i] = 0.f;
+      for (int i = 0; i < 4; ++i) s[r][i] = s2[r][i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < kK; ++i) {
+    for (int i = 0; i < kK; ++i)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
         const uint4 k = stage[(2 * i + r) * 32 + k_slot(lane >> 2, lane & 3, i)];
         mma_bf16(s[r], q[i].x, 0u, q[i].y, 0u, k.x, k.y);
-        mma_bf16(s[r], q[i].z, 0u, q[i].w, 0u, k.z, k.w);
+        mma_bf16(s2[r], q[i].z, 0u, q[i].w, 0u, k.z, k.w);
       }
-    }
     // rows 8 r + 2 (lane & 3) + i at [r][i]
     float x[2][2];
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        x[r][i] = 8 * r + 2 * (lane & 3) + i < limit ? s[r][i] * scale : -INFINITY;
+        x[r][i] = 8 * r + 2 * (lane & 3) + i < limit ? (s[r][i] + s2[r][i]) * scale : -INFINITY;
     float t = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
     t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
     t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
@@ -548,20 +549,29 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
 #pragma unroll
     for (int y = 0; y < kMine; ++y) {
       const int x = threadIdx.x + y * kThreads, g = x / (D / 4);
+      float2 ms[2 * kWarps];
+      float4 w[2 * kWarps];
+#pragma unroll
+      for (int k = 0; k < 2 * kWarps; ++k) {
+        ms[k] = make_float2(-INFINITY, 0.f);
+        w[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (same >> k & 1) {
+          ms[k] = reinterpret_cast<const float2 *>(piece_at(k) + kStats)[g];
+          w[k] = reinterpret_cast<const float4 *>(piece_at(k))[x];
+        }
+      }
       float m = -INFINITY;
-      for (unsigned k = same; k; k &= k - 1)
-        m = fmaxf(m, piece_at(__ffs(k) - 1)[kStats + 2 * g]);
+#pragma unroll
+      for (int k = 0; k < 2 * kWarps; ++k) m = fmaxf(m, ms[k].x);
       const float ref = m == -INFINITY ? 0.f : m;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       float s = 0.f;
-      for (unsigned k = same; k; k &= k - 1) {
-        const float *from = piece_at(__ffs(k) - 1);
-        const float2 ms = reinterpret_cast<const float2 *>(from + kStats)[g];
-        const float a = ex2(ms.x - ref);
-        const float4 w = reinterpret_cast<const float4 *>(from)[x];
-        v.x = fmaf(w.x, a, v.x), v.y = fmaf(w.y, a, v.y);
-        v.z = fmaf(w.z, a, v.z), v.w = fmaf(w.w, a, v.w);
-        s = fmaf(ms.y, a, s);
+#pragma unroll
+      for (int k = 0; k < 2 * kWarps; ++k) {
+        const float a = ex2(ms[k].x - ref);
+        v.x = fmaf(w[k].x, a, v.x), v.y = fmaf(w[k].y, a, v.y);
+        v.z = fmaf(w[k].z, a, v.z), v.w = fmaf(w[k].w, a, v.w);
+        s = fmaf(ms[k].y, a, s);
       }
       if (!whole) {
         put4(part + 4 * x, v);
@@ -602,7 +612,7 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
     __syncthreads();
     // Shared memory is free now, for the greatest logits of all parts.
     float *logit = reinterpret_cast<float *>(smem);
-    constexpr int kAhead = 8;
+    constexpr int kAhead = 12;
 #pragma unroll 1
     for (int w = 0; w < 2; ++w) {
       if (!s_last[w]) continue;
@@ -623,11 +633,25 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
       {
         const int g = lane & 7;
         float m = -INFINITY, s = 0.f;
-        for (int k = threadIdx.x >> 3; k < N; k += kThreads / 8) {
-          const float2 ms = __ldcg(reinterpret_cast<const float2 *>(part(k) + kStats) + g);
-          logit[k * kHeads + g] = ms.x;
-          const float now = fmaxf(m, ms.x), ref = now == -INFINITY ? 0.f : now;
-          s = fmaf(s, ex2(m - ref), ms.y * ex2(ms.x - ref));
+        for (int k0 = threadIdx.x >> 3; k0 < N; k0 += 4 * (kThreads / 8)) {
+          float2 ms[4];
+          float now = m;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = k0 + i * (kThreads / 8);
+            ms[i] = k < N ? __ldcg(reinterpret_cast<const float2 *>(part(k) + kStats) + g)
+                          : make_float2(-INFINITY, 0.f);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = k0 + i * (kThreads / 8);
+            if (k < N) logit[k * kHeads + g] = ms[i].x;
+            now = fmaxf(now, ms[i].x);
+          }
+          const float ref = now == -INFINITY ? 0.f : now;
+          s *= ex2(m - ref);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s = fmaf(ms[i].y, ex2(ms[i].x - ref), s);
           m = now;
         }
 #pragma unroll
