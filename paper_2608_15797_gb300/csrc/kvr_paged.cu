@@ -20,9 +20,10 @@ namespace {
 
 // ---- plan -------------------------------------------------------------------
 
-constexpr int kPlan = 1024;       // threads of the plan's CTA, sequences of a span
-constexpr int kPlanFew = 256;     // the same of a small call
-constexpr int kOneCta = 16384;    // slots that the plan's CTA writes itself
+constexpr int kPlan = 1024;       // threads of a CTA of the plan, sequences of a span
+constexpr int kPlanFew = 256;     // the same for as many sequences or fewer
+constexpr int kCluster = 8;       // CTAs of the plan
+constexpr int kInPlan = 16384;    // slots that the plan's cluster writes itself
 constexpr int kFill = 256, kFillTokens = 2048;  // of a CTA that writes slots alone
 
 __global__ void __launch_bounds__(256) init_kernel(const __grid_constant__ View c) {
@@ -118,19 +119,30 @@ __device__ __forceinline__ int place(const View &c, int s, int t, int from, int 
   return (page << c.psh) + (pos & (c.P - 1));
 }
 
-// One CTA: S lengths are little work, and what they ask of the stack is a sum over
-// all of them.  Pages that go back (an ended sequence has hundreds) are dealt out to
-// all threads.  Pages are taken by whoever
-// writes the slots of their tokens: this CTA, or for many slots the launch that
-// follows (256 prompts of up to 8,191 tokens, both plans of a pass: 641 us with this
-// CTA alone).
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// One cluster.  S lengths are little work, and what they ask of the stack is a sum
+// over all of them, which every CTA forms for itself; pages that go back (an ended
+// sequence has hundreds), and the new tokens' slots with the pages they need, are
+// dealt out to all threads of the cluster.  Many slots are left to the launch that
+// follows.  64 sequences that drop their drafts and take five tokens more, two plans:
+// 7.5 us; 256 prompts of up to 8,191 tokens given up and taken: 29 thousand pages
+// and two million slots, 641 us in one CTA, 59 with the slots in a launch of their
+// own, 21 with the cluster.
 template <int N>
 __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
                                                  const int32_t *want, int n_new, int32_t *slots) {
   kvr::pdl_begin();
   __shared__ Sums s_warp[N / 32];
-  __shared__ int s_start[N], s_page[N], s_many[N];
-  const int tid = threadIdx.x;
+  __shared__ int s_start[N], s_page[N];
+  const int tid = threadIdx.x, rank = (int)cluster_rank();
   const int spans = (c.S + N - 1) / N;
   const int had = c.free[0];
   Change x{};
@@ -148,60 +160,56 @@ __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
     bad |= x.bad;
   }
   bad = __syncthreads_or(bad);
+  cluster_sync();  // every CTA has read the state
   const long long top = (long long)had + total.back;
+  const long long many = slots ? (long long)c.S * n_new : 0;
   if (bad || total.take > top || top > c.n_pages) {
-    if (tid == 0) {
+    if (tid == 0 && rank == 0) {
       atomicOr(c.err, bad ? (unsigned)kvr::ERR_LENGTH : (unsigned)kvr::ERR_CAPACITY);
       c.free[1] = 0;
     }
-    if (slots && (long long)c.S * n_new <= kOneCta)
-      for (int i = tid; i < c.S * n_new; i += N) slots[i] = -1;
+    if (many <= kInPlan)
+      for (int i = rank * N + tid; i < many; i += kCluster * N) slots[i] = -1;
     return;
   }
   Sums before{};
-  for (int k = 0; k < spans; ++k) {
+  for (int k = 0; k < spans && total.back > 0; ++k) {
     if (spans > 1) sums(k);
-    const int s = k * N + tid;
-    if (all.back > 0) {
-      s_start[tid] = at.back;
-      s_page[tid] = x.need;
-      s_many[tid] = x.back();
-      __syncthreads();
-      auto give = [&](int i, int e) {
-        int32_t *entry = c.table + (long long)(k * N + i) * c.tstride + s_page[i] + e;
-        const long long to = top - 1 - (before.back + s_start[i] + e);
-        if (to >= 0 && to < c.n_pages) c.stack[to] = *entry;
-        *entry = -1;
-      };
-      if (c.S >= N / 32) {  // a warp a sequence
-        for (int i = tid >> 5; i < min(N, c.S - k * N); i += N / 32) {
-          const int many = s_many[i];
+    __syncthreads();
+    s_start[tid] = at.back;
+    s_page[tid] = x.need;
+    __syncthreads();
 #pragma unroll 4
-          for (int e = tid & 31; e < many; e += 32) give(i, e);
-        }
-      } else {  // few sequences: each page looks for its own
-#pragma unroll 4
-        for (int e = tid; e < all.back; e += N) {
-          const int i = find<N>(s_start, e);
-          give(i, e - s_start[i]);
-        }
-      }
-      __syncthreads();
+    for (int e = rank * N + tid; e < all.back; e += kCluster * N) {
+      const int i = find<N>(s_start, e);
+      int32_t *entry = c.table + (long long)(k * N + i) * c.tstride + s_page[i] + (e - s_start[i]);
+      const long long to = top - 1 - (before.back + e);
+      if (to >= 0 && to < c.n_pages) c.stack[to] = *entry;
+      *entry = -1;
     }
-    if (s < c.S) {
-      const Sums mine = before + at;
-      c.len[s] = x.want;
-      c.from[s] = min(x.old, x.want);
-      c.first[s] = (int)(top - 1 - mine.take);
-      c.tiles[s] = mine.tiles;
-      if (s == c.S - 1) c.tiles[c.S] = total.tiles;
-    }
-    before = before + all;
+    before.back += all.back;
   }
-  if (tid == 0) c.free[0] = (int)(top - total.take), c.free[1] = 1;
-  if (!slots || (long long)c.S * n_new > kOneCta) return;
-  __syncthreads();
-  for (int i = tid; i < c.S * n_new; i += N) {
+  if (spans > 1) cluster_sync();  // every CTA has read the lengths again
+  if (rank == 0) {
+    before = Sums{};
+    for (int k = 0; k < spans; ++k) {
+      if (spans > 1) sums(k);
+      const int s = k * N + tid;
+      if (s < c.S) {
+        const Sums mine = before + at;
+        c.len[s] = x.want;
+        c.from[s] = min(x.old, x.want);
+        c.first[s] = (int)(top - 1 - mine.take);
+        c.tiles[s] = mine.tiles;
+        if (s == c.S - 1) c.tiles[c.S] = total.tiles;
+      }
+      before = before + all;
+    }
+    if (tid == 0) c.free[0] = (int)(top - total.take), c.free[1] = 1;
+  }
+  if (many == 0 || many > kInPlan) return;
+  cluster_sync();  // pages are back, the state is written
+  for (int i = rank * N + tid; i < many; i += kCluster * N) {
     const int s = i / n_new;
     slots[i] = place(c, s, i - s * n_new, c.from[s], c.len[s], c.first[s]);
   }
@@ -221,6 +229,24 @@ __global__ void __launch_bounds__(kFill) fill_kernel(const __grid_constant__ Vie
       if (t < n_new) to[t] = done ? place(c, s, t, from, len, first) : -1;
     }
   }
+}
+
+template <int N>
+cudaError_t launch_plan(const View &c, const int32_t *lens, int n_new, int32_t *slots,
+                        cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kCluster);
+  cfg.blockDim = dim3(N);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, plan_kernel<N>, c, lens, n_new, slots);
 }
 
 // ---- append -----------------------------------------------------------------
@@ -564,15 +590,12 @@ kvr_status kvr_paged_plan(kvr_paged *c, const int32_t *lens, int n_new, int32_t 
   const View &w = c->view;
   const cudaStream_t cs = as_stream(stream);
   const long long many = (long long)w.S * n_new;
-  cudaError_t e =
-      w.S <= kvr::paged::kPlanFew && (many <= 4096 || many > kvr::paged::kOneCta)
-          ? kvr::launch_pdl(kvr::paged::plan_kernel<kvr::paged::kPlanFew>, dim3(1),
-                            dim3(kvr::paged::kPlanFew), 0, cs, w, lens, n_new, slots)
-          : kvr::launch_pdl(kvr::paged::plan_kernel<kvr::paged::kPlan>, dim3(1),
-                            dim3(kvr::paged::kPlan), 0, cs, w, lens, n_new, slots);
+  cudaError_t e = w.S <= kvr::paged::kPlanFew
+                      ? kvr::paged::launch_plan<kvr::paged::kPlanFew>(w, lens, n_new, slots, cs)
+                      : kvr::paged::launch_plan<kvr::paged::kPlan>(w, lens, n_new, slots, cs);
   if (e != cudaSuccess) return cuda_fail("kvr_paged_plan", e);
   c->launches += 1;
-  if (many > kvr::paged::kOneCta) {
+  if (many > kvr::paged::kInPlan) {
     const dim3 grid((n_new + kvr::paged::kFillTokens - 1) / kvr::paged::kFillTokens,
                     std::min(w.S, 65535));
     e = kvr::launch_pdl(kvr::paged::fill_kernel, grid, dim3(kvr::paged::kFill), 0, cs, w, n_new,

@@ -141,32 +141,56 @@ __global__ void __launch_bounds__(kThreads) score_mma_kernel(const __grid_consta
   const int groups = (c.tstride + 15) / 16;
   const long long items = (long long)c.S * p.nl * c.H * groups;
   const uint8_t *qs = static_cast<const uint8_t *>(p.q);
-  for (long long it = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); it < items;
-       it += (long long)gridDim.x * kWarps) {
-    const long long unit = it / groups;
-    const int first = (int)(it - unit * groups) * 16;
-    const int s = (int)(unit / ((long long)p.nl * c.H)), u = (int)(unit - (long long)s * p.nl * c.H);
-    const int lr = u / c.H, h = u - lr * c.H;
-    const int have = pages_of(c, s), end = have - p.window;
-    if (have <= p.budget + p.window || first >= end) continue;
-    const int32_t *table = c.table + (long long)s * c.tstride + first;
+  // An item: 16 pages of a unit.  The pages of the next one are looked up while the
+  // bounds of this one come.
+  struct Item {
+    long long unit;
+    int first, end, l, h, page[2];
+  };
+  const long long step = (long long)gridDim.x * kWarps;
+  long long it = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  auto next = [&](Item &x) {  // the next item that has pages to score, from `it` on
+    for (; it < items; it += step) {
+      x.unit = it / groups;
+      x.first = (int)(it - x.unit * groups) * 16;
+      const int s = (int)(x.unit / ((long long)p.nl * c.H));
+      const int u = (int)(x.unit - (long long)s * p.nl * c.H);
+      const int have = pages_of(c, s);
+      x.end = have - p.window;
+      if (have <= p.budget + p.window || x.first >= x.end) continue;
+      const int lr = u / c.H;
+      x.h = u - lr * c.H;
+      x.l = p.lb + lr;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int at = x.first + row + 8 * r;
+        x.page[r] = c.table[(long long)s * c.tstride + (at < x.end ? at : x.first)];
+      }
+      it += step;
+      return true;
+    }
+    return false;
+  };
+  Item x;
+  bool more = next(x);
+  while (more) {
+    const long long unit = x.unit;
+    const int first = x.first, end = x.end;
     Words lo[2][kX], hi[2][kX];
     bool there[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      const int at = row + 8 * r;
-      const int page = table[first + at < end ? at : 0];
-      there[r] = (unsigned)page < (unsigned)c.n_pages;
-      const uint8_t *b = c.bounds +
-                         (((long long)(p.lb + lr) * c.n_pages + (there[r] ? page : 0)) * c.H + h) *
-                             (4 * D) +
-                         j * 32;
+      there[r] = (unsigned)x.page[r] < (unsigned)c.n_pages;
+      const uint8_t *b =
+          c.bounds +
+          (((long long)x.l * c.n_pages + (there[r] ? x.page[r] : 0)) * c.H + x.h) * (4 * D) + j * 32;
 #pragma unroll
-      for (int x = 0; x < kX; ++x) {
-        lo[r][x] = ld32(b + x * 128);
-        hi[r][x] = ld32(b + 2 * D + x * 128);
+      for (int y = 0; y < kX; ++y) {
+        lo[r][y] = ld32(b + y * 128);
+        hi[r][y] = ld32(b + 2 * D + y * 128);
       }
     }
+    more = next(x);
     float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f}, size[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < kX; ++x) {
@@ -294,6 +318,40 @@ __device__ K nth(int n, int need, int top, F key, unsigned *hist, int *s_digit, 
   return prefix;
 }
 
+// One warp: a page's score in 64 bits, as a key.  (All heads at once: a chain of
+// them costs the latency of as many sums.)  No bounds: 0, below every score's.
+template <typename T, int D>
+__device__ __forceinline__ unsigned long long exact_key(const T *q, const T *b, int G, int lane) {
+  if (!b) return 0;
+  constexpr int kPer = D / 32;
+  double lo[kPer], hi[kPer], z[kHeads];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    lo[e] = (double)to_f(b[e * 32 + lane]);
+    hi[e] = (double)to_f(b[D + e * 32 + lane]);
+  }
+#pragma unroll
+  for (int g = 0; g < kHeads; ++g) {
+    z[g] = 0.0;
+    if (g < G)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const float w = to_f(q[g * D + e * 32 + lane]);
+        z[g] += (double)w * (w > 0.f ? hi[e] : lo[e]);
+      }
+  }
+  unsigned long long best = 0;
+#pragma unroll
+  for (int g = 0; g < kHeads; ++g) {
+    if (g >= G) continue;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) z[g] += __shfl_xor_sync(0xffffffffu, z[g], o);
+    const unsigned long long y = key64(z[g]);
+    best = y > best ? y : best;
+  }
+  return best;
+}
+
 constexpr int kHeld = 8192;  // scores of a unit that are held on chip
 
 template <typename T, int D>
@@ -304,6 +362,8 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
   __shared__ int s_digit, s_left, s_warp[kWarps], s_ties[kWarps], s_count[2];
   __shared__ float s_err[kWarps];
   __shared__ unsigned s_and[kWarps], s_or[kWarps], s_held[kHeld];
+  __shared__ int s_near[kThreads];  // pages to be scored again, if they are few
+  __shared__ unsigned long long s_key[kThreads];
   const View &c = p.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int U = p.nl * c.H;
@@ -359,8 +419,8 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
   const int old = have - p.window, B = p.budget;
   float2 *sc = p.score + unit * c.tstride;
   auto held = [&](int i) { return i < kHeld ? s_held[i] : key32(sc[i].x); };
-  // Keys from `top` up stay, those from `low` to it do if there is room for all of
-  // them; else 64-bit keys say which.
+  // Keys above `top` stay, those from `low` to it do if there is room for all of
+  // them; else their scores in 64 bits say which.
   unsigned low = ~0u, top = ~0u;
   bool settle = false;
   unsigned long long cut = 0;  // settled: the last key that stays
@@ -403,47 +463,58 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
     // twice the error on either side, rounded away from t
     top = all ? ~0u : key32(__fadd_ru(t, 2.f * err));
     low = all ? 0u : key32(__fadd_rd(t, -2.f * err));
-    int n_sure = 0, n_near = 0;
+    auto is_near = [&](unsigned x) { return all || (x >= low && x <= top); };
+    int n_sure = 0;
     for (int i = tid; i < old; i += kThreads) {
       const unsigned x = held(i);
       n_sure += !all && x > top;
-      n_near += all || (x >= low && x <= top);
+      if (is_near(x)) {
+        const int at = atomicAdd(&s_count[1], 1);
+        if (at < kThreads) s_near[at] = i;
+      }
     }
     n_sure = __reduce_add_sync(0xffffffffu, n_sure);
-    n_near = __reduce_add_sync(0xffffffffu, n_near);
-    if (lane == 0) atomicAdd(&s_count[0], n_sure), atomicAdd(&s_count[1], n_near);
+    if (lane == 0) atomicAdd(&s_count[0], n_sure);
     __syncthreads();
-    settle = s_count[0] + s_count[1] != B;
-    if (settle) {
-      const T *q = static_cast<const T *>(p.q) + unit * c.G * D;
+    const int near = s_count[1], need = B - s_count[0];
+    const T *q = static_cast<const T *>(p.q) + unit * c.G * D;
+    if (near == need) {
+      // all of them stay
+    } else if (near <= kThreads && old <= kHeld) {
+      // few: each counts those that go before it, and its key on chip says the rest
+      for (int k = warp; k < near; k += kWarps) {
+        const unsigned long long y =
+            exact_key<T, D>(q, bounds_of<T>(c, p.lb + lr, s, h, s_near[k]), c.G, lane);
+        if (lane == 0) s_key[k] = y;
+      }
+      __syncthreads();
+      if (tid < near) {
+        const unsigned long long y = s_key[tid];
+        const int i = s_near[tid];
+        int above = 0;
+        for (int k = 0; k < near; ++k)
+          above += s_key[k] > y || (s_key[k] == y && s_near[k] < i);
+        s_held[i] = above < need ? ~0u : 0u;
+      }
+      low = all ? ~0u : low > 0 ? low : 1u;
+      __syncthreads();
+    } else {
+      settle = true;
       for (int i0 = warp * 32; i0 < old; i0 += kThreads) {
         const int i = i0 + lane;
         const unsigned x = i < old ? held(i) : 0u;
-        const bool sure = i < old && !all && x > top;
-        unsigned ask = __ballot_sync(0xffffffffu, i < old && (all || (x >= low && x <= top)));
-        unsigned long long key = sure ? ~0ull : 0ull;
+        unsigned ask = __ballot_sync(0xffffffffu, i < old && is_near(x));
+        unsigned long long key = i < old && !all && x > top ? ~0ull : 0ull;
         while (ask) {
           const int at = __ffs(ask) - 1;
           ask &= ask - 1;
-          const T *b = bounds_of<T>(c, p.lb + lr, s, h, i0 + at);
-          unsigned long long best = 0;
-          for (int g = 0; b && g < c.G; ++g) {
-            double z = 0.0;
-            for (int e = lane; e < D; e += 32) {
-              const double w = (double)to_f(q[g * D + e]);
-              z += w * (double)to_f(w > 0.0 ? b[D + e] : b[e]);
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-            const unsigned long long y = key64(z);
-            best = y > best ? y : best;
-          }
-          if (lane == at) key = best;
+          const unsigned long long y =
+              exact_key<T, D>(q, bounds_of<T>(c, p.lb + lr, s, h, i0 + at), c.G, lane);
+          if (lane == at) key = y;
         }
         if (i < old) keys[i] = key;
       }
       __syncthreads();
-      // no bounds of a page: key 0, below every score's
       cut = nth<unsigned long long>(old, B, 63, [&](int i) { return keys[i]; }, hist, &s_digit,
                                     &s_left, &equal);
     }

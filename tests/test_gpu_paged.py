@@ -453,6 +453,17 @@ def test_equal_scores_keep_the_lower_page():
             b.check_pages(budget, 1)
 
 
+@pytest.mark.parametrize("pages", [8190, 8193, 9000])
+def test_more_pages_than_are_held_on_chip(pages):
+    """Ordinary scores, and ties across the whole sequence."""
+    b = Book(1, 1, 1, 2, 64, pages, 16, pages)
+    k = rnd(3, (1, 1, 16 * pages, 1, 64))
+    k[0, 0, 16 * (pages - 300):] = k[0, 0, :16 * 300]
+    b.grow([16 * pages], k=k)
+    for budget in (1, 100, 4000):
+        b.check_pages(budget, 5)
+
+
 def test_scores_that_round_alike():
     """Scores that differ by less than fp32 can tell: the choice is that of 64
     bits."""
