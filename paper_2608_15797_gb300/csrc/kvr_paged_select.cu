@@ -4,12 +4,16 @@
 // lo and hi the least and greatest key of each channel: no logit of its rows is above
 // it.  The window newest pages stay, and the budget others of the greatest score.
 //
-//   score_kernel   every page's score in fp32 and a bound of its rounding error
-//   select_kernel  a CTA a unit: the budget-th greatest score by radix passes.  Pages
-//                  nearer to it than both their errors are scored again in 64 bits
-//                  if not all of them stay, so that the choice is the definition's;
-//                  equal scores keep the lower page, and a NaN ranks above every
-//                  number.
+// Pages are scored in fp32, with a bound of each score's rounding error.  A CTA a unit
+// then chooses: the budget-th greatest score by a histogram and a count; pages nearer
+// to it than both their errors, if not all of them stay, are scored again with sums
+// held in two floats, and what that leaves open in 64 bits, so that the choice is the
+// definition's.  Equal scores keep the lower page, a NaN ranks above every number.
+//
+// Few pages (latency): one launch, in which the last CTA of a unit to score chooses.
+// Many (the bounds' bytes): a launch that scores and one that chooses.  us, one and
+// two launches: 4 units of 513 pages 13.6 and 16.8; 112 units of 4,096 pages 83 and
+// 73, 672 of 235 to 469 pages 60 and 53.
 #include "kvr_paged.cuh"
 
 #include <cuda_bf16.h>
@@ -27,7 +31,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kChunk = 64;  // pages of an item of the scores
+constexpr int kPartPages = 16 * kWarps;  // of a CTA, where a unit's pages are shared
 
 using kvr::dev::to_f;
 
@@ -46,59 +50,95 @@ __device__ __forceinline__ float nan_max(float a, float b) {
   return a != a ? a : b != b ? b : fmaxf(a, b);
 }
 
-// A warp a page: a lane sums D / 32 channels' products a head in a chain, then
+// A call's unit, and what is to be done for it.
+struct Unit {
+  long long at;   // of the call
+  int l, s, h;    // layer of the cache, sequence, KV head
+  int have, old;  // its pages; those that have to be chosen from (0: all stay)
+};
+__device__ __forceinline__ Unit unit_of(const SelectParams &p, long long at) {
+  const View &c = p.c;
+  const int U = p.nl * c.H;
+  Unit x;
+  x.at = at;
+  x.s = (int)(at / U);
+  const int u = (int)(at - (long long)x.s * U), lr = u / c.H;
+  x.h = u - lr * c.H;
+  x.l = p.lb + lr;
+  x.have = pages_of(c, x.s);
+  x.old = x.have > p.budget + p.window && p.budget > 0 ? x.have - p.window : 0;
+  return x;
+}
+
+// Items: 16 pages of a unit each, unit by unit.  A warp scores items it, it + step and
+// so on below `end`.
+__device__ __forceinline__ int groups_of(const View &c) { return (c.tstride + 15) / 16; }
+
+struct Item {
+  Unit u;
+  int first;
+};
+// The next item from `it` on that has pages to score.
+__device__ __forceinline__ bool next_item(const SelectParams &p, long long &it, long long end,
+                                          long long step, Item &x) {
+  const int groups = groups_of(p.c);
+  for (; it < end; it += step) {
+    const long long unit = it / groups;
+    x.u = unit_of(p, unit);
+    x.first = (int)(it - unit * groups) * 16;
+    if (x.first >= x.u.old) continue;
+    it += step;
+    return true;
+  }
+  return false;
+}
+
+// fp32: a page at a time; a lane sums D / 32 channels' products a head in a chain, then
 // five steps between lanes.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__ SelectParams p) {
-  kvr::pdl_begin();
+template <int D>
+__device__ __forceinline__ void score_items(const SelectParams &p, long long it, long long stop,
+                                            long long step, const float *) {
   constexpr int kPer = D / 32;
   const View &c = p.c;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int chunks = (c.tstride + kChunk - 1) / kChunk;
-  const long long items = (long long)c.S * p.nl * c.H * chunks;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const long long unit = it / chunks;
-    const int first = (int)(it - unit * chunks) * kChunk;
-    const int h = (int)(unit % c.H), lr = (int)(unit / c.H % p.nl);
-    const int s = (int)(unit / c.H / p.nl);
-    const int have = pages_of(c, s);
-    if (have <= p.budget + p.window) continue;  // all of them stay
-    const int end = min(first + kChunk, have - p.window);
-    if (first >= end) continue;
+  const int lane = threadIdx.x & 31;
+  Item x;
+  while (next_item(p, it, stop, step, x)) {
+    const Unit &u = x.u;
     float q[kHeads][kPer];
     float most = 0.f;  // the greatest sum of |q| of a head
-    const T *qs = static_cast<const T *>(p.q) + unit * c.G * D;
+    const float *qs = static_cast<const float *>(p.q) + u.at * c.G * D;
 #pragma unroll
     for (int g = 0; g < kHeads; ++g) {
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
-        q[g][e] = g < c.G ? to_f(qs[g * D + lane * kPer + e]) : 0.f;
+        q[g][e] = g < c.G ? qs[g * D + lane * kPer + e] : 0.f;
         sum += fabsf(q[g][e]);
       }
       most = nan_max(most, kvr::dev::warp_sum(sum));
     }
-    for (int at = first + warp; at < end; at += kWarps) {
-      const T *b = bounds_of<T>(c, p.lb + lr, s, h, at);
+    const int end = min(x.first + 16, u.old);
+#pragma unroll 2
+    for (int at = x.first; at < end; ++at) {
+      const float *b = bounds_of<float>(c, u.l, u.s, u.h, at);
       float score = -INFINITY, big = 0.f;
       if (b) {
         float lo[kPer], hi[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-          lo[e] = to_f(b[lane * kPer + e]);
-          hi[e] = to_f(b[D + lane * kPer + e]);
+          lo[e] = b[lane * kPer + e];
+          hi[e] = b[D + lane * kPer + e];
           big = nan_max(big, nan_max(fabsf(lo[e]), fabsf(hi[e])));
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) big = nan_max(big, __shfl_xor_sync(0xffffffffu, big, o));
 #pragma unroll
         for (int g = 0; g < kHeads; ++g) {
-          float x = 0.f;
+          float y = 0.f;
 #pragma unroll
-          for (int e = 0; e < kPer; ++e)
-            x = fmaf(q[g][e], q[g][e] > 0.f ? hi[e] : lo[e], x);
-          x = kvr::dev::warp_sum(x);
-          if (g < c.G) score = nan_max(score, x);
+          for (int e = 0; e < kPer; ++e) y = fmaf(q[g][e], q[g][e] > 0.f ? hi[e] : lo[e], y);
+          y = kvr::dev::warp_sum(y);
+          if (g < c.G) score = nan_max(score, y);
         }
       } else if (lane == 0) {
         atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
@@ -106,7 +146,7 @@ __global__ void __launch_bounds__(kThreads) score_kernel(const __grid_constant__
       // Each of the D / 32 + 5 additions rounds by 2^-24 of a sum that is at most
       // sum |q| max |k|; products that underflow add 2^-149 each at most.
       if (lane == 0)
-        p.score[unit * c.tstride + at] = make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f));
+        p.score[u.at * c.tstride + at] = make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f));
     }
   }
 }
@@ -129,75 +169,52 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
   return r;
 }
 
-// bf16 on tensor cores: 16 pages a warp against the 8 query heads, the positive part
-// of q with the greatest keys and the negative part with the least.  A third product,
-// |q| with max(|least|, |greatest|), says how large the terms of the sums are.
+// bf16 on tensor cores: 16 pages against the 8 query heads, the positive part of q
+// with the greatest keys and the negative part with the least.  A third product, |q|
+// with max(|least|, |greatest|), says how large the terms of the sums are.  The pages
+// of the next item are looked up while the bounds of this one come.
 template <int D>
-__global__ void __launch_bounds__(kThreads) score_mma_kernel(const __grid_constant__ SelectParams p) {
-  kvr::pdl_begin();
+__device__ __forceinline__ void score_items(const SelectParams &p, long long it, long long stop,
+                                            long long step, const __nv_bfloat16 *) {
   constexpr int kX = D / 64;  // 32-byte pieces of a lane in a row
   const View &c = p.c;
   const int lane = threadIdx.x & 31, row = lane >> 2, j = lane & 3;
-  const int groups = (c.tstride + 15) / 16;
-  const long long items = (long long)c.S * p.nl * c.H * groups;
-  const uint8_t *qs = static_cast<const uint8_t *>(p.q);
-  // An item: 16 pages of a unit.  The pages of the next one are looked up while the
-  // bounds of this one come.
-  struct Item {
-    long long unit;
-    int first, end, l, h, page[2];
-  };
-  const long long step = (long long)gridDim.x * kWarps;
-  long long it = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  auto next = [&](Item &x) {  // the next item that has pages to score, from `it` on
-    for (; it < items; it += step) {
-      x.unit = it / groups;
-      x.first = (int)(it - x.unit * groups) * 16;
-      const int s = (int)(x.unit / ((long long)p.nl * c.H));
-      const int u = (int)(x.unit - (long long)s * p.nl * c.H);
-      const int have = pages_of(c, s);
-      x.end = have - p.window;
-      if (have <= p.budget + p.window || x.first >= x.end) continue;
-      const int lr = u / c.H;
-      x.h = u - lr * c.H;
-      x.l = p.lb + lr;
+  Item ahead;
+  int page[2];
+  auto look = [&]() {
+    if (!next_item(p, it, stop, step, ahead)) return false;
+    const int32_t *table = c.table + (long long)ahead.u.s * c.tstride;
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int at = x.first + row + 8 * r;
-        x.page[r] = c.table[(long long)s * c.tstride + (at < x.end ? at : x.first)];
-      }
-      it += step;
-      return true;
-    }
-    return false;
+    for (int r = 0; r < 2; ++r) page[r] = table[min(ahead.first + row + 8 * r, ahead.u.old - 1)];
+    return true;
   };
-  Item x;
-  bool more = next(x);
-  while (more) {
-    const long long unit = x.unit;
-    const int first = x.first, end = x.end;
+  for (bool more = look(); more;) {
+    const long long unit = ahead.u.at;
+    const int i0 = ahead.first, end = ahead.u.old;
     Words lo[2][kX], hi[2][kX];
     bool there[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      there[r] = (unsigned)x.page[r] < (unsigned)c.n_pages;
-      const uint8_t *b =
-          c.bounds +
-          (((long long)x.l * c.n_pages + (there[r] ? x.page[r] : 0)) * c.H + x.h) * (4 * D) + j * 32;
+      there[r] = (unsigned)page[r] < (unsigned)c.n_pages;
+      const uint8_t *b = c.bounds +
+                         (((long long)ahead.u.l * c.n_pages + (there[r] ? page[r] : 0)) * c.H +
+                          ahead.u.h) *
+                             (4 * D) +
+                         j * 32;
 #pragma unroll
-      for (int y = 0; y < kX; ++y) {
-        lo[r][y] = ld32(b + y * 128);
-        hi[r][y] = ld32(b + 2 * D + y * 128);
+      for (int x = 0; x < kX; ++x) {
+        lo[r][x] = ld32(b + x * 128);
+        hi[r][x] = ld32(b + 2 * D + x * 128);
       }
     }
-    more = next(x);
+    more = look();
     float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f}, size[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < kX; ++x) {
       Words q{};
       if (row < c.G) {  // (16-byte aligned, no more)
-        const uint4 *at = reinterpret_cast<const uint4 *>(qs + ((unit * c.G + row) * D) * 2 +
-                                                          j * 32 + x * 128);
+        const uint4 *at = reinterpret_cast<const uint4 *>(
+            static_cast<const uint8_t *>(p.q) + ((unit * c.G + row) * D) * 2 + j * 32 + x * 128);
         const uint4 a = __ldg(at), b = __ldg(at + 1);
         q = Words{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
       }
@@ -237,7 +254,7 @@ __global__ void __launch_bounds__(kThreads) score_mma_kernel(const __grid_consta
         score = nan_max(score, __shfl_xor_sync(0xffffffffu, score, o));
         err = nan_max(err, __shfl_xor_sync(0xffffffffu, err, o));
       }
-      const int at = first + row + 8 * r;
+      const int at = i0 + row + 8 * r;
       if (j == 0 && at < end) {
         if (!there[r]) {
           score = -INFINITY;
@@ -352,87 +369,97 @@ __device__ __forceinline__ unsigned long long exact_key(const T *q, const T *b, 
   return best;
 }
 
+// One warp: a page's score less t, from sums held as two floats: within 2^-35 of the
+// sum of magnitudes where the score is within 2^-12 of it from t (products by fma, the
+// sums' errors kept: 2^-40; then one rounding of the difference).
+__device__ __forceinline__ void add_exact(float &hi, float &lo, float x) {
+  const float s = __fadd_rn(hi, x), b = __fsub_rn(s, hi);
+  lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(x, b)));
+  hi = s;
+}
+template <typename T, int D>
+__device__ __forceinline__ float near_offset(const T *q, const T *b, int G, float t, int lane) {
+  if (!b) return -INFINITY;
+  constexpr int kPer = D / 32;
+  float least[kPer], most[kPer], best = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    least[e] = to_f(b[e * 32 + lane]);
+    most[e] = to_f(b[D + e * 32 + lane]);
+  }
+#pragma unroll
+  for (int g = 0; g < kHeads; ++g) {
+    float hi = 0.f, lo = 0.f;
+    if (g < G)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const float w = to_f(q[g * D + e * 32 + lane]), k = w > 0.f ? most[e] : least[e];
+        const float x = __fmul_rn(w, k);
+        add_exact(hi, lo, x);
+        lo = __fadd_rn(lo, __fmaf_rn(w, k, -x));
+      }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float h2 = __shfl_xor_sync(0xffffffffu, hi, o), l2 = __shfl_xor_sync(0xffffffffu, lo, o);
+      lo = __fadd_rn(lo, l2);
+      add_exact(hi, lo, h2);
+    }
+    if (g < G) best = nan_max(best, __fadd_rn(__fsub_rn(hi, t), lo));
+  }
+  return best;
+}
+
 constexpr int kHeld = 8192;  // scores of a unit that are held on chip
 
+// The choice for one unit, whose scores are there.  The whole CTA.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant__ SelectParams p) {
-  kvr::pdl_begin();
+__device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   static_assert(kThreads == 256, "a thread a digit");
   __shared__ unsigned hist[256];
-  __shared__ int s_digit, s_left, s_warp[kWarps], s_ties[kWarps], s_count[2];
+  __shared__ int s_digit, s_left, s_stay[kWarps], s_ties[kWarps], s_sure, s_few;
   __shared__ float s_err[kWarps];
-  __shared__ unsigned s_and[kWarps], s_or[kWarps], s_held[kHeld];
-  __shared__ int s_near[kThreads];  // pages to be scored again, if they are few
+  __shared__ unsigned s_and[kWarps], s_or[kWarps], s_kth;
+  __shared__ unsigned s_held[kHeld + kHeld / 32];
+  __shared__ unsigned s_near[kThreads];  // keys of a digit; pages to be scored again
   __shared__ unsigned long long s_key[kThreads];
+  __shared__ float s_off[kThreads];
+  __shared__ bool s_open[kThreads];
   const View &c = p.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int U = p.nl * c.H;
-  const long long unit = blockIdx.x;
-  if (unit == (long long)c.S * U) {
-    // what the attention reads of each sequence
-    int before = 0;
-    for (int s0 = 0; s0 < c.S; s0 += kThreads) {
-      const int s = s0 + tid;
-      int rows = 0;
-      if (s < c.S) {
-        const int have = pages_of(c, s), kept = min(have, p.keep);
-        rows = c.len[s] - ((have - kept) << c.psh);
-        p.rows[s] = rows;
-      }
-      const int mine = (rows + kTile - 1) / kTile;
-      int x = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      __syncthreads();
-      if (lane == 31) s_warp[warp] = x;
-      __syncthreads();
-      int all = 0;
-      for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) x += s_warp[w];
-        all += s_warp[w];
-      }
-      if (s < c.S) p.tiles[s] = before + x - mine;
-      before += all;
-    }
-    if (tid == 0) p.tiles[c.S] = before;
-    return;
-  }
-  const int s = (int)(unit / U), u = (int)(unit - (long long)s * U);
-  const int lr = u / c.H, h = u - lr * c.H;
-  const int have = pages_of(c, s);
-  const int32_t *table = c.table + (long long)s * c.tstride;
-  int32_t *list = p.list + unit * p.keep;
-  int32_t *chosen = p.chosen ? p.chosen + unit * ((long long)p.budget + p.window) : nullptr;
-  const int kept = (int)min((long long)have, (long long)p.budget + p.window);
+  const int32_t *table = c.table + (long long)u.s * c.tstride;
+  const int have = u.have, old = u.old, B = p.budget;
+  int32_t *list = p.list + u.at * p.keep;
+  int32_t *chosen = p.chosen ? p.chosen + u.at * ((long long)B + p.window) : nullptr;
+  const int kept = (int)min((long long)have, (long long)B + p.window);
   if (chosen)
-    for (int i = kept + tid; i < p.budget + p.window; i += kThreads) chosen[i] = -1;
-  if (have <= p.budget + p.window) {
+    for (int i = kept + tid; i < B + p.window; i += kThreads) chosen[i] = -1;
+  if (old == 0) {
+    // all pages stay, or (no budget) the newest
     for (int i = tid; i < kept; i += kThreads) {
-      list[i] = table[i];
-      if (chosen) chosen[i] = i;
+      list[i] = table[have - kept + i];
+      if (chosen) chosen[i] = have - kept + i;
     }
     return;
   }
-  const int old = have - p.window, B = p.budget;
-  float2 *sc = p.score + unit * c.tstride;
-  auto held = [&](int i) { return i < kHeld ? s_held[i] : key32(sc[i].x); };
+  float2 *sc = p.score + u.at * c.tstride;
+  auto place = [](int i) { return i + (i >> 5); };  // (threads read runs of keys)
+  auto held = [&](int i) { return i < kHeld ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
   // Keys above `top` stay, those from `low` to it do if there is room for all of
   // them; else their scores in 64 bits say which.
-  unsigned low = ~0u, top = ~0u;
+  unsigned low, top;
   bool settle = false;
   unsigned long long cut = 0;  // settled: the last key that stays
   int equal = 0;               // and how many with that key do
   unsigned long long *keys = reinterpret_cast<unsigned long long *>(sc);
-  if (B > 0) {
+  {
     float err = 0.f;
     unsigned both = ~0u, any = 0;
+    hist[tid] = 0;
+#pragma unroll 8
     for (int i = tid; i < old; i += kThreads) {
-      const float2 x = sc[i];
+      const float2 x = __ldcg(sc + i);
       const unsigned k = key32(x.x);
-      if (i < kHeld) s_held[i] = k;
+      if (i < kHeld) s_held[place(i)] = k;
       err = nan_max(err, x.y);
       both &= k, any |= k;
     }
@@ -441,61 +468,120 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
     both = __reduce_and_sync(0xffffffffu, both);
     any = __reduce_or_sync(0xffffffffu, any);
     if (lane == 0) s_err[warp] = err, s_and[warp] = both, s_or[warp] = any;
-    if (tid < 2) s_count[tid] = 0;
+    if (tid == 0) s_sure = s_few = 0;
     __syncthreads();
     err = s_err[0], both = s_and[0], any = s_or[0];
+#pragma unroll
     for (int w = 1; w < kWarps; ++w) {
       err = nan_max(err, s_err[w]);
       both &= s_and[w], any |= s_or[w];
     }
-    // bits above the first that differs are alike in all keys
+    // The bits above the first that differs are alike in all keys; eight from there
+    // on make a histogram, and what falls where the budget ends is counted out.
     const unsigned differ = both ^ any;
-    unsigned k = both;
+    unsigned kth = both;
     if (differ) {
-      const int bit = 31 - __clz(differ);
-      int left;
+      const int bit = 31 - __clz(differ), shift = max(bit - 7, 0);
       const unsigned rest = bit == 31 ? ~0u : (1u << (bit + 1)) - 1u;
-      k = (both & ~rest) | nth<unsigned>(old, B, bit, [&](int i) { return held(i) & rest; }, hist,
-                                         &s_digit, &s_left, &left);
+      auto digit = [&](unsigned k) { return (k & rest) >> shift; };
+#pragma unroll 8
+      for (int i = tid; i < old; i += kThreads) atomicAdd(&hist[digit(held(i))], 1u);
+      __syncthreads();
+      if (warp == 0) digit_of(hist, B, lane, &s_digit, &s_left);
+      __syncthreads();
+      const unsigned d = s_digit;
+      const int left = s_left, in = (int)hist[d];
+      if (in <= kThreads) {
+#pragma unroll 8
+        for (int i = tid; i < old; i += kThreads) {
+          const unsigned k = held(i);
+          if (digit(k) == d) s_near[atomicAdd(&s_few, 1)] = k;
+        }
+        __syncthreads();
+        if (tid < in) {
+          const unsigned mine = s_near[tid];
+          int above = 0, alike = 0;
+#pragma unroll 8
+          for (int k = 0; k < in; ++k) {
+            above += s_near[k] > mine;
+            alike += s_near[k] == mine;
+          }
+          if (above < left && above + alike >= left) s_kth = mine;
+        }
+        __syncthreads();
+        kth = s_kth;
+      } else {
+        int unused;
+        kth = (both & ~rest) |
+              nth<unsigned>(old, B, bit, [&](int i) { return held(i) & rest; }, hist, &s_digit,
+                            &s_left, &unused);
+      }
+      __syncthreads();
+      if (tid == 0) s_few = 0;
+      __syncthreads();
     }
-    const float t = __uint_as_float((k >> 31) ? k & 0x7FFFFFFFu : ~k);
+    const float t = __uint_as_float((kth >> 31) ? kth & 0x7FFFFFFFu : ~kth);
     const bool all = !(fabsf(t) < INFINITY && err < INFINITY);
     // twice the error on either side, rounded away from t
     top = all ? ~0u : key32(__fadd_ru(t, 2.f * err));
     low = all ? 0u : key32(__fadd_rd(t, -2.f * err));
     auto is_near = [&](unsigned x) { return all || (x >= low && x <= top); };
     int n_sure = 0;
+#pragma unroll 8
     for (int i = tid; i < old; i += kThreads) {
       const unsigned x = held(i);
       n_sure += !all && x > top;
       if (is_near(x)) {
-        const int at = atomicAdd(&s_count[1], 1);
+        const int at = atomicAdd(&s_few, 1);
         if (at < kThreads) s_near[at] = i;
       }
     }
     n_sure = __reduce_add_sync(0xffffffffu, n_sure);
-    if (lane == 0) atomicAdd(&s_count[0], n_sure);
+    if (lane == 0) atomicAdd(&s_sure, n_sure);
     __syncthreads();
-    const int near = s_count[1], need = B - s_count[0];
-    const T *q = static_cast<const T *>(p.q) + unit * c.G * D;
+    const int near = s_few, need = B - s_sure;
+    const T *q = static_cast<const T *>(p.q) + u.at * c.G * D;
     if (near == need) {
       // all of them stay
     } else if (near <= kThreads && old <= kHeld) {
-      // few: each counts those that go before it, and its key on chip says the rest
+      // Few: what two floats say of each, and 64 bits of those they leave open; keys
+      // on chip then say who stays.  (64-bit arithmetic runs at 1/64 of the rate: ten
+      // pages cost 9 us with it alone.)
       for (int k = warp; k < near; k += kWarps) {
-        const unsigned long long y =
-            exact_key<T, D>(q, bounds_of<T>(c, p.lb + lr, s, h, s_near[k]), c.G, lane);
-        if (lane == 0) s_key[k] = y;
+        const float y = near_offset<T, D>(q, bounds_of<T>(c, u.l, u.s, u.h, s_near[k]), c.G, t, lane);
+        if (lane == 0) s_off[k] = y;
       }
       __syncthreads();
+      bool in = false, open = false;
+      const float off = tid < near ? s_off[tid] : 0.f, e2 = 2.f * (err * 0x1p-21f + 1e-40f);
       if (tid < near) {
-        const unsigned long long y = s_key[tid];
-        const int i = s_near[tid];
-        int above = 0;
-        for (int k = 0; k < near; ++k)
-          above += s_key[k] > y || (s_key[k] == y && s_near[k] < i);
-        s_held[i] = above < need ? ~0u : 0u;
+        int maybe = 0, surely = 0;  // that go before it
+        for (int k = 0; k < near; ++k) {
+          maybe += k != tid && !(s_off[k] < off - e2);
+          surely += s_off[k] > off + e2;
+        }
+        in = maybe < need;
+        open = !in && surely < need;
       }
+      const int n_in = __syncthreads_count(in);
+      s_open[tid] = open;
+      if (__syncthreads_or(open)) {
+        for (int k = warp; k < near; k += kWarps) {
+          if (!s_open[k]) continue;
+          const unsigned long long y =
+              exact_key<T, D>(q, bounds_of<T>(c, u.l, u.s, u.h, s_near[k]), c.G, lane);
+          if (lane == 0) s_key[k] = y;
+        }
+        __syncthreads();
+        if (open) {
+          const unsigned long long y = s_key[tid];
+          int above = 0;
+          for (int k = 0; k < near; ++k)
+            above += s_open[k] && (s_key[k] > y || (s_key[k] == y && s_near[k] < s_near[tid]));
+          in = above < need - n_in;
+        }
+      }
+      if (tid < near) s_held[place(s_near[tid])] = in ? ~0u : 0u;
       low = all ? ~0u : low > 0 ? low : 1u;
       __syncthreads();
     } else {
@@ -509,7 +595,7 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
           const int at = __ffs(ask) - 1;
           ask &= ask - 1;
           const unsigned long long y =
-              exact_key<T, D>(q, bounds_of<T>(c, p.lb + lr, s, h, i0 + at), c.G, lane);
+              exact_key<T, D>(q, bounds_of<T>(c, u.l, u.s, u.h, i0 + at), c.G, lane);
           if (lane == at) key = y;
         }
         if (i < old) keys[i] = key;
@@ -519,71 +605,149 @@ __global__ void __launch_bounds__(kThreads) select_kernel(const __grid_constant_
                                     &s_left, &equal);
     }
   }
-  // The pages that stay, in order: a warp goes through an equal part of them, once to
-  // count and once to write.
-  const int part = ((have + kWarps - 1) / kWarps + 31) / 32 * 32;
-  const int from = min(warp * part, have), upto = min(from + part, have);
-  auto state = [&](int i, bool &tie) {  // does page i stay, or is it a tie
-    tie = false;
-    if (i >= old) return i < have;
-    if (settle) {
-      const unsigned long long k = keys[i];
-      tie = k == cut;
-      return k > cut;
-    }
-    return B > 0 && held(i) >= low;
-  };
+  // The pages that stay, in order: a thread goes through a run of them, once to count
+  // and once to write.
+  const int run = (old + kThreads - 1) / kThreads;
+  const int from = min(tid * run, old), upto = min(from + run, old);
   int stay = 0, ties = 0;
-  for (int i0 = from; i0 < upto; i0 += 32) {
-    bool tie;
-    const bool in = state(i0 + lane, tie) && i0 + lane < upto;
-    stay += __popc(__ballot_sync(0xffffffffu, in));
-    ties += __popc(__ballot_sync(0xffffffffu, tie && i0 + lane < upto));
-  }
-  if (lane == 0) s_warp[warp] = stay, s_ties[warp] = ties;
-  __syncthreads();
-  int at = 0, rank = 0;  // of the warp's first page that stays, of its first tie
-  for (int w = 0; w < warp; ++w) {
-    at += s_warp[w] + min(max(equal - rank, 0), s_ties[w]);
-    rank += s_ties[w];
-  }
-  for (int i0 = from; i0 < upto; i0 += 32) {
-    const int i = i0 + lane;
-    bool tie;
-    bool in = state(i, tie) && i < upto;
-    // ties stay in order of position while there is room
-    const unsigned tied = __ballot_sync(0xffffffffu, tie && i < upto);
-    in |= tie && i < upto && rank + __popc(tied & ((1u << lane) - 1u)) < equal;
-    const unsigned kept_here = __ballot_sync(0xffffffffu, in);
-    const int to = at + __popc(kept_here & ((1u << lane) - 1u));
-    if (in && to < kept) {
-      list[to] = table[i];
-      if (chosen) chosen[to] = i;
+  for (int i = from; i < upto; ++i) {
+    if (settle) {
+      stay += keys[i] > cut;
+      ties += keys[i] == cut;
+    } else {
+      stay += held(i) >= low;
     }
-    at += __popc(kept_here);
-    rank += __popc(tied);
+  }
+  int stay_upto = stay, ties_upto = ties;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int a = __shfl_up_sync(0xffffffffu, stay_upto, o);
+    const int b = __shfl_up_sync(0xffffffffu, ties_upto, o);
+    if (lane >= o) stay_upto += a, ties_upto += b;
+  }
+  if (lane == 31) s_stay[warp] = stay_upto, s_ties[warp] = ties_upto;
+  __syncthreads();
+  int at = stay_upto - stay, rank = ties_upto - ties;
+  for (int w = 0; w < warp; ++w) at += s_stay[w], rank += s_ties[w];
+  at += min(rank, equal);  // ties stay in order of position while there is room
+  for (int i = from; i < upto; ++i) {
+    bool in;
+    if (settle) {
+      in = keys[i] > cut || (keys[i] == cut && rank < equal);
+      rank += keys[i] == cut;
+    } else {
+      in = held(i) >= low;
+    }
+    if (in && at < kept) {
+      list[at] = table[i];
+      if (chosen) chosen[at] = i;
+    }
+    at += in;
+  }
+  for (int i = tid; i < p.window; i += kThreads) {
+    list[B + i] = table[old + i];
+    if (chosen) chosen[B + i] = old + i;
   }
 }
 
-template <typename T, int D>
-cudaError_t launch(const SelectParams &p, int sms, cudaStream_t st, int *launches) {
-  const long long units = (long long)p.c.S * p.nl * p.c.H;
-  if (p.budget > 0) {
-    cudaError_t e;
-    if constexpr (sizeof(T) == 2) {
-      const long long ctas = (units * ((p.c.tstride + 15) / 16) + kWarps - 1) / kWarps;
-      e = kvr::launch_pdl(score_mma_kernel<D>, dim3((unsigned)std::min<long long>(ctas, 8ll * sms)),
-                          dim3(kThreads), 0, st, p);
-    } else {
-      const long long ctas = units * ((p.c.tstride + kChunk - 1) / kChunk);
-      e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(ctas, 8ll * sms)),
-                          dim3(kThreads), 0, st, p);
+// What the attention reads of each sequence: rows of the pages that stay, and the
+// tiles of the sequences before it.
+__device__ void sequences(const SelectParams &p) {
+  __shared__ int s_warp[kWarps];
+  const View &c = p.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int before = 0;
+  for (int s0 = 0; s0 < c.S; s0 += kThreads) {
+    const int s = s0 + tid;
+    int rows = 0;
+    if (s < c.S) {
+      const int have = pages_of(c, s), kept = min(have, p.keep);
+      rows = c.len[s] - ((have - kept) << c.psh);
+      p.rows[s] = rows;
     }
+    const int mine = (rows + kTile - 1) / kTile;
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) x += s_warp[w];
+      all += s_warp[w];
+    }
+    if (s < c.S) p.tiles[s] = before + x - mine;
+    before += all;
+  }
+  if (tid == 0) p.tiles[c.S] = before;
+}
+
+// CTA 0: sequences(); the others: part i of a unit's pages each, p.parts of them.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 2) select_kernel(const __grid_constant__ SelectParams p) {
+  kvr::pdl_begin();
+  __shared__ int s_last;
+  if (blockIdx.x == 0) return sequences(p);
+  const unsigned job = blockIdx.x - 1;
+  const Unit u = unit_of(p, job / p.parts);
+  const int part = job % p.parts;
+  const int parts = max((u.old + kPartPages - 1) / kPartPages, 1);
+  if (part >= parts) return;
+  if (u.old > 0) {
+    const long long first = u.at * groups_of(p.c) + part * (kPartPages / 16);
+    score_items<D>(p, first + (threadIdx.x >> 5),
+                   min(first + kPartPages / 16, (u.at + 1) * groups_of(p.c)), kWarps,
+                   (const T *)nullptr);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      // (the barrier and this fence order every thread's scores before the arrival)
+      __threadfence();
+      unsigned *ticket = p.c.uticket + u.at;
+      s_last = parts == 1 || atomicAdd(ticket, 1u) == (unsigned)parts - 1;
+      if (s_last && parts > 1) *ticket = 0;
+      __threadfence();
+    }
+    __syncthreads();
+    if (!s_last) return;
+  }
+  choose<T, D>(p, u);
+}
+
+// The same in two launches.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 2) score_kernel(const __grid_constant__ SelectParams p) {
+  kvr::pdl_begin();
+  const long long all = (long long)p.c.S * p.nl * p.c.H * groups_of(p.c);
+  score_items<D>(p, (long long)blockIdx.x * kWarps + (threadIdx.x >> 5), all,
+                 (long long)gridDim.x * kWarps, (const T *)nullptr);
+}
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant__ SelectParams p) {
+  kvr::pdl_begin();
+  if (blockIdx.x == 0) return sequences(p);
+  choose<T, D>(p, unit_of(p, blockIdx.x - 1));
+}
+
+template <typename T, int D>
+cudaError_t launch(SelectParams p, int sms, cudaStream_t st, int *launches) {
+  const long long units = (long long)p.c.S * p.nl * p.c.H;
+  p.parts = p.budget > 0 ? (p.c.tstride + kPartPages - 1) / kPartPages : 1;
+  const long long jobs = units * p.parts;
+  cudaError_t e;
+  if (p.budget == 0 || jobs <= 2 * sms) {
+    if (jobs >= 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+    e = kvr::launch_pdl(select_kernel<T, D>, dim3((unsigned)jobs + 1), dim3(kThreads), 0, st, p);
+  } else {
+    e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(jobs, 8ll * sms)),
+                        dim3(kThreads), 0, st, p);
     if (e != cudaSuccess) return e;
     *launches += 1;
+    e = kvr::launch_pdl(choose_kernel<T, D>, dim3((unsigned)units + 1), dim3(kThreads), 0, st, p);
   }
-  const cudaError_t e = kvr::launch_pdl(select_kernel<T, D>, dim3((unsigned)(units + 1)),
-                                        dim3(kThreads), 0, st, p);
   if (e == cudaSuccess) *launches += 1;
   return e;
 }
