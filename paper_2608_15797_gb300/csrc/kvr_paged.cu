@@ -475,6 +475,8 @@ long long most_tiles(const kvr_paged *c, int nl, int keep) {
   return pages * a_page * units;
 }
 
+size_t score_stride(const kvr_paged *c) { return ((size_t)c->desc.table_pages + 1) / 2 * 2; }
+
 // Parts of a workspace of either attention; `pages` of a choice, or none.
 struct Work {
   size_t parts, score, list, rows, tiles, total;
@@ -498,7 +500,7 @@ Work work_of(const kvr_paged *c, int nl, int budget, int window) {
                  kvr::paged::part_floats(d.head_dim) * sizeof(float));
   if (window > 0) {
     const size_t units = (size_t)d.n_seq * nl * d.n_kv_heads;
-    w.score = take(units * d.table_pages * sizeof(float2));
+    w.score = take(units * score_stride(c) * sizeof(float2));
     w.list = take(units * w.keep * sizeof(int32_t));
     w.rows = take((size_t)d.n_seq * sizeof(int32_t));
     w.tiles = take(((size_t)d.n_seq + 1) * sizeof(int32_t));
@@ -702,6 +704,7 @@ kvr_status kvr_paged_attend_pages(kvr_paged *c, int lb, int le, const void *q, i
   s.window = window;
   s.keep = w.keep;
   s.score = reinterpret_cast<float2 *>(ws + w.score);
+  s.sstride = (int)score_stride(c);
   s.list = reinterpret_cast<int32_t *>(ws + w.list);
   s.rows = reinterpret_cast<int32_t *>(ws + w.rows);
   s.tiles = reinterpret_cast<int32_t *>(ws + w.tiles);

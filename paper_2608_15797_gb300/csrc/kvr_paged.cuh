@@ -68,7 +68,8 @@ struct SelectParams {
   const void *q;
   int budget, window;
   int keep;           // pages of a list
-  float2 *score;      // [unit of the call][tstride]: score, bound of its error
+  float2 *score;      // [unit of the call][sstride]: score, bound of its error
+  int sstride;        // even
   int32_t *list;      // [unit][keep]
   int32_t *rows;      // [S]
   int32_t *tiles;     // [S + 1]

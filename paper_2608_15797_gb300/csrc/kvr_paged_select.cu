@@ -58,11 +58,11 @@ struct Unit {
 };
 __device__ __forceinline__ Unit unit_of(const SelectParams &p, long long at) {
   const View &c = p.c;
-  const int U = p.nl * c.H;
+  const unsigned U = p.nl * c.H, n = (unsigned)at;  // (units are fewer than 2^31)
   Unit x;
   x.at = at;
-  x.s = (int)(at / U);
-  const int u = (int)(at - (long long)x.s * U), lr = u / c.H;
+  x.s = n / U;
+  const unsigned u = n - x.s * U, lr = u / (unsigned)c.H;
   x.h = u - lr * c.H;
   x.l = p.lb + lr;
   x.have = pages_of(c, x.s);
@@ -70,25 +70,31 @@ __device__ __forceinline__ Unit unit_of(const SelectParams &p, long long at) {
   return x;
 }
 
-// Items: 16 pages of a unit each, unit by unit.  A warp scores items it, it + step and
-// so on below `end`.
+// Items: 16 pages of a unit each, unit by unit.  A warp scores an item, the one `step`
+// further and so on, up to unit `units`.
 __device__ __forceinline__ int groups_of(const View &c) { return (c.tstride + 15) / 16; }
 
+struct Items {
+  int unit, group;            // the next item
+  int unit_step, group_step;  // to the one after it
+  int units, groups;
+  __device__ __forceinline__ Items(int unit, int group, unsigned step, int units, int groups)
+      : unit(unit), group(group), unit_step(step / groups), group_step(step % groups), units(units),
+        groups(groups) {}
+};
 struct Item {
   Unit u;
   int first;
 };
-// The next item from `it` on that has pages to score.
-__device__ __forceinline__ bool next_item(const SelectParams &p, long long &it, long long end,
-                                          long long step, Item &x) {
-  const int groups = groups_of(p.c);
-  for (; it < end; it += step) {
-    const long long unit = it / groups;
-    x.u = unit_of(p, unit);
-    x.first = (int)(it - unit * groups) * 16;
-    if (x.first >= x.u.old) continue;
-    it += step;
-    return true;
+// The next item that has pages to score.
+__device__ __forceinline__ bool next_item(const SelectParams &p, Items &it, Item &x) {
+  while (it.unit < it.units) {
+    x.u = unit_of(p, it.unit);
+    x.first = it.group * 16;
+    it.unit += it.unit_step;
+    it.group += it.group_step;
+    if (it.group >= it.groups) it.group -= it.groups, ++it.unit;
+    if (x.first < x.u.old) return true;
   }
   return false;
 }
@@ -96,13 +102,12 @@ __device__ __forceinline__ bool next_item(const SelectParams &p, long long &it, 
 // fp32: a page at a time; a lane sums D / 32 channels' products a head in a chain, then
 // five steps between lanes.
 template <int D>
-__device__ __forceinline__ void score_items(const SelectParams &p, long long it, long long stop,
-                                            long long step, const float *) {
+__device__ __forceinline__ void score_items(const SelectParams &p, Items it, const float *) {
   constexpr int kPer = D / 32;
   const View &c = p.c;
   const int lane = threadIdx.x & 31;
   Item x;
-  while (next_item(p, it, stop, step, x)) {
+  while (next_item(p, it, x)) {
     const Unit &u = x.u;
     float q[kHeads][kPer];
     float most = 0.f;  // the greatest sum of |q| of a head
@@ -146,7 +151,7 @@ __device__ __forceinline__ void score_items(const SelectParams &p, long long it,
       // Each of the D / 32 + 5 additions rounds by 2^-24 of a sum that is at most
       // sum |q| max |k|; products that underflow add 2^-149 each at most.
       if (lane == 0)
-        p.score[u.at * c.tstride + at] = make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f));
+        p.score[u.at * p.sstride + at] = make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f));
     }
   }
 }
@@ -174,15 +179,15 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
 // with max(|least|, |greatest|), says how large the terms of the sums are.  The pages
 // of the next item are looked up while the bounds of this one come.
 template <int D>
-__device__ __forceinline__ void score_items(const SelectParams &p, long long it, long long stop,
-                                            long long step, const __nv_bfloat16 *) {
+__device__ __forceinline__ void score_items(const SelectParams &p, Items it,
+                                            const __nv_bfloat16 *) {
   constexpr int kX = D / 64;  // 32-byte pieces of a lane in a row
   const View &c = p.c;
   const int lane = threadIdx.x & 31, row = lane >> 2, j = lane & 3;
   Item ahead;
   int page[2];
   auto look = [&]() {
-    if (!next_item(p, it, stop, step, ahead)) return false;
+    if (!next_item(p, it, ahead)) return false;
     const int32_t *table = c.table + (long long)ahead.u.s * c.tstride;
 #pragma unroll
     for (int r = 0; r < 2; ++r) page[r] = table[min(ahead.first + row + 8 * r, ahead.u.old - 1)];
@@ -264,7 +269,7 @@ __device__ __forceinline__ void score_items(const SelectParams &p, long long it,
         // Of each of the D / 16 products of a chain, 17 terms may be cut at 2^-23 of
         // the sum of magnitudes: 136 x 2^-23 of it for d = 128, the same again for
         // the other chain and for the sum of magnitudes itself.
-        p.score[unit * c.tstride + at] = make_float2(score, fmaf(err, 0x1p-14f, 1e-37f));
+        p.score[unit * p.sstride + at] = make_float2(score, fmaf(err, 0x1p-14f, 1e-37f));
       }
     }
   }
@@ -272,6 +277,9 @@ __device__ __forceinline__ void score_items(const SelectParams &p, long long it,
 
 __device__ __forceinline__ unsigned key32(float x) {
   return x != x ? 0xFFFFFFFFu : kvr::dev::ord_bits(x + 0.f);
+}
+__device__ __forceinline__ float value32(unsigned k) {
+  return __uint_as_float((k >> 31) ? k & 0x7FFFFFFFu : ~k);
 }
 __device__ __forceinline__ unsigned long long key64(double x) {
   if (x != x) return ~0ull - 1;
@@ -418,7 +426,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   __shared__ unsigned hist[256];
   __shared__ int s_digit, s_left, s_stay[kWarps], s_ties[kWarps], s_sure, s_few;
   __shared__ float s_err[kWarps];
-  __shared__ unsigned s_and[kWarps], s_or[kWarps], s_kth;
+  __shared__ unsigned s_least[kWarps], s_most[kWarps], s_kth;
   __shared__ unsigned s_held[kHeld + kHeld / 32];
   __shared__ unsigned s_near[kThreads];  // keys of a digit; pages to be scored again
   __shared__ unsigned long long s_key[kThreads];
@@ -441,7 +449,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
     }
     return;
   }
-  float2 *sc = p.score + u.at * c.tstride;
+  float2 *sc = p.score + u.at * p.sstride;
   auto place = [](int i) { return i + (i >> 5); };  // (threads read runs of keys)
   auto held = [&](int i) { return i < kHeld ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
   // Keys above `top` stay, those from `low` to it do if there is room for all of
@@ -453,39 +461,43 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   unsigned long long *keys = reinterpret_cast<unsigned long long *>(sc);
   {
     float err = 0.f;
-    unsigned both = ~0u, any = 0;
+    unsigned least = ~0u, most = 0;
     hist[tid] = 0;
 #pragma unroll 8
-    for (int i = tid; i < old; i += kThreads) {
-      const float2 x = __ldcg(sc + i);
-      const unsigned k = key32(x.x);
-      if (i < kHeld) s_held[place(i)] = k;
-      err = nan_max(err, x.y);
-      both &= k, any |= k;
+    for (int i = 2 * tid; i < old; i += 2 * kThreads) {
+      // (the last one's neighbour is there, and not counted)
+      const float4 x = __ldcg(reinterpret_cast<const float4 *>(sc + i));
+      const unsigned k0 = key32(x.x), k1 = i + 1 < old ? key32(x.z) : k0;
+      if (i < kHeld) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
+      err = nan_max(err, i + 1 < old ? nan_max(x.y, x.w) : x.y);
+      least = min(least, min(k0, k1)), most = max(most, max(k0, k1));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) err = nan_max(err, __shfl_xor_sync(0xffffffffu, err, o));
-    both = __reduce_and_sync(0xffffffffu, both);
-    any = __reduce_or_sync(0xffffffffu, any);
-    if (lane == 0) s_err[warp] = err, s_and[warp] = both, s_or[warp] = any;
+    least = __reduce_min_sync(0xffffffffu, least);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) s_err[warp] = err, s_least[warp] = least, s_most[warp] = most;
     if (tid == 0) s_sure = s_few = 0;
     __syncthreads();
-    err = s_err[0], both = s_and[0], any = s_or[0];
+    err = s_err[0], least = s_least[0], most = s_most[0];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) {
       err = nan_max(err, s_err[w]);
-      both &= s_and[w], any |= s_or[w];
+      least = min(least, s_least[w]), most = max(most, s_most[w]);
     }
-    // The bits above the first that differs are alike in all keys; eight from there
-    // on make a histogram, and what falls where the budget ends is counted out.
-    const unsigned differ = both ^ any;
-    unsigned kth = both;
-    if (differ) {
-      const int bit = 31 - __clz(differ), shift = max(bit - 7, 0);
-      const unsigned rest = bit == 31 ? ~0u : (1u << (bit + 1)) - 1u;
-      auto digit = [&](unsigned k) { return (k & rest) >> shift; };
+    const float from = value32(least), to = value32(most);
+    const bool all = !(fabsf(from) < INFINITY && fabsf(to) < INFINITY && err < INFINITY);
+    float t = from;
+    if (!all && least != most) {
+      // 256 equal parts of the scores' range make a histogram, and what falls into the
+      // part where the budget ends is counted out.  (Rounding keeps the order, which
+      // is all that is asked of the parts.)
+      const float scale = fminf(256.f / fmaxf(to - from, 0x1p-120f), 0x1p120f);
+      auto part = [&](unsigned k) {
+        return (unsigned)fminf(fmaxf((value32(k) - from) * scale, 0.f), 255.f);
+      };
 #pragma unroll 8
-      for (int i = tid; i < old; i += kThreads) atomicAdd(&hist[digit(held(i))], 1u);
+      for (int i = tid; i < old; i += kThreads) atomicAdd(&hist[part(held(i))], 1u);
       __syncthreads();
       if (warp == 0) digit_of(hist, B, lane, &s_digit, &s_left);
       __syncthreads();
@@ -495,7 +507,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
 #pragma unroll 8
         for (int i = tid; i < old; i += kThreads) {
           const unsigned k = held(i);
-          if (digit(k) == d) s_near[atomicAdd(&s_few, 1)] = k;
+          if (part(k) == d) s_near[atomicAdd(&s_few, 1)] = k;
         }
         __syncthreads();
         if (tid < in) {
@@ -509,19 +521,14 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
           if (above < left && above + alike >= left) s_kth = mine;
         }
         __syncthreads();
-        kth = s_kth;
+        if (tid == 0) s_few = 0;
+        t = value32(s_kth);
       } else {
         int unused;
-        kth = (both & ~rest) |
-              nth<unsigned>(old, B, bit, [&](int i) { return held(i) & rest; }, hist, &s_digit,
-                            &s_left, &unused);
+        t = value32(nth<unsigned>(old, B, 31, held, hist, &s_digit, &s_left, &unused));
       }
       __syncthreads();
-      if (tid == 0) s_few = 0;
-      __syncthreads();
     }
-    const float t = __uint_as_float((kth >> 31) ? kth & 0x7FFFFFFFu : ~kth);
-    const bool all = !(fabsf(t) < INFINITY && err < INFINITY);
     // twice the error on either side, rounded away from t
     top = all ? ~0u : key32(__fadd_ru(t, 2.f * err));
     low = all ? 0u : key32(__fadd_rd(t, -2.f * err));
@@ -610,13 +617,11 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   const int run = (old + kThreads - 1) / kThreads;
   const int from = min(tid * run, old), upto = min(from + run, old);
   int stay = 0, ties = 0;
-  for (int i = from; i < upto; ++i) {
-    if (settle) {
-      stay += keys[i] > cut;
-      ties += keys[i] == cut;
-    } else {
-      stay += held(i) >= low;
-    }
+  if (settle) {
+    for (int i = from; i < upto; ++i) stay += keys[i] > cut, ties += keys[i] == cut;
+  } else {
+#pragma unroll 4
+    for (int i = from; i < upto; ++i) stay += held(i) >= low;
   }
   int stay_upto = stay, ties_upto = ties;
 #pragma unroll
@@ -630,24 +635,33 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   int at = stay_upto - stay, rank = ties_upto - ties;
   for (int w = 0; w < warp; ++w) at += s_stay[w], rank += s_ties[w];
   at += min(rank, equal);  // ties stay in order of position while there is room
-  for (int i = from; i < upto; ++i) {
-    bool in;
-    if (settle) {
-      in = keys[i] > cut || (keys[i] == cut && rank < equal);
-      rank += keys[i] == cut;
-    } else {
-      in = held(i) >= low;
+  const bool few = B <= kThreads;  // positions on chip, so that pages are looked up together
+  auto put = [&](int at, int i) {
+    list[at] = table[i];
+    if (chosen) chosen[at] = i;
+  };
+  if (settle || stay > 0) {
+#pragma unroll 4
+    for (int i = from; i < upto; ++i) {
+      bool in;
+      if (settle) {
+        in = keys[i] > cut || (keys[i] == cut && rank < equal);
+        rank += keys[i] == cut;
+      } else {
+        in = held(i) >= low;
+      }
+      if (in && at < B) {
+        if (few)
+          s_near[at] = i;
+        else
+          put(at, i);
+      }
+      at += in;
     }
-    if (in && at < kept) {
-      list[at] = table[i];
-      if (chosen) chosen[at] = i;
-    }
-    at += in;
   }
-  for (int i = tid; i < p.window; i += kThreads) {
-    list[B + i] = table[old + i];
-    if (chosen) chosen[B + i] = old + i;
-  }
+  __syncthreads();
+  if (few && tid < B) put(tid, s_near[tid]);
+  for (int i = tid; i < p.window; i += kThreads) put(B + i, old + i);
 }
 
 // What the attention reads of each sequence: rows of the pages that stay, and the
@@ -698,9 +712,9 @@ __global__ void __launch_bounds__(kThreads, 2) select_kernel(const __grid_consta
   const int parts = max((u.old + kPartPages - 1) / kPartPages, 1);
   if (part >= parts) return;
   if (u.old > 0) {
-    const long long first = u.at * groups_of(p.c) + part * (kPartPages / 16);
-    score_items<D>(p, first + (threadIdx.x >> 5),
-                   min(first + kPartPages / 16, (u.at + 1) * groups_of(p.c)), kWarps,
+    // (an item a warp: the step leads out of the unit)
+    score_items<D>(p, Items((int)u.at, part * kWarps + (threadIdx.x >> 5), groups_of(p.c),
+                            (int)u.at + 1, groups_of(p.c)),
                    (const T *)nullptr);
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -721,9 +735,11 @@ __global__ void __launch_bounds__(kThreads, 2) select_kernel(const __grid_consta
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 2) score_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
-  const long long all = (long long)p.c.S * p.nl * p.c.H * groups_of(p.c);
-  score_items<D>(p, (long long)blockIdx.x * kWarps + (threadIdx.x >> 5), all,
-                 (long long)gridDim.x * kWarps, (const T *)nullptr);
+  const int groups = groups_of(p.c);
+  const unsigned warp = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  score_items<D>(p, Items(warp / groups, warp % groups, gridDim.x * kWarps,
+                          p.c.S * p.nl * p.c.H, groups),
+                 (const T *)nullptr);
 }
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant__ SelectParams p) {
