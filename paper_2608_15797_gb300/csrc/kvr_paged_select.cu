@@ -343,77 +343,79 @@ __device__ K nth(int n, int need, int top, F key, unsigned *hist, int *s_digit, 
   return prefix;
 }
 
-// One warp: a page's score in 64 bits, as a key.  (All heads at once: a chain of
-// them costs the latency of as many sums.)  No bounds: 0, below every score's.
+// Scoring again, a warp a page: four lanes a head, each a quarter of the channels in a
+// row.  q lies on chip as fp32, quarters apart so that 32 lanes hit 32 banks.
+template <int D>
+__device__ __forceinline__ int q_at(int g, int channel) {
+  return g * (D + 4) + channel + channel / (D / 4);
+}
+// f(w, k) for the lane's channels, k the bound that q's sign asks for.
+template <typename T, int D, typename F>
+__device__ __forceinline__ void each_term(const float *q, const T *b, int lane, F f) {
+  constexpr int kN = D / 4, kVec = 16 / (int)sizeof(T);
+  const float *w = q + q_at<D>(lane >> 2, (lane & 3) * kN);
+  const uint4 *lo = reinterpret_cast<const uint4 *>(b + (lane & 3) * kN);
+  const uint4 *hi = reinterpret_cast<const uint4 *>(b + D + (lane & 3) * kN);
+#pragma unroll
+  for (int i = 0; i < kN / kVec; ++i) {
+    const uint4 x = lo[i], y = hi[i];
+    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const float v = w[i * kVec + e];
+      uint32_t k = v > 0.f ? ys[e * (int)sizeof(T) / 4] : xs[e * (int)sizeof(T) / 4];
+      if (sizeof(T) == 2) k = e & 1 ? k & 0xFFFF0000u : k << 16;
+      f(e & 1, v, __uint_as_float(k));
+    }
+  }
+}
+
+// A page's score in 64 bits, as a key.  No bounds: 0, below every score's.
 template <typename T, int D>
-__device__ __forceinline__ unsigned long long exact_key(const T *q, const T *b, int G, int lane) {
+__device__ __forceinline__ unsigned long long exact_key(const float *q, const T *b, int G,
+                                                        int lane) {
   if (!b) return 0;
-  constexpr int kPer = D / 32;
-  double lo[kPer], hi[kPer], z[kHeads];
+  double z = 0.0;
+  each_term<T, D>(q, b, lane, [&](int, float w, float k) { z += (double)w * (double)k; });
+  z += __shfl_xor_sync(0xffffffffu, z, 1);
+  z += __shfl_xor_sync(0xffffffffu, z, 2);
+  unsigned long long best = (lane >> 2) < G ? key64(z) : 0;
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    lo[e] = (double)to_f(b[e * 32 + lane]);
-    hi[e] = (double)to_f(b[D + e * 32 + lane]);
-  }
-#pragma unroll
-  for (int g = 0; g < kHeads; ++g) {
-    z[g] = 0.0;
-    if (g < G)
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const float w = to_f(q[g * D + e * 32 + lane]);
-        z[g] += (double)w * (w > 0.f ? hi[e] : lo[e]);
-      }
-  }
-  unsigned long long best = 0;
-#pragma unroll
-  for (int g = 0; g < kHeads; ++g) {
-    if (g >= G) continue;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) z[g] += __shfl_xor_sync(0xffffffffu, z[g], o);
-    const unsigned long long y = key64(z[g]);
+  for (int o = 4; o < 32; o <<= 1) {
+    const unsigned long long y = __shfl_xor_sync(0xffffffffu, best, o);
     best = y > best ? y : best;
   }
   return best;
 }
 
-// One warp: a page's score less t, from sums held as two floats: within 2^-35 of the
-// sum of magnitudes where the score is within 2^-12 of it from t (products by fma, the
-// sums' errors kept: 2^-40; then one rounding of the difference).
+// A page's score less t, from sums held as two floats: within 2^-35 of the sum of
+// magnitudes where the score is within 2^-12 of it from t (products by fma, the sums'
+// errors kept: 2^-40; then one rounding of the difference).
 __device__ __forceinline__ void add_exact(float &hi, float &lo, float x) {
   const float s = __fadd_rn(hi, x), b = __fsub_rn(s, hi);
   lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(x, b)));
   hi = s;
 }
 template <typename T, int D>
-__device__ __forceinline__ float near_offset(const T *q, const T *b, int G, float t, int lane) {
+__device__ __forceinline__ float near_offset(const float *q, const T *b, int G, float t, int lane) {
   if (!b) return -INFINITY;
-  constexpr int kPer = D / 32;
-  float least[kPer], most[kPer], best = -INFINITY;
+  float hi[2] = {0.f, 0.f}, lo[2] = {0.f, 0.f};
+  each_term<T, D>(q, b, lane, [&](int i, float w, float k) {
+    const float x = __fmul_rn(w, k);
+    add_exact(hi[i], lo[i], x);
+    if (sizeof(T) == 4) lo[i] = __fadd_rn(lo[i], __fmaf_rn(w, k, -x));  // (bf16: exact)
+  });
+  lo[0] = __fadd_rn(lo[0], lo[1]);
+  add_exact(hi[0], lo[0], hi[1]);
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) {
-    least[e] = to_f(b[e * 32 + lane]);
-    most[e] = to_f(b[D + e * 32 + lane]);
+  for (int o = 1; o < 4; o <<= 1) {
+    const float h2 = __shfl_xor_sync(0xffffffffu, hi[0], o);
+    lo[0] = __fadd_rn(lo[0], __shfl_xor_sync(0xffffffffu, lo[0], o));
+    add_exact(hi[0], lo[0], h2);
   }
+  float best = (lane >> 2) < G ? __fadd_rn(__fsub_rn(hi[0], t), lo[0]) : -INFINITY;
 #pragma unroll
-  for (int g = 0; g < kHeads; ++g) {
-    float hi = 0.f, lo = 0.f;
-    if (g < G)
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const float w = to_f(q[g * D + e * 32 + lane]), k = w > 0.f ? most[e] : least[e];
-        const float x = __fmul_rn(w, k);
-        add_exact(hi, lo, x);
-        lo = __fadd_rn(lo, __fmaf_rn(w, k, -x));
-      }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float h2 = __shfl_xor_sync(0xffffffffu, hi, o), l2 = __shfl_xor_sync(0xffffffffu, lo, o);
-      lo = __fadd_rn(lo, l2);
-      add_exact(hi, lo, h2);
-    }
-    if (g < G) best = nan_max(best, __fadd_rn(__fsub_rn(hi, t), lo));
-  }
+  for (int o = 4; o < 32; o <<= 1) best = nan_max(best, __shfl_xor_sync(0xffffffffu, best, o));
   return best;
 }
 
@@ -430,6 +432,8 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   __shared__ unsigned s_held[kHeld + kHeld / 32];
   __shared__ unsigned s_near[kThreads];  // keys of a digit; pages to be scored again
   __shared__ unsigned long long s_key[kThreads];
+  __shared__ const T *s_at[kThreads];
+  __shared__ float s_q[kHeads * (D + 4)];
   __shared__ float s_off[kThreads];
   __shared__ bool s_open[kThreads];
   const View &c = p.c;
@@ -451,7 +455,20 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   }
   float2 *sc = p.score + u.at * p.sstride;
   auto place = [](int i) { return i + (i >> 5); };  // (threads read runs of keys)
+  constexpr int kBatch = 8;  // keys of a thread that are read together
   auto held = [&](int i) { return i < kHeld ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
+  // f(i, key) for the thread's share of the keys.
+  auto each = [&](auto f) {
+    for (int i0 = tid; i0 < old; i0 += kBatch * kThreads) {
+      unsigned k[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r)
+        if (i0 + r * kThreads < old) k[r] = held(i0 + r * kThreads);
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r)
+        if (i0 + r * kThreads < old) f(i0 + r * kThreads, k[r]);
+    }
+  };
   // Keys above `top` stay, those from `low` to it do if there is room for all of
   // them; else their scores in 64 bits say which.
   unsigned low, top;
@@ -463,14 +480,27 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
     float err = 0.f;
     unsigned least = ~0u, most = 0;
     hist[tid] = 0;
-#pragma unroll 8
-    for (int i = 2 * tid; i < old; i += 2 * kThreads) {
-      // (the last one's neighbour is there, and not counted)
-      const float4 x = __ldcg(reinterpret_cast<const float4 *>(sc + i));
-      const unsigned k0 = key32(x.x), k1 = i + 1 < old ? key32(x.z) : k0;
-      if (i < kHeld) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
-      err = nan_max(err, i + 1 < old ? nan_max(x.y, x.w) : x.y);
-      least = min(least, min(k0, k1)), most = max(most, max(k0, k1));
+    {
+      const T *q = static_cast<const T *>(p.q) + u.at * c.G * D;
+      for (int i = tid; i < kHeads * D; i += kThreads)
+        s_q[q_at<D>(i / D, i % D)] = i < c.G * D ? to_f(q[i]) : 0.f;
+    }
+    for (int i0 = 2 * tid; i0 < old; i0 += 2 * kBatch * kThreads) {
+      float4 x[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r)
+        if (i0 + 2 * r * kThreads < old)
+          x[r] = __ldcg(reinterpret_cast<const float4 *>(sc + i0 + 2 * r * kThreads));
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        const int i = i0 + 2 * r * kThreads;
+        if (i >= old) break;
+        // (the last one's neighbour is there, and not counted)
+        const unsigned k0 = key32(x[r].x), k1 = i + 1 < old ? key32(x[r].z) : k0;
+        if (i < kHeld) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
+        err = nan_max(err, i + 1 < old ? nan_max(x[r].y, x[r].w) : x[r].y);
+        least = min(least, min(k0, k1)), most = max(most, max(k0, k1));
+      }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) err = nan_max(err, __shfl_xor_sync(0xffffffffu, err, o));
@@ -496,19 +526,16 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
       auto part = [&](unsigned k) {
         return (unsigned)fminf(fmaxf((value32(k) - from) * scale, 0.f), 255.f);
       };
-#pragma unroll 8
-      for (int i = tid; i < old; i += kThreads) atomicAdd(&hist[part(held(i))], 1u);
+      each([&](int, unsigned k) { atomicAdd(&hist[part(k)], 1u); });
       __syncthreads();
       if (warp == 0) digit_of(hist, B, lane, &s_digit, &s_left);
       __syncthreads();
       const unsigned d = s_digit;
       const int left = s_left, in = (int)hist[d];
       if (in <= kThreads) {
-#pragma unroll 8
-        for (int i = tid; i < old; i += kThreads) {
-          const unsigned k = held(i);
+        each([&](int, unsigned k) {
           if (part(k) == d) s_near[atomicAdd(&s_few, 1)] = k;
-        }
+        });
         __syncthreads();
         if (tid < in) {
           const unsigned mine = s_near[tid];
@@ -534,28 +561,27 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
     low = all ? 0u : key32(__fadd_rd(t, -2.f * err));
     auto is_near = [&](unsigned x) { return all || (x >= low && x <= top); };
     int n_sure = 0;
-#pragma unroll 8
-    for (int i = tid; i < old; i += kThreads) {
-      const unsigned x = held(i);
+    each([&](int i, unsigned x) {
       n_sure += !all && x > top;
       if (is_near(x)) {
         const int at = atomicAdd(&s_few, 1);
         if (at < kThreads) s_near[at] = i;
       }
-    }
+    });
     n_sure = __reduce_add_sync(0xffffffffu, n_sure);
     if (lane == 0) atomicAdd(&s_sure, n_sure);
     __syncthreads();
     const int near = s_few, need = B - s_sure;
-    const T *q = static_cast<const T *>(p.q) + u.at * c.G * D;
     if (near == need) {
       // all of them stay
     } else if (near <= kThreads && old <= kHeld) {
       // Few: what two floats say of each, and 64 bits of those they leave open; keys
       // on chip then say who stays.  (64-bit arithmetic runs at 1/64 of the rate: ten
       // pages cost 9 us with it alone.)
+      if (tid < near) s_at[tid] = bounds_of<T>(c, u.l, u.s, u.h, s_near[tid]);
+      __syncthreads();
       for (int k = warp; k < near; k += kWarps) {
-        const float y = near_offset<T, D>(q, bounds_of<T>(c, u.l, u.s, u.h, s_near[k]), c.G, t, lane);
+        const float y = near_offset<T, D>(s_q, s_at[k], c.G, t, lane);
         if (lane == 0) s_off[k] = y;
       }
       __syncthreads();
@@ -575,8 +601,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
       if (__syncthreads_or(open)) {
         for (int k = warp; k < near; k += kWarps) {
           if (!s_open[k]) continue;
-          const unsigned long long y =
-              exact_key<T, D>(q, bounds_of<T>(c, u.l, u.s, u.h, s_near[k]), c.G, lane);
+          const unsigned long long y = exact_key<T, D>(s_q, s_at[k], c.G, lane);
           if (lane == 0) s_key[k] = y;
         }
         __syncthreads();
@@ -602,7 +627,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
           const int at = __ffs(ask) - 1;
           ask &= ask - 1;
           const unsigned long long y =
-              exact_key<T, D>(q, bounds_of<T>(c, u.l, u.s, u.h, i0 + at), c.G, lane);
+              exact_key<T, D>(s_q, bounds_of<T>(c, u.l, u.s, u.h, i0 + at), c.G, lane);
           if (lane == at) key = y;
         }
         if (i < old) keys[i] = key;
