@@ -234,19 +234,8 @@ __global__ void __launch_bounds__(kFill) fill_kernel(const __grid_constant__ Vie
 template <int N>
 cudaError_t launch_plan(const View &c, const int32_t *lens, int n_new, int32_t *slots,
                         cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kCluster);
-  cfg.blockDim = dim3(N);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kCluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, plan_kernel<N>, c, lens, n_new, slots);
+  return kvr::launch_pdl_cluster(plan_kernel<N>, dim3(kCluster), dim3(N), kCluster, 0, st, c, lens,
+                                 n_new, slots);
 }
 
 // ---- append -----------------------------------------------------------------

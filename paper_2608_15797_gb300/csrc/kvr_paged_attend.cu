@@ -45,6 +45,34 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// A place in the shared memory of a CTA of the cluster, and what lies there.
+__device__ __forceinline__ uint32_t in_cta(uint32_t here, unsigned rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(here), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float4 ld4_cluster(uint32_t at) {
+  float4 x;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+               : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
+               : "r"(at)
+               : "memory");
+  return x;
+}
+__device__ __forceinline__ float2 ld2_cluster(uint32_t at) {
+  float2 x;
+  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];"
+               : "=f"(x.x), "=f"(x.y)
+               : "r"(at)
+               : "memory");
+  return x;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
+          : "memory");
+}
+
 template <typename T>
 struct Elems;
 template <>
@@ -348,7 +376,9 @@ struct Piece {
   unsigned begin;
 };
 
-template <typename T, int D, typename P, typename O>
+// kCluster > 1: a cluster a unit, whose parts are joined through the CTAs' shared
+// memory.
+template <typename T, int D, typename P, typename O, int kCluster>
 __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_constant__ AttendParams p) {
   kvr::pdl_begin();
   using S = Shape<T, D>;
@@ -373,9 +403,22 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
   uint8_t *own = smem + kWarps * (kStages * S::kStage + kPart * 4) + warp * P::kOwn;
   const uint32_t ring32 = smem_u32(ring);
   const unsigned U = p.nl * c.H;  // units of a sequence
-  const unsigned total = tiles * U, warps = gridDim.x * kWarps;
-  const unsigned span = max((unsigned)kLeast, (total + warps - 1) / warps);
-  const unsigned t0 = min(total, (blockIdx.x * kWarps + warp) * span), t1 = min(total, t0 + span);
+  unsigned t0, t1, span;  // the warp's tiles
+  int many = 0;           // CTAs of the cluster that have any
+  if constexpr (kCluster > 1) {
+    const unsigned unit = blockIdx.x / kCluster, s = unit / U, base = p.src.tiles[s];
+    const unsigned n = p.src.tiles[s + 1] - base, from = base * U + (unit - s * U) * n;
+    const unsigned mine = blockIdx.x % kCluster * kWarps + warp;
+    span = max((n + kCluster * kWarps - 1) / (kCluster * kWarps), 1u);
+    t0 = from + min(n, mine * span);
+    t1 = from + min(n, (mine + 1) * span);
+    many = (n + span * kWarps - 1) / (span * kWarps);
+  } else {
+    const unsigned total = tiles * U, warps = gridDim.x * kWarps;
+    span = max((unsigned)kLeast, (total + warps - 1) / warps);
+    t0 = min(total, (blockIdx.x * kWarps + warp) * span);
+    t1 = min(total, t0 + span);
+  }
 
   auto locate = [&](unsigned t) {
     // the last sequence that starts at or before t, 32 of them asked at a time
@@ -545,7 +588,9 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
     const int upto = __shfl_sync(0xffffffffu, mine.upto, 31 - __clz(same));
     const bool whole = first == 0 && upto == n;
     const int which = first == 0;
-    float *part = p.parts + (2ll * blockIdx.x + which) * kPart;
+    // (in a cluster nobody has an early piece: the CTA's part goes there)
+    float *part = kCluster > 1 ? reinterpret_cast<float *>(smem + kWarps * kStages * S::kStage)
+                               : p.parts + (2ll * blockIdx.x + which) * kPart;
 #pragma unroll
     for (int y = 0; y < kMine; ++y) {
       const int x = threadIdx.x + y * kThreads, g = x / (D / 4);
@@ -587,7 +632,44 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
       owed_begin[0] = which ? owed_begin[0] : begin, owed_begin[1] = which ? begin : owed_begin[1];
     }
   }
-  if (owed[0] >= 0 || owed[1] >= 0) {
+  if constexpr (kCluster > 1) {
+    if (many > 1) {
+      cluster_sync();
+      constexpr int kSlice = kHeads * D / 4 / kCluster;  // of the outputs, a CTA's
+      static_assert(kHeads * D / 4 % kCluster == 0 && kSlice <= kThreads, "slices");
+      const unsigned here = smem_u32(smem + kWarps * kStages * S::kStage);
+      const int x = blockIdx.x % kCluster * kSlice + threadIdx.x, g = x / (D / 4);
+      if ((int)threadIdx.x < kSlice && g < c.G) {
+        float2 ms[kCluster];
+        float4 w[kCluster];
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+          ms[k] = make_float2(-INFINITY, 0.f);
+          w[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k < many) {
+            const uint32_t at = in_cta(here, k);
+            ms[k] = ld2_cluster(at + (kStats + 2 * g) * 4);
+            w[k] = ld4_cluster(at + x * 16);
+          }
+        }
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) m = fmaxf(m, ms[k].x);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < kCluster; ++k) {
+          const float a = ex2(ms[k].x - ref);
+          v.x = fmaf(w[k].x, a, v.x), v.y = fmaf(w[k].y, a, v.y);
+          v.z = fmaf(w[k].z, a, v.z), v.w = fmaf(w[k].w, a, v.w);
+          s = fmaf(ms[k].y, a, s);
+        }
+        put(out_of(blockIdx.x / kCluster) + 4 * x, v, s);
+      }
+      cluster_sync();  // nobody leaves while its part is read
+    }
+  } else if (owed[0] >= 0 || owed[1] >= 0) {
     // CTAs that share the unit: the first has its part behind, the others before
     unsigned from[2], many[2];
 #pragma unroll
@@ -731,17 +813,28 @@ struct Choice<__nv_bfloat16, D> {
   using P = Mma<D>;
 };
 
-template <typename T, int D>
-cudaError_t prepare() {
+// CTAs of a unit's cluster, where the call has few tiles.
+constexpr int kUnitCtas = 16;
+
+template <typename T, int D, typename O>
+cudaError_t prepare_as() {
   using P = typename Choice<T, D>::P;
   constexpr size_t bytes = smem_bytes<T, D, P>();
-  static_assert(bytes + 2 * P::kWarps * sizeof(Piece) + 64 <= 227 * 1024, "shared memory");
-  cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, P, float>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  static_assert(bytes + 2 * P::kWarps * (sizeof(Piece) + 32) + 64 <= 227 * 1024, "shared memory");
+  constexpr auto kSize = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, 1>, kSize, (int)bytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attend_kernel<T, D, P, __nv_bfloat16>,
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, kUnitCtas>, kSize, (int)bytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, kUnitCtas>,
+                             cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   return e;
+}
+
+template <typename T, int D>
+cudaError_t prepare() {
+  const cudaError_t e = prepare_as<T, D, float>();
+  return e == cudaSuccess ? prepare_as<T, D, __nv_bfloat16>() : e;
 }
 
 // CTAs of a launch: as many as run at once, or several times as many, where the
@@ -752,21 +845,37 @@ int ctas_of(const AttendParams &p, int sms) {
   using P = typename Choice<T, D>::P;
   // (of an SM's 228 KB a CTA takes 1 KB more than it asks for)
   constexpr int kResident =
-      228 * 1024 / (int)(smem_bytes<T, D, P>() + 2 * P::kWarps * sizeof(Piece) + 64 + 1024);
+      228 * 1024 / (int)(smem_bytes<T, D, P>() + 2 * P::kWarps * (sizeof(Piece) + 32) + 64 + 1024);
   static_assert(kResident >= 1, "shared memory");
   const int at_once = std::min(sms * kResident, kMaxCtas);
   const long long waves = p.most / ((long long)at_once * P::kWarps * 24);
   return at_once * (int)std::max(1ll, std::min<long long>(waves, std::min(8, kMaxCtas / at_once)));
 }
 
+// A cluster a unit: where all of them run at once and even the largest call gives a
+// warp no more than 8 tiles.  Parts then meet in shared memory and not across the
+// L2's halves.  us a call, one sequence of 4,099 rows (4 units): 8 and 12.
+bool small_call(const AttendParams &p, int sms) {
+  const long long units = (long long)p.c.S * p.nl * p.c.H;
+  return units * kUnitCtas <= sms && p.most <= units * kUnitCtas * 4 * 8;
+}
+
+template <typename T, int D, typename O>
+cudaError_t launch_as(const AttendParams &p, int sms, cudaStream_t st) {
+  using P = typename Choice<T, D>::P;
+  constexpr size_t bytes = smem_bytes<T, D, P>();
+  const dim3 block(P::kWarps * 32);
+  if (!small_call(p, sms))
+    return kvr::launch_pdl(attend_kernel<T, D, P, O, 1>, dim3(ctas_of<T, D>(p, sms)), block, bytes,
+                           st, p);
+  return kvr::launch_pdl_cluster(attend_kernel<T, D, P, O, kUnitCtas>,
+                                 dim3(p.c.S * p.nl * p.c.H * kUnitCtas), block, kUnitCtas, bytes,
+                                 st, p);
+}
+
 template <typename T, int D>
 cudaError_t launch(const AttendParams &p, int sms, cudaStream_t st) {
-  using P = typename Choice<T, D>::P;
-  const dim3 grid(ctas_of<T, D>(p, sms)), block(P::kWarps * 32);
-  return p.c.out_bf16 ? kvr::launch_pdl(attend_kernel<T, D, P, __nv_bfloat16>, grid, block,
-                                        smem_bytes<T, D, P>(), st, p)
-                      : kvr::launch_pdl(attend_kernel<T, D, P, float>, grid, block,
-                                        smem_bytes<T, D, P>(), st, p);
+  return p.c.out_bf16 ? launch_as<T, D, __nv_bfloat16>(p, sms, st) : launch_as<T, D, float>(p, sms, st);
 }
 
 }  // namespace
