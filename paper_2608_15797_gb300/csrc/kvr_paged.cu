@@ -110,8 +110,8 @@ __device__ __forceinline__ int find(const int *start, int e) {
 // Token t of a sequence's growth: its slot, and its page's entry in the table where
 // the page is new.  Pages behind the first `have` are the stack's, from `top` down.
 __device__ __forceinline__ int place(const View &c, int s, int t, int from, int len, int top) {
+  if (t >= len - from) return -1;
   const int pos = from + t;
-  if (pos >= len) return -1;
   const int at = pos >> c.psh, have = (from + c.P - 1) >> c.psh;
   int32_t *entry = c.table + (long long)s * c.tstride + at;
   const int page = at < have ? *entry : c.stack[top - (at - have)];
@@ -374,7 +374,7 @@ using kvr::paged::View;
 struct kvr_paged {
   kvr_paged_desc desc;
   View view;
-  int sms = 0;
+  kvr::paged::Device device;
   uint64_t launches = 0;
 };
 
@@ -485,7 +485,7 @@ Work work_of(const kvr_paged *c, int nl, int budget, int window) {
   p.c = c->view;
   p.nl = nl;
   p.most = most_tiles(c, nl, w.keep);
-  w.parts = take((size_t)2 * kvr::paged::attend_ctas(p, c->sms) *
+  w.parts = take((size_t)2 * kvr::paged::attend_ctas(p, c->device) *
                  kvr::paged::part_floats(d.head_dim) * sizeof(float));
   if (window > 0) {
     const size_t units = (size_t)d.n_seq * nl * d.n_kv_heads;
@@ -550,17 +550,13 @@ kvr_status kvr_paged_create(const kvr_paged_desc *desc, void *dev_buf, size_t by
                                       : 1.0f / std::sqrt((float)desc->head_dim);
   v.io_bf16 = desc->kv_dtype == KVR_BF16;
   v.out_bf16 = desc->out_dtype == KVR_BF16;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess)
-    e = cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = kvr::paged::prepare_attend(v);
+  cudaError_t e = kvr::paged::prepare_attend(v, &c->device);
   // tickets and the error word lie side by side
   if (e == cudaSuccess)
     e = cudaMemsetAsync(b + l.ticket, 0, l.total - l.ticket, as_stream(stream));
   if (e == cudaSuccess) {
     const long long most = std::max<long long>((long long)v.S * v.tstride, v.n_pages);
-    const int grid = (int)std::min<long long>((most + 255) / 256, 4ll * c->sms);
+    const int grid = (int)std::min<long long>((most + 255) / 256, 4ll * c->device.sms);
     e = kvr::launch_pdl(kvr::paged::init_kernel, dim3(grid), dim3(256), 0, as_stream(stream), v);
   }
   if (e != cudaSuccess) {
@@ -622,11 +618,11 @@ kvr_status kvr_paged_append(kvr_paged *c, int lb, int le, int n, int n_new,
   const cudaStream_t cs = as_stream(stream);
   cudaError_t e;
   if (c->view.io_bf16)
-    e = c->view.d == 128 ? kvr::paged::launch_append<__nv_bfloat16, 128>(p, c->sms, cs)
-                         : kvr::paged::launch_append<__nv_bfloat16, 64>(p, c->sms, cs);
+    e = c->view.d == 128 ? kvr::paged::launch_append<__nv_bfloat16, 128>(p, c->device.sms, cs)
+                         : kvr::paged::launch_append<__nv_bfloat16, 64>(p, c->device.sms, cs);
   else
-    e = c->view.d == 128 ? kvr::paged::launch_append<float, 128>(p, c->sms, cs)
-                         : kvr::paged::launch_append<float, 64>(p, c->sms, cs);
+    e = c->view.d == 128 ? kvr::paged::launch_append<float, 128>(p, c->device.sms, cs)
+                         : kvr::paged::launch_append<float, 64>(p, c->device.sms, cs);
   if (e != cudaSuccess) return cuda_fail("kvr_paged_append", e);
   c->launches += 1;
   return KVR_OK;
@@ -663,7 +659,7 @@ kvr_status kvr_paged_attend(kvr_paged *c, int lb, int le, const void *q, void *o
   p.out = out;
   p.most = most_tiles(c, p.nl, 0);
   p.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.parts);
-  const cudaError_t e = kvr::paged::launch_attend(p, c->sms, as_stream(stream));
+  const cudaError_t e = kvr::paged::launch_attend(p, c->device, as_stream(stream));
   if (e != cudaSuccess) return cuda_fail("kvr_paged_attend", e);
   c->launches += 1;
   return KVR_OK;
@@ -699,7 +695,7 @@ kvr_status kvr_paged_attend_pages(kvr_paged *c, int lb, int le, const void *q, i
   s.tiles = reinterpret_cast<int32_t *>(ws + w.tiles);
   s.chosen = pages;
   int n = 0;
-  cudaError_t e = kvr::paged::launch_select(s, c->sms, as_stream(stream), &n);
+  cudaError_t e = kvr::paged::launch_select(s, c->device.sms, as_stream(stream), &n);
   c->launches += n;
   if (e != cudaSuccess) return cuda_fail("kvr_paged_attend_pages: choice", e);
   const long long units = (long long)(le - lb) * v.H;
@@ -712,7 +708,7 @@ kvr_status kvr_paged_attend_pages(kvr_paged *c, int lb, int le, const void *q, i
   p.out = out;
   p.most = most_tiles(c, p.nl, w.keep);
   p.parts = reinterpret_cast<float *>(ws + w.parts);
-  e = kvr::paged::launch_attend(p, c->sms, as_stream(stream));
+  e = kvr::paged::launch_attend(p, c->device, as_stream(stream));
   if (e != cudaSuccess) return cuda_fail("kvr_paged_attend_pages", e);
   c->launches += 1;
   return KVR_OK;

@@ -54,11 +54,17 @@ struct AttendParams {
 };
 __host__ __device__ constexpr int part_floats(int d) { return kHeads * d + 2 * kHeads; }
 
+// What launches need to know of the handle's device, which is the current one when
+// the handle is made (limits of shared memory are raised then too).
+struct Device {
+  int sms;
+  int clusters;  // of units, that run at once
+};
 // CTAs of a launch, a matter of p.c, p.nl and p.most.
 constexpr int kMostCtas = 2560;
-int attend_ctas(const AttendParams &p, int sms);
-cudaError_t prepare_attend(const View &c);
-cudaError_t launch_attend(const AttendParams &p, int sms, cudaStream_t st);
+int attend_ctas(const AttendParams &p, const Device &dev);
+cudaError_t prepare_attend(const View &c, Device *dev);
+cudaError_t launch_attend(const AttendParams &p, const Device &dev, cudaStream_t st);
 
 // The choice of pages over layers [lb, lb + nl): scores, then each unit's list of
 // pool pages in ascending order of position, and what the attention reads of it.
@@ -70,6 +76,7 @@ struct SelectParams {
   int keep;           // pages of a list
   float2 *score;      // [unit of the call][sstride]: score, bound of its error
   int sstride;        // even
+  int held;           // scores of a unit that are held on chip, even
   int32_t *list;      // [unit][keep]
   int32_t *rows;      // [S]
   int32_t *tiles;     // [S + 1]

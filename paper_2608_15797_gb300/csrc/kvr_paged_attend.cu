@@ -817,56 +817,67 @@ struct Choice<__nv_bfloat16, D> {
 constexpr int kUnitCtas = 16;
 
 template <typename T, int D, typename O>
-cudaError_t prepare_as() {
+cudaError_t prepare_as(int *clusters) {
   using P = typename Choice<T, D>::P;
   constexpr size_t bytes = smem_bytes<T, D, P>();
   static_assert(bytes + 2 * P::kWarps * (sizeof(Piece) + 32) + 64 <= 227 * 1024, "shared memory");
   constexpr auto kSize = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  constexpr auto unit = attend_kernel<T, D, P, O, kUnitCtas>;
   cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, 1>, kSize, (int)bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(unit, kSize, (int)bytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, kUnitCtas>, kSize, (int)bytes);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, kUnitCtas>,
-                             cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  return e;
+    e = cudaFuncSetAttribute(unit, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  // (how SMs lie in clusters' reach differs from device to device)
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kUnitCtas);
+  cfg.blockDim = dim3(P::kWarps * 32);
+  cfg.dynamicSmemBytes = bytes;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kUnitCtas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaOccupancyMaxActiveClusters(clusters, unit, &cfg);
 }
 
 template <typename T, int D>
-cudaError_t prepare() {
-  const cudaError_t e = prepare_as<T, D, float>();
-  return e == cudaSuccess ? prepare_as<T, D, __nv_bfloat16>() : e;
+cudaError_t prepare(bool bf16_out, int *clusters) {
+  return bf16_out ? prepare_as<T, D, __nv_bfloat16>(clusters) : prepare_as<T, D, float>(clusters);
 }
 
 // CTAs of a launch: as many as run at once, or several times as many, where the
 // largest call would still give every warp 24 tiles: SMs do not get the same share of
 // the memory's rate, and shorter spans even that out.
 template <typename T, int D>
-int ctas_of(const AttendParams &p, int sms) {
+int ctas_of(const AttendParams &p, const Device &dev) {
   using P = typename Choice<T, D>::P;
   // (of an SM's 228 KB a CTA takes 1 KB more than it asks for)
   constexpr int kResident =
       228 * 1024 / (int)(smem_bytes<T, D, P>() + 2 * P::kWarps * (sizeof(Piece) + 32) + 64 + 1024);
   static_assert(kResident >= 1, "shared memory");
-  const int at_once = std::min(sms * kResident, kMaxCtas);
+  const int at_once = std::min(dev.sms * kResident, kMaxCtas);
   const long long waves = p.most / ((long long)at_once * P::kWarps * 24);
   return at_once * (int)std::max(1ll, std::min<long long>(waves, std::min(8, kMaxCtas / at_once)));
 }
 
 // A cluster a unit: where all of them run at once and even the largest call gives a
 // warp no more than 8 tiles.  Parts then meet in shared memory and not across the
-// L2's halves.  us a call, one sequence of 4,099 rows (4 units): 8 and 12.
-bool small_call(const AttendParams &p, int sms) {
+// L2's halves.  us a call in a graph, one sequence of 4,099 rows (7B, 4 units): 9.1 and
+// 12.0.
+bool small_call(const AttendParams &p, const Device &dev) {
   const long long units = (long long)p.c.S * p.nl * p.c.H;
-  return units * kUnitCtas <= sms && p.most <= units * kUnitCtas * 4 * 8;
+  return units <= dev.clusters && p.most <= units * kUnitCtas * 4 * 8;
 }
 
 template <typename T, int D, typename O>
-cudaError_t launch_as(const AttendParams &p, int sms, cudaStream_t st) {
+cudaError_t launch_as(const AttendParams &p, const Device &dev, cudaStream_t st) {
   using P = typename Choice<T, D>::P;
   constexpr size_t bytes = smem_bytes<T, D, P>();
   const dim3 block(P::kWarps * 32);
-  if (!small_call(p, sms))
-    return kvr::launch_pdl(attend_kernel<T, D, P, O, 1>, dim3(ctas_of<T, D>(p, sms)), block, bytes,
+  if (!small_call(p, dev))
+    return kvr::launch_pdl(attend_kernel<T, D, P, O, 1>, dim3(ctas_of<T, D>(p, dev)), block, bytes,
                            st, p);
   return kvr::launch_pdl_cluster(attend_kernel<T, D, P, O, kUnitCtas>,
                                  dim3(p.c.S * p.nl * p.c.H * kUnitCtas), block, kUnitCtas, bytes,
@@ -874,28 +885,38 @@ cudaError_t launch_as(const AttendParams &p, int sms, cudaStream_t st) {
 }
 
 template <typename T, int D>
-cudaError_t launch(const AttendParams &p, int sms, cudaStream_t st) {
-  return p.c.out_bf16 ? launch_as<T, D, __nv_bfloat16>(p, sms, st) : launch_as<T, D, float>(p, sms, st);
+cudaError_t launch(const AttendParams &p, const Device &dev, cudaStream_t st) {
+  return p.c.out_bf16 ? launch_as<T, D, __nv_bfloat16>(p, dev, st)
+                      : launch_as<T, D, float>(p, dev, st);
 }
 
 }  // namespace
 
-int attend_ctas(const AttendParams &p, int sms) {
+int attend_ctas(const AttendParams &p, const Device &dev) {
   if (p.c.io_bf16)
-    return p.c.d == 128 ? ctas_of<__nv_bfloat16, 128>(p, sms) : ctas_of<__nv_bfloat16, 64>(p, sms);
-  return p.c.d == 128 ? ctas_of<float, 128>(p, sms) : ctas_of<float, 64>(p, sms);
+    return p.c.d == 128 ? ctas_of<__nv_bfloat16, 128>(p, dev) : ctas_of<__nv_bfloat16, 64>(p, dev);
+  return p.c.d == 128 ? ctas_of<float, 128>(p, dev) : ctas_of<float, 64>(p, dev);
 }
 
-cudaError_t prepare_attend(const View &c) {
-  if (c.io_bf16) return c.d == 128 ? prepare<__nv_bfloat16, 128>() : prepare<__nv_bfloat16, 64>();
-  return c.d == 128 ? prepare<float, 128>() : prepare<float, 64>();
+cudaError_t prepare_attend(const View &c, Device *dev) {
+  int now = 0;
+  cudaError_t e = cudaGetDevice(&now);
+  if (e == cudaSuccess)
+    e = cudaDeviceGetAttribute(&dev->sms, cudaDevAttrMultiProcessorCount, now);
+  if (e != cudaSuccess) return e;
+  const bool out = c.out_bf16 != 0;
+  if (c.io_bf16)
+    return c.d == 128 ? prepare<__nv_bfloat16, 128>(out, &dev->clusters)
+                      : prepare<__nv_bfloat16, 64>(out, &dev->clusters);
+  return c.d == 128 ? prepare<float, 128>(out, &dev->clusters)
+                    : prepare<float, 64>(out, &dev->clusters);
 }
 
-cudaError_t launch_attend(const AttendParams &p, int sms, cudaStream_t st) {
+cudaError_t launch_attend(const AttendParams &p, const Device &dev, cudaStream_t st) {
   if (p.c.io_bf16)
-    return p.c.d == 128 ? launch<__nv_bfloat16, 128>(p, sms, st)
-                        : launch<__nv_bfloat16, 64>(p, sms, st);
-  return p.c.d == 128 ? launch<float, 128>(p, sms, st) : launch<float, 64>(p, sms, st);
+    return p.c.d == 128 ? launch<__nv_bfloat16, 128>(p, dev, st)
+                        : launch<__nv_bfloat16, 64>(p, dev, st);
+  return p.c.d == 128 ? launch<float, 128>(p, dev, st) : launch<float, 64>(p, dev, st);
 }
 
 }  // namespace paged

@@ -419,7 +419,7 @@ __device__ __forceinline__ float near_offset(const float *q, const T *b, int G, 
   return best;
 }
 
-constexpr int kHeld = 8192;  // scores of a unit that are held on chip
+constexpr int kHeld = 8192;  // scores of a unit that are held on chip, at most
 
 // The choice for one unit, whose scores are there.  The whole CTA.
 template <typename T, int D>
@@ -429,7 +429,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   __shared__ int s_digit, s_left, s_stay[kWarps], s_ties[kWarps], s_sure, s_few;
   __shared__ float s_err[kWarps];
   __shared__ unsigned s_least[kWarps], s_most[kWarps], s_kth;
-  __shared__ unsigned s_held[kHeld + kHeld / 32];
+  extern __shared__ unsigned s_held[];  // [p.held], padded
   __shared__ unsigned s_near[kThreads];  // keys of a digit; pages to be scored again
   __shared__ unsigned long long s_key[kThreads];
   __shared__ const T *s_at[kThreads];
@@ -456,7 +456,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
   float2 *sc = p.score + u.at * p.sstride;
   auto place = [](int i) { return i + (i >> 5); };  // (threads read runs of keys)
   constexpr int kBatch = 8;  // keys of a thread that are read together
-  auto held = [&](int i) { return i < kHeld ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
+  auto held = [&](int i) { return i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
   // f(i, key) for the thread's share of the keys.
   auto each = [&](auto f) {
     for (int i0 = tid; i0 < old; i0 += kBatch * kThreads) {
@@ -497,7 +497,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
         if (i >= old) break;
         // (the last one's neighbour is there, and not counted)
         const unsigned k0 = key32(x[r].x), k1 = i + 1 < old ? key32(x[r].z) : k0;
-        if (i < kHeld) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
+        if (i < p.held) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
         err = nan_max(err, i + 1 < old ? nan_max(x[r].y, x[r].w) : x[r].y);
         least = min(least, min(k0, k1)), most = max(most, max(k0, k1));
       }
@@ -574,7 +574,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
     const int near = s_few, need = B - s_sure;
     if (near == need) {
       // all of them stay
-    } else if (near <= kThreads && old <= kHeld) {
+    } else if (near <= kThreads && old <= p.held) {
       // Few: what two floats say of each, and 64 bits of those they leave open; keys
       // on chip then say who stays.  (64-bit arithmetic runs at 1/64 of the rate: ten
       // pages cost 9 us with it alone.)
@@ -767,7 +767,7 @@ __global__ void __launch_bounds__(kThreads, 2) score_kernel(const __grid_constan
                  (const T *)nullptr);
 }
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(kThreads, 5) choose_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
   if (blockIdx.x == 0) return sequences(p);
   choose<T, D>(p, unit_of(p, blockIdx.x - 1));
@@ -778,16 +778,20 @@ cudaError_t launch(SelectParams p, int sms, cudaStream_t st, int *launches) {
   const long long units = (long long)p.c.S * p.nl * p.c.H;
   p.parts = p.budget > 0 ? (p.c.tstride + kPartPages - 1) / kPartPages : 1;
   const long long jobs = units * p.parts;
+  p.held = std::min(p.sstride, kHeld);  // (both even)
+  const size_t smem = (p.held + p.held / 32) * sizeof(unsigned);
   cudaError_t e;
   if (p.budget == 0 || jobs <= 2 * sms) {
     if (jobs >= 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-    e = kvr::launch_pdl(select_kernel<T, D>, dim3((unsigned)jobs + 1), dim3(kThreads), 0, st, p);
+    e = kvr::launch_pdl(select_kernel<T, D>, dim3((unsigned)jobs + 1), dim3(kThreads), smem, st,
+                        p);
   } else {
     e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(jobs, 8ll * sms)),
                         dim3(kThreads), 0, st, p);
     if (e != cudaSuccess) return e;
     *launches += 1;
-    e = kvr::launch_pdl(choose_kernel<T, D>, dim3((unsigned)units + 1), dim3(kThreads), 0, st, p);
+    e = kvr::launch_pdl(choose_kernel<T, D>, dim3((unsigned)units + 1), dim3(kThreads), smem, st,
+                        p);
   }
   if (e == cudaSuccess) *launches += 1;
   return e;

@@ -1155,9 +1155,13 @@ class PagedCache:
     def _at(self, stream):
         """The call's stream; a ValueError where kernels would run on another
         device than the cache's."""
-        if _raw_device is not None and _raw_device() != self._device:
-            raise ValueError(f"the cache lies on cuda:{self._device}, the "
-                             f"current device is cuda:{_raw_device()}")
+        if _raw_device is not None:
+            now = _raw_device()
+            if now != self._device:
+                raise ValueError(f"the cache lies on cuda:{self._device}, the "
+                                 f"current device is cuda:{now}")
+            if stream is None and _raw_stream is not None:
+                return _raw_stream(now)
         return _stream(stream)
 
     def _tensor(self, x, shape, dtype, what):

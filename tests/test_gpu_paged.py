@@ -327,6 +327,52 @@ def test_attend(dtype, out_dtype, d, G, page, lens):
     b.c.sync_status()
 
 
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 7), ("bf16", 64, 8),
+                                       ("f32", 128, 5), ("f32", 64, 1)])
+@pytest.mark.parametrize("lens", [[1], [16], [17], [1023], [1025, 0], [5000]])
+def test_attend_few_units(dtype, d, G, lens):
+    """A layer a call: few units, from one row to some thousand."""
+    most = max(lens)
+    b = Book(len(lens), 2, 2, G, d, sum(-(-n // 16) for n in lens), 16,
+             -(-most // 16), dtype, "f32")
+    b.grow(lens)
+    q = b.queries()
+    out = torch.cat([b.c.attend(dev(q[:, l:l + 1], dtype), layers=(l, l + 1))
+                     for l in range(2)], 1)
+    b.check_out(q, out.cpu().numpy())
+    b.c.sync_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_long_unit(dtype):
+    """Shared by many CTAs: lengths around the ends of their spans."""
+    n = 40000
+    b = Book(1, 1, 1, 3, 64, n // 16, 16, n // 16, dtype, "f32")
+    b.grow([n])
+    for m in (n, n - 1, 3 * 16 * 4 * 100 + 1, 3 * 16 * 4 * 100, 12289):
+        b.plan([m])
+        b.check_attend()
+    b.c.sync_status()
+
+
+def test_several_waves():
+    """More CTAs than run at once; some units are looked at."""
+    n, P = 8000, 64
+    b = Book(8, 4, 4, 7, 128, 8 * 125, P, 125, out_dtype="f32")
+    b.grow([n, 1, 0, n - 1, n // 2, n, 77, n])
+    q = b.queries()
+    out = b.c.attend(dev(q)).cpu().numpy()
+    b.c.sync_status()
+    for s in range(8):
+        for l, h in ((0, 0), (1, 2), (3, 3)):
+            g = slice(7 * h, 7 * h + 7)
+            ref, mag, top = paged.attend(q[s, l, g], b.k[s][l, h], b.v[s][l, h])
+            some = 2 * 2.0**-16 * top[:, None] + 2.0**-18 + 2.0**-16 \
+                + (n / 16 + 64) * 2.0**-23 if len(b.k[s][l, h]) else 0
+            assert (np.abs(out[s, l, g] - ref)
+                    <= 2.0**-24 * np.abs(ref) + mag * some + 1e-30).all()
+
+
 @pytest.mark.parametrize("scale", [0.3, 1e-3])
 def test_softmax_scale(scale):
     b = Book(2, 1, 2, 4, 128, 8, 64, 4, "bf16", "f32", softmax_scale=scale)

@@ -92,7 +92,7 @@ def cache(monkeypatch):
     c.buf = torch.zeros(16, dtype=torch.uint8)
     monkeypatch.setattr(kvr, "lib", Forbidden())
     monkeypatch.setattr(kvr, "_raw_device", lambda: 0)
-    monkeypatch.setattr(kvr, "_stream", lambda s: 0)
+    monkeypatch.setattr(kvr, "_raw_stream", lambda device: 0)
     return c
 
 
