@@ -399,7 +399,7 @@ cudaStream_t as_stream(void *s) { return static_cast<cudaStream_t>(s); }
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 struct Layout {
-  size_t K, V, bounds, table, len, from, first, tiles, stack, free, ticket, uticket, err, total;
+  size_t K, V, bounds, table, len, from, first, tiles, stack, free, ticket, err, total;
 };
 
 bool layout_of(const kvr_paged_desc *d, Layout *l) {
@@ -437,7 +437,6 @@ bool layout_of(const kvr_paged_desc *d, Layout *l) {
   l->stack = take((size_t)d->n_pages * 4);
   l->free = take(2 * 4);
   l->ticket = take(kvr::paged::kMostCtas * 4);
-  l->uticket = take((size_t)d->n_seq * d->n_layers * d->n_kv_heads * 4);
   l->err = take(16);
   l->total = off;
   return true;
@@ -535,7 +534,6 @@ kvr_status kvr_paged_create(const kvr_paged_desc *desc, void *dev_buf, size_t by
   v.stack = i32(l.stack);
   v.free = i32(l.free);
   v.ticket = reinterpret_cast<unsigned *>(b + l.ticket);
-  v.uticket = reinterpret_cast<unsigned *>(b + l.uticket);
   v.err = reinterpret_cast<unsigned *>(b + l.err);
   v.S = desc->n_seq;
   v.L = desc->n_layers;

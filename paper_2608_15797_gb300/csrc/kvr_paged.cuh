@@ -25,7 +25,6 @@ struct View {
   int32_t *stack;    // [n_pages] free pages, the next one to go at free[0] - 1
   int32_t *free;     // [0]: how many; [1]: whether the last plan was carried out
   unsigned *ticket;  // [CTAs] arrivals of a unit split over CTAs, 0 between calls
-  unsigned *uticket; // [S * L * H] the same of a unit whose pages are scored, by the call
   unsigned *err;     // device error word
   int S, L, H, G, d, P, n_pages, tstride;
   int psh;           // log2(P)
@@ -76,12 +75,11 @@ struct SelectParams {
   int keep;           // pages of a list
   float2 *score;      // [unit of the call][sstride]: score, bound of its error
   int sstride;        // even
-  int held;           // scores of a unit that are held on chip, even
+  int held;           // keys of a unit that are held on chip, even
   int32_t *list;      // [unit][keep]
   int32_t *rows;      // [S]
   int32_t *tiles;     // [S + 1]
   int32_t *chosen;    // [unit][budget + window] or null: positions, then -1
-  int parts;          // CTAs that share a unit's pages, at most
 };
 cudaError_t launch_select(const SelectParams &p, int sms, cudaStream_t st, int *launches);
 

@@ -10,10 +10,8 @@
 // held in two floats, and what that leaves open in 64 bits, so that the choice is the
 // definition's.  Equal scores keep the lower page, a NaN ranks above every number.
 //
-// Few pages (latency): one launch, in which the last CTA of a unit to score chooses.
-// Many (the bounds' bytes): a launch that scores and one that chooses.  us, one and
-// two launches: 4 units of 513 pages 13.6 and 16.8; 112 units of 4,096 pages 83 and
-// 73, 672 of 235 to 469 pages 60 and 53.
+// Few units (latency): one launch, a cluster a unit, scores in shared memory.  Many (the
+// bounds' bytes): a launch that scores and one that chooses.
 #include "kvr_paged.cuh"
 
 #include <cuda_bf16.h>
@@ -31,7 +29,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kPartPages = 16 * kWarps;  // of a CTA, where a unit's pages are shared
 
 using kvr::dev::to_f;
 
@@ -71,7 +68,7 @@ __device__ __forceinline__ Unit unit_of(const SelectParams &p, long long at) {
 }
 
 // Items: 16 pages of a unit each, unit by unit.  A warp scores an item, the one `step`
-// further and so on, up to unit `units`.
+// further and so on, up to unit `units`; put(unit, page, (score, bound of its error)).
 __device__ __forceinline__ int groups_of(const View &c) { return (c.tstride + 15) / 16; }
 
 struct Items {
@@ -101,8 +98,8 @@ __device__ __forceinline__ bool next_item(const SelectParams &p, Items &it, Item
 
 // fp32: a page at a time; a lane sums D / 32 channels' products a head in a chain, then
 // five steps between lanes.
-template <int D>
-__device__ __forceinline__ void score_items(const SelectParams &p, Items it, const float *) {
+template <int D, typename F>
+__device__ __forceinline__ void score_items(const SelectParams &p, Items it, const float *, F put) {
   constexpr int kPer = D / 32;
   const View &c = p.c;
   const int lane = threadIdx.x & 31;
@@ -151,7 +148,7 @@ __device__ __forceinline__ void score_items(const SelectParams &p, Items it, con
       // Each of the D / 32 + 5 additions rounds by 2^-24 of a sum that is at most
       // sum |q| max |k|; products that underflow add 2^-149 each at most.
       if (lane == 0)
-        p.score[u.at * p.sstride + at] = make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f));
+        put(u.at, at, make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f)));
     }
   }
 }
@@ -178,9 +175,9 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
 // with the greatest keys and the negative part with the least.  A third product, |q|
 // with max(|least|, |greatest|), says how large the terms of the sums are.  The pages
 // of the next item are looked up while the bounds of this one come.
-template <int D>
-__device__ __forceinline__ void score_items(const SelectParams &p, Items it,
-                                            const __nv_bfloat16 *) {
+template <int D, typename F>
+__device__ __forceinline__ void score_items(const SelectParams &p, Items it, const __nv_bfloat16 *,
+                                            F put) {
   constexpr int kX = D / 64;  // 32-byte pieces of a lane in a row
   const View &c = p.c;
   const int lane = threadIdx.x & 31, row = lane >> 2, j = lane & 3;
@@ -269,7 +266,7 @@ __device__ __forceinline__ void score_items(const SelectParams &p, Items it,
         // Of each of the D / 16 products of a chain, 17 terms may be cut at 2^-23 of
         // the sum of magnitudes: 136 x 2^-23 of it for d = 128, the same again for
         // the other chain and for the sum of magnitudes itself.
-        p.score[unit * p.sstride + at] = make_float2(score, fmaf(err, 0x1p-14f, 1e-37f));
+        put(unit, at, make_float2(score, fmaf(err, 0x1p-14f, 1e-37f)));
       }
     }
   }
@@ -419,11 +416,15 @@ __device__ __forceinline__ float near_offset(const float *q, const T *b, int G, 
   return best;
 }
 
-constexpr int kHeld = 8192;  // scores of a unit that are held on chip, at most
+constexpr int kHeld = 8192;    // keys of a unit that are held on chip, at most
+constexpr int kOnChip = 2048;  // scores of a unit that lie on chip with them, at most
+// Words of n keys, padded (threads read runs of keys) to whole vectors.
+__host__ __device__ constexpr int keys_words(int n) { return (n + n / 32 + 3) / 4 * 4; }
 
-// The choice for one unit, whose scores are there.  The whole CTA.
-template <typename T, int D>
-__device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
+// The choice for one unit, whose scores lie at sc: on chip, or in memory.  The whole
+// CTA.
+template <typename T, int D, bool kOnChip>
+__device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, float2 *sc) {
   static_assert(kThreads == 256, "a thread a digit");
   __shared__ unsigned hist[256];
   __shared__ int s_digit, s_left, s_stay[kWarps], s_ties[kWarps], s_sure, s_few;
@@ -453,10 +454,9 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
     }
     return;
   }
-  float2 *sc = p.score + u.at * p.sstride;
   auto place = [](int i) { return i + (i >> 5); };  // (threads read runs of keys)
   constexpr int kBatch = 8;  // keys of a thread that are read together
-  auto held = [&](int i) { return i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
+  auto held = [&](int i) { return kOnChip || i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
   // f(i, key) for the thread's share of the keys.
   auto each = [&](auto f) {
     for (int i0 = tid; i0 < old; i0 += kBatch * kThreads) {
@@ -490,14 +490,15 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u) {
 #pragma unroll
       for (int r = 0; r < kBatch; ++r)
         if (i0 + 2 * r * kThreads < old)
-          x[r] = __ldcg(reinterpret_cast<const float4 *>(sc + i0 + 2 * r * kThreads));
+          x[r] = kOnChip ? *reinterpret_cast<const float4 *>(sc + i0 + 2 * r * kThreads)
+                         : __ldcg(reinterpret_cast<const float4 *>(sc + i0 + 2 * r * kThreads));
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
         const int i = i0 + 2 * r * kThreads;
         if (i >= old) break;
         // (the last one's neighbour is there, and not counted)
         const unsigned k0 = key32(x[r].x), k1 = i + 1 < old ? key32(x[r].z) : k0;
-        if (i < p.held) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
+        if (kOnChip || i < p.held) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
         err = nan_max(err, i + 1 < old ? nan_max(x[r].y, x[r].w) : x[r].y);
         least = min(least, min(k0, k1)), most = max(most, max(k0, k1));
       }
@@ -725,38 +726,45 @@ __device__ void sequences(const SelectParams &p) {
   if (tid == 0) p.tiles[c.S] = before;
 }
 
-// CTA 0: sequences(); the others: part i of a unit's pages each, p.parts of them.
+// A cluster a unit: its CTAs score its pages into the shared memory of the first, which
+// chooses.  One cluster more: sequences().
+constexpr int kUnitCtas = 8;
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 2) select_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
-  __shared__ int s_last;
-  if (blockIdx.x == 0) return sequences(p);
-  const unsigned job = blockIdx.x - 1;
-  const Unit u = unit_of(p, job / p.parts);
-  const int part = job % p.parts;
-  const int parts = max((u.old + kPartPages - 1) / kPartPages, 1);
-  if (part >= parts) return;
-  if (u.old > 0) {
-    // (an item a warp: the step leads out of the unit)
-    score_items<D>(p, Items((int)u.at, part * kWarps + (threadIdx.x >> 5), groups_of(p.c),
-                            (int)u.at + 1, groups_of(p.c)),
-                   (const T *)nullptr);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      // (the barrier and this fence order every thread's scores before the arrival)
-      __threadfence();
-      unsigned *ticket = p.c.uticket + u.at;
-      s_last = parts == 1 || atomicAdd(ticket, 1u) == (unsigned)parts - 1;
-      if (s_last && parts > 1) *ticket = 0;
-      __threadfence();
-    }
-    __syncthreads();
-    if (!s_last) return;
+  extern __shared__ __align__(16) unsigned s_dynamic[];
+  const unsigned unit = blockIdx.x / kUnitCtas, rank = blockIdx.x % kUnitCtas;
+  if (unit == gridDim.x / kUnitCtas - 1) {
+    if (rank == 0) sequences(p);
+    return;
   }
-  choose<T, D>(p, u);
+  // (the first CTA runs before anything is written to its memory)
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  const Unit u = unit_of(p, unit);
+  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  // behind the keys: pairs
+  float2 *sc = reinterpret_cast<float2 *>(s_dynamic + keys_words(p.held));
+  if (u.old > 0) {
+    uint32_t to;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(kvr::ptx::smem_u32(sc)), "r"(0));
+    const int groups = groups_of(p.c);
+    // (the step stays in the unit, and then leads out of it)
+    for (int i = rank * kWarps + (threadIdx.x >> 5); i < groups; i += kUnitCtas * kWarps)
+      score_items<D>(p, Items((int)unit, i, groups, (int)unit + 1, groups), (const T *)nullptr,
+                     [&](long long, int at, float2 x) {
+                       asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to + 8 * at),
+                                    "f"(x.x), "f"(x.y)
+                                    : "memory");
+                     });
+    asm volatile(
+        "barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
+            : "memory");
+  }
+  if (rank == 0) choose<T, D, true>(p, u, sc);
 }
 
-// The same in two launches.
+// The same in two launches, scores in memory.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 2) score_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
@@ -764,34 +772,37 @@ __global__ void __launch_bounds__(kThreads, 2) score_kernel(const __grid_constan
   const unsigned warp = blockIdx.x * kWarps + (threadIdx.x >> 5);
   score_items<D>(p, Items(warp / groups, warp % groups, gridDim.x * kWarps,
                           p.c.S * p.nl * p.c.H, groups),
-                 (const T *)nullptr);
+                 (const T *)nullptr,
+                 [&](long long unit, int at, float2 x) { p.score[unit * p.sstride + at] = x; });
 }
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 5) choose_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
   if (blockIdx.x == 0) return sequences(p);
-  choose<T, D>(p, unit_of(p, blockIdx.x - 1));
+  const Unit u = unit_of(p, blockIdx.x - 1);
+  choose<T, D, false>(p, u, p.score + u.at * p.sstride);
 }
 
 template <typename T, int D>
 cudaError_t launch(SelectParams p, int sms, cudaStream_t st, int *launches) {
   const long long units = (long long)p.c.S * p.nl * p.c.H;
-  p.parts = p.budget > 0 ? (p.c.tstride + kPartPages - 1) / kPartPages : 1;
-  const long long jobs = units * p.parts;
-  p.held = std::min(p.sstride, kHeld);  // (both even)
-  const size_t smem = (p.held + p.held / 32) * sizeof(unsigned);
   cudaError_t e;
-  if (p.budget == 0 || jobs <= 2 * sms) {
-    if (jobs >= 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-    e = kvr::launch_pdl(select_kernel<T, D>, dim3((unsigned)jobs + 1), dim3(kThreads), smem, st,
-                        p);
+  if (units * kUnitCtas <= 2 * sms && p.sstride <= kOnChip) {
+    p.held = p.sstride;
+    const size_t smem = keys_words(p.held) * 4 + (size_t)p.held * 8;
+    e = kvr::launch_pdl_cluster(select_kernel<T, D>, dim3((unsigned)(units + 1) * kUnitCtas),
+                                dim3(kThreads), kUnitCtas, smem, st, p);
   } else {
-    e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(jobs, 8ll * sms)),
-                        dim3(kThreads), 0, st, p);
-    if (e != cudaSuccess) return e;
-    *launches += 1;
-    e = kvr::launch_pdl(choose_kernel<T, D>, dim3((unsigned)units + 1), dim3(kThreads), smem, st,
-                        p);
+    if (p.budget > 0) {
+      const long long ctas = (units * ((p.c.tstride + 15) / 16) + kWarps - 1) / kWarps;
+      e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(ctas, 8ll * sms)),
+                          dim3(kThreads), 0, st, p);
+      if (e != cudaSuccess) return e;
+      *launches += 1;
+    }
+    p.held = std::min(p.sstride, kHeld);  // (both even)
+    e = kvr::launch_pdl(choose_kernel<T, D>, dim3((unsigned)units + 1), dim3(kThreads),
+                        keys_words(p.held) * 4, st, p);
   }
   if (e == cudaSuccess) *launches += 1;
   return e;
