@@ -549,6 +549,7 @@ kvr_status kvr_paged_create(const kvr_paged_desc *desc, void *dev_buf, size_t by
   v.io_bf16 = desc->kv_dtype == KVR_BF16;
   v.out_bf16 = desc->out_dtype == KVR_BF16;
   cudaError_t e = kvr::paged::prepare_attend(v, &c->device);
+  if (e == cudaSuccess) e = kvr::paged::prepare_select(v);
   // tickets and the error word lie side by side
   if (e == cudaSuccess)
     e = cudaMemsetAsync(b + l.ticket, 0, l.total - l.ticket, as_stream(stream));

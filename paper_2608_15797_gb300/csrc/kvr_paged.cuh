@@ -81,6 +81,7 @@ struct SelectParams {
   int32_t *tiles;     // [S + 1]
   int32_t *chosen;    // [unit][budget + window] or null: positions, then -1
 };
+cudaError_t prepare_select(const View &c);
 cudaError_t launch_select(const SelectParams &p, int sms, cudaStream_t st, int *launches);
 
 __host__ __device__ __forceinline__ long long pool_row(const View &c, int l, int page, int h) {

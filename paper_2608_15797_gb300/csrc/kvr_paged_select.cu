@@ -27,8 +27,9 @@ namespace kvr {
 namespace paged {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kBlock = 256;        // threads, where no other number is given
+constexpr int kBlockWarps = kBlock / 32;
+constexpr int kWide = 1024;        // of a CTA that chooses alone on its SM
 
 using kvr::dev::to_f;
 
@@ -312,7 +313,7 @@ __device__ __forceinline__ void digit_of(const unsigned *hist, int need, int lan
 // The need-th greatest of key(0 .. n - 1), by digits of 8 bits from bit `top` down
 // (above it all keys are alike); *left: how many equal to it belong to the first
 // `need`.
-template <typename K, typename F>
+template <int kThreads, typename K, typename F>
 __device__ K nth(int n, int need, int top, F key, unsigned *hist, int *s_digit, int *s_left,
                  int *left) {
   const int lane = threadIdx.x & 31;
@@ -320,7 +321,7 @@ __device__ K nth(int n, int need, int top, F key, unsigned *hist, int *s_digit, 
   bool first = true;
   for (int shift = top - 7; ; shift -= 8) {
     const int low = max(shift, 0), width = shift + 8 - low;
-    hist[threadIdx.x] = 0;
+    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads) {
       const K k = key(i);
@@ -423,9 +424,10 @@ __host__ __device__ constexpr int keys_words(int n) { return (n + n / 32 + 3) / 
 
 // The choice for one unit, whose scores lie at sc: on chip, or in memory.  The whole
 // CTA.
-template <typename T, int D, bool kOnChip>
+template <typename T, int D, bool kOnChip, int kThreads>
 __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, float2 *sc) {
-  static_assert(kThreads == 256, "a thread a digit");
+  constexpr int kWarps = kThreads / 32;
+  static_assert(kThreads >= 256, "a thread a digit");
   __shared__ unsigned hist[256];
   __shared__ int s_digit, s_left, s_stay[kWarps], s_ties[kWarps], s_sure, s_few;
   __shared__ float s_err[kWarps];
@@ -479,7 +481,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
   {
     float err = 0.f;
     unsigned least = ~0u, most = 0;
-    hist[tid] = 0;
+    if (tid < 256) hist[tid] = 0;
     {
       const T *q = static_cast<const T *>(p.q) + u.at * c.G * D;
       for (int i = tid; i < kHeads * D; i += kThreads)
@@ -553,7 +555,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
         t = value32(s_kth);
       } else {
         int unused;
-        t = value32(nth<unsigned>(old, B, 31, held, hist, &s_digit, &s_left, &unused));
+        t = value32(nth<kThreads, unsigned>(old, B, 31, held, hist, &s_digit, &s_left, &unused));
       }
       __syncthreads();
     }
@@ -634,7 +636,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
         if (i < old) keys[i] = key;
       }
       __syncthreads();
-      cut = nth<unsigned long long>(old, B, 63, [&](int i) { return keys[i]; }, hist, &s_digit,
+      cut = nth<kThreads, unsigned long long>(old, B, 63, [&](int i) { return keys[i]; }, hist, &s_digit,
                                     &s_left, &equal);
     }
   }
@@ -692,7 +694,9 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
 
 // What the attention reads of each sequence: rows of the pages that stay, and the
 // tiles of the sequences before it.
+template <int kThreads>
 __device__ void sequences(const SelectParams &p) {
+  constexpr int kWarps = kThreads / 32;
   __shared__ int s_warp[kWarps];
   const View &c = p.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -731,12 +735,12 @@ __device__ void sequences(const SelectParams &p) {
 constexpr int kUnitCtas = 8;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) select_kernel(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(kBlock, 2) select_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
   extern __shared__ __align__(16) unsigned s_dynamic[];
   const unsigned unit = blockIdx.x / kUnitCtas, rank = blockIdx.x % kUnitCtas;
   if (unit == gridDim.x / kUnitCtas - 1) {
-    if (rank == 0) sequences(p);
+    if (rank == 0) sequences<kBlock>(p);
     return;
   }
   // (the first CTA runs before anything is written to its memory)
@@ -750,7 +754,8 @@ __global__ void __launch_bounds__(kThreads, 2) select_kernel(const __grid_consta
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(kvr::ptx::smem_u32(sc)), "r"(0));
     const int groups = groups_of(p.c);
     // (the step stays in the unit, and then leads out of it)
-    for (int i = rank * kWarps + (threadIdx.x >> 5); i < groups; i += kUnitCtas * kWarps)
+    for (int i = rank * kBlockWarps + (threadIdx.x >> 5); i < groups;
+         i += kUnitCtas * kBlockWarps)
       score_items<D>(p, Items((int)unit, i, groups, (int)unit + 1, groups), (const T *)nullptr,
                      [&](long long, int at, float2 x) {
                        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to + 8 * at),
@@ -761,26 +766,27 @@ __global__ void __launch_bounds__(kThreads, 2) select_kernel(const __grid_consta
         "barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
             : "memory");
   }
-  if (rank == 0) choose<T, D, true>(p, u, sc);
+  if (rank == 0) choose<T, D, true, kBlock>(p, u, sc);
 }
 
 // The same in two launches, scores in memory.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) score_kernel(const __grid_constant__ SelectParams p) {
+__global__ void __launch_bounds__(kBlock, 2) score_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
   const int groups = groups_of(p.c);
-  const unsigned warp = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  score_items<D>(p, Items(warp / groups, warp % groups, gridDim.x * kWarps,
+  const unsigned warp = blockIdx.x * kBlockWarps + (threadIdx.x >> 5);
+  score_items<D>(p, Items(warp / groups, warp % groups, gridDim.x * kBlockWarps,
                           p.c.S * p.nl * p.c.H, groups),
                  (const T *)nullptr,
                  [&](long long unit, int at, float2 x) { p.score[unit * p.sstride + at] = x; });
 }
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 5) choose_kernel(const __grid_constant__ SelectParams p) {
+template <typename T, int D, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == kWide ? 1 : 5)
+    choose_kernel(const __grid_constant__ SelectParams p) {
   kvr::pdl_begin();
-  if (blockIdx.x == 0) return sequences(p);
+  if (blockIdx.x == 0) return sequences<kThreads>(p);
   const Unit u = unit_of(p, blockIdx.x - 1);
-  choose<T, D, false>(p, u, p.score + u.at * p.sstride);
+  choose<T, D, false, kThreads>(p, u, p.score + u.at * p.sstride);
 }
 
 template <typename T, int D>
@@ -791,24 +797,40 @@ cudaError_t launch(SelectParams p, int sms, cudaStream_t st, int *launches) {
     p.held = p.sstride;
     const size_t smem = keys_words(p.held) * 4 + (size_t)p.held * 8;
     e = kvr::launch_pdl_cluster(select_kernel<T, D>, dim3((unsigned)(units + 1) * kUnitCtas),
-                                dim3(kThreads), kUnitCtas, smem, st, p);
+                                dim3(kBlock), kUnitCtas, smem, st, p);
   } else {
     if (p.budget > 0) {
-      const long long ctas = (units * ((p.c.tstride + 15) / 16) + kWarps - 1) / kWarps;
+      const long long ctas = (units * ((p.c.tstride + 15) / 16) + kBlockWarps - 1) / kBlockWarps;
       e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(ctas, 8ll * sms)),
-                          dim3(kThreads), 0, st, p);
+                          dim3(kBlock), 0, st, p);
       if (e != cudaSuccess) return e;
       *launches += 1;
     }
     p.held = std::min(p.sstride, kHeld);  // (both even)
-    e = kvr::launch_pdl(choose_kernel<T, D>, dim3((unsigned)units + 1), dim3(kThreads),
-                        keys_words(p.held) * 4, st, p);
+    const dim3 grid((unsigned)units + 1);
+    const size_t smem = keys_words(p.held) * 4;
+    // (4,096 pages, a unit an SM: 20 us with 256 threads)
+    e = units < sms && p.c.tstride > kWide
+            ? kvr::launch_pdl(choose_kernel<T, D, kWide>, grid, dim3(kWide), smem, st, p)
+            : kvr::launch_pdl(choose_kernel<T, D, kBlock>, grid, dim3(kBlock), smem, st, p);
   }
   if (e == cudaSuccess) *launches += 1;
   return e;
 }
 
+// The wide form's lists and keys are more than a CTA gets unasked.
+template <typename T, int D>
+cudaError_t prepare() {
+  return cudaFuncSetAttribute(choose_kernel<T, D, kWide>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize, keys_words(kHeld) * 4);
+}
+
 }  // namespace
+
+cudaError_t prepare_select(const View &c) {
+  if (c.io_bf16) return c.d == 128 ? prepare<__nv_bfloat16, 128>() : prepare<__nv_bfloat16, 64>();
+  return c.d == 128 ? prepare<float, 128>() : prepare<float, 64>();
+}
 
 cudaError_t launch_select(const SelectParams &p, int sms, cudaStream_t st, int *launches) {
   if (p.c.io_bf16)
