@@ -386,9 +386,10 @@ __device__ __forceinline__ unsigned long long exact_key(const float *q, const T 
   return best;
 }
 
-// A page's score less t, from sums held as two floats: within 2^-35 of the sum of
-// magnitudes where the score is within 2^-12 of it from t (products by fma, the sums'
-// errors kept: 2^-40; then one rounding of the difference).
+// A page's score less t, from sums held as two floats.  Of the sum of magnitudes M:
+// the errors that sums leave, 2^-24 M each, are added up over 32 terms with as many
+// roundings, 2^-38 M; the difference from t, at most three bounds of a score's error
+// (2^-14 M in bf16, 2^-20 of what bounds M in fp32), rounds twice.
 __device__ __forceinline__ void add_exact(float &hi, float &lo, float x) {
   const float s = __fadd_rn(hi, x), b = __fsub_rn(s, hi);
   lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(x, b)));
@@ -458,6 +459,9 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
   }
   auto place = [](int i) { return i + (i >> 5); };  // (threads read runs of keys)
   constexpr int kBatch = 8;  // keys of a thread that are read together
+  // of a score's bound, what near_offset is within: 2^-35 and 2^-37 of what sums are
+  // bounded by
+  constexpr float kOff = sizeof(T) == 2 ? 0x1p-21f : 0x1p-17f;
   auto held = [&](int i) { return kOnChip || i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
   // f(i, key) for the thread's share of the keys.
   auto each = [&](auto f) {
@@ -589,7 +593,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
       }
       __syncthreads();
       bool in = false, open = false;
-      const float off = tid < near ? s_off[tid] : 0.f, e2 = 2.f * (err * 0x1p-21f + 1e-40f);
+      const float off = tid < near ? s_off[tid] : 0.f, e2 = 2.f * (err * kOff + 1e-40f);
       if (tid < near) {
         int maybe = 0, surely = 0;  // that go before it
         for (int k = 0; k < near; ++k) {
