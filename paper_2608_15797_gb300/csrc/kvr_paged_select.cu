@@ -805,7 +805,7 @@ cudaError_t launch(SelectParams p, int sms, cudaStream_t st, int *launches) {
   } else {
     if (p.budget > 0) {
       const long long ctas = (units * ((p.c.tstride + 15) / 16) + kBlockWarps - 1) / kBlockWarps;
-      e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(ctas, 8ll * sms)),
+      e = kvr::launch_pdl(score_kernel<T, D>, dim3((unsigned)std::min<long long>(ctas, 2ll * sms)),
                           dim3(kBlock), 0, st, p);
       if (e != cudaSuccess) return e;
       *launches += 1;
