@@ -9,10 +9,16 @@
 // copy instruction takes 512 bytes in a row from memory, whole lines, and puts each
 // vector where the lane that needs it reads without bank conflicts: with the
 // lanes fetching their own 64 bytes of eight rows instead, 16 sequences of 16,384
-// rows (1.5B geometry) took 1,348 us, now 1,096 (6.86 TB/s).  A unit that lies in one warp's span is written
-// out by it; the pieces (greatest logit, sum, weighted values) of one that does not
-// are joined in the CTA in order, and where it goes on in another CTA by the last of
-// its CTAs to arrive, in order again, so that results do not depend on who is last.
+// rows (1.5B geometry) took 1,348 us, now 1,076 (6.99 TB/s; bound by those bytes).
+//
+// A unit that lies in one warp's span is written out by it; the pieces (greatest
+// logit, sum, weighted values) of one that does not are joined in the CTA in order,
+// and where it goes on in another CTA by the last of its CTAs to arrive, in order
+// again, so that results do not depend on who is last.  A call of few units and tiles
+// takes a cluster a unit instead, whose CTAs' parts meet in shared memory: 28 calls of
+// a layer, one sequence of 4,099 rows (7B), in a graph 335 us with arrivals and 253 so.
+// What is left there is latency: lengths, pages and rows one after the other, tiles of
+// 0.4 us, and three joins.
 #include "kvr_paged.cuh"
 
 #include <cuda_bf16.h>
@@ -31,8 +37,10 @@ namespace {
 using namespace kvr::ptx;
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxCtas = kMostCtas;  // whose weights the last one holds for 8 heads
-constexpr int kLeast = 3;       // tiles of a warp, where there are as many
+constexpr int kMaxCtas = kMostCtas;  // whose logits the last one holds for 8 heads
+// Tiles of a warp, where there are as many: what its copies hold.  (28 calls of 257
+// tiles a unit with 2, 3, 4 and 6: 348, 335, 333 and 376 us.)
+constexpr int kLeast = 3;
 
 // 16 bytes to shared memory, zeros where `bytes` is 0 (nothing is read then).
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {

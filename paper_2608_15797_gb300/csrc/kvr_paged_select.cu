@@ -10,8 +10,12 @@
 // held in two floats, and what that leaves open in 64 bits, so that the choice is the
 // definition's.  Equal scores keep the lower page, a NaN ranks above every number.
 //
-// Few units (latency): one launch, a cluster a unit, scores in shared memory.  Many (the
-// bounds' bytes): a launch that scores and one that chooses.
+// Few units (latency): one launch, a cluster a unit, scores in shared memory (4 units of
+// 513 pages, choice and attention: 24 us a call with scores in memory and arrivals,
+// 16 so).  Many (the bounds' bytes): a launch that scores, 16 warps an SM with a page's
+// bounds as whole lines straight to registers (112 units of 4,096 pages 41 us, 5.7
+// TB/s; through rings of copies as in the attention 74, since a warp's 16 pages are a
+// long chain of steps), and one that chooses (15 us, of dependent steps).
 #include "kvr_paged.cuh"
 
 #include <cuda_bf16.h>
@@ -813,7 +817,7 @@ cudaError_t launch(SelectParams p, int sms, cudaStream_t st, int *launches) {
     p.held = std::min(p.sstride, kHeld);  // (both even)
     const dim3 grid((unsigned)units + 1);
     const size_t smem = keys_words(p.held) * 4;
-    // (4,096 pages, a unit an SM: 20 us with 256 threads)
+    // (112 units of 4,096 pages: 15 us, with 256 threads 20)
     e = units < sms && p.c.tstride > kWide
             ? kvr::launch_pdl(choose_kernel<T, D, kWide>, grid, dim3(kWide), smem, st, p)
             : kvr::launch_pdl(choose_kernel<T, D, kBlock>, grid, dim3(kBlock), smem, st, p);

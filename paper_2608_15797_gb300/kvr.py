@@ -1124,6 +1124,7 @@ class PagedCache:
                                    dtype, out_dtype, softmax_scale)
         self.S, self.L, self.H, self.G, self.d = (n_seq, n_layers, n_kv_heads,
                                                   group, head_dim)
+        self._hg = n_kv_heads * group
         self.n_pages, self.page_rows = n_pages, page_rows
         self.table_pages = self.desc.table_pages
         self.dtype, self.out_dtype = dtype, out_dtype
@@ -1220,28 +1221,41 @@ class PagedCache:
         return self._workspace("kvr_paged_attend_pages_workspace_bytes",
                                *(layers or self._all), budget, window)
 
-    def _outputs(self, q, out, layers, stream):
-        lb, le = layers
-        shape = (self.S, le - lb, self.H * self.G, self.d)
-        qp = self._tensor(q, shape, self._io, "q")
+    def _outputs(self, q, out, shape, stream):
+        """The output tensor: `out`, or a new one.  (A call a layer spends its time
+        on the host, so what is usual is asked without another call.)"""
+        at = self._device
+        if q.shape != shape or q.dtype is not self._io or \
+                not q.is_contiguous() or q.get_device() != at:
+            self._tensor(q, shape, self._io, "q")  # raises
         if out is None:
-            out = _empty(shape, self._out, q.device, stream)
-        return qp, out, self._tensor(out, shape, self._out, "out")
+            return _empty(shape, self._out, q.device, stream)
+        if out.shape != shape or out.dtype is not self._out or \
+                not out.is_contiguous() or out.get_device() != at:
+            self._tensor(out, shape, self._out, "out")  # raises
+        return out
+
+    def _given(self, workspace):
+        if workspace.get_device() != self._device or \
+                not workspace.is_contiguous():
+            _given_workspace(workspace, self._device)  # raises
+        return workspace
 
     def attend(self, q, out=None, layers=None, workspace=None, stream=None):
         """Attention of each sequence's newest token: q [S][nl][H*G][d] -> out,
         the same shape in out_dtype (kvr_paged_attend)."""
         lb, le = layers or self._all
         at = self._at(stream)
-        qp, out, op = self._outputs(q, out, (lb, le), stream)
-        if workspace is None:
-            workspace = _scratch(int(lib.kvr_paged_attend_workspace_bytes(
+        out = self._outputs(q, out, (self.S, le - lb, self._hg, self.d),
+                            stream)
+        workspace = self._given(workspace) if workspace is not None else \
+            _scratch(int(lib.kvr_paged_attend_workspace_bytes(
                 self.handle, lb, le)), q.device, stream)
-        else:
-            _given_workspace(workspace, self._device)
-        _check(lib.kvr_paged_attend(self.handle, lb, le, qp, op,
-                                    workspace.data_ptr(), workspace.nbytes,
-                                    at), "kvr_paged_attend")
+        st = lib.kvr_paged_attend(self.handle, lb, le, q.data_ptr(),
+                                  out.data_ptr(), workspace.data_ptr(),
+                                  workspace.nbytes, at)
+        if st:
+            _check(st, "kvr_paged_attend")
         return out
 
     def attend_pages(self, q, budget, window=1, out=None, pages=None,
@@ -1251,20 +1265,19 @@ class PagedCache:
         [S][nl][H][budget + window] for the choice."""
         lb, le = layers or self._all
         at = self._at(stream)
-        qp, out, op = self._outputs(q, out, (lb, le), stream)
-        pp = None if pages is None else self._tensor(
+        out = self._outputs(q, out, (self.S, le - lb, self._hg, self.d),
+                            stream)
+        to = None if pages is None else self._tensor(
             pages, (self.S, le - lb, self.H, budget + window), torch.int32,
             "pages")
-        if workspace is None:
-            workspace = _scratch(
-                int(lib.kvr_paged_attend_pages_workspace_bytes(
-                    self.handle, lb, le, budget, window)), q.device, stream)
-        else:
-            _given_workspace(workspace, self._device)
-        _check(lib.kvr_paged_attend_pages(
-            self.handle, lb, le, qp, budget, window, op, pp,
-            workspace.data_ptr(), workspace.nbytes, at),
-            "kvr_paged_attend_pages")
+        workspace = self._given(workspace) if workspace is not None else \
+            _scratch(int(lib.kvr_paged_attend_pages_workspace_bytes(
+                self.handle, lb, le, budget, window)), q.device, stream)
+        st = lib.kvr_paged_attend_pages(
+            self.handle, lb, le, q.data_ptr(), budget, window, out.data_ptr(),
+            to, workspace.data_ptr(), workspace.nbytes, at)
+        if st:
+            _check(st, "kvr_paged_attend_pages")
         return out
 
     def tables_view(self):

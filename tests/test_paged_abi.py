@@ -84,7 +84,7 @@ def cache(monkeypatch):
             return called
     c = kvr.PagedCache.__new__(kvr.PagedCache)
     c.S, c.L, c.H, c.G, c.d = 2, 1, 1, 2, 128
-    c.n_pages, c.page_rows, c.table_pages = 4, 16, 2
+    c._hg, c.n_pages, c.page_rows, c.table_pages = 2, 4, 16, 2
     c.dtype = c.out_dtype = "bf16"
     c._io = c._out = torch.bfloat16
     c._all, c._tables, c._pool = (0, 1), None, None
