@@ -482,11 +482,7 @@ Work work_of(const kvr_paged *c, int nl, int budget, int window) {
     return at;
   };
   if (window > 0) w.keep = (int)std::min<long long>((long long)budget + window, d.table_pages);
-  kvr::paged::AttendParams p{};
-  p.c = c->view;
-  p.nl = nl;
-  p.most = most_tiles(c, nl, w.keep);
-  w.parts = take((size_t)2 * kvr::paged::attend_ctas(p, c->device) *
+  w.parts = take((size_t)2 * kvr::paged::attend_ctas(c->view, c->device) *
                  kvr::paged::part_floats(d.head_dim) * sizeof(float));
   if (window > 0) {
     const size_t units = (size_t)d.n_seq * nl * d.n_kv_heads;

@@ -59,9 +59,9 @@ struct Device {
   int sms;
   int clusters;  // of units, that run at once
 };
-// CTAs of a launch, a matter of p.c, p.nl and p.most.
-constexpr int kMostCtas = 2560;
-int attend_ctas(const AttendParams &p, const Device &dev);
+// CTAs of a launch.
+constexpr int kMostCtas = 1024;
+int attend_ctas(const View &c, const Device &dev);
 cudaError_t prepare_attend(const View &c, Device *dev);
 cudaError_t launch_attend(const AttendParams &p, const Device &dev, cudaStream_t st);
 

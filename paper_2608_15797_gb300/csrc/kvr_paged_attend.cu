@@ -855,19 +855,18 @@ cudaError_t prepare(bool bf16_out, int *clusters) {
   return bf16_out ? prepare_as<T, D, __nv_bfloat16>(clusters) : prepare_as<T, D, float>(clusters);
 }
 
-// CTAs of a launch: as many as run at once, or several times as many, where the
-// largest call would still give every warp 24 tiles: SMs do not get the same share of
-// the memory's rate, and shorter spans even that out.
+// CTAs of a launch: as many as run at once.  (Two, four and eight times as many, so that
+// SMs with a smaller share of the memory's rate do less: 1,067, 1,074 and 1,074 us
+// against 1,070 for 16 sequences of 16,384 rows, and 274, 279 and 282 against 269 for
+// chosen pages of six.)
 template <typename T, int D>
-int ctas_of(const AttendParams &p, const Device &dev) {
+int ctas_of(const Device &dev) {
   using P = typename Choice<T, D>::P;
   // (of an SM's 228 KB a CTA takes 1 KB more than it asks for)
   constexpr int kResident =
       228 * 1024 / (int)(smem_bytes<T, D, P>() + 2 * P::kWarps * (sizeof(Piece) + 32) + 64 + 1024);
   static_assert(kResident >= 1, "shared memory");
-  const int at_once = std::min(dev.sms * kResident, kMaxCtas);
-  const long long waves = p.most / ((long long)at_once * P::kWarps * 24);
-  return at_once * (int)std::max(1ll, std::min<long long>(waves, std::min(8, kMaxCtas / at_once)));
+  return std::min(dev.sms * kResident, kMaxCtas);
 }
 
 // A cluster a unit: where all of them run at once and even the largest call gives a
@@ -885,7 +884,7 @@ cudaError_t launch_as(const AttendParams &p, const Device &dev, cudaStream_t st)
   constexpr size_t bytes = smem_bytes<T, D, P>();
   const dim3 block(P::kWarps * 32);
   if (!small_call(p, dev))
-    return kvr::launch_pdl(attend_kernel<T, D, P, O, 1>, dim3(ctas_of<T, D>(p, dev)), block, bytes,
+    return kvr::launch_pdl(attend_kernel<T, D, P, O, 1>, dim3(ctas_of<T, D>(dev)), block, bytes,
                            st, p);
   return kvr::launch_pdl_cluster(attend_kernel<T, D, P, O, kUnitCtas>,
                                  dim3(p.c.S * p.nl * p.c.H * kUnitCtas), block, kUnitCtas, bytes,
@@ -900,10 +899,10 @@ cudaError_t launch(const AttendParams &p, const Device &dev, cudaStream_t st) {
 
 }  // namespace
 
-int attend_ctas(const AttendParams &p, const Device &dev) {
-  if (p.c.io_bf16)
-    return p.c.d == 128 ? ctas_of<__nv_bfloat16, 128>(p, dev) : ctas_of<__nv_bfloat16, 64>(p, dev);
-  return p.c.d == 128 ? ctas_of<float, 128>(p, dev) : ctas_of<float, 64>(p, dev);
+int attend_ctas(const View &c, const Device &dev) {
+  if (c.io_bf16)
+    return c.d == 128 ? ctas_of<__nv_bfloat16, 128>(dev) : ctas_of<__nv_bfloat16, 64>(dev);
+  return c.d == 128 ? ctas_of<float, 128>(dev) : ctas_of<float, 64>(dev);
 }
 
 cudaError_t prepare_attend(const View &c, Device *dev) {
