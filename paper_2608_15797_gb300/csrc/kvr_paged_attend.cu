@@ -126,9 +126,9 @@ struct Fma : Shape<T, D> {
   using S = Shape<T, D>;
   static constexpr int kWarps = 4, kStages = 3;
   static constexpr int kRowsAtOnce = 32 / S::kVecs;
-  // of a warp: q fp32 [8][D], probabilities [16][8], the rescaling [8]
-  static constexpr int kOwn = (kHeads * D + kTile * kHeads + kHeads) * 4;
-  float *q, *p, *up;
+  static constexpr int kOwn = kHeads * D * 4;  // of a warp: q fp32 [8][D]
+  static constexpr int kUnroll = D == 128 ? 4 : 2;
+  float *q;
   float scale;
   float m[2], l[2];          // heads 2 j, 2 j + 1
   float o[kHeads][S::E];
@@ -146,8 +146,6 @@ struct Fma : Shape<T, D> {
 
   __device__ __forceinline__ void init(uint8_t *own, float scale_log2e) {
     q = reinterpret_cast<float *>(own);
-    p = q + kHeads * D;
-    up = p + kTile * kHeads;
     scale = scale_log2e;
   }
   __device__ __forceinline__ void start(const T *from, int G, int lane) {
@@ -162,13 +160,17 @@ struct Fma : Shape<T, D> {
 #pragma unroll
       for (int e = 0; e < S::E; ++e) o[g][e] = 0.f;
   }
-  // One tile; rows from `limit` on do not exist.
-  __device__ __forceinline__ void step(const uint4 *stage, int limit, int lane) {
+  // One tile; rows from `limit` on do not exist.  Probabilities [16][8] and the
+  // rescaling [8] take the place of K, once it has been read: two CTAs fit an SM at d =
+  // 64 so.
+  __device__ __forceinline__ void step(uint4 *stage, int limit, int lane) {
     const int j = lane & 3;
+    float *p = reinterpret_cast<float *>(stage), *up = p + kTile * kHeads;
+    static_assert(S::kPer * 512 >= (kTile * kHeads + kHeads) * 4, "room in K's place");
     float x[2][kHeads];
 #pragma unroll
     for (int g = 0; g < kHeads; ++g) x[0][g] = x[1][g] = 0.f;
-#pragma unroll 2
+#pragma unroll kUnroll
     for (int i = 0; i < S::kPer / 2; ++i) {
       float a[S::E], b[S::E];
       Elems<T>::get(stage[(2 * i) * 32 + lane], a);
@@ -195,7 +197,7 @@ struct Fma : Shape<T, D> {
         y += __shfl_xor_sync(0xffffffffu, y, 2);
         if ((g >> 1) == j) mine[r][g & 1] = (lane >> 2) + 8 * r < limit ? y : -INFINITY;
       }
-    __syncwarp();  // the last tile's probabilities have been read
+    __syncwarp();  // K has been read
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       float t = fmaxf(mine[0][g], mine[1][g]);
@@ -218,7 +220,7 @@ struct Fma : Shape<T, D> {
       for (int e = 0; e < S::E; ++e) o[g][e] *= a;
     }
     const uint4 *vs = stage + S::kPer * 32;
-#pragma unroll 4
+#pragma unroll 2 * kUnroll
     for (int i = 0; i < S::kPer; ++i) {
       float v[S::E];
       Elems<T>::get(vs[i * 32 + lane], v);
@@ -299,7 +301,7 @@ struct Mma : Shape<__nv_bfloat16, D> {
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[v][e][0] = o[v][e][1] = 0.f;
   }
-  __device__ __forceinline__ void step(const uint4 *stage, int limit, int lane) {
+  __device__ __forceinline__ void step(uint4 *stage, int limit, int lane) {
     float s[2][4], s2[2][4];  // two chains a row of the tile
 #pragma unroll
     for (int r = 0; r < 2; ++r)
@@ -534,7 +536,7 @@ __global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_con
       }
       issue();  // where tile k - 1 was, which the warp has read
       if (k < 0) continue;
-      work.step(reinterpret_cast<const uint4 *>(ring + (uint32_t)stage * S::kStage),
+      work.step(reinterpret_cast<uint4 *>(ring + (uint32_t)stage * S::kStage),
                 at.rows - at.tile * kTile, lane);
       stage = stage + 1 == kStages ? 0 : stage + 1;
       const bool last = t0 + k + 1 == t1;
