@@ -1178,7 +1178,9 @@ class PagedCache:
     def plan(self, lens, n_new=0, slots=None, stream=None):
         """The sequences' lengths become lens (int32 [S] on the device); returns
         the slots [S][n_new] of the tokens they grow by, None where n_new is 0
-        (kvr_paged_plan)."""
+        (kvr_paged_plan).  Where one grows by more than n_new tokens or the free
+        pages do not reach, nothing changes, every slot is -1, and
+        sync_status() raises."""
         at = self._at(stream)
         want = self._tensor(lens, (self.S,), torch.int32, "lens")
         if n_new < 0 or n_new > 1 << 24:

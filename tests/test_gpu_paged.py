@@ -685,3 +685,78 @@ def test_refusals():
     c.attend(q)
     assert c.launch_count() == n + 1
     c.sync_status()
+
+
+# ---- sizes that pass 32 bits, and long ones ---------------------------------
+
+def test_offsets_past_32_bits():
+    """Rows in pages whose place in the pool passes 2^32 bytes and 2^31
+    elements, keys and values alike."""
+    S, L, H, G, d, P, n_pages = 2, 2, 8, 2, 128, 64, 20000
+    c = kvr.PagedCache(S, L, H, G, d, n_pages, P, n_pages - 50)
+    first = n_pages - 60
+    c.plan(i32([first * P, 0]), first * P)
+    n = 300
+    slots = c.plan(i32([first * P, n]), n)
+    c.plan(i32([0, n]))
+    assert int(c.tables_view()[0][1, 0]) == first
+    assert 2 * ((n_pages * L - 60) * H * P * d) > 2**32
+    k, v = (rnd(i, (1, L, n, H, d), heavy=True) for i in (1, 2))
+    c.append(dev(k), dev(v), slots[1:])
+    q = rnd(3, (S, L, H * G, d))
+    pages = torch.empty((S, L, H, 3), dtype=torch.int32, device="cuda")
+    out = c.attend(dev(q)).float().cpu().numpy()
+    some = c.attend_pages(dev(q), 2, 1, pages=pages).float().cpu().numpy()
+    pages = pages.cpu().numpy()
+    assert (out[0] == 0).all() and (some[0] == 0).all()
+    for l in range(L):
+        for h in range(H):
+            g = slice(G * h, G * h + G)
+            kk, vv = k[0, l, :, h], v[0, l, :, h]
+            want = paged.choose(q[1, l, g], kk, P, 2, 1)
+            assert pages[1, l, h].tolist() == want
+            for got, rows in ((out, np.arange(n)),
+                              (some, paged.rows_of(want, n, P))):
+                ref, mag, top = paged.attend(q[1, l, g], kk[rows], vv[rows])
+                tol = 2.0**-8 * np.abs(ref) + mag * (
+                    2 * 2.0**-16 * top[:, None] + 2.0**-15) + 1e-30
+                assert (np.abs(got[1, l, g] - ref) <= tol).all()
+    c.sync_status()
+
+
+def test_a_very_long_sequence():
+    """Four million rows of one unit: all of them, and 65 of 262,145 pages.  A
+    warp of 608 sums 432 tiles one after the other, and as many parts are joined:
+    2^-13 covers what their sums round by."""
+    n, d, P = (1 << 22) + 5, 64, 16
+    pages = -(-n // P)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.randn((1, 1, n, 1, d), generator=g, device="cuda",
+                        dtype=torch.bfloat16) for _ in range(2))
+    c = kvr.PagedCache(1, 1, 1, 2, d, pages, P, pages, out_dtype="f32")
+    c.append(k, v, c.plan(i32([n]), n))
+    q = dev(rnd(6, (1, 1, 2, d)))
+    qd = q[0, 0].double()
+
+    def check(out, kk, vv):
+        x = qd @ kk.double().T / 8.0
+        p = torch.softmax(x, -1)
+        ref, mag = p @ vv.double(), p @ vv.double().abs()
+        top = (qd.abs() @ kk.double().abs().T).amax(-1, keepdim=True) / 8.0
+        tol = mag * (2 * 2.0**-16 * top + 2.0**-13 + 2.0**-15)
+        assert ((out[0, 0].double() - ref).abs() <= tol).all()
+
+    check(c.attend(q), k[0, 0, :, 0], v[0, 0, :, 0])
+    got = torch.empty((1, 1, 1, 65), dtype=torch.int32, device="cuda")
+    out = c.attend_pages(q, 64, 1, pages=got)
+    full = k[0, 0, :(n // P) * P, 0].view(-1, P, d)
+    lo, hi = full.amin(1).double(), full.amax(1).double()
+    score = (qd.clamp(min=0) @ hi.T + qd.clamp(max=0) @ lo.T).amax(0)
+    order = torch.sort(score, descending=True, stable=True).indices[:64]
+    want = torch.cat((order.sort().values,
+                      torch.tensor([pages - 1], device="cuda")))
+    assert torch.equal(got.flatten().long(), want)
+    rows = (want[:, None] * P + torch.arange(P, device="cuda")).flatten()
+    rows = rows[rows < n]
+    check(out, k[0, 0, rows, 0], v[0, 0, rows, 0])
+    c.sync_status()
