@@ -20,10 +20,10 @@ namespace {
 
 // ---- plan -------------------------------------------------------------------
 
-constexpr int kPlan = 1024;       // threads of a CTA of the plan, sequences of a span
+constexpr int kPlan = 512;        // threads of a CTA of the plan
 constexpr int kPlanFew = 256;     // the same for as many sequences or fewer
 constexpr int kCluster = 8;       // CTAs of the plan
-constexpr int kInPlan = 16384;    // slots that the plan's cluster writes itself
+constexpr int kInPlan = 2048;     // slots that the plan's cluster writes itself
 constexpr int kFill = 256, kFillTokens = 2048;  // of a CTA that writes slots alone
 
 __global__ void __launch_bounds__(256) init_kernel(const __grid_constant__ View c) {
@@ -129,13 +129,15 @@ __device__ __forceinline__ void cluster_sync() {
 }
 
 // One cluster.  S lengths are little work, and what they ask of the stack is a sum
-// over all of them, which every CTA forms for itself; pages that go back (an ended
-// sequence has hundreds), and the new tokens' slots with the pages they need, are
-// dealt out to all threads of the cluster.  Many slots are left to the launch that
-// follows.  Latency binds.  64 sequences that drop their drafts and take five tokens
-// more, two plans: 7.1 us; 256 prompts of up to 8,191 tokens given up and taken: 29 thousand pages
-// and two million slots, 641 us in one CTA, 59 with the slots in a launch of their
-// own, 15 with the cluster.
+// over all of them, which every CTA forms for itself, a thread the same number of
+// neighbours; pages that go back (an ended sequence has hundreds), and the new tokens'
+// slots with the pages they need, are dealt out to all threads of the cluster.  Many
+// slots are left to the launch that follows.  Latency binds.  us a pass of two plans:
+// 64 sequences that drop five tokens and take five 5.7 in a graph (512 threads a CTA
+// 6.9, 1,024 22); 64 x 64 slots 6.2 in the cluster and 5.8 in a launch of their own, 64
+// x 255 9.5 and 6.0; 256 prompts of up to 8,191 tokens given up and taken, 29 thousand
+// pages and two million slots, 641 in one CTA, 59 with slots in a launch of their own,
+// 15 with the cluster.
 template <int N>
 __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
                                                  const int32_t *want, int n_new, int32_t *slots) {
@@ -143,22 +145,21 @@ __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
   __shared__ Sums s_warp[N / 32];
   __shared__ int s_start[N], s_page[N];
   const int tid = threadIdx.x, rank = (int)cluster_rank();
-  const int spans = (c.S + N - 1) / N;
+  const int each = (c.S + N - 1) / N, first = tid * each;  // sequences of a thread
   const int had = c.free[0];
-  Change x{};
-  Sums all{}, at{};
-  // one span: its sums are kept
-  auto sums = [&](int k) {
-    x = change_of(c, want, k * N + tid, n_new);
-    at = scan<N>(Sums{x.take(), x.back(), (x.want + kTile - 1) / kTile}, s_warp, &all);
+  auto sums_of = [](const Change &x) {
+    return Sums{x.take(), x.back(), (x.want + kTile - 1) / kTile};
   };
-  Sums total{};
+  Change x{};
+  Sums mine{}, total{};
   bool bad = false;
-  for (int k = 0; k < spans; ++k) {
-    sums(k);
-    total = total + all;
+#pragma unroll 4
+  for (int j = 0; j < each; ++j) {
+    x = change_of(c, want, first + j, n_new);
+    mine = mine + sums_of(x);
     bad |= x.bad;
   }
+  const Sums at = scan<N>(mine, s_warp, &total);
   bad = __syncthreads_or(bad);
   cluster_sync();  // every CTA has read the state
   const long long top = (long long)had + total.back;
@@ -172,40 +173,51 @@ __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
       for (int i = rank * N + tid; i < many; i += kCluster * N) slots[i] = -1;
     return;
   }
-  Sums before{};
-  for (int k = 0; k < spans && total.back > 0; ++k) {
-    if (spans > 1) sums(k);
-    __syncthreads();
-    s_start[tid] = at.back;
-    s_page[tid] = x.need;
-    __syncthreads();
+  // Page `page` of sequence s goes back, the e-th of the call.
+  auto give = [&](int s, int page, long long e) {
+    int32_t *entry = c.table + (long long)s * c.tstride + page;
+    const long long to = top - 1 - e;
+    if (to >= 0 && to < c.n_pages) c.stack[to] = *entry;
+    *entry = -1;
+  };
+  if (each == 1) {
+    if (total.back > 0) {
+      s_start[tid] = at.back;
+      s_page[tid] = x.need;
+      __syncthreads();
 #pragma unroll 4
-    for (int e = rank * N + tid; e < all.back; e += kCluster * N) {
-      const int i = find<N>(s_start, e);
-      int32_t *entry = c.table + (long long)(k * N + i) * c.tstride + s_page[i] + (e - s_start[i]);
-      const long long to = top - 1 - (before.back + e);
-      if (to >= 0 && to < c.n_pages) c.stack[to] = *entry;
-      *entry = -1;
-    }
-    before.back += all.back;
-  }
-  if (spans > 1) cluster_sync();  // every CTA has read the lengths again
-  if (rank == 0) {
-    before = Sums{};
-    for (int k = 0; k < spans; ++k) {
-      if (spans > 1) sums(k);
-      const int s = k * N + tid;
-      if (s < c.S) {
-        const Sums mine = before + at;
-        c.len[s] = x.want;
-        c.from[s] = min(x.old, x.want);
-        c.first[s] = (int)(top - 1 - mine.take);
-        c.tiles[s] = mine.tiles;
-        if (s == c.S - 1) c.tiles[c.S] = total.tiles;
+      for (int e = rank * N + tid; e < total.back; e += kCluster * N) {
+        const int i = find<N>(s_start, e);
+        give(i, s_page[i] + e - s_start[i], e);
       }
-      before = before + all;
     }
-    if (tid == 0) c.free[0] = (int)(top - total.take), c.free[1] = 1;
+  } else {
+    Sums before = at;
+    for (int j = 0; j < each && total.back > 0; ++j) {
+      const Change y = change_of(c, want, first + j, n_new);
+      if (j % kCluster == rank)
+        for (int e = 0; e < y.back(); ++e) give(first + j, y.need + e, (long long)before.back + e);
+      before = before + sums_of(y);
+    }
+    cluster_sync();  // every CTA has read the lengths again
+  }
+  if (rank == 0) {
+    Sums before = at;
+#pragma unroll 4
+    for (int j = 0; j < each; ++j) {
+      const int s = first + j;
+      if (s >= c.S) break;
+      if (each > 1) x = change_of(c, want, s, n_new);
+      c.len[s] = x.want;
+      c.from[s] = min(x.old, x.want);
+      c.first[s] = (int)(top - 1 - before.take);
+      c.tiles[s] = before.tiles;
+      before = before + sums_of(x);
+    }
+    if (tid == 0) {
+      c.tiles[c.S] = total.tiles;
+      c.free[0] = (int)(top - total.take), c.free[1] = 1;
+    }
   }
   if (many == 0 || many > kInPlan) return;
   cluster_sync();  // pages are back, the state is written

@@ -198,7 +198,8 @@ def test_plans_at_random(page):
     assert sorted(b.p.stack) == list(range(40))
 
 
-@pytest.mark.parametrize("S", [1, 31, 33, 1023, 1024, 1025, 2500])
+@pytest.mark.parametrize("S", [1, 31, 33, 255, 256, 257, 511, 513, 1024, 2500,
+                               9000])
 def test_plans_of_many_sequences(S):
     rng = np.random.default_rng(S)
     b = Book(S, 1, 1, 1, 64, 3 * S + 1, 16, 6)
