@@ -622,8 +622,9 @@ kvr_status kvr_kv4_sync_status(kvr_kv4 *cache, void *stream);
  * waits, and a captured decode step (plan, append, attend) replays as sequences
  * grow, come and go.
  *
- * Tensors are dense, row-major and 16-byte aligned (KVR_EINVAL otherwise).  What
- * only the device can see goes to the error word (kvr_paged_sync_status).  Calls
+ * Tensors are dense and row-major; those of K, V, q and outputs, and workspaces,
+ * are 16-byte aligned, those of int32 4-byte (KVR_EINVAL otherwise).  What only the
+ * device can see goes to the error word (kvr_paged_sync_status).  Calls
  * on one handle must be ordered on one stream. */
 typedef struct {
   int n_seq;           /* S, places for sequences, 1..65535 */
@@ -673,8 +674,9 @@ kvr_status kvr_paged_plan(kvr_paged *cache, const int32_t *lens, int n_new,
  * [layer_begin, layer_end):
  *   k, v  dev [n][nl][n_new][H][d]
  *   slots dev [n][n_new] int32: a row of kvr_paged_plan's for each of the n
- * n need not be n_seq: any rows of a plan's slots, in any order, each once.  A row
- * ends at its first -1.  A page whose last row is written by the call gets its
+ * n need not be n_seq: any rows of a plan's slots, in any order, each once, or some
+ * columns of them, where a prompt comes in parts; the tokens of a sequence are
+ * appended in their order.  A row ends at its first -1.  A page whose last row is written by the call gets its
  * bounds, the least and the greatest of its page_rows keys in every channel (NaN
  * where one is NaN), which kvr_paged_attend_pages reads.  Slots that do not follow
  * one another as a plan's do, or lie outside the pool, are not written where that

@@ -411,6 +411,7 @@ kvr_status cuda_fail(const char *where, cudaError_t e) {
 }
 cudaStream_t as_stream(void *s) { return static_cast<cudaStream_t>(s); }
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool aligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 struct Layout {
   size_t K, V, bounds, table, len, from, first, tiles, stack, free, ticket, err, total;
@@ -585,6 +586,8 @@ kvr_status kvr_paged_plan(kvr_paged *c, const int32_t *lens, int n_new, int32_t 
   if (n_new < 0 || n_new > (1 << 24)) return fail(KVR_EINVAL, "%d new tokens", n_new);
   if ((n_new > 0) != (slots != nullptr))
     return fail(KVR_EINVAL, "slots go with new tokens: %d of them", n_new);
+  if (!aligned4(lens) || !aligned4(slots))
+    return fail(KVR_EINVAL, "lengths and slots must be 4-byte aligned");
   const View &w = c->view;
   const cudaStream_t cs = as_stream(stream);
   const long long many = (long long)w.S * n_new;
@@ -613,6 +616,7 @@ kvr_status kvr_paged_append(kvr_paged *c, int lb, int le, int n, int n_new,
   if (!slots || !k || !v) return fail(KVR_EINVAL, "null slots, k or v");
   if (!aligned16(k) || !aligned16(v))
     return fail(KVR_EINVAL, "k and v must be 16-byte aligned");
+  if (!aligned4(slots)) return fail(KVR_EINVAL, "slots must be 4-byte aligned");
   kvr::paged::AppendParams p{};
   p.c = c->view;
   p.lb = lb;
@@ -684,6 +688,7 @@ kvr_status kvr_paged_attend_pages(kvr_paged *c, int lb, int le, const void *q, i
   if (!q || !out || !workspace) return fail(KVR_EINVAL, "null q, out or workspace");
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace))
     return fail(KVR_EINVAL, "q, out and workspace must be 16-byte aligned");
+  if (!aligned4(pages)) return fail(KVR_EINVAL, "pages must be 4-byte aligned");
   const Work w = work_of(c, le - lb, budget, window);
   if (workspace_bytes < w.total)
     return fail(KVR_ENOMEM, "workspace of %zu bytes < required %zu", workspace_bytes, w.total);

@@ -276,6 +276,22 @@ def test_append_any_rows_of_a_plan():
     b.check_rows()
 
 
+def test_a_prompt_in_parts():
+    """Columns of a plan's slots, one part after the other."""
+    b = Book(2, 2, 2, 1, 64, 20, 32, 10)
+    slots = b.plan([150, 77], 150)
+    shape = (2, 2, 150, 2, 64)
+    k, v = rnd(1, shape, heavy=True), rnd(2, shape)
+    for a, e in ((0, 40), (40, 41), (41, 96), (96, 150)):
+        b.c.append(dev(k[:, :, a:e]), dev(v[:, :, a:e]),
+                   slots[:, a:e].contiguous())
+    for s, n in enumerate((150, 77)):
+        b.k[s], b.v[s] = (x[s, :, :n].transpose(0, 2, 1, 3) for x in (k, v))
+    b.check_rows()
+    b.check_pages(1, 1)
+    b.c.sync_status()
+
+
 def test_bounds_of_extreme_keys():
     """Infinities, NaN and the types' ends are in the bounds of their page."""
     for dtype in ("bf16", "f32"):
