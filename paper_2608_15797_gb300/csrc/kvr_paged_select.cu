@@ -101,16 +101,21 @@ __device__ __forceinline__ bool next_item(const SelectParams &p, Items &it, Item
   return false;
 }
 
-// fp32: a page at a time; a lane sums D / 32 channels' products a head in a chain, then
-// five steps between lanes.
+// fp32: four pages' bounds on their way at a time; a lane sums D / 32 channels' products a
+// head in a chain, then five steps between lanes, which are what it costs: 896 units of
+// 60 pages at d = 128 48 us (each head summed over all lanes for itself 61, a page at a
+// time 68).  A page that is none counts as one of zeros.
 template <int D, typename F>
 __device__ __forceinline__ void score_items(const SelectParams &p, Items it, const float *, F put) {
-  constexpr int kPer = D / 32;
+  constexpr int kPer = D / 32, kAhead = 4;
   const View &c = p.c;
   const int lane = threadIdx.x & 31;
   Item x;
   while (next_item(p, it, x)) {
     const Unit &u = x.u;
+    const int mine =
+        c.table[(long long)u.s * c.tstride + min(x.first + (lane & 15), u.old - 1)];
+    if ((unsigned)mine >= (unsigned)c.n_pages) atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
     float q[kHeads][kPer];
     float most = 0.f;  // the greatest sum of |q| of a head
     const float *qs = static_cast<const float *>(p.q) + u.at * c.G * D;
@@ -124,36 +129,61 @@ __device__ __forceinline__ void score_items(const SelectParams &p, Items it, con
       }
       most = nan_max(most, kvr::dev::warp_sum(sum));
     }
-    const int end = min(x.first + 16, u.old);
-#pragma unroll 2
-    for (int at = x.first; at < end; ++at) {
-      const float *b = bounds_of<float>(c, u.l, u.s, u.h, at);
-      float score = -INFINITY, big = 0.f;
-      if (b) {
-        float lo[kPer], hi[kPer];
+    const int many = min(16, u.old - x.first);
+#pragma unroll 1
+    for (int i0 = 0; i0 < many; i0 += kAhead) {
+      float lo[kAhead][kPer], hi[kAhead][kPer];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int page = __shfl_sync(0xffffffffu, mine, i0 + i);
+        const bool there = (unsigned)page < (unsigned)c.n_pages;
+        const float *b = reinterpret_cast<const float *>(c.bounds) +
+                         (((long long)u.l * c.n_pages + (there ? page : 0)) * c.H + u.h) * 2 * D +
+                         lane * kPer;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-          lo[e] = b[lane * kPer + e];
-          hi[e] = b[D + lane * kPer + e];
-          big = nan_max(big, nan_max(fabsf(lo[e]), fabsf(hi[e])));
+          lo[i][e] = there ? __ldg(b + e) : 0.f;
+          hi[i][e] = there ? __ldg(b + D + e) : 0.f;
         }
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (i0 + i >= many) break;
+        float score = -INFINITY, big = 0.f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+          big = nan_max(big, nan_max(fabsf(lo[i][e]), fabsf(hi[i][e])));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) big = nan_max(big, __shfl_xor_sync(0xffffffffu, big, o));
+        float y[kHeads];
 #pragma unroll
         for (int g = 0; g < kHeads; ++g) {
-          float y = 0.f;
+          y[g] = 0.f;
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) y = fmaf(q[g][e], q[g][e] > 0.f ? hi[e] : lo[e], y);
-          y = kvr::dev::warp_sum(y);
-          if (g < c.G) score = nan_max(score, y);
+          for (int e = 0; e < kPer; ++e)
+            y[g] = fmaf(q[g][e], q[g][e] > 0.f ? hi[i][e] : lo[i][e], y[g]);
         }
-      } else if (lane == 0) {
-        atomicOr(c.err, (unsigned)kvr::ERR_LENGTH);
+        // eight sums over 32 lanes: each step halves the sums that a lane holds
+#pragma unroll
+        for (int n = kHeads / 2, o = 16; n > 0; n >>= 1, o >>= 1) {
+          const bool upper = lane & o;
+#pragma unroll
+          for (int k = 0; k < n; ++k) {
+            const float keep = upper ? y[k + n] : y[k], give = upper ? y[k] : y[k + n];
+            y[k] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+          }
+        }
+        y[0] += __shfl_xor_sync(0xffffffffu, y[0], 2);
+        y[0] += __shfl_xor_sync(0xffffffffu, y[0], 1);
+        if ((lane >> 2) < c.G) score = y[0];  // the head that the lane is left with
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1)
+          score = nan_max(score, __shfl_xor_sync(0xffffffffu, score, o));
+        // Each of the D / 32 + 5 additions rounds by 2^-24 of a sum that is at most
+        // sum |q| max |k|; products that underflow add 2^-149 each at most.
+        if (lane == 0)
+          put(u.at, x.first + i0 + i, make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f)));
       }
-      // Each of the D / 32 + 5 additions rounds by 2^-24 of a sum that is at most
-      // sum |q| max |k|; products that underflow add 2^-149 each at most.
-      if (lane == 0)
-        put(u.at, at, make_float2(score, fmaf(most * big, 0x1p-20f, 1e-40f)));
     }
   }
 }
