@@ -635,7 +635,8 @@ typedef struct {
   int n_pages;         /* pages of the pool (>= 1), n_pages * page_rows < 2^31,
                           L * H * n_pages * page_rows < 2^35 */
   int page_rows;       /* 16, 32, 64 or 128 */
-  int table_pages;     /* pages of a sequence at most (>= 1), times page_rows < 2^31 */
+  int table_pages;     /* pages of a sequence at most (>= 1), times page_rows
+                          < 2^31 */
   kvr_dtype kv_dtype;  /* K, V and q element type */
   kvr_dtype out_dtype; /* attention output element type */
   float softmax_scale; /* 0 selects 1/sqrt(d) */
@@ -676,11 +677,12 @@ kvr_status kvr_paged_plan(kvr_paged *cache, const int32_t *lens, int n_new,
  *   slots dev [n][n_new] int32: a row of kvr_paged_plan's for each of the n
  * n need not be n_seq: any rows of a plan's slots, in any order, each once, or some
  * columns of them, where a prompt comes in parts; the tokens of a sequence are
- * appended in their order.  A row ends at its first -1.  A page whose last row is written by the call gets its
- * bounds, the least and the greatest of its page_rows keys in every channel (NaN
- * where one is NaN), which kvr_paged_attend_pages reads.  Slots that do not follow
- * one another as a plan's do, or lie outside the pool, are not written where that
- * shows, and set the error word (length); slots given twice leave either's row. */
+ * appended in their order.  A row ends at its first -1.  A page whose last row is
+ * written by the call gets its bounds, the least and the greatest of its page_rows
+ * keys in every channel (NaN where one is NaN), which kvr_paged_attend_pages reads.
+ * Slots that do not follow one another as a plan's do, or lie outside the pool, are
+ * not written where that shows, and set the error word (length); slots given twice
+ * leave either's row. */
 kvr_status kvr_paged_append(kvr_paged *cache, int layer_begin, int layer_end,
                             int n, int n_new, const int32_t *slots,
                             const void *k, const void *v, void *stream);

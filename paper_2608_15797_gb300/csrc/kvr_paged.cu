@@ -13,6 +13,7 @@
 
 #include "../../include/kvr.h"
 #include "kvr_internal.h"
+#include "kvr_ptx.cuh"
 
 namespace kvr {
 namespace paged {
@@ -119,15 +120,6 @@ __device__ __forceinline__ int place(const View &c, int s, int t, int from, int 
   return (page << c.psh) + (pos & (c.P - 1));
 }
 
-__device__ __forceinline__ unsigned cluster_rank() {
-  unsigned r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
 // One cluster.  S lengths are little work, and what they ask of the stack is a sum
 // over all of them, which every CTA forms for itself, a thread the same number of
 // neighbours; pages that go back (an ended sequence has hundreds), and the new tokens'
@@ -144,7 +136,7 @@ __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
   kvr::pdl_begin();
   __shared__ Sums s_warp[N / 32];
   __shared__ int s_start[N], s_page[N];
-  const int tid = threadIdx.x, rank = (int)cluster_rank();
+  const int tid = threadIdx.x, rank = (int)ptx::cluster_rank();
   const int each = (c.S + N - 1) / N, first = tid * each;  // sequences of a thread
   const int had = c.free[0];
   auto sums_of = [](const Change &x) {
@@ -161,7 +153,7 @@ __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
   }
   const Sums at = scan<N>(mine, s_warp, &total);
   bad = __syncthreads_or(bad);
-  cluster_sync();  // every CTA has read the state
+  ptx::cluster_sync();  // every CTA has read the state
   const long long top = (long long)had + total.back;
   const long long many = slots ? (long long)c.S * n_new : 0;
   if (bad || total.take > top || top > c.n_pages) {
@@ -199,7 +191,7 @@ __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
         for (int e = 0; e < y.back(); ++e) give(first + j, y.need + e, (long long)before.back + e);
       before = before + sums_of(y);
     }
-    cluster_sync();  // every CTA has read the lengths again
+    ptx::cluster_sync();  // every CTA has read the lengths again
   }
   if (rank == 0) {
     Sums before = at;
@@ -220,7 +212,7 @@ __global__ void __launch_bounds__(N) plan_kernel(const __grid_constant__ View c,
     }
   }
   if (many == 0 || many > kInPlan) return;
-  cluster_sync();  // pages are back, the state is written
+  ptx::cluster_sync();  // pages are back, the state is written
   for (int i = rank * N + tid; i < many; i += kCluster * N) {
     const int s = i / n_new;
     slots[i] = place(c, s, i - s * n_new, c.from[s], c.len[s], c.first[s]);
@@ -473,8 +465,8 @@ bool choice_ok(int budget, int window) {
 long long most_tiles(const kvr_paged *c, int nl, int keep) {
   const kvr_paged_desc &d = c->desc;
   const long long a_page = d.page_rows / kvr::paged::kTile, units = (long long)nl * d.n_kv_heads;
-  const long long pages = std::min<long long>(d.n_pages, (long long)d.n_seq *
-                                              (keep ? std::min(keep, d.table_pages) : d.table_pages));
+  const long long of_one = keep ? std::min(keep, d.table_pages) : d.table_pages;
+  const long long pages = std::min<long long>(d.n_pages, d.n_seq * of_one);
   return pages * a_page * units;
 }
 

@@ -47,7 +47,9 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes)
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
                : "memory");
 }
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_end() {
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
 template <int N>
 __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -75,34 +77,10 @@ __device__ __forceinline__ float2 ld2_cluster(uint32_t at) {
                : "memory");
   return x;
 }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile(
-      "barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
-          : "memory");
+__device__ __forceinline__ void get4(const uint4 &w, float (&x)[4]) {
+  x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y);
+  x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
 }
-
-template <typename T>
-struct Elems;
-template <>
-struct Elems<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void get(const uint4 &w, float (&x)[4]) {
-    x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y);
-    x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
-  }
-};
-template <>
-struct Elems<__nv_bfloat16> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void get(const uint4 &w, float (&x)[8]) {
-    const uint32_t a[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(a[i] << 16);
-      x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
-    }
-  }
-};
 
 __device__ __forceinline__ void put4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
 __device__ __forceinline__ void put4(__nv_bfloat16 *p, float4 x) {
@@ -116,14 +94,14 @@ struct Shape {
   static constexpr int kVecs = kRow / 16;
   static constexpr int kPer = kVecs / 2;           // vectors of a lane, K or V
   static constexpr int kStage = 2 * kTile * kRow;
-  static constexpr int E = Elems<T>::N;
 };
 
 // Plain arithmetic in fp32, for fp32 rows.  Logits: four lanes share a row, each a
 // quarter of its channels.  Values: a lane owns E channels.
-template <typename T, int D>
-struct Fma : Shape<T, D> {
-  using S = Shape<T, D>;
+template <int D>
+struct Fma : Shape<float, D> {
+  using S = Shape<float, D>;
+  static constexpr int E = 4;
   static constexpr int kWarps = 4, kStages = 3;
   static constexpr int kRowsAtOnce = 32 / S::kVecs;
   static constexpr int kOwn = kHeads * D * 4;  // of a warp: q fp32 [8][D]
@@ -131,7 +109,7 @@ struct Fma : Shape<T, D> {
   float *q;
   float scale;
   float m[2], l[2];          // heads 2 j, 2 j + 1
-  float o[kHeads][S::E];
+  float o[kHeads][E];
 
   // Where a row's vector lies in its half of the stage.
   static __device__ __forceinline__ int k_at(int row, int vec) {
@@ -148,17 +126,17 @@ struct Fma : Shape<T, D> {
     q = reinterpret_cast<float *>(own);
     scale = scale_log2e;
   }
-  __device__ __forceinline__ void start(const T *from, int G, int lane) {
+  __device__ __forceinline__ void start(const float *from, int G, int lane) {
     __syncwarp();
     for (int i = lane; i < kHeads * D; i += 32)
-      q[i] = i < G * D ? kvr::dev::to_f(from[i]) * scale : 0.f;
+      q[i] = i < G * D ? from[i] * scale : 0.f;
     __syncwarp();
     m[0] = m[1] = -INFINITY;
     l[0] = l[1] = 0.f;
 #pragma unroll
     for (int g = 0; g < kHeads; ++g)
 #pragma unroll
-      for (int e = 0; e < S::E; ++e) o[g][e] = 0.f;
+      for (int e = 0; e < E; ++e) o[g][e] = 0.f;
   }
   // One tile; rows from `limit` on do not exist.  Probabilities [16][8] and the
   // rescaling [8] take the place of K, once it has been read: two CTAs fit an SM at d =
@@ -172,14 +150,14 @@ struct Fma : Shape<T, D> {
     for (int g = 0; g < kHeads; ++g) x[0][g] = x[1][g] = 0.f;
 #pragma unroll kUnroll
     for (int i = 0; i < S::kPer / 2; ++i) {
-      float a[S::E], b[S::E];
-      Elems<T>::get(stage[(2 * i) * 32 + lane], a);
-      Elems<T>::get(stage[(2 * i + 1) * 32 + lane], b);
-      const float *qc = q + (j + 4 * i) * S::E;
+      float a[E], b[E];
+      get4(stage[(2 * i) * 32 + lane], a);
+      get4(stage[(2 * i + 1) * 32 + lane], b);
+      const float *qc = q + (j + 4 * i) * E;
 #pragma unroll
       for (int g = 0; g < kHeads; ++g)
 #pragma unroll
-        for (int e = 0; e < S::E; e += 4) {
+        for (int e = 0; e < E; e += 4) {
           const float4 w = *reinterpret_cast<const float4 *>(qc + g * D + e);
           x[0][g] = fmaf(a[e], w.x, x[0][g]), x[1][g] = fmaf(b[e], w.x, x[1][g]);
           x[0][g] = fmaf(a[e + 1], w.y, x[0][g]), x[1][g] = fmaf(b[e + 1], w.y, x[1][g]);
@@ -217,20 +195,20 @@ struct Fma : Shape<T, D> {
     for (int g = 0; g < kHeads; ++g) {
       const float a = up[g];
 #pragma unroll
-      for (int e = 0; e < S::E; ++e) o[g][e] *= a;
+      for (int e = 0; e < E; ++e) o[g][e] *= a;
     }
     const uint4 *vs = stage + S::kPer * 32;
 #pragma unroll 2 * kUnroll
     for (int i = 0; i < S::kPer; ++i) {
-      float v[S::E];
-      Elems<T>::get(vs[i * 32 + lane], v);
+      float v[E];
+      get4(vs[i * 32 + lane], v);
       const float4 *pr = reinterpret_cast<const float4 *>(p + v_row(lane, i) * kHeads);
       const float4 pa = pr[0], pb = pr[1];
       const float w[kHeads] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
 #pragma unroll
       for (int g = 0; g < kHeads; ++g)
 #pragma unroll
-        for (int e = 0; e < S::E; ++e) o[g][e] = fmaf(w[g], v[e], o[g][e]);
+        for (int e = 0; e < E; ++e) o[g][e] = fmaf(w[g], v[e], o[g][e]);
     }
   }
   // Sums over the lanes; then f(head, channel, four weighted sums, greatest logit,
@@ -246,13 +224,13 @@ struct Fma : Shape<T, D> {
       const float mg = __shfl_sync(0xffffffffu, m[g & 1], g >> 1);
       const float lg = __shfl_sync(0xffffffffu, l[g & 1], g >> 1);
 #pragma unroll
-      for (int e = 0; e < S::E; ++e)
+      for (int e = 0; e < E; ++e)
 #pragma unroll
         for (int s = S::kVecs; s < 32; s <<= 1) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], s);
       if (lane < S::kVecs)
 #pragma unroll
-        for (int e = 0; e < S::E; e += 4)
-          f(g, lane * S::E + e, make_float4(o[g][e], o[g][e + 1], o[g][e + 2], o[g][e + 3]), mg,
+        for (int e = 0; e < E; e += 4)
+          f(g, lane * E + e, make_float4(o[g][e], o[g][e + 1], o[g][e + 2], o[g][e + 3]), mg,
             lg);
     }
   }
@@ -284,7 +262,8 @@ struct Mma : Shape<__nv_bfloat16, D> {
     return (2 * (vec >> 2) + (row >> 3)) * 512 + k_slot(row & 7, vec & 3, vec >> 2) * 16;
   }
   static __device__ __forceinline__ int v_at(int row, int vec) {
-    return (4 * (vec >> 3) + 2 * (row >> 3) + (row & 1)) * 512 + v_slot((row & 7) >> 1, vec & 7) * 16;
+    return (4 * (vec >> 3) + 2 * (row >> 3) + (row & 1)) * 512 +
+           v_slot((row & 7) >> 1, vec & 7) * 16;
   }
 
   __device__ __forceinline__ void init(uint8_t *, float scale_log2e) { scale = scale_log2e; }
@@ -389,7 +368,8 @@ struct Piece {
 // kCluster > 1: a cluster a unit, whose parts are joined through the CTAs' shared
 // memory.
 template <typename T, int D, typename P, typename O, int kCluster>
-__global__ void __launch_bounds__(P::kWarps * 32) attend_kernel(const __grid_constant__ AttendParams p) {
+__global__ void __launch_bounds__(P::kWarps * 32)
+    attend_kernel(const __grid_constant__ AttendParams p) {
   kvr::pdl_begin();
   using S = Shape<T, D>;
   constexpr int kWarps = P::kWarps, kStages = P::kStages, kPart = part_floats(D);
@@ -816,7 +796,7 @@ constexpr size_t smem_bytes() {
 
 template <typename T, int D>
 struct Choice {
-  using P = Fma<T, D>;
+  using P = Fma<D>;
 };
 template <int D>
 struct Choice<__nv_bfloat16, D> {

@@ -245,7 +245,8 @@ __device__ __forceinline__ void score_items(const SelectParams &p, Items it, con
       }
     }
     more = look();
-    float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f}, size[4] = {0.f, 0.f, 0.f, 0.f};
+    float up[4] = {0.f, 0.f, 0.f, 0.f}, down[4] = {0.f, 0.f, 0.f, 0.f};
+    float size[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < kX; ++x) {
       Words q{};
@@ -267,7 +268,8 @@ __device__ __forceinline__ void score_items(const SelectParams &p, Items it, con
           mag[y] = w & 0x7FFF7FFFu;
 #pragma unroll
           for (int r = 0; r < 2; ++r)
-            big[r][y] = max2(lo[r][x].w[2 * i + y] & 0x7FFF7FFFu, hi[r][x].w[2 * i + y] & 0x7FFF7FFFu);
+            big[r][y] = max2(lo[r][x].w[2 * i + y] & 0x7FFF7FFFu,
+                             hi[r][x].w[2 * i + y] & 0x7FFF7FFFu);
         }
         kvr::ptx::mma_bf16(up, hi[0][x].w[2 * i], hi[1][x].w[2 * i], hi[0][x].w[2 * i + 1],
                            hi[1][x].w[2 * i + 1], pos[0], pos[1]);
@@ -496,7 +498,9 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
   // of a score's bound, what near_offset is within: 2^-35 and 2^-37 of what sums are
   // bounded by
   constexpr float kOff = sizeof(T) == 2 ? 0x1p-21f : 0x1p-17f;
-  auto held = [&](int i) { return kOnChip || i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x); };
+  auto held = [&](int i) {
+    return kOnChip || i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x);
+  };
   // f(i, key) for the thread's share of the keys.
   auto each = [&](auto f) {
     for (int i0 = tid; i0 < old; i0 += kBatch * kThreads) {
@@ -674,8 +678,8 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
         if (i < old) keys[i] = key;
       }
       __syncthreads();
-      cut = nth<kThreads, unsigned long long>(old, B, 63, [&](int i) { return keys[i]; }, hist, &s_digit,
-                                    &s_left, &equal);
+      cut = nth<kThreads, unsigned long long>(old, B, 63, [&](int i) { return keys[i]; }, hist,
+                                              &s_digit, &s_left, &equal);
     }
   }
   // The pages that stay, in order: a thread goes through a run of them, once to count
@@ -800,9 +804,7 @@ __global__ void __launch_bounds__(kBlock, 2) select_kernel(const __grid_constant
                                     "f"(x.x), "f"(x.y)
                                     : "memory");
                      });
-    asm volatile(
-        "barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
-            : "memory");
+    kvr::ptx::cluster_sync();
   }
   if (rank == 0) choose<T, D, true, kBlock>(p, u, sc);
 }

@@ -188,6 +188,18 @@ __device__ __forceinline__ void cp_async_arrive_noinc(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar)
                : "memory");
 }
+// Thread-block clusters: a CTA's number in its own, and a barrier of all threads after
+// which what they wrote before it is seen.
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
+          : "memory");
+}
 // Hardware base-2 exponential (ex2.approx, relative error about 2^-22;
 // ex2(-inf) = +0; results below 2^-126 flush to zero).
 __device__ __forceinline__ float ex2(float x) {

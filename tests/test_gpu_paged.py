@@ -502,6 +502,27 @@ def test_attend_pages(dtype, d, G, page, budget, window):
     b.c.sync_status()
 
 
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 16), ("bf16", 64, 32),
+                                          ("f32", 128, 16), ("f32", 64, 16)])
+def test_attend_pages_of_many_units(dtype, d, page):
+    """Scores and choice in launches of their own: all layers of a batch."""
+    lens = [page * 40 + 1, 0, page * 33, page * 9 + 5, page * 40, page * 12]
+    b = Book(6, 4, 2, 3, d, 136, page, 41, dtype, "f32")
+    b.grow(lens)
+    for budget, window in ((1, 1), (7, 3), (30, 1), (0, 2)):
+        b.check_pages(budget, window)
+    b.c.sync_status()
+
+
+def test_many_pages_of_fp32():
+    b = Book(1, 1, 1, 2, 64, 2200, 16, 2200, "f32")
+    k = rnd(3, (1, 1, 16 * 2190, 1, 64), "f32")
+    k[0, 0, 16 * 2000:] = k[0, 0, :16 * 190]
+    b.grow([16 * 2190], k=k)
+    for budget in (1, 60, 900):
+        b.check_pages(budget, 2)
+
+
 def test_equal_scores_keep_the_lower_page():
     """Every page alike, and pages alike in groups."""
     for dtype in ("bf16", "f32"):
