@@ -57,7 +57,7 @@ __host__ __device__ constexpr int part_floats(int d) { return kHeads * d + 2 * k
 // the handle is made (limits of shared memory are raised then too).
 struct Device {
   int sms;
-  int clusters;  // of units, that run at once
+  int clusters[2];  // of 16 and of 8 CTAs, that run at once
 };
 // CTAs of a launch.
 constexpr int kMostCtas = 1024;

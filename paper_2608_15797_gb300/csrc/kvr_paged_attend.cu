@@ -803,38 +803,49 @@ struct Choice<__nv_bfloat16, D> {
   using P = Mma<D>;
 };
 
-// CTAs of a unit's cluster, where the call has few tiles.
-constexpr int kUnitCtas = 16;
+// CTAs of a unit's cluster, where the call has few tiles: the first that fits.
+constexpr int kUnitCtas[] = {16, 8};
 
-template <typename T, int D, typename O>
-cudaError_t prepare_as(int *clusters) {
+// How many clusters of N CTAs run at once (SMs lie differently in clusters' reach from
+// device to device).
+template <typename T, int D, typename O, int N>
+cudaError_t prepare_unit(int *clusters) {
   using P = typename Choice<T, D>::P;
   constexpr size_t bytes = smem_bytes<T, D, P>();
-  static_assert(bytes + 2 * P::kWarps * (sizeof(Piece) + 32) + 64 <= 227 * 1024, "shared memory");
-  constexpr auto kSize = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  constexpr auto unit = attend_kernel<T, D, P, O, kUnitCtas>;
-  cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, 1>, kSize, (int)bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(unit, kSize, (int)bytes);
+  constexpr auto unit = attend_kernel<T, D, P, O, N>;
+  cudaError_t e =
+      cudaFuncSetAttribute(unit, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(unit, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
-  // (how SMs lie in clusters' reach differs from device to device)
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kUnitCtas);
+  cfg.gridDim = dim3(N);
   cfg.blockDim = dim3(P::kWarps * 32);
   cfg.dynamicSmemBytes = bytes;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kUnitCtas;
+  attr[0].val.clusterDim.x = N;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaOccupancyMaxActiveClusters(clusters, unit, &cfg);
 }
 
+template <typename T, int D, typename O>
+cudaError_t prepare_as(Device *dev) {
+  using P = typename Choice<T, D>::P;
+  constexpr size_t bytes = smem_bytes<T, D, P>();
+  static_assert(bytes + 2 * P::kWarps * (sizeof(Piece) + 32) + 64 <= 227 * 1024, "shared memory");
+  cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, P, O, 1>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) e = prepare_unit<T, D, O, kUnitCtas[0]>(&dev->clusters[0]);
+  if (e == cudaSuccess) e = prepare_unit<T, D, O, kUnitCtas[1]>(&dev->clusters[1]);
+  return e;
+}
+
 template <typename T, int D>
-cudaError_t prepare(bool bf16_out, int *clusters) {
-  return bf16_out ? prepare_as<T, D, __nv_bfloat16>(clusters) : prepare_as<T, D, float>(clusters);
+cudaError_t prepare(bool bf16_out, Device *dev) {
+  return bf16_out ? prepare_as<T, D, __nv_bfloat16>(dev) : prepare_as<T, D, float>(dev);
 }
 
 // CTAs of a launch: as many as run at once.  (Two, four and eight times as many, so that
@@ -851,26 +862,30 @@ int ctas_of(const Device &dev) {
   return std::min(dev.sms * kResident, kMaxCtas);
 }
 
-// A cluster a unit: where all of them run at once and even the largest call gives a
-// warp no more than 8 tiles.  Parts then meet in shared memory and not across the
-// L2's halves.  us a call in a graph, one sequence of 4,099 rows (7B, 4 units): 9.1 and
-// 12.0.
-bool small_call(const AttendParams &p, const Device &dev) {
+// A cluster of n CTAs a unit: where all of them run at once and even the largest call
+// gives a warp no more than 8 tiles.  Parts then meet in shared memory and not across
+// the L2's halves.  us a call in a graph, 4 units (7B, a layer of one sequence) of 32,
+// 128, 512 and 1,500 tiles: 5.2, 6.5, 11.3 and 26.0, by spans 9.5, 10.3, 16.0 and 21.3;
+// 16 units of 32 and 128, in clusters of 8, 6.0 and 9.6, by spans 10.6 and 12.9.
+bool fits(const AttendParams &p, int clusters, int n) {
   const long long units = (long long)p.c.S * p.nl * p.c.H;
-  return units <= dev.clusters && p.most <= units * kUnitCtas * 4 * 8;
+  return units <= clusters && p.most <= units * n * 4 * 8;
+}
+
+template <typename T, int D, typename O, int N>
+cudaError_t launch_units(const AttendParams &p, cudaStream_t st) {
+  using P = typename Choice<T, D>::P;
+  return kvr::launch_pdl_cluster(attend_kernel<T, D, P, O, N>, dim3(p.c.S * p.nl * p.c.H * N),
+                                 dim3(P::kWarps * 32), N, smem_bytes<T, D, P>(), st, p);
 }
 
 template <typename T, int D, typename O>
 cudaError_t launch_as(const AttendParams &p, const Device &dev, cudaStream_t st) {
   using P = typename Choice<T, D>::P;
-  constexpr size_t bytes = smem_bytes<T, D, P>();
-  const dim3 block(P::kWarps * 32);
-  if (!small_call(p, dev))
-    return kvr::launch_pdl(attend_kernel<T, D, P, O, 1>, dim3(ctas_of<T, D>(dev)), block, bytes,
-                           st, p);
-  return kvr::launch_pdl_cluster(attend_kernel<T, D, P, O, kUnitCtas>,
-                                 dim3(p.c.S * p.nl * p.c.H * kUnitCtas), block, kUnitCtas, bytes,
-                                 st, p);
+  if (fits(p, dev.clusters[0], kUnitCtas[0])) return launch_units<T, D, O, kUnitCtas[0]>(p, st);
+  if (fits(p, dev.clusters[1], kUnitCtas[1])) return launch_units<T, D, O, kUnitCtas[1]>(p, st);
+  return kvr::launch_pdl(attend_kernel<T, D, P, O, 1>, dim3(ctas_of<T, D>(dev)),
+                         dim3(P::kWarps * 32), smem_bytes<T, D, P>(), st, p);
 }
 
 template <typename T, int D>
@@ -895,10 +910,10 @@ cudaError_t prepare_attend(const View &c, Device *dev) {
   if (e != cudaSuccess) return e;
   const bool out = c.out_bf16 != 0;
   if (c.io_bf16)
-    return c.d == 128 ? prepare<__nv_bfloat16, 128>(out, &dev->clusters)
-                      : prepare<__nv_bfloat16, 64>(out, &dev->clusters);
-  return c.d == 128 ? prepare<float, 128>(out, &dev->clusters)
-                    : prepare<float, 64>(out, &dev->clusters);
+    return c.d == 128 ? prepare<__nv_bfloat16, 128>(out, dev)
+                      : prepare<__nv_bfloat16, 64>(out, dev);
+  return c.d == 128 ? prepare<float, 128>(out, dev)
+                    : prepare<float, 64>(out, dev);
 }
 
 cudaError_t launch_attend(const AttendParams &p, const Device &dev, cudaStream_t st) {

@@ -833,7 +833,9 @@ template <typename T, int D>
 cudaError_t launch(SelectParams p, int sms, cudaStream_t st, int *launches) {
   const long long units = (long long)p.c.S * p.nl * p.c.H;
   cudaError_t e;
-  if (units * kUnitCtas <= 2 * sms && p.sstride <= kOnChip) {
+  // (choice and attention in a graph, us a call: 4 units of 512 pages 14.1, in two launches
+  // 15.5; 16 units 22.3 and 23.9; 36 units 25.9 and 25.1)
+  if (units * kUnitCtas <= sms && p.sstride <= kOnChip) {
     p.held = p.sstride;
     const size_t smem = keys_words(p.held) * 4 + (size_t)p.held * 8;
     e = kvr::launch_pdl_cluster(select_kernel<T, D>, dim3((unsigned)(units + 1) * kUnitCtas),

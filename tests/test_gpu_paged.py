@@ -360,11 +360,12 @@ def test_attend_few_units(dtype, d, G, lens):
     b.c.sync_status()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_one_long_unit(dtype):
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64),
+                                     ("f32", 128), ("f32", 64)])
+def test_one_long_unit(dtype, d):
     """Shared by many CTAs: lengths around the ends of their spans."""
     n = 40000
-    b = Book(1, 1, 1, 3, 64, n // 16, 16, n // 16, dtype, "f32")
+    b = Book(1, 1, 1, 3, d, n // 16, 16, n // 16, dtype, "f32")
     b.grow([n])
     for m in (n, n - 1, 3 * 16 * 4 * 100 + 1, 3 * 16 * 4 * 100, 12289):
         b.plan([m])
