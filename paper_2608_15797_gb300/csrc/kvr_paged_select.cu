@@ -348,13 +348,14 @@ __device__ __forceinline__ void digit_of(const unsigned *hist, int need, int lan
 
 // The need-th greatest of key(0 .. n - 1), by digits of 8 bits from bit `top` down
 // (above it all keys are alike); *left: how many equal to it belong to the first
-// `need`.
+// `need`.  The whole CTA; hist, *s_digit and *s_left may hold what threads still read.
 template <int kThreads, typename K, typename F>
 __device__ K nth(int n, int need, int top, F key, unsigned *hist, int *s_digit, int *s_left,
                  int *left) {
   const int lane = threadIdx.x & 31;
   K prefix = 0, mask = 0;
   bool first = true;
+  __syncthreads();
   for (int shift = top - 7; ; shift -= 8) {
     const int low = max(shift, 0), width = shift + 8 - low;
     if (threadIdx.x < 256) hist[threadIdx.x] = 0;
