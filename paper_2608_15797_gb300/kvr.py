@@ -1330,7 +1330,7 @@ class PagedCache:
         return int(n.value)
 
     def sync_status(self, stream=None):
-        _check(lib.kvr_paged_sync_status(self.handle, _stream(stream)),
+        _check(lib.kvr_paged_sync_status(self.handle, self._at(stream)),
                "kvr_paged_sync_status")
 
 
