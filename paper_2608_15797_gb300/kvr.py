@@ -881,11 +881,27 @@ def _scratch(nbytes, device, stream):
     return _empty(max(nbytes, 16), torch.uint8, device, stream)
 
 
+def _stream_of(cache, stream):
+    """A call's stream; a ValueError where kernels would run on another device
+    than the cache's."""
+    if _raw_device is not None:
+        now = _raw_device()
+        if now != cache._device:
+            raise ValueError(f"the cache lies on cuda:{cache._device}, the "
+                             f"current device is cuda:{now}")
+        if stream is None and _raw_stream is not None:
+            return _raw_stream(now)
+    return _stream(stream)
+
+
 class Kv4Cache:
     """A full-context cache held in 4 bits (kvr_kv4_*; the format stands in
     include/kvr.h): owner of the handle and of the torch buffer it lives in.
     What a call allocates, outputs that it was not given among them, belongs to
-    the call's stream, as tensors do that are made under torch.cuda.stream."""
+    the call's stream, as tensors do that are made under torch.cuda.stream.
+    Calls run on the current device, which has to be the cache's."""
+
+    _at = _stream_of
 
     def __init__(self, n_seq, n_layers, n_kv_heads, group, head_dim, capacity,
                  dtype="bf16", out_dtype="bf16", softmax_scale=0.0,
@@ -913,7 +929,7 @@ class Kv4Cache:
         self._device = _on_device(buf, "buf")
         h = _P()
         _check(lib.kvr_kv4_create(ctypes.byref(self.desc), _ptr(buf),
-                                  self.nbytes, _stream(stream),
+                                  self.nbytes, self._at(stream),
                                   ctypes.byref(h)), "kvr_kv4_create")
         self.handle = h
 
@@ -948,7 +964,7 @@ class Kv4Cache:
         shape = (self.L, self.H, k.shape[2], self.d)
         _check(lib.kvr_kv4_load(self.handle, seq, self._rows(k, shape, "k"),
                                 self._rows(v, shape, "v"), shape[2],
-                                _stream(stream)), "kvr_kv4_load")
+                                self._at(stream)), "kvr_kv4_load")
 
     def append(self, k, v, counts=None, layers=None, stream=None):
         """Append tokens: k, v [S][nl][n][H][d]; counts: how many of them each
@@ -960,7 +976,7 @@ class Kv4Cache:
             self.handle, lb, le, shape[2],
             None if counts is None else counts.ctypes.data,
             self._rows(k, shape, "k"), self._rows(v, shape, "v"),
-            _stream(stream)), "kvr_kv4_append")
+            self._at(stream)), "kvr_kv4_append")
 
     def truncate(self, lens):
         """Each sequence keeps its first lens[s] rows (kvr_kv4_truncate)."""
@@ -984,7 +1000,7 @@ class Kv4Cache:
                 for _ in range(2))
         _check(lib.kvr_kv4_read(self.handle, lb, le, n,
                                 None if counts is None else counts.ctypes.data,
-                                k.data_ptr(), v.data_ptr(), _stream(stream)),
+                                k.data_ptr(), v.data_ptr(), self._at(stream)),
                "kvr_kv4_read")
         return k, v
 
@@ -1020,7 +1036,7 @@ class Kv4Cache:
             self.handle, lb, le, shape[2],
             None if counts is None else counts.ctypes.data, qp,
             out.data_ptr(), 1 if scores else 0, workspace.data_ptr(),
-            workspace.nbytes, _stream(stream)), "kvr_kv4_attend")
+            workspace.nbytes, self._at(stream)), "kvr_kv4_attend")
         return out
 
     def evict_into(self, cache: Cache, budget, window, stream=None):
@@ -1029,7 +1045,7 @@ class Kv4Cache:
             raise ValueError(f"the destination must be a Cache, not {cache!r}")
         _on_device(cache.buf, "the destination", self._device)
         _check(lib.kvr_kv4_evict(self.handle, cache.handle, budget, window,
-                                 _stream(stream)), "kvr_kv4_evict")
+                                 self._at(stream)), "kvr_kv4_evict")
 
     def scores_view(self):
         """The scores as a device tensor viewing the buffer,
@@ -1051,7 +1067,7 @@ class Kv4Cache:
         return int(n.value)
 
     def sync_status(self, stream=None):
-        _check(lib.kvr_kv4_sync_status(self.handle, _stream(stream)),
+        _check(lib.kvr_kv4_sync_status(self.handle, self._at(stream)),
                "kvr_kv4_sync_status")
 
 
@@ -1153,17 +1169,7 @@ class PagedCache:
             lib.kvr_paged_destroy(h)
             self.handle = None
 
-    def _at(self, stream):
-        """The call's stream; a ValueError where kernels would run on another
-        device than the cache's."""
-        if _raw_device is not None:
-            now = _raw_device()
-            if now != self._device:
-                raise ValueError(f"the cache lies on cuda:{self._device}, the "
-                                 f"current device is cuda:{now}")
-            if stream is None and _raw_stream is not None:
-                return _raw_stream(now)
-        return _stream(stream)
+    _at = _stream_of
 
     def _tensor(self, x, shape, dtype, what):
         """The address of x, a dense tensor of this shape on the cache's
