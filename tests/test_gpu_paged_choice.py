@@ -7,7 +7,9 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_paged import Book, rnd
+from oracle import paged
+from paper_2608_15797_gb300 import kvr
+from tests.test_gpu_paged import Book, dev, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +85,31 @@ def test_pages_that_stretch_the_range(dtype, many, pages, far):
     for budget in (1, 2, 100, pages // 2, pages - 2, pages - 1):
         b.check_pages(budget, 1, q)
     b.c.sync_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("many,pages", [(False, 38), (True, 38), (False, 2100)])
+def test_a_nan_ranks_above_infinity(dtype, many, pages):
+    """One page of each kind beside ordinary ones, each budget's choice for itself:
+    NaN, then +inf, then numbers, and -inf behind all of them."""
+    k = rnd(31, (pages * P, D), dtype).reshape(pages, P, D)
+    k[20, 3, 7] = np.nan
+    k[9, 1, 8] = np.inf
+    k[11, :, 9] = -np.inf       # both bounds
+    b = book(pages, many, dtype)
+    fill(b, k.reshape(-1, D), pages)
+    c = b.c
+    q = np.abs(b.queries()) + 1
+    for budget in (1, 2, 3, pages - 1):
+        got = torch.full((c.S, c.L, 1, budget + 1), -7, dtype=torch.int32,
+                         device="cuda")
+        c.attend_pages(dev(q, dtype), budget, 1, pages=got)
+        want = paged.choose(q[0, 0], b.k[0][0, 0], P, budget, 1)
+        first = got[0, 0, 0].tolist()
+        assert first == want
+        assert 20 in first and (budget == 1) == (9 not in first)
+        assert 11 not in first
+        for s in range(1, c.S):
+            assert got[s, :, 0, 0].eq(0).all() and got[s, :, 0, 1:].eq(-1).all()
+    with pytest.raises(kvr.KvrError, match="non-finite"):
+        c.sync_status()
