@@ -461,13 +461,13 @@ bool choice_ok(int budget, int window) {
 }
 
 // Tiles of an attention over nl layers at most: of a pool that is full, or of `keep`
-// pages of every unit.
-long long most_tiles(const kvr_paged *c, int nl, int keep) {
+// pages of every unit; and of one unit.
+void set_most(const kvr_paged *c, int keep, kvr::paged::AttendParams *p) {
   const kvr_paged_desc &d = c->desc;
-  const long long a_page = d.page_rows / kvr::paged::kTile, units = (long long)nl * d.n_kv_heads;
+  const long long a_page = d.page_rows / kvr::paged::kTile, units = (long long)p->nl * d.n_kv_heads;
   const long long of_one = keep ? std::min(keep, d.table_pages) : d.table_pages;
-  const long long pages = std::min<long long>(d.n_pages, d.n_seq * of_one);
-  return pages * a_page * units;
+  p->most = std::min<long long>(d.n_pages, d.n_seq * of_one) * a_page * units;
+  p->longest = std::min<long long>(d.n_pages, of_one) * a_page;
 }
 
 size_t score_stride(const kvr_paged *c) { return ((size_t)c->desc.table_pages + 1) / 2 * 2; }
@@ -662,7 +662,7 @@ kvr_status kvr_paged_attend(kvr_paged *c, int lb, int le, const void *q, void *o
   p.nl = le - lb;
   p.q = q;
   p.out = out;
-  p.most = most_tiles(c, p.nl, 0);
+  set_most(c, 0, &p);
   p.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.parts);
   const cudaError_t e = kvr::paged::launch_attend(p, c->device, as_stream(stream));
   if (e != cudaSuccess) return cuda_fail("kvr_paged_attend", e);
@@ -712,7 +712,7 @@ kvr_status kvr_paged_attend_pages(kvr_paged *c, int lb, int le, const void *q, i
   p.nl = le - lb;
   p.q = q;
   p.out = out;
-  p.most = most_tiles(c, p.nl, w.keep);
+  set_most(c, w.keep, &p);
   p.parts = reinterpret_cast<float *>(ws + w.parts);
   e = kvr::paged::launch_attend(p, c->device, as_stream(stream));
   if (e != cudaSuccess) return cuda_fail("kvr_paged_attend_pages", e);

@@ -50,6 +50,7 @@ struct AttendParams {
   void *out;
   float *parts;    // [2 * CTAs][part_floats(d)]
   long long most;  // tiles that the call can have, whatever the lengths
+  long long longest;  // and one unit of it
 };
 __host__ __device__ constexpr int part_floats(int d) { return kHeads * d + 2 * kHeads; }
 

@@ -863,13 +863,19 @@ int ctas_of(const Device &dev) {
 }
 
 // A cluster of n CTAs a unit: where all of them run at once and even the largest call
-// gives a warp no more than 8 tiles.  Parts then meet in shared memory and not across
-// the L2's halves.  us a call in a graph, 4 units (7B, a layer of one sequence) of 32,
-// 128, 512 and 1,500 tiles: 5.2, 6.5, 11.3 and 26.0, by spans 9.5, 10.3, 16.0 and 21.3;
-// 16 units of 32 and 128, in clusters of 8, 6.0 and 9.6, by spans 10.6 and 12.9.
+// gives a warp no more than 8 tiles on average, and none more than 16.  Parts then meet
+// in shared memory and not across the L2's halves.  us a call in a graph, 4 units (7B, a
+// layer of one sequence) of 32, 128, 512 and 1,500 tiles: 5.2, 6.5, 11.3 and 26.0, by
+// spans 9.5, 10.3, 16.0 and 21.3; 16 units of 32 and 128, in clusters of 8, 6.0 and 9.6,
+// by spans 10.6 and 12.9.  Lengths are the device's, and one sequence may hold nearly
+// all of the pool, which is then one cluster's work: 18 units that share 288, 576, 1,152
+// and 4,608 tiles, alike 5.3, 5.6, 6.8 and 13.6 (by spans 10.8, 10.5, 10.7 and 11.8),
+// all in one unit 11.8, 19.6, 35.0 and 127 (11.5, 12.7, 18.5 and 33.2).  The bound of
+// 16 lies where a wrong guess costs about as much either way; tables no longer than the
+// sequences get keep batches that are alike in clusters.
 bool fits(const AttendParams &p, int clusters, int n) {
-  const long long units = (long long)p.c.S * p.nl * p.c.H;
-  return units <= clusters && p.most <= units * n * 4 * 8;
+  const long long units = (long long)p.c.S * p.nl * p.c.H, warps = n * 4;
+  return units <= clusters && p.most <= units * warps * 8 && p.longest <= warps * 16;
 }
 
 template <typename T, int D, typename O, int N>
