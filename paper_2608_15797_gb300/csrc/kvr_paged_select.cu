@@ -460,9 +460,9 @@ constexpr int kOnChip = 2048;  // scores of a unit that lie on chip with them, a
 // Words of n keys, padded (threads read runs of keys) to whole vectors.
 __host__ __device__ constexpr int keys_words(int n) { return (n + n / 32 + 3) / 4 * 4; }
 
-// The choice for one unit, whose scores lie at sc: on chip, or in memory.  The whole
-// CTA.
-template <typename T, int D, bool kOnChip, int kThreads>
+// The choice for one unit, whose scores lie at sc: on chip (kLocal), or in memory.  The
+// whole CTA.
+template <typename T, int D, bool kLocal, int kThreads>
 __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, float2 *sc) {
   constexpr int kWarps = kThreads / 32;
   static_assert(kThreads >= 256, "a thread a digit");
@@ -500,7 +500,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
   // bounded by
   constexpr float kOff = sizeof(T) == 2 ? 0x1p-21f : 0x1p-17f;
   auto held = [&](int i) {
-    return kOnChip || i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x);
+    return kLocal || i < p.held ? s_held[place(i)] : key32(__ldcg(sc + i).x);
   };
   // f(i, key) for the thread's share of the keys.
   auto each = [&](auto f) {
@@ -535,7 +535,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
 #pragma unroll
       for (int r = 0; r < kBatch; ++r)
         if (i0 + 2 * r * kThreads < old)
-          x[r] = kOnChip ? *reinterpret_cast<const float4 *>(sc + i0 + 2 * r * kThreads)
+          x[r] = kLocal ? *reinterpret_cast<const float4 *>(sc + i0 + 2 * r * kThreads)
                          : __ldcg(reinterpret_cast<const float4 *>(sc + i0 + 2 * r * kThreads));
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
@@ -543,7 +543,7 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
         if (i >= old) break;
         // (the last one's neighbour is there, and not counted)
         const unsigned k0 = key32(x[r].x), k1 = i + 1 < old ? key32(x[r].z) : k0;
-        if (kOnChip || i < p.held) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
+        if (kLocal || i < p.held) s_held[place(i)] = k0, s_held[place(i + 1)] = k1;
         err = nan_max(err, i + 1 < old ? nan_max(x[r].y, x[r].w) : x[r].y);
         least = min(least, min(k0, k1)), most = max(most, max(k0, k1));
       }
