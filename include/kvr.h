@@ -677,9 +677,10 @@ kvr_status kvr_paged_plan(kvr_paged *cache, const int32_t *lens, int n_new,
  *   slots dev [n][n_new] int32: a row of kvr_paged_plan's for each of the n
  * n need not be n_seq: any rows of a plan's slots, in any order, each once, or some
  * columns of them, where a prompt comes in parts; the tokens of a sequence are
- * appended in their order.  A row ends at its first -1.  A page whose last row is
- * written by the call gets its bounds, the least and the greatest of its page_rows
- * keys in every channel (NaN where one is NaN), which kvr_paged_attend_pages reads.
+ * appended in their order.  A row ends at its first -1, which only others follow.  A
+ * page whose last row is written by the call gets its bounds, the least and the
+ * greatest of its page_rows keys in every channel (NaN where one is NaN), which
+ * kvr_paged_attend_pages reads.
  * Slots that do not follow one another as a plan's do, or lie outside the pool, are
  * not written where that shows, and set the error word (length); slots given twice
  * leave either's row. */
@@ -692,8 +693,11 @@ kvr_status kvr_paged_append(kvr_paged *cache, int layer_begin, int layer_end,
  *   q, out dev [S][nl][H*G][d] (out_dtype for out)
  * A sequence without rows gets zeros.  Softmax statistics and sums are fp32;
  * values are summed before they are normalised, so |v| times the rows has to stay
- * below 2^127.  A normaliser that is not finite sets the error word.  Results do
- * not depend on which pages hold the rows, and equal calls give equal bits.
+ * below 2^127 (an infinite value can give NaN, and sets no error word).  Caches of bf16
+ * work on tensor cores, whatever the outputs' type: a logit is within 2^-16 of its
+ * terms' magnitudes summed, and a probability is two bf16 numbers, 2^-16 of it at most
+ * from the exponential.  A normaliser that is not finite sets the error word.  Results
+ * do not depend on which pages hold the rows, and equal calls give equal bits.
  * workspace: device, 16-byte aligned, caller-owned, at least
  * kvr_paged_attend_workspace_bytes(...) bytes (KVR_ENOMEM otherwise); nothing in
  * it is kept between calls. */
@@ -712,7 +716,10 @@ kvr_status kvr_paged_attend(kvr_paged *cache, int layer_begin, int layer_end,
  * sequence of no more than budget + window pages is read whole.
  *   pages  dev [S][nl][H][budget + window] int32 or NULL: the chosen pages as
  *          positions in the table, ascending, then -1
- * The workspace depends on budget and window too. */
+ * The workspace depends on budget and window too; eight bytes of it are for each page
+ * of each unit's table (S * nl * H * table_pages).  Tables tens of times as long as the
+ * sequences also cost the scores time.  Many pages whose scores are as good as equal
+ * where the budget ends (repeated content) are told apart in 64 bits, which is slow. */
 size_t kvr_paged_attend_pages_workspace_bytes(const kvr_paged *cache,
                                               int layer_begin, int layer_end,
                                               int budget, int window);

@@ -663,6 +663,9 @@ __device__ __forceinline__ void choose(const SelectParams &p, const Unit &u, flo
       low = all ? ~0u : low > 0 ? low : 1u;
       __syncthreads();
     } else {
+      // Many: 64 bits for each of them, and digit by digit.  (4 units of 513 pages, of
+      // which 30 and 70% are alike: 182 and 345 us a call, else 16; 112 of 4,097 pages 1.2
+      // and 2.6 ms, else 88 us.)
       settle = true;
       for (int i0 = warp * 32; i0 < old; i0 += kThreads) {
         const int i = i0 + lane;
