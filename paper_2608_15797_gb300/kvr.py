@@ -1116,7 +1116,9 @@ class PagedCache:
     def make_desc(n_seq, n_layers, n_kv_heads, group, head_dim, n_pages,
                   page_rows=64, table_pages=None, dtype="bf16",
                   out_dtype="bf16", softmax_scale=0.0):
-        """table_pages: pages a sequence may hold, by default the whole pool."""
+        """table_pages: pages a sequence may hold, by default the whole pool.
+        Workspaces of attend_pages grow with it, and a call of few sequences is
+        faster where it is no more than they need."""
         return kvr_paged_desc(
             n_seq, n_layers, n_kv_heads, group, head_dim, n_pages, page_rows,
             n_pages if table_pages is None else table_pages, DTYPES[dtype],
